@@ -365,6 +365,161 @@ FLAREPP_API flarepp_status flarepp_route_device_status(const flarepp_shape* shap
  */
 FLAREPP_API void flarepp_test_wait_fault(int kernel, int64_t ring_item, uint64_t wait_ns);
 
+/* ------------------------------------------------------------------------------------------
+ * The layers around the mixer in a FLARE++ model (the backbone of Tab. config_shared): pointwise
+ * linear layers with the MLP's activation and the block's residual in their epilogue, token
+ * embeddings, and the AdamW step.
+ *
+ * The conventions of the top of this file hold: dense row-major device buffers, 16-byte
+ * aligned, owned by the caller; arguments are checked before anything is enqueued; work is
+ * enqueued on `stream` and the call returns. `status` of these calls is NULL or a device int32
+ * that the kernels set (and never clear) when something went wrong that only they can see:
+ * FLAREPP_ERR_TIMEOUT for a bounded wait that gave up (the outputs are then invalid),
+ * FLAREPP_ERR_INVALID_ARGUMENT for an embedding id beyond the table.
+ * ------------------------------------------------------------------------------------------ */
+typedef enum {
+    FLAREPP_ACT_NONE = 0,
+    FLAREPP_ACT_RELU = 1,
+    FLAREPP_ACT_GELU = 2, /* z Phi(z), Phi the normal distribution function */
+    FLAREPP_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} flarepp_activation;
+
+typedef struct {
+    int64_t rows; /* tokens: 0 (a no-op) to 2^31 - 1 */
+    int64_t in;   /* input features, 1 to 2^20 */
+    int64_t out;  /* output features, 1 to 2^20 */
+    int32_t dtype; /* FLAREPP_BF16 (FLAREPP_F32: FLAREPP_ERR_UNSUPPORTED, as for the mixer) */
+    int32_t act;   /* flarepp_activation */
+} flarepp_linear_shape;
+
+/*
+ * The pointwise linear layer Z = X W^T + b, Y = act(Z) + R, bf16 operands, float32 sums, each
+ * output rounded once.
+ *   X [rows, in]; W [out, in] (out x in, as in the mixer); b [out] or NULL; R [rows, out] or
+ *   NULL; Y [rows, out].
+ *   Z: NULL, or [rows, out]: the sums with the bias, rounded to bf16, which flarepp_linear_bwd
+ *     takes (Y itself is computed from the unrounded ones). Needed for training when act is not
+ *     FLAREPP_ACT_NONE.
+ *   Any widths: `in` or `out` that are not multiples of 8 cost a copy of the operands they pad.
+ *   workspace: at least flarepp_linear_workspace_bytes(shape) bytes, 256-byte aligned.
+ *   Y, Z and the workspace must not overlap each other or an input.
+ * Errors: FLAREPP_ERR_INVALID_ARGUMENT, FLAREPP_ERR_UNSUPPORTED, FLAREPP_ERR_WORKSPACE,
+ * FLAREPP_ERR_CUDA, as for flarepp_route_fwd.
+ */
+FLAREPP_API size_t flarepp_linear_workspace_bytes(const flarepp_linear_shape* shape);
+FLAREPP_API flarepp_status flarepp_linear_fwd(const flarepp_linear_shape* shape, const void* X,
+                                              const void* W, const void* b, const void* R,
+                                              void* Y, void* Z, void* workspace,
+                                              size_t workspace_bytes, int32_t* status,
+                                              void* stream);
+
+/*
+ * The gradients of flarepp_linear_fwd for the output gradient dY [rows, out]:
+ *   dZ = dY o act'(Z), dX = dZ W [rows, in], dW = dZ^T X [out, in], db = sum over rows of dZ
+ * [out], all bf16, written (not accumulated); the gradient of R is dY itself. dX and dW are
+ * products of dZ rounded to bf16; db adds the unrounded values. The sums over rows run in a
+ * fixed order: two calls on the same inputs give the same bits.
+ *   Z: what flarepp_linear_fwd kept; may be NULL for FLAREPP_ACT_NONE (it is then not read).
+ *   dX, dW, db: each may be NULL, and its work is then left out (X is only read for dW, W only
+ *     for dX; either may be NULL when it is not read).
+ *   workspace: at least flarepp_linear_bwd_workspace_bytes(shape) bytes, 256-byte aligned.
+ *   The outputs and the workspace must not overlap each other or an input.
+ * rows = 0 writes zeros to dW and db. Errors as for flarepp_linear_fwd.
+ */
+FLAREPP_API size_t flarepp_linear_bwd_workspace_bytes(const flarepp_linear_shape* shape);
+FLAREPP_API flarepp_status flarepp_linear_bwd(const flarepp_linear_shape* shape, const void* X,
+                                              const void* W, const void* Z, const void* dY,
+                                              void* dX, void* dW, void* db, void* workspace,
+                                              size_t workspace_bytes, int32_t* status,
+                                              void* stream);
+
+typedef struct {
+    int64_t T; /* tokens, 0 to 2^31 - 1 */
+    int64_t V; /* rows of the table, 1 to 2^31 - 2 */
+    int64_t C; /* channels, 1 to 2^20 */
+    int32_t dtype;    /* flarepp_dtype of the table, of its gradient, of Y and of dY */
+    int32_t id_bytes; /* 4: int32 ids, 8: int64 ids */
+} flarepp_embedding_shape;
+
+/*
+ * Y[t] = scale * table[ids[t]] (one float32 product per value, rounded once). A negative id
+ * marks an empty position: its row of Y is 0, and it adds nothing to the gradient. So does an
+ * id of V or more, which is an error that `status` reports (FLAREPP_ERR_INVALID_ARGUMENT).
+ *   ids [T]; table [V, C]; Y [T, C], disjoint from both.
+ */
+FLAREPP_API flarepp_status flarepp_embedding_fwd(const flarepp_embedding_shape* shape,
+                                                 const void* ids, const void* table, float scale,
+                                                 void* Y, int32_t* status, void* stream);
+
+/*
+ * The table's gradient for dY [T, C]: dtable[v] = scale * sum over the t with ids[t] = v of
+ * dY[t], [V, C], written in full (rows that no id names are 0). The positions are sorted by id
+ * and the sums run in float32 in a fixed order: two calls on the same inputs give the same
+ * bits, whatever the ids.
+ *   workspace: at least flarepp_embedding_bwd_workspace_bytes(shape) bytes, 256-byte aligned,
+ *   disjoint from the inputs and dtable. T = 0 writes zeros.
+ */
+FLAREPP_API size_t flarepp_embedding_bwd_workspace_bytes(const flarepp_embedding_shape* shape);
+FLAREPP_API flarepp_status flarepp_embedding_bwd(const flarepp_embedding_shape* shape,
+                                                 const void* ids, const void* dY, float scale,
+                                                 void* dtable, void* workspace,
+                                                 size_t workspace_bytes, int32_t* status,
+                                                 void* stream);
+
+/*
+ * One tensor of an AdamW step: n values. param and grad: float32 or bf16 each. master: NULL, or
+ * the float32 weights that a bf16 param is a rounded copy of. m, v: the moments; with 32-bit
+ * states float32 [n] (m_scale, v_scale NULL); with 8-bit states one byte per value and one
+ * float32 scale per block of 256 values (the last block may be shorter), [ceil(n / 256)].
+ * Every pointer 16-byte aligned; no two buffers that a step writes may overlap.
+ */
+typedef struct {
+    void* param;
+    const void* grad;
+    float* master;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    int64_t n;
+    int32_t param_dtype; /* flarepp_dtype */
+    int32_t grad_dtype;
+} flarepp_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;       /* 1 for the first step */
+    int32_t state_bits; /* 32 or 8 */
+} flarepp_adamw_hyper;
+
+/*
+ * One AdamW step (decoupled weight decay) over all n_tensors tensors, in one launch for each
+ * combination of types and each few hundred tensors:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   w = (1 - lr wd) w - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
+ * every operation in float32, rounded to nearest (no contraction), w being master where there
+ * is one, else param; param takes w rounded to its type.
+ * 8-bit states hold m as 8-bit floats (e4m3) times the block's scale, max |m| / 256, and
+ * sqrt(v) as unsigned 8-bit floats with 4 exponent and 4 mantissa bits (code c stands for c / 16
+ * below 16 and for (1 + (c % 16) / 16) 2^(c / 16 - 1) from there on) times max sqrt(v) / 2^14, both
+ * rounded to nearest; a v that is not zero never becomes zero, and a block whose largest value is
+ * below 2^-100 is stored as zeros with scale 0. A gradient that is not finite spoils its value (8-bit
+ * states: the block of 256).
+ * `tensors` and `hyper` are host memory, read before the call returns; the hyperparameters are
+ * part of the launch (a captured graph replays them). n_tensors = 0 is a no-op.
+ */
+FLAREPP_API flarepp_status flarepp_adamw_step(const flarepp_adamw_tensor* tensors,
+                                              int64_t n_tensors, const flarepp_adamw_hyper* hyper,
+                                              void* stream);
+
+/*
+ * The values that 8-bit states stand for: m_out[i], v_out[i] (float32 [n] each, 16-byte aligned;
+ * host arrays of n_tensors device pointers) from tensors[i].m, .v, .m_scale, .v_scale.
+ */
+FLAREPP_API flarepp_status flarepp_adamw_moments(const flarepp_adamw_tensor* tensors,
+                                                 int64_t n_tensors, float* const* m_out,
+                                                 float* const* v_out, void* stream);
+
 /* Static description of a status code (never NULL). */
 FLAREPP_API const char* flarepp_status_string(flarepp_status status);
 

@@ -1,0 +1,471 @@
+// The AdamW step over all tensors of a model (flarepp_adamw_step) and the values of its 8-bit
+// states (flarepp_adamw_moments).
+//
+// The step is bound by its bytes: per value the weight and both moments are read and written and
+// the gradient is read (28 bytes in 32 bits; 14 to 16 with bf16 gradients, a float32 master and
+// 8-bit states), against some 20 operations. So one launch walks all tensors of a kind: the
+// table of tensors is a kernel parameter (no copy to the device, nothing to keep until the kernel
+// has run), a block takes 2,048 values of one tensor and finds it by bisection of the tensors'
+// first blocks, and a warp takes 256 of them, which is also the block that shares a scale in an
+// 8-bit state: its largest value is a warp reduction, and a state is read and written once.
+//
+// Every operation is rounded on its own (no contraction): the step is then a function of its inputs
+// that any float32 implementation of the same formulas gives bit for bit, 8-bit codes included.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "flarepp_internal.h"
+#include "tc_ptx.cuh"
+
+namespace flarepp {
+namespace {
+
+constexpr int kBlockVals = 256;               // values that share a scale
+constexpr int kThreads = 256;
+constexpr int kItem = kThreads * 8;           // values per thread block
+constexpr float kMTop = 256.f;                // what the largest |m| of a block is stored as
+constexpr float kRTop = 16384.f;              // what the largest sqrt(v) of a block is stored as
+constexpr float kTiny = 7.8886090522101181e-31f;  // 2^-100
+
+struct Entry {
+    void* param;
+    const void* grad;
+    float* master;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    int64_t n;
+};
+// CAP tensors of one kind; tensor i owns the thread blocks [first[i], first[i + 1])
+template <int CAP>
+struct Table {
+    Entry e[CAP];
+    uint32_t first[CAP + 1];
+    int count;
+};
+struct Coef {
+    float b1, c1, b2, c2, by_bias, eps, keep, rate;
+};
+
+template <int CAP>
+__device__ __forceinline__ int find_tensor(const Table<CAP>& t, uint32_t block) {
+    int lo = 0, hi = t.count;  // first[lo] <= block < first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (t.first[mid] <= block) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Four values at p[i .. i + 4), those from n on as zeros.
+__device__ __forceinline__ void load4(const float* p, int64_t i, int64_t n, float* x) {
+    if (i + 4 <= n) {
+        const float4 v = *reinterpret_cast<const float4*>(p + i);
+        x[0] = v.x;
+        x[1] = v.y;
+        x[2] = v.z;
+        x[3] = v.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = i + k < n ? p[i + k] : 0.f;
+    }
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, int64_t i, int64_t n, float* x) {
+    if (i + 4 <= n) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p + i);
+        x[0] = __uint_as_float(v.x << 16);
+        x[1] = __uint_as_float(v.x & 0xffff0000u);
+        x[2] = __uint_as_float(v.y << 16);
+        x[3] = __uint_as_float(v.y & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = i + k < n ? __bfloat162float(p[i + k]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store4(float* p, int64_t i, int64_t n, const float* x) {
+    if (i + 4 <= n) {
+        *reinterpret_cast<float4*>(p + i) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k < n) p[i + k] = x[k];
+    }
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t i, int64_t n, const float* x) {
+    if (i + 4 <= n) {
+        __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+        *reinterpret_cast<uint2*>(p + i) = make_uint2(*reinterpret_cast<uint32_t*>(&a),
+                                                      *reinterpret_cast<uint32_t*>(&b));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k < n) p[i + k] = __float2bfloat16_rn(x[k]);
+    }
+}
+__device__ __forceinline__ uint32_t load4_bytes(const void* p, int64_t i, int64_t n) {
+    const uint8_t* b = reinterpret_cast<const uint8_t*>(p);
+    if (i + 4 <= n) return *reinterpret_cast<const uint32_t*>(b + i);
+    uint32_t v = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (i + k < n) v |= (uint32_t)b[i + k] << (8 * k);
+    return v;
+}
+__device__ __forceinline__ void store4_bytes(void* p, int64_t i, int64_t n, uint32_t v) {
+    uint8_t* b = reinterpret_cast<uint8_t*>(p);
+    if (i + 4 <= n) {
+        *reinterpret_cast<uint32_t*>(b + i) = v;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k < n) b[i + k] = (uint8_t)(v >> (8 * k));
+    }
+}
+
+// Four e4m3 codes and their values (exact both ways but for the rounding of `pack`).
+__device__ __forceinline__ void unpack_m(uint32_t code, float* x) {
+    uint32_t lo, hi;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(code));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+    const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    x[0] = f.x;
+    x[1] = f.y;
+    x[2] = g.x;
+    x[3] = g.y;
+}
+__device__ __forceinline__ uint32_t pack_m(const float* x) {
+    uint32_t code;
+    asm("{\n\t.reg .b16 a, b;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\t"
+        "mov.b32 %0, {a, b};\n\t}"
+        : "=r"(code)
+        : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
+    return code;
+}
+// One code of sqrt(v): c / 16 below 16, (1 + (c % 16) / 16) 2^(c / 16 - 1) from there on.
+__device__ __forceinline__ float unpack_r(uint32_t c) {
+    return c < 16 ? (float)c * 0.0625f : __uint_as_float((c + (126u << 4)) << 19);
+}
+__device__ __forceinline__ uint32_t pack_r(float y) {
+    const uint32_t bits = __float_as_uint(y);
+    // to four mantissa bits, ties to even; below 1 the steps are sixteenths
+    int c = (int)((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (126 << 4);
+    if (y < 1.f) c = (int)rintf(__fmul_rn(y, 16.f));
+    c = min(max(c, y > 0.f ? 1 : 0), 255);
+    return (uint32_t)c;
+}
+
+// The largest |x| over the warp, as bits (so that a NaN is the largest of all).
+__device__ __forceinline__ float warp_most(const float (*x)[4]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = max(most, __float_as_uint(x[h][k]) & 0x7fffffffu);
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, most));
+}
+
+// P, G: types of the weights and the gradients. MASTER: the weights have a float32 master.
+// Q8: 8-bit states. A lane holds values 4 lane + 128 h + (0..3) of its warp's 256.
+template <typename P, typename G, bool MASTER, bool Q8, int CAP>
+__global__ void __launch_bounds__(kThreads)
+    adamw_kernel(const __grid_constant__ Table<CAP> table, const Coef c) {
+    const int t = find_tensor(table, blockIdx.x);
+    const Entry& e = table.e[t];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t n = e.n;
+    const int64_t at = (int64_t)(blockIdx.x - table.first[t]) * kItem + warp * kBlockVals;
+    if (at >= n) return;
+    const int64_t block = at / kBlockVals;
+    float w[2][4], g[2][4], m[2][4], v[2][4];
+    uint32_t mc[2], vc[2];
+    float ms, vs;
+    if (Q8) {
+        ms = e.m_scale[block];
+        vs = e.v_scale[block];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t i = at + 128 * h + 4 * lane;
+        load4(reinterpret_cast<const G*>(e.grad), i, n, g[h]);
+        if (MASTER) load4(e.master, i, n, w[h]);
+        else load4(reinterpret_cast<const P*>(e.param), i, n, w[h]);
+        if (Q8) {
+            mc[h] = load4_bytes(e.m, i, n);
+            vc[h] = load4_bytes(e.v, i, n);
+        } else {
+            load4(reinterpret_cast<const float*>(e.m), i, n, m[h]);
+            load4(reinterpret_cast<const float*>(e.v), i, n, v[h]);
+        }
+    }
+    float r[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (Q8) {
+            unpack_m(mc[h], m[h]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                m[h][k] = __fmul_rn(m[h][k], ms);
+                const float root = __fmul_rn(unpack_r((vc[h] >> (8 * k)) & 255u), vs);
+                v[h][k] = __fmul_rn(root, root);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float gr = g[h][k];
+            m[h][k] = __fadd_rn(__fmul_rn(m[h][k], c.b1), __fmul_rn(gr, c.c1));
+            v[h][k] = __fadd_rn(__fmul_rn(v[h][k], c.b2), __fmul_rn(__fmul_rn(gr, gr), c.c2));
+            r[h][k] = __fsqrt_rn(v[h][k]);
+            const float over = __fadd_rn(__fmul_rn(r[h][k], c.by_bias), c.eps);
+            w[h][k] = __fsub_rn(__fmul_rn(w[h][k], c.keep),
+                                __fmul_rn(__fdiv_rn(m[h][k], over), c.rate));
+        }
+        const int64_t i = at + 128 * h + 4 * lane;
+        if (MASTER) store4(e.master, i, n, w[h]);
+        store4(reinterpret_cast<P*>(e.param), i, n, w[h]);
+        if (!Q8) {
+            store4(reinterpret_cast<float*>(e.m), i, n, m[h]);
+            store4(reinterpret_cast<float*>(e.v), i, n, v[h]);
+        }
+    }
+    if (!Q8) return;
+    // values from n on are zeros and do not count
+    const float m_most = warp_most(m), r_most = warp_most(r);
+    const bool m_live = !(m_most < kTiny), r_live = !(r_most < kTiny);
+    const float m_by = m_live ? __fdiv_rn(kMTop, m_most) : 0.f;
+    const float r_by = r_live ? __fdiv_rn(kRTop, r_most) : 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t i = at + 128 * h + 4 * lane;
+        float y[4];
+        uint32_t code = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            y[k] = __fmul_rn(m[h][k], m_by);
+            code |= pack_r(__fmul_rn(r[h][k], r_by)) << (8 * k);
+        }
+        store4_bytes(e.m, i, n, pack_m(y));
+        store4_bytes(e.v, i, n, code);
+    }
+    if (lane == 0) {
+        e.m_scale[block] = m_live ? m_most * (1.f / kMTop) : 0.f;
+        e.v_scale[block] = r_live ? r_most * (1.f / kRTop) : 0.f;
+    }
+}
+
+// The values of 8-bit states; e.param and e.master are the outputs for m and v.
+template <int CAP>
+__global__ void __launch_bounds__(kThreads)
+    moments_kernel(const __grid_constant__ Table<CAP> table) {
+    const int t = find_tensor(table, blockIdx.x);
+    const Entry& e = table.e[t];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t n = e.n;
+    const int64_t at = (int64_t)(blockIdx.x - table.first[t]) * kItem + warp * kBlockVals;
+    if (at >= n) return;
+    const float ms = e.m_scale[at / kBlockVals], vs = e.v_scale[at / kBlockVals];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t i = at + 128 * h + 4 * lane;
+        const uint32_t mc = load4_bytes(e.m, i, n), vc = load4_bytes(e.v, i, n);
+        float m[4], v[4];
+        unpack_m(mc, m);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            m[k] = __fmul_rn(m[k], ms);
+            const float root = __fmul_rn(unpack_r((vc >> (8 * k)) & 255u), vs);
+            v[k] = __fmul_rn(root, root);
+        }
+        store4(reinterpret_cast<float*>(e.param), i, n, m);
+        store4(e.master, i, n, v);
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+// Tensors per launch: a table of kFew stays within the 4 KB of parameters that every launch
+// carries cheaply; one of kMany takes most of the 32 KB that a launch may carry.
+constexpr int kFew = 48;
+constexpr int kMany = 384;
+
+bool type_ok(int32_t t) { return t == FLAREPP_F32 || t == FLAREPP_BF16; }
+
+// 0..5 for the type combinations of the step
+int kind_of(const flarepp_adamw_tensor& t) {
+    const int g = t.grad_dtype == FLAREPP_BF16;
+    if (t.param_dtype == FLAREPP_F32) return g;
+    return 2 + 2 * (t.master != nullptr) + g;
+}
+
+flarepp_status check_tensor(const flarepp_adamw_tensor& t, bool q8) {
+    if (t.n < 0 || !type_ok(t.param_dtype) || !type_ok(t.grad_dtype))
+        return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (t.n == 0) return FLAREPP_OK;
+    const void* need[4] = {t.param, t.grad, t.m, t.v};
+    for (const void* p : need)
+        if (!p || !aligned16(p)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (!aligned16(t.master) || (t.master && t.param_dtype == FLAREPP_F32))
+        return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (q8 && (!t.m_scale || !t.v_scale || !aligned16(t.m_scale) || !aligned16(t.v_scale)))
+        return FLAREPP_ERR_INVALID_ARGUMENT;
+    const size_t n = (size_t)t.n, sb = (size_t)cdiv(t.n, kBlockVals) * 4;
+    const size_t state = n * (q8 ? 1 : 4);
+    const Span outs[6] = {{t.param, n * (t.param_dtype == FLAREPP_BF16 ? 2 : 4)},
+                          {t.master, n * 4},
+                          {t.m, state},
+                          {t.v, state},
+                          {q8 ? t.m_scale : nullptr, sb},
+                          {q8 ? t.v_scale : nullptr, sb}};
+    const Span in{t.grad, n * (t.grad_dtype == FLAREPP_BF16 ? 2 : 4)};
+    return disjoint(outs, 6, &in, 1) ? FLAREPP_OK : FLAREPP_ERR_INVALID_ARGUMENT;
+}
+
+// Launch once per CAP tensors that `pick` accepts; `fill` makes a tensor's entry.
+template <int CAP, typename Pick, typename Fill, typename Go>
+cudaError_t each_table(int64_t n_tensors, Pick pick, Fill fill, Go go) {
+    Table<CAP> t;
+    t.count = 0;
+    uint64_t blocks = 0;
+    for (int64_t i = 0; i <= n_tensors; ++i) {
+        const bool end = i == n_tensors;
+        if (!end && !pick(i)) continue;
+        Entry e{};
+        uint64_t more = 0;
+        if (!end) {
+            e = fill(i);
+            more = (uint64_t)cdiv(e.n, kItem);
+        }
+        if (t.count && (end || t.count == CAP || blocks + more > 0x7fffffffull)) {
+            t.first[t.count] = (uint32_t)blocks;
+            const cudaError_t err = go(t, (unsigned)blocks);
+            if (err != cudaSuccess) return err;
+            t.count = 0;
+            blocks = 0;
+        }
+        if (end) break;
+        if (more > 0x7fffffffull) return cudaErrorInvalidValue;
+        t.first[t.count] = (uint32_t)blocks;
+        t.e[t.count++] = e;
+        blocks += more;
+    }
+    return cudaSuccess;
+}
+
+template <typename P, typename G, bool MASTER, bool Q8, int CAP>
+cudaError_t go_step(const Table<CAP>& t, unsigned blocks, const Coef& c, cudaStream_t st) {
+    adamw_kernel<P, G, MASTER, Q8, CAP><<<blocks, kThreads, 0, st>>>(t, c);
+    return cudaGetLastError();
+}
+
+template <bool Q8, int CAP>
+cudaError_t step_all(const flarepp_adamw_tensor* ts, int64_t n, const Coef& c, cudaStream_t st) {
+    for (int kind = 0; kind < 6; ++kind) {
+        const cudaError_t e = each_table<CAP>(
+            n, [&](int64_t i) { return ts[i].n > 0 && kind_of(ts[i]) == kind; },
+            [&](int64_t i) {
+                const flarepp_adamw_tensor& t = ts[i];
+                return Entry{t.param, t.grad, t.master, t.m, t.v, t.m_scale, t.v_scale, t.n};
+            },
+            [&](const Table<CAP>& t, unsigned blocks) {
+                using B = __nv_bfloat16;
+                switch (kind) {
+                    case 0: return go_step<float, float, false, Q8, CAP>(t, blocks, c, st);
+                    case 1: return go_step<float, B, false, Q8, CAP>(t, blocks, c, st);
+                    case 2: return go_step<B, float, false, Q8, CAP>(t, blocks, c, st);
+                    case 3: return go_step<B, B, false, Q8, CAP>(t, blocks, c, st);
+                    case 4: return go_step<B, float, true, Q8, CAP>(t, blocks, c, st);
+                }
+                return go_step<B, B, true, Q8, CAP>(t, blocks, c, st);
+            });
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+flarepp_status adamw_step(const flarepp_adamw_tensor* ts, int64_t n, const flarepp_adamw_hyper* h,
+                          cudaStream_t st) {
+    if (!h || n < 0 || (n && !ts)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (h->state_bits != 32 && h->state_bits != 8) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (!isfinite(h->lr) || !isfinite(h->weight_decay) || !(h->eps >= 0) || !isfinite(h->eps) ||
+        !(h->beta1 >= 0 && h->beta1 < 1) || !(h->beta2 >= 0 && h->beta2 < 1) || h->step < 1)
+        return FLAREPP_ERR_INVALID_ARGUMENT;
+    const bool q8 = h->state_bits == 8;
+    for (int64_t i = 0; i < n; ++i) {
+        const flarepp_status s = check_tensor(ts[i], q8);
+        if (s != FLAREPP_OK) return s;
+    }
+    Coef c;
+    c.b1 = (float)h->beta1;
+    c.c1 = (float)(1 - h->beta1);
+    c.b2 = (float)h->beta2;
+    c.c2 = (float)(1 - h->beta2);
+    c.by_bias = (float)(1 / sqrt(1 - pow(h->beta2, (double)h->step)));
+    c.eps = (float)h->eps;
+    c.keep = (float)(1 - h->lr * h->weight_decay);
+    c.rate = (float)(h->lr / (1 - pow(h->beta1, (double)h->step)));
+    const cudaError_t e = n <= kFew ? (q8 ? step_all<true, kFew>(ts, n, c, st)
+                                          : step_all<false, kFew>(ts, n, c, st))
+                                    : (q8 ? step_all<true, kMany>(ts, n, c, st)
+                                          : step_all<false, kMany>(ts, n, c, st));
+    return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
+}
+
+template <int CAP>
+cudaError_t moments_all(const flarepp_adamw_tensor* ts, int64_t n, float* const* m_out,
+                        float* const* v_out, cudaStream_t st) {
+    return each_table<CAP>(
+        n, [&](int64_t i) { return ts[i].n > 0; },
+        [&](int64_t i) {
+            const flarepp_adamw_tensor& t = ts[i];
+            return Entry{m_out[i], nullptr, v_out[i], t.m, t.v, t.m_scale, t.v_scale, t.n};
+        },
+        [&](const Table<CAP>& t, unsigned blocks) {
+            moments_kernel<CAP><<<blocks, kThreads, 0, st>>>(t);
+            return cudaGetLastError();
+        });
+}
+
+flarepp_status adamw_moments(const flarepp_adamw_tensor* ts, int64_t n, float* const* m_out,
+                             float* const* v_out, cudaStream_t st) {
+    if (n < 0 || (n && (!ts || !m_out || !v_out))) return FLAREPP_ERR_INVALID_ARGUMENT;
+    for (int64_t i = 0; i < n; ++i) {
+        const flarepp_adamw_tensor& t = ts[i];
+        if (t.n < 0) return FLAREPP_ERR_INVALID_ARGUMENT;
+        if (t.n == 0) continue;
+        const void* need[6] = {t.m, t.v, t.m_scale, t.v_scale, m_out[i], v_out[i]};
+        for (const void* p : need)
+            if (!p || !aligned16(p)) return FLAREPP_ERR_INVALID_ARGUMENT;
+        const size_t sb = (size_t)cdiv(t.n, kBlockVals) * 4;
+        const Span outs[2] = {{m_out[i], (size_t)t.n * 4}, {v_out[i], (size_t)t.n * 4}};
+        const Span ins[4] = {{t.m, (size_t)t.n}, {t.v, (size_t)t.n}, {t.m_scale, sb}, {t.v_scale, sb}};
+        if (!disjoint(outs, 2, ins, 4)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    }
+    const cudaError_t e = n <= kFew ? moments_all<kFew>(ts, n, m_out, v_out, st)
+                                    : moments_all<kMany>(ts, n, m_out, v_out, st);
+    return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace flarepp
+
+extern "C" {
+
+flarepp_status flarepp_adamw_step(const flarepp_adamw_tensor* tensors, int64_t n_tensors,
+                                  const flarepp_adamw_hyper* hyper, void* stream) {
+    return flarepp::adamw_step(tensors, n_tensors, hyper, (cudaStream_t)stream);
+}
+
+flarepp_status flarepp_adamw_moments(const flarepp_adamw_tensor* tensors, int64_t n_tensors,
+                                     float* const* m_out, float* const* v_out, void* stream) {
+    return flarepp::adamw_moments(tensors, n_tensors, m_out, v_out, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,551 @@
+// Token embeddings (flarepp_embedding_*): the scaled lookup and the gradient of the table.
+//
+// The gradient sums the rows of dY by id. Adding them with atomics would make the result depend on
+// their order and serialises where ids repeat (byte sequences meet each row hundreds of times), so
+// the positions are sorted by id first: a stable least-digit-first radix sort of (id, position) in
+// one pass for tables of up to 2,047 rows, two up to 4 M, three beyond. Then equal stretches of
+// the sorted positions are summed in parallel whatever the lengths of the runs of one id; a run that
+// crosses from one stretch into the next leaves float32 partial sums, which a last kernel adds in
+// order.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "flarepp_internal.h"
+#include "tc_ptx.cuh"
+
+namespace flarepp {
+namespace {
+
+// ------------------------------------------------------------------ vectors of 2 to 16 bytes
+template <int BYTES>
+struct Raw;
+template <>
+struct Raw<16> { using t = uint4; };
+template <>
+struct Raw<8> { using t = uint2; };
+template <>
+struct Raw<4> { using t = uint32_t; };
+template <>
+struct Raw<2> { using t = uint16_t; };
+
+template <typename E, int N>
+struct alignas(sizeof(E) * N) Vec {
+    E v[N];
+};
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_f32(float& d, float x) { d = x; }
+__device__ __forceinline__ void from_f32(__nv_bfloat16& d, float x) { d = __float2bfloat16_rn(x); }
+
+template <typename E, int N>
+__device__ __forceinline__ Vec<E, N> load_vec(const E* p) {
+    using R = typename Raw<sizeof(E) * N>::t;
+    const R r = *reinterpret_cast<const R*>(p);
+    Vec<E, N> v;
+    *reinterpret_cast<R*>(&v) = r;
+    return v;
+}
+template <typename E, int N>
+__device__ __forceinline__ void store_vec(E* p, const Vec<E, N>& v) {
+    using R = typename Raw<sizeof(E) * N>::t;
+    *reinterpret_cast<R*>(p) = *reinterpret_cast<const R*>(&v);
+}
+
+// The row that an id names, or -1 for an empty position (an id of V or more is recorded).
+template <typename I>
+__device__ __forceinline__ int64_t row_of(I id, int64_t V, int* status) {
+    if (id < 0) return -1;
+    if ((int64_t)id >= V) {
+        if (status) atomicExch(status, (int)FLAREPP_ERR_INVALID_ARGUMENT);
+        return -1;
+    }
+    return (int64_t)id;
+}
+
+// ------------------------------------------------------------------ lookup
+// threadIdx.x walks a row's vectors, threadIdx.y the block's rows; four rows a thread, so that
+// four table loads are in flight.
+constexpr int kLookupRows = 4;
+
+template <typename E, int N, typename I>
+__global__ void __launch_bounds__(256)
+    lookup_kernel(const I* __restrict__ ids, const E* __restrict__ table, int64_t T, int64_t V,
+                  int64_t C, float scale, E* __restrict__ Y, int* status) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int64_t t0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * kLookupRows;
+    int64_t row[kLookupRows];
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k)
+        row[k] = t0 + k < T ? row_of(ids[t0 + k], V, status) : -1;
+    for (int64_t c = (int64_t)threadIdx.x * N; c < C; c += (int64_t)blockDim.x * N) {
+        Vec<E, N> x[kLookupRows];
+#pragma unroll
+        for (int k = 0; k < kLookupRows; ++k)
+            if (row[k] >= 0) x[k] = load_vec<E, N>(table + row[k] * C + c);
+#pragma unroll
+        for (int k = 0; k < kLookupRows; ++k) {
+            if (t0 + k >= T) break;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                from_f32(x[k].v[i], row[k] >= 0 ? to_f32(x[k].v[i]) * scale : 0.f);
+            store_vec<E, N>(Y + (t0 + k) * C + c, x[k]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ sort
+// A block sorts a contiguous tile of the positions, a warp a contiguous stretch of the tile, 32
+// positions a step: the order of equal digits is the order of the tiles, stretches, steps and
+// lanes, so the sort is stable.
+constexpr int kSortThreads = 256;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kMaxBits = 11;
+
+struct SortPlan {
+    int passes, bits;     // digits, and bits of each
+    int64_t tile, tiles;  // positions per block, blocks
+};
+
+// The id of position i as a sort key: empty positions come last, as V.
+template <typename I>
+__device__ __forceinline__ uint32_t key_at(const I* ids, const uint32_t* keys, int64_t i,
+                                           int64_t V, int* status) {
+    if (keys) return keys[i];
+    const int64_t r = row_of(ids[i], V, status);
+    return r < 0 ? (uint32_t)V : (uint32_t)r;
+}
+
+// hist[digit][tile] = how often the tile has the digit.
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads)
+    count_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ keys, int64_t T,
+                 int64_t V, int64_t tile, int shift, int bins, uint32_t* __restrict__ hist,
+                 int* status) {
+    extern __shared__ uint32_t cnt[];
+    tc::pdl_trigger();
+    for (int d = threadIdx.x; d < bins; d += kSortThreads) cnt[d] = 0;
+    __syncthreads();
+    tc::pdl_wait();
+    const int64_t i0 = (int64_t)blockIdx.x * tile, i1 = min(T, i0 + tile);
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
+        atomicAdd(&cnt[(key_at(ids, keys, i, V, status) >> shift) & (bins - 1)], 1u);
+    __syncthreads();
+    for (int d = threadIdx.x; d < bins; d += kSortThreads)
+        hist[(int64_t)d * gridDim.x + blockIdx.x] = cnt[d];
+}
+
+// Turn each digit's counts into what precedes a tile within the digit; total[digit] = all of it.
+// One warp per digit.
+__global__ void __launch_bounds__(256)
+    scan_kernel(uint32_t* __restrict__ hist, int64_t tiles, int bins,
+                uint32_t* __restrict__ total) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int d = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (d >= bins) return;
+    uint32_t* h = hist + (int64_t)d * tiles;
+    uint32_t sum = 0;
+    for (int64_t b = 0; b < tiles; b += 32) {
+        const uint32_t v = b + lane < tiles ? h[b + lane] : 0;
+        uint32_t s = v;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const uint32_t u = __shfl_up_sync(0xffffffffu, s, o);
+            if (lane >= o) s += u;
+        }
+        if (b + lane < tiles) h[b + lane] = sum + s - v;
+        sum += __shfl_sync(0xffffffffu, s, 31);
+    }
+    if (lane == 0) total[d] = sum;
+}
+
+// Move every position to its place in the order of the digit.
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads)
+    place_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ keys,
+                 const uint32_t* __restrict__ pos, int64_t T, int64_t V, int64_t tile, int shift,
+                 int bins, const uint32_t* __restrict__ hist, const uint32_t* __restrict__ total,
+                 uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out) {
+    extern __shared__ uint32_t sm[];  // [kSortWarps][bins] places, [bins] starts of the digits
+    uint32_t* start = sm + kSortWarps * bins;
+    __shared__ uint32_t warp_sum[kSortWarps];
+    tc::pdl_trigger();
+    for (int d = threadIdx.x; d < kSortWarps * bins; d += kSortThreads) sm[d] = 0;
+    tc::pdl_wait();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    // starts: an exclusive scan of the totals, a stretch of bins per thread
+    const int per = (bins + kSortThreads - 1) / kSortThreads;
+    uint32_t mine = 0;
+    for (int k = 0; k < per; ++k) {
+        const int d = threadIdx.x * per + k;
+        if (d < bins) {
+            start[d] = mine;
+            mine += total[d];
+        }
+    }
+    uint32_t s = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += u;
+    }
+    if (lane == 31) warp_sum[warp] = s;
+    __syncthreads();
+    uint32_t before = s - mine;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    for (int k = 0; k < per; ++k) {
+        const int d = threadIdx.x * per + k;
+        if (d < bins) start[d] += before;
+    }
+    // counts of each warp's stretch
+    const int64_t t0 = (int64_t)blockIdx.x * tile, t1 = min(T, t0 + tile);
+    const int64_t stretch = (tile + kSortWarps * 32 - 1) / (kSortWarps * 32) * 32;
+    const int64_t i0 = t0 + warp * stretch, i1 = min(t1, i0 + stretch);
+    uint32_t* mine_at = sm + warp * bins;
+    for (int64_t i = i0 + lane; i < i1; i += 32)
+        atomicAdd(&mine_at[(key_at(ids, keys, i, V, nullptr) >> shift) & (bins - 1)], 1u);
+    __syncthreads();
+    // places: start of the digit + tiles before + stretches before
+    for (int d = threadIdx.x; d < bins; d += kSortThreads) {
+        uint32_t at = start[d] + hist[(int64_t)d * gridDim.x + blockIdx.x];
+        for (int w = 0; w < kSortWarps; ++w) {
+            const uint32_t n = sm[w * bins + d];
+            sm[w * bins + d] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    for (int64_t i = i0; i < i1; i += 32) {
+        const bool in = i + lane < i1;
+        const uint32_t key = in ? key_at(ids, keys, i + lane, V, nullptr) : 0xffffffffu;
+        const uint32_t d = in ? (key >> shift) & (bins - 1) : 0xffffffffu;
+        const uint32_t same = __match_any_sync(0xffffffffu, d);
+        const uint32_t rank = __popc(same & ((1u << lane) - 1u));
+        uint32_t at = 0;
+        if (in) at = mine_at[d] + rank;
+        __syncwarp();
+        if (in && rank == 0) mine_at[d] += __popc(same);
+        __syncwarp();
+        if (in) {
+            keys_out[at] = key;
+            pos_out[at] = pos ? pos[i + lane] : (uint32_t)(i + lane);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ sums
+constexpr int kStretch = 64;  // sorted positions per thread row
+constexpr int kBatch = 8;     // rows of dY in flight per thread
+
+// Thread (x, y): N columns of stretch blockIdx.x * blockDim.y + y. A run that lies within the
+// stretch goes to the table; one that began before it leaves its sum in head[stretch], one that
+// begins here and goes on in tail[stretch].
+template <typename E, int N>
+__global__ void __launch_bounds__(256)
+    sum_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos,
+               const E* __restrict__ dY, int64_t T, int64_t V, int64_t C, float scale,
+               E* __restrict__ dtable, float* __restrict__ head, float* __restrict__ tail) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
+    const int64_t st = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int64_t i0 = st * kStretch, i1 = min(T, i0 + kStretch);
+    if (c >= C || i0 >= T) return;
+    uint32_t cur = keys[i0];
+    if (cur == (uint32_t)V) return;  // empty positions come last
+    bool began = i0 == 0 || keys[i0 - 1] != cur;
+    float acc[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = 0.f;
+    auto flush = [&](bool more) {
+        if (began && !more) {
+            Vec<E, N> o;
+#pragma unroll
+            for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
+            store_vec<E, N>(dtable + (int64_t)cur * C + c, o);
+        } else {
+            float* d = (began ? tail : head) + st * C + c;
+#pragma unroll
+            for (int k = 0; k < N; ++k) d[k] = acc[k];
+        }
+    };
+    bool ended = false;
+    for (int64_t i = i0; i < i1 && !ended; i += kBatch) {
+        uint32_t key[kBatch];
+        Vec<E, N> x[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            key[k] = i + k < i1 ? keys[i + k] : (uint32_t)V;
+            if (key[k] != (uint32_t)V) x[k] = load_vec<E, N>(dY + (int64_t)pos[i + k] * C + c);
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (i + k >= i1 || ended) break;
+            if (key[k] != cur) {
+                flush(false);
+                began = true;
+                cur = key[k];
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] = 0.f;
+                if (cur == (uint32_t)V) {
+                    ended = true;
+                    break;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j] += to_f32(x[k].v[j]);
+        }
+    }
+    if (!ended) flush(i1 < T && keys[i1] == cur);
+}
+
+// The runs that cross stretches: the stretch where such a run begins adds its parts in order.
+template <typename E, int N>
+__global__ void __launch_bounds__(256)
+    join_kernel(const uint32_t* __restrict__ keys, int64_t T, int64_t V, int64_t C, float scale,
+                const float* __restrict__ head, const float* __restrict__ tail,
+                E* __restrict__ dtable) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
+    const int64_t st = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int64_t i0 = st * kStretch, i1 = i0 + kStretch;
+    if (c >= C || i1 >= T) return;
+    const uint32_t key = keys[i1 - 1];
+    if (key == (uint32_t)V || keys[i1] != key) return;          // nothing goes on from here
+    if (keys[i0] == key && i0 > 0 && keys[i0 - 1] == key) return;  // it did not begin here
+    float acc[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = tail[st * C + c + k];
+    for (int64_t s = st + 1; s * kStretch < T && keys[s * kStretch] == key; ++s)
+#pragma unroll
+        for (int k = 0; k < N; ++k) acc[k] += head[s * C + c + k];
+    Vec<E, N> o;
+#pragma unroll
+    for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
+    store_vec<E, N>(dtable + (int64_t)key * C + c, o);
+}
+
+// ------------------------------------------------------------------ host side
+
+flarepp_status check_shape(const flarepp_embedding_shape* s) {
+    if (!s || s->T < 0 || s->V < 1 || s->C < 1) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s->dtype != FLAREPP_F32 && s->dtype != FLAREPP_BF16) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s->id_bytes != 4 && s->id_bytes != 8) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s->T > 0x7fffffff || s->V > 0x7ffffffe || s->C > (1 << 20)) return FLAREPP_ERR_UNSUPPORTED;
+    return FLAREPP_OK;
+}
+
+size_t elem(const flarepp_embedding_shape& s) { return s.dtype == FLAREPP_BF16 ? 2 : 4; }
+
+// Values per vector: the widest that divides a row (rows then keep the base's alignment).
+int vec_of(const flarepp_embedding_shape& s) {
+    int n = (int)(16 / elem(s));
+    while (s.C % n) n /= 2;
+    return n;
+}
+// Threads along a row: enough for its vectors, a power of two up to `most`.
+int lanes_for(int64_t vecs, int most) {
+    int x = 1;
+    while (x < most && x < vecs) x *= 2;
+    return x;
+}
+
+SortPlan sort_plan(const flarepp_embedding_shape& s) {
+    SortPlan p{};
+    int bits = 1;
+    while (((int64_t)1 << bits) <= s.V) ++bits;  // keys 0..V
+    p.passes = (int)cdiv(bits, kMaxBits);
+    p.bits = (int)cdiv(bits, p.passes);
+    p.tile = cdiv(cdiv(s.T, kNumSMs), 1024) * 1024;  // about a block per SM
+    p.tiles = cdiv(s.T, p.tile);
+    return p;
+}
+
+struct Layout {
+    SortPlan sort;
+    int64_t stretches;
+    size_t off_keys[2], off_pos[2], off_hist, off_total, off_head, off_tail, total;
+};
+Layout layout_of(const flarepp_embedding_shape& s) {
+    Layout L{};
+    L.sort = sort_plan(s);
+    L.stretches = cdiv(s.T, kStretch);
+    auto take = [&](int64_t bytes) {
+        const size_t at = L.total;
+        L.total = align_up(at + (size_t)bytes, kWsAlign);
+        return at;
+    };
+    const int64_t bins = (int64_t)1 << L.sort.bits;
+    for (int i = 0; i < 2; ++i) {
+        L.off_keys[i] = take(s.T * 4);
+        L.off_pos[i] = take(s.T * 4);
+    }
+    L.off_hist = take(bins * L.sort.tiles * 4);
+    L.off_total = take(bins * 4);
+    L.off_head = take(L.stretches * s.C * 4);
+    L.off_tail = take(L.stretches * s.C * 4);
+    return L;
+}
+
+template <typename E, int N, typename I>
+cudaError_t lookup(const flarepp_embedding_shape& s, const void* ids, const void* table,
+                   float scale, void* Y, int* status, cudaStream_t st) {
+    const int x = lanes_for(cdiv(s.C, N), 256), y = 256 / x;
+    return launch_pdl(lookup_kernel<E, N, I>, dim3((unsigned)cdiv(s.T, y * kLookupRows)),
+                      dim3(x, y), 0, st, (const I*)ids, (const E*)table, s.T, s.V, s.C, scale,
+                      (E*)Y, status);
+}
+template <typename E, int N>
+cudaError_t lookup(const flarepp_embedding_shape& s, const void* ids, const void* table,
+                   float scale, void* Y, int* status, cudaStream_t st) {
+    return s.id_bytes == 4 ? lookup<E, N, int32_t>(s, ids, table, scale, Y, status, st)
+                           : lookup<E, N, int64_t>(s, ids, table, scale, Y, status, st);
+}
+
+// keys and positions in order of the id; returns which of the two buffers holds them
+template <typename I>
+cudaError_t sort(const flarepp_embedding_shape& s, const Layout& L, const void* ids, char* ws,
+                 int* status, int* at, cudaStream_t st) {
+    const int bins = 1 << L.sort.bits;
+    uint32_t* hist = (uint32_t*)(ws + L.off_hist);
+    uint32_t* total = (uint32_t*)(ws + L.off_total);
+    const uint32_t *keys = nullptr, *pos = nullptr;
+    const unsigned tiles = (unsigned)L.sort.tiles;
+    for (int p = 0; p < L.sort.passes; ++p) {
+        const int shift = p * L.sort.bits;
+        *at = p & 1;
+        uint32_t* ko = (uint32_t*)(ws + L.off_keys[*at]);
+        uint32_t* po = (uint32_t*)(ws + L.off_pos[*at]);
+        cudaError_t e = launch_pdl(count_kernel<I>, dim3(tiles), dim3(kSortThreads), bins * 4, st,
+                                   (const I*)ids, keys, s.T, s.V, L.sort.tile, shift, bins, hist,
+                                   p == 0 ? status : nullptr);
+        if (e == cudaSuccess)
+            e = launch_pdl(scan_kernel, dim3((unsigned)cdiv(bins, 8)), dim3(256), 0, st, hist,
+                           L.sort.tiles, bins, total);
+        const size_t smem = (size_t)(kSortWarps + 1) * bins * 4;
+        if (e == cudaSuccess && smem > 48 * 1024)
+            e = cudaFuncSetAttribute(place_kernel<I>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (kSortWarps + 1) << (kMaxBits + 2));
+        if (e == cudaSuccess)
+            e = launch_pdl(place_kernel<I>, dim3(tiles), dim3(kSortThreads), smem, st,
+                           (const I*)ids, keys, pos, s.T, s.V, L.sort.tile, shift, bins,
+                           (const uint32_t*)hist, (const uint32_t*)total, ko, po);
+        if (e != cudaSuccess) return e;
+        keys = ko;
+        pos = po;
+    }
+    return cudaSuccess;
+}
+
+template <typename E, int N>
+cudaError_t sums(const flarepp_embedding_shape& s, const Layout& L, int at, const void* dY,
+                 float scale, void* dtable, char* ws, cudaStream_t st) {
+    const int64_t vecs = cdiv(s.C, N);
+    const int x = lanes_for(vecs, 32), y = 256 / x;
+    const dim3 grid((unsigned)cdiv(L.stretches, y), (unsigned)cdiv(vecs, x));
+    const uint32_t* keys = (const uint32_t*)(ws + L.off_keys[at]);
+    const uint32_t* pos = (const uint32_t*)(ws + L.off_pos[at]);
+    float* head = (float*)(ws + L.off_head);
+    float* tail = (float*)(ws + L.off_tail);
+    cudaError_t e = launch_pdl(sum_kernel<E, N>, grid, dim3(x, y), 0, st, keys, pos,
+                               (const E*)dY, s.T, s.V, s.C, scale, (E*)dtable, head, tail);
+    if (e == cudaSuccess && L.stretches > 1)
+        e = launch_pdl(join_kernel<E, N>, grid, dim3(x, y), 0, st, keys, s.T, s.V, s.C, scale,
+                       (const float*)head, (const float*)tail, (E*)dtable);
+    return e;
+}
+
+flarepp_status embedding_fwd(const flarepp_embedding_shape* shape, const void* ids,
+                             const void* table, float scale, void* Y, int32_t* status,
+                             cudaStream_t st) {
+    const flarepp_status bad = check_shape(shape);
+    if (bad != FLAREPP_OK) return bad;
+    const flarepp_embedding_shape s = *shape;
+    if (!isfinite(scale)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s.T == 0) return FLAREPP_OK;
+    if (!ids || !table || !Y || !aligned16(ids) || !aligned16(table) || !aligned16(Y))
+        return FLAREPP_ERR_INVALID_ARGUMENT;
+    const Span outs[2] = {{Y, (size_t)s.T * s.C * elem(s)}, {status, 4}};
+    const Span ins[2] = {{ids, (size_t)s.T * s.id_bytes}, {table, (size_t)s.V * s.C * elem(s)}};
+    if (!disjoint(outs, 2, ins, 2)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    using B = __nv_bfloat16;
+    cudaError_t e;
+    if (s.dtype == FLAREPP_BF16) switch (vec_of(s)) {
+        case 8: e = lookup<B, 8>(s, ids, table, scale, Y, status, st); break;
+        case 4: e = lookup<B, 4>(s, ids, table, scale, Y, status, st); break;
+        case 2: e = lookup<B, 2>(s, ids, table, scale, Y, status, st); break;
+        default: e = lookup<B, 1>(s, ids, table, scale, Y, status, st);
+    } else switch (vec_of(s)) {
+        case 4: e = lookup<float, 4>(s, ids, table, scale, Y, status, st); break;
+        case 2: e = lookup<float, 2>(s, ids, table, scale, Y, status, st); break;
+        default: e = lookup<float, 1>(s, ids, table, scale, Y, status, st);
+    }
+    return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
+}
+
+flarepp_status embedding_bwd(const flarepp_embedding_shape* shape, const void* ids, const void* dY,
+                             float scale, void* dtable, void* workspace, size_t workspace_bytes,
+                             int32_t* status, cudaStream_t st) {
+    const flarepp_status bad = check_shape(shape);
+    if (bad != FLAREPP_OK) return bad;
+    const flarepp_embedding_shape s = *shape;
+    if (!isfinite(scale)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (!dtable || !aligned16(dtable)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    const size_t out_bytes = (size_t)s.V * s.C * elem(s);
+    const Layout L = s.T ? layout_of(s) : Layout{};
+    if (s.T) {
+        if (!ids || !dY || !aligned16(ids) || !aligned16(dY)) return FLAREPP_ERR_INVALID_ARGUMENT;
+        if (!workspace || (uintptr_t)workspace % kWsAlign || workspace_bytes < L.total)
+            return FLAREPP_ERR_WORKSPACE;
+        const Span outs[3] = {{dtable, out_bytes}, {workspace, L.total}, {status, 4}};
+        const Span ins[2] = {{ids, (size_t)s.T * s.id_bytes}, {dY, (size_t)s.T * s.C * elem(s)}};
+        if (!disjoint(outs, 3, ins, 2)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    }
+    if (cudaMemsetAsync(dtable, 0, out_bytes, st) != cudaSuccess) return FLAREPP_ERR_CUDA;
+    if (s.T == 0) return FLAREPP_OK;
+    char* ws = (char*)workspace;
+    int at = 0;
+    cudaError_t e = s.id_bytes == 4 ? sort<int32_t>(s, L, ids, ws, status, &at, st)
+                                    : sort<int64_t>(s, L, ids, ws, status, &at, st);
+    if (e != cudaSuccess) return FLAREPP_ERR_CUDA;
+    using B = __nv_bfloat16;
+    if (s.dtype == FLAREPP_BF16) switch (vec_of(s)) {
+        case 8: e = sums<B, 8>(s, L, at, dY, scale, dtable, ws, st); break;
+        case 4: e = sums<B, 4>(s, L, at, dY, scale, dtable, ws, st); break;
+        case 2: e = sums<B, 2>(s, L, at, dY, scale, dtable, ws, st); break;
+        default: e = sums<B, 1>(s, L, at, dY, scale, dtable, ws, st);
+    } else switch (vec_of(s)) {
+        case 4: e = sums<float, 4>(s, L, at, dY, scale, dtable, ws, st); break;
+        case 2: e = sums<float, 2>(s, L, at, dY, scale, dtable, ws, st); break;
+        default: e = sums<float, 1>(s, L, at, dY, scale, dtable, ws, st);
+    }
+    return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace flarepp
+
+extern "C" {
+
+flarepp_status flarepp_embedding_fwd(const flarepp_embedding_shape* shape, const void* ids,
+                                     const void* table, float scale, void* Y, int32_t* status,
+                                     void* stream) {
+    return flarepp::embedding_fwd(shape, ids, table, scale, Y, status, (cudaStream_t)stream);
+}
+
+size_t flarepp_embedding_bwd_workspace_bytes(const flarepp_embedding_shape* shape) {
+    if (flarepp::check_shape(shape) != FLAREPP_OK || shape->T == 0) return 0;
+    return flarepp::layout_of(*shape).total;
+}
+
+flarepp_status flarepp_embedding_bwd(const flarepp_embedding_shape* shape, const void* ids,
+                                     const void* dY, float scale, void* dtable, void* workspace,
+                                     size_t workspace_bytes, int32_t* status, void* stream) {
+    return flarepp::embedding_bwd(shape, ids, dY, scale, dtable, workspace, workspace_bytes,
+                                  status, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -39,14 +39,6 @@ namespace {
 
 constexpr int kStageEvents = 6;
 
-bool aligned16(const void* ptr) { return ((uintptr_t)ptr & 15u) == 0; }
-
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-    if (!a || !b || na == 0 || nb == 0) return false;
-    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-    return a0 < b0 + nb && b0 < a0 + na;
-}
-
 bool spans_overlap(const void* const* ptrs, const size_t* bytes, int n, const void* p,
                    size_t nb) {
     for (int i = 0; i < n; ++i)

@@ -1,0 +1,390 @@
+// The linear layer (flarepp_linear_*): argument checks, workspace layout, the launch sequence of
+// its products (tc_linear.cu), and the memory-bound kernels around them.
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "linear_internal.h"
+#include "tc_ptx.cuh"
+
+namespace flarepp {
+namespace {
+
+// Rows up to which a product runs with the weights as its tile rows: the weights fill the
+// 128 rows of the tensor core's tile whatever the number of tokens, which become its columns.
+constexpr int64_t kFewRows = 128;
+constexpr int kDzCols = 256;  // columns per block of dz_kernel: 32 lanes x 8
+constexpr int kDzRows = 8;    // rows a block of dz_kernel reads at once
+
+int64_t pad8(int64_t n) { return cdiv(n, 8) * 8; }
+
+// dst [rows][pitch] = src [rows][cols] with zeros behind each row: the 16-byte line pitch that
+// TMA asks for. One thread per eight values.
+__global__ void pad_kernel(const __nv_bfloat16* __restrict__ src, int64_t rows, int64_t cols,
+                           int64_t pitch, __nv_bfloat16* __restrict__ dst) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int64_t per = pitch / 8, n = rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
+         i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t r = i / per, c = (i - r * per) * 8;
+        __align__(16) __nv_bfloat16 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = c + k < cols ? src[r * cols + c + k] : __float2bfloat16_rn(0.f);
+        *reinterpret_cast<uint4*>(dst + r * pitch + c) = *reinterpret_cast<const uint4*>(v);
+    }
+}
+
+// What follows the float32 sums of a cut contraction: the chunks added in order, then the
+// epilogue (bias, activation, residual). One thread per four columns.
+__global__ void finish_kernel(const float* __restrict__ part, int chunks, int64_t rows,
+                              int64_t cols, int64_t ldp, int act,
+                              const __nv_bfloat16* __restrict__ bias,
+                              const __nv_bfloat16* __restrict__ R, __nv_bfloat16* __restrict__ Y,
+                              __nv_bfloat16* __restrict__ Z) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int64_t per = ldp / 4;
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= rows * per) return;
+    const int64_t r = i / per, c = (i - r * per) * 4;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    const float* p = part + r * ldp + c;
+#pragma unroll 4
+    for (int k = 0; k < chunks; ++k, p += rows * ldp) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        x[0] += v.x;
+        x[1] += v.y;
+        x[2] += v.z;
+        x[3] += v.w;
+    }
+    const int64_t at = r * cols + c;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (c + k >= cols) break;
+        float z = x[k];
+        if (bias) z += __bfloat162float(bias[c + k]);
+        if (Z) Z[at + k] = __float2bfloat16_rn(z);
+        z = act_value(act, z);
+        if (R) z += __bfloat162float(R[at + k]);
+        Y[at + k] = __float2bfloat16_rn(z);
+    }
+}
+
+// dZ = dY o act'(Z) into lines of `ldz` values (not written when dZ is null), and the column sums
+// of the unrounded dZ over the block's rows into db_part[blockIdx.y][ldz]. VEC: eight values at
+// a time (cols a multiple of 8).
+template <bool VEC>
+__global__ void __launch_bounds__(256)
+    dz_kernel(const __nv_bfloat16* __restrict__ dY, const __nv_bfloat16* __restrict__ Z,
+              int64_t rows, int64_t cols, int64_t rows_per, int act, int64_t ldz,
+              __nv_bfloat16* __restrict__ dZ, float* __restrict__ db_part) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    __shared__ float sums[kDzRows][kDzCols];
+    const int lane = threadIdx.x % 32, ty = threadIdx.x / 32;
+    const int64_t c = (int64_t)blockIdx.x * kDzCols + lane * 8;
+    const int64_t r1 = min(rows, (int64_t)(blockIdx.y + 1) * rows_per);
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < cols) {
+#pragma unroll 2
+        for (int64_t r = (int64_t)blockIdx.y * rows_per + ty; r < r1; r += kDzRows) {
+            __align__(16) __nv_bfloat16 g[8], z[8];
+            const int64_t at = r * cols + c;
+            if (VEC) {
+                *reinterpret_cast<uint4*>(g) = *reinterpret_cast<const uint4*>(dY + at);
+                if (Z) *reinterpret_cast<uint4*>(z) = *reinterpret_cast<const uint4*>(Z + at);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const bool in = c + k < cols;
+                    g[k] = in ? dY[at + k] : __float2bfloat16_rn(0.f);
+                    if (Z) z[k] = in ? Z[at + k] : __float2bfloat16_rn(0.f);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float v = __bfloat162float(g[k]);
+                if (Z) v *= act_slope(act, __bfloat162float(z[k]));
+                sum[k] += v;
+                g[k] = __float2bfloat16_rn(v);
+            }
+            if (dZ) *reinterpret_cast<uint4*>(dZ + r * ldz + c) = *reinterpret_cast<uint4*>(g);
+        }
+    }
+    if (!db_part) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sums[ty][lane * 8 + k] = sum[k];
+    __syncthreads();
+    const int64_t col = (int64_t)blockIdx.x * kDzCols + threadIdx.x;
+    if (col < cols) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < kDzRows; ++k) s += sums[k][threadIdx.x];
+        db_part[(int64_t)blockIdx.y * ldz + col] = s;
+    }
+}
+
+// db = the sum of the blocks' partial sums: 32 columns a block, eight threads a column, each
+// over a stretch of the partials in order.
+__global__ void __launch_bounds__(256)
+    db_kernel(const float* __restrict__ part, int n_part, int64_t cols, int64_t ldz,
+              __nv_bfloat16* __restrict__ db) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    __shared__ float sums[8][32];
+    const int lane = threadIdx.x % 32, ty = threadIdx.x / 32;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    const int per = (n_part + 7) / 8;
+    float s = 0.f;
+    if (c < cols)
+#pragma unroll 4
+        for (int k = ty * per; k < min(n_part, (ty + 1) * per); ++k) s += part[k * ldz + c];
+    sums[ty][lane] = s;
+    __syncthreads();
+    if (ty == 0 && c < cols) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) s += sums[k][lane];
+        db[c] = __float2bfloat16_rn(s);
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+struct Shape {
+    int64_t T, K, N;
+    int act;
+};
+
+flarepp_status check_shape(const flarepp_linear_shape* s, Shape* o) {
+    if (!s || s->rows < 0 || s->in < 1 || s->out < 1) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s->dtype != FLAREPP_F32 && s->dtype != FLAREPP_BF16) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s->act < FLAREPP_ACT_NONE || s->act > FLAREPP_ACT_SILU) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s->dtype != FLAREPP_BF16 || s->rows > 0x7fffffff || s->in > (1 << 20) || s->out > (1 << 20))
+        return FLAREPP_ERR_UNSUPPORTED;
+    *o = {s->rows, s->in, s->out, s->act};
+    return FLAREPP_OK;
+}
+
+size_t take(size_t* off, int64_t bytes) {
+    const size_t at = *off;
+    *off = align_up(at + (size_t)bytes, kWsAlign);
+    return at;
+}
+
+size_t part_bytes(const LinPlan& p, int64_t rows, int64_t cols) {
+    return (size_t)p.chunks * (size_t)rows * (size_t)(cdiv(cols, 4) * 4) * 4;
+}
+
+struct FwdLayout {
+    LinPlan plan;
+    bool split;  // the sums go through partials and finish_kernel
+    size_t off_x, off_w, off_part, total;
+};
+FwdLayout fwd_layout(const Shape& s) {
+    FwdLayout L{};
+    const bool few = s.T <= kFewRows;
+    L.plan = few ? lin_plan(s.N, s.T, s.K, true) : lin_plan(s.T, s.N, s.K, false);
+    L.split = few || L.plan.chunks > 1;
+    const bool pad = s.K % 8 != 0;
+    L.off_x = take(&L.total, pad ? s.T * pad8(s.K) * 2 : 0);
+    L.off_w = take(&L.total, pad ? s.N * pad8(s.K) * 2 : 0);
+    L.off_part = take(&L.total, L.split ? (int64_t)part_bytes(L.plan, s.T, s.N) : 0);
+    return L;
+}
+
+struct BwdLayout {
+    LinPlan plan_x, plan_w;
+    bool split_x, split_w;
+    bool own_dz;  // dZ is laid out in the workspace (else the products read dY)
+    int64_t dz_blocks, dz_rows;
+    size_t off_x, off_w, off_dz, off_db, off_px, off_pw, total;
+};
+BwdLayout bwd_layout(const Shape& s) {
+    BwdLayout L{};
+    const bool few = s.T <= kFewRows;
+    L.plan_x = few ? lin_plan(s.K, s.T, s.N, true) : lin_plan(s.T, s.K, s.N, false);
+    L.plan_w = lin_plan(s.N, s.K, s.T, false);
+    L.split_x = few || L.plan_x.chunks > 1;
+    L.split_w = L.plan_w.chunks > 1;
+    L.own_dz = s.act != FLAREPP_ACT_NONE || s.N % 8 != 0;
+    // about eight blocks of dz_kernel per SM, each of at least 32 rows
+    const int64_t col_blocks = cdiv(s.N, kDzCols);
+    int64_t want = cdiv(8 * kNumSMs, col_blocks);
+    if (want > cdiv(s.T, 32)) want = cdiv(s.T, 32);
+    L.dz_rows = cdiv(cdiv(s.T, want), kDzRows) * kDzRows;
+    L.dz_blocks = cdiv(s.T, L.dz_rows);
+    const bool pad = s.K % 8 != 0;
+    L.off_x = take(&L.total, pad ? s.T * pad8(s.K) * 2 : 0);
+    L.off_w = take(&L.total, pad ? s.N * pad8(s.K) * 2 : 0);
+    L.off_dz = take(&L.total, L.own_dz ? s.T * pad8(s.N) * 2 : 0);
+    L.off_db = take(&L.total, L.dz_blocks * pad8(s.N) * 4);
+    L.off_px = take(&L.total, L.split_x ? (int64_t)part_bytes(L.plan_x, s.T, s.K) : 0);
+    L.off_pw = take(&L.total, L.split_w ? (int64_t)part_bytes(L.plan_w, s.N, s.K) : 0);
+    return L;
+}
+
+cudaError_t pad(const void* src, int64_t rows, int64_t cols, void* dst, cudaStream_t st) {
+    const int64_t n = rows * pad8(cols) / 8;
+    const int64_t blocks = cdiv(n, 256) < 32 * kNumSMs ? cdiv(n, 256) : 32 * kNumSMs;
+    return launch_pdl(pad_kernel, dim3((unsigned)blocks), dim3(256), 0, st,
+                      (const __nv_bfloat16*)src, rows, cols, pad8(cols), (__nv_bfloat16*)dst);
+}
+
+cudaError_t finish(const float* part, const LinPlan& plan, int64_t rows, int64_t cols,
+                   const LinEpilogue& e, cudaStream_t st) {
+    const int64_t ldp = cdiv(cols, 4) * 4, n = rows * (ldp / 4);
+    return launch_pdl(finish_kernel, dim3((unsigned)cdiv(n, 128)), dim3(128), 0, st, part,
+                      plan.chunks, rows, cols, ldp, e.act, (const __nv_bfloat16*)e.bias,
+                      (const __nv_bfloat16*)e.R, (__nv_bfloat16*)e.Y, (__nv_bfloat16*)e.Z);
+}
+
+// out [rows][cols] = epilogue(sum_k a(row, k) b(col, k)), through partials where the plan cuts
+// the contraction or swaps the operands
+cudaError_t product(const LinPlan& plan, bool split, int64_t rows, int64_t cols, int64_t depth,
+                    const LinOperand& a, const LinOperand& b, const LinEpilogue& e, float* part,
+                    int* status, cudaStream_t st) {
+    if (!split) return lin_gemm(plan, rows, cols, depth, a, b, e, status, st);
+    LinEpilogue sums{};
+    sums.part = part;
+    sums.ldp = cdiv(cols, 4) * 4;
+    const cudaError_t err = plan.transposed
+                                ? lin_gemm(plan, cols, rows, depth, b, a, sums, status, st)
+                                : lin_gemm(plan, rows, cols, depth, a, b, sums, status, st);
+    return err != cudaSuccess ? err : finish(part, plan, rows, cols, e, st);
+}
+
+flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, const void* W,
+                          const void* b, const void* R, void* Y, void* Z, void* workspace,
+                          size_t workspace_bytes, int32_t* status, cudaStream_t st) {
+    Shape s;
+    const flarepp_status bad = check_shape(shape, &s);
+    if (bad != FLAREPP_OK) return bad;
+    if (s.T == 0) return FLAREPP_OK;
+    const void* all[6] = {X, W, Y, b, R, Z};
+    for (int i = 0; i < 6; ++i)
+        if ((i < 3 && !all[i]) || !aligned16(all[i])) return FLAREPP_ERR_INVALID_ARGUMENT;
+    const size_t y_bytes = (size_t)s.T * s.N * 2;
+    const FwdLayout L = fwd_layout(s);
+    if (L.total && (!workspace || (uintptr_t)workspace % kWsAlign || workspace_bytes < L.total))
+        return FLAREPP_ERR_WORKSPACE;
+    const Span outs[4] = {{Y, y_bytes}, {Z, y_bytes}, {workspace, L.total}, {status, 4}};
+    const Span ins[4] = {{X, (size_t)s.T * s.K * 2}, {W, (size_t)s.N * s.K * 2},
+                         {b, (size_t)s.N * 2}, {R, y_bytes}};
+    if (!disjoint(outs, 4, ins, 4)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    char* ws = (char*)workspace;
+    LinOperand x{X, s.K, 0}, w{W, s.K, 0};
+    if (s.K % 8) {
+        if (pad(X, s.T, s.K, ws + L.off_x, st) != cudaSuccess ||
+            pad(W, s.N, s.K, ws + L.off_w, st) != cudaSuccess)
+            return FLAREPP_ERR_CUDA;
+        x = {ws + L.off_x, pad8(s.K), 0};
+        w = {ws + L.off_w, pad8(s.K), 0};
+    }
+    const LinEpilogue e{s.act, b, R, Y, Z, nullptr, 0};
+    return product(L.plan, L.split, s.T, s.N, s.K, x, w, e, (float*)(ws + L.off_part), status,
+                   st) == cudaSuccess
+               ? FLAREPP_OK
+               : FLAREPP_ERR_CUDA;
+}
+
+flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, const void* W,
+                          const void* Z, const void* dY, void* dX, void* dW, void* db,
+                          void* workspace, size_t workspace_bytes, int32_t* status,
+                          cudaStream_t st) {
+    Shape s;
+    const flarepp_status bad = check_shape(shape, &s);
+    if (bad != FLAREPP_OK) return bad;
+    if (s.act == FLAREPP_ACT_NONE) Z = nullptr;
+    if (!dW) X = nullptr;
+    if (!dX) W = nullptr;
+    const void* all[7] = {X, W, Z, dY, dX, dW, db};
+    for (const void* p : all)
+        if (!aligned16(p)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    const size_t w_bytes = (size_t)s.N * s.K * 2, b_bytes = (size_t)s.N * 2;
+    const size_t x_bytes = (size_t)s.T * s.K * 2, y_bytes = (size_t)s.T * s.N * 2;
+    const BwdLayout L = s.T ? bwd_layout(s) : BwdLayout{};
+    if (s.T) {
+        if (!dY || (dW && !X) || (dX && !W) || (s.act != FLAREPP_ACT_NONE && !Z))
+            return FLAREPP_ERR_INVALID_ARGUMENT;
+        if (!workspace || (uintptr_t)workspace % kWsAlign || workspace_bytes < L.total)
+            return FLAREPP_ERR_WORKSPACE;
+    }
+    const Span outs[5] = {{dX, x_bytes}, {dW, w_bytes}, {db, b_bytes}, {workspace, L.total}, {status, 4}};
+    const Span ins[4] = {{X, x_bytes}, {W, w_bytes}, {Z, y_bytes}, {dY, y_bytes}};
+    if (!disjoint(outs, 5, ins, 4)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (s.T == 0) {
+        if ((dW && cudaMemsetAsync(dW, 0, w_bytes, st) != cudaSuccess) ||
+            (db && cudaMemsetAsync(db, 0, b_bytes, st) != cudaSuccess))
+            return FLAREPP_ERR_CUDA;
+        return FLAREPP_OK;
+    }
+    char* ws = (char*)workspace;
+    const int64_t ldz = pad8(s.N);
+    const bool own_dz = L.own_dz && (dX || dW);
+    cudaError_t e = cudaSuccess;
+    if (own_dz || db) {
+        const dim3 grid((unsigned)cdiv(s.N, kDzCols), (unsigned)L.dz_blocks);
+        auto kernel = s.N % 8 ? dz_kernel<false> : dz_kernel<true>;
+        e = launch_pdl(kernel, grid, dim3(256), 0, st, (const __nv_bfloat16*)dY,
+                       (const __nv_bfloat16*)Z, s.T, s.N, L.dz_rows, s.act, ldz,
+                       (__nv_bfloat16*)(own_dz ? ws + L.off_dz : nullptr),
+                       (float*)(db ? ws + L.off_db : nullptr));
+        if (e == cudaSuccess && db)
+            e = launch_pdl(db_kernel, dim3((unsigned)cdiv(s.N, 32)), dim3(256), 0, st,
+                           (const float*)(ws + L.off_db), (int)L.dz_blocks, s.N, ldz,
+                           (__nv_bfloat16*)db);
+    }
+    LinOperand x{X, s.K, 0}, w{W, s.K, 0};
+    if (s.K % 8) {
+        if (e == cudaSuccess && dW) e = pad(X, s.T, s.K, ws + L.off_x, st);
+        if (e == cudaSuccess && dX) e = pad(W, s.N, s.K, ws + L.off_w, st);
+        x = {ws + L.off_x, pad8(s.K), 0};
+        w = {ws + L.off_w, pad8(s.K), 0};
+    }
+    const LinOperand dz{own_dz ? ws + L.off_dz : dY, ldz, 0};
+    if (e == cudaSuccess && dX)
+        e = product(L.plan_x, L.split_x, s.T, s.K, s.N, dz, {w.t, w.pitch, 1},
+                    {FLAREPP_ACT_NONE, nullptr, nullptr, dX, nullptr, nullptr, 0},
+                    (float*)(ws + L.off_px), status, st);
+    if (e == cudaSuccess && dW)
+        e = product(L.plan_w, L.split_w, s.N, s.K, s.T, {dz.t, dz.pitch, 1}, {x.t, x.pitch, 1},
+                    {FLAREPP_ACT_NONE, nullptr, nullptr, dW, nullptr, nullptr, 0},
+                    (float*)(ws + L.off_pw), status, st);
+    return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace flarepp
+
+extern "C" {
+
+size_t flarepp_linear_workspace_bytes(const flarepp_linear_shape* shape) {
+    flarepp::Shape s;
+    if (flarepp::check_shape(shape, &s) != FLAREPP_OK || s.T == 0) return 0;
+    return flarepp::fwd_layout(s).total;
+}
+
+flarepp_status flarepp_linear_fwd(const flarepp_linear_shape* shape, const void* X, const void* W,
+                                  const void* b, const void* R, void* Y, void* Z,
+                                  void* workspace, size_t workspace_bytes, int32_t* status,
+                                  void* stream) {
+    return flarepp::linear_fwd(shape, X, W, b, R, Y, Z, workspace, workspace_bytes, status,
+                               (cudaStream_t)stream);
+}
+
+size_t flarepp_linear_bwd_workspace_bytes(const flarepp_linear_shape* shape) {
+    flarepp::Shape s;
+    if (flarepp::check_shape(shape, &s) != FLAREPP_OK || s.T == 0) return 0;
+    return flarepp::bwd_layout(s).total;
+}
+
+flarepp_status flarepp_linear_bwd(const flarepp_linear_shape* shape, const void* X, const void* W,
+                                  const void* Z, const void* dY, void* dX, void* dW, void* db,
+                                  void* workspace, size_t workspace_bytes, int32_t* status,
+                                  void* stream) {
+    return flarepp::linear_bwd(shape, X, W, Z, dY, dX, dW, db, workspace, workspace_bytes, status,
+                               (cudaStream_t)stream);
+}
+
+}  // extern "C"

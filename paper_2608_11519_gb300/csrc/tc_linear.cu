@@ -1,0 +1,676 @@
+// The tensor-core product of the linear layer (tcgen05 / TMEM / TMA, bf16 operands, float32 sums):
+//   D[m][n] = sum_k A(m, k) B(n, k)
+// with either operand stored contraction-innermost (K-major) or row-innermost (MN-major), which
+// covers the layer's three products without a transposed copy: Z = X W^T (both K-major),
+// dX = dZ W (W MN-major), dW = dZ^T X (both MN-major).
+//
+// Cut: a tile is 128 rows per CTA x NT <= 256 columns, the contraction runs in slices of 64 (a
+// 128-byte swizzled row). With CG = 2 a pair of CTAs shares a 256-row tile (cta_group::2): each CTA
+// loads its own 128 rows of A and half of the columns of B, so a slice costs 32 KB of
+// shared-memory fill per CTA instead of 48 KB and B crosses the L2 half as often. The walk over
+// tiles is persistent; chunks cut a long contraction when there are few tiles.
+//
+// Roles (12 warps): warp 0 the TMA producer, warp 1 the MMA issuer (in the pair's leader),
+// warps 4..11 two epilogue warpgroups (TMEM lane = tile row), which take the tile's 64-column blocks
+// in turn. Two TMEM accumulators of 256 columns let the epilogue of a tile overlap the products of
+// the next. Every wait is bounded (2 s of %globaltimer): on expiry the kernel records
+// FLAREPP_ERR_TIMEOUT in the status word, every role leaves its loops, the producer waits for its
+// copies in flight, the issuer for its products, and TMEM is freed.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <atomic>
+
+#include "linear_internal.h"
+#include "tc_ptx.cuh"
+
+namespace flarepp {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 384;
+constexpr int kFirstEpiWarp = 4;
+constexpr int kEpiWarps = 8;
+constexpr int kSlice = 64;  // contraction values per ring stage: one 128-byte row
+constexpr int kATile = 128 * kSlice * 2;
+constexpr int kMaxNT = 256;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint64_t kWaitLimitNs = 2000000000ull;
+constexpr int kMaxStages = 8;
+constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + kEpiWarps;
+
+enum Out { kOutEpilogue, kOutPart, kOutPartT };
+
+template <int CG, int OUT>
+struct Cfg {
+    static constexpr int kBTile = kMaxNT / CG * kSlice * 2;
+    static constexpr int kStage = kATile + kBTile;
+    // per epilogue warp: two 32-row x 64-column bf16 blocks
+    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * 2 * 4096 : 0;
+    static constexpr int kFit = (232448 - 1024 - kStaging - kNumBars * 8 - 16) / kStage;
+    static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
+    static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kNumBars * 8 + 16;
+};
+
+struct Gemm {
+    int M, N, NT;
+    int row_tiles, col_tiles, tiles, n_work;
+    int slices, chunk_slices;  // of the whole contraction, of a chunk
+    uint32_t idesc;
+    int act;
+    int tma_out;  // the output's pitch suits TMA
+    const __nv_bfloat16* bias;
+    const __nv_bfloat16* R;
+    __nv_bfloat16* Y;
+    __nv_bfloat16* Z;
+    float* part;
+    int64_t ldp;
+    int* status;
+};
+
+struct Work {
+    int rt, ct, chunk;
+};
+
+// Work item v: the tiles of a chunk in groups of 8 row tiles, columns outermost within a group, so
+// that the CTAs at work at one time share few rows of A and few columns of B in the L2.
+__device__ __forceinline__ Work work_of(const Gemm& p, int v) {
+    Work w;
+    w.chunk = v / p.tiles;
+    const int t = v - w.chunk * p.tiles;
+    const int per = 8 * p.col_tiles;
+    const int g = t / per, in = t - g * per;
+    const int rows = min(8, p.row_tiles - 8 * g);
+    w.ct = in / rows;
+    w.rt = 8 * g + in - w.ct * rows;
+    return w;
+}
+
+template <int CG>
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    return CG == 2 ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity);
+}
+
+// All lanes of a warp wait for a phase; false once this wait or another one of the CTA gave up.
+template <int CG>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                          int* status) {
+    bool got = try_wait<CG>(bar, parity);
+    if (!got) {
+        const uint64_t t0 = globaltimer_ns();
+        for (uint32_t i = 1;; ++i) {
+            got = try_wait<CG>(bar, parity);
+            if (got) break;
+            if ((i & 63u) == 0) {
+                if (*abort_flag) break;
+                if (globaltimer_ns() - t0 > kWaitLimitNs) {
+                    *abort_flag = 1;
+                    if (status) atomicExch(status, (int)FLAREPP_ERR_TIMEOUT);
+                    break;
+                }
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, got);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ float2 unpack_bf16(uint32_t v) {
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+
+// One operand's tile of `rows` rows for the slice at contraction index k: K-major as one box of
+// 64 x rows, MN-major as boxes of 64 rows x 64 contraction values ("atoms").
+template <int CG, bool MN>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* m, int row, int rows,
+                                          int k, uint32_t bar) {
+    if (!MN) {
+        if (CG == 2) tma_load_2d_pair(dst, m, k, row, bar);
+        else tma_load_2d(dst, m, k, row, bar);
+    } else {
+        for (int r = 0; r < rows; r += 64, dst += 64 * kSlice * 2) {
+            if (CG == 2) tma_load_2d_pair(dst, m, row + r, k, bar);
+            else tma_load_2d(dst, m, row + r, k, bar);
+        }
+    }
+}
+
+// The descriptor of the 16 contraction values at step s of a slice.
+template <bool MN>
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, int s) {
+    return MN ? smem_desc(addr + s * 16 * 128, 64 * kSlice * 2, 1024, kSw128)
+              : smem_desc(addr + s * 32, 16, 1024, kSw128);
+}
+
+template <int CG, bool A_MN, bool B_MN, int OUT>
+__global__ void __launch_bounds__(kThreads, 1)
+    lin_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                    const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmZ,
+                    const __grid_constant__ CUtensorMap tmR, const Gemm prm) {
+    using C = Cfg<CG, OUT>;
+    constexpr int kS = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    // the same offset in both CTAs of a pair: the dynamic shared memory starts at one address
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t* staging = smem + kS * C::kStage;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + C::kStaging);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const uint32_t full0 = smem_u32(bars);
+    const uint32_t empty0 = full0 + 8u * kMaxStages;
+    const uint32_t accfull0 = empty0 + 8u * kMaxStages;
+    const uint32_t accempty0 = accfull0 + 16u;
+    const uint32_t fin = accempty0 + 16u;
+    const uint32_t rfull0 = fin + 8u;  // one per epilogue warp
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int pair = (int)blockIdx.x / CG, pairs = (int)gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kS; ++s) {
+            mbar_init(full0 + 8u * s, 1);
+            mbar_init(empty0 + 8u * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(accfull0 + 8u * b, 1);
+            mbar_init(accempty0 + 8u * b, kEpiWarps * CG);
+        }
+        mbar_init(fin, 1);
+        for (int w = 0; w < kEpiWarps; ++w) mbar_init(rfull0 + 8u * w, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tmap(&tmA);
+        prefetch_tmap(&tmB);
+    }
+    if (warp == 1) {
+        if (CG == 2) {
+            tmem_alloc_pair(smem_u32(tmem_slot), kTmemCols);
+            tmem_relinquish_pair();
+        } else {
+            tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+            tmem_relinquish();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();  // the other CTA's barriers exist
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pdl_trigger();
+    pdl_wait();
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ TMA producer
+        uint32_t it = 0;
+        bool ok = true;
+        const int b_rows = prm.NT / CG;
+        // MN-major tiles come in whole 64-row atoms
+        const uint32_t b_bytes = (uint32_t)(B_MN ? (b_rows + 63) / 64 * 64 : b_rows) * kSlice * 2;
+        const uint32_t bytes = CG * (kATile + b_bytes);
+        for (int v = pair; v < prm.n_work && ok; v += pairs) {
+            const Work w = work_of(prm, v);
+            const int m0 = (w.rt * CG + (int)rank) * 128;
+            const int n0 = w.ct * prm.NT + (int)rank * b_rows;
+            const int s1 = min(prm.slices, (w.chunk + 1) * prm.chunk_slices);
+            for (int s = w.chunk * prm.chunk_slices; s < s1; ++s, ++it) {
+                const int st = it % kS;
+                if (it >= (uint32_t)kS &&
+                    !warp_wait<CG>(empty0 + 8u * st, (it / kS - 1) & 1, abort_flag, prm.status)) {
+                    ok = false;
+                    break;
+                }
+                if (elect_one()) {
+                    const uint32_t dst = smem_u32(smem + st * C::kStage);
+                    const uint32_t full = full0 + 8u * st;
+                    if (rank == 0) mbar_expect_tx(full, bytes);
+                    // both CTAs' bytes count on the leader's barrier
+                    const uint32_t bar = CG == 2 ? map_to_rank(full, 0) : full;
+                    load_tile<CG, A_MN>(dst, &tmA, m0, 128, s * kSlice, bar);
+                    load_tile<CG, B_MN>(dst + kATile, &tmB, n0, b_rows, s * kSlice, bar);
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok && rank == 0) {  // wait (bounded) until every copy issued has landed
+            const uint64_t t0 = globaltimer_ns();
+            for (int st = 0; st < kS && (uint32_t)st < it; ++st) {
+                const uint32_t x = it - 1 - ((it - 1 - st) % kS);
+                while (!mbar_try_wait(full0 + 8u * st, (x / kS) & 1) &&
+                       globaltimer_ns() - t0 < kWaitLimitNs) {
+                }
+            }
+        } else if (!ok) {  // its bytes count on the leader's barriers: give them a millisecond
+            const uint64_t t0 = globaltimer_ns();
+            while (globaltimer_ns() - t0 < 1000000ull) {
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------------------ MMA issuer
+        uint32_t it = 0, j = 0;
+        bool ok = true;
+        for (int v = pair; v < prm.n_work && ok; v += pairs, ++j) {
+            const Work w = work_of(prm, v);
+            const int ab = j & 1;
+            if (j >= 2 &&
+                !warp_wait<CG>(accempty0 + 8u * ab, ((j >> 1) - 1) & 1, abort_flag, prm.status)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const uint32_t acc = tmem + ab * kMaxNT;
+            const int s0 = w.chunk * prm.chunk_slices;
+            const int s1 = min(prm.slices, s0 + prm.chunk_slices);
+            for (int s = s0; s < s1; ++s, ++it) {
+                const int st = it % kS;
+                if (!warp_wait<CG>(full0 + 8u * st, (it / kS) & 1, abort_flag, prm.status)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t a = smem_u32(smem + st * C::kStage);
+                const uint32_t b = a + kATile;
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kSlice / 16; ++k) {
+                        const uint64_t ad = tile_desc<A_MN>(a, k), bd = tile_desc<B_MN>(b, k);
+                        const uint32_t more = (s > s0 || k > 0) ? 1u : 0u;
+                        if (CG == 2) mma_ss_pair(acc, ad, bd, prm.idesc, more);
+                        else mma_ss(acc, ad, bd, prm.idesc, more);
+                    }
+                    if (CG == 2) mma_commit_pair(empty0 + 8u * st);
+                    else mma_commit(empty0 + 8u * st);
+                }
+                __syncwarp();
+            }
+            if (!ok) break;
+            if (elect_one()) {
+                if (CG == 2) mma_commit_pair(accfull0 + 8u * ab);
+                else mma_commit(accfull0 + 8u * ab);
+            }
+            __syncwarp();
+        }
+        if (elect_one()) {
+            if (CG == 2) mma_commit_pair(fin);
+            else mma_commit(fin);
+        }
+        __syncwarp();
+        const uint64_t tw = globaltimer_ns();
+        while (!__all_sync(0xffffffffu, mbar_try_wait(fin, 0)) &&
+               globaltimer_ns() - tw < kWaitLimitNs) {
+        }
+    } else if (warp >= kFirstEpiWarp) {
+        // ------------------------------------------------------------ epilogue
+        const int e = warp - kFirstEpiWarp;
+        const int q = warp % 4;  // the TMEM lanes this warp may read
+        const uint32_t lane_off = (uint32_t)(32 * q) << 16;
+        uint8_t* stage = staging + e * 2 * 4096;
+        uint32_t j = 0, r_phase = 0;
+        int buf = 0;
+        bool r_pending = false;
+        for (int v = pair; v < prm.n_work; v += pairs, ++j) {
+            const Work w = work_of(prm, v);
+            const int ab = j & 1;
+            const int row0 = (w.rt * CG + (int)rank) * 128 + 32 * q;
+            bool waited = false, ok = true;
+            for (int c = 64 * (e / 4); c < prm.NT; c += 128) {
+                const int col0 = w.ct * prm.NT + c;
+                const bool live = row0 < prm.M && col0 < prm.N;
+                uint8_t* yb = stage + 4096 * buf;
+                if (OUT == kOutEpilogue && live && prm.R && prm.tma_out) {
+                    // the block of R comes into the buffer that Y leaves from
+                    if (lane == 0) {
+                        if (prm.Z) bulk_wait_read();
+                        else bulk_wait_read_1();
+                        mbar_expect_tx(rfull0 + 8u * e, 4096);
+                        tma_load_2d(smem_u32(yb), &tmR, col0, row0, rfull0 + 8u * e);
+                    }
+                    r_pending = true;
+                }
+                if (!waited) {
+                    ok = warp_wait<CG>(accfull0 + 8u * ab, (j >> 1) & 1, abort_flag, prm.status);
+                    waited = true;
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                if (!live) continue;
+                float x[64];
+                tmem_ld32(tmem + lane_off + ab * kMaxNT + c, reinterpret_cast<uint32_t*>(x));
+                tmem_ld32(tmem + lane_off + ab * kMaxNT + c + 32, reinterpret_cast<uint32_t*>(x + 32));
+                tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
+                tmem_wait_ld32(reinterpret_cast<uint32_t*>(x + 32));
+                const int row = row0 + lane;
+                if (OUT == kOutPart) {
+                    if (row < prm.M) {
+                        float* d = prm.part + ((int64_t)w.chunk * prm.M + row) * prm.ldp + col0;
+                        const int n = min(64, min(prm.NT - c, (int)prm.ldp - col0));
+#pragma unroll
+                        for (int i = 0; i < 64; i += 4)
+                            if (i < n)
+                                *reinterpret_cast<float4*>(d + i) =
+                                    make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                    }
+                    continue;
+                }
+                if (OUT == kOutPartT) {
+                    if (row < prm.M) {
+                        float* d = prm.part + ((int64_t)w.chunk * prm.N + col0) * prm.ldp + row;
+                        const int n = min(64, min(prm.NT - c, prm.N - col0));
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            if (i < n) d[i * prm.ldp] = x[i];
+                    }
+                    continue;
+                }
+                if (prm.bias) {
+                    if (col0 + 64 <= prm.N) {
+                        const uint4* b4 = reinterpret_cast<const uint4*>(prm.bias + col0);
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) {
+                            const uint4 u = __ldg(b4 + g);
+                            const uint32_t p[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float2 f = unpack_bf16(p[i]);
+                                x[8 * g + 2 * i] += f.x;
+                                x[8 * g + 2 * i + 1] += f.y;
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            if (col0 + i < prm.N) x[i] += __bfloat162float(prm.bias[col0 + i]);
+                    }
+                }
+                // The block goes through shared memory swizzled as the store map undoes it: 16-byte
+                // piece g of row r at g ^ (r % 8), free of bank conflicts.
+                const uint32_t line = lane * 128;
+                if (prm.Z) {
+                    uint8_t* zb = stage + 4096 * (buf ^ 1);
+                    if (lane == 0 && !(prm.R && prm.tma_out)) bulk_wait_read();
+                    __syncwarp();
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        uint4 u;
+                        u.x = pack_bf16(x[8 * g], x[8 * g + 1]);
+                        u.y = pack_bf16(x[8 * g + 2], x[8 * g + 3]);
+                        u.z = pack_bf16(x[8 * g + 4], x[8 * g + 5]);
+                        u.w = pack_bf16(x[8 * g + 6], x[8 * g + 7]);
+                        *reinterpret_cast<uint4*>(zb + line + ((g ^ (lane & 7)) << 4)) = u;
+                    }
+                    if (prm.tma_out) {
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&tmZ, smem_u32(zb), col0, row0);
+                            bulk_commit();
+                        }
+                    } else {
+                        __syncwarp();
+                        for (int i = lane; i < 32 * 64; i += 32) {
+                            const int r = i >> 6, cc = i & 63;
+                            if (row0 + r < prm.M && col0 + cc < prm.N && c + cc < prm.NT)
+                                prm.Z[(int64_t)(row0 + r) * prm.N + col0 + cc] =
+                                    *reinterpret_cast<__nv_bfloat16*>(
+                                        zb + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2);
+                        }
+                    }
+                }
+                switch (prm.act) {
+                    case FLAREPP_ACT_RELU:
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) x[i] = act_value(FLAREPP_ACT_RELU, x[i]);
+                        break;
+                    case FLAREPP_ACT_GELU:
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) x[i] = act_value(FLAREPP_ACT_GELU, x[i]);
+                        break;
+                    case FLAREPP_ACT_SILU:
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) x[i] = act_value(FLAREPP_ACT_SILU, x[i]);
+                        break;
+                }
+                if (prm.R) {
+                    if (prm.tma_out) {
+                        ok = warp_wait<1>(rfull0 + 8u * e, r_phase, abort_flag, prm.status);
+                        if (!ok) break;
+                        r_phase ^= 1;
+                        r_pending = false;
+                    } else {
+                        __syncwarp();
+                        for (int i = lane; i < 32 * 64; i += 32) {
+                            const int r = i >> 6, cc = i & 63;
+                            if (row0 + r < prm.M && col0 + cc < prm.N)
+                                *reinterpret_cast<__nv_bfloat16*>(
+                                    yb + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2) =
+                                    prm.R[(int64_t)(row0 + r) * prm.N + col0 + cc];
+                        }
+                        __syncwarp();
+                    }
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(yb + line + ((g ^ (lane & 7)) << 4));
+                        const uint32_t p[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 f = unpack_bf16(p[i]);
+                            x[8 * g + 2 * i] += f.x;
+                            x[8 * g + 2 * i + 1] += f.y;
+                        }
+                    }
+                } else if (!prm.Z) {
+                    if (lane == 0) bulk_wait_read_1();
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    uint4 u;
+                    u.x = pack_bf16(x[8 * g], x[8 * g + 1]);
+                    u.y = pack_bf16(x[8 * g + 2], x[8 * g + 3]);
+                    u.z = pack_bf16(x[8 * g + 4], x[8 * g + 5]);
+                    u.w = pack_bf16(x[8 * g + 6], x[8 * g + 7]);
+                    *reinterpret_cast<uint4*>(yb + line + ((g ^ (lane & 7)) << 4)) = u;
+                }
+                if (prm.tma_out) {
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&tmY, smem_u32(yb), col0, row0);
+                        bulk_commit();
+                    }
+                    if (!prm.Z) buf ^= 1;
+                } else {
+                    __syncwarp();
+                    for (int i = lane; i < 32 * 64; i += 32) {
+                        const int r = i >> 6, cc = i & 63;
+                        if (row0 + r < prm.M && col0 + cc < prm.N && c + cc < prm.NT)
+                            prm.Y[(int64_t)(row0 + r) * prm.N + col0 + cc] =
+                                *reinterpret_cast<__nv_bfloat16*>(
+                                    yb + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!waited)
+                ok = warp_wait<CG>(accfull0 + 8u * ab, (j >> 1) & 1, abort_flag, prm.status);
+            if (!ok) break;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {  // this warp has read its part of the accumulator
+                if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
+                else mbar_arrive(accempty0 + 8u * ab);
+            }
+        }
+        if (OUT == kOutEpilogue) {
+            if (r_pending) {  // only after a wait that gave up: let the copy in flight land
+                const uint64_t t0 = globaltimer_ns();
+                while (!mbar_try_wait(rfull0 + 8u * e, r_phase) &&
+                       globaltimer_ns() - t0 < kWaitLimitNs) {
+                }
+            }
+            if (lane == 0) bulk_wait_all();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    // no CTA leaves while the other one may still signal it or read its shared memory
+    if (CG == 2) cluster_sync();
+    tc_fence_after();
+    if (warp == 1) {
+        if (CG == 2) tmem_dealloc_pair(tmem, kTmemCols);
+        else tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> fn{nullptr};
+    PFN_cuTensorMapEncodeTiled_v12000 f = fn.load(std::memory_order_acquire);
+    if (f) return f;
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+        fn.store(f = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p),
+                 std::memory_order_release);
+    return f;
+}
+
+// bf16 [lines][inner] with `pitch` elements from line to line, boxes of box_inner x box_lines
+bool make_map(CUtensorMap* m, const void* base, int64_t inner, int64_t lines, int64_t pitch,
+              int box_inner, int box_lines) {
+    auto fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)lines};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch * 2};
+    cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_lines};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int CG, bool A_MN, bool B_MN, int OUT>
+cudaError_t launch(const CUtensorMap* m, const Gemm& p, cudaStream_t st) {
+    using C = Cfg<CG, OUT>;
+    static_assert(C::kSmem <= 232448 && C::kStages >= 3, "shared memory budget");
+    auto kernel = lin_gemm_kernel<CG, A_MN, B_MN, OUT>;
+    static std::atomic<int> fits[64];  // tiles that run at once on each device (0: not asked yet)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG == 2 ? 2 : 1;
+    int n = fits[dev].load();
+    if (n == 0) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+        if (e != cudaSuccess) return e;
+        n = kNumSMs / CG;
+        if (CG == 2) {  // a die's odd SM cannot hold a pair
+            cfg.gridDim = dim3((unsigned)(kNumSMs / CG * CG));
+            int most = 0;
+            cudaLaunchConfig_t ask = cfg;
+            ask.attrs = &attr[1];
+            ask.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&most, kernel, &ask);
+            if (e != cudaSuccess) return e;
+            if (most > 0 && most < n) n = most;
+        }
+        fits[dev].store(n);
+    }
+    cfg.gridDim = dim3((unsigned)((p.n_work < n ? p.n_work : n) * CG));
+    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], m[4], p);
+}
+
+}  // namespace
+
+LinPlan lin_plan(int64_t M, int64_t N, int64_t K, bool few_columns) {
+    LinPlan p{};
+    p.transposed = few_columns;
+    p.cg = few_columns ? 1 : 2;
+    // equal column tiles, in whole 64-column blocks where there are several
+    const int64_t ct = cdiv(N, kMaxNT);
+    p.NT = (int)(ct == 1 ? cdiv(N, 16) * 16 : cdiv(cdiv(N, ct), 64) * 64);
+    const int64_t tiles = cdiv(M, 128 * p.cg) * cdiv(N, p.NT);
+    const int64_t slices = cdiv(K, kSlice), units = kNumSMs / p.cg;
+    // fill the SMs once, with at least four slices a chunk
+    int64_t want = tiles >= units ? 1 : units / tiles;
+    if (want > slices / 4) want = slices / 4;
+    if (want < 1) want = 1;
+    const int64_t per = cdiv(slices, want);
+    p.chunks = (int)cdiv(slices, per);
+    return p;
+}
+
+cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const LinOperand& a,
+                     const LinOperand& b, const LinEpilogue& e, int* status, cudaStream_t st) {
+    Gemm p{};
+    p.M = (int)M;
+    p.N = (int)N;
+    p.NT = plan.NT;
+    const int64_t row_tiles = cdiv(M, 128 * plan.cg), col_tiles = cdiv(N, plan.NT);
+    if (row_tiles * col_tiles * plan.chunks > 0x7fffffff) return cudaErrorInvalidValue;
+    p.row_tiles = (int)row_tiles;
+    p.col_tiles = (int)col_tiles;
+    p.tiles = (int)(row_tiles * col_tiles);
+    p.n_work = p.tiles * plan.chunks;
+    p.slices = (int)cdiv(K, kSlice);
+    p.chunk_slices = (int)cdiv(p.slices, plan.chunks);
+    p.idesc = idesc_bf16_f32(128 * plan.cg, plan.NT, a.mn, b.mn);
+    p.act = e.act;
+    p.tma_out = N % 8 == 0;
+    p.bias = (const __nv_bfloat16*)e.bias;
+    p.R = (const __nv_bfloat16*)e.R;
+    p.Y = (__nv_bfloat16*)e.Y;
+    p.Z = (__nv_bfloat16*)e.Z;
+    p.part = e.part;
+    p.ldp = e.ldp;
+    p.status = status;
+    CUtensorMap m[5];
+    const int b_rows = plan.NT / plan.cg;
+    bool ok = a.mn ? make_map(&m[0], a.t, M, K, a.pitch, 64, kSlice)
+                   : make_map(&m[0], a.t, K, M, a.pitch, kSlice, 128);
+    ok = ok && (b.mn ? make_map(&m[1], b.t, N, K, b.pitch, 64, kSlice)
+                     : make_map(&m[1], b.t, K, N, b.pitch, kSlice, b_rows));
+    m[2] = m[3] = m[4] = m[0];  // unused unless set below
+    if (!e.part && p.tma_out) {
+        ok = ok && make_map(&m[2], e.Y, N, M, N, 64, 32);
+        if (e.Z) ok = ok && make_map(&m[3], e.Z, N, M, N, 64, 32);
+        if (e.R) ok = ok && make_map(&m[4], e.R, N, M, N, 64, 32);
+    }
+    if (!ok) return cudaErrorInvalidValue;
+    const int out = !e.part ? kOutEpilogue : plan.transposed ? kOutPartT : kOutPart;
+    if (plan.cg == 1) {
+        if (out != kOutPartT) return cudaErrorInvalidValue;
+        return a.mn ? launch<1, true, false, kOutPartT>(m, p, st)
+                    : launch<1, false, false, kOutPartT>(m, p, st);
+    }
+    if (a.mn)
+        return out == kOutPart ? launch<2, true, true, kOutPart>(m, p, st)
+                               : launch<2, true, true, kOutEpilogue>(m, p, st);
+    if (b.mn)
+        return out == kOutPart ? launch<2, false, true, kOutPart>(m, p, st)
+                               : launch<2, false, true, kOutEpilogue>(m, p, st);
+    return out == kOutPart ? launch<2, false, false, kOutPart>(m, p, st)
+                           : launch<2, false, false, kOutEpilogue>(m, p, st);
+}
+
+}  // namespace flarepp

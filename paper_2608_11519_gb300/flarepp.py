@@ -32,7 +32,11 @@ EXPORTED = ("flarepp_route_workspace_bytes", "flarepp_route_fwd", "flarepp_route
             "flarepp_mixer_bwd_workspace_bytes", "flarepp_mixer_bwd",
             "flarepp_route_saved_bytes", "flarepp_route_fwd_train",
             "flarepp_route_bwd_workspace_bytes", "flarepp_route_bwd",
-            "flarepp_route_device_status", "flarepp_status_string", "flarepp_version")
+            "flarepp_route_device_status", "flarepp_status_string", "flarepp_version",
+            "flarepp_linear_workspace_bytes", "flarepp_linear_fwd",
+            "flarepp_linear_bwd_workspace_bytes", "flarepp_linear_bwd",
+            "flarepp_embedding_fwd", "flarepp_embedding_bwd_workspace_bytes",
+            "flarepp_embedding_bwd", "flarepp_adamw_step", "flarepp_adamw_moments")
 N_STAGE_EVENTS = 6
 STAGES = ("encode1", "combine1", "encode2", "combine2", "decode")
 
@@ -41,6 +45,34 @@ class Shape(ctypes.Structure):
     """Mirror of ``flarepp_shape`` in include/flarepp.h."""
     _fields_ = [("B", ctypes.c_int64), ("H", ctypes.c_int64), ("N", ctypes.c_int64),
                 ("M", ctypes.c_int64), ("D", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class LinearShape(ctypes.Structure):
+    """Mirror of ``flarepp_linear_shape`` in include/flarepp.h."""
+    _fields_ = [("rows", ctypes.c_int64), ("in_", ctypes.c_int64), ("out", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
+class EmbeddingShape(ctypes.Structure):
+    """Mirror of ``flarepp_embedding_shape`` in include/flarepp.h."""
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int64), ("C", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("id_bytes", ctypes.c_int32)]
+
+
+class AdamwTensor(ctypes.Structure):
+    """Mirror of ``flarepp_adamw_tensor`` in include/flarepp.h."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("master", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("param_dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32)]
+
+
+class AdamwHyper(ctypes.Structure):
+    """Mirror of ``flarepp_adamw_hyper`` in include/flarepp.h."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("step", ctypes.c_int64), ("state_bits", ctypes.c_int32)]
 
 
 class FlareppError(RuntimeError):
@@ -121,6 +153,22 @@ def load(path: str = None):
                                       vp, vp, vp, vp, vp, vp, sz, vp]
     lib.flarepp_route_device_status.restype = ctypes.c_int
     lib.flarepp_route_device_status.argtypes = [sp, vp, vp, ctypes.POINTER(ctypes.c_int32)]
+    lp, ep = ctypes.POINTER(LinearShape), ctypes.POINTER(EmbeddingShape)
+    tp, hp = ctypes.POINTER(AdamwTensor), ctypes.POINTER(AdamwHyper)
+    for name, args in (
+            ("linear_workspace_bytes", [lp]), ("linear_bwd_workspace_bytes", [lp]),
+            ("embedding_bwd_workspace_bytes", [ep])):
+        getattr(lib, "flarepp_" + name).restype = sz
+        getattr(lib, "flarepp_" + name).argtypes = args
+    for name, args in (
+            ("linear_fwd", [lp] + [vp] * 7 + [sz, vp, vp]),
+            ("linear_bwd", [lp] + [vp] * 8 + [sz, vp, vp]),
+            ("embedding_fwd", [ep, vp, vp, ctypes.c_float, vp, vp, vp]),
+            ("embedding_bwd", [ep, vp, vp, ctypes.c_float, vp, vp, sz, vp, vp]),
+            ("adamw_step", [tp, ctypes.c_int64, hp, vp]),
+            ("adamw_moments", [tp, ctypes.c_int64, vp, vp, vp])):
+        getattr(lib, "flarepp_" + name).restype = ctypes.c_int
+        getattr(lib, "flarepp_" + name).argtypes = args
     lib.flarepp_status_string.restype = ctypes.c_char_p
     lib.flarepp_status_string.argtypes = [ctypes.c_int]
     lib.flarepp_version.restype = ctypes.c_char_p
@@ -664,3 +712,310 @@ def flare_fwd_host(Q, K, V, scale=None, Y_host=None, device="cuda", workspace=No
         raise FlareppError(rc, "flarepp_flare_fwd_host")
     st.synchronize()
     return Y_host
+
+
+# ---------------------------------------------------------------- layers around the mixer
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+STATE_BLOCK = 256  # values that share one scale in an 8-bit optimiser state
+
+
+def _need(t, what, shape, dtype, device, optional=False):
+    """A contiguous tensor of this shape, dtype and CUDA device; returns its address (0 for an
+    optional one that is missing)."""
+    if t is None and optional:
+        return 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, expected {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+def _cuda_device(t, what):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a torch tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{what} must be a device tensor")
+    return t.device
+
+
+def _enqueue(name, device, stream, *args):
+    """Call entry ``flarepp_<name>`` with the device current, the stream as last argument."""
+    fn = getattr(load(), "flarepp_" + name)
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, handle)
+    if rc != OK:
+        raise FlareppError(rc, "flarepp_" + name)
+
+
+def _scratch(workspace, nbytes, device):
+    """(tensor to keep until the call is enqueued, its address, its bytes)"""
+    if isinstance(workspace, Workspace):
+        buf = workspace.get(nbytes, device)
+    elif workspace is None:
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    else:
+        _check_device("the call", device, workspace=workspace)
+        buf = workspace
+    return buf, 0 if buf is None else buf.data_ptr(), _nbytes(buf)
+
+
+def _status_word(status, device):
+    return _need(status, "status", (1,), torch.int32, device, optional=True)
+
+
+def _linear_shape(X, W, act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {tuple(ACTIVATIONS)}")
+    if not isinstance(X, torch.Tensor) or not isinstance(W, torch.Tensor):
+        raise TypeError("X and W must be torch tensors")
+    if X.dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {X.dtype}; the linear layer takes bfloat16")
+    if W.dim() != 2 or X.dim() < 1 or X.shape[-1] != W.shape[1]:
+        raise ValueError(f"expected X [..., in] and W [out, in], got {tuple(X.shape)} and "
+                         f"{tuple(W.shape)}")
+    out, in_ = W.shape
+    rows = X.numel() // in_ if in_ else 0
+    return LinearShape(rows, in_, out, _DTYPES[X.dtype], ACTIVATIONS[act])
+
+
+def _linear(X, W, b, residual, act, Y, Z, keep, workspace, status, stream):
+    dev = _cuda_device(X, "X")
+    s = _linear_shape(X, W, act)
+    dt, shape = X.dtype, (*X.shape[:-1], s.out)
+    xp, wp = _need(X, "X", X.shape, dt, dev), _need(W, "W", W.shape, dt, dev)
+    bp = _need(b, "b", (s.out,), dt, dev, optional=True)
+    rp = _need(residual, "residual", shape, dt, dev, optional=True)
+    if Y is None:
+        Y = torch.empty(shape, dtype=dt, device=dev)
+    if keep and Z is None:
+        Z = torch.empty(shape, dtype=dt, device=dev)
+    yp = _need(Y, "Y", shape, dt, dev)
+    zp = _need(Z, "Z", shape, dt, dev, optional=True)
+    ref = ctypes.byref(s)
+    buf, wsp, wsn = _scratch(workspace, load().flarepp_linear_workspace_bytes(ref), dev)
+    _enqueue("linear_fwd", dev, stream, ref, xp, wp, bp, rp, yp, zp, wsp, wsn,
+             _status_word(status, dev))
+    return Y, Z
+
+
+def linear_fwd(X, W, b=None, residual=None, act="none", Y=None, workspace=None, status=None,
+               stream=None):
+    """Y = act(X W^T + b) + residual [..., out] for X [..., in], W [out, in], b [out], in bf16;
+    ``act`` one of ``ACTIVATIONS``. ``status``: a device int32 [1] that a timeout sets."""
+    return _linear(X, W, b, residual, act, Y, None, False, workspace, status, stream)[0]
+
+
+def linear_fwd_train(X, W, b=None, residual=None, act="none", Y=None, Z=None, workspace=None,
+                     status=None, stream=None):
+    """``linear_fwd`` that also returns Z = X W^T + b, which ``linear_bwd`` takes (None for
+    ``act="none"``, whose backward does not need it)."""
+    if act == "none" and Z is not None:
+        raise ValueError("act='none' keeps no Z")
+    return _linear(X, W, b, residual, act, Y, Z, act != "none", workspace, status, stream)
+
+
+def linear_bwd(X, W, dY, Z=None, act="none", bias=True, dX=None, dW=None, db=None,
+               need=(True, True), workspace=None, status=None, stream=None):
+    """(dX, dW, db), the gradients of ``linear_fwd_train`` for the output gradient dY [..., out]
+    (the residual's gradient is dY). ``bias=False`` leaves db out, ``need`` dX or dW; what is left
+    out is returned as None."""
+    dev = _cuda_device(X, "X")
+    s = _linear_shape(X, W, act)
+    dt, shape = X.dtype, (*X.shape[:-1], s.out)
+    xp, wp = _need(X, "X", X.shape, dt, dev), _need(W, "W", W.shape, dt, dev)
+    gp = _need(dY, "dY", shape, dt, dev)
+    zp = _need(Z, "Z", shape, dt, dev, optional=act == "none")
+    if need[0] and dX is None:
+        dX = torch.empty_like(X)
+    if need[1] and dW is None:
+        dW = torch.empty_like(W)
+    if bias and db is None:
+        db = torch.empty(s.out, dtype=dt, device=dev)
+    dX, dW, db = dX if need[0] else None, dW if need[1] else None, db if bias else None
+    dxp = _need(dX, "dX", X.shape, dt, dev, optional=True)
+    dwp = _need(dW, "dW", W.shape, dt, dev, optional=True)
+    dbp = _need(db, "db", (s.out,), dt, dev, optional=True)
+    ref = ctypes.byref(s)
+    buf, wsp, wsn = _scratch(workspace, load().flarepp_linear_bwd_workspace_bytes(ref), dev)
+    _enqueue("linear_bwd", dev, stream, ref, xp, wp, zp, gp, dxp, dwp, dbp, wsp, wsn,
+             _status_word(status, dev))
+    return dX, dW, db
+
+
+def _ids_of(ids):
+    dev = _cuda_device(ids, "ids")
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"ids have dtype {ids.dtype}, expected int32 or int64")
+    return dev, _need(ids, "ids", ids.shape, ids.dtype, dev), ids.element_size()
+
+
+def _float_dtype(t, what):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a torch tensor")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {t.dtype}; use float32 or bfloat16")
+    return t.dtype
+
+
+def embedding_fwd(ids, table, scale=1.0, Y=None, status=None, stream=None):
+    """Y [..., C] = scale * table[ids] for ids [...] (int32 or int64) and table [V, C] (float32 or
+    bf16). A negative id gives a row of zeros; one of V or more too, and sets ``status`` (a device
+    int32 [1]) to ERR_INVALID_ARGUMENT."""
+    dev, ip, size = _ids_of(ids)
+    dt = _float_dtype(table, "table")
+    if table.dim() != 2:
+        raise ValueError("expected table [V, C]")
+    V, C = table.shape
+    tp = _need(table, "table", (V, C), dt, dev)
+    if Y is None:
+        Y = torch.empty((*ids.shape, C), dtype=dt, device=dev)
+    s = EmbeddingShape(ids.numel(), V, C, _DTYPES[dt], size)
+    _enqueue("embedding_fwd", dev, stream, ctypes.byref(s), ip, tp, float(scale),
+             _need(Y, "Y", (*ids.shape, C), dt, dev), _status_word(status, dev))
+    return Y
+
+
+def embedding_bwd(ids, dY, V, scale=1.0, dtable=None, workspace=None, status=None, stream=None):
+    """dtable [V, C], the gradient of ``embedding_fwd``'s table for dY [..., C]: the rows of dY
+    summed by id in a fixed order, times ``scale``; rows that no id names are 0."""
+    dev, ip, size = _ids_of(ids)
+    dt = _float_dtype(dY, "dY")
+    if dY.dim() != ids.dim() + 1:
+        raise ValueError("expected dY of the ids' shape and one more dimension")
+    C = dY.shape[-1]
+    gp = _need(dY, "dY", (*ids.shape, C), dt, dev)
+    if dtable is None:
+        dtable = torch.empty((V, C), dtype=dt, device=dev)
+    s = EmbeddingShape(ids.numel(), V, C, _DTYPES[dt], size)
+    ref = ctypes.byref(s)
+    buf, wsp, wsn = _scratch(workspace, load().flarepp_embedding_bwd_workspace_bytes(ref), dev)
+    _enqueue("embedding_bwd", dev, stream, ref, ip, gp, float(scale),
+             _need(dtable, "dtable", (V, C), dt, dev), wsp, wsn, _status_word(status, dev))
+    return dtable
+
+
+class AdamW:
+    """AdamW over fixed buffers: parameters, their gradients, and the state it keeps.
+
+        opt = flarepp.AdamW(params, grads, lr=1e-3, state_bits=8, masters=True)
+        ...                      # a step's gradients are written into ``grads``
+        opt.step()
+
+    params, grads: lists of contiguous CUDA tensors of the same shapes, float32 or bf16 each.
+    masters: True makes a float32 master of every bf16 parameter (whose rounded copy it then is), a
+    list gives them (None where there is none). state_bits: 32, or 8 (the moments in 8 bits with
+    a scale for every ``STATE_BLOCK`` values: a quarter of the memory; include/flarepp.h says how).
+    state: the state to go on from, as ``state_dict`` returns it (its tensors are used, not
+    copied). The optimiser works on the buffers that it was given, whose storage it keeps alive:
+    a parameter or gradient that moves to another buffer needs a new optimiser (give it
+    ``state_dict()``). ``lr`` and ``weight_decay`` are attributes that a schedule may change."""
+
+    def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2,
+                 state_bits=32, masters=None, state=None):
+        params, grads = [p.detach() for p in params], [g.detach() for g in grads]
+        if len(params) != len(grads):
+            raise ValueError(f"{len(params)} parameters, {len(grads)} gradients")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self.lr, self.betas, self.eps = lr, betas, eps
+        self.weight_decay, self.state_bits = weight_decay, state_bits
+        self.params, self.grads = params, grads
+        self.device = _cuda_device(params[0], "params[0]") if params else None
+        if masters is True:
+            masters = [p.float() if p.dtype == torch.bfloat16 else None for p in params]
+        def own(ts):  # aliases, which keep the storage whatever becomes of the caller's tensors
+            return [None if t is None else t.detach() for t in ts or [None] * len(params)]
+
+        self.masters = own(masters)
+        made = self._zero_state() if state is None else state
+        self.m, self.v = own(made["m"]), own(made["v"])
+        self.m_scale, self.v_scale = own(made.get("m_scale")), own(made.get("v_scale"))
+        self.steps = int(made.get("step", 0))
+        self._table = (AdamwTensor * max(1, len(params)))()
+        lists = (grads, self.masters, self.m, self.v, self.m_scale, self.v_scale)
+        if any(len(x) != len(params) for x in lists):
+            raise ValueError("the lists of tensors differ in length")
+        for i, p in enumerate(params):
+            self._fill(i, p)
+
+    def _zero_state(self):
+        def zeros(n, dtype):
+            return torch.zeros(n, dtype=dtype, device=self.device)
+        if self.state_bits == 32:
+            return {k: [zeros(p.shape, torch.float32) for p in self.params] for k in "mv"}
+        ns = [p.numel() for p in self.params]
+        blocks = [-(-n // STATE_BLOCK) for n in ns]
+        return {"m": [zeros(n, torch.float8_e4m3fn) for n in ns],
+                "v": [zeros(n, torch.uint8) for n in ns],
+                "m_scale": [zeros(b, torch.float32) for b in blocks],
+                "v_scale": [zeros(b, torch.float32) for b in blocks]}
+
+    def _fill(self, i, p):
+        dev, f32, e = self.device, torch.float32, self._table[i]
+        dt = _float_dtype(p, f"params[{i}]")
+        g = self.grads[i]
+        n = p.numel()
+        e.param = _need(p, f"params[{i}]", p.shape, dt, dev)
+        e.grad = _need(g, f"grads[{i}]", p.shape, _float_dtype(g, f"grads[{i}]"), dev)
+        e.master = _need(self.masters[i], f"masters[{i}]", p.shape, f32, dev, optional=True)
+        e.n, e.param_dtype, e.grad_dtype = n, _DTYPES[dt], _DTYPES[g.dtype]
+        if self.state_bits == 32:
+            for k in ("m", "v"):
+                t = getattr(self, k)[i]
+                setattr(e, k, _need(t.view(p.shape), f"{k}[{i}]", p.shape, f32, dev))
+            return
+        blocks = -(-n // STATE_BLOCK)
+        e.m = _need(self.m[i].view(-1), f"m[{i}]", (n,), torch.float8_e4m3fn, dev)
+        e.v = _need(self.v[i].view(-1), f"v[{i}]", (n,), torch.uint8, dev)
+        e.m_scale = _need(self.m_scale[i], f"m_scale[{i}]", (blocks,), f32, dev)
+        e.v_scale = _need(self.v_scale[i], f"v_scale[{i}]", (blocks,), f32, dev)
+
+    def step(self, stream=None):
+        """One step from what the gradients hold now."""
+        if not self.params:
+            return
+        h = AdamwHyper(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
+                       self.steps + 1, self.state_bits)
+        _enqueue("adamw_step", self.device, stream, self._table, len(self.params),
+                 ctypes.byref(h))
+        self.steps += 1
+
+    def moments(self, m_out=None, v_out=None, stream=None):
+        """The moments as lists of float32 tensors: the state itself with 32 bits, the values that
+        it stands for with 8 (written into m_out and v_out where they are given)."""
+        if self.state_bits == 32:
+            if m_out is not None or v_out is not None:
+                raise ValueError("32-bit moments are the state itself: m_out and v_out are not used")
+            return self.m, self.v
+        outs = []
+        for given, name in ((m_out, "m_out"), (v_out, "v_out")):
+            if given is None:
+                given = [torch.empty(p.shape, device=self.device) for p in self.params]
+            if len(given) != len(self.params):
+                raise ValueError(f"{name} has {len(given)} tensors, expected {len(self.params)}")
+            ptrs = (ctypes.c_void_p * max(1, len(given)))()
+            for i, (t, p) in enumerate(zip(given, self.params)):
+                ptrs[i] = _need(t, f"{name}[{i}]", p.shape, torch.float32, self.device)
+            outs.append((given, ptrs))
+        if self.params:
+            _enqueue("adamw_moments", self.device, stream, self._table, len(self.params),
+                     outs[0][1], outs[1][1])
+        return outs[0][0], outs[1][0]
+
+    def state_dict(self):
+        """The state to save and to go on from; its tensors are the optimiser's own."""
+        return {"m": self.m, "v": self.v, "m_scale": self.m_scale, "v_scale": self.v_scale,
+                "step": self.steps}
