@@ -35,39 +35,73 @@ __global__ void pad_kernel(const __nv_bfloat16* __restrict__ src, int64_t rows, 
     }
 }
 
-// What follows the float32 sums of a cut contraction: the chunks added in order, then the
-// epilogue (bias, activation, residual). One thread per four columns.
-__global__ void finish_kernel(const float* __restrict__ part, int chunks, int64_t rows,
+// What follows the float32 sums of a cut contraction: the chunks added in order (with SPLIT > 1 as
+// SPLIT stretches of chunks, the stretches in order after that: many chunks would otherwise be one
+// long chain of loads), then the epilogue (bias, activation, residual). SPLIT threads per four
+// columns.
+constexpr int kFinishThreads = 128;
+template <int SPLIT>
+__global__ void __launch_bounds__(kFinishThreads)
+    finish_kernel(const float* __restrict__ part, int chunks, int64_t rows,
                               int64_t cols, int64_t ldp, int act,
                               const __nv_bfloat16* __restrict__ bias,
                               const __nv_bfloat16* __restrict__ R, __nv_bfloat16* __restrict__ Y,
                               __nv_bfloat16* __restrict__ Z) {
     tc::pdl_trigger();
     tc::pdl_wait();
+    constexpr int kQuads = kFinishThreads / SPLIT;
     const int64_t per = ldp / 4;
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= rows * per) return;
-    const int64_t r = i / per, c = (i - r * per) * 4;
+    const int quad = threadIdx.x % kQuads, part_of = threadIdx.x / kQuads;
+    const int64_t i = (int64_t)blockIdx.x * kQuads + quad;
+    const bool in = i < rows * per;
+    const int64_t r = in ? i / per : 0, c = in ? (i - r * per) * 4 : 0;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
-    const float* p = part + r * ldp + c;
-#pragma unroll 4
-    for (int k = 0; k < chunks; ++k, p += rows * ldp) {
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        x[0] += v.x;
-        x[1] += v.y;
-        x[2] += v.z;
-        x[3] += v.w;
+    const int stretch = (chunks + SPLIT - 1) / SPLIT;
+    const int k1 = min(chunks, (part_of + 1) * stretch);
+    const float* p = part + ((int64_t)part_of * stretch * rows + r) * ldp + c;
+    if (in)
+#pragma unroll 8
+        for (int k = part_of * stretch; k < k1; ++k, p += rows * ldp) {
+            const float4 v = *reinterpret_cast<const float4*>(p);
+            x[0] += v.x;
+            x[1] += v.y;
+            x[2] += v.z;
+            x[3] += v.w;
+        }
+    if (SPLIT > 1) {
+        __shared__ float4 sums[SPLIT][kQuads];
+        sums[part_of][quad] = make_float4(x[0], x[1], x[2], x[3]);
+        __syncthreads();
+        if (part_of > 0) return;
+#pragma unroll
+        for (int k = 1; k < SPLIT; ++k) {
+            const float4 v = sums[k][quad];
+            x[0] += v.x;
+            x[1] += v.y;
+            x[2] += v.z;
+            x[3] += v.w;
+        }
     }
+    if (!in) return;
     const int64_t at = r * cols + c;
+    if (bias)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] += c + k < cols ? __bfloat162float(bias[c + k]) : 0.f;
+    if (Z)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (c + k < cols) Z[at + k] = __float2bfloat16_rn(x[k]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float2 y = halves(act_value2(act, pair(x[2 * h], x[2 * h + 1])));
+        x[2 * h] = y.x;
+        x[2 * h + 1] = y.y;
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         if (c + k >= cols) break;
-        float z = x[k];
-        if (bias) z += __bfloat162float(bias[c + k]);
-        if (Z) Z[at + k] = __float2bfloat16_rn(z);
-        z = act_value(act, z);
-        if (R) z += __bfloat162float(R[at + k]);
-        Y[at + k] = __float2bfloat16_rn(z);
+        if (R) x[k] += __bfloat162float(R[at + k]);
+        Y[at + k] = __float2bfloat16_rn(x[k]);
     }
 }
 
@@ -85,7 +119,7 @@ __global__ void __launch_bounds__(256)
     const int lane = threadIdx.x % 32, ty = threadIdx.x / 32;
     const int64_t c = (int64_t)blockIdx.x * kDzCols + lane * 8;
     const int64_t r1 = min(rows, (int64_t)(blockIdx.y + 1) * rows_per);
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    uint64_t sum[4] = {0, 0, 0, 0};  // pairs
     if (c < cols) {
 #pragma unroll 2
         for (int64_t r = (int64_t)blockIdx.y * rows_per + ty; r < r1; r += kDzRows) {
@@ -102,19 +136,22 @@ __global__ void __launch_bounds__(256)
                     if (Z) z[k] = in ? Z[at + k] : __float2bfloat16_rn(0.f);
                 }
             }
+            uint32_t* gp = reinterpret_cast<uint32_t*>(g);
+            const uint32_t* zp = reinterpret_cast<const uint32_t*>(z);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                float v = __bfloat162float(g[k]);
-                if (Z) v *= act_slope(act, __bfloat162float(z[k]));
-                sum[k] += v;
-                g[k] = __float2bfloat16_rn(v);
+            for (int k = 0; k < 4; ++k) {
+                uint64_t v = unpack_bf16x2(gp[k]);
+                if (Z) v = mul2(v, act_slope2(act, unpack_bf16x2(zp[k])));
+                sum[k] = add2(sum[k], v);
+                gp[k] = pack_bf16x2(v);
             }
             if (dZ) *reinterpret_cast<uint4*>(dZ + r * ldz + c) = *reinterpret_cast<uint4*>(g);
         }
     }
     if (!db_part) return;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sums[ty][lane * 8 + k] = sum[k];
+    for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<float2*>(&sums[ty][lane * 8 + 2 * k]) = halves(sum[k]);
     __syncthreads();
     const int64_t col = (int64_t)blockIdx.x * kDzCols + threadIdx.x;
     if (col < cols) {
@@ -125,26 +162,26 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-// db = the sum of the blocks' partial sums: 32 columns a block, eight threads a column, each
-// over a stretch of the partials in order.
-__global__ void __launch_bounds__(256)
+// db = the sum of the blocks' partial sums: 32 columns a block, 32 threads a column, each over a
+// stretch of the partials in order.
+__global__ void __launch_bounds__(1024)
     db_kernel(const float* __restrict__ part, int n_part, int64_t cols, int64_t ldz,
               __nv_bfloat16* __restrict__ db) {
     tc::pdl_trigger();
     tc::pdl_wait();
-    __shared__ float sums[8][32];
+    __shared__ float sums[32][33];
     const int lane = threadIdx.x % 32, ty = threadIdx.x / 32;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
-    const int per = (n_part + 7) / 8;
+    const int per = (n_part + 31) / 32;
     float s = 0.f;
     if (c < cols)
-#pragma unroll 4
+#pragma unroll 8
         for (int k = ty * per; k < min(n_part, (ty + 1) * per); ++k) s += part[k * ldz + c];
     sums[ty][lane] = s;
     __syncthreads();
     if (ty == 0 && c < cols) {
 #pragma unroll
-        for (int k = 1; k < 8; ++k) s += sums[k][lane];
+        for (int k = 1; k < 32; ++k) s += sums[k][lane];
         db[c] = __float2bfloat16_rn(s);
     }
 }
@@ -234,8 +271,11 @@ cudaError_t pad(const void* src, int64_t rows, int64_t cols, void* dst, cudaStre
 cudaError_t finish(const float* part, const LinPlan& plan, int64_t rows, int64_t cols,
                    const LinEpilogue& e, cudaStream_t st) {
     const int64_t ldp = cdiv(cols, 4) * 4, n = rows * (ldp / 4);
-    return launch_pdl(finish_kernel, dim3((unsigned)cdiv(n, 128)), dim3(128), 0, st, part,
-                      plan.chunks, rows, cols, ldp, e.act, (const __nv_bfloat16*)e.bias,
+    // over 16 chunks: eight threads share them (38 chunks of 512 x 256 sums: 14 us with one)
+    const int split = plan.chunks > 16 ? 8 : 1;
+    auto kernel = split == 8 ? finish_kernel<8> : finish_kernel<1>;
+    return launch_pdl(kernel, dim3((unsigned)cdiv(n * split, kFinishThreads)),
+                      dim3(kFinishThreads), 0, st, part, plan.chunks, rows, cols, ldp, e.act, (const __nv_bfloat16*)e.bias,
                       (const __nv_bfloat16*)e.R, (__nv_bfloat16*)e.Y, (__nv_bfloat16*)e.Z);
 }
 
@@ -331,7 +371,7 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
                        (__nv_bfloat16*)(own_dz ? ws + L.off_dz : nullptr),
                        (float*)(db ? ws + L.off_db : nullptr));
         if (e == cudaSuccess && db)
-            e = launch_pdl(db_kernel, dim3((unsigned)cdiv(s.N, 32)), dim3(256), 0, st,
+            e = launch_pdl(db_kernel, dim3((unsigned)cdiv(s.N, 32)), dim3(1024), 0, st,
                            (const float*)(ws + L.off_db), (int)L.dz_blocks, s.N, ldz,
                            (__nv_bfloat16*)db);
     }

@@ -53,50 +53,98 @@ __device__ __forceinline__ float ex2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// The normal distribution function Phi(z), and e = exp(-z^2 / 2). Abramowitz and Stegun's
-// rational approximation 7.1.26 of erf (absolute error 1.5e-7, against the 2^-8 of the bf16 result)
-// at |z| / sqrt 2, taken as the lower tail so that a large negative z keeps its digits: six
-// multiply-adds, one reciprocal and one exponential, which the slope uses again.
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-    const float a = fabsf(z);
-    const float t = rcp_approx(fmaf(a, 0.3275911f * 0.70710678f, 1.f));
-    e = ex2_approx(z * z * -0.72134752f);  // log2(e) / 2
-    float p = fmaf(t, 1.061405429f, -1.453152027f);
-    p = fmaf(t, p, 1.421413741f);
-    p = fmaf(t, p, -0.284496736f);
-    p = fmaf(t, p, 0.254829592f);
-    const float tail = 0.5f * t * p * e;
-    return z > 0.f ? 1.f - tail : tail;
+// Two floats as one operand of the packed float32 instructions.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
 }
-__device__ __forceinline__ float logistic(float z) {
-    return rcp_approx(1.f + ex2_approx(z * -1.44269504f));
+__device__ __forceinline__ float2 halves(uint64_t v) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
 }
-// (The last product is rounded on its own: fused into the residual's addition in one of the
-// compiler's copies of a loop and not in another, the same call would not give the same bits with
-// and without Z.)
-__device__ __forceinline__ float act_value(int act, float z) {
-    float e;
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// 1 / (1 + 2^-u) of both halves: 2 exponentials, 2 reciprocals, one packed addition.
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t minus_u) {
+    const float2 u = halves(minus_u);
+    const float2 d = halves(add2(pair(ex2_approx(u.x), ex2_approx(u.y)), pair(1.f, 1.f)));
+    return pair(rcp_approx(d.x), rcp_approx(d.y));
+}
+// The normal distribution function as 1 / (1 + 2^-u), u(z) = log2(Phi(z) / Phi(-z)): odd and smooth,
+// so an odd polynomial of degree 13 does, fitted for the least largest error of z Phi(z) over
+// |z| <= 5 (2.2e-7; 3.3e-7 with float32 arithmetic; beyond 5 it grows faster than u, and z Phi(z)
+// is below 1.5e-6 from its limits). Both tails keep relative precision (2e-3 at z = -5, half a unit of
+// the bf16 result), and it takes about 8 issue slots a value in pairs, where the epilogue of a
+// memory-bound layer has about 16 for everything.
+__device__ __forceinline__ uint64_t normal_cdf2(uint64_t z) {
+    const uint64_t s = mul2(z, z);
+    uint64_t p = pair(-4.122593377786643e-09f, -4.122593377786643e-09f);
+    p = fma2(p, s, pair(3.340366276916029e-07f, 3.340366276916029e-07f));
+    p = fma2(p, s, pair(-1.0618686246743891e-05f, -1.0618686246743891e-05f));
+    p = fma2(p, s, pair(1.5339275705628097e-04f, 1.5339275705628097e-04f));
+    p = fma2(p, s, pair(1.15053633635398e-04f, 1.15053633635398e-04f));
+    p = fma2(p, s, pair(-1.0486429184675217e-01f, -1.0486429184675217e-01f));
+    p = fma2(p, s, pair(-2.3021974563598633f, -2.3021974563598633f));
+    return sigmoid2(mul2(p, z));
+}
+__device__ __forceinline__ uint64_t logistic2(uint64_t z) {
+    return sigmoid2(mul2(z, pair(-1.44269504f, -1.44269504f)));
+}
+// act of both halves. Every operation is an instruction of its own, so that a value has the same
+// bits wherever it is computed.
+__device__ __forceinline__ uint64_t act_value2(int act, uint64_t z) {
     switch (act) {
-        case FLAREPP_ACT_RELU: return z < 0.f ? 0.f : z;  // keeps a NaN
-        case FLAREPP_ACT_GELU: return __fmul_rn(z, normal_cdf(z, e));
-        case FLAREPP_ACT_SILU: return __fmul_rn(z, logistic(z));
+        case FLAREPP_ACT_RELU: {
+            const float2 f = halves(z);
+            return pair(f.x < 0.f ? 0.f : f.x, f.y < 0.f ? 0.f : f.y);  // keeps a NaN
+        }
+        case FLAREPP_ACT_GELU: return mul2(z, normal_cdf2(z));
+        case FLAREPP_ACT_SILU: return mul2(z, logistic2(z));
     }
     return z;
 }
-__device__ __forceinline__ float act_slope(int act, float z) {
-    float e;
+// act' of both halves: 1 or 0; Phi(z) + z phi(z); s (1 + z (1 - s)) with s = logistic(z).
+__device__ __forceinline__ uint64_t act_slope2(int act, uint64_t z) {
     switch (act) {
-        case FLAREPP_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+        case FLAREPP_ACT_RELU: {
+            const float2 f = halves(z);
+            return pair(f.x > 0.f ? 1.f : 0.f, f.y > 0.f ? 1.f : 0.f);
+        }
         case FLAREPP_ACT_GELU: {
-            const float cdf = normal_cdf(z, e);
-            return fmaf(z * 0.39894228f, e, cdf);
+            const float2 q = halves(mul2(mul2(z, z), pair(-0.72134752f, -0.72134752f)));
+            const uint64_t e = pair(ex2_approx(q.x), ex2_approx(q.y));  // exp(-z^2 / 2)
+            return fma2(mul2(z, pair(0.39894228f, 0.39894228f)), e, normal_cdf2(z));
         }
         case FLAREPP_ACT_SILU: {
-            const float s = logistic(z);
-            return s * fmaf(z, 1.f - s, 1.f);
+            const uint64_t s = logistic2(z), one = pair(1.f, 1.f);
+            const uint64_t t = fma2(s, pair(-1.f, -1.f), one);
+            return mul2(s, fma2(z, t, one));
         }
     }
-    return 1.f;
+    return pair(1.f, 1.f);
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(uint64_t v) {
+    const float2 f = halves(v);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint64_t unpack_bf16x2(uint32_t v) {
+    return pair(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
 }
 
 }  // namespace flarepp

@@ -10,10 +10,13 @@
 // shared-memory fill per CTA instead of 48 KB and B crosses the L2 half as often. The walk over
 // tiles is persistent; chunks cut a long contraction when there are few tiles.
 //
-// Roles (12 warps): warp 0 the TMA producer, warp 1 the MMA issuer (in the pair's leader),
-// warps 4..11 two epilogue warpgroups (TMEM lane = tile row), which take the tile's 64-column blocks
-// in turn. Two TMEM accumulators of 256 columns let the epilogue of a tile overlap the products of
-// the next. Every wait is bounded (2 s of %globaltimer): on expiry the kernel records
+// Roles (20 warps): warp 0 the TMA producer, warp 1 the MMA issuer (in the pair's leader),
+// warps 4..19 the epilogue: each takes one 32-row x 64-column block of the tile (TMEM lane = tile
+// row), in two halves of 32 columns. Two TMEM accumulators of 256 columns let the epilogue of a tile
+// overlap the products of the next. Sixteen epilogue warps, because a memory-bound layer leaves
+// about 16 issue slots per output value for everything, and the activation's chain of dependent
+// instructions needs four warps per scheduler to hide (with eight warps of 64 columns a half and
+// unpaired arithmetic the 65,536 x 256 -> 512 GELU layer took 46 us). Every wait is bounded (2 s of %globaltimer): on expiry the kernel records
 // FLAREPP_ERR_TIMEOUT in the status word, every role leaves its loops, the producer waits for its
 // copies in flight, the issuer for its products, and TMEM is freed.
 #include <cuda.h>
@@ -29,9 +32,9 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;
 constexpr int kFirstEpiWarp = 4;
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 16;
 constexpr int kSlice = 64;  // contraction values per ring stage: one 128-byte row
 constexpr int kATile = 128 * kSlice * 2;
 constexpr int kMaxNT = 256;
@@ -46,8 +49,8 @@ template <int CG, int OUT>
 struct Cfg {
     static constexpr int kBTile = kMaxNT / CG * kSlice * 2;
     static constexpr int kStage = kATile + kBTile;
-    // per epilogue warp: two 32-row x 64-column bf16 blocks
-    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * 2 * 4096 : 0;
+    // per epilogue warp: one 32-row x 64-column bf16 block
+    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * 4096 : 0;
     static constexpr int kFit = (232448 - 1024 - kStaging - kNumBars * 8 - 16) / kStage;
     static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
     static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kNumBars * 8 + 16;
@@ -115,14 +118,6 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, got);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t*>(&v);
-}
-__device__ __forceinline__ float2 unpack_bf16(uint32_t v) {
-    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-}
-
 // One operand's tile of `rows` rows for the slice at contraction index k: K-major as one box of
 // 64 x rows, MN-major as boxes of 64 rows x 64 contraction values ("atoms").
 template <int CG, bool MN>
@@ -169,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const int pair = (int)blockIdx.x / CG, pairs = (int)gridDim.x / CG;
+    const int first = (int)blockIdx.x / CG, pairs = (int)gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kS; ++s) {
@@ -212,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // MN-major tiles come in whole 64-row atoms
         const uint32_t b_bytes = (uint32_t)(B_MN ? (b_rows + 63) / 64 * 64 : b_rows) * kSlice * 2;
         const uint32_t bytes = CG * (kATile + b_bytes);
-        for (int v = pair; v < prm.n_work && ok; v += pairs) {
+        for (int v = first; v < prm.n_work && ok; v += pairs) {
             const Work w = work_of(prm, v);
             const int m0 = (w.rt * CG + (int)rank) * 128;
             const int n0 = w.ct * prm.NT + (int)rank * b_rows;
@@ -253,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------ MMA issuer
         uint32_t it = 0, j = 0;
         bool ok = true;
-        for (int v = pair; v < prm.n_work && ok; v += pairs, ++j) {
+        for (int v = first; v < prm.n_work && ok; v += pairs, ++j) {
             const Work w = work_of(prm, v);
             const int ab = j & 1;
             if (j >= 2 &&
@@ -307,209 +302,205 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------ epilogue
         const int e = warp - kFirstEpiWarp;
         const int q = warp % 4;  // the TMEM lanes this warp may read
-        const uint32_t lane_off = (uint32_t)(32 * q) << 16;
-        uint8_t* stage = staging + e * 2 * 4096;
+        const int c = 64 * (e / 4);
+        uint8_t* block = staging + e * 4096;
+        uint8_t* line = block + lane * 128;
+        const uint32_t rfull = rfull0 + 8u * e;
         uint32_t j = 0, r_phase = 0;
-        int buf = 0;
         bool r_pending = false;
-        for (int v = pair; v < prm.n_work; v += pairs, ++j) {
+        for (int v = first; v < prm.n_work; v += pairs, ++j) {
             const Work w = work_of(prm, v);
             const int ab = j & 1;
             const int row0 = (w.rt * CG + (int)rank) * 128 + 32 * q;
-            bool waited = false, ok = true;
-            for (int c = 64 * (e / 4); c < prm.NT; c += 128) {
-                const int col0 = w.ct * prm.NT + c;
-                const bool live = row0 < prm.M && col0 < prm.N;
-                uint8_t* yb = stage + 4096 * buf;
-                if (OUT == kOutEpilogue && live && prm.R && prm.tma_out) {
-                    // the block of R comes into the buffer that Y leaves from
-                    if (lane == 0) {
-                        if (prm.Z) bulk_wait_read();
-                        else bulk_wait_read_1();
-                        mbar_expect_tx(rfull0 + 8u * e, 4096);
-                        tma_load_2d(smem_u32(yb), &tmR, col0, row0, rfull0 + 8u * e);
-                    }
-                    r_pending = true;
+            const int col0 = w.ct * prm.NT + c;
+            const bool live = c < prm.NT && row0 < prm.M && col0 < prm.N;
+            const uint32_t acc = tmem + ((uint32_t)(32 * q) << 16) + ab * kMaxNT + c;
+            // the block of R, into the buffer that Y leaves from
+            auto fetch_r = [&] {
+                if (lane == 0) {
+                    bulk_wait_read();
+                    mbar_expect_tx(rfull, 4096);
+                    tma_load_2d(smem_u32(block), &tmR, col0, row0, rfull);
                 }
-                if (!waited) {
-                    ok = warp_wait<CG>(accfull0 + 8u * ab, (j >> 1) & 1, abort_flag, prm.status);
-                    waited = true;
-                    if (!ok) break;
-                    tc_fence_after();
+                r_pending = true;
+            };
+            const bool tma_r = OUT == kOutEpilogue && live && prm.R && prm.tma_out;
+            if (tma_r && !prm.Z) fetch_r();
+            if (!warp_wait<CG>(accfull0 + 8u * ab, (j >> 1) & 1, abort_flag, prm.status)) break;
+            tc_fence_after();
+            auto release = [&] {  // this warp has read its part of the accumulator
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
+                    else mbar_arrive(accempty0 + 8u * ab);
                 }
-                if (!live) continue;
-                float x[64];
-                tmem_ld32(tmem + lane_off + ab * kMaxNT + c, reinterpret_cast<uint32_t*>(x));
-                tmem_ld32(tmem + lane_off + ab * kMaxNT + c + 32, reinterpret_cast<uint32_t*>(x + 32));
-                tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
-                tmem_wait_ld32(reinterpret_cast<uint32_t*>(x + 32));
+            };
+            if (!live) {
+                release();
+                continue;
+            }
+            if (OUT != kOutEpilogue) {
                 const int row = row0 + lane;
-                if (OUT == kOutPart) {
-                    if (row < prm.M) {
-                        float* d = prm.part + ((int64_t)w.chunk * prm.M + row) * prm.ldp + col0;
-                        const int n = min(64, min(prm.NT - c, (int)prm.ldp - col0));
 #pragma unroll
-                        for (int i = 0; i < 64; i += 4)
+                for (int h = 0; h < 2; ++h) {
+                    float x[32];
+                    tmem_ld32(acc + 32 * h, reinterpret_cast<uint32_t*>(x));
+                    tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
+                    if (h == 1) release();
+                    if (row >= prm.M) continue;
+                    if (OUT == kOutPart) {
+                        const int at = col0 + 32 * h;
+                        float* d = prm.part + ((int64_t)w.chunk * prm.M + row) * prm.ldp + at;
+                        const int n = min(prm.NT - c - 32 * h, (int)prm.ldp - at);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
                             if (i < n)
                                 *reinterpret_cast<float4*>(d + i) =
                                     make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-                    }
-                    continue;
-                }
-                if (OUT == kOutPartT) {
-                    if (row < prm.M) {
-                        float* d = prm.part + ((int64_t)w.chunk * prm.N + col0) * prm.ldp + row;
-                        const int n = min(64, min(prm.NT - c, prm.N - col0));
+                    } else {
+                        const int at = col0 + 32 * h;
+                        float* d = prm.part + ((int64_t)w.chunk * prm.N + at) * prm.ldp + row;
+                        const int n = min(prm.NT - c - 32 * h, prm.N - at);
 #pragma unroll
-                        for (int i = 0; i < 64; ++i)
+                        for (int i = 0; i < 32; ++i)
                             if (i < n) d[i * prm.ldp] = x[i];
                     }
-                    continue;
                 }
-                if (prm.bias) {
-                    if (col0 + 64 <= prm.N) {
-                        const uint4* b4 = reinterpret_cast<const uint4*>(prm.bias + col0);
+                continue;
+            }
+            // Columns 32 h .. 32 h + 31 of the block: sums with the bias, as 16 pairs.
+            auto load_half = [&](int h, uint64_t* x) {
+                uint32_t r[32];
+                tmem_ld32(acc + 32 * h, r);
+                tmem_wait_ld32(r);
 #pragma unroll
-                        for (int g = 0; g < 8; ++g) {
-                            const uint4 u = __ldg(b4 + g);
-                            const uint32_t p[4] = {u.x, u.y, u.z, u.w};
+                for (int i = 0; i < 16; ++i)
+                    x[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+                if (!prm.bias) return;
+                const int at = col0 + 32 * h;
+                if (at + 32 <= prm.N) {
+                    const uint4* b4 = reinterpret_cast<const uint4*>(prm.bias + at);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float2 f = unpack_bf16(p[i]);
-                                x[8 * g + 2 * i] += f.x;
-                                x[8 * g + 2 * i + 1] += f.y;
-                            }
-                        }
-                    } else {
+                    for (int g = 0; g < 4; ++g) {
+                        const uint4 u = __ldg(b4 + g);
+                        x[4 * g] = add2(x[4 * g], unpack_bf16x2(u.x));
+                        x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u.y));
+                        x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u.z));
+                        x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u.w));
+                    }
+                } else {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i)
-                            if (col0 + i < prm.N) x[i] += __bfloat162float(prm.bias[col0 + i]);
+                    for (int i = 0; i < 16; ++i) {
+                        const int n = at + 2 * i;
+                        x[i] = add2(x[i], pair(n < prm.N ? __bfloat162float(prm.bias[n]) : 0.f,
+                                               n + 1 < prm.N ? __bfloat162float(prm.bias[n + 1]) : 0.f));
                     }
                 }
-                // The block goes through shared memory swizzled as the store map undoes it: 16-byte
-                // piece g of row r at g ^ (r % 8), free of bank conflicts.
-                const uint32_t line = lane * 128;
-                if (prm.Z) {
-                    uint8_t* zb = stage + 4096 * (buf ^ 1);
-                    if (lane == 0 && !(prm.R && prm.tma_out)) bulk_wait_read();
-                    __syncwarp();
+            };
+            // The block goes through shared memory swizzled as the store map undoes it: 16-byte
+            // piece g of row r at g ^ (r % 8), free of bank conflicts.
+            auto store_half = [&](int h, const uint64_t* x) {
 #pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        uint4 u;
-                        u.x = pack_bf16(x[8 * g], x[8 * g + 1]);
-                        u.y = pack_bf16(x[8 * g + 2], x[8 * g + 3]);
-                        u.z = pack_bf16(x[8 * g + 4], x[8 * g + 5]);
-                        u.w = pack_bf16(x[8 * g + 6], x[8 * g + 7]);
-                        *reinterpret_cast<uint4*>(zb + line + ((g ^ (lane & 7)) << 4)) = u;
-                    }
-                    if (prm.tma_out) {
-                        fence_proxy_async();
-                        __syncwarp();
-                        if (lane == 0) {
-                            tma_store_2d(&tmZ, smem_u32(zb), col0, row0);
-                            bulk_commit();
-                        }
-                    } else {
-                        __syncwarp();
-                        for (int i = lane; i < 32 * 64; i += 32) {
-                            const int r = i >> 6, cc = i & 63;
-                            if (row0 + r < prm.M && col0 + cc < prm.N && c + cc < prm.NT)
-                                prm.Z[(int64_t)(row0 + r) * prm.N + col0 + cc] =
-                                    *reinterpret_cast<__nv_bfloat16*>(
-                                        zb + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2);
-                        }
-                    }
-                }
-                switch (prm.act) {
-                    case FLAREPP_ACT_RELU:
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) x[i] = act_value(FLAREPP_ACT_RELU, x[i]);
-                        break;
-                    case FLAREPP_ACT_GELU:
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) x[i] = act_value(FLAREPP_ACT_GELU, x[i]);
-                        break;
-                    case FLAREPP_ACT_SILU:
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) x[i] = act_value(FLAREPP_ACT_SILU, x[i]);
-                        break;
-                }
-                if (prm.R) {
-                    if (prm.tma_out) {
-                        ok = warp_wait<1>(rfull0 + 8u * e, r_phase, abort_flag, prm.status);
-                        if (!ok) break;
-                        r_phase ^= 1;
-                        r_pending = false;
-                    } else {
-                        __syncwarp();
-                        for (int i = lane; i < 32 * 64; i += 32) {
-                            const int r = i >> 6, cc = i & 63;
-                            if (row0 + r < prm.M && col0 + cc < prm.N)
-                                *reinterpret_cast<__nv_bfloat16*>(
-                                    yb + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2) =
-                                    prm.R[(int64_t)(row0 + r) * prm.N + col0 + cc];
-                        }
-                        __syncwarp();
-                    }
-#pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(yb + line + ((g ^ (lane & 7)) << 4));
-                        const uint32_t p[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float2 f = unpack_bf16(p[i]);
-                            x[8 * g + 2 * i] += f.x;
-                            x[8 * g + 2 * i + 1] += f.y;
-                        }
-                    }
-                } else if (!prm.Z) {
-                    if (lane == 0) bulk_wait_read_1();
-                    __syncwarp();
-                }
-#pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    uint4 u;
-                    u.x = pack_bf16(x[8 * g], x[8 * g + 1]);
-                    u.y = pack_bf16(x[8 * g + 2], x[8 * g + 3]);
-                    u.z = pack_bf16(x[8 * g + 4], x[8 * g + 5]);
-                    u.w = pack_bf16(x[8 * g + 6], x[8 * g + 7]);
-                    *reinterpret_cast<uint4*>(yb + line + ((g ^ (lane & 7)) << 4)) = u;
-                }
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<uint4*>(line + (((4 * h + g) ^ (lane & 7)) << 4)) =
+                        make_uint4(pack_bf16x2(x[4 * g]), pack_bf16x2(x[4 * g + 1]),
+                                   pack_bf16x2(x[4 * g + 2]), pack_bf16x2(x[4 * g + 3]));
+            };
+            // value (r, cc) of the block, for outputs whose lines TMA cannot address
+            auto at_block = [&](int r, int cc) {
+                return reinterpret_cast<__nv_bfloat16*>(
+                    block + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2);
+            };
+            const int rows = min(32, prm.M - row0);
+            const int cols = min(64, min(prm.NT - c, prm.N - col0));
+            auto flush = [&](const CUtensorMap* map, __nv_bfloat16* out) {
                 if (prm.tma_out) {
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(&tmY, smem_u32(yb), col0, row0);
+                        tma_store_2d(map, smem_u32(block), col0, row0);
                         bulk_commit();
                     }
-                    if (!prm.Z) buf ^= 1;
                 } else {
                     __syncwarp();
-                    for (int i = lane; i < 32 * 64; i += 32) {
-                        const int r = i >> 6, cc = i & 63;
-                        if (row0 + r < prm.M && col0 + cc < prm.N && c + cc < prm.NT)
-                            prm.Y[(int64_t)(row0 + r) * prm.N + col0 + cc] =
-                                *reinterpret_cast<__nv_bfloat16*>(
-                                    yb + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2);
-                    }
+                    for (int r = 0; r < rows; ++r)
+                        for (int cc = lane; cc < cols; cc += 32)
+                            out[(int64_t)(row0 + r) * prm.N + col0 + cc] = *at_block(r, cc);
                     __syncwarp();
                 }
+            };
+            auto block_free = [&] {  // the stores from the block have read it
+                if (lane == 0) bulk_wait_read();
+                __syncwarp();
+            };
+            uint64_t x[16];
+            if (prm.Z) {
+                block_free();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    load_half(h, x);
+                    store_half(h, x);
+                }
+                flush(&tmZ, prm.Z);
             }
-            if (!waited)
-                ok = warp_wait<CG>(accfull0 + 8u * ab, (j >> 1) & 1, abort_flag, prm.status);
+            if (tma_r && prm.Z) fetch_r();
+            if (prm.R && !prm.tma_out) {
+                for (int r = 0; r < rows; ++r)
+                    for (int cc = lane; cc < cols; cc += 32)
+                        *at_block(r, cc) = prm.R[(int64_t)(row0 + r) * prm.N + col0 + cc];
+                __syncwarp();
+            }
+            bool ok = true;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                load_half(h, x);
+                if (h == 1) release();
+                switch (prm.act) {
+                    case FLAREPP_ACT_RELU:
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = act_value2(FLAREPP_ACT_RELU, x[i]);
+                        break;
+                    case FLAREPP_ACT_GELU:
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = act_value2(FLAREPP_ACT_GELU, x[i]);
+                        break;
+                    case FLAREPP_ACT_SILU:
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = act_value2(FLAREPP_ACT_SILU, x[i]);
+                        break;
+                }
+                if (h == 0) {
+                    if (tma_r) {
+                        ok = warp_wait<1>(rfull, r_phase, abort_flag, prm.status);
+                        if (ok) {
+                            r_phase ^= 1;
+                            r_pending = false;
+                        }
+                    } else if (!prm.R) {
+                        block_free();
+                    }
+                }
+                if (prm.R) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(
+                            line + (((4 * h + g) ^ (lane & 7)) << 4));
+                        x[4 * g] = add2(x[4 * g], unpack_bf16x2(u.x));
+                        x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u.y));
+                        x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u.z));
+                        x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u.w));
+                    }
+                }
+                store_half(h, x);
+            }
             if (!ok) break;
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {  // this warp has read its part of the accumulator
-                if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
-                else mbar_arrive(accempty0 + 8u * ab);
-            }
+            flush(&tmY, prm.Y);
         }
         if (OUT == kOutEpilogue) {
             if (r_pending) {  // only after a wait that gave up: let the copy in flight land
                 const uint64_t t0 = globaltimer_ns();
-                while (!mbar_try_wait(rfull0 + 8u * e, r_phase) &&
-                       globaltimer_ns() - t0 < kWaitLimitNs) {
+                while (!mbar_try_wait(rfull, r_phase) && globaltimer_ns() - t0 < kWaitLimitNs) {
                 }
             }
             if (lane == 0) bulk_wait_all();
