@@ -6,7 +6,7 @@
 // one pass for tables of up to 2,047 rows, two up to 4 M, three beyond. Then equal stretches of
 // the sorted positions are summed in parallel whatever the lengths of the runs of one id; a run that
 // crosses from one stretch into the next leaves float32 partial sums, which a last kernel adds in
-// order.
+// order. The gradient is written once: a bit per row says which rows no id names.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(256)
 constexpr int kSortThreads = 256;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kMaxBits = 11;
+constexpr int kHeld = 4;  // positions per lane held in registers: a stretch of a tile of 1,024
 
 struct SortPlan {
     int passes, bits;     // digits, and bits of each
@@ -129,6 +130,7 @@ __global__ void __launch_bounds__(kSortThreads)
     __syncthreads();
     tc::pdl_wait();
     const int64_t i0 = (int64_t)blockIdx.x * tile, i1 = min(T, i0 + tile);
+#pragma unroll 4
     for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
         atomicAdd(&cnt[(key_at(ids, keys, i, V, status) >> shift) & (bins - 1)], 1u);
     __syncthreads();
@@ -175,6 +177,18 @@ __global__ void __launch_bounds__(kSortThreads)
     for (int d = threadIdx.x; d < kSortWarps * bins; d += kSortThreads) sm[d] = 0;
     tc::pdl_wait();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t t0 = (int64_t)blockIdx.x * tile, t1 = min(T, t0 + tile);
+    const int64_t stretch = (tile + kSortWarps * 32 - 1) / (kSortWarps * 32) * 32;
+    const int64_t i0 = t0 + warp * stretch, i1 = min(t1, i0 + stretch);
+    uint32_t key[kHeld];  // of the positions b + 32 k + lane
+    auto load_keys = [&](int64_t b) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int64_t i = b + 32 * k + lane;
+            key[k] = i < i1 ? key_at(ids, keys, i, V, nullptr) : (uint32_t)V;
+        }
+    };
+    load_keys(i0);
     // starts: an exclusive scan of the totals, a stretch of bins per thread
     const int per = (bins + kSortThreads - 1) / kSortThreads;
     uint32_t mine = 0;
@@ -200,12 +214,13 @@ __global__ void __launch_bounds__(kSortThreads)
         if (d < bins) start[d] += before;
     }
     // counts of each warp's stretch
-    const int64_t t0 = (int64_t)blockIdx.x * tile, t1 = min(T, t0 + tile);
-    const int64_t stretch = (tile + kSortWarps * 32 - 1) / (kSortWarps * 32) * 32;
-    const int64_t i0 = t0 + warp * stretch, i1 = min(t1, i0 + stretch);
     uint32_t* mine_at = sm + warp * bins;
-    for (int64_t i = i0 + lane; i < i1; i += 32)
-        atomicAdd(&mine_at[(key_at(ids, keys, i, V, nullptr) >> shift) & (bins - 1)], 1u);
+    for (int64_t b = i0; b < i1; b += 32 * kHeld) {
+        if (b != i0) load_keys(b);
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            if (b + 32 * k + lane < i1) atomicAdd(&mine_at[(key[k] >> shift) & (bins - 1)], 1u);
+    }
     __syncthreads();
     // places: start of the digit + tiles before + stretches before
     for (int d = threadIdx.x; d < bins; d += kSortThreads) {
@@ -217,115 +232,212 @@ __global__ void __launch_bounds__(kSortThreads)
         }
     }
     __syncthreads();
-    for (int64_t i = i0; i < i1; i += 32) {
-        const bool in = i + lane < i1;
-        const uint32_t key = in ? key_at(ids, keys, i + lane, V, nullptr) : 0xffffffffu;
-        const uint32_t d = in ? (key >> shift) & (bins - 1) : 0xffffffffu;
-        const uint32_t same = __match_any_sync(0xffffffffu, d);
-        const uint32_t rank = __popc(same & ((1u << lane) - 1u));
-        uint32_t at = 0;
-        if (in) at = mine_at[d] + rank;
-        __syncwarp();
-        if (in && rank == 0) mine_at[d] += __popc(same);
-        __syncwarp();
-        if (in) {
-            keys_out[at] = key;
-            pos_out[at] = pos ? pos[i + lane] : (uint32_t)(i + lane);
+    for (int64_t b = i0; b < i1; b += 32 * kHeld) {
+        if (i1 - i0 > 32 * kHeld) load_keys(b);
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int64_t i = b + 32 * k + lane;
+            if (b + 32 * k >= i1) break;
+            const bool in = i < i1;
+            const uint32_t d = in ? (key[k] >> shift) & (bins - 1) : 0xffffffffu;
+            const uint32_t same = __match_any_sync(0xffffffffu, d);
+            const uint32_t rank = __popc(same & ((1u << lane) - 1u));
+            uint32_t at = 0;
+            if (in) at = mine_at[d] + rank;
+            __syncwarp();
+            if (in && rank == 0) mine_at[d] += __popc(same);
+            __syncwarp();
+            if (in) {
+                keys_out[at] = key[k];
+                pos_out[at] = pos ? pos[i] : (uint32_t)i;
+            }
         }
     }
 }
 
 // ------------------------------------------------------------------ sums
-constexpr int kStretch = 64;  // sorted positions per thread row
-constexpr int kBatch = 8;     // rows of dY in flight per thread
+// Thread (x, y) of a block sums N columns of one stretch of the sorted positions, a batch of rows
+// of dY in flight while the batch before is added. A run that lies within the stretch goes to the
+// table; one that began before it leaves its sum in head[stretch], one that begins here and goes on in
+// tail[stretch], and the stretch on the list of `crossing` runs (whose order does not matter: each
+// is a sum of its own). A run's first stretch sets the row's bit in `met`.
+constexpr int kSumThreads = 256;
+constexpr int kMinStretch = 16, kMaxStretch = 256;
+constexpr int kMaxHeld = 8192;   // positions whose keys and places a block holds
+constexpr int kJoinThreads = 1024;
+constexpr int kZeroRows = 32;    // rows per warp that writes zeros: a word of `met`
 
-// Thread (x, y): N columns of stretch blockIdx.x * blockDim.y + y. A run that lies within the
-// stretch goes to the table; one that began before it leaves its sum in head[stretch], one that
-// begins here and goes on in tail[stretch].
 template <typename E, int N>
-__global__ void __launch_bounds__(256)
+__device__ void zero_rows(const uint32_t* __restrict__ met, int64_t word, int64_t V, int64_t C,
+                          E* __restrict__ dtable) {
+    const int lane = threadIdx.x % 32;
+    Vec<E, N> zero;
+#pragma unroll
+    for (int k = 0; k < N; ++k) from_f32(zero.v[k], 0.f);
+    const int64_t v0 = word * kZeroRows;
+    if (v0 >= V) return;
+    uint32_t gone = ~met[word];
+    if (V - v0 < kZeroRows) gone &= (1u << (V - v0)) - 1u;
+    while (gone) {
+        const int v = __ffs(gone) - 1;
+        gone &= gone - 1;
+        for (int64_t c = lane * N; c < C; c += 32 * N) store_vec<E, N>(dtable + (v0 + v) * C + c, zero);
+    }
+}
+
+template <typename E, int N>
+__global__ void __launch_bounds__(kSumThreads)
     sum_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos,
-               const E* __restrict__ dY, int64_t T, int64_t V, int64_t C, float scale,
-               E* __restrict__ dtable, float* __restrict__ head, float* __restrict__ tail) {
+               const E* __restrict__ dY, int64_t T, int64_t V, int64_t C, int stretch, float scale,
+               E* __restrict__ dtable, float* __restrict__ head, float* __restrict__ tail,
+               uint32_t* __restrict__ met, uint32_t* __restrict__ crossing,
+               uint32_t* __restrict__ n_crossing) {
+    constexpr int kBatch = sizeof(E) * N == 16 && N == 8 ? 4 : 8;  // two blocks fit an SM
+    extern __shared__ uint32_t held[];  // the block's keys, its positions
+    const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     tc::pdl_trigger();
     tc::pdl_wait();
+    const int span = blockDim.y * stretch;
+    const int64_t b0 = (int64_t)blockIdx.x * span;
+    uint32_t* held_pos = held + span;
+    for (int i = tid; i < span; i += kSumThreads) {
+        const bool in = b0 + i < T;
+        held[i] = in ? keys[b0 + i] : (uint32_t)V;
+        held_pos[i] = in ? pos[b0 + i] : 0;
+    }
+    __syncthreads();
     const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
     const int64_t st = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    const int64_t i0 = st * kStretch, i1 = min(T, i0 + kStretch);
+    const int64_t i0 = st * stretch;
     if (c >= C || i0 >= T) return;
-    uint32_t cur = keys[i0];
-    if (cur == (uint32_t)V) return;  // empty positions come last
+    const uint32_t* key = held + threadIdx.y * stretch;
+    const uint32_t* at = held_pos + threadIdx.y * stretch;
+    uint32_t cur = key[0];
+    if (cur == (uint32_t)V) return;  // empty positions come last, and those beyond T count as such
     bool began = i0 == 0 || keys[i0 - 1] != cur;
+    const bool goes_on = i0 + stretch < T && keys[i0 + stretch] == key[stretch - 1];
     float acc[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) acc[k] = 0.f;
+    const bool first = blockIdx.y == 0 && threadIdx.x == 0;
     auto flush = [&](bool more) {
+        if (began && first) {
+            atomicOr(met + (cur >> 5), 1u << (cur & 31));
+            if (more) crossing[atomicAdd(n_crossing, 1u)] = (uint32_t)st;
+        }
         if (began && !more) {
             Vec<E, N> o;
 #pragma unroll
             for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
             store_vec<E, N>(dtable + (int64_t)cur * C + c, o);
         } else {
-            float* d = (began ? tail : head) + st * C + c;
+            Vec<float, N> o;
 #pragma unroll
-            for (int k = 0; k < N; ++k) d[k] = acc[k];
+            for (int k = 0; k < N; ++k) o.v[k] = acc[k];
+            *reinterpret_cast<Vec<float, N>*>((began ? tail : head) + st * C + c) = o;
         }
     };
-    bool ended = false;
-    for (int64_t i = i0; i < i1 && !ended; i += kBatch) {
-        uint32_t key[kBatch];
-        Vec<E, N> x[kBatch];
+    Vec<E, N> x[2][kBatch];
+    auto fetch = [&](Vec<E, N>* d, int i) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (key[i + k] != (uint32_t)V) d[k] = load_vec<E, N>(dY + (int64_t)at[i + k] * C + c);
+    };
+    auto take = [&](const Vec<E, N>* d, int i) {  // false at the first empty position
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            key[k] = i + k < i1 ? keys[i + k] : (uint32_t)V;
-            if (key[k] != (uint32_t)V) x[k] = load_vec<E, N>(dY + (int64_t)pos[i + k] * C + c);
-        }
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            if (i + k >= i1 || ended) break;
-            if (key[k] != cur) {
+            if (key[i + k] != cur) {
                 flush(false);
                 began = true;
-                cur = key[k];
+                cur = key[i + k];
 #pragma unroll
                 for (int j = 0; j < N; ++j) acc[j] = 0.f;
-                if (cur == (uint32_t)V) {
-                    ended = true;
-                    break;
-                }
+                if (cur == (uint32_t)V) return false;
             }
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] += to_f32(x[k].v[j]);
+            for (int j = 0; j < N; ++j) acc[j] += to_f32(d[k].v[j]);
         }
+        return true;
+    };
+    // stretches are multiples of two batches
+    fetch(x[0], 0);
+    for (int i = 0; i < stretch; i += 2 * kBatch) {
+        fetch(x[1], i + kBatch);
+        if (!take(x[0], i)) return;
+        if (i + 2 * kBatch < stretch) fetch(x[0], i + 2 * kBatch);
+        if (!take(x[1], i + kBatch)) return;
     }
-    if (!ended) flush(i1 < T && keys[i1] == cur);
+    flush(goes_on);
 }
 
-// The runs that cross stretches: the stretch where such a run begins adds its parts in order.
+// The runs that cross stretches, a block at a time: its threads look at one stretch each to find
+// where the run ends, its rows of threads add equal shares of the parts in order, and the shares are
+// added in order. Blocks from `join_blocks` on write the zeros of the rows that no id names.
 template <typename E, int N>
-__global__ void __launch_bounds__(256)
-    join_kernel(const uint32_t* __restrict__ keys, int64_t T, int64_t V, int64_t C, float scale,
-                const float* __restrict__ head, const float* __restrict__ tail,
+__global__ void __launch_bounds__(kJoinThreads)
+    join_kernel(const uint32_t* __restrict__ keys, int64_t T, int64_t V, int64_t C, int stretch,
+                unsigned join_blocks, float scale, const float* __restrict__ head,
+                const float* __restrict__ tail, const uint32_t* __restrict__ met,
+                const uint32_t* __restrict__ crossing, const uint32_t* __restrict__ n_crossing,
                 E* __restrict__ dtable) {
+    extern __shared__ float share[];  // [blockDim.y][blockDim.x * N]
+    const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     tc::pdl_trigger();
     tc::pdl_wait();
+    if (blockIdx.x >= join_blocks) {
+        if (blockIdx.y == 0)
+            zero_rows<E, N>(met, (int64_t)(blockIdx.x - join_blocks) * (kJoinThreads / 32) + tid / 32,
+                            V, C, dtable);
+        return;
+    }
+    const unsigned n = *n_crossing;
     const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
-    const int64_t st = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    const int64_t i0 = st * kStretch, i1 = i0 + kStretch;
-    if (c >= C || i1 >= T) return;
-    const uint32_t key = keys[i1 - 1];
-    if (key == (uint32_t)V || keys[i1] != key) return;          // nothing goes on from here
-    if (keys[i0] == key && i0 > 0 && keys[i0 - 1] == key) return;  // it did not begin here
-    float acc[N];
+    const int row = blockDim.x * N;
+    for (unsigned item = blockIdx.x; item < n; item += join_blocks) {
+        const int64_t st = crossing[item];
+        const uint32_t key = keys[(st + 1) * stretch];
+        int64_t parts = 0;  // stretches st + 1 .. st + parts begin with the run's key
+        for (;;) {
+            const int64_t at = (st + 1 + parts + tid) * stretch;
+            const int more = __syncthreads_count(at < T && keys[at] == key);
+            parts += more;
+            if (more < kJoinThreads) break;
+        }
+        const int64_t per = (parts + blockDim.y - 1) / blockDim.y;
+        const int64_t p0 = threadIdx.y * per, p1 = min(parts, p0 + per);
+        float acc[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) acc[k] = tail[st * C + c + k];
-    for (int64_t s = st + 1; s * kStretch < T && keys[s * kStretch] == key; ++s)
+        for (int k = 0; k < N; ++k) acc[k] = 0.f;
+        if (c < C) {
+            if (threadIdx.y == 0) {
+                const Vec<float, N> v = *reinterpret_cast<const Vec<float, N>*>(tail + st * C + c);
 #pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] += head[s * C + c + k];
-    Vec<E, N> o;
+                for (int k = 0; k < N; ++k) acc[k] = v.v[k];
+            }
+#pragma unroll 4
+            for (int64_t p = p0; p < p1; ++p) {
+                const Vec<float, N> v =
+                    *reinterpret_cast<const Vec<float, N>*>(head + (st + 1 + p) * C + c);
 #pragma unroll
-    for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
-    store_vec<E, N>(dtable + (int64_t)key * C + c, o);
+                for (int k = 0; k < N; ++k) acc[k] += v.v[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) share[threadIdx.y * row + threadIdx.x * N + k] = acc[k];
+        __syncthreads();
+        if (threadIdx.y == 0 && c < C) {
+            const int ys = (int)min((int64_t)blockDim.y, parts);  // the rest have no share
+#pragma unroll 4
+            for (int y = 1; y < ys; ++y)
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] += share[y * row + threadIdx.x * N + k];
+            Vec<E, N> o;
+#pragma unroll
+            for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
+            store_vec<E, N>(dtable + (int64_t)key * C + c, o);
+        }
+        __syncthreads();
+    }
 }
 
 // ------------------------------------------------------------------ host side
@@ -366,19 +478,32 @@ SortPlan sort_plan(const flarepp_embedding_shape& s) {
 
 struct Layout {
     SortPlan sort;
+    int stretch;
     int64_t stretches;
-    size_t off_keys[2], off_pos[2], off_hist, off_total, off_head, off_tail, total;
+    size_t off_met, met_bytes;  // the number of crossing runs, then a bit per row
+    size_t off_crossing, off_keys[2], off_pos[2], off_hist, off_total, off_head, off_tail, total;
 };
 Layout layout_of(const flarepp_embedding_shape& s) {
     Layout L{};
     L.sort = sort_plan(s);
-    L.stretches = cdiv(s.T, kStretch);
+    // stretches so long that about sixteen rows of threads per SM have one each
+    const int64_t vecs = cdiv(s.C, vec_of(s)), x = lanes_for(vecs, 32);
+    const int64_t want = cdiv(s.T * cdiv(vecs, x) * x, (int64_t)16 * 32 * kNumSMs);
+    int64_t most = kMaxHeld / (kSumThreads / x);
+    if (most > kMaxStretch) most = kMaxStretch;
+    L.stretch = (int)(cdiv(want, kMinStretch) * kMinStretch);
+    if (L.stretch < kMinStretch) L.stretch = kMinStretch;
+    if (want > most) L.stretch = (int)most;
+    L.stretches = cdiv(s.T, L.stretch);
     auto take = [&](int64_t bytes) {
         const size_t at = L.total;
         L.total = align_up(at + (size_t)bytes, kWsAlign);
         return at;
     };
     const int64_t bins = (int64_t)1 << L.sort.bits;
+    L.met_bytes = 4 + (size_t)cdiv(s.V, 32) * 4;
+    L.off_met = take((int64_t)L.met_bytes);
+    L.off_crossing = take(L.stretches * 4);
     for (int i = 0; i < 2; ++i) {
         L.off_keys[i] = take(s.T * 4);
         L.off_pos[i] = take(s.T * 4);
@@ -444,17 +569,33 @@ template <typename E, int N>
 cudaError_t sums(const flarepp_embedding_shape& s, const Layout& L, int at, const void* dY,
                  float scale, void* dtable, char* ws, cudaStream_t st) {
     const int64_t vecs = cdiv(s.C, N);
-    const int x = lanes_for(vecs, 32), y = 256 / x;
-    const dim3 grid((unsigned)cdiv(L.stretches, y), (unsigned)cdiv(vecs, x));
+    const int x = lanes_for(vecs, 32), y = kSumThreads / x;
+    const unsigned col_blocks = (unsigned)cdiv(vecs, x);
+    const unsigned sum_blocks = (unsigned)cdiv(L.stretches, y);
+    const unsigned join_blocks = L.stretches < 2 * kNumSMs ? (unsigned)L.stretches : 2 * kNumSMs;
+    const unsigned zero_blocks = (unsigned)cdiv(s.V, kZeroRows * (kJoinThreads / 32));
     const uint32_t* keys = (const uint32_t*)(ws + L.off_keys[at]);
     const uint32_t* pos = (const uint32_t*)(ws + L.off_pos[at]);
+    uint32_t* n_crossing = (uint32_t*)(ws + L.off_met);
+    uint32_t* met = n_crossing + 1;
+    uint32_t* crossing = (uint32_t*)(ws + L.off_crossing);
     float* head = (float*)(ws + L.off_head);
     float* tail = (float*)(ws + L.off_tail);
-    cudaError_t e = launch_pdl(sum_kernel<E, N>, grid, dim3(x, y), 0, st, keys, pos,
-                               (const E*)dY, s.T, s.V, s.C, scale, (E*)dtable, head, tail);
-    if (e == cudaSuccess && L.stretches > 1)
-        e = launch_pdl(join_kernel<E, N>, grid, dim3(x, y), 0, st, keys, s.T, s.V, s.C, scale,
-                       (const float*)head, (const float*)tail, (E*)dtable);
+    const size_t held = (size_t)y * L.stretch * 8;
+    cudaError_t e = cudaSuccess;
+    if (held > 48 * 1024)
+        e = cudaFuncSetAttribute(sum_kernel<E, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kMaxHeld * 8);
+    if (e == cudaSuccess)
+        e = launch_pdl(sum_kernel<E, N>, dim3(sum_blocks, col_blocks), dim3(x, y), held, st, keys,
+                       pos, (const E*)dY, s.T, s.V, s.C, L.stretch, scale, (E*)dtable, head, tail,
+                       met, crossing, n_crossing);
+    if (e == cudaSuccess)
+        e = launch_pdl(join_kernel<E, N>, dim3(join_blocks + zero_blocks, col_blocks),
+                       dim3(x, kJoinThreads / x), (size_t)kJoinThreads * N * 4, st, keys, s.T, s.V,
+                       s.C, L.stretch, join_blocks, scale, (const float*)head, (const float*)tail,
+                       (const uint32_t*)met, (const uint32_t*)crossing,
+                       (const uint32_t*)n_crossing, (E*)dtable);
     return e;
 }
 
@@ -504,11 +645,12 @@ flarepp_status embedding_bwd(const flarepp_embedding_shape* shape, const void* i
         const Span ins[2] = {{ids, (size_t)s.T * s.id_bytes}, {dY, (size_t)s.T * s.C * elem(s)}};
         if (!disjoint(outs, 3, ins, 2)) return FLAREPP_ERR_INVALID_ARGUMENT;
     }
-    if (cudaMemsetAsync(dtable, 0, out_bytes, st) != cudaSuccess) return FLAREPP_ERR_CUDA;
-    if (s.T == 0) return FLAREPP_OK;
+    if (s.T == 0)
+        return cudaMemsetAsync(dtable, 0, out_bytes, st) == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
     char* ws = (char*)workspace;
     int at = 0;
-    cudaError_t e = s.id_bytes == 4 ? sort<int32_t>(s, L, ids, ws, status, &at, st)
+    cudaError_t e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
+    if (e == cudaSuccess) e = s.id_bytes == 4 ? sort<int32_t>(s, L, ids, ws, status, &at, st)
                                     : sort<int64_t>(s, L, ids, ws, status, &at, st);
     if (e != cudaSuccess) return FLAREPP_ERR_CUDA;
     using B = __nv_bfloat16;
