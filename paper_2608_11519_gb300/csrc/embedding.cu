@@ -65,7 +65,7 @@ __device__ __forceinline__ int64_t row_of(I id, int64_t V, int* status) {
 
 // ------------------------------------------------------------------ lookup
 // threadIdx.x walks a row's vectors, threadIdx.y the block's rows; four rows a thread, so that
-// four table loads are in flight.
+// four table loads are in flight (eight: 22 us instead of 17 for 131,072 rows of 512 bytes).
 constexpr int kLookupRows = 4;
 
 template <typename E, int N, typename I>
@@ -256,27 +256,44 @@ __global__ void __launch_bounds__(kSortThreads)
 }
 
 // ------------------------------------------------------------------ sums
-// Thread (x, y) of a block sums N columns of one stretch of the sorted positions, a batch of rows
-// of dY in flight while the batch before is added. A run that lies within the stretch goes to the
+// Thread (x, y) of a block sums N columns of one stretch of the sorted positions. A run that lies within the stretch goes to the
 // table; one that began before it leaves its sum in head[stretch], one that begins here and goes on in
-// tail[stretch], and the stretch on the list of `crossing` runs (whose order does not matter: each
-// is a sum of its own). A run's first stretch sets the row's bit in `met`.
+// tail[stretch], and the stretch on a list of crossing runs: those of few parts from the front of
+// `crossing`, those of many from its back (the order does not matter: each run is a sum of its own).
+// A run's first stretch sets the row's bit in `met`.
 constexpr int kSumThreads = 256;
 constexpr int kMinStretch = 16, kMaxStretch = 256;
-constexpr int kMaxHeld = 8192;   // positions whose keys and places a block holds
+// a crossing run of more parts is joined by a whole block (what a row of threads can hold at once)
+constexpr int short_run(int n) { return n == 8 ? 4 : 8; }
+constexpr int kMaxHeld = 4096;   // positions whose keys and places a block holds
+constexpr int kBatch = 4;        // rows of a group of copies
+constexpr int kRing = 16;        // rows in flight per thread
 constexpr int kJoinThreads = 1024;
-constexpr int kZeroRows = 32;    // rows per warp that writes zeros: a word of `met`
+constexpr int kZeroRows = 8;     // rows per warp that writes zeros
+
+// An asynchronous copy of one vector into shared memory (two bytes, which the instruction does not
+// know, at once).
+template <typename E, int N>
+__device__ __forceinline__ void copy_async(Vec<E, N>* dst, const E* src) {
+    constexpr int kBytes = sizeof(E) * N;
+    if constexpr (kBytes >= 4)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(tc::smem_u32(dst)), "l"(src),
+                     "n"(kBytes)
+                     : "memory");
+    else
+        *dst = load_vec<E, N>(src);
+}
 
 template <typename E, int N>
-__device__ void zero_rows(const uint32_t* __restrict__ met, int64_t word, int64_t V, int64_t C,
+__device__ void zero_rows(const uint32_t* __restrict__ met, int64_t group, int64_t V, int64_t C,
                           E* __restrict__ dtable) {
     const int lane = threadIdx.x % 32;
     Vec<E, N> zero;
 #pragma unroll
     for (int k = 0; k < N; ++k) from_f32(zero.v[k], 0.f);
-    const int64_t v0 = word * kZeroRows;
+    const int64_t v0 = group * kZeroRows;
     if (v0 >= V) return;
-    uint32_t gone = ~met[word];
+    uint32_t gone = ~met[v0 / 32] >> (v0 % 32) & ((1u << kZeroRows) - 1u);
     if (V - v0 < kZeroRows) gone &= (1u << (V - v0)) - 1u;
     while (gone) {
         const int v = __ffs(gone) - 1;
@@ -290,10 +307,12 @@ __global__ void __launch_bounds__(kSumThreads)
     sum_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos,
                const E* __restrict__ dY, int64_t T, int64_t V, int64_t C, int stretch, float scale,
                E* __restrict__ dtable, float* __restrict__ head, float* __restrict__ tail,
-               uint32_t* __restrict__ met, uint32_t* __restrict__ crossing,
+               uint32_t* __restrict__ met, uint32_t* __restrict__ crossing, int64_t stretches,
                uint32_t* __restrict__ n_crossing) {
-    constexpr int kBatch = sizeof(E) * N == 16 && N == 8 ? 4 : 8;  // two blocks fit an SM
-    extern __shared__ uint32_t held[];  // the block's keys, its positions
+    extern __shared__ uint8_t sum_smem[];
+    // the rows in flight, a slot per thread: [kRing][kSumThreads]; the block's keys; its positions
+    Vec<E, N>* ring = reinterpret_cast<Vec<E, N>*>(sum_smem);
+    uint32_t* held = reinterpret_cast<uint32_t*>(sum_smem + sizeof(Vec<E, N>) * kRing * kSumThreads);
     const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -323,7 +342,13 @@ __global__ void __launch_bounds__(kSumThreads)
     auto flush = [&](bool more) {
         if (began && first) {
             atomicOr(met + (cur >> 5), 1u << (cur & 31));
-            if (more) crossing[atomicAdd(n_crossing, 1u)] = (uint32_t)st;
+            if (more) {
+                const int64_t far = (st + 1 + short_run(N)) * stretch;
+                if (far < T && keys[far] == cur)
+                    crossing[stretches - 1 - atomicAdd(n_crossing + 1, 1u)] = (uint32_t)st;
+                else
+                    crossing[atomicAdd(n_crossing, 1u)] = (uint32_t)st;
+            }
         }
         if (began && !more) {
             Vec<E, N> o;
@@ -337,64 +362,98 @@ __global__ void __launch_bounds__(kSumThreads)
             *reinterpret_cast<Vec<float, N>*>((began ? tail : head) + st * C + c) = o;
         }
     };
-    Vec<E, N> x[2][kBatch];
-    auto fetch = [&](Vec<E, N>* d, int i) {
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-            if (key[i + k] != (uint32_t)V) d[k] = load_vec<E, N>(dY + (int64_t)at[i + k] * C + c);
-    };
-    auto take = [&](const Vec<E, N>* d, int i) {  // false at the first empty position
+    // Batches of rows come in by asynchronous copies, each thread's vectors into slots of its own:
+    // kRing rows in flight per thread without registers to hold them.
+    auto fetch = [&](int batch) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            if (key[i + k] != cur) {
+            const int i = batch * kBatch + k;
+            if (i < stretch && key[i] != (uint32_t)V)
+                copy_async(ring + (i % kRing) * kSumThreads + tid,
+                           dY + (int64_t)at[i] * C + c);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int b = 0; b < kRing / kBatch - 1; ++b) fetch(b);
+    for (int b = 0; b < stretch / kBatch; ++b) {
+        fetch(b + kRing / kBatch - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing / kBatch - 1) : "memory");
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int i = b * kBatch + k;
+            if (key[i] != cur) {
                 flush(false);
                 began = true;
-                cur = key[i + k];
+                cur = key[i];
 #pragma unroll
                 for (int j = 0; j < N; ++j) acc[j] = 0.f;
-                if (cur == (uint32_t)V) return false;
+                if (cur == (uint32_t)V) return;  // only empty positions follow, none was fetched
             }
+            const Vec<E, N> x = ring[(i % kRing) * kSumThreads + tid];
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] += to_f32(d[k].v[j]);
+            for (int j = 0; j < N; ++j) acc[j] += to_f32(x.v[j]);
         }
-        return true;
-    };
-    // stretches are multiples of two batches
-    fetch(x[0], 0);
-    for (int i = 0; i < stretch; i += 2 * kBatch) {
-        fetch(x[1], i + kBatch);
-        if (!take(x[0], i)) return;
-        if (i + 2 * kBatch < stretch) fetch(x[0], i + 2 * kBatch);
-        if (!take(x[1], i + kBatch)) return;
     }
     flush(goes_on);
 }
 
-// The runs that cross stretches, a block at a time: its threads look at one stretch each to find
-// where the run ends, its rows of threads add equal shares of the parts in order, and the shares are
-// added in order. Blocks from `join_blocks` on write the zeros of the rows that no id names.
+// The runs that cross stretches. Blocks below `join_blocks` take the runs of many parts one at a
+// time: the threads look at one stretch each to find where the run ends, the rows of threads add equal
+// shares of the parts in order, and the shares are added in order. The next `join_blocks` blocks take the
+// runs of up to short_run parts, a row of threads each. The rest write the zeros of the rows that no id
+// names.
 template <typename E, int N>
 __global__ void __launch_bounds__(kJoinThreads)
     join_kernel(const uint32_t* __restrict__ keys, int64_t T, int64_t V, int64_t C, int stretch,
                 unsigned join_blocks, float scale, const float* __restrict__ head,
                 const float* __restrict__ tail, const uint32_t* __restrict__ met,
-                const uint32_t* __restrict__ crossing, const uint32_t* __restrict__ n_crossing,
-                E* __restrict__ dtable) {
+                const uint32_t* __restrict__ crossing, int64_t stretches,
+                const uint32_t* __restrict__ n_crossing, E* __restrict__ dtable) {
     extern __shared__ float share[];  // [blockDim.y][blockDim.x * N]
     const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     tc::pdl_trigger();
     tc::pdl_wait();
-    if (blockIdx.x >= join_blocks) {
+    if (blockIdx.x >= 2 * join_blocks) {
         if (blockIdx.y == 0)
-            zero_rows<E, N>(met, (int64_t)(blockIdx.x - join_blocks) * (kJoinThreads / 32) + tid / 32,
+            zero_rows<E, N>(met,
+                            (int64_t)(blockIdx.x - 2 * join_blocks) * (kJoinThreads / 32) + tid / 32,
                             V, C, dtable);
         return;
     }
-    const unsigned n = *n_crossing;
     const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
+    if (blockIdx.x >= join_blocks) {
+        constexpr int kShortRun = short_run(N);
+        const unsigned n = n_crossing[0], step = join_blocks * blockDim.y;
+        if (c >= C) return;
+        for (unsigned item = (blockIdx.x - join_blocks) * blockDim.y + threadIdx.y; item < n; item += step) {
+            const int64_t st = crossing[item];
+            const uint32_t key = keys[(st + 1) * stretch];
+            Vec<float, N> part[kShortRun];
+            bool in[kShortRun];
+#pragma unroll
+            for (int p = 0; p < kShortRun; ++p) {
+                const int64_t at = (st + 1 + p) * stretch;
+                in[p] = at < T && keys[at] == key;
+                if (in[p]) part[p] = *reinterpret_cast<const Vec<float, N>*>(head + (st + 1 + p) * C + c);
+            }
+            Vec<float, N> acc = *reinterpret_cast<const Vec<float, N>*>(tail + st * C + c);
+#pragma unroll
+            for (int p = 0; p < kShortRun; ++p)
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (in[p]) acc.v[k] += part[p].v[k];
+            Vec<E, N> o;
+#pragma unroll
+            for (int k = 0; k < N; ++k) from_f32(o.v[k], acc.v[k] * scale);
+            store_vec<E, N>(dtable + (int64_t)key * C + c, o);
+        }
+        return;
+    }
+    const unsigned n = n_crossing[1];
     const int row = blockDim.x * N;
     for (unsigned item = blockIdx.x; item < n; item += join_blocks) {
-        const int64_t st = crossing[item];
+        const int64_t st = crossing[stretches - 1 - item];
         const uint32_t key = keys[(st + 1) * stretch];
         int64_t parts = 0;  // stretches st + 1 .. st + parts begin with the run's key
         for (;;) {
@@ -471,7 +530,7 @@ SortPlan sort_plan(const flarepp_embedding_shape& s) {
     while (((int64_t)1 << bits) <= s.V) ++bits;  // keys 0..V
     p.passes = (int)cdiv(bits, kMaxBits);
     p.bits = (int)cdiv(bits, p.passes);
-    p.tile = cdiv(cdiv(s.T, kNumSMs), 1024) * 1024;  // about a block per SM
+    p.tile = cdiv(cdiv(s.T, 2 * kNumSMs), 512) * 512;  // about two blocks per SM
     p.tiles = cdiv(s.T, p.tile);
     return p;
 }
@@ -480,15 +539,15 @@ struct Layout {
     SortPlan sort;
     int stretch;
     int64_t stretches;
-    size_t off_met, met_bytes;  // the number of crossing runs, then a bit per row
+    size_t off_met, met_bytes;  // the numbers of short and long crossing runs, then a bit per row
     size_t off_crossing, off_keys[2], off_pos[2], off_hist, off_total, off_head, off_tail, total;
 };
 Layout layout_of(const flarepp_embedding_shape& s) {
     Layout L{};
     L.sort = sort_plan(s);
-    // stretches so long that about sixteen rows of threads per SM have one each
+    // stretches so long that about 24 warps per SM have one each
     const int64_t vecs = cdiv(s.C, vec_of(s)), x = lanes_for(vecs, 32);
-    const int64_t want = cdiv(s.T * cdiv(vecs, x) * x, (int64_t)16 * 32 * kNumSMs);
+    const int64_t want = cdiv(s.T * cdiv(vecs, x) * x, (int64_t)24 * 32 * kNumSMs);
     int64_t most = kMaxHeld / (kSumThreads / x);
     if (most > kMaxStretch) most = kMaxStretch;
     L.stretch = (int)(cdiv(want, kMinStretch) * kMinStretch);
@@ -501,7 +560,7 @@ Layout layout_of(const flarepp_embedding_shape& s) {
         return at;
     };
     const int64_t bins = (int64_t)1 << L.sort.bits;
-    L.met_bytes = 4 + (size_t)cdiv(s.V, 32) * 4;
+    L.met_bytes = 8 + (size_t)cdiv(s.V, 32) * 4;
     L.off_met = take((int64_t)L.met_bytes);
     L.off_crossing = take(L.stretches * 4);
     for (int i = 0; i < 2; ++i) {
@@ -572,29 +631,30 @@ cudaError_t sums(const flarepp_embedding_shape& s, const Layout& L, int at, cons
     const int x = lanes_for(vecs, 32), y = kSumThreads / x;
     const unsigned col_blocks = (unsigned)cdiv(vecs, x);
     const unsigned sum_blocks = (unsigned)cdiv(L.stretches, y);
-    const unsigned join_blocks = L.stretches < 2 * kNumSMs ? (unsigned)L.stretches : 2 * kNumSMs;
+    const unsigned join_blocks = L.stretches < kNumSMs ? (unsigned)L.stretches : kNumSMs;
     const unsigned zero_blocks = (unsigned)cdiv(s.V, kZeroRows * (kJoinThreads / 32));
     const uint32_t* keys = (const uint32_t*)(ws + L.off_keys[at]);
     const uint32_t* pos = (const uint32_t*)(ws + L.off_pos[at]);
     uint32_t* n_crossing = (uint32_t*)(ws + L.off_met);
-    uint32_t* met = n_crossing + 1;
+    uint32_t* met = n_crossing + 2;
     uint32_t* crossing = (uint32_t*)(ws + L.off_crossing);
     float* head = (float*)(ws + L.off_head);
     float* tail = (float*)(ws + L.off_tail);
-    const size_t held = (size_t)y * L.stretch * 8;
+    constexpr size_t kRingBytes = sizeof(E) * N * kRing * kSumThreads;
+    const size_t held = kRingBytes + (size_t)y * L.stretch * 8;
     cudaError_t e = cudaSuccess;
     if (held > 48 * 1024)
         e = cudaFuncSetAttribute(sum_kernel<E, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kMaxHeld * 8);
+                                 (int)kRingBytes + kMaxHeld * 8);
     if (e == cudaSuccess)
         e = launch_pdl(sum_kernel<E, N>, dim3(sum_blocks, col_blocks), dim3(x, y), held, st, keys,
                        pos, (const E*)dY, s.T, s.V, s.C, L.stretch, scale, (E*)dtable, head, tail,
-                       met, crossing, n_crossing);
+                       met, crossing, L.stretches, n_crossing);
     if (e == cudaSuccess)
-        e = launch_pdl(join_kernel<E, N>, dim3(join_blocks + zero_blocks, col_blocks),
+        e = launch_pdl(join_kernel<E, N>, dim3(2 * join_blocks + zero_blocks, col_blocks),
                        dim3(x, kJoinThreads / x), (size_t)kJoinThreads * N * 4, st, keys, s.T, s.V,
                        s.C, L.stretch, join_blocks, scale, (const float*)head, (const float*)tail,
-                       (const uint32_t*)met, (const uint32_t*)crossing,
+                       (const uint32_t*)met, (const uint32_t*)crossing, L.stretches,
                        (const uint32_t*)n_crossing, (E*)dtable);
     return e;
 }
