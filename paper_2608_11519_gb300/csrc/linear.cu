@@ -15,7 +15,93 @@ constexpr int64_t kFewRows = 128;
 constexpr int kDzCols = 256;  // columns per block of dz_kernel: 32 lanes x 8
 constexpr int kDzRows = 8;    // rows a block of dz_kernel reads at once
 
+// Rows up to which the layer runs on the CUDA cores (gemv_kernel): a weight then meets so few
+// multiplications that its bytes are the bound, and one launch without workspace is the shortest
+// path (one row of 2048 -> 2048: 7.0 us through the tensor cores and their chunk sums).
+constexpr int64_t kGemvRows = 4;
+constexpr int kGemvWarps = 8;
+
 int64_t pad8(int64_t n) { return cdiv(n, 8) * 8; }
+
+// The layer for T <= RT rows, `in` a multiple of 8. A warp takes RW rows of W at a time, a lane every
+// 32nd vector of eight weights of each, U of them in flight (RW * U = 8 loads of 16 bytes a lane
+// keep the memory busy from a thousand warps); `split` warps share a row where there are few rows of
+// W, and their sums are added in order.
+template <int RT, int RW>
+__global__ void __launch_bounds__(kGemvWarps * 32)
+    gemv_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W, int T,
+                int K, int N, int split, int act, const __nv_bfloat16* __restrict__ bias,
+                const __nv_bfloat16* __restrict__ R, __nv_bfloat16* __restrict__ Y,
+                __nv_bfloat16* __restrict__ Z) {
+    constexpr int U = 8 / RW;
+    __shared__ float sums[kGemvWarps][RW][RT];
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int share = warp % split;
+    const int n0 = (blockIdx.x * (kGemvWarps / split) + warp / split) * RW;
+    const int vecs = K / 8, per = (vecs + split - 1) / split;
+    const int v1 = min(vecs, (share + 1) * per);
+    uint64_t acc[RW][RT];
+#pragma unroll
+    for (int r = 0; r < RW; ++r)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[r][t] = 0;
+    for (int v = share * per + lane; v < v1; v += 32 * U) {
+        uint4 w[U][RW];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < RW; ++r)
+                w[u][r] = v + 32 * u < v1 && n0 + r < N
+                              ? __ldg(reinterpret_cast<const uint4*>(W + (int64_t)(n0 + r) * K) + v + 32 * u)
+                              : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (v + 32 * u >= v1) break;
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                if (t >= T) break;
+                const uint4 x = __ldg(reinterpret_cast<const uint4*>(X + (int64_t)t * K) + v + 32 * u);
+                const uint64_t x0 = unpack_bf16x2(x.x), x1 = unpack_bf16x2(x.y);
+                const uint64_t x2 = unpack_bf16x2(x.z), x3 = unpack_bf16x2(x.w);
+#pragma unroll
+                for (int r = 0; r < RW; ++r) {
+                    acc[r][t] = fma2(x0, unpack_bf16x2(w[u][r].x), acc[r][t]);
+                    acc[r][t] = fma2(x1, unpack_bf16x2(w[u][r].y), acc[r][t]);
+                    acc[r][t] = fma2(x2, unpack_bf16x2(w[u][r].z), acc[r][t]);
+                    acc[r][t] = fma2(x3, unpack_bf16x2(w[u][r].w), acc[r][t]);
+                }
+            }
+        }
+    }
+    float mine = 0.f;  // the sum of output (r, t) in lane r * RT + t
+#pragma unroll
+    for (int r = 0; r < RW; ++r)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const float2 f = halves(acc[r][t]);
+            float s = f.x + f.y;
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (lane == r * RT + t) mine = s;
+        }
+    const int r = lane / RT, t = lane % RT, n = n0 + r;
+    if (split > 1) {
+        if (lane < RW * RT) sums[warp][r][t] = mine;
+        __syncthreads();
+        if (share) return;
+        if (lane < RW * RT)
+            for (int k = 1; k < split; ++k) mine += sums[warp + k][r][t];
+    }
+    if (lane >= RW * RT || t >= T || n >= N) return;
+    if (bias) mine += __bfloat162float(bias[n]);
+    const int64_t at = (int64_t)t * N + n;
+    if (Z) Z[at] = __float2bfloat16_rn(mine);
+    float y = halves(act_value2(act, pair(mine, mine))).x;
+    if (R) y += __bfloat162float(R[at]);
+    Y[at] = __float2bfloat16_rn(y);
+}
 
 // dst [rows][pitch] = src [rows][cols] with zeros behind each row: the 16-byte line pitch that
 // TMA asks for. One thread per eight values.
@@ -214,12 +300,15 @@ size_t part_bytes(const LinPlan& p, int64_t rows, int64_t cols) {
 }
 
 struct FwdLayout {
+    bool gemv;
     LinPlan plan;
     bool split;  // the sums go through partials and finish_kernel
     size_t off_x, off_w, off_part, total;
 };
 FwdLayout fwd_layout(const Shape& s) {
     FwdLayout L{};
+    L.gemv = s.T <= kGemvRows && s.K % 8 == 0;
+    if (L.gemv) return L;
     const bool few = s.T <= kFewRows;
     L.plan = few ? lin_plan(s.N, s.T, s.K, true) : lin_plan(s.T, s.N, s.K, false);
     L.split = few || L.plan.chunks > 1;
@@ -294,6 +383,21 @@ cudaError_t product(const LinPlan& plan, bool split, int64_t rows, int64_t cols,
     return err != cudaSuccess ? err : finish(part, plan, rows, cols, e, st);
 }
 
+template <int RT>
+cudaError_t gemv(const Shape& s, const void* X, const void* W, const LinEpilogue& e,
+                 cudaStream_t st) {
+    // four rows of W at once where a row alone is less than half of a warp's loads in flight
+    const int rw = s.K <= 1024 ? 4 : 1;
+    int split = 1;  // at least eight warps per SM, and half a kilobyte of a row for each
+    while (split < kGemvWarps && cdiv(s.N, rw) * split < 8 * kNumSMs && s.K / split > 512) split *= 2;
+    const unsigned blocks = (unsigned)cdiv(cdiv(s.N, rw), kGemvWarps / split);
+    auto kernel = rw == 4 ? gemv_kernel<RT, 4> : gemv_kernel<RT, 1>;
+    using B = __nv_bfloat16;
+    return launch_pdl(kernel, dim3(blocks), dim3(kGemvWarps * 32), 0, st, (const B*)X, (const B*)W,
+                      (int)s.T, (int)s.K, (int)s.N, split, e.act, (const B*)e.bias,
+                      (const B*)e.R, (B*)e.Y, (B*)e.Z);
+}
+
 flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, const void* W,
                           const void* b, const void* R, void* Y, void* Z, void* workspace,
                           size_t workspace_bytes, int32_t* status, cudaStream_t st) {
@@ -312,6 +416,13 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
     const Span ins[4] = {{X, (size_t)s.T * s.K * 2}, {W, (size_t)s.N * s.K * 2},
                          {b, (size_t)s.N * 2}, {R, y_bytes}};
     if (!disjoint(outs, 4, ins, 4)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    const LinEpilogue e{s.act, b, R, Y, Z, nullptr, 0};
+    if (L.gemv) {
+        const cudaError_t err = s.T == 1   ? gemv<1>(s, X, W, e, st)
+                                : s.T == 2 ? gemv<2>(s, X, W, e, st)
+                                           : gemv<4>(s, X, W, e, st);
+        return err == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
+    }
     char* ws = (char*)workspace;
     LinOperand x{X, s.K, 0}, w{W, s.K, 0};
     if (s.K % 8) {
@@ -321,7 +432,6 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
         x = {ws + L.off_x, pad8(s.K), 0};
         w = {ws + L.off_w, pad8(s.K), 0};
     }
-    const LinEpilogue e{s.act, b, R, Y, Z, nullptr, 0};
     return product(L.plan, L.split, s.T, s.N, s.K, x, w, e, (float*)(ws + L.off_part), status,
                    st) == cudaSuccess
                ? FLAREPP_OK

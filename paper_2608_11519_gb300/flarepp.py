@@ -722,19 +722,20 @@ STATE_BLOCK = 256  # values that share one scale in an 8-bit optimiser state
 def _need(t, what, shape, dtype, device, optional=False):
     """A contiguous tensor of this shape, dtype and CUDA device; returns its address (0 for an
     optional one that is missing)."""
-    if t is None and optional:
+    if isinstance(t, torch.Tensor):
+        if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+            return t.data_ptr()
+    elif t is None and optional:
         return 0
-    if not isinstance(t, torch.Tensor):
+    else:
         raise TypeError(f"{what} must be a torch tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what} has dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{what} is on {t.device}, expected {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{what} must be contiguous")
 
 
 def _cuda_device(t, what):
@@ -745,12 +746,29 @@ def _cuda_device(t, what):
     return t.device
 
 
+_ENTRIES = {}  # name -> entry point
+
+
+def _entry(name):
+    fn = _ENTRIES.get(name)
+    if fn is None:
+        fn = _ENTRIES[name] = getattr(load(), "flarepp_" + name)
+    return fn
+
+
+def _current_stream(device):
+    """The handle of torch's current stream on ``device``."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # spares building a Stream object
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
+
+
 def _enqueue(name, device, stream, *args):
     """Call entry ``flarepp_<name>`` with the device current, the stream as last argument."""
-    fn = getattr(load(), "flarepp_" + name)
+    fn = _entry(name)
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        handle = _current_stream(device)
+    else:
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     if torch.cuda.current_device() == device.index:
         rc = fn(*args, handle)
     else:
@@ -762,10 +780,12 @@ def _enqueue(name, device, stream, *args):
 
 def _scratch(workspace, nbytes, device):
     """(tensor to keep until the call is enqueued, its address, its bytes)"""
+    if nbytes == 0 and workspace is None:
+        return None, 0, 0
     if isinstance(workspace, Workspace):
         buf = workspace.get(nbytes, device)
     elif workspace is None:
-        buf = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
     else:
         _check_device("the call", device, workspace=workspace)
         buf = workspace
@@ -805,7 +825,7 @@ def _linear(X, W, b, residual, act, Y, Z, keep, workspace, status, stream):
     yp = _need(Y, "Y", shape, dt, dev)
     zp = _need(Z, "Z", shape, dt, dev, optional=True)
     ref = ctypes.byref(s)
-    buf, wsp, wsn = _scratch(workspace, load().flarepp_linear_workspace_bytes(ref), dev)
+    buf, wsp, wsn = _scratch(workspace, _entry("linear_workspace_bytes")(ref), dev)
     _enqueue("linear_fwd", dev, stream, ref, xp, wp, bp, rp, yp, zp, wsp, wsn,
              _status_word(status, dev))
     return Y, Z
@@ -849,7 +869,7 @@ def linear_bwd(X, W, dY, Z=None, act="none", bias=True, dX=None, dW=None, db=Non
     dwp = _need(dW, "dW", W.shape, dt, dev, optional=True)
     dbp = _need(db, "db", (s.out,), dt, dev, optional=True)
     ref = ctypes.byref(s)
-    buf, wsp, wsn = _scratch(workspace, load().flarepp_linear_bwd_workspace_bytes(ref), dev)
+    buf, wsp, wsn = _scratch(workspace, _entry("linear_bwd_workspace_bytes")(ref), dev)
     _enqueue("linear_bwd", dev, stream, ref, xp, wp, zp, gp, dxp, dwp, dbp, wsp, wsn,
              _status_word(status, dev))
     return dX, dW, db
@@ -901,7 +921,7 @@ def embedding_bwd(ids, dY, V, scale=1.0, dtable=None, workspace=None, status=Non
         dtable = torch.empty((V, C), dtype=dt, device=dev)
     s = EmbeddingShape(ids.numel(), V, C, _DTYPES[dt], size)
     ref = ctypes.byref(s)
-    buf, wsp, wsn = _scratch(workspace, load().flarepp_embedding_bwd_workspace_bytes(ref), dev)
+    buf, wsp, wsn = _scratch(workspace, _entry("embedding_bwd_workspace_bytes")(ref), dev)
     _enqueue("embedding_bwd", dev, stream, ref, ip, gp, float(scale),
              _need(dtable, "dtable", (V, C), dt, dev), wsp, wsn, _status_word(status, dev))
     return dtable
