@@ -11,9 +11,10 @@
 // tiles is persistent; chunks cut a long contraction when there are few tiles.
 //
 // Roles (20 warps): warp 0 the TMA producer, warp 1 the MMA issuer (in the pair's leader),
-// warps 4..19 the epilogue: each takes one 32-row x 64-column block of the tile (TMEM lane = tile
-// row), in two halves of 32 columns. Two TMEM accumulators of 256 columns let the epilogue of a tile
-// overlap the products of the next. Sixteen epilogue warps, because a memory-bound layer leaves
+// warps 4..19 the epilogue: two groups of eight warps take the tiles in turn, so that one group's
+// loads and stores fall into the other one's arithmetic; a warp takes four 32-row x 32-column blocks of
+// a tile (TMEM lane = tile row), staged in shared memory by turns for their TMA stores. Group g reads TMEM accumulator g
+// of 256 columns, so the epilogue of a tile overlaps the products of the next. Sixteen epilogue warps, because a memory-bound layer leaves
 // about 16 issue slots per output value for everything, and the activation's chain of dependent
 // instructions needs four warps per scheduler to hide (with eight warps of 64 columns a half and
 // unpaired arithmetic the 65,536 x 256 -> 512 GELU layer took 46 us). Every wait is bounded (2 s of %globaltimer): on expiry the kernel records
@@ -41,7 +42,8 @@ constexpr int kMaxNT = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int kMaxStages = 8;
-constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + kEpiWarps;
+constexpr int kBlockBytes = 32 * 32 * 2;  // what an epilogue warp stages at a time
+constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + 2 * kEpiWarps;
 
 enum Out { kOutEpilogue, kOutPart, kOutPartT };
 
@@ -49,8 +51,8 @@ template <int CG, int OUT>
 struct Cfg {
     static constexpr int kBTile = kMaxNT / CG * kSlice * 2;
     static constexpr int kStage = kATile + kBTile;
-    // per epilogue warp: one 32-row x 64-column bf16 block
-    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * 4096 : 0;
+    // per epilogue warp: two 32-row x 32-column bf16 blocks
+    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * 2 * kBlockBytes : 0;
     static constexpr int kFit = (232448 - 1024 - kStaging - kNumBars * 8 - 16) / kStage;
     static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
     static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kNumBars * 8 + 16;
@@ -160,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t accfull0 = empty0 + 8u * kMaxStages;
     const uint32_t accempty0 = accfull0 + 16u;
     const uint32_t fin = accempty0 + 16u;
-    const uint32_t rfull0 = fin + 8u;  // one per epilogue warp
+    const uint32_t rfull0 = fin + 8u;  // one per staged block
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
@@ -173,10 +175,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(accfull0 + 8u * b, 1);
-            mbar_init(accempty0 + 8u * b, kEpiWarps * CG);
+            mbar_init(accempty0 + 8u * b, kEpiWarps / 2 * CG);
         }
         mbar_init(fin, 1);
-        for (int w = 0; w < kEpiWarps; ++w) mbar_init(rfull0 + 8u * w, 1);
+        for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(rfull0 + 8u * w, 1);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tmap(&tmA);
@@ -301,161 +303,146 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp >= kFirstEpiWarp) {
         // ------------------------------------------------------------ epilogue
         const int e = warp - kFirstEpiWarp;
-        const int q = warp % 4;  // the TMEM lanes this warp may read
-        const int c = 64 * (e / 4);
-        uint8_t* block = staging + e * 4096;
-        uint8_t* line = block + lane * 128;
-        const uint32_t rfull = rfull0 + 8u * e;
-        uint32_t j = 0, r_phase = 0;
-        bool r_pending = false;
-        for (int v = first; v < prm.n_work; v += pairs, ++j) {
+        const int ab = e / (kEpiWarps / 2);  // this warp's group and accumulator
+        const int q = warp % 4;              // the TMEM lanes this warp may read
+        const int cfirst = 64 * (e % (kEpiWarps / 2) / 4);
+        uint8_t* staged = staging + e * 2 * kBlockBytes;
+        // 16-byte piece g of this lane's row in a staged block, swizzled as the maps expect it
+        auto piece = [&](int h, int g) {
+            return reinterpret_cast<uint4*>(staged + h * kBlockBytes + lane * 64 +
+                                            ((g ^ (lane >> 1 & 3)) << 4));
+        };
+        const uint32_t rfull = rfull0 + 16u * e;
+        uint32_t phase = 0, r_phase = 0;
+        bool ok = true;
+        for (int v = first + ab * pairs; v < prm.n_work && ok; v += 2 * pairs, phase ^= 1) {
             const Work w = work_of(prm, v);
-            const int ab = j & 1;
             const int row0 = (w.rt * CG + (int)rank) * 128 + 32 * q;
-            const int col0 = w.ct * prm.NT + c;
-            const bool live = c < prm.NT && row0 < prm.M && col0 < prm.N;
-            const uint32_t acc = tmem + ((uint32_t)(32 * q) << 16) + ab * kMaxNT + c;
-            // the block of R, into the buffer that Y leaves from
-            auto fetch_r = [&] {
+            const int n0 = w.ct * prm.NT;  // first column of the tile
+            // columns of the tile that exist
+            const int width = row0 < prm.M ? min(prm.NT, prm.N - n0) : 0;
+            const int rows = min(32, prm.M - row0);
+            const uint32_t acc = tmem + ((uint32_t)(32 * q) << 16) + ab * kMaxNT;
+            const bool tma_r = OUT == kOutEpilogue && prm.R && prm.tma_out;
+            // block h of R at column c, into the staged block that Y leaves from
+            auto fetch_r = [&](int h, int c) {
                 if (lane == 0) {
-                    bulk_wait_read();
-                    mbar_expect_tx(rfull, 4096);
-                    tma_load_2d(smem_u32(block), &tmR, col0, row0, rfull);
-                }
-                r_pending = true;
-            };
-            const bool tma_r = OUT == kOutEpilogue && live && prm.R && prm.tma_out;
-            if (tma_r && !prm.Z) fetch_r();
-            if (!warp_wait<CG>(accfull0 + 8u * ab, (j >> 1) & 1, abort_flag, prm.status)) break;
-            tc_fence_after();
-            auto release = [&] {  // this warp has read its part of the accumulator
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
-                    else mbar_arrive(accempty0 + 8u * ab);
+                    mbar_expect_tx(rfull + 8u * h, kBlockBytes);
+                    tma_load_2d(smem_u32(staged + h * kBlockBytes), &tmR, n0 + c, row0, rfull + 8u * h);
                 }
             };
-            if (!live) {
-                release();
-                continue;
+            if (tma_r && !prm.Z) {  // ahead of the products
+                if (lane == 0) bulk_wait_read();
+                for (int h = 0; h < 2; ++h)
+                    if (cfirst + 32 * h < width) fetch_r(h, cfirst + 32 * h);
             }
-            if (OUT != kOutEpilogue) {
-                const int row = row0 + lane;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
+            ok = warp_wait<CG>(accfull0 + 8u * ab, phase, abort_flag, prm.status);
+            tc_fence_after();
+            for (int c = cfirst; c < width && ok; c += c % 64 ? 96 : 32) {
+                const int h = c / 32 & 1;  // staged block
+                if (OUT != kOutEpilogue) {
                     float x[32];
-                    tmem_ld32(acc + 32 * h, reinterpret_cast<uint32_t*>(x));
+                    tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(x));
                     tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
-                    if (h == 1) release();
+                    const int row = row0 + lane, at = n0 + c;
                     if (row >= prm.M) continue;
                     if (OUT == kOutPart) {
-                        const int at = col0 + 32 * h;
                         float* d = prm.part + ((int64_t)w.chunk * prm.M + row) * prm.ldp + at;
-                        const int n = min(prm.NT - c - 32 * h, (int)prm.ldp - at);
+                        const int n = min(prm.NT - c, (int)prm.ldp - at);
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
                             if (i < n)
                                 *reinterpret_cast<float4*>(d + i) =
                                     make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
                     } else {
-                        const int at = col0 + 32 * h;
                         float* d = prm.part + ((int64_t)w.chunk * prm.N + at) * prm.ldp + row;
-                        const int n = min(prm.NT - c - 32 * h, prm.N - at);
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i < n) d[i * prm.ldp] = x[i];
+                            if (i < width - c) d[i * prm.ldp] = x[i];
                     }
+                    continue;
                 }
-                continue;
-            }
-            // Columns 32 h .. 32 h + 31 of the block: sums with the bias, as 16 pairs.
-            auto load_half = [&](int h, uint64_t* x) {
-                uint32_t r[32];
-                tmem_ld32(acc + 32 * h, r);
-                tmem_wait_ld32(r);
+                // sums with the bias, as 16 pairs
+                uint64_t x[16];
+                auto load = [&] {
+                    uint32_t r[32];
+                    uint4 u[4];
+                    const int at = n0 + c;
+                    const bool whole = at + 32 <= prm.N;
+                    if (prm.bias && whole)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    x[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-                if (!prm.bias) return;
-                const int at = col0 + 32 * h;
-                if (at + 32 <= prm.N) {
-                    const uint4* b4 = reinterpret_cast<const uint4*>(prm.bias + at);
+                        for (int g = 0; g < 4; ++g)
+                            u[g] = __ldg(reinterpret_cast<const uint4*>(prm.bias + at) + g);
+                    tmem_ld32(acc + c, r);
+                    tmem_wait_ld32(r);
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const uint4 u = __ldg(b4 + g);
-                        x[4 * g] = add2(x[4 * g], unpack_bf16x2(u.x));
-                        x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u.y));
-                        x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u.z));
-                        x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u.w));
+                    for (int i = 0; i < 16; ++i)
+                        x[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+                    if (!prm.bias) return;
+                    if (whole) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            x[4 * g] = add2(x[4 * g], unpack_bf16x2(u[g].x));
+                            x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u[g].y));
+                            x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u[g].z));
+                            x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u[g].w));
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int n = at + 2 * i;
+                            x[i] = add2(x[i], pair(n < prm.N ? __bfloat162float(prm.bias[n]) : 0.f,
+                                                   n + 1 < prm.N ? __bfloat162float(prm.bias[n + 1]) : 0.f));
+                        }
                     }
-                } else {
+                };
+                auto store = [&](int hb) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int n = at + 2 * i;
-                        x[i] = add2(x[i], pair(n < prm.N ? __bfloat162float(prm.bias[n]) : 0.f,
-                                               n + 1 < prm.N ? __bfloat162float(prm.bias[n + 1]) : 0.f));
+                    for (int g = 0; g < 4; ++g)
+                        *piece(hb, g) = make_uint4(pack_bf16x2(x[4 * g]), pack_bf16x2(x[4 * g + 1]),
+                                                   pack_bf16x2(x[4 * g + 2]), pack_bf16x2(x[4 * g + 3]));
+                };
+                // value (r, cc) of a staged block, for outputs whose lines TMA cannot address
+                auto value = [&](int hb, int r, int cc) {
+                    return reinterpret_cast<__nv_bfloat16*>(staged + hb * kBlockBytes + r * 64 +
+                                                            (((cc >> 3) ^ (r >> 1 & 3)) << 4) + (cc & 7) * 2);
+                };
+                const int cols = min(32, width - c);
+                auto flush = [&](int hb, const CUtensorMap* map, __nv_bfloat16* out) {
+                    if (prm.tma_out) {
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(map, smem_u32(staged + hb * kBlockBytes), n0 + c, row0);
+                            bulk_commit();
+                        }
+                    } else {
+                        __syncwarp();
+                        for (int r = 0; r < rows; ++r)
+                            if (lane < cols)
+                                out[(int64_t)(row0 + r) * prm.N + n0 + c + lane] = *value(hb, r, lane);
+                        __syncwarp();
                     }
+                };
+                // Without Z and R, block h was last stored two blocks ago; with Z the two staged blocks are
+                // Z's and Y's, and each waits for the store before.
+                const int hy = prm.Z ? 0 : h;
+                load();
+                if (prm.Z) {
+                    if (lane == 0) bulk_wait_read();
+                    __syncwarp();
+                    store(1);
+                    flush(1, &tmZ, prm.Z);
+                    if (tma_r) fetch_r(0, c);
                 }
-            };
-            // The block goes through shared memory swizzled as the store map undoes it: 16-byte
-            // piece g of row r at g ^ (r % 8), free of bank conflicts.
-            auto store_half = [&](int h, const uint64_t* x) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<uint4*>(line + (((4 * h + g) ^ (lane & 7)) << 4)) =
-                        make_uint4(pack_bf16x2(x[4 * g]), pack_bf16x2(x[4 * g + 1]),
-                                   pack_bf16x2(x[4 * g + 2]), pack_bf16x2(x[4 * g + 3]));
-            };
-            // value (r, cc) of the block, for outputs whose lines TMA cannot address
-            auto at_block = [&](int r, int cc) {
-                return reinterpret_cast<__nv_bfloat16*>(
-                    block + r * 128 + (((cc >> 3) ^ (r & 7)) << 4) + (cc & 7) * 2);
-            };
-            const int rows = min(32, prm.M - row0);
-            const int cols = min(64, min(prm.NT - c, prm.N - col0));
-            auto flush = [&](const CUtensorMap* map, __nv_bfloat16* out) {
-                if (prm.tma_out) {
-                    fence_proxy_async();
+                if (c + (c % 64 ? 96 : 32) >= width) {  // the last block: the accumulator is read
+                    tc_fence_before();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(map, smem_u32(block), col0, row0);
-                        bulk_commit();
+                        if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
+                        else mbar_arrive(accempty0 + 8u * ab);
                     }
-                } else {
-                    __syncwarp();
-                    for (int r = 0; r < rows; ++r)
-                        for (int cc = lane; cc < cols; cc += 32)
-                            out[(int64_t)(row0 + r) * prm.N + col0 + cc] = *at_block(r, cc);
-                    __syncwarp();
                 }
-            };
-            auto block_free = [&] {  // the stores from the block have read it
-                if (lane == 0) bulk_wait_read();
-                __syncwarp();
-            };
-            uint64_t x[16];
-            if (prm.Z) {
-                block_free();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    load_half(h, x);
-                    store_half(h, x);
-                }
-                flush(&tmZ, prm.Z);
-            }
-            if (tma_r && prm.Z) fetch_r();
-            if (prm.R && !prm.tma_out) {
-                for (int r = 0; r < rows; ++r)
-                    for (int cc = lane; cc < cols; cc += 32)
-                        *at_block(r, cc) = prm.R[(int64_t)(row0 + r) * prm.N + col0 + cc];
-                __syncwarp();
-            }
-            bool ok = true;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                load_half(h, x);
-                if (h == 1) release();
                 switch (prm.act) {
                     case FLAREPP_ACT_RELU:
 #pragma unroll
@@ -470,37 +457,49 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int i = 0; i < 16; ++i) x[i] = act_value2(FLAREPP_ACT_SILU, x[i]);
                         break;
                 }
-                if (h == 0) {
-                    if (tma_r) {
-                        ok = warp_wait<1>(rfull, r_phase, abort_flag, prm.status);
-                        if (ok) {
-                            r_phase ^= 1;
-                            r_pending = false;
-                        }
-                    } else if (!prm.R) {
-                        block_free();
-                    }
-                }
                 if (prm.R) {
+                    if (tma_r) {
+                        ok = warp_wait<1>(rfull + 8u * hy, r_phase >> hy & 1, abort_flag, prm.status);
+                        if (!ok) break;
+                        r_phase ^= 1u << hy;
+                    } else {
+                        for (int r = 0; r < rows; ++r)
+                            if (lane < cols)
+                                *value(hy, r, lane) = prm.R[(int64_t)(row0 + r) * prm.N + n0 + c + lane];
+                        __syncwarp();
+                    }
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(
-                            line + (((4 * h + g) ^ (lane & 7)) << 4));
+                        const uint4 u = *piece(hy, g);
                         x[4 * g] = add2(x[4 * g], unpack_bf16x2(u.x));
                         x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u.y));
                         x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u.z));
                         x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u.w));
                     }
+                } else if (!prm.Z) {
+                    if (lane == 0) bulk_wait_read_1();
+                    __syncwarp();
                 }
-                store_half(h, x);
+                store(hy);
+                flush(hy, &tmY, prm.Y);
+                if (tma_r && !prm.Z && c + 128 < width) {  // this block's place in the next pair of blocks
+                    if (lane == 0) bulk_wait_read();
+                    fetch_r(h, c + 128);
+                }
             }
-            if (!ok) break;
-            flush(&tmY, prm.Y);
+            if (ok && (width <= cfirst || OUT != kOutEpilogue)) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
+                    else mbar_arrive(accempty0 + 8u * ab);
+                }
+            }
         }
         if (OUT == kOutEpilogue) {
-            if (r_pending) {  // only after a wait that gave up: let the copy in flight land
+            if (!ok && prm.R) {  // a wait gave up: let the copies in flight land (a millisecond)
                 const uint64_t t0 = globaltimer_ns();
-                while (!mbar_try_wait(rfull, r_phase) && globaltimer_ns() - t0 < kWaitLimitNs) {
+                while (globaltimer_ns() - t0 < 1000000ull) {
                 }
             }
             if (lane == 0) bulk_wait_all();
@@ -533,7 +532,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
     return f;
 }
 
-// bf16 [lines][inner] with `pitch` elements from line to line, boxes of box_inner x box_lines
+// bf16 [lines][inner] with `pitch` elements from line to line, boxes of box_inner x box_lines,
+// swizzled to their 128- or 64-byte lines
 bool make_map(CUtensorMap* m, const void* base, int64_t inner, int64_t lines, int64_t pitch,
               int box_inner, int box_lines) {
     auto fn = encode_fn();
@@ -543,7 +543,8 @@ bool make_map(CUtensorMap* m, const void* base, int64_t inner, int64_t lines, in
     cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_lines};
     cuuint32_t estr[2] = {1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
-              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              box_inner == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -643,9 +644,9 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
                      : make_map(&m[1], b.t, K, N, b.pitch, kSlice, b_rows));
     m[2] = m[3] = m[4] = m[0];  // unused unless set below
     if (!e.part && p.tma_out) {
-        ok = ok && make_map(&m[2], e.Y, N, M, N, 64, 32);
-        if (e.Z) ok = ok && make_map(&m[3], e.Z, N, M, N, 64, 32);
-        if (e.R) ok = ok && make_map(&m[4], e.R, N, M, N, 64, 32);
+        ok = ok && make_map(&m[2], e.Y, N, M, N, 32, 32);
+        if (e.Z) ok = ok && make_map(&m[3], e.Z, N, M, N, 32, 32);
+        if (e.R) ok = ok && make_map(&m[4], e.R, N, M, N, 32, 32);
     }
     if (!ok) return cudaErrorInvalidValue;
     const int out = !e.part ? kOutEpilogue : plan.transposed ? kOutPartT : kOutPart;
