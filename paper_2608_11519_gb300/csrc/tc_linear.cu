@@ -53,9 +53,11 @@ struct Cfg {
     static constexpr int kStage = kATile + kBTile;
     // per epilogue warp: two 32-row x 32-column bf16 blocks
     static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * 2 * kBlockBytes : 0;
-    static constexpr int kFit = (232448 - 1024 - kStaging - kNumBars * 8 - 16) / kStage;
+    // per epilogue warp: the bias of its 128 columns of the tile, float32
+    static constexpr int kBias = OUT == kOutEpilogue ? kEpiWarps * 128 * 4 : 0;
+    static constexpr int kFit = (232448 - 1024 - kStaging - kBias - kNumBars * 8 - 16) / kStage;
     static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
-    static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kNumBars * 8 + 16;
+    static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kBias + kNumBars * 8 + 16;
 };
 
 struct Gemm {
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // the same offset in both CTAs of a pair: the dynamic shared memory starts at one address
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* staging = smem + kS * C::kStage;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + C::kStaging);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + C::kStaging + C::kBias);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const uint32_t full0 = smem_u32(bars);
@@ -307,6 +309,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int q = warp % 4;              // the TMEM lanes this warp may read
         const int cfirst = 64 * (e % (kEpiWarps / 2) / 4);
         uint8_t* staged = staging + e * 2 * kBlockBytes;
+        // the bias of columns cfirst .. cfirst + 63 and cfirst + 128 .. cfirst + 191 of the tile
+        float* my_bias = reinterpret_cast<float*>(staging + C::kStaging) + e * 128;
+        int bias_ct = -1;
         // 16-byte piece g of this lane's row in a staged block, swizzled as the maps expect it
         auto piece = [&](int h, int g) {
             return reinterpret_cast<uint4*>(staged + h * kBlockBytes + lane * 64 +
@@ -335,6 +340,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) bulk_wait_read();
                 for (int h = 0; h < 2; ++h)
                     if (cfirst + 32 * h < width) fetch_r(h, cfirst + 32 * h);
+            }
+            if (OUT == kOutEpilogue && prm.bias && bias_ct != w.ct) {
+                bias_ct = w.ct;
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = n0 + cfirst + 128 * (i / 2) + 32 * (i % 2) + lane;
+                    my_bias[32 * i + lane] = n < prm.N ? __bfloat162float(prm.bias[n]) : 0.f;
+                }
+                __syncwarp();
             }
             ok = warp_wait<CG>(accfull0 + 8u * ab, phase, abort_flag, prm.status);
             tc_fence_after();
@@ -366,34 +381,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint64_t x[16];
                 auto load = [&] {
                     uint32_t r[32];
-                    uint4 u[4];
-                    const int at = n0 + c;
-                    const bool whole = at + 32 <= prm.N;
-                    if (prm.bias && whole)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g)
-                            u[g] = __ldg(reinterpret_cast<const uint4*>(prm.bias + at) + g);
                     tmem_ld32(acc + c, r);
                     tmem_wait_ld32(r);
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         x[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
                     if (!prm.bias) return;
-                    if (whole) {
+                    const float4* b4 = reinterpret_cast<const float4*>(my_bias + (c / 128) * 64 + (c & 32));
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            x[4 * g] = add2(x[4 * g], unpack_bf16x2(u[g].x));
-                            x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u[g].y));
-                            x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u[g].z));
-                            x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u[g].w));
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int n = at + 2 * i;
-                            x[i] = add2(x[i], pair(n < prm.N ? __bfloat162float(prm.bias[n]) : 0.f,
-                                                   n + 1 < prm.N ? __bfloat162float(prm.bias[n + 1]) : 0.f));
-                        }
+                    for (int g = 0; g < 8; ++g) {
+                        const float4 f = b4[g];
+                        x[2 * g] = add2(x[2 * g], pair(f.x, f.y));
+                        x[2 * g + 1] = add2(x[2 * g + 1], pair(f.z, f.w));
                     }
                 };
                 auto store = [&](int hb) {
