@@ -21,7 +21,9 @@ constexpr int kDzRows = 8;    // rows a block of dz_kernel reads at once
 constexpr int64_t kGemvRows = 4;
 constexpr int kGemvWarps = 8;
 
-int64_t pad8(int64_t n) { return cdiv(n, 8) * 8; }
+// The pitch of lines that the layer lays out itself: whole 128-byte lines, so that a 128-byte row of
+// a TMA box is one line and not parts of two.
+int64_t pitch_of(int64_t n) { return cdiv(n, 64) * 64; }
 
 // The layer for T <= RT rows, `in` a multiple of 8. A warp takes RW rows of W at a time, a lane every
 // 32nd vector of eight weights of each, U of them in flight (RW * U = 8 loads of 16 bytes a lane
@@ -313,8 +315,8 @@ FwdLayout fwd_layout(const Shape& s) {
     L.plan = few ? lin_plan(s.N, s.T, s.K, true) : lin_plan(s.T, s.N, s.K, false);
     L.split = few || L.plan.chunks > 1;
     const bool pad = s.K % 8 != 0;
-    L.off_x = take(&L.total, pad ? s.T * pad8(s.K) * 2 : 0);
-    L.off_w = take(&L.total, pad ? s.N * pad8(s.K) * 2 : 0);
+    L.off_x = take(&L.total, pad ? s.T * pitch_of(s.K) * 2 : 0);
+    L.off_w = take(&L.total, pad ? s.N * pitch_of(s.K) * 2 : 0);
     L.off_part = take(&L.total, L.split ? (int64_t)part_bytes(L.plan, s.T, s.N) : 0);
     return L;
 }
@@ -341,20 +343,20 @@ BwdLayout bwd_layout(const Shape& s) {
     L.dz_rows = cdiv(cdiv(s.T, want), kDzRows) * kDzRows;
     L.dz_blocks = cdiv(s.T, L.dz_rows);
     const bool pad = s.K % 8 != 0;
-    L.off_x = take(&L.total, pad ? s.T * pad8(s.K) * 2 : 0);
-    L.off_w = take(&L.total, pad ? s.N * pad8(s.K) * 2 : 0);
-    L.off_dz = take(&L.total, L.own_dz ? s.T * pad8(s.N) * 2 : 0);
-    L.off_db = take(&L.total, L.dz_blocks * pad8(s.N) * 4);
+    L.off_x = take(&L.total, pad ? s.T * pitch_of(s.K) * 2 : 0);
+    L.off_w = take(&L.total, pad ? s.N * pitch_of(s.K) * 2 : 0);
+    L.off_dz = take(&L.total, L.own_dz ? s.T * pitch_of(s.N) * 2 : 0);
+    L.off_db = take(&L.total, L.dz_blocks * pitch_of(s.N) * 4);
     L.off_px = take(&L.total, L.split_x ? (int64_t)part_bytes(L.plan_x, s.T, s.K) : 0);
     L.off_pw = take(&L.total, L.split_w ? (int64_t)part_bytes(L.plan_w, s.N, s.K) : 0);
     return L;
 }
 
 cudaError_t pad(const void* src, int64_t rows, int64_t cols, void* dst, cudaStream_t st) {
-    const int64_t n = rows * pad8(cols) / 8;
+    const int64_t n = rows * pitch_of(cols) / 8;
     const int64_t blocks = cdiv(n, 256) < 32 * kNumSMs ? cdiv(n, 256) : 32 * kNumSMs;
     return launch_pdl(pad_kernel, dim3((unsigned)blocks), dim3(256), 0, st,
-                      (const __nv_bfloat16*)src, rows, cols, pad8(cols), (__nv_bfloat16*)dst);
+                      (const __nv_bfloat16*)src, rows, cols, pitch_of(cols), (__nv_bfloat16*)dst);
 }
 
 cudaError_t finish(const float* part, const LinPlan& plan, int64_t rows, int64_t cols,
@@ -416,7 +418,7 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
     const Span ins[4] = {{X, (size_t)s.T * s.K * 2}, {W, (size_t)s.N * s.K * 2},
                          {b, (size_t)s.N * 2}, {R, y_bytes}};
     if (!disjoint(outs, 4, ins, 4)) return FLAREPP_ERR_INVALID_ARGUMENT;
-    const LinEpilogue e{s.act, b, R, Y, Z, nullptr, 0};
+    const LinEpilogue e{s.act, b, R, Y, Z, nullptr, 0, 0};
     if (L.gemv) {
         const cudaError_t err = s.T == 1   ? gemv<1>(s, X, W, e, st)
                                 : s.T == 2 ? gemv<2>(s, X, W, e, st)
@@ -429,8 +431,8 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
         if (pad(X, s.T, s.K, ws + L.off_x, st) != cudaSuccess ||
             pad(W, s.N, s.K, ws + L.off_w, st) != cudaSuccess)
             return FLAREPP_ERR_CUDA;
-        x = {ws + L.off_x, pad8(s.K), 0};
-        w = {ws + L.off_w, pad8(s.K), 0};
+        x = {ws + L.off_x, pitch_of(s.K), 0};
+        w = {ws + L.off_w, pitch_of(s.K), 0};
     }
     return product(L.plan, L.split, s.T, s.N, s.K, x, w, e, (float*)(ws + L.off_part), status,
                    st) == cudaSuccess
@@ -470,7 +472,7 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
         return FLAREPP_OK;
     }
     char* ws = (char*)workspace;
-    const int64_t ldz = pad8(s.N);
+    const int64_t ldz = pitch_of(s.N);
     const bool own_dz = L.own_dz && (dX || dW);
     cudaError_t e = cudaSuccess;
     if (own_dz || db) {
@@ -489,17 +491,19 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
     if (s.K % 8) {
         if (e == cudaSuccess && dW) e = pad(X, s.T, s.K, ws + L.off_x, st);
         if (e == cudaSuccess && dX) e = pad(W, s.N, s.K, ws + L.off_w, st);
-        x = {ws + L.off_x, pad8(s.K), 0};
-        w = {ws + L.off_w, pad8(s.K), 0};
+        x = {ws + L.off_x, pitch_of(s.K), 0};
+        w = {ws + L.off_w, pitch_of(s.K), 0};
     }
-    const LinOperand dz{own_dz ? ws + L.off_dz : dY, ldz, 0};
+    const LinOperand dz{own_dz ? ws + L.off_dz : dY, own_dz ? ldz : s.N, 0};
+    // dX takes the rows from the last to the first and dW from the first on: each then finds in the L2
+    // what was written or read last
     if (e == cudaSuccess && dX)
         e = product(L.plan_x, L.split_x, s.T, s.K, s.N, dz, {w.t, w.pitch, 1},
-                    {FLAREPP_ACT_NONE, nullptr, nullptr, dX, nullptr, nullptr, 0},
+                    {FLAREPP_ACT_NONE, nullptr, nullptr, dX, nullptr, nullptr, 0, 1},
                     (float*)(ws + L.off_px), status, st);
     if (e == cudaSuccess && dW)
         e = product(L.plan_w, L.split_w, s.N, s.K, s.T, {dz.t, dz.pitch, 1}, {x.t, x.pitch, 1},
-                    {FLAREPP_ACT_NONE, nullptr, nullptr, dW, nullptr, nullptr, 0},
+                    {FLAREPP_ACT_NONE, nullptr, nullptr, dW, nullptr, nullptr, 0, 0},
                     (float*)(ws + L.off_pw), status, st);
     return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
 }

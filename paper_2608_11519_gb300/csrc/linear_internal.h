@@ -27,6 +27,7 @@ struct LinEpilogue {
     void* Z;
     float* part;
     int64_t ldp;
+    int backward;  // take the rows from the last to the first
 };
 
 // How a product is cut: tiles of 128 * cg rows x NT columns, `chunks` parts of the contraction.

@@ -42,19 +42,24 @@ constexpr int kMaxNT = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int kMaxStages = 8;
+constexpr int kDeepSlices = 12;  // slices of a contraction from which the deep form runs
 constexpr int kBlockBytes = 32 * 32 * 2;  // what an epilogue warp stages at a time
 constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + 2 * kEpiWarps;
 
 enum Out { kOutEpilogue, kOutPart, kOutPartT };
 
-template <int CG, int OUT>
+// DEEP: the epilogue gives most of its shared memory to the ring (one staged block per warp, the
+// bias read from global memory): for long contractions, where the products are the bound and their
+// loads have to be further ahead.
+template <int CG, int OUT, bool DEEP>
 struct Cfg {
     static constexpr int kBTile = kMaxNT / CG * kSlice * 2;
     static constexpr int kStage = kATile + kBTile;
-    // per epilogue warp: two 32-row x 32-column bf16 blocks
-    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * 2 * kBlockBytes : 0;
+    // per epilogue warp: 32-row x 32-column bf16 blocks
+    static constexpr int kBlocks = DEEP ? 1 : 2;
+    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * kBlocks * kBlockBytes : 0;
     // per epilogue warp: the bias of its 128 columns of the tile, float32
-    static constexpr int kBias = OUT == kOutEpilogue ? kEpiWarps * 128 * 4 : 0;
+    static constexpr int kBias = OUT == kOutEpilogue && !DEEP ? kEpiWarps * 128 * 4 : 0;
     static constexpr int kFit = (232448 - 1024 - kStaging - kBias - kNumBars * 8 - 16) / kStage;
     static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
     static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kBias + kNumBars * 8 + 16;
@@ -63,7 +68,8 @@ struct Cfg {
 struct Gemm {
     int M, N, NT;
     int row_tiles, col_tiles, tiles, n_work;
-    int slices, chunk_slices;  // of the whole contraction, of a chunk
+    int slices, chunks;  // of the contraction; chunk c takes the slices c, c + chunks, ...
+    int backward;        // walk the tiles from the last to the first
     uint32_t idesc;
     int act;
     int tma_out;  // the output's pitch suits TMA
@@ -84,6 +90,7 @@ struct Work {
 // that the CTAs at work at one time share few rows of A and few columns of B in the L2.
 __device__ __forceinline__ Work work_of(const Gemm& p, int v) {
     Work w;
+    if (p.backward) v = p.n_work - 1 - v;
     w.chunk = v / p.tiles;
     const int t = v - w.chunk * p.tiles;
     const int per = 8 * p.col_tiles;
@@ -145,12 +152,12 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, int s) {
               : smem_desc(addr + s * 32, 16, 1024, kSw128);
 }
 
-template <int CG, bool A_MN, bool B_MN, int OUT>
+template <int CG, bool A_MN, bool B_MN, int OUT, bool DEEP>
 __global__ void __launch_bounds__(kThreads, 1)
     lin_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                     const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmZ,
                     const __grid_constant__ CUtensorMap tmR, const Gemm prm) {
-    using C = Cfg<CG, OUT>;
+    using C = Cfg<CG, OUT, DEEP>;
     constexpr int kS = C::kStages;
     extern __shared__ uint8_t smem_raw[];
     // the same offset in both CTAs of a pair: the dynamic shared memory starts at one address
@@ -215,8 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Work w = work_of(prm, v);
             const int m0 = (w.rt * CG + (int)rank) * 128;
             const int n0 = w.ct * prm.NT + (int)rank * b_rows;
-            const int s1 = min(prm.slices, (w.chunk + 1) * prm.chunk_slices);
-            for (int s = w.chunk * prm.chunk_slices; s < s1; ++s, ++it) {
+            for (int s = w.chunk; s < prm.slices; s += prm.chunks, ++it) {
                 const int st = it % kS;
                 if (it >= (uint32_t)kS &&
                     !warp_wait<CG>(empty0 + 8u * st, (it / kS - 1) & 1, abort_flag, prm.status)) {
@@ -262,9 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tc_fence_after();
             const uint32_t acc = tmem + ab * kMaxNT;
-            const int s0 = w.chunk * prm.chunk_slices;
-            const int s1 = min(prm.slices, s0 + prm.chunk_slices);
-            for (int s = s0; s < s1; ++s, ++it) {
+            for (int s = w.chunk; s < prm.slices; s += prm.chunks, ++it) {
                 const int st = it % kS;
                 if (!warp_wait<CG>(full0 + 8u * st, (it / kS) & 1, abort_flag, prm.status)) {
                     ok = false;
@@ -277,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int k = 0; k < kSlice / 16; ++k) {
                         const uint64_t ad = tile_desc<A_MN>(a, k), bd = tile_desc<B_MN>(b, k);
-                        const uint32_t more = (s > s0 || k > 0) ? 1u : 0u;
+                        const uint32_t more = (s > w.chunk || k > 0) ? 1u : 0u;
                         if (CG == 2) mma_ss_pair(acc, ad, bd, prm.idesc, more);
                         else mma_ss(acc, ad, bd, prm.idesc, more);
                     }
@@ -308,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int ab = e / (kEpiWarps / 2);  // this warp's group and accumulator
         const int q = warp % 4;              // the TMEM lanes this warp may read
         const int cfirst = 64 * (e % (kEpiWarps / 2) / 4);
-        uint8_t* staged = staging + e * 2 * kBlockBytes;
+        uint8_t* staged = staging + e * C::kBlocks * kBlockBytes;
         // the bias of columns cfirst .. cfirst + 63 and cfirst + 128 .. cfirst + 191 of the tile
         float* my_bias = reinterpret_cast<float*>(staging + C::kStaging) + e * 128;
         int bias_ct = -1;
@@ -338,10 +342,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             if (tma_r && !prm.Z) {  // ahead of the products
                 if (lane == 0) bulk_wait_read();
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < C::kBlocks; ++h)
                     if (cfirst + 32 * h < width) fetch_r(h, cfirst + 32 * h);
             }
-            if (OUT == kOutEpilogue && prm.bias && bias_ct != w.ct) {
+            if (C::kBias && prm.bias && bias_ct != w.ct) {
                 bias_ct = w.ct;
                 __syncwarp();
 #pragma unroll
@@ -354,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = warp_wait<CG>(accfull0 + 8u * ab, phase, abort_flag, prm.status);
             tc_fence_after();
             for (int c = cfirst; c < width && ok; c += c % 64 ? 96 : 32) {
-                const int h = c / 32 & 1;  // staged block
+                const int h = DEEP ? 0 : c / 32 & 1;  // staged block
                 if (OUT != kOutEpilogue) {
                     float x[32];
                     tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(x));
@@ -387,6 +391,27 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int i = 0; i < 16; ++i)
                         x[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
                     if (!prm.bias) return;
+                    if (DEEP) {
+                        const int at = n0 + c;
+                        if (at + 32 <= prm.N) {
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) {
+                                const uint4 u = __ldg(reinterpret_cast<const uint4*>(prm.bias + at) + g);
+                                x[4 * g] = add2(x[4 * g], unpack_bf16x2(u.x));
+                                x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u.y));
+                                x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u.z));
+                                x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u.w));
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int n = at + 2 * i;
+                                x[i] = add2(x[i], pair(n < prm.N ? __bfloat162float(prm.bias[n]) : 0.f,
+                                                       n + 1 < prm.N ? __bfloat162float(prm.bias[n + 1]) : 0.f));
+                            }
+                        }
+                        return;
+                    }
                     const float4* b4 = reinterpret_cast<const float4*>(my_bias + (c / 128) * 64 + (c & 32));
 #pragma unroll
                     for (int g = 0; g < 8; ++g) {
@@ -430,8 +455,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (prm.Z) {
                     if (lane == 0) bulk_wait_read();
                     __syncwarp();
-                    store(1);
-                    flush(1, &tmZ, prm.Z);
+                    store(C::kBlocks - 1);
+                    flush(C::kBlocks - 1, &tmZ, prm.Z);
+                    if (DEEP) {  // Y leaves from the same block
+                        if (lane == 0) bulk_wait_read();
+                        __syncwarp();
+                    }
                     if (tma_r) fetch_r(0, c);
                 }
                 if (c + (c % 64 ? 96 : 32) >= width) {  // the last block: the accumulator is read
@@ -476,14 +505,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                         x[4 * g + 3] = add2(x[4 * g + 3], unpack_bf16x2(u.w));
                     }
                 } else if (!prm.Z) {
-                    if (lane == 0) bulk_wait_read_1();
+                    if (lane == 0) {
+                        if (DEEP) bulk_wait_read();
+                        else bulk_wait_read_1();
+                    }
                     __syncwarp();
                 }
                 store(hy);
                 flush(hy, &tmY, prm.Y);
-                if (tma_r && !prm.Z && c + 128 < width) {  // this block's place in the next pair of blocks
+                // this staged block's next turn
+                const int then = DEEP ? c + (c % 64 ? 96 : 32) : c + 128;
+                if (tma_r && !prm.Z && then < width) {
                     if (lane == 0) bulk_wait_read();
-                    fetch_r(h, c + 128);
+                    fetch_r(h, then);
                 }
             }
             if (ok && (width <= cfirst || OUT != kOutEpilogue)) {
@@ -547,11 +581,11 @@ bool make_map(CUtensorMap* m, const void* base, int64_t inner, int64_t lines, in
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CG, bool A_MN, bool B_MN, int OUT>
+template <int CG, bool A_MN, bool B_MN, int OUT, bool DEEP>
 cudaError_t launch(const CUtensorMap* m, const Gemm& p, cudaStream_t st) {
-    using C = Cfg<CG, OUT>;
+    using C = Cfg<CG, OUT, DEEP>;
     static_assert(C::kSmem <= 232448 && C::kStages >= 3, "shared memory budget");
-    auto kernel = lin_gemm_kernel<CG, A_MN, B_MN, OUT>;
+    auto kernel = lin_gemm_kernel<CG, A_MN, B_MN, OUT, DEEP>;
     static std::atomic<int> fits[64];  // tiles that run at once on each device (0: not asked yet)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -597,17 +631,24 @@ LinPlan lin_plan(int64_t M, int64_t N, int64_t K, bool few_columns) {
     LinPlan p{};
     p.transposed = few_columns;
     p.cg = few_columns ? 1 : 2;
-    // equal column tiles, in whole 64-column blocks where there are several
+    // equal column tiles, in whole 32-column blocks where there are several
     const int64_t ct = cdiv(N, kMaxNT);
-    p.NT = (int)(ct == 1 ? cdiv(N, 16) * 16 : cdiv(cdiv(N, ct), 64) * 64);
+    p.NT = (int)(ct == 1 ? cdiv(N, 16) * 16 : cdiv(cdiv(N, ct), 32) * 32);
     const int64_t tiles = cdiv(M, 128 * p.cg) * cdiv(N, p.NT);
+    // How many chunks: the time of the waves of work items (0.3 us a slice and about 4 us of a wave's
+    // own) and, with more than one, of writing and reading the partial sums (8 bytes a value at about 5 TB/s)
+    // and of one launch more. Chunks have at least four slices.
     const int64_t slices = cdiv(K, kSlice), units = kNumSMs / p.cg;
-    // fill the SMs once, with at least four slices a chunk
-    int64_t want = tiles >= units ? 1 : units / tiles;
-    if (want > slices / 4) want = slices / 4;
-    if (want < 1) want = 1;
-    const int64_t per = cdiv(slices, want);
-    p.chunks = (int)cdiv(slices, per);
+    double best = 0;
+    for (int64_t c = 1; c <= 64 && (c == 1 || slices / c >= 4); ++c) {
+        const double waves = (double)cdiv(tiles * c, units);
+        const double us = waves * (0.3 * (double)cdiv(slices, c) * p.NT / kMaxNT + 4) +
+                          (c > 1 || few_columns ? 3 + (double)c * M * N * 8 / 5e6 : 0);
+        if (c == 1 || us < best) {
+            best = us;
+            p.chunks = (int)c;
+        }
+    }
     return p;
 }
 
@@ -624,7 +665,8 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     p.tiles = (int)(row_tiles * col_tiles);
     p.n_work = p.tiles * plan.chunks;
     p.slices = (int)cdiv(K, kSlice);
-    p.chunk_slices = (int)cdiv(p.slices, plan.chunks);
+    p.chunks = plan.chunks;
+    p.backward = e.backward;
     p.idesc = idesc_bf16_f32(128 * plan.cg, plan.NT, a.mn, b.mn);
     p.act = e.act;
     p.tma_out = N % 8 == 0;
@@ -651,17 +693,21 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     const int out = !e.part ? kOutEpilogue : plan.transposed ? kOutPartT : kOutPart;
     if (plan.cg == 1) {
         if (out != kOutPartT) return cudaErrorInvalidValue;
-        return a.mn ? launch<1, true, false, kOutPartT>(m, p, st)
-                    : launch<1, false, false, kOutPartT>(m, p, st);
+        return a.mn ? launch<1, true, false, kOutPartT, true>(m, p, st)
+                    : launch<1, false, false, kOutPartT, true>(m, p, st);
     }
+    const bool deep = p.slices >= kDeepSlices;
     if (a.mn)
-        return out == kOutPart ? launch<2, true, true, kOutPart>(m, p, st)
-                               : launch<2, true, true, kOutEpilogue>(m, p, st);
+        return out == kOutPart ? launch<2, true, true, kOutPart, true>(m, p, st)
+               : deep          ? launch<2, true, true, kOutEpilogue, true>(m, p, st)
+                               : launch<2, true, true, kOutEpilogue, false>(m, p, st);
     if (b.mn)
-        return out == kOutPart ? launch<2, false, true, kOutPart>(m, p, st)
-                               : launch<2, false, true, kOutEpilogue>(m, p, st);
-    return out == kOutPart ? launch<2, false, false, kOutPart>(m, p, st)
-                           : launch<2, false, false, kOutEpilogue>(m, p, st);
+        return out == kOutPart ? launch<2, false, true, kOutPart, true>(m, p, st)
+               : deep          ? launch<2, false, true, kOutEpilogue, true>(m, p, st)
+                               : launch<2, false, true, kOutEpilogue, false>(m, p, st);
+    return out == kOutPart ? launch<2, false, false, kOutPart, true>(m, p, st)
+           : deep          ? launch<2, false, false, kOutEpilogue, true>(m, p, st)
+                           : launch<2, false, false, kOutEpilogue, false>(m, p, st);
 }
 
 }  // namespace flarepp
