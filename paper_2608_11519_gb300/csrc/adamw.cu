@@ -5,9 +5,14 @@
 // the gradient is read (28 bytes in 32 bits; 14 to 16 with bf16 gradients, a float32 master and
 // 8-bit states), against some 20 operations. So one launch walks all tensors of a kind: the
 // table of tensors is a kernel parameter (no copy to the device, nothing to keep until the kernel
-// has run), a block takes 2,048 values of one tensor and finds it by bisection of the tensors'
-// first blocks, and a warp takes 256 of them, which is also the block that shares a scale in an
-// 8-bit state: its largest value is a warp reduction, and a state is read and written once.
+// has run), a block takes 2,048 values of one tensor, which it finds by bisection of the tensors'
+// first blocks, and a warp takes 256 of them, which is also the block that shares a scale in an 8-bit
+// state: its largest value is a warp reduction, and a state is read and written once. (Warps that
+// take several such blocks in turn measured slower, 192 M values with 8-bit states 939 us instead of
+// 819 with the moments read back: each turn waits for its own loads.)
+// With 8-bit states the memory leaves about 60 issue slots a value: the codes of sqrt(v) are those
+// of a half-precision number of 4 exponent and 4 mantissa bits, so two shifts and a conversion read
+// them, and only whole blocks skip the checks of a tensor's end.
 //
 // Every operation is rounded on its own (no contraction): the step is then a function of its inputs
 // that any float32 implementation of the same formulas gives bit for bit, 8-bit codes included.
@@ -39,12 +44,15 @@ struct Entry {
     float* v_scale;
     int64_t n;
 };
+constexpr int kHints = 64;
 // CAP tensors of one kind; tensor i owns the thread blocks [first[i], first[i + 1])
 template <int CAP>
 struct Table {
     Entry e[CAP];
     uint32_t first[CAP + 1];
     int count;
+    int shift;                       // block b looks from tensor hint[b >> shift] on,
+    uint16_t hint[kHints + 1];       // at most to hint[(b >> shift) + 1]
 };
 struct Coef {
     float b1, c1, b2, c2, by_bias, eps, keep, rate;
@@ -52,8 +60,8 @@ struct Coef {
 
 template <int CAP>
 __device__ __forceinline__ int find_tensor(const Table<CAP>& t, uint32_t block) {
-    int lo = 0, hi = t.count;  // first[lo] <= block < first[hi]
-    while (hi - lo > 1) {
+    int lo = t.hint[block >> t.shift], hi = t.hint[(block >> t.shift) + 1] + 1;
+    while (hi - lo > 1) {  // first[lo] <= block < first[hi]
         const int mid = (lo + hi) / 2;
         if (t.first[mid] <= block) lo = mid;
         else hi = mid;
@@ -61,9 +69,10 @@ __device__ __forceinline__ int find_tensor(const Table<CAP>& t, uint32_t block) 
     return lo;
 }
 
-// Four values at p[i .. i + 4), those from n on as zeros.
+// Four values at p[i .. i + 4), those from n on as zeros (FULL: there are none).
+template <bool FULL>
 __device__ __forceinline__ void load4(const float* p, int64_t i, int64_t n, float* x) {
-    if (i + 4 <= n) {
+    if (FULL || i + 4 <= n) {
         const float4 v = *reinterpret_cast<const float4*>(p + i);
         x[0] = v.x;
         x[1] = v.y;
@@ -74,8 +83,9 @@ __device__ __forceinline__ void load4(const float* p, int64_t i, int64_t n, floa
         for (int k = 0; k < 4; ++k) x[k] = i + k < n ? p[i + k] : 0.f;
     }
 }
+template <bool FULL>
 __device__ __forceinline__ void load4(const __nv_bfloat16* p, int64_t i, int64_t n, float* x) {
-    if (i + 4 <= n) {
+    if (FULL || i + 4 <= n) {
         const uint2 v = *reinterpret_cast<const uint2*>(p + i);
         x[0] = __uint_as_float(v.x << 16);
         x[1] = __uint_as_float(v.x & 0xffff0000u);
@@ -86,8 +96,9 @@ __device__ __forceinline__ void load4(const __nv_bfloat16* p, int64_t i, int64_t
         for (int k = 0; k < 4; ++k) x[k] = i + k < n ? __bfloat162float(p[i + k]) : 0.f;
     }
 }
+template <bool FULL>
 __device__ __forceinline__ void store4(float* p, int64_t i, int64_t n, const float* x) {
-    if (i + 4 <= n) {
+    if (FULL || i + 4 <= n) {
         *reinterpret_cast<float4*>(p + i) = make_float4(x[0], x[1], x[2], x[3]);
     } else {
 #pragma unroll
@@ -95,8 +106,9 @@ __device__ __forceinline__ void store4(float* p, int64_t i, int64_t n, const flo
             if (i + k < n) p[i + k] = x[k];
     }
 }
+template <bool FULL>
 __device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t i, int64_t n, const float* x) {
-    if (i + 4 <= n) {
+    if (FULL || i + 4 <= n) {
         __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
         *reinterpret_cast<uint2*>(p + i) = make_uint2(*reinterpret_cast<uint32_t*>(&a),
                                                       *reinterpret_cast<uint32_t*>(&b));
@@ -106,18 +118,20 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t i, int64_t n, c
             if (i + k < n) p[i + k] = __float2bfloat16_rn(x[k]);
     }
 }
+template <bool FULL>
 __device__ __forceinline__ uint32_t load4_bytes(const void* p, int64_t i, int64_t n) {
     const uint8_t* b = reinterpret_cast<const uint8_t*>(p);
-    if (i + 4 <= n) return *reinterpret_cast<const uint32_t*>(b + i);
+    if (FULL || i + 4 <= n) return *reinterpret_cast<const uint32_t*>(b + i);
     uint32_t v = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
         if (i + k < n) v |= (uint32_t)b[i + k] << (8 * k);
     return v;
 }
+template <bool FULL>
 __device__ __forceinline__ void store4_bytes(void* p, int64_t i, int64_t n, uint32_t v) {
     uint8_t* b = reinterpret_cast<uint8_t*>(p);
-    if (i + 4 <= n) {
+    if (FULL || i + 4 <= n) {
         *reinterpret_cast<uint32_t*>(b + i) = v;
     } else {
 #pragma unroll
@@ -150,17 +164,24 @@ __device__ __forceinline__ uint32_t pack_m(const float* x) {
         : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
     return code;
 }
-// One code of sqrt(v): c / 16 below 16, (1 + (c % 16) / 16) 2^(c / 16 - 1) from there on.
-__device__ __forceinline__ float unpack_r(uint32_t c) {
-    return c < 16 ? (float)c * 0.0625f : __uint_as_float((c + (126u << 4)) << 19);
+// Four codes of sqrt(v) (c / 16 below 16, (1 + (c % 16) / 16) 2^(c / 16 - 1) from there on), times
+// 2^-14: a code is the upper eight of the ten used bits of such a half-precision number.
+__device__ __forceinline__ void unpack_r(uint32_t codes, float* x) {
+    const uint32_t lo = __byte_perm(codes, 0, 0x4140) << 6, hi = __byte_perm(codes, 0, 0x4342) << 6;
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+    const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    x[0] = f.x;
+    x[1] = f.y;
+    x[2] = g.x;
+    x[3] = g.y;
 }
+// The code of y (in its low eight bits): y rounded to four mantissa bits, ties to even; below 1 the
+// steps are sixteenths, which adding 2^19 rounds to. A y that is not zero never becomes zero.
 __device__ __forceinline__ uint32_t pack_r(float y) {
     const uint32_t bits = __float_as_uint(y);
-    // to four mantissa bits, ties to even; below 1 the steps are sixteenths
-    int c = (int)((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (126 << 4);
-    if (y < 1.f) c = (int)rintf(__fmul_rn(y, 16.f));
-    c = min(max(c, y > 0.f ? 1 : 0), 255);
-    return (uint32_t)c;
+    const uint32_t high = (bits + (0x3FFFFu - (126u << 23)) + ((bits >> 19) & 1u)) >> 19;
+    const uint32_t low = __float_as_uint(__fadd_rn(y, 524288.f)) - __float_as_uint(524288.f);
+    return max(y < 1.f ? low : high, min(bits, 1u));
 }
 
 // The largest |x| over the warp, as bits (so that a NaN is the largest of all).
@@ -173,37 +194,33 @@ __device__ __forceinline__ float warp_most(const float (*x)[4]) {
     return __uint_as_float(__reduce_max_sync(0xffffffffu, most));
 }
 
-// P, G: types of the weights and the gradients. MASTER: the weights have a float32 master.
-// Q8: 8-bit states. A lane holds values 4 lane + 128 h + (0..3) of its warp's 256.
-template <typename P, typename G, bool MASTER, bool Q8, int CAP>
-__global__ void __launch_bounds__(kThreads)
-    adamw_kernel(const __grid_constant__ Table<CAP> table, const Coef c) {
-    const int t = find_tensor(table, blockIdx.x);
-    const Entry& e = table.e[t];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+// 256 values from `at` on, by one warp. P, G: types of the weights and the gradients. MASTER: the
+// weights have a float32 master. Q8: 8-bit states. FULL: all 256 exist. A lane holds values
+// 4 lane + 128 h + (0..3).
+template <typename P, typename G, bool MASTER, bool Q8, bool FULL>
+__device__ __forceinline__ void step_block(const Entry& e, const Coef& c, int64_t at) {
+    const int lane = threadIdx.x % 32;
     const int64_t n = e.n;
-    const int64_t at = (int64_t)(blockIdx.x - table.first[t]) * kItem + warp * kBlockVals;
-    if (at >= n) return;
     const int64_t block = at / kBlockVals;
     float w[2][4], g[2][4], m[2][4], v[2][4];
     uint32_t mc[2], vc[2];
     float ms, vs;
     if (Q8) {
         ms = e.m_scale[block];
-        vs = e.v_scale[block];
+        vs = e.v_scale[block] * kRTop;  // exact, like the codes' 2^-14
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int64_t i = at + 128 * h + 4 * lane;
-        load4(reinterpret_cast<const G*>(e.grad), i, n, g[h]);
-        if (MASTER) load4(e.master, i, n, w[h]);
-        else load4(reinterpret_cast<const P*>(e.param), i, n, w[h]);
+        load4<FULL>(reinterpret_cast<const G*>(e.grad), i, n, g[h]);
+        if (MASTER) load4<FULL>(e.master, i, n, w[h]);
+        else load4<FULL>(reinterpret_cast<const P*>(e.param), i, n, w[h]);
         if (Q8) {
-            mc[h] = load4_bytes(e.m, i, n);
-            vc[h] = load4_bytes(e.v, i, n);
+            mc[h] = load4_bytes<FULL>(e.m, i, n);
+            vc[h] = load4_bytes<FULL>(e.v, i, n);
         } else {
-            load4(reinterpret_cast<const float*>(e.m), i, n, m[h]);
-            load4(reinterpret_cast<const float*>(e.v), i, n, v[h]);
+            load4<FULL>(reinterpret_cast<const float*>(e.m), i, n, m[h]);
+            load4<FULL>(reinterpret_cast<const float*>(e.v), i, n, v[h]);
         }
     }
     float r[2][4];
@@ -211,10 +228,11 @@ __global__ void __launch_bounds__(kThreads)
     for (int h = 0; h < 2; ++h) {
         if (Q8) {
             unpack_m(mc[h], m[h]);
+            unpack_r(vc[h], v[h]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 m[h][k] = __fmul_rn(m[h][k], ms);
-                const float root = __fmul_rn(unpack_r((vc[h] >> (8 * k)) & 255u), vs);
+                const float root = __fmul_rn(v[h][k], vs);
                 v[h][k] = __fmul_rn(root, root);
             }
         }
@@ -229,11 +247,11 @@ __global__ void __launch_bounds__(kThreads)
                                 __fmul_rn(__fdiv_rn(m[h][k], over), c.rate));
         }
         const int64_t i = at + 128 * h + 4 * lane;
-        if (MASTER) store4(e.master, i, n, w[h]);
-        store4(reinterpret_cast<P*>(e.param), i, n, w[h]);
+        if (MASTER) store4<FULL>(e.master, i, n, w[h]);
+        store4<FULL>(reinterpret_cast<P*>(e.param), i, n, w[h]);
         if (!Q8) {
-            store4(reinterpret_cast<float*>(e.m), i, n, m[h]);
-            store4(reinterpret_cast<float*>(e.v), i, n, v[h]);
+            store4<FULL>(reinterpret_cast<float*>(e.m), i, n, m[h]);
+            store4<FULL>(reinterpret_cast<float*>(e.v), i, n, v[h]);
         }
     }
     if (!Q8) return;
@@ -246,14 +264,16 @@ __global__ void __launch_bounds__(kThreads)
     for (int h = 0; h < 2; ++h) {
         const int64_t i = at + 128 * h + 4 * lane;
         float y[4];
-        uint32_t code = 0;
+        uint32_t rc[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             y[k] = __fmul_rn(m[h][k], m_by);
-            code |= pack_r(__fmul_rn(r[h][k], r_by)) << (8 * k);
+            rc[k] = pack_r(__fmul_rn(r[h][k], r_by));
         }
-        store4_bytes(e.m, i, n, pack_m(y));
-        store4_bytes(e.v, i, n, code);
+        const uint32_t code = __byte_perm(__byte_perm(rc[0], rc[1], 0x0040),
+                                          __byte_perm(rc[2], rc[3], 0x0040), 0x5410);
+        store4_bytes<FULL>(e.m, i, n, pack_m(y));
+        store4_bytes<FULL>(e.v, i, n, code);
     }
     if (lane == 0) {
         e.m_scale[block] = m_live ? m_most * (1.f / kMTop) : 0.f;
@@ -261,32 +281,49 @@ __global__ void __launch_bounds__(kThreads)
     }
 }
 
+template <typename P, typename G, bool MASTER, bool Q8, int CAP>
+__global__ void __launch_bounds__(kThreads, 5)
+    adamw_kernel(const __grid_constant__ Table<CAP> table, const Coef c) {
+    const int t = find_tensor(table, blockIdx.x);
+    const Entry& e = table.e[t];
+    const int64_t n = e.n;
+    const int64_t at = (int64_t)(blockIdx.x - table.first[t]) * kItem + threadIdx.x / 32 * kBlockVals;
+    if (at + kBlockVals <= n) step_block<P, G, MASTER, Q8, true>(e, c, at);
+    else if (at < n) step_block<P, G, MASTER, Q8, false>(e, c, at);
+}
+
 // The values of 8-bit states; e.param and e.master are the outputs for m and v.
+template <bool FULL>
+__device__ __forceinline__ void moments_block(const Entry& e, int64_t at) {
+    const int lane = threadIdx.x % 32;
+    const float ms = e.m_scale[at / kBlockVals], vs = e.v_scale[at / kBlockVals] * kRTop;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t i = at + 128 * h + 4 * lane;
+        const uint32_t mc = load4_bytes<FULL>(e.m, i, e.n), vc = load4_bytes<FULL>(e.v, i, e.n);
+        float m[4], v[4];
+        unpack_m(mc, m);
+        unpack_r(vc, v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            m[k] = __fmul_rn(m[k], ms);
+            const float root = __fmul_rn(v[k], vs);
+            v[k] = __fmul_rn(root, root);
+        }
+        store4<FULL>(reinterpret_cast<float*>(e.param), i, e.n, m);
+        store4<FULL>(e.master, i, e.n, v);
+    }
+}
+
 template <int CAP>
 __global__ void __launch_bounds__(kThreads)
     moments_kernel(const __grid_constant__ Table<CAP> table) {
     const int t = find_tensor(table, blockIdx.x);
     const Entry& e = table.e[t];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int64_t n = e.n;
-    const int64_t at = (int64_t)(blockIdx.x - table.first[t]) * kItem + warp * kBlockVals;
-    if (at >= n) return;
-    const float ms = e.m_scale[at / kBlockVals], vs = e.v_scale[at / kBlockVals];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t i = at + 128 * h + 4 * lane;
-        const uint32_t mc = load4_bytes(e.m, i, n), vc = load4_bytes(e.v, i, n);
-        float m[4], v[4];
-        unpack_m(mc, m);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            m[k] = __fmul_rn(m[k], ms);
-            const float root = __fmul_rn(unpack_r((vc >> (8 * k)) & 255u), vs);
-            v[k] = __fmul_rn(root, root);
-        }
-        store4(reinterpret_cast<float*>(e.param), i, n, m);
-        store4(e.master, i, n, v);
-    }
+    const int64_t at = (int64_t)(blockIdx.x - table.first[t]) * kItem + threadIdx.x / 32 * kBlockVals;
+    if (at + kBlockVals <= n) moments_block<true>(e, at);
+    else if (at < n) moments_block<false>(e, at);
 }
 
 // ------------------------------------------------------------------ host side
@@ -328,6 +365,18 @@ flarepp_status check_tensor(const flarepp_adamw_tensor& t, bool q8) {
     return disjoint(outs, 6, &in, 1) ? FLAREPP_OK : FLAREPP_ERR_INVALID_ARGUMENT;
 }
 
+template <int CAP>
+void set_hints(Table<CAP>* t, uint32_t blocks) {
+    t->shift = 0;
+    while ((blocks - 1) >> t->shift >= kHints) ++t->shift;
+    int i = 0;
+    for (int h = 0; h <= kHints; ++h) {  // the tensor of block h << shift, or the last one
+        const uint64_t b = (uint64_t)h << t->shift;
+        while (i + 1 < t->count && t->first[i + 1] <= b) ++i;
+        t->hint[h] = (uint16_t)i;
+    }
+}
+
 // Launch once per CAP tensors that `pick` accepts; `fill` makes a tensor's entry.
 template <int CAP, typename Pick, typename Fill, typename Go>
 cudaError_t each_table(int64_t n_tensors, Pick pick, Fill fill, Go go) {
@@ -345,6 +394,7 @@ cudaError_t each_table(int64_t n_tensors, Pick pick, Fill fill, Go go) {
         }
         if (t.count && (end || t.count == CAP || blocks + more > 0x7fffffffull)) {
             t.first[t.count] = (uint32_t)blocks;
+            set_hints(&t, (uint32_t)blocks);
             const cudaError_t err = go(t, (unsigned)blocks);
             if (err != cudaSuccess) return err;
             t.count = 0;
