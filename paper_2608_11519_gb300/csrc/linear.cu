@@ -123,20 +123,59 @@ __global__ void pad_kernel(const __nv_bfloat16* __restrict__ src, int64_t rows, 
     }
 }
 
+// The column sums of dZ: what dz_kernel's blocks left in part[n_part][ldz], for db.
+struct DbSums {
+    const float* part;
+    int n_part;
+    int64_t cols, ldz;
+    __nv_bfloat16* db;
+};
+
+// db of 32 columns: YS threads a column, each over a stretch of the partial sums in order, the
+// stretches added in order.
+template <int YS>
+__device__ void sum_db(const DbSums& d, int64_t group) {
+    __shared__ float sums[YS][33];
+    const int lane = threadIdx.x % 32, ty = threadIdx.x / 32;
+    const int64_t c = group * 32 + lane;
+    const int per = (d.n_part + YS - 1) / YS;
+    float s = 0.f;
+    if (c < d.cols)
+#pragma unroll 16
+        for (int k = ty * per; k < min(d.n_part, (ty + 1) * per); ++k) s += d.part[k * d.ldz + c];
+    sums[ty][lane] = s;
+    __syncthreads();
+    if (ty == 0 && c < d.cols) {
+#pragma unroll
+        for (int k = 1; k < YS; ++k) s += sums[k][lane];
+        d.db[c] = __float2bfloat16_rn(s);
+    }
+}
+constexpr int kDbThreads = 1024;
+__global__ void __launch_bounds__(kDbThreads) db_kernel(const DbSums d) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    sum_db<kDbThreads / 32>(d, blockIdx.x);
+}
+
 // What follows the float32 sums of a cut contraction: the chunks added in order (with SPLIT > 1 as
 // SPLIT stretches of chunks, the stretches in order after that: many chunks would otherwise be one
 // long chain of loads), then the epilogue (bias, activation, residual). SPLIT threads per four
-// columns.
-constexpr int kFinishThreads = 128;
+// columns. The blocks from `blocks` on sum db instead, which then needs no launch of its own.
+constexpr int kFinishThreads = 256;
 template <int SPLIT>
 __global__ void __launch_bounds__(kFinishThreads)
     finish_kernel(const float* __restrict__ part, int chunks, int64_t rows,
                               int64_t cols, int64_t ldp, int act,
                               const __nv_bfloat16* __restrict__ bias,
                               const __nv_bfloat16* __restrict__ R, __nv_bfloat16* __restrict__ Y,
-                              __nv_bfloat16* __restrict__ Z) {
+                              __nv_bfloat16* __restrict__ Z, unsigned blocks, const DbSums db) {
     tc::pdl_trigger();
     tc::pdl_wait();
+    if (blockIdx.x >= blocks) {
+        sum_db<kFinishThreads / 32>(db, blockIdx.x - blocks);
+        return;
+    }
     constexpr int kQuads = kFinishThreads / SPLIT;
     const int64_t per = ldp / 4;
     const int quad = threadIdx.x % kQuads, part_of = threadIdx.x / kQuads;
@@ -197,7 +236,7 @@ __global__ void __launch_bounds__(kFinishThreads)
 // of the unrounded dZ over the block's rows into db_part[blockIdx.y][ldz]. VEC: eight values at
 // a time (cols a multiple of 8).
 template <bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 4)
     dz_kernel(const __nv_bfloat16* __restrict__ dY, const __nv_bfloat16* __restrict__ Z,
               int64_t rows, int64_t cols, int64_t rows_per, int act, int64_t ldz,
               __nv_bfloat16* __restrict__ dZ, float* __restrict__ db_part) {
@@ -247,30 +286,6 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
         for (int k = 0; k < kDzRows; ++k) s += sums[k][threadIdx.x];
         db_part[(int64_t)blockIdx.y * ldz + col] = s;
-    }
-}
-
-// db = the sum of the blocks' partial sums: 32 columns a block, 32 threads a column, each over a
-// stretch of the partials in order.
-__global__ void __launch_bounds__(1024)
-    db_kernel(const float* __restrict__ part, int n_part, int64_t cols, int64_t ldz,
-              __nv_bfloat16* __restrict__ db) {
-    tc::pdl_trigger();
-    tc::pdl_wait();
-    __shared__ float sums[32][33];
-    const int lane = threadIdx.x % 32, ty = threadIdx.x / 32;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
-    const int per = (n_part + 31) / 32;
-    float s = 0.f;
-    if (c < cols)
-#pragma unroll 8
-        for (int k = ty * per; k < min(n_part, (ty + 1) * per); ++k) s += part[k * ldz + c];
-    sums[ty][lane] = s;
-    __syncthreads();
-    if (ty == 0 && c < cols) {
-#pragma unroll
-        for (int k = 1; k < 32; ++k) s += sums[k][lane];
-        db[c] = __float2bfloat16_rn(s);
     }
 }
 
@@ -336,9 +351,10 @@ BwdLayout bwd_layout(const Shape& s) {
     L.split_x = few || L.plan_x.chunks > 1;
     L.split_w = L.plan_w.chunks > 1;
     L.own_dz = s.act != FLAREPP_ACT_NONE || s.N % 8 != 0;
-    // about eight blocks of dz_kernel per SM, each of at least 32 rows
+    // one wave of dz_kernel's blocks, four per SM, each of at least 32 rows
     const int64_t col_blocks = cdiv(s.N, kDzCols);
-    int64_t want = cdiv(8 * kNumSMs, col_blocks);
+    int64_t want = 4 * kNumSMs / col_blocks;
+    if (want < 1) want = 1;
     if (want > cdiv(s.T, 32)) want = cdiv(s.T, 32);
     L.dz_rows = cdiv(cdiv(s.T, want), kDzRows) * kDzRows;
     L.dz_blocks = cdiv(s.T, L.dz_rows);
@@ -360,21 +376,24 @@ cudaError_t pad(const void* src, int64_t rows, int64_t cols, void* dst, cudaStre
 }
 
 cudaError_t finish(const float* part, const LinPlan& plan, int64_t rows, int64_t cols,
-                   const LinEpilogue& e, cudaStream_t st) {
+                   const LinEpilogue& e, const DbSums& db, cudaStream_t st) {
     const int64_t ldp = cdiv(cols, 4) * 4, n = rows * (ldp / 4);
     // over 16 chunks: eight threads share them (38 chunks of 512 x 256 sums: 14 us with one)
     const int split = plan.chunks > 16 ? 8 : 1;
     auto kernel = split == 8 ? finish_kernel<8> : finish_kernel<1>;
-    return launch_pdl(kernel, dim3((unsigned)cdiv(n * split, kFinishThreads)),
-                      dim3(kFinishThreads), 0, st, part, plan.chunks, rows, cols, ldp, e.act, (const __nv_bfloat16*)e.bias,
-                      (const __nv_bfloat16*)e.R, (__nv_bfloat16*)e.Y, (__nv_bfloat16*)e.Z);
+    const unsigned blocks = (unsigned)cdiv(n * split, kFinishThreads);
+    const unsigned more = db.db ? (unsigned)cdiv(db.cols, 32) : 0;
+    return launch_pdl(kernel, dim3(blocks + more), dim3(kFinishThreads), 0, st, part, plan.chunks,
+                      rows, cols, ldp, e.act, (const __nv_bfloat16*)e.bias,
+                      (const __nv_bfloat16*)e.R, (__nv_bfloat16*)e.Y, (__nv_bfloat16*)e.Z, blocks,
+                      db);
 }
 
 // out [rows][cols] = epilogue(sum_k a(row, k) b(col, k)), through partials where the plan cuts
 // the contraction or swaps the operands
 cudaError_t product(const LinPlan& plan, bool split, int64_t rows, int64_t cols, int64_t depth,
                     const LinOperand& a, const LinOperand& b, const LinEpilogue& e, float* part,
-                    int* status, cudaStream_t st) {
+                    int* status, cudaStream_t st, const DbSums& db = DbSums{}) {
     if (!split) return lin_gemm(plan, rows, cols, depth, a, b, e, status, st);
     LinEpilogue sums{};
     sums.part = part;
@@ -382,7 +401,7 @@ cudaError_t product(const LinPlan& plan, bool split, int64_t rows, int64_t cols,
     const cudaError_t err = plan.transposed
                                 ? lin_gemm(plan, cols, rows, depth, b, a, sums, status, st)
                                 : lin_gemm(plan, rows, cols, depth, a, b, sums, status, st);
-    return err != cudaSuccess ? err : finish(part, plan, rows, cols, e, st);
+    return err != cudaSuccess ? err : finish(part, plan, rows, cols, e, db, st);
 }
 
 template <int RT>
@@ -482,10 +501,11 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
                        (const __nv_bfloat16*)Z, s.T, s.N, L.dz_rows, s.act, ldz,
                        (__nv_bfloat16*)(own_dz ? ws + L.off_dz : nullptr),
                        (float*)(db ? ws + L.off_db : nullptr));
-        if (e == cudaSuccess && db)
-            e = launch_pdl(db_kernel, dim3((unsigned)cdiv(s.N, 32)), dim3(1024), 0, st,
-                           (const float*)(ws + L.off_db), (int)L.dz_blocks, s.N, ldz,
-                           (__nv_bfloat16*)db);
+    }
+    DbSums sums{(const float*)(ws + L.off_db), (int)L.dz_blocks, s.N, ldz, (__nv_bfloat16*)db};
+    if (e == cudaSuccess && db && !(dW && L.split_w)) {
+        e = launch_pdl(db_kernel, dim3((unsigned)cdiv(s.N, 32)), dim3(kDbThreads), 0, st, sums);
+        sums.db = nullptr;
     }
     LinOperand x{X, s.K, 0}, w{W, s.K, 0};
     if (s.K % 8) {
@@ -504,7 +524,7 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
     if (e == cudaSuccess && dW)
         e = product(L.plan_w, L.split_w, s.N, s.K, s.T, {dz.t, dz.pitch, 1}, {x.t, x.pitch, 1},
                     {FLAREPP_ACT_NONE, nullptr, nullptr, dW, nullptr, nullptr, 0, 0},
-                    (float*)(ws + L.off_pw), status, st);
+                    (float*)(ws + L.off_pw), status, st, sums);
     return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
 }
 
