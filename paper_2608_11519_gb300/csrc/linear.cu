@@ -9,16 +9,21 @@
 namespace flarepp {
 namespace {
 
-// Rows up to which a product runs with the weights as its tile rows: the weights fill the
-// 128 rows of the tensor core's tile whatever the number of tokens, which become its columns.
-constexpr int64_t kFewRows = 128;
 constexpr int kDzCols = 256;  // columns per block of dz_kernel: 32 lanes x 8
 constexpr int kDzRows = 8;    // rows a block of dz_kernel reads at once
 
-// Rows up to which the layer runs on the CUDA cores (gemv_kernel): a weight then meets so few
-// multiplications that its bytes are the bound, and one launch without workspace is the shortest
-// path (one row of 2048 -> 2048: 7.0 us through the tensor cores and their chunk sums).
+// Up to four rows the layer can run on the CUDA cores (gemv_kernel): a weight then meets so few
+// multiplications that its bytes are the bound, and one launch without tensor maps is the shortest
+// path. That ends where rows x weights pass about 12 M: 2 rows of 4096 -> 1001 take 4.4 us here and 5.6 in
+// lin_few, 4 rows 7.2 and 5.6, 2 rows of 4096 -> 4096 11.2 and 7.8. One row is always faster here.
 constexpr int64_t kGemvRows = 4;
+bool use_gemv(int64_t T, int64_t K, int64_t N) {
+    return K % 8 == 0 && (T == 1 || (T <= kGemvRows && T * K * N <= 12000000));
+}
+// Rows up to which lin_few is faster than tiles of 256 rows: 200 rows of 4096 -> 4096 take 13.2 us in
+// lin_few and 22 in tiles, 200 rows of 256 -> 512 10.5 and 9.0 (a short contraction leaves lin_few's CTAs
+// mostly with their epilogues).
+bool use_few(int64_t T, int64_t depth) { return T <= (depth >= 1024 ? kFewRows : kFewRows / 2); }
 constexpr int kGemvWarps = 8;
 
 // The pitch of lines that the layer lays out itself: whole 128-byte lines, so that a 128-byte row of
@@ -317,18 +322,18 @@ size_t part_bytes(const LinPlan& p, int64_t rows, int64_t cols) {
 }
 
 struct FwdLayout {
-    bool gemv;
+    bool gemv, few;
     LinPlan plan;
     bool split;  // the sums go through partials and finish_kernel
     size_t off_x, off_w, off_part, total;
 };
 FwdLayout fwd_layout(const Shape& s) {
     FwdLayout L{};
-    L.gemv = s.T <= kGemvRows && s.K % 8 == 0;
+    L.gemv = use_gemv(s.T, s.K, s.N);
     if (L.gemv) return L;
-    const bool few = s.T <= kFewRows;
-    L.plan = few ? lin_plan(s.N, s.T, s.K, true) : lin_plan(s.T, s.N, s.K, false);
-    L.split = few || L.plan.chunks > 1;
+    L.few = use_few(s.T, s.K);
+    if (!L.few) L.plan = lin_plan(s.T, s.N, s.K);
+    L.split = L.plan.chunks > 1;
     const bool pad = s.K % 8 != 0;
     L.off_x = take(&L.total, pad ? s.T * pitch_of(s.K) * 2 : 0);
     L.off_w = take(&L.total, pad ? s.N * pitch_of(s.K) * 2 : 0);
@@ -337,6 +342,7 @@ FwdLayout fwd_layout(const Shape& s) {
 }
 
 struct BwdLayout {
+    bool few;
     LinPlan plan_x, plan_w;
     bool split_x, split_w;
     bool own_dz;  // dZ is laid out in the workspace (else the products read dY)
@@ -345,10 +351,10 @@ struct BwdLayout {
 };
 BwdLayout bwd_layout(const Shape& s) {
     BwdLayout L{};
-    const bool few = s.T <= kFewRows;
-    L.plan_x = few ? lin_plan(s.K, s.T, s.N, true) : lin_plan(s.T, s.K, s.N, false);
-    L.plan_w = lin_plan(s.N, s.K, s.T, false);
-    L.split_x = few || L.plan_x.chunks > 1;
+    L.few = use_few(s.T, s.N);
+    if (!L.few) L.plan_x = lin_plan(s.T, s.K, s.N);
+    L.plan_w = lin_plan(s.N, s.K, s.T);
+    L.split_x = L.plan_x.chunks > 1;
     L.split_w = L.plan_w.chunks > 1;
     L.own_dz = s.act != FLAREPP_ACT_NONE || s.N % 8 != 0;
     // one wave of dz_kernel's blocks, four per SM, each of at least 32 rows
@@ -390,7 +396,7 @@ cudaError_t finish(const float* part, const LinPlan& plan, int64_t rows, int64_t
 }
 
 // out [rows][cols] = epilogue(sum_k a(row, k) b(col, k)), through partials where the plan cuts
-// the contraction or swaps the operands
+// the contraction
 cudaError_t product(const LinPlan& plan, bool split, int64_t rows, int64_t cols, int64_t depth,
                     const LinOperand& a, const LinOperand& b, const LinEpilogue& e, float* part,
                     int* status, cudaStream_t st, const DbSums& db = DbSums{}) {
@@ -398,9 +404,7 @@ cudaError_t product(const LinPlan& plan, bool split, int64_t rows, int64_t cols,
     LinEpilogue sums{};
     sums.part = part;
     sums.ldp = cdiv(cols, 4) * 4;
-    const cudaError_t err = plan.transposed
-                                ? lin_gemm(plan, cols, rows, depth, b, a, sums, status, st)
-                                : lin_gemm(plan, rows, cols, depth, a, b, sums, status, st);
+    const cudaError_t err = lin_gemm(plan, rows, cols, depth, a, b, sums, status, st);
     return err != cudaSuccess ? err : finish(part, plan, rows, cols, e, db, st);
 }
 
@@ -453,10 +457,10 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
         x = {ws + L.off_x, pitch_of(s.K), 0};
         w = {ws + L.off_w, pitch_of(s.K), 0};
     }
-    return product(L.plan, L.split, s.T, s.N, s.K, x, w, e, (float*)(ws + L.off_part), status,
-                   st) == cudaSuccess
-               ? FLAREPP_OK
-               : FLAREPP_ERR_CUDA;
+    const cudaError_t err = L.few ? lin_few(s.T, s.N, s.K, x, w, e, status, st)
+                                  : product(L.plan, L.split, s.T, s.N, s.K, x, w, e,
+                                            (float*)(ws + L.off_part), status, st);
+    return err == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
 }
 
 flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, const void* W,
@@ -517,10 +521,13 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
     const LinOperand dz{own_dz ? ws + L.off_dz : dY, own_dz ? ldz : s.N, 0};
     // dX takes the rows from the last to the first and dW from the first on: each then finds in the L2
     // what was written or read last
-    if (e == cudaSuccess && dX)
-        e = product(L.plan_x, L.split_x, s.T, s.K, s.N, dz, {w.t, w.pitch, 1},
-                    {FLAREPP_ACT_NONE, nullptr, nullptr, dX, nullptr, nullptr, 0, 1},
-                    (float*)(ws + L.off_px), status, st);
+    if (e == cudaSuccess && dX) {
+        const LinEpilogue to_dx{FLAREPP_ACT_NONE, nullptr, nullptr, dX, nullptr, nullptr, 0, 1};
+        const LinOperand wt{w.t, w.pitch, 1};
+        e = L.few ? lin_few(s.T, s.K, s.N, dz, wt, to_dx, status, st)
+                  : product(L.plan_x, L.split_x, s.T, s.K, s.N, dz, wt, to_dx,
+                            (float*)(ws + L.off_px), status, st);
+    }
     if (e == cudaSuccess && dW)
         e = product(L.plan_w, L.split_w, s.N, s.K, s.T, {dz.t, dz.pitch, 1}, {x.t, x.pitch, 1},
                     {FLAREPP_ACT_NONE, nullptr, nullptr, dW, nullptr, nullptr, 0, 0},

@@ -17,8 +17,7 @@ struct LinOperand {
 
 // What happens to the sums. Either the epilogue: z = sum + bias[n] (kept in Z when it is not
 // null), Y = act(z) + R, all [M][N] bf16; or, when `part` is set, the float32 sums of each
-// chunk of the contraction go to part[chunk][M][ldp] (transposed: part[chunk][N][ldp], for
-// products whose rows are the output's columns).
+// chunk of the contraction go to part[chunk][M][ldp].
 struct LinEpilogue {
     int act;
     const void* bias;
@@ -30,18 +29,22 @@ struct LinEpilogue {
     int backward;  // take the rows from the last to the first
 };
 
-// How a product is cut: tiles of 128 * cg rows x NT columns, `chunks` parts of the contraction.
+// How a product is cut: tiles of 256 rows x NT columns, `chunks` parts of the contraction.
 struct LinPlan {
-    int cg;       // CTAs that share a tile: 1, or 2 (cta_group::2)
     int NT;
     int chunks;
-    bool transposed;
 };
-LinPlan lin_plan(int64_t M, int64_t N, int64_t K, bool few_columns);
+LinPlan lin_plan(int64_t M, int64_t N, int64_t K);
 
 // Enqueue the product (tc_linear.cu). M, N, K below 2^31.
 cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const LinOperand& a,
                      const LinOperand& b, const LinEpilogue& e, int* status, cudaStream_t st);
+
+// The product of up to kFewRows rows of x (contraction innermost) with w: [rows][cols], with the
+// epilogue, in one launch.
+constexpr int64_t kFewRows = 256;
+cudaError_t lin_few(int64_t rows, int64_t cols, int64_t K, const LinOperand& x,
+                    const LinOperand& w, const LinEpilogue& e, int* status, cudaStream_t st);
 
 // ---- activations (flarepp_activation) and their slopes, float32
 __device__ __forceinline__ float rcp_approx(float x) {

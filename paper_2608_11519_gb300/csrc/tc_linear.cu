@@ -4,11 +4,11 @@
 // covers the layer's three products without a transposed copy: Z = X W^T (both K-major),
 // dX = dZ W (W MN-major), dW = dZ^T X (both MN-major).
 //
-// Cut: a tile is 128 rows per CTA x NT <= 256 columns, the contraction runs in slices of 64 (a
-// 128-byte swizzled row). With CG = 2 a pair of CTAs shares a 256-row tile (cta_group::2): each CTA
-// loads its own 128 rows of A and half of the columns of B, so a slice costs 32 KB of
-// shared-memory fill per CTA instead of 48 KB and B crosses the L2 half as often. The walk over
-// tiles is persistent; chunks cut a long contraction when there are few tiles.
+// Cut: a pair of CTAs (cta_group::2) shares a tile of 256 rows x NT <= 256 columns, the contraction
+// runs in slices of 64 (a 128-byte swizzled row). Each CTA loads its own 128 rows of A and half of
+// the columns of B, so a slice costs 32 KB of shared-memory fill per CTA instead of 48 KB and B crosses
+// the L2 half as often. The walk over tiles is persistent; chunks cut a long contraction when there are few
+// tiles. Few tokens have a kernel of their own below.
 //
 // Roles (20 warps): warp 0 the TMA producer, warp 1 the MMA issuer (in the pair's leader),
 // warps 4..19 the epilogue: two groups of eight warps take the tiles in turn, so that one group's
@@ -46,14 +46,14 @@ constexpr int kDeepSlices = 12;  // slices of a contraction from which the deep 
 constexpr int kBlockBytes = 32 * 32 * 2;  // what an epilogue warp stages at a time
 constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + 2 * kEpiWarps;
 
-enum Out { kOutEpilogue, kOutPart, kOutPartT };
+enum Out { kOutEpilogue, kOutPart };
 
 // DEEP: the epilogue gives most of its shared memory to the ring (one staged block per warp, the
 // bias read from global memory): for long contractions, where the products are the bound and their
 // loads have to be further ahead.
-template <int CG, int OUT, bool DEEP>
+template <int OUT, bool DEEP>
 struct Cfg {
-    static constexpr int kBTile = kMaxNT / CG * kSlice * 2;
+    static constexpr int kBTile = kMaxNT / 2 * kSlice * 2;
     static constexpr int kStage = kATile + kBTile;
     // per epilogue warp: 32-row x 32-column bf16 blocks
     static constexpr int kBlocks = DEEP ? 1 : 2;
@@ -152,12 +152,12 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, int s) {
               : smem_desc(addr + s * 32, 16, 1024, kSw128);
 }
 
-template <int CG, bool A_MN, bool B_MN, int OUT, bool DEEP>
+template <bool A_MN, bool B_MN, int OUT, bool DEEP>
 __global__ void __launch_bounds__(kThreads, 1)
     lin_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                     const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmZ,
                     const __grid_constant__ CUtensorMap tmR, const Gemm prm) {
-    using C = Cfg<CG, OUT, DEEP>;
+    using C = Cfg<OUT, DEEP>;
     constexpr int kS = C::kStages;
     extern __shared__ uint8_t smem_raw[];
     // the same offset in both CTAs of a pair: the dynamic shared memory starts at one address
@@ -174,8 +174,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t rfull0 = fin + 8u;  // one per staged block
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const int first = (int)blockIdx.x / CG, pairs = (int)gridDim.x / CG;
+    const uint32_t rank = cluster_rank();
+    const int first = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kS; ++s) {
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(accfull0 + 8u * b, 1);
-            mbar_init(accempty0 + 8u * b, kEpiWarps / 2 * CG);
+            mbar_init(accempty0 + 8u * b, kEpiWarps / 2 * 2);
         }
         mbar_init(fin, 1);
         for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(rfull0 + 8u * w, 1);
@@ -194,17 +194,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         prefetch_tmap(&tmB);
     }
     if (warp == 1) {
-        if (CG == 2) {
-            tmem_alloc_pair(smem_u32(tmem_slot), kTmemCols);
-            tmem_relinquish_pair();
-        } else {
-            tmem_alloc(smem_u32(tmem_slot), kTmemCols);
-            tmem_relinquish();
-        }
+        tmem_alloc_pair(smem_u32(tmem_slot), kTmemCols);
+        tmem_relinquish_pair();
     }
     tc_fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();  // the other CTA's barriers exist
+    cluster_sync();  // the other CTA's barriers exist
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     pdl_trigger();
@@ -214,18 +209,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------ TMA producer
         uint32_t it = 0;
         bool ok = true;
-        const int b_rows = prm.NT / CG;
+        const int b_rows = prm.NT / 2;
         // MN-major tiles come in whole 64-row atoms
         const uint32_t b_bytes = (uint32_t)(B_MN ? (b_rows + 63) / 64 * 64 : b_rows) * kSlice * 2;
-        const uint32_t bytes = CG * (kATile + b_bytes);
+        const uint32_t bytes = 2 * (kATile + b_bytes);
         for (int v = first; v < prm.n_work && ok; v += pairs) {
             const Work w = work_of(prm, v);
-            const int m0 = (w.rt * CG + (int)rank) * 128;
+            const int m0 = (w.rt * 2 + (int)rank) * 128;
             const int n0 = w.ct * prm.NT + (int)rank * b_rows;
             for (int s = w.chunk; s < prm.slices; s += prm.chunks, ++it) {
                 const int st = it % kS;
                 if (it >= (uint32_t)kS &&
-                    !warp_wait<CG>(empty0 + 8u * st, (it / kS - 1) & 1, abort_flag, prm.status)) {
+                    !warp_wait<2>(empty0 + 8u * st, (it / kS - 1) & 1, abort_flag, prm.status)) {
                     ok = false;
                     break;
                 }
@@ -234,9 +229,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint32_t full = full0 + 8u * st;
                     if (rank == 0) mbar_expect_tx(full, bytes);
                     // both CTAs' bytes count on the leader's barrier
-                    const uint32_t bar = CG == 2 ? map_to_rank(full, 0) : full;
-                    load_tile<CG, A_MN>(dst, &tmA, m0, 128, s * kSlice, bar);
-                    load_tile<CG, B_MN>(dst + kATile, &tmB, n0, b_rows, s * kSlice, bar);
+                    const uint32_t bar = map_to_rank(full, 0);
+                    load_tile<2, A_MN>(dst, &tmA, m0, 128, s * kSlice, bar);
+                    load_tile<2, B_MN>(dst + kATile, &tmB, n0, b_rows, s * kSlice, bar);
                 }
                 __syncwarp();
             }
@@ -262,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Work w = work_of(prm, v);
             const int ab = j & 1;
             if (j >= 2 &&
-                !warp_wait<CG>(accempty0 + 8u * ab, ((j >> 1) - 1) & 1, abort_flag, prm.status)) {
+                !warp_wait<2>(accempty0 + 8u * ab, ((j >> 1) - 1) & 1, abort_flag, prm.status)) {
                 ok = false;
                 break;
             }
@@ -270,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t acc = tmem + ab * kMaxNT;
             for (int s = w.chunk; s < prm.slices; s += prm.chunks, ++it) {
                 const int st = it % kS;
-                if (!warp_wait<CG>(full0 + 8u * st, (it / kS) & 1, abort_flag, prm.status)) {
+                if (!warp_wait<2>(full0 + 8u * st, (it / kS) & 1, abort_flag, prm.status)) {
                     ok = false;
                     break;
                 }
@@ -282,24 +277,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int k = 0; k < kSlice / 16; ++k) {
                         const uint64_t ad = tile_desc<A_MN>(a, k), bd = tile_desc<B_MN>(b, k);
                         const uint32_t more = (s > w.chunk || k > 0) ? 1u : 0u;
-                        if (CG == 2) mma_ss_pair(acc, ad, bd, prm.idesc, more);
-                        else mma_ss(acc, ad, bd, prm.idesc, more);
+                        mma_ss_pair(acc, ad, bd, prm.idesc, more);
                     }
-                    if (CG == 2) mma_commit_pair(empty0 + 8u * st);
-                    else mma_commit(empty0 + 8u * st);
+                    mma_commit_pair(empty0 + 8u * st);
                 }
                 __syncwarp();
             }
             if (!ok) break;
             if (elect_one()) {
-                if (CG == 2) mma_commit_pair(accfull0 + 8u * ab);
-                else mma_commit(accfull0 + 8u * ab);
+                mma_commit_pair(accfull0 + 8u * ab);
             }
             __syncwarp();
         }
         if (elect_one()) {
-            if (CG == 2) mma_commit_pair(fin);
-            else mma_commit(fin);
+            mma_commit_pair(fin);
         }
         __syncwarp();
         const uint64_t tw = globaltimer_ns();
@@ -326,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         for (int v = first + ab * pairs; v < prm.n_work && ok; v += 2 * pairs, phase ^= 1) {
             const Work w = work_of(prm, v);
-            const int row0 = (w.rt * CG + (int)rank) * 128 + 32 * q;
+            const int row0 = (w.rt * 2 + (int)rank) * 128 + 32 * q;
             const int n0 = w.ct * prm.NT;  // first column of the tile
             // columns of the tile that exist
             const int width = row0 < prm.M ? min(prm.NT, prm.N - n0) : 0;
@@ -355,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 __syncwarp();
             }
-            ok = warp_wait<CG>(accfull0 + 8u * ab, phase, abort_flag, prm.status);
+            ok = warp_wait<2>(accfull0 + 8u * ab, phase, abort_flag, prm.status);
             tc_fence_after();
             for (int c = cfirst; c < width && ok; c += c % 64 ? 96 : 32) {
                 const int h = DEEP ? 0 : c / 32 & 1;  // staged block
@@ -365,20 +356,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
                     const int row = row0 + lane, at = n0 + c;
                     if (row >= prm.M) continue;
-                    if (OUT == kOutPart) {
-                        float* d = prm.part + ((int64_t)w.chunk * prm.M + row) * prm.ldp + at;
-                        const int n = min(prm.NT - c, (int)prm.ldp - at);
+                    float* d = prm.part + ((int64_t)w.chunk * prm.M + row) * prm.ldp + at;
+                    const int n = min(prm.NT - c, (int)prm.ldp - at);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            if (i < n)
-                                *reinterpret_cast<float4*>(d + i) =
-                                    make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-                    } else {
-                        float* d = prm.part + ((int64_t)w.chunk * prm.N + at) * prm.ldp + row;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i < width - c) d[i * prm.ldp] = x[i];
-                    }
+                    for (int i = 0; i < 32; i += 4)
+                        if (i < n)
+                            *reinterpret_cast<float4*>(d + i) =
+                                make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
                     continue;
                 }
                 // sums with the bias, as 16 pairs
@@ -466,10 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (c + (c % 64 ? 96 : 32) >= width) {  // the last block: the accumulator is read
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
-                        else mbar_arrive(accempty0 + 8u * ab);
-                    }
+                    if (lane == 0) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
                 }
                 switch (prm.act) {
                     case FLAREPP_ACT_RELU:
@@ -523,10 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ok && (width <= cfirst || OUT != kOutEpilogue)) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    if (CG == 2) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
-                    else mbar_arrive(accempty0 + 8u * ab);
-                }
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
             }
         }
         if (OUT == kOutEpilogue) {
@@ -541,12 +519,204 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_before();
     __syncthreads();
     // no CTA leaves while the other one may still signal it or read its shared memory
-    if (CG == 2) cluster_sync();
+    cluster_sync();
     tc_fence_after();
-    if (warp == 1) {
-        if (CG == 2) tmem_dealloc_pair(tmem, kTmemCols);
-        else tmem_dealloc(tmem, kTmemCols);
+    if (warp == 1) tmem_dealloc_pair(tmem, kTmemCols);
+}
+
+// ------------------------------------------------------------------ few rows
+// The layer for up to 256 rows of tokens: the weights are the tile's rows (128 of them, whatever the
+// number of tokens) and the tokens its columns, so the tensor cores' 128 rows are never idle and the
+// weights, whose bytes are the bound, are read once. A cluster of up to eight CTAs shares a tile, each
+// with every S-th slice of the contraction, so that a few tiles still draw on many SMs; the CTAs
+// leave their float32 sums in shared memory, and each adds a share of the columns over the cluster in
+// rank order and runs the epilogue on it. One launch, no workspace (48 rows of 4096 -> 1001 took 8.8 us
+// as chunk sums in memory and a second kernel).
+constexpr int kFewThreads = 256;
+constexpr int kFewStages = 4;
+constexpr int kFewRing = kFewStages * (kATile + kMaxNT * kSlice * 2);
+constexpr int kFewBars = 2 * kFewStages + 1;
+constexpr int kFewSmem = 1024 + kFewRing + kFewBars * 8 + 16;
+static_assert(kMaxNT * 128 * 4 <= kFewRing, "the sums reuse the ring");
+
+struct Few {
+    int M, N, NT;  // weights' rows, tokens, columns of the tile
+    int slices, share;  // slices of the contraction, CTAs per tile
+    uint32_t idesc, tmem_cols;
+    int act;
+    const __nv_bfloat16* bias;  // [M]
+    const __nv_bfloat16* R;     // [N][M], as Y and Z
+    __nv_bfloat16* Y;
+    __nv_bfloat16* Z;
+    int* status;
+};
+
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr));
+    return v;
+}
+
+template <bool A_MN>
+__global__ void __launch_bounds__(kFewThreads, 1)
+    lin_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                   const Few prm) {
+    extern __shared__ uint8_t smem_raw[];
+    // the same offset in every CTA of the cluster
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kFewRing);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kFewBars);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8u * kFewStages;
+    const uint32_t done = empty0 + 8u * kFewStages;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = prm.share > 1 ? (int)cluster_rank() : 0;
+    const int m0 = (int)blockIdx.x / prm.share * 128;
+    const uint32_t stage_bytes = kATile + prm.NT * kSlice * 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kFewStages; ++s) {
+            mbar_init(full0 + 8u * s, 1);
+            mbar_init(empty0 + 8u * s, 1);
+        }
+        mbar_init(done, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tmap(&tmA);
+        prefetch_tmap(&tmB);
     }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), prm.tmem_cols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pdl_trigger();
+    pdl_wait();
+
+    if (warp == 0) {
+        uint32_t it = 0;
+        bool ok = true;
+        for (int s = rank; s < prm.slices; s += prm.share, ++it) {
+            const int st = it % kFewStages;
+            if (it >= (uint32_t)kFewStages &&
+                !warp_wait<1>(empty0 + 8u * st, (it / kFewStages - 1) & 1, abort_flag, prm.status)) {
+                ok = false;
+                break;
+            }
+            if (elect_one()) {
+                const uint32_t dst = smem_u32(smem + st * (kFewRing / kFewStages));
+                mbar_expect_tx(full0 + 8u * st, stage_bytes);
+                load_tile<1, A_MN>(dst, &tmA, m0, 128, s * kSlice, full0 + 8u * st);
+                load_tile<1, false>(dst + kATile, &tmB, 0, prm.NT, s * kSlice, full0 + 8u * st);
+            }
+            __syncwarp();
+        }
+        if (!ok) {  // wait (bounded) until every copy issued has landed
+            const uint64_t t0 = globaltimer_ns();
+            for (int st = 0; st < kFewStages && (uint32_t)st < it; ++st) {
+                const uint32_t x = it - 1 - ((it - 1 - st) % kFewStages);
+                while (!mbar_try_wait(full0 + 8u * st, (x / kFewStages) & 1) &&
+                       globaltimer_ns() - t0 < kWaitLimitNs) {
+                }
+            }
+        }
+    } else if (warp == 1) {
+        uint32_t it = 0;
+        for (int s = rank; s < prm.slices; s += prm.share, ++it) {
+            const int st = it % kFewStages;
+            if (!warp_wait<1>(full0 + 8u * st, (it / kFewStages) & 1, abort_flag, prm.status)) break;
+            tc_fence_after();
+            const uint32_t a = smem_u32(smem + st * (kFewRing / kFewStages)), b = a + kATile;
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < kSlice / 16; ++k)
+                    mma_ss(tmem, tile_desc<A_MN>(a, k), tile_desc<false>(b, k), prm.idesc,
+                           (it > 0 || k > 0) ? 1u : 0u);
+                mma_commit(empty0 + 8u * st);
+            }
+            __syncwarp();
+        }
+        if (elect_one()) mma_commit(done);
+        __syncwarp();
+    }
+    __syncwarp();
+    // every warp: the sums from TMEM into sums[token][128], over the ring (its copies and products
+    // are done)
+    const bool ok = warp_wait<1>(done, 0, abort_flag, prm.status);
+    float* sums = reinterpret_cast<float*>(smem);
+    __syncthreads();  // an issuer that gave up has left its loop too
+    tc_fence_after();
+    if (ok) {
+        const int q = warp % 4;
+        float* mine = sums + 32 * q + lane;
+        for (int c = 16 * (warp / 4); c < prm.NT; c += 32) {
+            uint32_t r[16];
+            tmem_ld16(tmem + ((uint32_t)(32 * q) << 16) + c, r);
+            tmem_wait_ld16(r);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mine[(c + i) * 128] = __uint_as_float(r[i]);
+        }
+    }
+    tc_fence_before();
+    if (prm.share > 1) cluster_sync();
+    else __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, prm.tmem_cols);
+    // a warp takes a token at a time, a lane four of its outputs
+    const int m = m0 + 4 * lane;
+    const bool vec = prm.M % 4 == 0;
+    for (int t = rank + prm.share * warp; t < prm.N; t += prm.share * (kFewThreads / 32)) {
+        if (m >= prm.M) break;
+        const uint32_t at = smem_u32(sums + t * 128 + 4 * lane);
+        float4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < prm.share) v[k] = load_cluster(prm.share > 1 ? map_to_rank(at, k) : at);
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < prm.share) {
+                x[0] += v[k].x;
+                x[1] += v[k].y;
+                x[2] += v[k].z;
+                x[3] += v[k].w;
+            }
+        const int64_t o = (int64_t)t * prm.M + m;
+        if (prm.bias)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (m + k < prm.M) x[k] += __bfloat162float(prm.bias[m + k]);
+        if (prm.Z) {
+            if (vec)
+                *reinterpret_cast<uint2*>(prm.Z + o) =
+                    make_uint2(pack_bf16x2(pair(x[0], x[1])), pack_bf16x2(pair(x[2], x[3])));
+            else
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (m + k < prm.M) prm.Z[o + k] = __float2bfloat16_rn(x[k]);
+        }
+        const float2 y0 = halves(act_value2(prm.act, pair(x[0], x[1])));
+        const float2 y1 = halves(act_value2(prm.act, pair(x[2], x[3])));
+        float y[4] = {y0.x, y0.y, y1.x, y1.y};
+        if (prm.R)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (m + k < prm.M) y[k] += __bfloat162float(prm.R[o + k]);
+        if (vec)
+            *reinterpret_cast<uint2*>(prm.Y + o) =
+                make_uint2(pack_bf16x2(pair(y[0], y[1])), pack_bf16x2(pair(y[2], y[3])));
+        else
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (m + k < prm.M) prm.Y[o + k] = __float2bfloat16_rn(y[k]);
+    }
+    __syncwarp();
+    if (prm.share > 1) cluster_sync();  // the other CTAs may still read this one's sums
 }
 
 // ------------------------------------------------------------------ host side
@@ -581,11 +751,11 @@ bool make_map(CUtensorMap* m, const void* base, int64_t inner, int64_t lines, in
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CG, bool A_MN, bool B_MN, int OUT, bool DEEP>
+template <bool A_MN, bool B_MN, int OUT, bool DEEP>
 cudaError_t launch(const CUtensorMap* m, const Gemm& p, cudaStream_t st) {
-    using C = Cfg<CG, OUT, DEEP>;
+    using C = Cfg<OUT, DEEP>;
     static_assert(C::kSmem <= 232448 && C::kStages >= 3, "shared memory budget");
-    auto kernel = lin_gemm_kernel<CG, A_MN, B_MN, OUT, DEEP>;
+    auto kernel = lin_gemm_kernel<A_MN, B_MN, OUT, DEEP>;
     static std::atomic<int> fits[64];  // tiles that run at once on each device (0: not asked yet)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -599,51 +769,106 @@ cudaError_t launch(const CUtensorMap* m, const Gemm& p, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.x = 2;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = CG == 2 ? 2 : 1;
+    cfg.numAttrs = 2;
     int n = fits[dev].load();
     if (n == 0) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
         if (e != cudaSuccess) return e;
-        n = kNumSMs / CG;
-        if (CG == 2) {  // a die's odd SM cannot hold a pair
-            cfg.gridDim = dim3((unsigned)(kNumSMs / CG * CG));
-            int most = 0;
-            cudaLaunchConfig_t ask = cfg;
-            ask.attrs = &attr[1];
-            ask.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&most, kernel, &ask);
-            if (e != cudaSuccess) return e;
-            if (most > 0 && most < n) n = most;
-        }
+        n = kNumSMs / 2;
+        // a die's odd SM cannot hold a pair
+        cfg.gridDim = dim3(kNumSMs / 2 * 2);
+        int most = 0;
+        cudaLaunchConfig_t ask = cfg;
+        ask.attrs = &attr[1];
+        ask.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&most, kernel, &ask);
+        if (e != cudaSuccess) return e;
+        if (most > 0 && most < n) n = most;
         fits[dev].store(n);
     }
-    cfg.gridDim = dim3((unsigned)((p.n_work < n ? p.n_work : n) * CG));
+    cfg.gridDim = dim3((unsigned)((p.n_work < n ? p.n_work : n) * 2));
     return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], m[4], p);
+}
+
+template <bool A_MN>
+cudaError_t launch_few(const CUtensorMap* m, const Few& p, unsigned tiles, cudaStream_t st) {
+    auto kernel = lin_few_kernel<A_MN>;
+    static std::atomic<uint64_t> ready{0};  // devices whose shared-memory limit is raised
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!(ready.load() >> dev & 1)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
+        if (e != cudaSuccess) return e;
+        ready.fetch_or(uint64_t(1) << dev);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(tiles * (unsigned)p.share);
+    cfg.blockDim = dim3(kFewThreads);
+    cfg.dynamicSmemBytes = kFewSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.share;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.share > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], p);
 }
 
 }  // namespace
 
-LinPlan lin_plan(int64_t M, int64_t N, int64_t K, bool few_columns) {
+cudaError_t lin_few(int64_t rows, int64_t cols, int64_t K, const LinOperand& x,
+                    const LinOperand& w, const LinEpilogue& e, int* status, cudaStream_t st) {
+    Few p{};
+    p.M = (int)cols;
+    p.N = (int)rows;
+    p.NT = (int)cdiv(rows, 16) * 16;
+    p.slices = (int)cdiv(K, kSlice);
+    const int64_t tiles = cdiv(cols, 128);
+    p.share = 1;  // as many CTAs as the SMs take, with two slices each at least
+    while (p.share < 8 && tiles * p.share * 2 <= kNumSMs && p.slices >= 4 * p.share) p.share *= 2;
+    p.idesc = idesc_bf16_f32(128, p.NT, w.mn, false);
+    p.tmem_cols = 32;
+    while ((int)p.tmem_cols < p.NT) p.tmem_cols *= 2;
+    p.act = e.act;
+    p.bias = (const __nv_bfloat16*)e.bias;
+    p.R = (const __nv_bfloat16*)e.R;
+    p.Y = (__nv_bfloat16*)e.Y;
+    p.Z = (__nv_bfloat16*)e.Z;
+    p.status = status;
+    CUtensorMap m[2];
+    const bool ok = (w.mn ? make_map(&m[0], w.t, cols, K, w.pitch, 64, kSlice)
+                          : make_map(&m[0], w.t, K, cols, w.pitch, kSlice, 128)) &&
+                    make_map(&m[1], x.t, K, rows, x.pitch, kSlice, p.NT);
+    if (!ok) return cudaErrorInvalidValue;
+    return w.mn ? launch_few<true>(m, p, (unsigned)tiles, st)
+                : launch_few<false>(m, p, (unsigned)tiles, st);
+}
+
+LinPlan lin_plan(int64_t M, int64_t N, int64_t K) {
     LinPlan p{};
-    p.transposed = few_columns;
-    p.cg = few_columns ? 1 : 2;
     // equal column tiles, in whole 32-column blocks where there are several
     const int64_t ct = cdiv(N, kMaxNT);
     p.NT = (int)(ct == 1 ? cdiv(N, 16) * 16 : cdiv(cdiv(N, ct), 32) * 32);
-    const int64_t tiles = cdiv(M, 128 * p.cg) * cdiv(N, p.NT);
+    const int64_t tiles = cdiv(M, 256) * cdiv(N, p.NT);
     // How many chunks: the time of the waves of work items (0.3 us a slice and about 4 us of a wave's
     // own) and, with more than one, of writing and reading the partial sums (8 bytes a value at about 5 TB/s)
     // and of one launch more. Chunks have at least four slices.
-    const int64_t slices = cdiv(K, kSlice), units = kNumSMs / p.cg;
+    const int64_t slices = cdiv(K, kSlice), units = kNumSMs / 2;
     double best = 0;
     for (int64_t c = 1; c <= 64 && (c == 1 || slices / c >= 4); ++c) {
         const double waves = (double)cdiv(tiles * c, units);
         const double us = waves * (0.3 * (double)cdiv(slices, c) * p.NT / kMaxNT + 4) +
-                          (c > 1 || few_columns ? 3 + (double)c * M * N * 8 / 5e6 : 0);
+                          (c > 1 ? 3 + (double)c * M * N * 8 / 5e6 : 0);
         if (c == 1 || us < best) {
             best = us;
             p.chunks = (int)c;
@@ -658,7 +883,7 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     p.M = (int)M;
     p.N = (int)N;
     p.NT = plan.NT;
-    const int64_t row_tiles = cdiv(M, 128 * plan.cg), col_tiles = cdiv(N, plan.NT);
+    const int64_t row_tiles = cdiv(M, 256), col_tiles = cdiv(N, plan.NT);
     if (row_tiles * col_tiles * plan.chunks > 0x7fffffff) return cudaErrorInvalidValue;
     p.row_tiles = (int)row_tiles;
     p.col_tiles = (int)col_tiles;
@@ -667,7 +892,7 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     p.slices = (int)cdiv(K, kSlice);
     p.chunks = plan.chunks;
     p.backward = e.backward;
-    p.idesc = idesc_bf16_f32(128 * plan.cg, plan.NT, a.mn, b.mn);
+    p.idesc = idesc_bf16_f32(256, plan.NT, a.mn, b.mn);
     p.act = e.act;
     p.tma_out = N % 8 == 0;
     p.bias = (const __nv_bfloat16*)e.bias;
@@ -678,7 +903,7 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     p.ldp = e.ldp;
     p.status = status;
     CUtensorMap m[5];
-    const int b_rows = plan.NT / plan.cg;
+    const int b_rows = plan.NT / 2;
     bool ok = a.mn ? make_map(&m[0], a.t, M, K, a.pitch, 64, kSlice)
                    : make_map(&m[0], a.t, K, M, a.pitch, kSlice, 128);
     ok = ok && (b.mn ? make_map(&m[1], b.t, N, K, b.pitch, 64, kSlice)
@@ -690,24 +915,19 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
         if (e.R) ok = ok && make_map(&m[4], e.R, N, M, N, 32, 32);
     }
     if (!ok) return cudaErrorInvalidValue;
-    const int out = !e.part ? kOutEpilogue : plan.transposed ? kOutPartT : kOutPart;
-    if (plan.cg == 1) {
-        if (out != kOutPartT) return cudaErrorInvalidValue;
-        return a.mn ? launch<1, true, false, kOutPartT, true>(m, p, st)
-                    : launch<1, false, false, kOutPartT, true>(m, p, st);
-    }
+    const bool part = e.part != nullptr;
     const bool deep = p.slices >= kDeepSlices;
     if (a.mn)
-        return out == kOutPart ? launch<2, true, true, kOutPart, true>(m, p, st)
-               : deep          ? launch<2, true, true, kOutEpilogue, true>(m, p, st)
-                               : launch<2, true, true, kOutEpilogue, false>(m, p, st);
+        return part ? launch<true, true, kOutPart, true>(m, p, st)
+               : deep          ? launch<true, true, kOutEpilogue, true>(m, p, st)
+                               : launch<true, true, kOutEpilogue, false>(m, p, st);
     if (b.mn)
-        return out == kOutPart ? launch<2, false, true, kOutPart, true>(m, p, st)
-               : deep          ? launch<2, false, true, kOutEpilogue, true>(m, p, st)
-                               : launch<2, false, true, kOutEpilogue, false>(m, p, st);
-    return out == kOutPart ? launch<2, false, false, kOutPart, true>(m, p, st)
-           : deep          ? launch<2, false, false, kOutEpilogue, true>(m, p, st)
-                           : launch<2, false, false, kOutEpilogue, false>(m, p, st);
+        return part ? launch<false, true, kOutPart, true>(m, p, st)
+               : deep          ? launch<false, true, kOutEpilogue, true>(m, p, st)
+                               : launch<false, true, kOutEpilogue, false>(m, p, st);
+    return part ? launch<false, false, kOutPart, true>(m, p, st)
+           : deep          ? launch<false, false, kOutEpilogue, true>(m, p, st)
+                           : launch<false, false, kOutEpilogue, false>(m, p, st);
 }
 
 }  // namespace flarepp

@@ -793,37 +793,45 @@ def _scratch(workspace, nbytes, device):
 
 
 def _status_word(status, device):
-    return _need(status, "status", (1,), torch.int32, device, optional=True)
+    return 0 if status is None else _need(status, "status", (1,), torch.int32, device)
 
 
 def _linear_shape(X, W, act):
-    if act not in ACTIVATIONS:
+    """(shape, address of X, address of W) of a linear layer on device tensors X and W."""
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError(f"act must be one of {tuple(ACTIVATIONS)}")
-    if not isinstance(X, torch.Tensor) or not isinstance(W, torch.Tensor):
-        raise TypeError("X and W must be torch tensors")
-    if X.dtype not in _DTYPES:
-        raise TypeError(f"unsupported dtype {X.dtype}; the linear layer takes bfloat16")
+    dev = _cuda_device(X, "X")
+    dt = X.dtype
+    if dt not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dt}; the linear layer takes bfloat16")
+    if not isinstance(W, torch.Tensor):
+        raise TypeError("W must be a torch tensor")
     if W.dim() != 2 or X.dim() < 1 or X.shape[-1] != W.shape[1]:
         raise ValueError(f"expected X [..., in] and W [out, in], got {tuple(X.shape)} and "
                          f"{tuple(W.shape)}")
     out, in_ = W.shape
-    rows = X.numel() // in_ if in_ else 0
-    return LinearShape(rows, in_, out, _DTYPES[X.dtype], ACTIVATIONS[act])
+    wp = _need(W, "W", W.shape, dt, dev)
+    if not X.is_contiguous():
+        raise ValueError("X must be contiguous")
+    s = LinearShape(X.numel() // in_ if in_ else 0, in_, out, _DTYPES[dt], code)
+    return s, X.data_ptr(), wp
 
 
 def _linear(X, W, b, residual, act, Y, Z, keep, workspace, status, stream):
-    dev = _cuda_device(X, "X")
-    s = _linear_shape(X, W, act)
-    dt, shape = X.dtype, (*X.shape[:-1], s.out)
-    xp, wp = _need(X, "X", X.shape, dt, dev), _need(W, "W", W.shape, dt, dev)
-    bp = _need(b, "b", (s.out,), dt, dev, optional=True)
-    rp = _need(residual, "residual", shape, dt, dev, optional=True)
+    s, xp, wp = _linear_shape(X, W, act)
+    dev, dt, out = X.device, X.dtype, W.shape[0]
+    shape = (*X.shape[:-1], out)
+    bp = 0 if b is None else _need(b, "b", (out,), dt, dev)
+    rp = 0 if residual is None else _need(residual, "residual", shape, dt, dev)
     if Y is None:
         Y = torch.empty(shape, dtype=dt, device=dev)
+        yp = Y.data_ptr()
+    else:
+        yp = _need(Y, "Y", shape, dt, dev)
     if keep and Z is None:
         Z = torch.empty(shape, dtype=dt, device=dev)
-    yp = _need(Y, "Y", shape, dt, dev)
-    zp = _need(Z, "Z", shape, dt, dev, optional=True)
+    zp = 0 if Z is None else _need(Z, "Z", shape, dt, dev)
     ref = ctypes.byref(s)
     buf, wsp, wsn = _scratch(workspace, _entry("linear_workspace_bytes")(ref), dev)
     _enqueue("linear_fwd", dev, stream, ref, xp, wp, bp, rp, yp, zp, wsp, wsn,
@@ -852,10 +860,9 @@ def linear_bwd(X, W, dY, Z=None, act="none", bias=True, dX=None, dW=None, db=Non
     """(dX, dW, db), the gradients of ``linear_fwd_train`` for the output gradient dY [..., out]
     (the residual's gradient is dY). ``bias=False`` leaves db out, ``need`` dX or dW; what is left
     out is returned as None."""
-    dev = _cuda_device(X, "X")
-    s = _linear_shape(X, W, act)
-    dt, shape = X.dtype, (*X.shape[:-1], s.out)
-    xp, wp = _need(X, "X", X.shape, dt, dev), _need(W, "W", W.shape, dt, dev)
+    s, xp, wp = _linear_shape(X, W, act)
+    dev, dt = X.device, X.dtype
+    shape = (*X.shape[:-1], s.out)
     gp = _need(dY, "dY", shape, dt, dev)
     zp = _need(Z, "Z", shape, dt, dev, optional=act == "none")
     if need[0] and dX is None:
@@ -879,7 +886,9 @@ def _ids_of(ids):
     dev = _cuda_device(ids, "ids")
     if ids.dtype not in (torch.int32, torch.int64):
         raise TypeError(f"ids have dtype {ids.dtype}, expected int32 or int64")
-    return dev, _need(ids, "ids", ids.shape, ids.dtype, dev), ids.element_size()
+    if not ids.is_contiguous():
+        raise ValueError("ids must be contiguous")
+    return dev, ids.data_ptr(), 4 if ids.dtype is torch.int32 else 8
 
 
 def _float_dtype(t, what):
@@ -900,11 +909,15 @@ def embedding_fwd(ids, table, scale=1.0, Y=None, status=None, stream=None):
         raise ValueError("expected table [V, C]")
     V, C = table.shape
     tp = _need(table, "table", (V, C), dt, dev)
+    shape = (*ids.shape, C)
     if Y is None:
-        Y = torch.empty((*ids.shape, C), dtype=dt, device=dev)
+        Y = torch.empty(shape, dtype=dt, device=dev)
+        yp = Y.data_ptr()
+    else:
+        yp = _need(Y, "Y", shape, dt, dev)
     s = EmbeddingShape(ids.numel(), V, C, _DTYPES[dt], size)
-    _enqueue("embedding_fwd", dev, stream, ctypes.byref(s), ip, tp, float(scale),
-             _need(Y, "Y", (*ids.shape, C), dt, dev), _status_word(status, dev))
+    _enqueue("embedding_fwd", dev, stream, ctypes.byref(s), ip, tp, float(scale), yp,
+             _status_word(status, dev))
     return Y
 
 

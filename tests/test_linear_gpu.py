@@ -303,8 +303,9 @@ def test_refusals():
     with pytest.raises(flarepp.FlareppError) as e:  # in place
         flarepp.linear_fwd(X, W[:16].contiguous(), residual=X, Y=X)
     assert e.value.status == flarepp.ERR_INVALID_ARGUMENT
+    X15, W15 = X[:, :15].contiguous(), W[:, :15].contiguous()  # padded in the workspace
     with pytest.raises(flarepp.FlareppError) as e:
-        flarepp.linear_fwd(X, W, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        flarepp.linear_fwd(X15, W15, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == flarepp.ERR_WORKSPACE
     with pytest.raises(TypeError):
         flarepp.linear_bwd(X, W, R, None, "gelu")
