@@ -471,7 +471,8 @@ FLAREPP_API flarepp_status flarepp_embedding_bwd(const flarepp_embedding_shape* 
  * the float32 weights that a bf16 param is a rounded copy of. m, v: the moments; with 32-bit
  * states float32 [n] (m_scale, v_scale NULL); with 8-bit states one byte per value and one
  * float32 scale per block of 256 values (the last block may be shorter), [ceil(n / 256)].
- * Every pointer 16-byte aligned; no two buffers that a step writes may overlap.
+ * Every pointer 16-byte aligned but the scales' (4 bytes); no two buffers that a step writes may
+ * overlap.
  */
 typedef struct {
     void* param;

@@ -333,6 +333,9 @@ __global__ void __launch_bounds__(kThreads)
 constexpr int kFew = 48;
 constexpr int kMany = 384;
 
+// the scales, one value at a time, may start anywhere in a buffer of all tensors' scales
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
 bool type_ok(int32_t t) { return t == FLAREPP_F32 || t == FLAREPP_BF16; }
 
 // 0..5 for the type combinations of the step
@@ -351,7 +354,7 @@ flarepp_status check_tensor(const flarepp_adamw_tensor& t, bool q8) {
         if (!p || !aligned16(p)) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (!aligned16(t.master) || (t.master && t.param_dtype == FLAREPP_F32))
         return FLAREPP_ERR_INVALID_ARGUMENT;
-    if (q8 && (!t.m_scale || !t.v_scale || !aligned16(t.m_scale) || !aligned16(t.v_scale)))
+    if (q8 && (!t.m_scale || !t.v_scale || !aligned4(t.m_scale) || !aligned4(t.v_scale)))
         return FLAREPP_ERR_INVALID_ARGUMENT;
     const size_t n = (size_t)t.n, sb = (size_t)cdiv(t.n, kBlockVals) * 4;
     const size_t state = n * (q8 ? 1 : 4);
@@ -490,9 +493,11 @@ flarepp_status adamw_moments(const flarepp_adamw_tensor* ts, int64_t n, float* c
         const flarepp_adamw_tensor& t = ts[i];
         if (t.n < 0) return FLAREPP_ERR_INVALID_ARGUMENT;
         if (t.n == 0) continue;
-        const void* need[6] = {t.m, t.v, t.m_scale, t.v_scale, m_out[i], v_out[i]};
+        const void* need[4] = {t.m, t.v, m_out[i], v_out[i]};
         for (const void* p : need)
             if (!p || !aligned16(p)) return FLAREPP_ERR_INVALID_ARGUMENT;
+        if (!t.m_scale || !t.v_scale || !aligned4(t.m_scale) || !aligned4(t.v_scale))
+            return FLAREPP_ERR_INVALID_ARGUMENT;
         const size_t sb = (size_t)cdiv(t.n, kBlockVals) * 4;
         const Span outs[2] = {{m_out[i], (size_t)t.n * 4}, {v_out[i], (size_t)t.n * 4}};
         const Span ins[4] = {{t.m, (size_t)t.n}, {t.v, (size_t)t.n}, {t.m_scale, sb}, {t.v_scale, sb}};

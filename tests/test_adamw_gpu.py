@@ -232,6 +232,29 @@ def test_state_goes_on():
             assert torch.equal(a, b)
 
 
+def test_scales_of_all_tensors_in_one_buffer():
+    """Views of one buffer of scales start at any multiple of four bytes."""
+    ns = [300, 5, 1000]
+    g, params, grads, _ = setup(ns, ("f32", "f32", False), 4)
+    for x in grads:
+        x.copy_(torch.randn(x.numel(), generator=g))
+    blocks = [-(-n // 256) for n in ns]
+    at = [sum(blocks[:i]) for i in range(len(ns))]
+    ms, vs = (torch.zeros(sum(blocks), device="cuda") for _ in "mv")
+    state = {"m": [torch.zeros(n, dtype=torch.float8_e4m3fn, device="cuda") for n in ns],
+             "v": [torch.zeros(n, dtype=torch.uint8, device="cuda") for n in ns],
+             "m_scale": [ms[a:a + b] for a, b in zip(at, blocks)],
+             "v_scale": [vs[a:a + b] for a, b in zip(at, blocks)], "step": 0}
+    other = [p.clone() for p in params]
+    apart = flarepp.AdamW(other, grads, state_bits=8, **HYPER)
+    opt = flarepp.AdamW(params, grads, state_bits=8, state=state, **HYPER)
+    for o in (opt, apart):
+        o.step()
+    for a, b in zip(opt.moments()[0] + opt.moments()[1] + params,
+                    apart.moments()[0] + apart.moments()[1] + other):
+        assert torch.equal(a, b)
+
+
 def test_the_optimiser_keeps_its_buffers():
     """A parameter that the caller points elsewhere leaves the optimiser with the old buffer."""
     p, g = torch.ones(1000, device="cuda"), torch.ones(1000, device="cuda")
