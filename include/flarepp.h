@@ -353,15 +353,16 @@ FLAREPP_API flarepp_status flarepp_route_device_status(const flarepp_shape* shap
  *   kernel: which launch of later calls it applies to: 1 or 2, the encode of call 1 or 2;
  *     3, the decode; 4 + p, pass p of flarepp_route_bwd's tensor-core passes (0: the route
  *     pass of call 3, 1: of call 2, 2: of call 1, 3: the token pass of calls 2 and 3, 4: of
- *     call 1, 5: the merged token pass of calls 2 and 3); 0 turns the hook off (the
- *     default).
+ *     call 1, 5: the merged token pass of calls 2 and 3); 16, the tiled products of the linear
+ *     layer; 17, its product for few rows; 0 turns the hook off (the default).
  *   ring_item: the index, in the order it is loaded, of an item of CTA 0's ring of K/V (or
  *     Q/Z) tiles that the kernel's load warp then never loads, so that the waits for it run
  *     out (-1: none).
  *   wait_ns: the bound of every wait of that launch (0: the default of 2 s).
  * Process-wide state, for tests only: it applies to every later call from any thread until it
  * is turned off. A launch whose wait ran out stops early and records FLAREPP_ERR_TIMEOUT in
- * the device status word (flarepp_route_device_status); its outputs are invalid.
+ * the device status word (flarepp_route_device_status; the linear layer: its `status`); its outputs
+ * are invalid.
  */
 FLAREPP_API void flarepp_test_wait_fault(int kernel, int64_t ring_item, uint64_t wait_ns);
 

@@ -3,7 +3,8 @@
 // The gradient sums the rows of dY by id. Adding them with atomics would make the result depend on
 // their order and serialises where ids repeat (byte sequences meet each row hundreds of times), so
 // the positions are sorted by id first: a stable least-digit-first radix sort of (id, position) in
-// one pass for tables of up to 2,047 rows, two up to 4 M, three beyond. Then equal stretches of
+// one pass for tables of up to 2,047 rows, two up to 4 M, three beyond (up to 1,024 positions: in one
+// block's shared memory). Then equal stretches of
 // the sorted positions are summed in parallel whatever the lengths of the runs of one id; a run that
 // crosses from one stretch into the next leaves float32 partial sums, which a last kernel adds in
 // order. The gradient is written once: a bit per row says which rows no id names.
@@ -252,6 +253,44 @@ __global__ void __launch_bounds__(kSortThreads)
                 pos_out[at] = pos ? pos[i] : (uint32_t)i;
             }
         }
+    }
+}
+
+// Few positions: one block sorts (id, position) pairs in shared memory by a bitonic network, in one
+// launch instead of three or six, and clears the words that the sums count on. A warp's 32 pairs at
+// distances up to 32 lie in 64 neighbouring places, so only the longer distances need the block.
+constexpr int kFewThreads = 1024;
+constexpr int64_t kFewPositions = 1024;  // 4,096 take 20 us, more than the radix passes
+constexpr int64_t kFewWords = 1 << 16;  // words that the block clears; more take a memset
+
+template <typename I>
+__global__ void __launch_bounds__(kFewThreads)
+    few_kernel(const I* __restrict__ ids, int T, int places, int64_t V,
+               uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out,
+               uint32_t* __restrict__ words, int64_t n_words, int* status) {
+    extern __shared__ uint64_t pairs[];  // [places], a power of two of at least 64
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    for (int64_t i = threadIdx.x; i < n_words; i += kFewThreads) words[i] = 0;
+    for (int i = threadIdx.x; i < places; i += kFewThreads)
+        pairs[i] = i < T ? (uint64_t)key_at(ids, nullptr, i, V, status) << 32 | (uint32_t)i : ~0ull;
+    __syncthreads();
+    for (int size = 2; size <= places; size *= 2)
+        for (int d = size / 2; d > 0; d /= 2) {
+            for (int p = threadIdx.x; p < places / 2; p += kFewThreads) {
+                const int lo = 2 * p - (p & (d - 1)), hi = lo + d;
+                const uint64_t a = pairs[lo], b = pairs[hi];
+                if ((a > b) == ((lo & size) == 0)) {
+                    pairs[lo] = b;
+                    pairs[hi] = a;
+                }
+            }
+            if (d > 32 || d == 1) __syncthreads();  // after d = 1 a longer distance follows
+            else __syncwarp();
+        }
+    for (int i = threadIdx.x; i < T; i += kFewThreads) {
+        keys_out[i] = (uint32_t)(pairs[i] >> 32);
+        pos_out[i] = (uint32_t)pairs[i];
     }
 }
 
@@ -624,6 +663,23 @@ cudaError_t sort(const flarepp_embedding_shape& s, const Layout& L, const void* 
     return cudaSuccess;
 }
 
+template <typename I>
+cudaError_t sort_few(const flarepp_embedding_shape& s, const Layout& L, const void* ids, char* ws,
+                     int* status, cudaStream_t st) {
+    int places = 64;
+    while (places < s.T) places *= 2;
+    const int64_t words = (int64_t)(L.met_bytes / 4);
+    const bool clear = words <= kFewWords;
+    if (!clear) {
+        const cudaError_t e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_pdl(few_kernel<I>, dim3(1), dim3(kFewThreads), (size_t)places * 8, st,
+                      (const I*)ids, (int)s.T, places, s.V, (uint32_t*)(ws + L.off_keys[0]),
+                      (uint32_t*)(ws + L.off_pos[0]), (uint32_t*)(ws + L.off_met),
+                      clear ? words : 0, status);
+}
+
 template <typename E, int N>
 cudaError_t sums(const flarepp_embedding_shape& s, const Layout& L, int at, const void* dY,
                  float scale, void* dtable, char* ws, cudaStream_t st) {
@@ -709,9 +765,16 @@ flarepp_status embedding_bwd(const flarepp_embedding_shape* shape, const void* i
         return cudaMemsetAsync(dtable, 0, out_bytes, st) == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
     char* ws = (char*)workspace;
     int at = 0;
-    cudaError_t e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
-    if (e == cudaSuccess) e = s.id_bytes == 4 ? sort<int32_t>(s, L, ids, ws, status, &at, st)
-                                    : sort<int64_t>(s, L, ids, ws, status, &at, st);
+    cudaError_t e;
+    if (s.T <= kFewPositions) {
+        e = s.id_bytes == 4 ? sort_few<int32_t>(s, L, ids, ws, status, st)
+                            : sort_few<int64_t>(s, L, ids, ws, status, st);
+    } else {
+        e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
+        if (e == cudaSuccess)
+            e = s.id_bytes == 4 ? sort<int32_t>(s, L, ids, ws, status, &at, st)
+                                : sort<int64_t>(s, L, ids, ws, status, &at, st);
+    }
     if (e != cudaSuccess) return FLAREPP_ERR_CUDA;
     using B = __nv_bfloat16;
     if (s.dtype == FLAREPP_BF16) switch (vec_of(s)) {

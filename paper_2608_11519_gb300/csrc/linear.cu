@@ -9,8 +9,7 @@
 namespace flarepp {
 namespace {
 
-constexpr int kDzCols = 256;  // columns per block of dz_kernel: 32 lanes x 8
-constexpr int kDzRows = 8;    // rows a block of dz_kernel reads at once
+constexpr int kDzThreads = 256;
 
 // Up to four rows the layer can run on the CUDA cores (gemv_kernel): a weight then meets so few
 // multiplications that its bytes are the bound, and one launch without tensor maps is the shortest
@@ -238,23 +237,24 @@ __global__ void __launch_bounds__(kFinishThreads)
 }
 
 // dZ = dY o act'(Z) into lines of `ldz` values (not written when dZ is null), and the column sums
-// of the unrounded dZ over the block's rows into db_part[blockIdx.y][ldz]. VEC: eight values at
-// a time (cols a multiple of 8).
+// of the unrounded dZ over the block's rows into db_part[blockIdx.y][ldz]. `lanes` threads (a power of
+// two up to 32) take eight columns each of a row, and the block as many rows at once as it has room for.
+// VEC: eight values at a time (cols a multiple of 8).
 template <bool VEC>
-__global__ void __launch_bounds__(256, 4)
+__global__ void __launch_bounds__(kDzThreads, 4)
     dz_kernel(const __nv_bfloat16* __restrict__ dY, const __nv_bfloat16* __restrict__ Z,
-              int64_t rows, int64_t cols, int64_t rows_per, int act, int64_t ldz,
+              int64_t rows, int64_t cols, int64_t rows_per, int lanes, int act, int64_t ldz,
               __nv_bfloat16* __restrict__ dZ, float* __restrict__ db_part) {
     tc::pdl_trigger();
     tc::pdl_wait();
-    __shared__ float sums[kDzRows][kDzCols];
-    const int lane = threadIdx.x % 32, ty = threadIdx.x / 32;
-    const int64_t c = (int64_t)blockIdx.x * kDzCols + lane * 8;
+    __shared__ float sums[kDzThreads * 8];  // [rows at once][lanes * 8]
+    const int lane = threadIdx.x % lanes, ty = threadIdx.x / lanes, at_once = kDzThreads / lanes;
+    const int64_t c = ((int64_t)blockIdx.x * lanes + lane) * 8;
     const int64_t r1 = min(rows, (int64_t)(blockIdx.y + 1) * rows_per);
     uint64_t sum[4] = {0, 0, 0, 0};  // pairs
     if (c < cols) {
 #pragma unroll 2
-        for (int64_t r = (int64_t)blockIdx.y * rows_per + ty; r < r1; r += kDzRows) {
+        for (int64_t r = (int64_t)blockIdx.y * rows_per + ty; r < r1; r += at_once) {
             __align__(16) __nv_bfloat16 g[8], z[8];
             const int64_t at = r * cols + c;
             if (VEC) {
@@ -283,13 +283,14 @@ __global__ void __launch_bounds__(256, 4)
     if (!db_part) return;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-        *reinterpret_cast<float2*>(&sums[ty][lane * 8 + 2 * k]) = halves(sum[k]);
+        *reinterpret_cast<float2*>(&sums[threadIdx.x * 8 + 2 * k]) = halves(sum[k]);
     __syncthreads();
-    const int64_t col = (int64_t)blockIdx.x * kDzCols + threadIdx.x;
-    if (col < cols) {
+    const int width = lanes * 8;
+    const int64_t col = (int64_t)blockIdx.x * width + threadIdx.x;
+    if ((int)threadIdx.x < width && col < cols) {
         float s = 0.f;
-#pragma unroll
-        for (int k = 0; k < kDzRows; ++k) s += sums[k][threadIdx.x];
+#pragma unroll 8
+        for (int k = 0; k < at_once; ++k) s += sums[k * width + threadIdx.x];
         db_part[(int64_t)blockIdx.y * ldz + col] = s;
     }
 }
@@ -346,6 +347,7 @@ struct BwdLayout {
     LinPlan plan_x, plan_w;
     bool split_x, split_w;
     bool own_dz;  // dZ is laid out in the workspace (else the products read dY)
+    int dz_lanes;
     int64_t dz_blocks, dz_rows;
     size_t off_x, off_w, off_dz, off_db, off_px, off_pw, total;
 };
@@ -357,12 +359,14 @@ BwdLayout bwd_layout(const Shape& s) {
     L.split_x = L.plan_x.chunks > 1;
     L.split_w = L.plan_w.chunks > 1;
     L.own_dz = s.act != FLAREPP_ACT_NONE || s.N % 8 != 0;
-    // one wave of dz_kernel's blocks, four per SM, each of at least 32 rows
-    const int64_t col_blocks = cdiv(s.N, kDzCols);
-    int64_t want = 4 * kNumSMs / col_blocks;
+    // one wave of dz_kernel's blocks, four per SM, each of at least four rounds of rows
+    L.dz_lanes = 1;
+    while (L.dz_lanes < 32 && L.dz_lanes * 8 < s.N) L.dz_lanes *= 2;
+    const int64_t at_once = kDzThreads / L.dz_lanes;
+    int64_t want = 4 * kNumSMs / cdiv(s.N, L.dz_lanes * 8);
+    if (want > cdiv(s.T, 4 * at_once)) want = cdiv(s.T, 4 * at_once);
     if (want < 1) want = 1;
-    if (want > cdiv(s.T, 32)) want = cdiv(s.T, 32);
-    L.dz_rows = cdiv(cdiv(s.T, want), kDzRows) * kDzRows;
+    L.dz_rows = cdiv(cdiv(s.T, want), at_once) * at_once;
     L.dz_blocks = cdiv(s.T, L.dz_rows);
     const bool pad = s.K % 8 != 0;
     L.off_x = take(&L.total, pad ? s.T * pitch_of(s.K) * 2 : 0);
@@ -499,10 +503,10 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
     const bool own_dz = L.own_dz && (dX || dW);
     cudaError_t e = cudaSuccess;
     if (own_dz || db) {
-        const dim3 grid((unsigned)cdiv(s.N, kDzCols), (unsigned)L.dz_blocks);
+        const dim3 grid((unsigned)cdiv(s.N, L.dz_lanes * 8), (unsigned)L.dz_blocks);
         auto kernel = s.N % 8 ? dz_kernel<false> : dz_kernel<true>;
-        e = launch_pdl(kernel, grid, dim3(256), 0, st, (const __nv_bfloat16*)dY,
-                       (const __nv_bfloat16*)Z, s.T, s.N, L.dz_rows, s.act, ldz,
+        e = launch_pdl(kernel, grid, dim3(kDzThreads), 0, st, (const __nv_bfloat16*)dY,
+                       (const __nv_bfloat16*)Z, s.T, s.N, L.dz_rows, L.dz_lanes, s.act, ldz,
                        (__nv_bfloat16*)(own_dz ? ws + L.off_dz : nullptr),
                        (float*)(db ? ws + L.off_db : nullptr));
     }

@@ -42,6 +42,8 @@ constexpr int kMaxNT = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int kMaxStages = 8;
+// the launches' numbers for the test hook of the bounded waits (flarepp_test_wait_fault)
+constexpr int kProductKernel = 16, kFewKernel = 17;
 constexpr int kDeepSlices = 12;  // slices of a contraction from which the deep form runs
 constexpr int kBlockBytes = 32 * 32 * 2;  // what an epilogue warp stages at a time
 constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + 2 * kEpiWarps;
@@ -65,6 +67,14 @@ struct Cfg {
     static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kBias + kNumBars * 8 + 16;
 };
 
+// The bound of every wait of a launch, where a wait that gave up is recorded, and (for tests) the ring
+// item that CTA 0's producer never loads, or -1.
+struct Waits {
+    uint64_t limit_ns;
+    int* status;
+    int64_t withheld;
+};
+
 struct Gemm {
     int M, N, NT;
     int row_tiles, col_tiles, tiles, n_work;
@@ -79,7 +89,7 @@ struct Gemm {
     __nv_bfloat16* Z;
     float* part;
     int64_t ldp;
-    int* status;
+    Waits waits;
 };
 
 struct Work {
@@ -109,7 +119,7 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
 // All lanes of a warp wait for a phase; false once this wait or another one of the CTA gave up.
 template <int CG>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                          int* status) {
+                                          const Waits& w) {
     bool got = try_wait<CG>(bar, parity);
     if (!got) {
         const uint64_t t0 = globaltimer_ns();
@@ -118,9 +128,9 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
             if (got) break;
             if ((i & 63u) == 0) {
                 if (*abort_flag) break;
-                if (globaltimer_ns() - t0 > kWaitLimitNs) {
+                if (globaltimer_ns() - t0 > w.limit_ns) {
                     *abort_flag = 1;
-                    if (status) atomicExch(status, (int)FLAREPP_ERR_TIMEOUT);
+                    if (w.status) atomicExch(w.status, (int)FLAREPP_ERR_TIMEOUT);
                     break;
                 }
             }
@@ -220,11 +230,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int s = w.chunk; s < prm.slices; s += prm.chunks, ++it) {
                 const int st = it % kS;
                 if (it >= (uint32_t)kS &&
-                    !warp_wait<2>(empty0 + 8u * st, (it / kS - 1) & 1, abort_flag, prm.status)) {
+                    !warp_wait<2>(empty0 + 8u * st, (it / kS - 1) & 1, abort_flag, prm.waits)) {
                     ok = false;
                     break;
                 }
-                if (elect_one()) {
+                if (elect_one() && !(blockIdx.x == 0 && it == prm.waits.withheld)) {
                     const uint32_t dst = smem_u32(smem + st * C::kStage);
                     const uint32_t full = full0 + 8u * st;
                     if (rank == 0) mbar_expect_tx(full, bytes);
@@ -257,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Work w = work_of(prm, v);
             const int ab = j & 1;
             if (j >= 2 &&
-                !warp_wait<2>(accempty0 + 8u * ab, ((j >> 1) - 1) & 1, abort_flag, prm.status)) {
+                !warp_wait<2>(accempty0 + 8u * ab, ((j >> 1) - 1) & 1, abort_flag, prm.waits)) {
                 ok = false;
                 break;
             }
@@ -265,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t acc = tmem + ab * kMaxNT;
             for (int s = w.chunk; s < prm.slices; s += prm.chunks, ++it) {
                 const int st = it % kS;
-                if (!warp_wait<2>(full0 + 8u * st, (it / kS) & 1, abort_flag, prm.status)) {
+                if (!warp_wait<2>(full0 + 8u * st, (it / kS) & 1, abort_flag, prm.waits)) {
                     ok = false;
                     break;
                 }
@@ -346,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 __syncwarp();
             }
-            ok = warp_wait<2>(accfull0 + 8u * ab, phase, abort_flag, prm.status);
+            ok = warp_wait<2>(accfull0 + 8u * ab, phase, abort_flag, prm.waits);
             tc_fence_after();
             for (int c = cfirst; c < width && ok; c += c % 64 ? 96 : 32) {
                 const int h = DEEP ? 0 : c / 32 & 1;  // staged block
@@ -426,8 +436,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     } else {
                         __syncwarp();
-                        for (int r = 0; r < rows; ++r)
-                            if (lane < cols)
+#pragma unroll 8
+                        for (int r = 0; r < 32; ++r)
+                            if (r < rows && lane < cols)
                                 out[(int64_t)(row0 + r) * prm.N + n0 + c + lane] = *value(hb, r, lane);
                         __syncwarp();
                     }
@@ -468,12 +479,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (prm.R) {
                     if (tma_r) {
-                        ok = warp_wait<1>(rfull + 8u * hy, r_phase >> hy & 1, abort_flag, prm.status);
+                        ok = warp_wait<1>(rfull + 8u * hy, r_phase >> hy & 1, abort_flag, prm.waits);
                         if (!ok) break;
                         r_phase ^= 1u << hy;
                     } else {
-                        for (int r = 0; r < rows; ++r)
-                            if (lane < cols)
+#pragma unroll 8
+                        for (int r = 0; r < 32; ++r)
+                            if (r < rows && lane < cols)
                                 *value(hy, r, lane) = prm.R[(int64_t)(row0 + r) * prm.N + n0 + c + lane];
                         __syncwarp();
                     }
@@ -548,7 +560,7 @@ struct Few {
     const __nv_bfloat16* R;     // [N][M], as Y and Z
     __nv_bfloat16* Y;
     __nv_bfloat16* Z;
-    int* status;
+    Waits waits;
 };
 
 __device__ __forceinline__ float4 load_cluster(uint32_t addr) {
@@ -604,11 +616,11 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         for (int s = rank; s < prm.slices; s += prm.share, ++it) {
             const int st = it % kFewStages;
             if (it >= (uint32_t)kFewStages &&
-                !warp_wait<1>(empty0 + 8u * st, (it / kFewStages - 1) & 1, abort_flag, prm.status)) {
+                !warp_wait<1>(empty0 + 8u * st, (it / kFewStages - 1) & 1, abort_flag, prm.waits)) {
                 ok = false;
                 break;
             }
-            if (elect_one()) {
+            if (elect_one() && !(blockIdx.x == 0 && it == prm.waits.withheld)) {
                 const uint32_t dst = smem_u32(smem + st * (kFewRing / kFewStages));
                 mbar_expect_tx(full0 + 8u * st, stage_bytes);
                 load_tile<1, A_MN>(dst, &tmA, m0, 128, s * kSlice, full0 + 8u * st);
@@ -629,7 +641,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         uint32_t it = 0;
         for (int s = rank; s < prm.slices; s += prm.share, ++it) {
             const int st = it % kFewStages;
-            if (!warp_wait<1>(full0 + 8u * st, (it / kFewStages) & 1, abort_flag, prm.status)) break;
+            if (!warp_wait<1>(full0 + 8u * st, (it / kFewStages) & 1, abort_flag, prm.waits)) break;
             tc_fence_after();
             const uint32_t a = smem_u32(smem + st * (kFewRing / kFewStages)), b = a + kATile;
             if (elect_one()) {
@@ -647,7 +659,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     __syncwarp();
     // every warp: the sums from TMEM into sums[token][128], over the ring (its copies and products
     // are done)
-    const bool ok = warp_wait<1>(done, 0, abort_flag, prm.status);
+    const bool ok = warp_wait<1>(done, 0, abort_flag, prm.waits);
     float* sums = reinterpret_cast<float*>(smem);
     __syncthreads();  // an issuer that gave up has left its loop too
     tc_fence_after();
@@ -844,7 +856,8 @@ cudaError_t lin_few(int64_t rows, int64_t cols, int64_t K, const LinOperand& x,
     p.R = (const __nv_bfloat16*)e.R;
     p.Y = (__nv_bfloat16*)e.Y;
     p.Z = (__nv_bfloat16*)e.Z;
-    p.status = status;
+    p.waits.status = status;
+    test_fault_for(kFewKernel, &p.waits.limit_ns, &p.waits.withheld);
     CUtensorMap m[2];
     const bool ok = (w.mn ? make_map(&m[0], w.t, cols, K, w.pitch, 64, kSlice)
                           : make_map(&m[0], w.t, K, cols, w.pitch, kSlice, 128)) &&
@@ -901,7 +914,8 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     p.Z = (__nv_bfloat16*)e.Z;
     p.part = e.part;
     p.ldp = e.ldp;
-    p.status = status;
+    p.waits.status = status;
+    test_fault_for(kProductKernel, &p.waits.limit_ns, &p.waits.withheld);
     CUtensorMap m[5];
     const int b_rows = plan.NT / 2;
     bool ok = a.mn ? make_map(&m[0], a.t, M, K, a.pitch, 64, kSlice)

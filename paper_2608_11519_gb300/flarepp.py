@@ -1039,10 +1039,9 @@ class AdamW:
                 given = [torch.empty(p.shape, device=self.device) for p in self.params]
             if len(given) != len(self.params):
                 raise ValueError(f"{name} has {len(given)} tensors, expected {len(self.params)}")
-            ptrs = (ctypes.c_void_p * max(1, len(given)))()
-            for i, (t, p) in enumerate(zip(given, self.params)):
-                ptrs[i] = _need(t, f"{name}[{i}]", p.shape, torch.float32, self.device)
-            outs.append((given, ptrs))
+            ptrs = [_need(t, name, p.shape, torch.float32, self.device)
+                    for t, p in zip(given, self.params)]
+            outs.append((given, (ctypes.c_void_p * max(1, len(ptrs)))(*ptrs)))
         if self.params:
             _enqueue("adamw_moments", self.device, stream, self._table, len(self.params),
                      outs[0][1], outs[1][1])
