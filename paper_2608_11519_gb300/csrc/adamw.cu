@@ -21,6 +21,7 @@
 #include <cuda_runtime.h>
 #include <math.h>
 
+#include "checks.h"
 #include "flarepp_internal.h"
 #include "tc_ptx.cuh"
 

@@ -10,6 +10,7 @@
 #include <utility>
 #include <vector>
 
+#include "checks.h"
 #include "flarepp_internal.h"
 
 namespace flarepp {

@@ -14,29 +14,6 @@ constexpr size_t kWsAlign = 256;  // alignment of every workspace sub-buffer
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-inline bool aligned16(const void* ptr) { return ((uintptr_t)ptr & 15u) == 0; }
-
-inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-    if (!a || !b || na == 0 || nb == 0) return false;
-    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-    return a0 < b0 + nb && b0 < a0 + na;
-}
-
-// A buffer of a call: what it writes must not overlap anything else of the call.
-struct Span {
-    const void* p;
-    size_t bytes;
-};
-inline bool disjoint(const Span* outs, int n_outs, const Span* ins, int n_ins) {
-    for (int i = 0; i < n_outs; ++i) {
-        for (int j = 0; j < n_ins; ++j)
-            if (overlaps(outs[i].p, outs[i].bytes, ins[j].p, ins[j].bytes)) return false;
-        for (int j = 0; j < i; ++j)
-            if (overlaps(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes)) return false;
-    }
-    return true;
-}
-
 // Which kernels a shape runs on.
 enum Path : int {
     kPathSimt = 0,  // CUDA-core kernels: the float32 dtype path

@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 #include <math.h>
 
+#include "checks.h"
 #include "linear_internal.h"
 #include "tc_ptx.cuh"
 
@@ -25,9 +26,16 @@ bool use_gemv(int64_t T, int64_t K, int64_t N) {
 bool use_few(int64_t T, int64_t depth) { return T <= (depth >= 1024 ? kFewRows : kFewRows / 2); }
 constexpr int kGemvWarps = 8;
 
+constexpr int64_t kPadWRows = 4096;
+
 // The pitch of lines that the layer lays out itself: whole 128-byte lines, so that a 128-byte row of
 // a TMA box is one line and not parts of two.
 int64_t pitch_of(int64_t n) { return cdiv(n, 64) * 64; }
+// What TMA cannot address is laid out anew; so is W where its lines are not whole 128-byte lines and
+// 16 or more row tiles read it (20,011 rows of 1000 -> 1544: 72 us as it lies, 61 with the copy, which is 3 of
+// them; the lines of X, read as often as written, are not worth one).
+bool pad_x(int64_t K) { return K % 8 != 0; }
+bool pad_w(int64_t K, int64_t T) { return K % 8 != 0 || (K % 64 != 0 && T >= kPadWRows); }
 
 // The layer for T <= RT rows, `in` a multiple of 8. A warp takes RW rows of W at a time, a lane every
 // 32nd vector of eight weights of each, U of them in flight (RW * U = 8 loads of 16 bytes a lane
@@ -335,9 +343,8 @@ FwdLayout fwd_layout(const Shape& s) {
     L.few = use_few(s.T, s.K);
     if (!L.few) L.plan = lin_plan(s.T, s.N, s.K);
     L.split = L.plan.chunks > 1;
-    const bool pad = s.K % 8 != 0;
-    L.off_x = take(&L.total, pad ? s.T * pitch_of(s.K) * 2 : 0);
-    L.off_w = take(&L.total, pad ? s.N * pitch_of(s.K) * 2 : 0);
+    L.off_x = take(&L.total, pad_x(s.K) ? s.T * pitch_of(s.K) * 2 : 0);
+    L.off_w = take(&L.total, pad_w(s.K, s.T) ? s.N * pitch_of(s.K) * 2 : 0);
     L.off_part = take(&L.total, L.split ? (int64_t)part_bytes(L.plan, s.T, s.N) : 0);
     return L;
 }
@@ -368,9 +375,8 @@ BwdLayout bwd_layout(const Shape& s) {
     if (want < 1) want = 1;
     L.dz_rows = cdiv(cdiv(s.T, want), at_once) * at_once;
     L.dz_blocks = cdiv(s.T, L.dz_rows);
-    const bool pad = s.K % 8 != 0;
-    L.off_x = take(&L.total, pad ? s.T * pitch_of(s.K) * 2 : 0);
-    L.off_w = take(&L.total, pad ? s.N * pitch_of(s.K) * 2 : 0);
+    L.off_x = take(&L.total, pad_x(s.K) ? s.T * pitch_of(s.K) * 2 : 0);
+    L.off_w = take(&L.total, pad_w(s.K, s.T) ? s.N * pitch_of(s.K) * 2 : 0);
     L.off_dz = take(&L.total, L.own_dz ? s.T * pitch_of(s.N) * 2 : 0);
     L.off_db = take(&L.total, L.dz_blocks * pitch_of(s.N) * 4);
     L.off_px = take(&L.total, L.split_x ? (int64_t)part_bytes(L.plan_x, s.T, s.K) : 0);
@@ -454,11 +460,12 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
     }
     char* ws = (char*)workspace;
     LinOperand x{X, s.K, 0}, w{W, s.K, 0};
-    if (s.K % 8) {
-        if (pad(X, s.T, s.K, ws + L.off_x, st) != cudaSuccess ||
-            pad(W, s.N, s.K, ws + L.off_w, st) != cudaSuccess)
-            return FLAREPP_ERR_CUDA;
+    if (pad_x(s.K)) {
+        if (pad(X, s.T, s.K, ws + L.off_x, st) != cudaSuccess) return FLAREPP_ERR_CUDA;
         x = {ws + L.off_x, pitch_of(s.K), 0};
+    }
+    if (pad_w(s.K, s.T)) {
+        if (pad(W, s.N, s.K, ws + L.off_w, st) != cudaSuccess) return FLAREPP_ERR_CUDA;
         w = {ws + L.off_w, pitch_of(s.K), 0};
     }
     const cudaError_t err = L.few ? lin_few(s.T, s.N, s.K, x, w, e, status, st)
@@ -516,10 +523,12 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
         sums.db = nullptr;
     }
     LinOperand x{X, s.K, 0}, w{W, s.K, 0};
-    if (s.K % 8) {
+    if (pad_x(s.K)) {
         if (e == cudaSuccess && dW) e = pad(X, s.T, s.K, ws + L.off_x, st);
-        if (e == cudaSuccess && dX) e = pad(W, s.N, s.K, ws + L.off_w, st);
         x = {ws + L.off_x, pitch_of(s.K), 0};
+    }
+    if (pad_w(s.K, s.T)) {
+        if (e == cudaSuccess && dX) e = pad(W, s.N, s.K, ws + L.off_w, st);
         w = {ws + L.off_w, pitch_of(s.K), 0};
     }
     const LinOperand dz{own_dz ? ws + L.off_dz : dY, own_dz ? ldz : s.N, 0};

@@ -26,7 +26,7 @@
 #include <atomic>
 
 #include "linear_internal.h"
-#include "tc_ptx.cuh"
+#include "tc_pair_ptx.cuh"
 
 namespace flarepp {
 namespace {
