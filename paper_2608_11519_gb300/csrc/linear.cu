@@ -349,8 +349,15 @@ FwdLayout fwd_layout(const Shape& s) {
     return L;
 }
 
+// Whether one kernel makes dZ on its way to dX (lin_fused): with rows for every pair of CTAs, and outputs
+// that fill its slices of 64.
+bool use_fused(const Shape& s) {
+    return s.act != FLAREPP_ACT_NONE && s.K % 8 == 0 && s.K <= kFusedIn && s.N % 8 == 0 &&
+           s.N >= 64 && s.N <= kFusedOut && s.T >= 64 * kNumSMs;
+}
+
 struct BwdLayout {
-    bool few;
+    bool few, fused;
     LinPlan plan_x, plan_w;
     bool split_x, split_w;
     bool own_dz;  // dZ is laid out in the workspace (else the products read dY)
@@ -361,6 +368,7 @@ struct BwdLayout {
 BwdLayout bwd_layout(const Shape& s) {
     BwdLayout L{};
     L.few = use_few(s.T, s.N);
+    L.fused = use_fused(s);
     if (!L.few) L.plan_x = lin_plan(s.T, s.K, s.N);
     L.plan_w = lin_plan(s.N, s.K, s.T);
     L.split_x = L.plan_x.chunks > 1;
@@ -378,7 +386,7 @@ BwdLayout bwd_layout(const Shape& s) {
     L.off_x = take(&L.total, pad_x(s.K) ? s.T * pitch_of(s.K) * 2 : 0);
     L.off_w = take(&L.total, pad_w(s.K, s.T) ? s.N * pitch_of(s.K) * 2 : 0);
     L.off_dz = take(&L.total, L.own_dz ? s.T * pitch_of(s.N) * 2 : 0);
-    L.off_db = take(&L.total, L.dz_blocks * pitch_of(s.N) * 4);
+    L.off_db = take(&L.total, (L.dz_blocks > kNumSMs ? L.dz_blocks : kNumSMs) * pitch_of(s.N) * 4);
     L.off_px = take(&L.total, L.split_x ? (int64_t)part_bytes(L.plan_x, s.T, s.K) : 0);
     L.off_pw = take(&L.total, L.split_w ? (int64_t)part_bytes(L.plan_w, s.N, s.K) : 0);
     return L;
@@ -509,18 +517,14 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
     const int64_t ldz = pitch_of(s.N);
     const bool own_dz = L.own_dz && (dX || dW);
     cudaError_t e = cudaSuccess;
-    if (own_dz || db) {
+    const bool fused = L.fused && dX;
+    if (!fused && (own_dz || db)) {
         const dim3 grid((unsigned)cdiv(s.N, L.dz_lanes * 8), (unsigned)L.dz_blocks);
         auto kernel = s.N % 8 ? dz_kernel<false> : dz_kernel<true>;
         e = launch_pdl(kernel, grid, dim3(kDzThreads), 0, st, (const __nv_bfloat16*)dY,
                        (const __nv_bfloat16*)Z, s.T, s.N, L.dz_rows, L.dz_lanes, s.act, ldz,
                        (__nv_bfloat16*)(own_dz ? ws + L.off_dz : nullptr),
                        (float*)(db ? ws + L.off_db : nullptr));
-    }
-    DbSums sums{(const float*)(ws + L.off_db), (int)L.dz_blocks, s.N, ldz, (__nv_bfloat16*)db};
-    if (e == cudaSuccess && db && !(dW && L.split_w)) {
-        e = launch_pdl(db_kernel, dim3((unsigned)cdiv(s.N, 32)), dim3(kDbThreads), 0, st, sums);
-        sums.db = nullptr;
     }
     LinOperand x{X, s.K, 0}, w{W, s.K, 0};
     if (pad_x(s.K)) {
@@ -531,10 +535,20 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
         if (e == cudaSuccess && dX) e = pad(W, s.N, s.K, ws + L.off_w, st);
         w = {ws + L.off_w, pitch_of(s.K), 0};
     }
+    int db_parts = (int)L.dz_blocks;
+    if (e == cudaSuccess && fused)
+        e = lin_fused(s.T, s.K, s.N, s.act, dY, Z, {w.t, w.pitch, 1}, dX,
+                      dW ? ws + L.off_dz : nullptr, (float*)(db ? ws + L.off_db : nullptr), ldz,
+                      &db_parts, status, st);
+    DbSums sums{(const float*)(ws + L.off_db), db_parts, s.N, ldz, (__nv_bfloat16*)db};
+    if (e == cudaSuccess && db && !(dW && L.split_w)) {
+        e = launch_pdl(db_kernel, dim3((unsigned)cdiv(s.N, 32)), dim3(kDbThreads), 0, st, sums);
+        sums.db = nullptr;
+    }
     const LinOperand dz{own_dz ? ws + L.off_dz : dY, own_dz ? ldz : s.N, 0};
     // dX takes the rows from the last to the first and dW from the first on: each then finds in the L2
     // what was written or read last
-    if (e == cudaSuccess && dX) {
+    if (e == cudaSuccess && dX && !fused) {
         const LinEpilogue to_dx{FLAREPP_ACT_NONE, nullptr, nullptr, dX, nullptr, nullptr, 0, 1};
         const LinOperand wt{w.t, w.pitch, 1};
         e = L.few ? lin_few(s.T, s.K, s.N, dz, wt, to_dx, status, st)

@@ -46,6 +46,15 @@ constexpr int64_t kFewRows = 256;
 cudaError_t lin_few(int64_t rows, int64_t cols, int64_t K, const LinOperand& x,
                     const LinOperand& w, const LinEpilogue& e, int* status, cudaStream_t st);
 
+// dX = (dY o act'(Z)) W for a layer of up to kFusedIn inputs (a multiple of 8) and kFusedOut outputs (a
+// multiple of 8) with an activation, in one pass that also leaves dZ (when it is not null, lines of `ldz`)
+// and per CTA the column sums of dZ (db_part[ctas][ldz], at most kNumSMs rows, when it is not null). w: W
+// with its inputs innermost.
+constexpr int64_t kFusedIn = 256, kFusedOut = 512;
+cudaError_t lin_fused(int64_t T, int64_t K, int64_t N, int act, const void* dY, const void* Z,
+                      const LinOperand& w, void* dX, void* dZ, float* db_part, int64_t ldz,
+                      int* ctas, int* status, cudaStream_t st);
+
 // ---- activations (flarepp_activation) and their slopes, float32
 __device__ __forceinline__ float rcp_approx(float x) {
     float r;

@@ -8,44 +8,37 @@
 // runs in slices of 64 (a 128-byte swizzled row). Each CTA loads its own 128 rows of A and half of
 // the columns of B, so a slice costs 32 KB of shared-memory fill per CTA instead of 48 KB and B crosses
 // the L2 half as often. The walk over tiles is persistent; chunks cut a long contraction when there are few
-// tiles. Few tokens have a kernel of their own below.
+// tiles. Few tokens (tc_linear_few.cu) and the backward of narrow layers (tc_linear_fused.cu) have kernels of
+// their own.
 //
 // Roles (20 warps): warp 0 the TMA producer, warp 1 the MMA issuer (in the pair's leader),
 // warps 4..19 the epilogue: two groups of eight warps take the tiles in turn, so that one group's
 // loads and stores fall into the other one's arithmetic; a warp takes four 32-row x 32-column blocks of
-// a tile (TMEM lane = tile row), staged in shared memory by turns for their TMA stores. Group g reads TMEM accumulator g
-// of 256 columns, so the epilogue of a tile overlaps the products of the next. Sixteen epilogue warps, because a memory-bound layer leaves
-// about 16 issue slots per output value for everything, and the activation's chain of dependent
-// instructions needs four warps per scheduler to hide (with eight warps of 64 columns a half and
-// unpaired arithmetic the 65,536 x 256 -> 512 GELU layer took 46 us). Every wait is bounded (2 s of %globaltimer): on expiry the kernel records
-// FLAREPP_ERR_TIMEOUT in the status word, every role leaves its loops, the producer waits for its
-// copies in flight, the issuer for its products, and TMEM is freed.
-#include <cuda.h>
-#include <cudaTypedefs.h>
-
-#include <atomic>
-
-#include "linear_internal.h"
-#include "tc_pair_ptx.cuh"
+// a tile (TMEM lane = tile row), staged in shared memory by turns for their TMA stores. Group g reads
+// TMEM accumulator g of 256 columns, so the epilogue of a tile overlaps the products of the next.
+// Every wait is bounded (2 s of %globaltimer): on expiry the kernel records FLAREPP_ERR_TIMEOUT in the
+// status word, every role leaves its loops, the producer waits for its copies in flight, the issuer for
+// its products, and TMEM is freed.
+//
+// What bounds it: long contractions the tensor cores (16384 x 4096 x 4096: 280 us cold, 1965 TFLOP/s; 317 us
+// once the power limit holds the clock); wide outputs of short contractions the writes, which HBM
+// takes at 4.0 TB/s where nothing is read (measured with fills) and at up to 2.4 beside twice as many reads. With
+// GELU or SiLU a pair of outputs takes 24 cycles of the special-function unit and 22 of the multiply-add
+// pipe per scheduler, about what the writes leave, and a group waits for its accumulator's next products after
+// that: 65,536 x 256 -> 512 takes 24 us without an activation and 31.5 with GELU. Measured and left: sixteen
+// warps on every tile (36 us: a tile's fixed latencies are then in every warp's way), 16-column halves with the
+// next loads ahead (38 us: too few independent chains), eight warps of 64 columns and unpaired arithmetic
+// (46 us), more registers for the epilogue by setmaxnreg (spills).
+#include "tc_linear_common.cuh"
 
 namespace flarepp {
 namespace {
 
-using namespace tc;
-
 constexpr int kThreads = 640;
 constexpr int kFirstEpiWarp = 4;
 constexpr int kEpiWarps = 16;
-constexpr int kSlice = 64;  // contraction values per ring stage: one 128-byte row
-constexpr int kATile = 128 * kSlice * 2;
-constexpr int kMaxNT = 256;
-constexpr uint32_t kTmemCols = 512;
-constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int kMaxStages = 8;
-// the launches' numbers for the test hook of the bounded waits (flarepp_test_wait_fault)
-constexpr int kProductKernel = 16, kFewKernel = 17;
 constexpr int kDeepSlices = 12;  // slices of a contraction from which the deep form runs
-constexpr int kBlockBytes = 32 * 32 * 2;  // what an epilogue warp stages at a time
 constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + 2 * kEpiWarps;
 
 enum Out { kOutEpilogue, kOutPart };
@@ -62,17 +55,9 @@ struct Cfg {
     static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * kBlocks * kBlockBytes : 0;
     // per epilogue warp: the bias of its 128 columns of the tile, float32
     static constexpr int kBias = OUT == kOutEpilogue && !DEEP ? kEpiWarps * 128 * 4 : 0;
-    static constexpr int kFit = (232448 - 1024 - kStaging - kBias - kNumBars * 8 - 16) / kStage;
+    static constexpr int kFit = (kMaxSmem - 1024 - kStaging - kBias - kNumBars * 8 - 16) / kStage;
     static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
     static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kBias + kNumBars * 8 + 16;
-};
-
-// The bound of every wait of a launch, where a wait that gave up is recorded, and (for tests) the ring
-// item that CTA 0's producer never loads, or -1.
-struct Waits {
-    uint64_t limit_ns;
-    int* status;
-    int64_t withheld;
 };
 
 struct Gemm {
@@ -109,57 +94,6 @@ __device__ __forceinline__ Work work_of(const Gemm& p, int v) {
     w.ct = in / rows;
     w.rt = 8 * g + in - w.ct * rows;
     return w;
-}
-
-template <int CG>
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-    return CG == 2 ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity);
-}
-
-// All lanes of a warp wait for a phase; false once this wait or another one of the CTA gave up.
-template <int CG>
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                          const Waits& w) {
-    bool got = try_wait<CG>(bar, parity);
-    if (!got) {
-        const uint64_t t0 = globaltimer_ns();
-        for (uint32_t i = 1;; ++i) {
-            got = try_wait<CG>(bar, parity);
-            if (got) break;
-            if ((i & 63u) == 0) {
-                if (*abort_flag) break;
-                if (globaltimer_ns() - t0 > w.limit_ns) {
-                    *abort_flag = 1;
-                    if (w.status) atomicExch(w.status, (int)FLAREPP_ERR_TIMEOUT);
-                    break;
-                }
-            }
-        }
-    }
-    return __all_sync(0xffffffffu, got);
-}
-
-// One operand's tile of `rows` rows for the slice at contraction index k: K-major as one box of
-// 64 x rows, MN-major as boxes of 64 rows x 64 contraction values ("atoms").
-template <int CG, bool MN>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* m, int row, int rows,
-                                          int k, uint32_t bar) {
-    if (!MN) {
-        if (CG == 2) tma_load_2d_pair(dst, m, k, row, bar);
-        else tma_load_2d(dst, m, k, row, bar);
-    } else {
-        for (int r = 0; r < rows; r += 64, dst += 64 * kSlice * 2) {
-            if (CG == 2) tma_load_2d_pair(dst, m, row + r, k, bar);
-            else tma_load_2d(dst, m, row + r, k, bar);
-        }
-    }
-}
-
-// The descriptor of the 16 contraction values at step s of a slice.
-template <bool MN>
-__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, int s) {
-    return MN ? smem_desc(addr + s * 16 * 128, 64 * kSlice * 2, 1024, kSw128)
-              : smem_desc(addr + s * 32, 16, 1024, kSw128);
 }
 
 template <bool A_MN, bool B_MN, int OUT, bool DEEP>
@@ -255,9 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         } else if (!ok) {  // its bytes count on the leader's barriers: give them a millisecond
-            const uint64_t t0 = globaltimer_ns();
-            while (globaltimer_ns() - t0 < 1000000ull) {
-            }
+            linger();
         }
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------ MMA issuer
@@ -520,11 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
         if (OUT == kOutEpilogue) {
-            if (!ok && prm.R) {  // a wait gave up: let the copies in flight land (a millisecond)
-                const uint64_t t0 = globaltimer_ns();
-                while (globaltimer_ns() - t0 < 1000000ull) {
-                }
-            }
+            if (!ok && prm.R) linger();  // the blocks of R in flight
             if (lane == 0) bulk_wait_all();
         }
     }
@@ -536,237 +464,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 1) tmem_dealloc_pair(tmem, kTmemCols);
 }
 
-// ------------------------------------------------------------------ few rows
-// The layer for up to 256 rows of tokens: the weights are the tile's rows (128 of them, whatever the
-// number of tokens) and the tokens its columns, so the tensor cores' 128 rows are never idle and the
-// weights, whose bytes are the bound, are read once. A cluster of up to eight CTAs shares a tile, each
-// with every S-th slice of the contraction, so that a few tiles still draw on many SMs; the CTAs
-// leave their float32 sums in shared memory, and each adds a share of the columns over the cluster in
-// rank order and runs the epilogue on it. One launch, no workspace (48 rows of 4096 -> 1001 took 8.8 us
-// as chunk sums in memory and a second kernel).
-constexpr int kFewThreads = 256;
-constexpr int kFewStages = 4;
-constexpr int kFewRing = kFewStages * (kATile + kMaxNT * kSlice * 2);
-constexpr int kFewBars = 2 * kFewStages + 1;
-constexpr int kFewSmem = 1024 + kFewRing + kFewBars * 8 + 16;
-static_assert(kMaxNT * 128 * 4 <= kFewRing, "the sums reuse the ring");
-
-struct Few {
-    int M, N, NT;  // weights' rows, tokens, columns of the tile
-    int slices, share;  // slices of the contraction, CTAs per tile
-    uint32_t idesc, tmem_cols;
-    int act;
-    const __nv_bfloat16* bias;  // [M]
-    const __nv_bfloat16* R;     // [N][M], as Y and Z
-    __nv_bfloat16* Y;
-    __nv_bfloat16* Z;
-    Waits waits;
-};
-
-__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(addr));
-    return v;
-}
-
-template <bool A_MN>
-__global__ void __launch_bounds__(kFewThreads, 1)
-    lin_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                   const Few prm) {
-    extern __shared__ uint8_t smem_raw[];
-    // the same offset in every CTA of the cluster
-    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kFewRing);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kFewBars);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8u * kFewStages;
-    const uint32_t done = empty0 + 8u * kFewStages;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = prm.share > 1 ? (int)cluster_rank() : 0;
-    const int m0 = (int)blockIdx.x / prm.share * 128;
-    const uint32_t stage_bytes = kATile + prm.NT * kSlice * 2;
-
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < kFewStages; ++s) {
-            mbar_init(full0 + 8u * s, 1);
-            mbar_init(empty0 + 8u * s, 1);
-        }
-        mbar_init(done, 1);
-        *abort_flag = 0;
-        fence_mbar_init();
-        prefetch_tmap(&tmA);
-        prefetch_tmap(&tmB);
-    }
-    if (warp == 1) {
-        tmem_alloc(smem_u32(tmem_slot), prm.tmem_cols);
-        tmem_relinquish();
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
-    pdl_trigger();
-    pdl_wait();
-
-    if (warp == 0) {
-        uint32_t it = 0;
-        bool ok = true;
-        for (int s = rank; s < prm.slices; s += prm.share, ++it) {
-            const int st = it % kFewStages;
-            if (it >= (uint32_t)kFewStages &&
-                !warp_wait<1>(empty0 + 8u * st, (it / kFewStages - 1) & 1, abort_flag, prm.waits)) {
-                ok = false;
-                break;
-            }
-            if (elect_one() && !(blockIdx.x == 0 && it == prm.waits.withheld)) {
-                const uint32_t dst = smem_u32(smem + st * (kFewRing / kFewStages));
-                mbar_expect_tx(full0 + 8u * st, stage_bytes);
-                load_tile<1, A_MN>(dst, &tmA, m0, 128, s * kSlice, full0 + 8u * st);
-                load_tile<1, false>(dst + kATile, &tmB, 0, prm.NT, s * kSlice, full0 + 8u * st);
-            }
-            __syncwarp();
-        }
-        if (!ok) {  // wait (bounded) until every copy issued has landed
-            const uint64_t t0 = globaltimer_ns();
-            for (int st = 0; st < kFewStages && (uint32_t)st < it; ++st) {
-                const uint32_t x = it - 1 - ((it - 1 - st) % kFewStages);
-                while (!mbar_try_wait(full0 + 8u * st, (x / kFewStages) & 1) &&
-                       globaltimer_ns() - t0 < kWaitLimitNs) {
-                }
-            }
-        }
-    } else if (warp == 1) {
-        uint32_t it = 0;
-        for (int s = rank; s < prm.slices; s += prm.share, ++it) {
-            const int st = it % kFewStages;
-            if (!warp_wait<1>(full0 + 8u * st, (it / kFewStages) & 1, abort_flag, prm.waits)) break;
-            tc_fence_after();
-            const uint32_t a = smem_u32(smem + st * (kFewRing / kFewStages)), b = a + kATile;
-            if (elect_one()) {
-#pragma unroll
-                for (int k = 0; k < kSlice / 16; ++k)
-                    mma_ss(tmem, tile_desc<A_MN>(a, k), tile_desc<false>(b, k), prm.idesc,
-                           (it > 0 || k > 0) ? 1u : 0u);
-                mma_commit(empty0 + 8u * st);
-            }
-            __syncwarp();
-        }
-        if (elect_one()) mma_commit(done);
-        __syncwarp();
-    }
-    __syncwarp();
-    // every warp: the sums from TMEM into sums[token][128], over the ring (its copies and products
-    // are done)
-    const bool ok = warp_wait<1>(done, 0, abort_flag, prm.waits);
-    float* sums = reinterpret_cast<float*>(smem);
-    __syncthreads();  // an issuer that gave up has left its loop too
-    tc_fence_after();
-    if (ok) {
-        const int q = warp % 4;
-        float* mine = sums + 32 * q + lane;
-        for (int c = 16 * (warp / 4); c < prm.NT; c += 32) {
-            uint32_t r[16];
-            tmem_ld16(tmem + ((uint32_t)(32 * q) << 16) + c, r);
-            tmem_wait_ld16(r);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mine[(c + i) * 128] = __uint_as_float(r[i]);
-        }
-    }
-    tc_fence_before();
-    if (prm.share > 1) cluster_sync();
-    else __syncthreads();
-    tc_fence_after();
-    if (warp == 1) tmem_dealloc(tmem, prm.tmem_cols);
-    // a warp takes a token at a time, a lane four of its outputs
-    const int m = m0 + 4 * lane;
-    const bool vec = prm.M % 4 == 0;
-    for (int t = rank + prm.share * warp; t < prm.N; t += prm.share * (kFewThreads / 32)) {
-        if (m >= prm.M) break;
-        const uint32_t at = smem_u32(sums + t * 128 + 4 * lane);
-        float4 v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < prm.share) v[k] = load_cluster(prm.share > 1 ? map_to_rank(at, k) : at);
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < prm.share) {
-                x[0] += v[k].x;
-                x[1] += v[k].y;
-                x[2] += v[k].z;
-                x[3] += v[k].w;
-            }
-        const int64_t o = (int64_t)t * prm.M + m;
-        if (prm.bias)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (m + k < prm.M) x[k] += __bfloat162float(prm.bias[m + k]);
-        if (prm.Z) {
-            if (vec)
-                *reinterpret_cast<uint2*>(prm.Z + o) =
-                    make_uint2(pack_bf16x2(pair(x[0], x[1])), pack_bf16x2(pair(x[2], x[3])));
-            else
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (m + k < prm.M) prm.Z[o + k] = __float2bfloat16_rn(x[k]);
-        }
-        const float2 y0 = halves(act_value2(prm.act, pair(x[0], x[1])));
-        const float2 y1 = halves(act_value2(prm.act, pair(x[2], x[3])));
-        float y[4] = {y0.x, y0.y, y1.x, y1.y};
-        if (prm.R)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (m + k < prm.M) y[k] += __bfloat162float(prm.R[o + k]);
-        if (vec)
-            *reinterpret_cast<uint2*>(prm.Y + o) =
-                make_uint2(pack_bf16x2(pair(y[0], y[1])), pack_bf16x2(pair(y[2], y[3])));
-        else
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (m + k < prm.M) prm.Y[o + k] = __float2bfloat16_rn(y[k]);
-    }
-    __syncwarp();
-    if (prm.share > 1) cluster_sync();  // the other CTAs may still read this one's sums
-}
-
 // ------------------------------------------------------------------ host side
-
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> fn{nullptr};
-    PFN_cuTensorMapEncodeTiled_v12000 f = fn.load(std::memory_order_acquire);
-    if (f) return f;
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-        fn.store(f = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p),
-                 std::memory_order_release);
-    return f;
-}
-
-// bf16 [lines][inner] with `pitch` elements from line to line, boxes of box_inner x box_lines,
-// swizzled to their 128- or 64-byte lines
-bool make_map(CUtensorMap* m, const void* base, int64_t inner, int64_t lines, int64_t pitch,
-              int box_inner, int box_lines) {
-    auto fn = encode_fn();
-    if (!fn) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)lines};
-    cuuint64_t strides[1] = {(cuuint64_t)pitch * 2};
-    cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_lines};
-    cuuint32_t estr[2] = {1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
-              estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              box_inner == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 template <bool A_MN, bool B_MN, int OUT, bool DEEP>
 cudaError_t launch(const CUtensorMap* m, const Gemm& p, cudaStream_t st) {
     using C = Cfg<OUT, DEEP>;
-    static_assert(C::kSmem <= 232448 && C::kStages >= 3, "shared memory budget");
+    static_assert(C::kSmem <= kMaxSmem && C::kStages >= 3, "shared memory budget");
     auto kernel = lin_gemm_kernel<A_MN, B_MN, OUT, DEEP>;
     static std::atomic<int> fits[64];  // tiles that run at once on each device (0: not asked yet)
     int dev = 0;
@@ -806,66 +509,7 @@ cudaError_t launch(const CUtensorMap* m, const Gemm& p, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], m[4], p);
 }
 
-template <bool A_MN>
-cudaError_t launch_few(const CUtensorMap* m, const Few& p, unsigned tiles, cudaStream_t st) {
-    auto kernel = lin_few_kernel<A_MN>;
-    static std::atomic<uint64_t> ready{0};  // devices whose shared-memory limit is raised
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (!(ready.load() >> dev & 1)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
-        if (e != cudaSuccess) return e;
-        ready.fetch_or(uint64_t(1) << dev);
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * (unsigned)p.share);
-    cfg.blockDim = dim3(kFewThreads);
-    cfg.dynamicSmemBytes = kFewSmem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)p.share;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = p.share > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], p);
-}
-
 }  // namespace
-
-cudaError_t lin_few(int64_t rows, int64_t cols, int64_t K, const LinOperand& x,
-                    const LinOperand& w, const LinEpilogue& e, int* status, cudaStream_t st) {
-    Few p{};
-    p.M = (int)cols;
-    p.N = (int)rows;
-    p.NT = (int)cdiv(rows, 16) * 16;
-    p.slices = (int)cdiv(K, kSlice);
-    const int64_t tiles = cdiv(cols, 128);
-    p.share = 1;  // as many CTAs as the SMs take, with two slices each at least
-    while (p.share < 8 && tiles * p.share * 2 <= kNumSMs && p.slices >= 4 * p.share) p.share *= 2;
-    p.idesc = idesc_bf16_f32(128, p.NT, w.mn, false);
-    p.tmem_cols = 32;
-    while ((int)p.tmem_cols < p.NT) p.tmem_cols *= 2;
-    p.act = e.act;
-    p.bias = (const __nv_bfloat16*)e.bias;
-    p.R = (const __nv_bfloat16*)e.R;
-    p.Y = (__nv_bfloat16*)e.Y;
-    p.Z = (__nv_bfloat16*)e.Z;
-    p.waits.status = status;
-    test_fault_for(kFewKernel, &p.waits.limit_ns, &p.waits.withheld);
-    CUtensorMap m[2];
-    const bool ok = (w.mn ? make_map(&m[0], w.t, cols, K, w.pitch, 64, kSlice)
-                          : make_map(&m[0], w.t, K, cols, w.pitch, kSlice, 128)) &&
-                    make_map(&m[1], x.t, K, rows, x.pitch, kSlice, p.NT);
-    if (!ok) return cudaErrorInvalidValue;
-    return w.mn ? launch_few<true>(m, p, (unsigned)tiles, st)
-                : launch_few<false>(m, p, (unsigned)tiles, st);
-}
 
 LinPlan lin_plan(int64_t M, int64_t N, int64_t K) {
     LinPlan p{};
