@@ -6,14 +6,16 @@
 // made where the product needs it: the slices of dY and Z come into the ring as they are, eight warps
 // turn dY's tile into dZ's in place (the swizzled tile that the tensor cores read), store it for dW and
 // add up its columns, and the pair's leader multiplies. A separate pass would read dZ once more, and its
-// launch: 131,072 rows of 256 -> 512 with GELU, dZ, dX and db, SEPARATE us apart and FUSED here, of which the
-// bytes (268 MB read, 201 MB written) are about 50.
+// launch: for 131,072 rows of 256 -> 512 with GELU, dZ with its column sums and dX take 107 us apart and 92
+// here, of which the bytes (268 MB read, 201 MB written) are about 50. What is left is the ring: four stages of
+// 32 KB, of which two are being made or multiplied, keep some 64 KB a SM in flight.
 //
 // Roles (28 warps): warp 0 the TMA producer of dY and Z, warp 2 that of W, warp 1 the MMA issuer (in the
 // pair's leader), warp 3 dZ's stores, warps 4..19 dZ, warps 20..27 the epilogue, which writes dX from two TMEM accumulators
 // of 256 columns by turns. The dZ warps are two groups of eight (16 rows of the CTA's 128 a warp) that take
 // the slices in turn: making a slice is a chain of latencies (shared memory, the slope, the proxy fence),
-// and one group alone, of eight or of sixteen warps, took 115 us for the layer above. A ring stage is
+// and one group alone, of eight or of sixteen warps, took 115 us for the layer above, as did stores
+// issued by the dZ warps themselves, which freed a stage only at their next slice. A ring stage is
 // free again when its products are done and its stores have read it. Waits are bounded as in tc_linear.cu.
 #include "tc_linear_common.cuh"
 
@@ -25,6 +27,8 @@ constexpr int kFirstDzWarp = 4, kGroups = 2, kGroupWarps = 8, kDzWarps = kGroups
 constexpr int kFirstEpiWarp = 20, kEpiWarps = 8;
 constexpr int kDzTile = 128 * kSlice * 2;           // of dY (then dZ), of Z
 constexpr uint32_t kS = 4, kStage = 2 * kDzTile;    // ring of dY and Z
+// a group sees every phase of its stages, without which a wait by parity would name two phases
+static_assert(kS % kGroups == 0, "a stage is always the same group's");
 constexpr uint32_t kSW = 3, kStageW = kMaxNT / 2 * kSlice * 2;  // ring of the CTA's half of W's columns
 constexpr int kStaging = kEpiWarps * kBlockBytes;
 constexpr int kNumBars = 4 * kS + 2 * kSW + 4 + 1;
