@@ -1,5 +1,8 @@
 // The linear layer (flarepp_linear_*): argument checks, workspace layout, the launch sequence of
 // its products (tc_linear.cu), and the memory-bound kernels around them.
+//
+// A kernel overlaps the one before it up to pdl_wait, and its inputs may come from there. They are
+// therefore not __restrict__: loads of memory promised to stay constant may move above that wait.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -43,9 +46,9 @@ bool pad_w(int64_t K, int64_t T) { return K % 8 != 0 || (K % 64 != 0 && T >= kPa
 // W, and their sums are added in order.
 template <int RT, int RW>
 __global__ void __launch_bounds__(kGemvWarps * 32)
-    gemv_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W, int T,
-                int K, int N, int split, int act, const __nv_bfloat16* __restrict__ bias,
-                const __nv_bfloat16* __restrict__ R, __nv_bfloat16* __restrict__ Y,
+    gemv_kernel(const __nv_bfloat16* X, const __nv_bfloat16* W, int T,
+                int K, int N, int split, int act, const __nv_bfloat16* bias,
+                const __nv_bfloat16* R, __nv_bfloat16* __restrict__ Y,
                 __nv_bfloat16* __restrict__ Z) {
     constexpr int U = 8 / RW;
     __shared__ float sums[kGemvWarps][RW][RT];
@@ -68,7 +71,7 @@ __global__ void __launch_bounds__(kGemvWarps * 32)
 #pragma unroll
             for (int r = 0; r < RW; ++r)
                 w[u][r] = v + 32 * u < v1 && n0 + r < N
-                              ? __ldg(reinterpret_cast<const uint4*>(W + (int64_t)(n0 + r) * K) + v + 32 * u)
+                              ? reinterpret_cast<const uint4*>(W + (int64_t)(n0 + r) * K)[v + 32 * u]
                               : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -76,7 +79,7 @@ __global__ void __launch_bounds__(kGemvWarps * 32)
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 if (t >= T) break;
-                const uint4 x = __ldg(reinterpret_cast<const uint4*>(X + (int64_t)t * K) + v + 32 * u);
+                const uint4 x = reinterpret_cast<const uint4*>(X + (int64_t)t * K)[v + 32 * u];
                 const uint64_t x0 = unpack_bf16x2(x.x), x1 = unpack_bf16x2(x.y);
                 const uint64_t x2 = unpack_bf16x2(x.z), x3 = unpack_bf16x2(x.w);
 #pragma unroll
@@ -119,7 +122,7 @@ __global__ void __launch_bounds__(kGemvWarps * 32)
 
 // dst [rows][pitch] = src [rows][cols] with zeros behind each row: the 16-byte line pitch that
 // TMA asks for. One thread per eight values.
-__global__ void pad_kernel(const __nv_bfloat16* __restrict__ src, int64_t rows, int64_t cols,
+__global__ void pad_kernel(const __nv_bfloat16* src, int64_t rows, int64_t cols,
                            int64_t pitch, __nv_bfloat16* __restrict__ dst) {
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -177,10 +180,10 @@ __global__ void __launch_bounds__(kDbThreads) db_kernel(const DbSums d) {
 constexpr int kFinishThreads = 256;
 template <int SPLIT>
 __global__ void __launch_bounds__(kFinishThreads)
-    finish_kernel(const float* __restrict__ part, int chunks, int64_t rows,
+    finish_kernel(const float* part, int chunks, int64_t rows,
                               int64_t cols, int64_t ldp, int act,
-                              const __nv_bfloat16* __restrict__ bias,
-                              const __nv_bfloat16* __restrict__ R, __nv_bfloat16* __restrict__ Y,
+                              const __nv_bfloat16* bias,
+                              const __nv_bfloat16* R, __nv_bfloat16* __restrict__ Y,
                               __nv_bfloat16* __restrict__ Z, unsigned blocks, const DbSums db) {
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -250,7 +253,7 @@ __global__ void __launch_bounds__(kFinishThreads)
 // VEC: eight values at a time (cols a multiple of 8).
 template <bool VEC>
 __global__ void __launch_bounds__(kDzThreads, 4)
-    dz_kernel(const __nv_bfloat16* __restrict__ dY, const __nv_bfloat16* __restrict__ Z,
+    dz_kernel(const __nv_bfloat16* dY, const __nv_bfloat16* Z,
               int64_t rows, int64_t cols, int64_t rows_per, int lanes, int act, int64_t ldz,
               __nv_bfloat16* __restrict__ dZ, float* __restrict__ db_part) {
     tc::pdl_trigger();

@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (at + 32 <= prm.N) {
 #pragma unroll
                             for (int g = 0; g < 4; ++g) {
-                                const uint4 u = __ldg(reinterpret_cast<const uint4*>(prm.bias + at) + g);
+                                const uint4 u = reinterpret_cast<const uint4*>(prm.bias + at)[g];
                                 x[4 * g] = add2(x[4 * g], unpack_bf16x2(u.x));
                                 x[4 * g + 1] = add2(x[4 * g + 1], unpack_bf16x2(u.y));
                                 x[4 * g + 2] = add2(x[4 * g + 2], unpack_bf16x2(u.z));
