@@ -8,6 +8,9 @@
 // the sorted positions are summed in parallel whatever the lengths of the runs of one id; a run that
 // crosses from one stretch into the next leaves float32 partial sums, which a last kernel adds in
 // order. The gradient is written once: a bit per row says which rows no id names.
+//
+// What a kernel reads may come from the kernel before it, which it overlaps up to pdl_wait. Inputs are
+// therefore not __restrict__: loads of memory promised to stay constant may move above that wait.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -72,7 +75,7 @@ constexpr int kLookupRows = 4;
 
 template <typename E, int N, typename I>
 __global__ void __launch_bounds__(256)
-    lookup_kernel(const I* __restrict__ ids, const E* __restrict__ table, int64_t T, int64_t V,
+    lookup_kernel(const I* ids, const E* table, int64_t T, int64_t V,
                   int64_t C, float scale, E* __restrict__ Y, int* status) {
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -123,7 +126,7 @@ __device__ __forceinline__ uint32_t key_at(const I* ids, const uint32_t* keys, i
 // hist[digit][tile] = how often the tile has the digit.
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
-    count_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ keys, int64_t T,
+    count_kernel(const I* ids, const uint32_t* keys, int64_t T,
                  int64_t V, int64_t tile, int shift, int bins, uint32_t* __restrict__ hist,
                  int* status) {
     extern __shared__ uint32_t cnt[];
@@ -168,9 +171,9 @@ __global__ void __launch_bounds__(256)
 // Move every position to its place in the order of the digit.
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
-    place_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ keys,
-                 const uint32_t* __restrict__ pos, int64_t T, int64_t V, int64_t tile, int shift,
-                 int bins, const uint32_t* __restrict__ hist, const uint32_t* __restrict__ total,
+    place_kernel(const I* ids, const uint32_t* keys,
+                 const uint32_t* pos, int64_t T, int64_t V, int64_t tile, int shift,
+                 int bins, const uint32_t* hist, const uint32_t* total,
                  uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out) {
     extern __shared__ uint32_t sm[];  // [kSortWarps][bins] places, [bins] starts of the digits
     uint32_t* start = sm + kSortWarps * bins;
@@ -266,7 +269,7 @@ constexpr int64_t kFewWords = 1 << 16;  // words that the block clears; more tak
 
 template <typename I>
 __global__ void __launch_bounds__(kFewThreads)
-    few_kernel(const I* __restrict__ ids, int T, int places, int64_t V,
+    few_kernel(const I* ids, int T, int places, int64_t V,
                uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out,
                uint32_t* __restrict__ words, int64_t n_words, int* status) {
     extern __shared__ uint64_t pairs[];  // [places], a power of two of at least 64
@@ -296,19 +299,26 @@ __global__ void __launch_bounds__(kFewThreads)
 }
 
 // ------------------------------------------------------------------ sums
-// Thread (x, y) of a block sums N columns of one stretch of the sorted positions. A run that lies within the stretch goes to the
+// Thread (x, y) of a block sums units_of<E, N>() vectors of N columns of one stretch of the sorted positions. A run that lies within the stretch goes to the
 // table; one that began before it leaves its sum in head[stretch], one that begins here and goes on in
 // tail[stretch], and the stretch on a list of crossing runs: those of few parts from the front of
 // `crossing`, those of many from its back (the order does not matter: each run is a sum of its own).
 // A run's first stretch sets the row's bit in `met`.
 constexpr int kSumThreads = 256;
 constexpr int kMinStretch = 16, kMaxStretch = 256;
-// a crossing run of more parts is joined by a whole block (what a row of threads can hold at once)
+// a crossing run of more parts is joined by a whole block, one of up to so many by a row of threads
+// (what it can hold at once)
 constexpr int short_run(int n) { return n == 8 ? 4 : 8; }
 constexpr int kMaxHeld = 4096;   // positions whose keys and places a block holds
 constexpr int kBatch = 4;        // rows of a group of copies
 constexpr int kRing = 16;        // rows in flight per thread
-constexpr int kJoinThreads = 1024;
+// Vectors per thread. What a position costs whatever its vectors (its key, its place, the turn of the
+// loop: some 30 instructions) bounds the sums of narrow vectors, so a thread takes several of those.
+template <typename E, int N>
+constexpr int units_of() {
+    return sizeof(E) * N >= 16 ? 1 : sizeof(E) * N == 8 ? 2 : 4;
+}
+constexpr int kJoinThreads = 512, kJoinBlocks = 2 * kNumSMs;
 constexpr int kZeroRows = 8;     // rows per warp that writes zeros
 
 // An asynchronous copy of one vector into shared memory (two bytes, which the instruction does not
@@ -324,35 +334,39 @@ __device__ __forceinline__ void copy_async(Vec<E, N>* dst, const E* src) {
         *dst = load_vec<E, N>(src);
 }
 
-template <typename E, int N>
-__device__ void zero_rows(const uint32_t* __restrict__ met, int64_t group, int64_t V, int64_t C,
-                          E* __restrict__ dtable) {
-    const int lane = threadIdx.x % 32;
-    Vec<E, N> zero;
-#pragma unroll
-    for (int k = 0; k < N; ++k) from_f32(zero.v[k], 0.f);
-    const int64_t v0 = group * kZeroRows;
-    if (v0 >= V) return;
+// Zeros for those of kZeroRows rows that no id names, in 16-byte stores whatever the alignment of a row.
+template <typename E>
+__device__ void zero_rows(const uint32_t* met, int64_t v0, int64_t V, int64_t C,
+                          int lane, E* __restrict__ dtable) {
+    E zero;
+    from_f32(zero, 0.f);
     uint32_t gone = ~met[v0 / 32] >> (v0 % 32) & ((1u << kZeroRows) - 1u);
     if (V - v0 < kZeroRows) gone &= (1u << (V - v0)) - 1u;
     while (gone) {
         const int v = __ffs(gone) - 1;
         gone &= gone - 1;
-        for (int64_t c = lane * N; c < C; c += 32 * N) store_vec<E, N>(dtable + (v0 + v) * C + c, zero);
+        E* row = dtable + (v0 + v) * C;
+        const int64_t before = min(C, (int64_t)((16 - (uintptr_t)row % 16) % 16 / sizeof(E)));
+        const int64_t wide = (C - before) * sizeof(E) / 16, after = before + wide * (16 / sizeof(E));
+        if (lane < before) row[lane] = zero;
+        for (int64_t k = lane; k < wide; k += 32)
+            reinterpret_cast<uint4*>(row + before)[k] = make_uint4(0, 0, 0, 0);
+        if (lane < C - after) row[after + lane] = zero;
     }
 }
 
 template <typename E, int N>
 __global__ void __launch_bounds__(kSumThreads)
-    sum_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pos,
-               const E* __restrict__ dY, int64_t T, int64_t V, int64_t C, int stretch, float scale,
+    sum_kernel(const uint32_t* keys, const uint32_t* pos,
+               const E* dY, int64_t T, int64_t V, int64_t C, int stretch, float scale,
                E* __restrict__ dtable, float* __restrict__ head, float* __restrict__ tail,
                uint32_t* __restrict__ met, uint32_t* __restrict__ crossing, int64_t stretches,
                uint32_t* __restrict__ n_crossing) {
     extern __shared__ uint8_t sum_smem[];
-    // the rows in flight, a slot per thread: [kRing][kSumThreads]; the block's keys; its positions
+    constexpr int U = units_of<E, N>();
+    // the rows in flight, U slots per thread: [kRing][U][kSumThreads]; the block's keys; its positions
     Vec<E, N>* ring = reinterpret_cast<Vec<E, N>*>(sum_smem);
-    uint32_t* held = reinterpret_cast<uint32_t*>(sum_smem + sizeof(Vec<E, N>) * kRing * kSumThreads);
+    uint32_t* held = reinterpret_cast<uint32_t*>(sum_smem + sizeof(Vec<E, N>) * kRing * U * kSumThreads);
     const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -365,19 +379,27 @@ __global__ void __launch_bounds__(kSumThreads)
         held_pos[i] = in ? pos[b0 + i] : 0;
     }
     __syncthreads();
-    const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
+    // unit u: the N columns at c + u * next (row of a block: neighbouring vectors), if they exist
+    const int64_t c = ((int64_t)blockIdx.y * U * blockDim.x + threadIdx.x) * N;
+    const int next = blockDim.x * N;
     const int64_t st = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     const int64_t i0 = st * stretch;
     if (c >= C || i0 >= T) return;
+    const int units = (int)min((int64_t)U, (C - 1 - c) / next + 1);
     const uint32_t* key = held + threadIdx.y * stretch;
     const uint32_t* at = held_pos + threadIdx.y * stretch;
     uint32_t cur = key[0];
     if (cur == (uint32_t)V) return;  // empty positions come last, and those beyond T count as such
     bool began = i0 == 0 || keys[i0 - 1] != cur;
     const bool goes_on = i0 + stretch < T && keys[i0 + stretch] == key[stretch - 1];
-    float acc[N];
+    float acc[U][N];
+    auto clear = [&] {
 #pragma unroll
-    for (int k = 0; k < N; ++k) acc[k] = 0.f;
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[u][k] = 0.f;
+    };
+    clear();
     const bool first = blockIdx.y == 0 && threadIdx.x == 0;
     auto flush = [&](bool more) {
         if (began && first) {
@@ -390,16 +412,20 @@ __global__ void __launch_bounds__(kSumThreads)
                     crossing[atomicAdd(n_crossing, 1u)] = (uint32_t)st;
             }
         }
-        if (began && !more) {
-            Vec<E, N> o;
 #pragma unroll
-            for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
-            store_vec<E, N>(dtable + (int64_t)cur * C + c, o);
-        } else {
-            Vec<float, N> o;
+        for (int u = 0; u < U; ++u) {
+            if (u >= units) break;
+            if (began && !more) {
+                Vec<E, N> o;
 #pragma unroll
-            for (int k = 0; k < N; ++k) o.v[k] = acc[k];
-            *reinterpret_cast<Vec<float, N>*>((began ? tail : head) + st * C + c) = o;
+                for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[u][k] * scale);
+                store_vec<E, N>(dtable + (int64_t)cur * C + c + u * next, o);
+            } else {
+                Vec<float, N> o;
+#pragma unroll
+                for (int k = 0; k < N; ++k) o.v[k] = acc[u][k];
+                *reinterpret_cast<Vec<float, N>*>((began ? tail : head) + st * C + c + u * next) = o;
+            }
         }
     };
     // Batches of rows come in by asynchronous copies, each thread's vectors into slots of its own:
@@ -408,9 +434,12 @@ __global__ void __launch_bounds__(kSumThreads)
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int i = batch * kBatch + k;
-            if (i < stretch && key[i] != (uint32_t)V)
-                copy_async(ring + (i % kRing) * kSumThreads + tid,
-                           dY + (int64_t)at[i] * C + c);
+            if (i < stretch && key[i] != (uint32_t)V) {
+                const E* row = dY + (uint64_t)at[i] * (uint32_t)C + c;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (u < units) copy_async(ring + (i % kRing * U + u) * kSumThreads + tid, row + u * next);
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -426,73 +455,46 @@ __global__ void __launch_bounds__(kSumThreads)
                 flush(false);
                 began = true;
                 cur = key[i];
-#pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] = 0.f;
+                clear();
                 if (cur == (uint32_t)V) return;  // only empty positions follow, none was fetched
             }
-            const Vec<E, N> x = ring[(i % kRing) * kSumThreads + tid];
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] += to_f32(x.v[j]);
+            for (int u = 0; u < U; ++u) {
+                if (u >= units) break;
+                const Vec<E, N> x = ring[(i % kRing * U + u) * kSumThreads + tid];
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[u][j] += to_f32(x.v[j]);
+            }
         }
     }
     flush(goes_on);
 }
 
-// The runs that cross stretches. Blocks below `join_blocks` take the runs of many parts one at a
-// time: the threads look at one stretch each to find where the run ends, the rows of threads add equal
-// shares of the parts in order, and the shares are added in order. The next `join_blocks` blocks take the
-// runs of up to short_run parts, a row of threads each. The rest write the zeros of the rows that no id
-// names.
+// The runs that cross stretches, then the zeros of the rows that no id names. A run of many parts takes
+// a block: the threads look at one stretch each to find where the run ends, the rows of threads add
+// equal shares of the parts in order, and the shares are added in order. A run of few parts takes a row of
+// threads, and the blocks that the long runs leave free take them first. A block does all three: as many as
+// run at once are launched.
 template <typename E, int N>
-__global__ void __launch_bounds__(kJoinThreads)
-    join_kernel(const uint32_t* __restrict__ keys, int64_t T, int64_t V, int64_t C, int stretch,
-                unsigned join_blocks, float scale, const float* __restrict__ head,
-                const float* __restrict__ tail, const uint32_t* __restrict__ met,
-                const uint32_t* __restrict__ crossing, int64_t stretches,
-                const uint32_t* __restrict__ n_crossing, E* __restrict__ dtable) {
+__global__ void __launch_bounds__(kJoinThreads, 2)
+    join_kernel(const uint32_t* keys, int64_t T, int64_t V, int64_t C, int stretch,
+                float scale, const float* head, const float* tail,
+                const uint32_t* met, const uint32_t* crossing,
+                int64_t stretches, const uint32_t* n_crossing, E* __restrict__ dtable) {
     extern __shared__ float share[];  // [blockDim.y][blockDim.x * N]
     const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     tc::pdl_trigger();
     tc::pdl_wait();
-    if (blockIdx.x >= 2 * join_blocks) {
-        if (blockIdx.y == 0)
-            zero_rows<E, N>(met,
-                            (int64_t)(blockIdx.x - 2 * join_blocks) * (kJoinThreads / 32) + tid / 32,
-                            V, C, dtable);
-        return;
-    }
     const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
-    if (blockIdx.x >= join_blocks) {
-        constexpr int kShortRun = short_run(N);
-        const unsigned n = n_crossing[0], step = join_blocks * blockDim.y;
-        if (c >= C) return;
-        for (unsigned item = (blockIdx.x - join_blocks) * blockDim.y + threadIdx.y; item < n; item += step) {
-            const int64_t st = crossing[item];
-            const uint32_t key = keys[(st + 1) * stretch];
-            Vec<float, N> part[kShortRun];
-            bool in[kShortRun];
-#pragma unroll
-            for (int p = 0; p < kShortRun; ++p) {
-                const int64_t at = (st + 1 + p) * stretch;
-                in[p] = at < T && keys[at] == key;
-                if (in[p]) part[p] = *reinterpret_cast<const Vec<float, N>*>(head + (st + 1 + p) * C + c);
-            }
-            Vec<float, N> acc = *reinterpret_cast<const Vec<float, N>*>(tail + st * C + c);
-#pragma unroll
-            for (int p = 0; p < kShortRun; ++p)
-#pragma unroll
-                for (int k = 0; k < N; ++k)
-                    if (in[p]) acc.v[k] += part[p].v[k];
-            Vec<E, N> o;
-#pragma unroll
-            for (int k = 0; k < N; ++k) from_f32(o.v[k], acc.v[k] * scale);
-            store_vec<E, N>(dtable + (int64_t)key * C + c, o);
-        }
-        return;
-    }
-    const unsigned n = n_crossing[1];
+    const unsigned n_short = n_crossing[0], n_long = n_crossing[1];
     const int row = blockDim.x * N;
-    for (unsigned item = blockIdx.x; item < n; item += join_blocks) {
+    auto write = [&](uint32_t key, const float* acc) {
+        Vec<E, N> o;
+#pragma unroll
+        for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
+        store_vec<E, N>(dtable + (int64_t)key * C + c, o);
+    };
+    for (unsigned item = blockIdx.x; item < n_long; item += gridDim.x) {
         const int64_t st = crossing[stretches - 1 - item];
         const uint32_t key = keys[(st + 1) * stretch];
         int64_t parts = 0;  // stretches st + 1 .. st + parts begin with the run's key
@@ -530,13 +532,37 @@ __global__ void __launch_bounds__(kJoinThreads)
             for (int y = 1; y < ys; ++y)
 #pragma unroll
                 for (int k = 0; k < N; ++k) acc[k] += share[y * row + threadIdx.x * N + k];
-            Vec<E, N> o;
-#pragma unroll
-            for (int k = 0; k < N; ++k) from_f32(o.v[k], acc[k] * scale);
-            store_vec<E, N>(dtable + (int64_t)key * C + c, o);
+            write(key, acc);
         }
         __syncthreads();
     }
+    if (c < C)
+        for (unsigned item = threadIdx.y * gridDim.x + (gridDim.x - 1 - blockIdx.x); item < n_short;
+             item += gridDim.x * blockDim.y) {
+            constexpr int kHold = short_run(N);
+            const int64_t st = crossing[item];
+            const uint32_t key = keys[(st + 1) * stretch];
+            Vec<float, N> part[kHold];
+            bool has[kHold];
+#pragma unroll
+            for (int p = 0; p < kHold; ++p) {
+                const int64_t at = (st + 1 + p) * stretch;
+                has[p] = at < T && keys[at] == key;
+                if (has[p]) part[p] = *reinterpret_cast<const Vec<float, N>*>(head + (st + 1 + p) * C + c);
+            }
+            Vec<float, N> acc = *reinterpret_cast<const Vec<float, N>*>(tail + st * C + c);
+#pragma unroll
+            for (int p = 0; p < kHold; ++p)
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (has[p]) acc.v[k] += part[p].v[k];
+            write(key, acc.v);
+        }
+    // whole warps from here: threads 32 w .. 32 w + 31 of the block
+    const int64_t warps = (int64_t)gridDim.x * gridDim.y * (kJoinThreads / 32);
+    for (int64_t g = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kJoinThreads / 32) + tid / 32;
+         g * kZeroRows < V; g += warps)
+        zero_rows<E>(met, g * kZeroRows, V, C, tid % 32, dtable);
 }
 
 // ------------------------------------------------------------------ host side
@@ -556,6 +582,10 @@ int vec_of(const flarepp_embedding_shape& s) {
     int n = (int)(16 / elem(s));
     while (s.C % n) n /= 2;
     return n;
+}
+int units_of(const flarepp_embedding_shape& s) {
+    const size_t bytes = elem(s) * vec_of(s);
+    return bytes >= 16 ? 1 : bytes == 8 ? 2 : 4;
 }
 // Threads along a row: enough for its vectors, a power of two up to `most`.
 int lanes_for(int64_t vecs, int most) {
@@ -586,8 +616,8 @@ Layout layout_of(const flarepp_embedding_shape& s) {
     Layout L{};
     L.sort = sort_plan(s);
     // stretches so long that about 24 warps per SM have one each
-    const int64_t vecs = cdiv(s.C, vec_of(s)), x = lanes_for(vecs, 32);
-    const int64_t want = cdiv(s.T * cdiv(vecs, x) * x, (int64_t)24 * 32 * kNumSMs);
+    const int64_t units = cdiv(cdiv(s.C, vec_of(s)), units_of(s)), x = lanes_for(units, 32);
+    const int64_t want = cdiv(s.T * cdiv(units, x) * x, (int64_t)24 * 32 * kNumSMs);
     int64_t most = kMaxHeld / (kSumThreads / x);
     if (most > kMaxStretch) most = kMaxStretch;
     L.stretch = (int)(cdiv(want, kMinStretch) * kMinStretch);
@@ -684,12 +714,17 @@ cudaError_t sort_few(const flarepp_embedding_shape& s, const Layout& L, const vo
 template <typename E, int N>
 cudaError_t sums(const flarepp_embedding_shape& s, const Layout& L, int at, const void* dY,
                  float scale, void* dtable, char* ws, cudaStream_t st) {
+    constexpr int U = units_of<E, N>();
     const int64_t vecs = cdiv(s.C, N);
-    const int x = lanes_for(vecs, 32), y = kSumThreads / x;
+    const int x = lanes_for(vecs, 32);
     const unsigned col_blocks = (unsigned)cdiv(vecs, x);
-    const unsigned sum_blocks = (unsigned)cdiv(L.stretches, y);
-    const unsigned join_blocks = L.stretches < kNumSMs ? (unsigned)L.stretches : kNumSMs;
-    const unsigned zero_blocks = (unsigned)cdiv(s.V, kZeroRows * (kJoinThreads / 32));
+    const int sum_x = lanes_for(cdiv(vecs, U), 32), sum_y = kSumThreads / sum_x;
+    const dim3 sum_grid((unsigned)cdiv(L.stretches, sum_y), (unsigned)cdiv(cdiv(vecs, U), sum_x));
+    // the join: as many blocks as run at once, fewer where there is less to do
+    const int64_t zero_blocks = cdiv(s.V, kZeroRows * (kJoinThreads / 32));
+    const int64_t useful = L.stretches > zero_blocks ? L.stretches : zero_blocks;
+    const int64_t join_most = cdiv(kJoinBlocks, col_blocks);
+    const unsigned join_blocks = (unsigned)(useful < join_most ? useful : join_most);
     const uint32_t* keys = (const uint32_t*)(ws + L.off_keys[at]);
     const uint32_t* pos = (const uint32_t*)(ws + L.off_pos[at]);
     uint32_t* n_crossing = (uint32_t*)(ws + L.off_met);
@@ -697,20 +732,20 @@ cudaError_t sums(const flarepp_embedding_shape& s, const Layout& L, int at, cons
     uint32_t* crossing = (uint32_t*)(ws + L.off_crossing);
     float* head = (float*)(ws + L.off_head);
     float* tail = (float*)(ws + L.off_tail);
-    constexpr size_t kRingBytes = sizeof(E) * N * kRing * kSumThreads;
-    const size_t held = kRingBytes + (size_t)y * L.stretch * 8;
+    constexpr size_t kRingBytes = sizeof(E) * N * U * kRing * kSumThreads;
+    const size_t held = kRingBytes + (size_t)sum_y * L.stretch * 8;
     cudaError_t e = cudaSuccess;
     if (held > 48 * 1024)
         e = cudaFuncSetAttribute(sum_kernel<E, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  (int)kRingBytes + kMaxHeld * 8);
     if (e == cudaSuccess)
-        e = launch_pdl(sum_kernel<E, N>, dim3(sum_blocks, col_blocks), dim3(x, y), held, st, keys,
+        e = launch_pdl(sum_kernel<E, N>, sum_grid, dim3(sum_x, sum_y), held, st, keys,
                        pos, (const E*)dY, s.T, s.V, s.C, L.stretch, scale, (E*)dtable, head, tail,
                        met, crossing, L.stretches, n_crossing);
     if (e == cudaSuccess)
-        e = launch_pdl(join_kernel<E, N>, dim3(2 * join_blocks + zero_blocks, col_blocks),
+        e = launch_pdl(join_kernel<E, N>, dim3(join_blocks, col_blocks),
                        dim3(x, kJoinThreads / x), (size_t)kJoinThreads * N * 4, st, keys, s.T, s.V,
-                       s.C, L.stretch, join_blocks, scale, (const float*)head, (const float*)tail,
+                       s.C, L.stretch, scale, (const float*)head, (const float*)tail,
                        (const uint32_t*)met, (const uint32_t*)crossing, L.stretches,
                        (const uint32_t*)n_crossing, (E*)dtable);
     return e;
