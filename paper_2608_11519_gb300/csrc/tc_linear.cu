@@ -29,6 +29,8 @@
 // warps on every tile (36 us: a tile's fixed latencies are then in every warp's way), 16-column halves with the
 // next loads ahead (38 us: too few independent chains), eight warps of 64 columns and unpaired arithmetic
 // (46 us), more registers for the epilogue by setmaxnreg (spills).
+#include <type_traits>
+
 #include "tc_linear_common.cuh"
 
 namespace flarepp {
@@ -41,7 +43,8 @@ constexpr int kMaxStages = 8;
 constexpr int kDeepSlices = 12;  // slices of a contraction from which the deep form runs
 constexpr int kNumBars = 2 * kMaxStages + 4 + 1 + 2 * kEpiWarps;
 
-enum Out { kOutEpilogue, kOutPart };
+// outputs by TMA (N a multiple of 8), by plain stores, or the partial sums of a cut contraction
+enum Out { kOutTma, kOutPlain, kOutPart };
 
 // DEEP: the epilogue gives most of its shared memory to the ring (one staged block per warp, the
 // bias read from global memory): for long contractions, where the products are the bound and their
@@ -52,9 +55,9 @@ struct Cfg {
     static constexpr int kStage = kATile + kBTile;
     // per epilogue warp: 32-row x 32-column bf16 blocks
     static constexpr int kBlocks = DEEP ? 1 : 2;
-    static constexpr int kStaging = OUT == kOutEpilogue ? kEpiWarps * kBlocks * kBlockBytes : 0;
+    static constexpr int kStaging = OUT != kOutPart ? kEpiWarps * kBlocks * kBlockBytes : 0;
     // per epilogue warp: the bias of its 128 columns of the tile, float32
-    static constexpr int kBias = OUT == kOutEpilogue && !DEEP ? kEpiWarps * 128 * 4 : 0;
+    static constexpr int kBias = OUT != kOutPart && !DEEP ? kEpiWarps * 128 * 4 : 0;
     static constexpr int kFit = (kMaxSmem - 1024 - kStaging - kBias - kNumBars * 8 - 16) / kStage;
     static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
     static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kBias + kNumBars * 8 + 16;
@@ -67,7 +70,6 @@ struct Gemm {
     int backward;        // walk the tiles from the last to the first
     uint32_t idesc;
     int act;
-    int tma_out;  // the output's pitch suits TMA
     const __nv_bfloat16* bias;
     const __nv_bfloat16* R;
     __nv_bfloat16* Y;
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int width = row0 < prm.M ? min(prm.NT, prm.N - n0) : 0;
             const int rows = min(32, prm.M - row0);
             const uint32_t acc = tmem + ((uint32_t)(32 * q) << 16) + ab * kMaxNT;
-            const bool tma_r = OUT == kOutEpilogue && prm.R && prm.tma_out;
+            const bool tma_r = OUT == kOutTma && prm.R;
             // block h of R at column c, into the staged block that Y leaves from
             auto fetch_r = [&](int h, int c) {
                 if (lane == 0) {
@@ -292,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_after();
             for (int c = cfirst; c < width && ok; c += c % 64 ? 96 : 32) {
                 const int h = DEEP ? 0 : c / 32 & 1;  // staged block
-                if (OUT != kOutEpilogue) {
+                if (OUT == kOutPart) {
                     float x[32];
                     tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(x));
                     tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
@@ -352,14 +354,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                         *piece(hb, g) = make_uint4(pack_bf16x2(x[4 * g]), pack_bf16x2(x[4 * g + 1]),
                                                    pack_bf16x2(x[4 * g + 2]), pack_bf16x2(x[4 * g + 3]));
                 };
-                // value (r, cc) of a staged block, for outputs whose lines TMA cannot address
+                // Value (r, cc) of a staged block, for outputs whose lines TMA cannot address. Those leave
+                // (and R comes) a row at a time in words of VW values, VW = 4, 2 or 1 by what divides N.
                 auto value = [&](int hb, int r, int cc) {
-                    return reinterpret_cast<__nv_bfloat16*>(staged + hb * kBlockBytes + r * 64 +
-                                                            (((cc >> 3) ^ (r >> 1 & 3)) << 4) + (cc & 7) * 2);
+                    return staged + hb * kBlockBytes + r * 64 + (((cc >> 3) ^ (r >> 1 & 3)) << 4) +
+                           (cc & 7) * 2;
                 };
                 const int cols = min(32, width - c);
+                auto each_word = [&](auto word, int hb, auto act_on) {
+                    using V = decltype(word);
+                    constexpr int VW = sizeof(V) / 2;
+                    const int cc = lane % (32 / VW) * VW;
+#pragma unroll 16
+                    for (int r = lane / (32 / VW); r < 32; r += VW)
+                        if (r < rows && cc < cols)
+                            act_on(reinterpret_cast<V*>(value(hb, r, cc)),
+                                   (int64_t)(row0 + r) * prm.N + n0 + c + cc);
+                };
+                auto copy_rows = [&](int hb, auto act_on) {
+                    if (prm.N % 4 == 0) each_word(uint2{}, hb, act_on);
+                    else if (prm.N % 2 == 0) each_word(uint32_t{}, hb, act_on);
+                    else each_word(uint16_t{}, hb, act_on);
+                };
                 auto flush = [&](int hb, const CUtensorMap* map, __nv_bfloat16* out) {
-                    if (prm.tma_out) {
+                    if (OUT == kOutTma) {
                         fence_proxy_async();
                         __syncwarp();
                         if (lane == 0) {
@@ -368,16 +386,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     } else {
                         __syncwarp();
-#pragma unroll 8
-                        for (int r = 0; r < 32; ++r)
-                            if (r < rows && lane < cols)
-                                out[(int64_t)(row0 + r) * prm.N + n0 + c + lane] = *value(hb, r, lane);
+                        copy_rows(hb, [&](auto* word, int64_t i) {
+                            *reinterpret_cast<decltype(word)>(out + i) = *word;
+                        });
                         __syncwarp();
                     }
                 };
                 // Without Z and R, block h was last stored two blocks ago; with Z the two staged blocks are
                 // Z's and Y's, and each waits for the store before.
                 const int hy = prm.Z ? 0 : h;
+                if (OUT == kOutPlain && prm.R) {  // while no sums take registers
+                    copy_rows(hy, [&](auto* word, int64_t i) {
+                        *word = *reinterpret_cast<const std::remove_pointer_t<decltype(word)>*>(prm.R + i);
+                    });
+                    __syncwarp();
+                }
                 load();
                 if (prm.Z) {
                     if (lane == 0) bulk_wait_read();
@@ -414,12 +437,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ok = warp_wait<1>(rfull + 8u * hy, r_phase >> hy & 1, abort_flag, prm.waits);
                         if (!ok) break;
                         r_phase ^= 1u << hy;
-                    } else {
-#pragma unroll 8
-                        for (int r = 0; r < 32; ++r)
-                            if (r < rows && lane < cols)
-                                *value(hy, r, lane) = prm.R[(int64_t)(row0 + r) * prm.N + n0 + c + lane];
-                        __syncwarp();
                     }
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
@@ -445,13 +462,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     fetch_r(h, then);
                 }
             }
-            if (ok && (width <= cfirst || OUT != kOutEpilogue)) {
+            if (ok && (width <= cfirst || OUT == kOutPart)) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(accempty0 + 8u * ab, 0));
             }
         }
-        if (OUT == kOutEpilogue) {
+        if (OUT == kOutTma) {
             if (!ok && prm.R) linger();  // the blocks of R in flight
             if (lane == 0) bulk_wait_all();
         }
@@ -551,7 +568,6 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     p.backward = e.backward;
     p.idesc = idesc_bf16_f32(256, plan.NT, a.mn, b.mn);
     p.act = e.act;
-    p.tma_out = N % 8 == 0;
     p.bias = (const __nv_bfloat16*)e.bias;
     p.R = (const __nv_bfloat16*)e.R;
     p.Y = (__nv_bfloat16*)e.Y;
@@ -567,25 +583,29 @@ cudaError_t lin_gemm(const LinPlan& plan, int64_t M, int64_t N, int64_t K, const
     ok = ok && (b.mn ? make_map(&m[1], b.t, N, K, b.pitch, 64, kSlice)
                      : make_map(&m[1], b.t, K, N, b.pitch, kSlice, b_rows));
     m[2] = m[3] = m[4] = m[0];  // unused unless set below
-    if (!e.part && p.tma_out) {
+    if (!e.part && N % 8 == 0) {
         ok = ok && make_map(&m[2], e.Y, N, M, N, 32, 32);
         if (e.Z) ok = ok && make_map(&m[3], e.Z, N, M, N, 32, 32);
         if (e.R) ok = ok && make_map(&m[4], e.R, N, M, N, 32, 32);
     }
     if (!ok) return cudaErrorInvalidValue;
-    const bool part = e.part != nullptr;
+    // plain stores need the second staged block (for R beside Z), so they run the form that has it
+    const Out out = e.part ? kOutPart : N % 8 ? kOutPlain : kOutTma;
     const bool deep = p.slices >= kDeepSlices;
     if (a.mn)
-        return part ? launch<true, true, kOutPart, true>(m, p, st)
-               : deep          ? launch<true, true, kOutEpilogue, true>(m, p, st)
-                               : launch<true, true, kOutEpilogue, false>(m, p, st);
+        return out == kOutPart    ? launch<true, true, kOutPart, true>(m, p, st)
+               : out == kOutPlain ? launch<true, true, kOutPlain, false>(m, p, st)
+               : deep             ? launch<true, true, kOutTma, true>(m, p, st)
+                                  : launch<true, true, kOutTma, false>(m, p, st);
     if (b.mn)
-        return part ? launch<false, true, kOutPart, true>(m, p, st)
-               : deep          ? launch<false, true, kOutEpilogue, true>(m, p, st)
-                               : launch<false, true, kOutEpilogue, false>(m, p, st);
-    return part ? launch<false, false, kOutPart, true>(m, p, st)
-           : deep          ? launch<false, false, kOutEpilogue, true>(m, p, st)
-                           : launch<false, false, kOutEpilogue, false>(m, p, st);
+        return out == kOutPart    ? launch<false, true, kOutPart, true>(m, p, st)
+               : out == kOutPlain ? launch<false, true, kOutPlain, false>(m, p, st)
+               : deep             ? launch<false, true, kOutTma, true>(m, p, st)
+                                  : launch<false, true, kOutTma, false>(m, p, st);
+    return out == kOutPart    ? launch<false, false, kOutPart, true>(m, p, st)
+           : out == kOutPlain ? launch<false, false, kOutPlain, false>(m, p, st)
+           : deep             ? launch<false, false, kOutTma, true>(m, p, st)
+                              : launch<false, false, kOutTma, false>(m, p, st);
 }
 
 }  // namespace flarepp
