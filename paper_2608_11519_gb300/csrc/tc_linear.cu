@@ -25,7 +25,7 @@
 // takes at 4.0 TB/s where nothing is read (measured with fills) and at up to 2.4 beside twice as many reads. With
 // GELU or SiLU a pair of outputs takes 24 cycles of the special-function unit and 22 of the multiply-add
 // pipe per scheduler, about what the writes leave, and a group waits for its accumulator's next products after
-// that: 65,536 x 256 -> 512 takes 24 us without an activation and 31.5 with GELU. Measured and left: sixteen
+// that: 65,536 x 256 -> 512 takes 23.6 us without an activation and 32.0 with GELU. Measured and left: sixteen
 // warps on every tile (36 us: a tile's fixed latencies are then in every warp's way), 16-column halves with the
 // next loads ahead (38 us: too few independent chains), eight warps of 64 columns and unpaired arithmetic
 // (46 us), more registers for the epilogue by setmaxnreg (spills).
