@@ -762,6 +762,16 @@ def _current_stream(device):
     return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
+def _current(stream, device):
+    """``stream`` (a torch stream, one with ``cuda_stream``, or a handle) as torch's current one: what
+    a call allocates is then that stream's, and not another stream's to have while the call runs."""
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        stream = (torch.cuda.ExternalStream(handle, device) if handle
+                  else torch.cuda.default_stream(device))
+    return torch.cuda.stream(stream)
+
+
 def _enqueue(name, device, stream, *args):
     """Call entry ``flarepp_<name>`` with the device current, the stream as last argument."""
     fn = _entry(name)
@@ -821,6 +831,9 @@ def _linear_shape(X, W, act):
 def _linear(X, W, b, residual, act, Y, Z, keep, workspace, status, stream):
     s, xp, wp = _linear_shape(X, W, act)
     dev, dt, out = X.device, X.dtype, W.shape[0]
+    if stream is not None:
+        with _current(stream, dev):
+            return _linear(X, W, b, residual, act, Y, Z, keep, workspace, status, None)
     shape = (*X.shape[:-1], out)
     bp = 0 if b is None else _need(b, "b", (out,), dt, dev)
     rp = 0 if residual is None else _need(residual, "residual", shape, dt, dev)
@@ -834,7 +847,7 @@ def _linear(X, W, b, residual, act, Y, Z, keep, workspace, status, stream):
     zp = 0 if Z is None else _need(Z, "Z", shape, dt, dev)
     ref = ctypes.byref(s)
     buf, wsp, wsn = _scratch(workspace, _entry("linear_workspace_bytes")(ref), dev)
-    _enqueue("linear_fwd", dev, stream, ref, xp, wp, bp, rp, yp, zp, wsp, wsn,
+    _enqueue("linear_fwd", dev, None, ref, xp, wp, bp, rp, yp, zp, wsp, wsn,
              _status_word(status, dev))
     return Y, Z
 
@@ -862,6 +875,9 @@ def linear_bwd(X, W, dY, Z=None, act="none", bias=True, dX=None, dW=None, db=Non
     out is returned as None."""
     s, xp, wp = _linear_shape(X, W, act)
     dev, dt = X.device, X.dtype
+    if stream is not None:
+        with _current(stream, dev):
+            return linear_bwd(X, W, dY, Z, act, bias, dX, dW, db, need, workspace, status)
     shape = (*X.shape[:-1], s.out)
     gp = _need(dY, "dY", shape, dt, dev)
     zp = _need(Z, "Z", shape, dt, dev, optional=act == "none")
@@ -877,7 +893,7 @@ def linear_bwd(X, W, dY, Z=None, act="none", bias=True, dX=None, dW=None, db=Non
     dbp = _need(db, "db", (s.out,), dt, dev, optional=True)
     ref = ctypes.byref(s)
     buf, wsp, wsn = _scratch(workspace, _entry("linear_bwd_workspace_bytes")(ref), dev)
-    _enqueue("linear_bwd", dev, stream, ref, xp, wp, zp, gp, dxp, dwp, dbp, wsp, wsn,
+    _enqueue("linear_bwd", dev, None, ref, xp, wp, zp, gp, dxp, dwp, dbp, wsp, wsn,
              _status_word(status, dev))
     return dX, dW, db
 
@@ -904,6 +920,9 @@ def embedding_fwd(ids, table, scale=1.0, Y=None, status=None, stream=None):
     bf16). A negative id gives a row of zeros; one of V or more too, and sets ``status`` (a device
     int32 [1]) to ERR_INVALID_ARGUMENT."""
     dev, ip, size = _ids_of(ids)
+    if stream is not None:
+        with _current(stream, dev):
+            return embedding_fwd(ids, table, scale, Y, status)
     dt = _float_dtype(table, "table")
     if table.dim() != 2:
         raise ValueError("expected table [V, C]")
@@ -916,7 +935,7 @@ def embedding_fwd(ids, table, scale=1.0, Y=None, status=None, stream=None):
     else:
         yp = _need(Y, "Y", shape, dt, dev)
     s = EmbeddingShape(ids.numel(), V, C, _DTYPES[dt], size)
-    _enqueue("embedding_fwd", dev, stream, ctypes.byref(s), ip, tp, float(scale), yp,
+    _enqueue("embedding_fwd", dev, None, ctypes.byref(s), ip, tp, float(scale), yp,
              _status_word(status, dev))
     return Y
 
@@ -925,6 +944,9 @@ def embedding_bwd(ids, dY, V, scale=1.0, dtable=None, workspace=None, status=Non
     """dtable [V, C], the gradient of ``embedding_fwd``'s table for dY [..., C]: the rows of dY
     summed by id in a fixed order, times ``scale``; rows that no id names are 0."""
     dev, ip, size = _ids_of(ids)
+    if stream is not None:
+        with _current(stream, dev):
+            return embedding_bwd(ids, dY, V, scale, dtable, workspace, status)
     dt = _float_dtype(dY, "dY")
     if dY.dim() != ids.dim() + 1:
         raise ValueError("expected dY of the ids' shape and one more dimension")
@@ -935,7 +957,7 @@ def embedding_bwd(ids, dY, V, scale=1.0, dtable=None, workspace=None, status=Non
     s = EmbeddingShape(ids.numel(), V, C, _DTYPES[dt], size)
     ref = ctypes.byref(s)
     buf, wsp, wsn = _scratch(workspace, _entry("embedding_bwd_workspace_bytes")(ref), dev)
-    _enqueue("embedding_bwd", dev, stream, ref, ip, gp, float(scale),
+    _enqueue("embedding_bwd", dev, None, ref, ip, gp, float(scale),
              _need(dtable, "dtable", (V, C), dt, dev), wsp, wsn, _status_word(status, dev))
     return dtable
 
@@ -1033,6 +1055,9 @@ class AdamW:
             if m_out is not None or v_out is not None:
                 raise ValueError("32-bit moments are the state itself: m_out and v_out are not used")
             return self.m, self.v
+        if stream is not None and self.params:
+            with _current(stream, self.device):
+                return self.moments(m_out, v_out)
         outs = []
         for given, name in ((m_out, "m_out"), (v_out, "v_out")):
             if given is None:
@@ -1043,7 +1068,7 @@ class AdamW:
                     for t, p in zip(given, self.params)]
             outs.append((given, (ctypes.c_void_p * max(1, len(ptrs)))(*ptrs)))
         if self.params:
-            _enqueue("adamw_moments", self.device, stream, self._table, len(self.params),
+            _enqueue("adamw_moments", self.device, None, self._table, len(self.params),
                      outs[0][1], outs[1][1])
         return outs[0][0], outs[1][0]
 
