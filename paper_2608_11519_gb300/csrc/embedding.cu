@@ -129,17 +129,21 @@ __device__ __forceinline__ uint32_t key_at(const I* ids, const uint32_t* keys, i
     return r < 0 ? (uint32_t)V : (uint32_t)r;
 }
 
-// hist[digit][tile] = how often the tile has the digit.
+// hist[digit][tile] = how often the tile has the digit. The first pass also clears the words that the sums
+// count and mark in (a memset's place in the stream, which no launch overlaps, costs 3 us).
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
     count_kernel(const I* ids, const uint32_t* keys, int64_t T,
                  int64_t V, int64_t tile, int shift, int bins, uint32_t* __restrict__ hist,
-                 int* status) {
+                 uint32_t* __restrict__ words, int64_t n_words, int* status) {
     extern __shared__ uint32_t cnt[];
     tc::pdl_trigger();
     for (int d = threadIdx.x; d < bins; d += kSortThreads) cnt[d] = 0;
     __syncthreads();
     tc::pdl_wait();
+    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < n_words;
+         i += (int64_t)gridDim.x * kSortThreads)
+        words[i] = 0;
     const int64_t i0 = (int64_t)blockIdx.x * tile, i1 = min(T, i0 + tile);
 #pragma unroll 4
     for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
@@ -271,7 +275,7 @@ __global__ void __launch_bounds__(kSortThreads)
 // distances up to 32 lie in 64 neighbouring places, so only the longer distances need the block.
 constexpr int kFewThreads = 1024;
 constexpr int64_t kFewPositions = 1024;  // 4,096 take 20 us, more than the radix passes
-constexpr int64_t kFewWords = 1 << 16;  // words that the block clears; more take a memset
+constexpr int64_t kFewWords = 1 << 16;  // words that a block clears; more take a memset
 
 template <typename I>
 __global__ void __launch_bounds__(kFewThreads)
@@ -674,6 +678,12 @@ cudaError_t sort(const flarepp_embedding_shape& s, const Layout& L, const void* 
     uint32_t* total = (uint32_t*)(ws + L.off_total);
     const uint32_t *keys = nullptr, *pos = nullptr;
     const unsigned tiles = (unsigned)L.sort.tiles;
+    int64_t words = (int64_t)(L.met_bytes / 4);
+    if (words > kFewWords * tiles) {
+        const cudaError_t e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
+        if (e != cudaSuccess) return e;
+        words = 0;
+    }
     for (int p = 0; p < L.sort.passes; ++p) {
         const int shift = p * L.sort.bits;
         *at = p & 1;
@@ -681,6 +691,7 @@ cudaError_t sort(const flarepp_embedding_shape& s, const Layout& L, const void* 
         uint32_t* po = (uint32_t*)(ws + L.off_pos[*at]);
         cudaError_t e = launch_pdl(count_kernel<I>, dim3(tiles), dim3(kSortThreads), bins * 4, st,
                                    (const I*)ids, keys, s.T, s.V, L.sort.tile, shift, bins, hist,
+                                   (uint32_t*)(ws + L.off_met), p == 0 ? words : 0,
                                    p == 0 ? status : nullptr);
         if (e == cudaSuccess)
             e = launch_pdl(scan_kernel, dim3((unsigned)cdiv(bins, 8)), dim3(256), 0, st, hist,
@@ -812,10 +823,8 @@ flarepp_status embedding_bwd(const flarepp_embedding_shape* shape, const void* i
         e = s.id_bytes == 4 ? sort_few<int32_t>(s, L, ids, ws, status, st)
                             : sort_few<int64_t>(s, L, ids, ws, status, st);
     } else {
-        e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
-        if (e == cudaSuccess)
-            e = s.id_bytes == 4 ? sort<int32_t>(s, L, ids, ws, status, &at, st)
-                                : sort<int64_t>(s, L, ids, ws, status, &at, st);
+        e = s.id_bytes == 4 ? sort<int32_t>(s, L, ids, ws, status, &at, st)
+                            : sort<int64_t>(s, L, ids, ws, status, &at, st);
     }
     if (e != cudaSuccess) return FLAREPP_ERR_CUDA;
     using B = __nv_bfloat16;
