@@ -3,15 +3,15 @@
 // The gradient sums the rows of dY by id. Adding them with atomics would make the result depend on
 // their order and serialises where ids repeat (byte sequences meet each row hundreds of times), so
 // the positions are sorted by id first: a stable least-digit-first radix sort of (id, position) in
-// one pass for tables of up to 2,047 rows, two up to 4 M, three beyond (up to 1,024 positions: in one
-// block's shared memory). Then equal stretches of
+// one pass for tables of up to 2,047 rows, two up to 4 M, three beyond (up to 1,024 positions: by
+// counting for each what comes before it). Then equal stretches of
 // the sorted positions are summed in parallel whatever the lengths of the runs of one id; a run that
 // crosses from one stretch into the next leaves float32 partial sums, which a last kernel adds in
 // order. The gradient is written once: a bit per row says which rows no id names.
 //
 // All of it is bound by bytes. Measured: the lookup of 131,072 rows of 256 bf16 values 17 us, 4.0 TB/s of
-// writes, as fast as HBM fills; the gradient of those rows (257 of a table) 40 us, of which the sums
-// 16 (4.2 TB/s), the sort 15 and the join 8, the latter two mostly the latencies of four short launches; the
+// writes, as fast as HBM fills; the gradient of those rows (257 of a table) 34 us, of which the sums
+// 16 (4.2 TB/s) and the rest the latencies of four short launches, which overlap in part; the
 // gradient of 262,144 rows of 512 float32 values (131,072 of a table, most of them met never) 181 us: the sums
 // 113 at the copy rate, the zeros 28, the sort 34.
 //
@@ -120,13 +120,17 @@ struct SortPlan {
     int64_t tile, tiles;  // positions per block, blocks
 };
 
-// The id of position i as a sort key: empty positions come last, as V.
+// An id as a sort key: empty positions come last, as V.
+template <typename I>
+__device__ __forceinline__ uint32_t key_of(I id, int64_t V, int* status) {
+    const int64_t r = row_of(id, V, status);
+    return r < 0 ? (uint32_t)V : (uint32_t)r;
+}
+// That of position i, from the pass before if there was one.
 template <typename I>
 __device__ __forceinline__ uint32_t key_at(const I* ids, const uint32_t* keys, int64_t i,
                                            int64_t V, int* status) {
-    if (keys) return keys[i];
-    const int64_t r = row_of(ids[i], V, status);
-    return r < 0 ? (uint32_t)V : (uint32_t)r;
+    return keys ? keys[i] : key_of(ids[i], V, status);
 }
 
 // hist[digit][tile] = how often the tile has the digit. The first pass also clears the words that the sums
@@ -270,41 +274,55 @@ __global__ void __launch_bounds__(kSortThreads)
     }
 }
 
-// Few positions: one block sorts (id, position) pairs in shared memory by a bitonic network, in one
-// launch instead of three or six, and clears the words that the sums count on. A warp's 32 pairs at
-// distances up to 32 lie in 64 neighbouring places, so only the longer distances need the block.
-constexpr int kFewThreads = 1024;
-constexpr int64_t kFewPositions = 1024;  // 4,096 take 20 us, more than the radix passes
-constexpr int64_t kFewWords = 1 << 16;  // words that a block clears; more take a memset
+// Few positions, in one launch instead of three or six: a position's place is the number of keys that come
+// before it, T comparisons each, which kFewSplit threads share. A block holds all keys and places
+// kFewPlaced positions; the blocks also clear the words that the sums count on.
+constexpr int kFewThreads = 256, kFewSplit = 4, kFewPlaced = kFewThreads / kFewSplit;
+constexpr int64_t kFewPositions = 1024;  // 2,000 take 22 us in all, with the radix passes 15 to 25
+constexpr int64_t kClearWords = 1 << 16;  // words that a block clears; more take a memset
 
 template <typename I>
 __global__ void __launch_bounds__(kFewThreads)
-    few_kernel(const I* ids, int T, int places, int64_t V,
-               uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out,
-               uint32_t* __restrict__ words, int64_t n_words, int* status) {
-    extern __shared__ uint64_t pairs[];  // [places], a power of two of at least 64
+    few_kernel(const I* ids, int T, int64_t V, uint32_t* __restrict__ keys_out,
+               uint32_t* __restrict__ pos_out, uint32_t* __restrict__ words, int64_t n_words,
+               int* status) {
+    extern __shared__ uint4 few_keys[];  // [groups]: four keys each, beyond T the largest number
+    uint32_t* key = reinterpret_cast<uint32_t*>(few_keys);
+    const int groups = (T + 3) / 4;
     tc::pdl_trigger();
     tc::pdl_wait();
-    for (int64_t i = threadIdx.x; i < n_words; i += kFewThreads) words[i] = 0;
-    for (int i = threadIdx.x; i < places; i += kFewThreads)
-        pairs[i] = i < T ? (uint64_t)key_at(ids, nullptr, i, V, status) << 32 | (uint32_t)i : ~0ull;
+    for (int64_t i = (int64_t)blockIdx.x * kFewThreads + threadIdx.x; i < n_words;
+         i += (int64_t)gridDim.x * kFewThreads)
+        words[i] = 0;
+    I id[kFewPositions / kFewThreads];
+#pragma unroll
+    for (int k = 0; k < kFewPositions / kFewThreads; ++k) {
+        const int i = k * kFewThreads + threadIdx.x;
+        if (i < T) id[k] = ids[i];
+    }
+#pragma unroll
+    for (int k = 0; k < kFewPositions / kFewThreads; ++k) {
+        const int i = k * kFewThreads + threadIdx.x;
+        if (i < 4 * groups)
+            key[i] = i < T ? key_of(id[k], V, blockIdx.x ? nullptr : status) : 0xffffffffu;
+    }
     __syncthreads();
-    for (int size = 2; size <= places; size *= 2)
-        for (int d = size / 2; d > 0; d /= 2) {
-            for (int p = threadIdx.x; p < places / 2; p += kFewThreads) {
-                const int lo = 2 * p - (p & (d - 1)), hi = lo + d;
-                const uint64_t a = pairs[lo], b = pairs[hi];
-                if ((a > b) == ((lo & size) == 0)) {
-                    pairs[lo] = b;
-                    pairs[hi] = a;
-                }
-            }
-            if (d > 32 || d == 1) __syncthreads();  // after d = 1 a longer distance follows
-            else __syncwarp();
-        }
-    for (int i = threadIdx.x; i < T; i += kFewThreads) {
-        keys_out[i] = (uint32_t)(pairs[i] >> 32);
-        pos_out[i] = (uint32_t)pairs[i];
+    const int i = blockIdx.x * kFewPlaced + threadIdx.x / kFewSplit;
+    const uint32_t mine = i < T ? key[i] : 0;
+    int before = 0;
+    // equal keys come in the order of their positions: those of earlier positions count too
+#pragma unroll 4
+    for (int g = threadIdx.x % kFewSplit; g < groups; g += kFewSplit) {
+        const uint4 k = few_keys[g];
+        const int j = 4 * g;
+        before += (k.x < mine + (j < i)) + (k.y < mine + (j + 1 < i)) + (k.z < mine + (j + 2 < i)) +
+                  (k.w < mine + (j + 3 < i));
+    }
+#pragma unroll
+    for (int o = 1; o < kFewSplit; o *= 2) before += __shfl_xor_sync(0xffffffffu, before, o);
+    if (i < T && threadIdx.x % kFewSplit == 0) {
+        keys_out[before] = mine;
+        pos_out[before] = (uint32_t)i;
     }
 }
 
@@ -344,7 +362,8 @@ __device__ __forceinline__ void copy_async(Vec<E, N>* dst, const E* src) {
         *dst = load_vec<E, N>(src);
 }
 
-// Zeros for those of kZeroRows rows that no id names, in 16-byte stores whatever the alignment of a row.
+// Zeros for those of kZeroRows rows that no id names: a stretch of such rows at a time, in 16-byte stores
+// whatever the alignment of a row.
 template <typename E>
 __device__ void zero_rows(const uint32_t* met, int64_t v0, int64_t V, int64_t C,
                           int lane, E* __restrict__ dtable) {
@@ -353,15 +372,17 @@ __device__ void zero_rows(const uint32_t* met, int64_t v0, int64_t V, int64_t C,
     uint32_t gone = ~met[v0 / 32] >> (v0 % 32) & ((1u << kZeroRows) - 1u);
     if (V - v0 < kZeroRows) gone &= (1u << (V - v0)) - 1u;
     while (gone) {
-        const int v = __ffs(gone) - 1;
-        gone &= gone - 1;
-        E* row = dtable + (v0 + v) * C;
-        const int64_t before = min(C, (int64_t)((16 - (uintptr_t)row % 16) % 16 / sizeof(E)));
-        const int64_t wide = (C - before) * sizeof(E) / 16, after = before + wide * (16 / sizeof(E));
-        if (lane < before) row[lane] = zero;
+        const int v = __ffs(gone) - 1, rows = __ffs(~(gone >> v)) - 1;
+        gone &= ~(((1u << rows) - 1u) << v);
+        E* at = dtable + (v0 + v) * C;
+        const int64_t n = rows * C;
+        const int64_t before = min(n, (int64_t)((16 - (uintptr_t)at % 16) % 16 / sizeof(E)));
+        const int64_t wide = (n - before) * sizeof(E) / 16, after = before + wide * (16 / sizeof(E));
+        if (lane < before) at[lane] = zero;
+#pragma unroll 4
         for (int64_t k = lane; k < wide; k += 32)
-            reinterpret_cast<uint4*>(row + before)[k] = make_uint4(0, 0, 0, 0);
-        if (lane < C - after) row[after + lane] = zero;
+            reinterpret_cast<uint4*>(at + before)[k] = make_uint4(0, 0, 0, 0);
+        if (lane < n - after) at[after + lane] = zero;
     }
 }
 
@@ -679,7 +700,7 @@ cudaError_t sort(const flarepp_embedding_shape& s, const Layout& L, const void* 
     const uint32_t *keys = nullptr, *pos = nullptr;
     const unsigned tiles = (unsigned)L.sort.tiles;
     int64_t words = (int64_t)(L.met_bytes / 4);
-    if (words > kFewWords * tiles) {
+    if (words > kClearWords * tiles) {
         const cudaError_t e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
         if (e != cudaSuccess) return e;
         words = 0;
@@ -714,18 +735,16 @@ cudaError_t sort(const flarepp_embedding_shape& s, const Layout& L, const void* 
 template <typename I>
 cudaError_t sort_few(const flarepp_embedding_shape& s, const Layout& L, const void* ids, char* ws,
                      int* status, cudaStream_t st) {
-    int places = 64;
-    while (places < s.T) places *= 2;
-    const int64_t words = (int64_t)(L.met_bytes / 4);
-    const bool clear = words <= kFewWords;
-    if (!clear) {
+    const unsigned blocks = (unsigned)cdiv(s.T, kFewPlaced);
+    int64_t words = (int64_t)(L.met_bytes / 4);
+    if (words > kClearWords * blocks) {
         const cudaError_t e = cudaMemsetAsync(ws + L.off_met, 0, L.met_bytes, st);
         if (e != cudaSuccess) return e;
+        words = 0;
     }
-    return launch_pdl(few_kernel<I>, dim3(1), dim3(kFewThreads), (size_t)places * 8, st,
-                      (const I*)ids, (int)s.T, places, s.V, (uint32_t*)(ws + L.off_keys[0]),
-                      (uint32_t*)(ws + L.off_pos[0]), (uint32_t*)(ws + L.off_met),
-                      clear ? words : 0, status);
+    return launch_pdl(few_kernel<I>, dim3(blocks), dim3(kFewThreads), (size_t)cdiv(s.T, 4) * 16, st,
+                      (const I*)ids, (int)s.T, s.V, (uint32_t*)(ws + L.off_keys[0]),
+                      (uint32_t*)(ws + L.off_pos[0]), (uint32_t*)(ws + L.off_met), words, status);
 }
 
 template <typename E, int N>
