@@ -13,7 +13,7 @@
 namespace flarepp {
 namespace {
 
-constexpr int kDzThreads = 256;
+constexpr int kDzThreads = 256;  // also of the blocks that copy lines
 
 // Up to four rows the layer can run on the CUDA cores (gemv_kernel): a weight then meets so few
 // multiplications that its bytes are the bound, and one launch without tensor maps is the shortest
@@ -120,22 +120,52 @@ __global__ void __launch_bounds__(kGemvWarps * 32)
     Y[at] = __float2bfloat16_rn(y);
 }
 
+template <int BYTES>
+struct Bytes;
+template <>
+struct Bytes<2> { using T = uint16_t; };
+template <>
+struct Bytes<4> { using T = uint32_t; };
+template <>
+struct Bytes<8> { using T = uint2; };
+template <>
+struct Bytes<16> { using T = uint4; };
+
 // dst [rows][pitch] = src [rows][cols] with zeros behind each row: the 16-byte line pitch that
-// TMA asks for. One thread per eight values.
-__global__ void pad_kernel(const __nv_bfloat16* src, int64_t rows, int64_t cols,
-                           int64_t pitch, __nv_bfloat16* __restrict__ dst) {
-    tc::pdl_trigger();
-    tc::pdl_wait();
-    const int64_t per = pitch / 8, n = rows * per;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
-         i += (int64_t)gridDim.x * blockDim.x) {
+// TMA asks for. One thread per eight values, read in words of VW, which `cols` is a multiple of.
+struct Pad {
+    const __nv_bfloat16* src;
+    int64_t rows, cols, pitch;
+    __nv_bfloat16* dst;
+    unsigned blocks;  // of 256 threads; 0: nothing to do
+};
+template <int VW>
+__device__ void pad_rows(const Pad& p, unsigned block) {
+    using Piece = typename Bytes<2 * VW>::T;
+    const int64_t per = p.pitch / 8, n = p.rows * per;
+    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)p.blocks * 256) {
         const int64_t r = i / per, c = (i - r * per) * 8;
         __align__(16) __nv_bfloat16 v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = c + k < cols ? src[r * cols + c + k] : __float2bfloat16_rn(0.f);
-        *reinterpret_cast<uint4*>(dst + r * pitch + c) = *reinterpret_cast<const uint4*>(v);
+        for (int k = 0; k < 8; k += VW)
+            *reinterpret_cast<Piece*>(v + k) =
+                c + k < p.cols ? *reinterpret_cast<const Piece*>(p.src + r * p.cols + c + k) : Piece{};
+        *reinterpret_cast<uint4*>(p.dst + r * p.pitch + c) = *reinterpret_cast<const uint4*>(v);
     }
+}
+// Blocks a.blocks + b.blocks: the first ones' share of a, the others' of b.
+__device__ void pad_both(const Pad& a, const Pad& b, unsigned block) {
+    const Pad& p = block < a.blocks ? a : b;
+    if (block >= a.blocks) block -= a.blocks;
+    if (p.cols % 8 == 0) pad_rows<8>(p, block);
+    else if (p.cols % 4 == 0) pad_rows<4>(p, block);
+    else if (p.cols % 2 == 0) pad_rows<2>(p, block);
+    else pad_rows<1>(p, block);
+}
+__global__ void __launch_bounds__(256) pad_kernel(const Pad a, const Pad b) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    pad_both(a, b, blockIdx.x);
 }
 
 // The column sums of dZ: what dz_kernel's blocks left in part[n_part][ldz], for db.
@@ -247,36 +277,32 @@ __global__ void __launch_bounds__(kFinishThreads)
     }
 }
 
-template <int BYTES>
-struct Bytes;
-template <>
-struct Bytes<2> { using T = uint16_t; };
-template <>
-struct Bytes<4> { using T = uint32_t; };
-template <>
-struct Bytes<8> { using T = uint2; };
-template <>
-struct Bytes<16> { using T = uint4; };
-
 // dZ = dY o act'(Z) into lines of `ldz` values (not written when dZ is null), and the column sums
 // of the unrounded dZ over the block's rows into db_part[blockIdx.y][ldz]. `lanes` threads (a power of
 // two up to 32) take eight columns each of a row, and the block as many rows at once as it has room for.
+// The blocks from gx * gy on copy a and b instead, which then need no launch of their own.
 // VW: values that a load takes, which `cols` is a multiple of (30,000 x 900: 37 us with single values).
 template <int VW>
 __global__ void __launch_bounds__(kDzThreads, 4)
     dz_kernel(const __nv_bfloat16* dY, const __nv_bfloat16* Z,
               int64_t rows, int64_t cols, int64_t rows_per, int lanes, int act, int64_t ldz,
-              __nv_bfloat16* __restrict__ dZ, float* __restrict__ db_part) {
+              __nv_bfloat16* __restrict__ dZ, float* __restrict__ db_part, unsigned gx, unsigned gy,
+              const Pad a, const Pad b) {
     tc::pdl_trigger();
     tc::pdl_wait();
+    if (blockIdx.x >= gx * gy) {
+        pad_both(a, b, blockIdx.x - gx * gy);
+        return;
+    }
+    const unsigned bx = blockIdx.x % gx, by = blockIdx.x / gx;
     __shared__ float sums[kDzThreads * 8];  // [rows at once][lanes * 8]
     const int lane = threadIdx.x % lanes, ty = threadIdx.x / lanes, at_once = kDzThreads / lanes;
-    const int64_t c = ((int64_t)blockIdx.x * lanes + lane) * 8;
-    const int64_t r1 = min(rows, (int64_t)(blockIdx.y + 1) * rows_per);
+    const int64_t c = ((int64_t)bx * lanes + lane) * 8;
+    const int64_t r1 = min(rows, (int64_t)(by + 1) * rows_per);
     uint64_t sum[4] = {0, 0, 0, 0};  // pairs
     if (c < cols) {
 #pragma unroll 2
-        for (int64_t r = (int64_t)blockIdx.y * rows_per + ty; r < r1; r += at_once) {
+        for (int64_t r = (int64_t)by * rows_per + ty; r < r1; r += at_once) {
             __align__(16) __nv_bfloat16 g[8], z[8];
             const int64_t at = r * cols + c;
             using Piece = typename Bytes<2 * VW>::T;
@@ -304,12 +330,12 @@ __global__ void __launch_bounds__(kDzThreads, 4)
         *reinterpret_cast<float2*>(&sums[threadIdx.x * 8 + 2 * k]) = halves(sum[k]);
     __syncthreads();
     const int width = lanes * 8;
-    const int64_t col = (int64_t)blockIdx.x * width + threadIdx.x;
+    const int64_t col = (int64_t)bx * width + threadIdx.x;
     if ((int)threadIdx.x < width && col < cols) {
         float s = 0.f;
 #pragma unroll 8
         for (int k = 0; k < at_once; ++k) s += sums[k * width + threadIdx.x];
-        db_part[(int64_t)blockIdx.y * ldz + col] = s;
+        db_part[(int64_t)by * ldz + col] = s;
     }
 }
 
@@ -402,11 +428,14 @@ BwdLayout bwd_layout(const Shape& s) {
     return L;
 }
 
-cudaError_t pad(const void* src, int64_t rows, int64_t cols, void* dst, cudaStream_t st) {
-    const int64_t n = rows * pitch_of(cols) / 8;
-    const int64_t blocks = cdiv(n, 256) < 32 * kNumSMs ? cdiv(n, 256) : 32 * kNumSMs;
-    return launch_pdl(pad_kernel, dim3((unsigned)blocks), dim3(256), 0, st,
-                      (const __nv_bfloat16*)src, rows, cols, pitch_of(cols), (__nv_bfloat16*)dst);
+Pad pad(const void* src, int64_t rows, int64_t cols, void* dst) {
+    const int64_t blocks = cdiv(rows * pitch_of(cols) / 8, 256);
+    return {(const __nv_bfloat16*)src, rows, cols, pitch_of(cols), (__nv_bfloat16*)dst,
+            (unsigned)(blocks < 32 * kNumSMs ? blocks : 32 * kNumSMs)};
+}
+cudaError_t pads(const Pad& a, const Pad& b, cudaStream_t st) {
+    if (a.blocks + b.blocks == 0) return cudaSuccess;
+    return launch_pdl(pad_kernel, dim3(a.blocks + b.blocks), dim3(256), 0, st, a, b);
 }
 
 cudaError_t finish(const float* part, const LinPlan& plan, int64_t rows, int64_t cols,
@@ -478,14 +507,16 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
     }
     char* ws = (char*)workspace;
     LinOperand x{X, s.K, 0}, w{W, s.K, 0};
+    Pad px{}, pw{};
     if (pad_x(s.K)) {
-        if (pad(X, s.T, s.K, ws + L.off_x, st) != cudaSuccess) return FLAREPP_ERR_CUDA;
-        x = {ws + L.off_x, pitch_of(s.K), 0};
+        px = pad(X, s.T, s.K, ws + L.off_x);
+        x = {px.dst, px.pitch, 0};
     }
     if (pad_w(s.K, s.T)) {
-        if (pad(W, s.N, s.K, ws + L.off_w, st) != cudaSuccess) return FLAREPP_ERR_CUDA;
-        w = {ws + L.off_w, pitch_of(s.K), 0};
+        pw = pad(W, s.N, s.K, ws + L.off_w);
+        w = {pw.dst, pw.pitch, 0};
     }
+    if (pads(px, pw, st) != cudaSuccess) return FLAREPP_ERR_CUDA;
     const cudaError_t err = L.few ? lin_few(s.T, s.N, s.K, x, w, e, status, st)
                                   : product(L.plan, L.split, s.T, s.N, s.K, x, w, e,
                                             (float*)(ws + L.off_part), status, st);
@@ -528,22 +559,25 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
     const bool own_dz = L.own_dz && (dX || dW);
     cudaError_t e = cudaSuccess;
     const bool fused = L.fused && dX;
-    if (!fused && (own_dz || db)) {
-        const dim3 grid((unsigned)cdiv(s.N, L.dz_lanes * 8), (unsigned)L.dz_blocks);
-        auto kernel = s.N % 2 ? dz_kernel<1> : s.N % 4 ? dz_kernel<2> : s.N % 8 ? dz_kernel<4> : dz_kernel<8>;
-        e = launch_pdl(kernel, grid, dim3(kDzThreads), 0, st, (const __nv_bfloat16*)dY,
-                       (const __nv_bfloat16*)Z, s.T, s.N, L.dz_rows, L.dz_lanes, s.act, ldz,
-                       (__nv_bfloat16*)(own_dz ? ws + L.off_dz : nullptr),
-                       (float*)(db ? ws + L.off_db : nullptr));
-    }
     LinOperand x{X, s.K, 0}, w{W, s.K, 0};
+    Pad px{}, pw{};
     if (pad_x(s.K)) {
-        if (e == cudaSuccess && dW) e = pad(X, s.T, s.K, ws + L.off_x, st);
+        if (dW) px = pad(X, s.T, s.K, ws + L.off_x);
         x = {ws + L.off_x, pitch_of(s.K), 0};
     }
     if (pad_w(s.K, s.T)) {
-        if (e == cudaSuccess && dX) e = pad(W, s.N, s.K, ws + L.off_w, st);
+        if (dX) pw = pad(W, s.N, s.K, ws + L.off_w);
         w = {ws + L.off_w, pitch_of(s.K), 0};
+    }
+    if (!fused && (own_dz || db)) {
+        const unsigned gx = (unsigned)cdiv(s.N, L.dz_lanes * 8), gy = (unsigned)L.dz_blocks;
+        auto kernel = s.N % 2 ? dz_kernel<1> : s.N % 4 ? dz_kernel<2> : s.N % 8 ? dz_kernel<4> : dz_kernel<8>;
+        e = launch_pdl(kernel, dim3(gx * gy + px.blocks + pw.blocks), dim3(kDzThreads), 0, st,
+                       (const __nv_bfloat16*)dY, (const __nv_bfloat16*)Z, s.T, s.N, L.dz_rows, L.dz_lanes,
+                       s.act, ldz, (__nv_bfloat16*)(own_dz ? ws + L.off_dz : nullptr),
+                       (float*)(db ? ws + L.off_db : nullptr), gx, gy, px, pw);
+    } else {
+        e = pads(px, pw, st);
     }
     int db_parts = (int)L.dz_blocks;
     if (e == cudaSuccess && fused)
