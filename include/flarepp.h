@@ -386,7 +386,7 @@ typedef enum {
 } flarepp_activation;
 
 typedef struct {
-    int64_t rows; /* tokens: 0 (a no-op) to 2^31 - 1 */
+    int64_t rows; /* tokens: 0 (a no-op) to 2^31 - 256 */
     int64_t in;   /* input features, 1 to 2^20 */
     int64_t out;  /* output features, 1 to 2^20 */
     int32_t dtype; /* FLAREPP_BF16 (FLAREPP_F32: FLAREPP_ERR_UNSUPPORTED, as for the mixer) */

@@ -350,7 +350,8 @@ flarepp_status check_shape(const flarepp_linear_shape* s, Shape* o) {
     if (!s || s->rows < 0 || s->in < 1 || s->out < 1) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (s->dtype != FLAREPP_F32 && s->dtype != FLAREPP_BF16) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (s->act < FLAREPP_ACT_NONE || s->act > FLAREPP_ACT_SILU) return FLAREPP_ERR_INVALID_ARGUMENT;
-    if (s->dtype != FLAREPP_BF16 || s->rows > 0x7fffffff || s->in > (1 << 20) || s->out > (1 << 20))
+    // the rows of the last tile of 256 have 32-bit numbers
+    if (s->dtype != FLAREPP_BF16 || s->rows > 0x7fffff00 || s->in > (1 << 20) || s->out > (1 << 20))
         return FLAREPP_ERR_UNSUPPORTED;
     *o = {s->rows, s->in, s->out, s->act};
     return FLAREPP_OK;

@@ -13,6 +13,15 @@ INVALID, UNSUPPORTED, WORKSPACE = (flarepp.ERR_INVALID_ARGUMENT, flarepp.ERR_UNS
                                    flarepp.ERR_WORKSPACE)
 
 
+def test_rows_whose_last_tile_would_pass_32_bits(lib):
+    for rows in ((1 << 31) - 255, (1 << 31) - 1):
+        s = linear_shape(rows=rows, in_=8, out=8)
+        assert fwd(lib, s) == bwd(lib, s) == UNSUPPORTED
+        assert lib.flarepp_linear_workspace_bytes(ctypes.byref(s)) == 0
+    s = linear_shape(rows=(1 << 31) - 256, in_=8, out=8)
+    assert fwd(lib, s, X=FAKE + 1) == INVALID  # large enough, refused for its address
+
+
 @pytest.fixture(scope="module")
 def lib():
     lib_build.build()
