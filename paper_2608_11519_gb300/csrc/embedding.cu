@@ -106,6 +106,86 @@ __global__ void __launch_bounds__(256)
     }
 }
 
+// Rows that only words of four bytes or less divide: threadIdx.x walks the 16-byte blocks of the output
+// that lie within the row. Each comes from the two blocks of the table that hold it, shifted by what the
+// row is off there; the values before the first block and behind the last are copied one by one.
+// 131,072 rows of 255 bf16 values take 31 us (57 value by value), of 254 31 (32 in pairs), 500,000 of 33 42
+// (53). Few rows are too few blocks (1,000 of 1,023: 6.6 us, 3.5 value by value) and rows without a
+// block in them all edges (2 M of 3: 27 and 16).
+constexpr int64_t kShiftedRows = 64 * kNumSMs;
+template <typename E, typename I>
+__global__ void __launch_bounds__(256)
+    lookup_shifted_kernel(const I* ids, const E* table, int64_t T, int64_t V, int64_t C, float scale,
+                          E* __restrict__ Y, int* status) {
+    constexpr int L = 16 / sizeof(E);
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    const int64_t t0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * kLookupRows;
+    const E* end = table + V * C;
+    const E* from[kLookupRows];   // the row, or null for zeros
+    int head[kLookupRows], blocks[kLookupRows];
+    int most = 0;
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k) {
+        const int64_t row = t0 + k < T ? row_of(ids[t0 + k], V, status) : -1;
+        from[k] = row >= 0 ? table + row * C : nullptr;
+        const unsigned off = (unsigned)((uintptr_t)(Y + (t0 + k) * C) % 16);
+        head[k] = (int)min(C, (int64_t)((16 - off) % 16 / sizeof(E)));
+        blocks[k] = t0 + k < T ? (int)((C - head[k]) / L) : 0;
+        most = max(most, blocks[k]);
+    }
+    for (int j = threadIdx.x; j < most; j += blockDim.x) {
+        uint4 lo[kLookupRows], hi[kLookupRows];
+#pragma unroll
+        for (int k = 0; k < kLookupRows; ++k) {
+            lo[k] = hi[k] = make_uint4(0, 0, 0, 0);
+            if (j >= blocks[k] || !from[k]) continue;
+            const E* src = from[k] + head[k] + j * L;
+            const uint4* base = reinterpret_cast<const uint4*>((uintptr_t)src / 16 * 16);
+            if (reinterpret_cast<const E*>(base + 2) <= end) {
+                lo[k] = base[0];
+                hi[k] = base[1];
+            } else {  // the table's last values, as they would come from there
+                __align__(16) E v[2 * L];
+                const E* b = reinterpret_cast<const E*>(base);
+#pragma unroll
+                for (int i = 0; i < 2 * L; ++i)
+                    if (b + i < end) v[i] = b[i];
+                    else from_f32(v[i], 0.f);
+                lo[k] = reinterpret_cast<const uint4*>(v)[0];
+                hi[k] = reinterpret_cast<const uint4*>(v)[1];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kLookupRows; ++k) {
+            if (j >= blocks[k]) continue;
+            uint32_t w[8] = {lo[k].x, lo[k].y, lo[k].z, lo[k].w, hi[k].x, hi[k].y, hi[k].z, hi[k].w};
+            const unsigned off = (unsigned)((uintptr_t)(from[k] + head[k]) % 16);
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = off & 8 ? w[i + 2] : w[i];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = off & 4 ? w[i + 1] : w[i];
+            if (sizeof(E) == 2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (off & 2) * 8);
+            Vec<E, L> o;
+            *reinterpret_cast<uint4*>(&o) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+            for (int i = 0; i < L; ++i) from_f32(o.v[i], from[k] ? to_f32(o.v[i]) * scale : 0.f);
+            store_vec<E, L>(Y + (t0 + k) * C + head[k] + j * L, o);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k) {
+        if (t0 + k >= T) break;
+        const int behind = head[k] + blocks[k] * L, n = (int)C - blocks[k] * L;
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const int c = i < head[k] ? i : behind + i - head[k];
+            from_f32(Y[(t0 + k) * C + c], from[k] ? to_f32(from[k][c]) * scale : 0.f);
+        }
+    }
+}
+
 // ------------------------------------------------------------------ sort
 // A block sorts a contiguous tile of the positions, a warp a contiguous stretch of the tile, 32
 // positions a step: the order of equal digits is the order of the tiles, stretches, steps and
@@ -678,6 +758,12 @@ Layout layout_of(const flarepp_embedding_shape& s) {
 template <typename E, int N, typename I>
 cudaError_t lookup(const flarepp_embedding_shape& s, const void* ids, const void* table,
                    float scale, void* Y, int* status, cudaStream_t st) {
+    if (sizeof(E) * N <= 4 && s.T >= kShiftedRows && s.C * sizeof(E) >= 32) {
+        const int x = lanes_for(cdiv(s.C * sizeof(E), 16), 32), y = 256 / x;
+        return launch_pdl(lookup_shifted_kernel<E, I>, dim3((unsigned)cdiv(s.T, y * kLookupRows)),
+                          dim3(x, y), 0, st, (const I*)ids, (const E*)table, s.T, s.V, s.C, scale,
+                          (E*)Y, status);
+    }
     const int x = lanes_for(cdiv(s.C, N), 256), y = 256 / x;
     return launch_pdl(lookup_kernel<E, N, I>, dim3((unsigned)cdiv(s.T, y * kLookupRows)),
                       dim3(x, y), 0, st, (const I*)ids, (const E*)table, s.T, s.V, s.C, scale,

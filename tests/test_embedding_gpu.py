@@ -75,6 +75,25 @@ def test_both_directions(T, V, C, kind):
         assert torch.equal(grad, flarepp.embedding_bwd(it, dY, V, scale))  # the same bits again
 
 
+@pytest.mark.parametrize("T", [9727, 9728, 20003])
+@pytest.mark.parametrize("C", [15, 17, 18, 33, 255, 346, 1023])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_lookup_of_rows_off_16_bytes(T, C, dt):
+    """Many rows whose lines start off 16-byte blocks, the table's last ones among them, and nothing is
+    written before or behind the output."""
+    V = 37
+    g = torch.Generator(device="cuda").manual_seed(C)
+    ids = torch.randint(-3, V, (T,), generator=g, device="cuda")
+    ids[-1] = V - 1
+    table = torch.randn(V, C, generator=g, device="cuda").to(dt)
+    table[3, 1], table[V - 1, C - 1] = float("inf"), float("nan")
+    buf = torch.full((T * C + 256,), 7.0, dtype=dt, device="cuda")
+    Y = flarepp.embedding_fwd(ids, table, 0.5, Y=buf[128:128 + T * C].view(T, C))
+    rows = torch.where((ids >= 0).unsqueeze(1), table[ids.clamp(min=0)] * 0.5, torch.zeros((), device="cuda"))
+    assert torch.equal(Y.nan_to_num(9.0), rows.to(dt).nan_to_num(9.0))  # a factor of 1/2 is exact
+    assert (buf[:128] == 7).all() and (buf[128 + T * C:] == 7).all()
+
+
 def test_gradient_against_differences():
     """The lookup is linear in the table: <dtable, D> is the change of the loss along D."""
     V, C = 50, 24
