@@ -407,11 +407,11 @@ __global__ void __launch_bounds__(kFewThreads)
 }
 
 // ------------------------------------------------------------------ sums
-// Thread (x, y) of a block sums units_of<E, N>() vectors of N columns of one stretch of the sorted positions. A run that lies within the stretch goes to the
-// table; one that began before it leaves its sum in head[stretch], one that begins here and goes on in
-// tail[stretch], and the stretch on a list of crossing runs: those of few parts from the front of
-// `crossing`, those of many from its back (the order does not matter: each run is a sum of its own).
-// A run's first stretch sets the row's bit in `met`.
+// Thread (x, y) of a block sums units_of<E, N>() vectors of N columns of one stretch of the sorted
+// positions. A run that lies within the stretch goes to the table; one that began before it leaves its sum
+// in head[stretch], one that begins here and goes on in tail[stretch], and the stretch on a list of crossing
+// runs: those of few parts from the front of `crossing`, those of many from its back (the order does not
+// matter: each run is a sum of its own). A run's first stretch sets the row's bit in `met`.
 constexpr int kSumThreads = 256;
 constexpr int kMinStretch = 16, kMaxStretch = 256;
 // a crossing run of more parts is joined by a whole block, one of up to so many by a row of threads
@@ -421,7 +421,8 @@ constexpr int kMaxHeld = 4096;   // positions whose keys and places a block hold
 constexpr int kBatch = 4;        // rows of a group of copies
 constexpr int kRing = 16;        // rows in flight per thread
 // Vectors per thread. What a position costs whatever its vectors (its key, its place, the turn of the
-// loop: some 30 instructions) bounds the sums of narrow vectors, so a thread takes several of those.
+// loop: some 30 instructions) bounds the sums of narrow vectors, so a thread takes several of those
+// (64,185 rows of 346 bf16 values: 75 us with one, 54 with four).
 template <typename E, int N>
 constexpr int units_of() {
     return sizeof(E) * N >= 16 ? 1 : sizeof(E) * N == 8 ? 2 : 4;

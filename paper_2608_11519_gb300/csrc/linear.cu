@@ -309,8 +309,11 @@ __global__ void __launch_bounds__(kDzThreads, 4)
 #pragma unroll
             for (int k = 0; k < 8; k += VW) {
                 const bool in = VW == 8 || c + k < cols;
-                *reinterpret_cast<Piece*>(g + k) = in ? *reinterpret_cast<const Piece*>(dY + at + k) : Piece{};
-                if (Z) *reinterpret_cast<Piece*>(z + k) = in ? *reinterpret_cast<const Piece*>(Z + at + k) : Piece{};
+                auto load = [&](const __nv_bfloat16* p) {
+                    return in ? *reinterpret_cast<const Piece*>(p + at + k) : Piece{};
+                };
+                *reinterpret_cast<Piece*>(g + k) = load(dY);
+                if (Z) *reinterpret_cast<Piece*>(z + k) = load(Z);
             }
             uint32_t* gp = reinterpret_cast<uint32_t*>(g);
             const uint32_t* zp = reinterpret_cast<const uint32_t*>(z);

@@ -7,12 +7,13 @@
 // turn dY's tile into dZ's in place (the swizzled tile that the tensor cores read), store it for dW and
 // add up its columns, and the pair's leader multiplies. A separate pass would read dZ once more, and its
 // launch: for 131,072 rows of 256 -> 512 with GELU, dZ with its column sums and dX take 107 us apart and 92
-// here, of which the bytes (268 MB read, 201 MB written) are about 50. What is left is the ring: four stages of
+// here, of which the bytes (268 MB read, 201 MB written) are about 70. What is left is the ring: four stages of
 // 32 KB, of which two are being made or multiplied, keep some 64 KB a SM in flight.
 //
 // Roles (28 warps): warp 0 the TMA producer of dY and Z, warp 2 that of W, warp 1 the MMA issuer (in the
-// pair's leader), warp 3 dZ's stores, warps 4..19 dZ, warps 20..27 the epilogue, which writes dX from two TMEM accumulators
-// of 256 columns by turns. The dZ warps are two groups of eight (16 rows of the CTA's 128 a warp) that take
+// pair's leader), warp 3 dZ's stores, warps 4..19 dZ, warps 20..27 the epilogue, which writes dX from two
+// TMEM accumulators of 256 columns by turns. The dZ warps are two groups of eight (16 rows of the CTA's 128 a
+// warp) that take
 // the slices in turn: making a slice is a chain of latencies (shared memory, the slope, the proxy fence),
 // and one group alone, of eight or of sixteen warps, took 115 us for the layer above, as did stores
 // issued by the dZ warps themselves, which freed a stage only at their next slice. A ring stage is
