@@ -732,7 +732,7 @@ Layout layout_of(const flarepp_embedding_shape& s) {
     const int64_t want = cdiv(s.T * cdiv(units, x) * x, (int64_t)24 * 32 * kNumSMs);
     int64_t most = kMaxHeld / (kSumThreads / x);
     if (most > kMaxStretch) most = kMaxStretch;
-    L.stretch = (int)(cdiv(want, kMinStretch) * kMinStretch);
+    L.stretch = (int)(cdiv(want, kBatch) * kBatch);
     if (L.stretch < kMinStretch) L.stretch = kMinStretch;
     if (want > most) L.stretch = (int)most;
     L.stretches = cdiv(s.T, L.stretch);
