@@ -10,8 +10,8 @@
 // order. The gradient is written once: a bit per row says which rows no id names.
 //
 // All of it is bound by bytes. Measured: the lookup of 131,072 rows of 256 bf16 values 17 us, 4.0 TB/s of
-// writes, as fast as HBM fills; the gradient of those rows (257 of a table) 34 us, of which the sums
-// 16 (4.2 TB/s) and the rest the latencies of four short launches, which overlap in part; the
+// writes, as fast as HBM fills; the gradient of those rows (257 of a table) 31 us, of which the sums
+// some 14 (16.6 alone on cold caches) and the rest the latencies of four short launches, which overlap in part; the
 // gradient of 262,144 rows of 512 float32 values (131,072 of a table, most of them met never) 181 us: the sums
 // 113 at the copy rate, the zeros 28, the sort 34.
 //
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kFewThreads)
 // runs: those of few parts from the front of `crossing`, those of many from its back (the order does not
 // matter: each run is a sum of its own). A run's first stretch sets the row's bit in `met`.
 constexpr int kSumThreads = 256;
-constexpr int kMinStretch = 16, kMaxStretch = 256;
+constexpr int kMaxStretch = 256;
 // a crossing run of more parts is joined by a whole block, one of up to so many by a row of threads
 // (what it can hold at once)
 constexpr int short_run(int n) { return n == 8 ? 4 : 8; }
@@ -727,13 +727,14 @@ struct Layout {
 Layout layout_of(const flarepp_embedding_shape& s) {
     Layout L{};
     L.sort = sort_plan(s);
-    // stretches so long that about 24 warps per SM have one each
+    // Stretches so long that about 24 warps per SM have one each (with 64 KB of rows in flight three blocks
+    // fit), in whole batches: in multiples of 16, and at least one, 131,072 rows of 256 values took 34 us
+    // instead of 31 and 257 rows 13 instead of 9.5.
     const int64_t units = cdiv(cdiv(s.C, vec_of(s)), units_of(s)), x = lanes_for(units, 32);
     const int64_t want = cdiv(s.T * cdiv(units, x) * x, (int64_t)24 * 32 * kNumSMs);
     int64_t most = kMaxHeld / (kSumThreads / x);
     if (most > kMaxStretch) most = kMaxStretch;
     L.stretch = (int)(cdiv(want, kBatch) * kBatch);
-    if (L.stretch < kMinStretch) L.stretch = kMinStretch;
     if (want > most) L.stretch = (int)most;
     L.stretches = cdiv(s.T, L.stretch);
     auto take = [&](int64_t bytes) {
