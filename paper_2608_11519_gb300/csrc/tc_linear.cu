@@ -258,6 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         const uint32_t rfull = rfull0 + 16u * e;
         uint32_t phase = 0, r_phase = 0;
+        int turn = 0;  // the staged block whose store is the longest ago
         bool ok = true;
         for (int v = first + ab * pairs; v < prm.n_work && ok; v += 2 * pairs, phase ^= 1) {
             const Work w = work_of(prm, v);
@@ -293,7 +294,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = warp_wait<2>(accfull0 + 8u * ab, phase, abort_flag, prm.waits);
             tc_fence_after();
             for (int c = cfirst; c < width && ok; c += c % 64 ? 96 : 32) {
-                const int h = DEEP ? 0 : c / 32 & 1;  // staged block
+                // Staged block: with R on its way into it, by the column; else the two by turns, across
+                // tiles too (widths such as 160 have an odd number of blocks), so that the wait for all
+                // stores but the last one is a wait for this block's.
+                const int h = DEEP ? 0 : tma_r ? c / 32 & 1 : turn;
                 if (OUT == kOutPart) {
                     float x[32];
                     tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(x));
@@ -392,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         __syncwarp();
                     }
                 };
-                // Without Z and R, block h was last stored two blocks ago; with Z the two staged blocks are
+                // Without Z and R, block h was last stored two stores ago; with Z the two staged blocks are
                 // Z's and Y's, and each waits for the store before.
                 const int hy = prm.Z ? 0 : h;
                 if (OUT == kOutPlain && prm.R) {  // while no sums take registers
@@ -455,6 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 store(hy);
                 flush(hy, &tmY, prm.Y);
+                turn ^= 1;
                 // this staged block's next turn
                 const int then = DEEP ? c + (c % 64 ? 96 : 32) : c + 128;
                 if (tma_r && !prm.Z && then < width) {
