@@ -303,14 +303,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_ld32(acc + c, reinterpret_cast<uint32_t*>(x));
                     tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
                     const int row = row0 + lane, at = n0 + c;
-                    if (row >= prm.M) continue;
+                    const int n = row < prm.M ? min(prm.NT - c, (int)prm.ldp - at) : 0;
                     float* d = prm.part + ((int64_t)w.chunk * prm.M + row) * prm.ldp + at;
-                    const int n = min(prm.NT - c, (int)prm.ldp - at);
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
                         if (i < n)
                             *reinterpret_cast<float4*>(d + i) =
                                 make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                    __syncwarp();  // the next load from TMEM wants the whole warp
                     continue;
                 }
                 // sums with the bias, as 16 pairs
@@ -466,6 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (lane == 0) bulk_wait_read();
                     fetch_r(h, then);
                 }
+                __syncwarp();  // lane 0 comes back before the next load from TMEM
             }
             if (ok && (width <= cfirst || OUT == kOutPart)) {
                 tc_fence_before();

@@ -326,6 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tma_store_2d(&tmX, smem_u32(staged), c, row0);
                     bulk_commit();
                 }
+                __syncwarp();  // the next load from TMEM wants the whole warp
             }
             tc_fence_before();
             __syncwarp();
@@ -343,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int w = 1; w < kDzWarps; ++w) f += db_sums[w * db_width + c];
             prm.db_part[(int64_t)blockIdx.x * prm.ldz + c] = f;
         }
+    __syncwarp();  // the sums end at different columns of a warp
     cluster_sync();  // no CTA leaves while the other one may still signal it or read its shared memory
     tc_fence_after();
     if (warp == 1) tmem_dealloc_pair(tmem, kTmemCols);
