@@ -374,7 +374,8 @@ FLAREPP_API void flarepp_test_wait_fault(int kernel, int64_t ring_item, uint64_t
  * The conventions of the top of this file hold: dense row-major device buffers, 16-byte
  * aligned, owned by the caller; arguments are checked before anything is enqueued; work is
  * enqueued on `stream` and the call returns. `status` of these calls is NULL or a device int32
- * that the kernels set (and never clear) when something went wrong that only they can see:
+ * (4-byte aligned) that the kernels set (and never clear) when something went wrong that only they
+ * can see:
  * FLAREPP_ERR_TIMEOUT for a bounded wait that gave up (the outputs are then invalid),
  * FLAREPP_ERR_INVALID_ARGUMENT for an embedding id beyond the table.
  * ------------------------------------------------------------------------------------------ */

@@ -336,9 +336,6 @@ __global__ void __launch_bounds__(kThreads)
 constexpr int kFew = 48;
 constexpr int kMany = 384;
 
-// the scales, one value at a time, may start anywhere in a buffer of all tensors' scales
-bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
-
 bool type_ok(int32_t t) { return t == FLAREPP_F32 || t == FLAREPP_BF16; }
 
 // 0..5 for the type combinations of the step
@@ -357,6 +354,7 @@ flarepp_status check_tensor(const flarepp_adamw_tensor& t, bool q8) {
         if (!p || !aligned16(p)) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (!aligned16(t.master) || (t.master && t.param_dtype == FLAREPP_F32))
         return FLAREPP_ERR_INVALID_ARGUMENT;
+    // the scales, one value at a time, may start anywhere in a buffer of all tensors' scales
     if (q8 && (!t.m_scale || !t.v_scale || !aligned4(t.m_scale) || !aligned4(t.v_scale)))
         return FLAREPP_ERR_INVALID_ARGUMENT;
     const size_t n = (size_t)t.n, sb = (size_t)cdiv(t.n, kBlockVals) * 4;

@@ -6,6 +6,7 @@
 namespace flarepp {
 
 inline bool aligned16(const void* ptr) { return ((uintptr_t)ptr & 15u) == 0; }
+inline bool aligned4(const void* ptr) { return ((uintptr_t)ptr & 3u) == 0; }
 
 inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     if (!a || !b || na == 0 || nb == 0) return false;

@@ -881,7 +881,7 @@ flarepp_status embedding_fwd(const flarepp_embedding_shape* shape, const void* i
     const flarepp_status bad = check_shape(shape);
     if (bad != FLAREPP_OK) return bad;
     const flarepp_embedding_shape s = *shape;
-    if (!isfinite(scale)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (!isfinite(scale) || !aligned4(status)) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (s.T == 0) return FLAREPP_OK;
     if (!ids || !table || !Y || !aligned16(ids) || !aligned16(table) || !aligned16(Y))
         return FLAREPP_ERR_INVALID_ARGUMENT;
@@ -909,7 +909,7 @@ flarepp_status embedding_bwd(const flarepp_embedding_shape* shape, const void* i
     const flarepp_status bad = check_shape(shape);
     if (bad != FLAREPP_OK) return bad;
     const flarepp_embedding_shape s = *shape;
-    if (!isfinite(scale)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (!isfinite(scale) || !aligned4(status)) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (!dtable || !aligned16(dtable)) return FLAREPP_ERR_INVALID_ARGUMENT;
     const size_t out_bytes = (size_t)s.V * s.C * elem(s);
     const Layout L = s.T ? layout_of(s) : Layout{};

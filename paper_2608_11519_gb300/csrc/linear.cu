@@ -494,6 +494,7 @@ flarepp_status linear_fwd(const flarepp_linear_shape* shape, const void* X, cons
     const void* all[6] = {X, W, Y, b, R, Z};
     for (int i = 0; i < 6; ++i)
         if ((i < 3 && !all[i]) || !aligned16(all[i])) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (!aligned4(status)) return FLAREPP_ERR_INVALID_ARGUMENT;
     const size_t y_bytes = (size_t)s.T * s.N * 2;
     const FwdLayout L = fwd_layout(s);
     if (L.total && (!workspace || (uintptr_t)workspace % kWsAlign || workspace_bytes < L.total))
@@ -540,6 +541,7 @@ flarepp_status linear_bwd(const flarepp_linear_shape* shape, const void* X, cons
     const void* all[7] = {X, W, Z, dY, dX, dW, db};
     for (const void* p : all)
         if (!aligned16(p)) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if (!aligned4(status)) return FLAREPP_ERR_INVALID_ARGUMENT;
     const size_t w_bytes = (size_t)s.N * s.K * 2, b_bytes = (size_t)s.N * 2;
     const size_t x_bytes = (size_t)s.T * s.K * 2, y_bytes = (size_t)s.T * s.N * 2;
     const BwdLayout L = s.T ? bwd_layout(s) : BwdLayout{};
