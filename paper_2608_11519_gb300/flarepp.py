@@ -971,7 +971,8 @@ class AdamW:
 
     params, grads: lists of contiguous CUDA tensors of the same shapes, float32 or bf16 each.
     masters: True makes a float32 master of every bf16 parameter (whose rounded copy it then is), a
-    list gives them (None where there is none). state_bits: 32, or 8 (the moments in 8 bits with
+    list gives them (None where there is none); masters that ``state`` holds are used before any is
+    made, and with ``masters=None`` too (False: none). state_bits: 32, or 8 (the moments in 8 bits with
     a scale for every ``STATE_BLOCK`` values: a quarter of the memory; include/flarepp.h says how).
     state: the state to go on from, as ``state_dict`` returns it (its tensors are used, not
     copied). The optimiser works on the buffers that it was given, whose storage it keeps alive:
@@ -989,8 +990,13 @@ class AdamW:
         self.weight_decay, self.state_bits = weight_decay, state_bits
         self.params, self.grads = params, grads
         self.device = _cuda_device(params[0], "params[0]") if params else None
-        if masters is True:
-            masters = [p.float() if p.dtype == torch.bfloat16 else None for p in params]
+        kept = state.get("masters") if state else None
+        if masters is None:
+            masters = kept
+        elif masters is True:
+            masters = [p.float() if p.dtype == torch.bfloat16 and k is None else k
+                       for p, k in zip(params, kept or [None] * len(params))]
+
         def own(ts):  # aliases, which keep the storage whatever becomes of the caller's tensors
             return [None if t is None else t.detach() for t in ts or [None] * len(params)]
 
@@ -1073,6 +1079,6 @@ class AdamW:
         return outs[0][0], outs[1][0]
 
     def state_dict(self):
-        """The state to save and to go on from; its tensors are the optimiser's own."""
+        """The state to save and to go on from, masters among it; its tensors are the optimiser's own."""
         return {"m": self.m, "v": self.v, "m_scale": self.m_scale, "v_scale": self.v_scale,
-                "step": self.steps}
+                "masters": self.masters, "step": self.steps}
