@@ -79,6 +79,13 @@ class Model:
         return loss, logits
 
 
+def check(dev):
+    """Stop where a layer's kernel gave up or met an id beyond the table: what it wrote is no result."""
+    status = flarepp.layers_status(dev)
+    if status != flarepp.OK:
+        raise flarepp.FlareppError(status, "a layer's kernel")
+
+
 def train(steps=60, B=16, N=1024, state_bits=8, lr=2e-3, seed=0, log=None):
     """The losses of ``steps`` steps, and the accuracy on a fresh batch at the end."""
     dev = torch.device("cuda", torch.cuda.current_device())
@@ -95,8 +102,10 @@ def train(steps=60, B=16, N=1024, state_bits=8, lr=2e-3, seed=0, log=None):
         losses.append(loss)
         if log and k % 10 == 0:
             log(f"step {k:3d}  loss {float(loss):.4f}")
+            check(dev)
     ids, cls = batch(gen, 4 * B, N, model.V, dev)
     _, logits = model.step(ids, cls)
+    check(dev)
     return [float(x) for x in losses], float((logits.argmax(1) == cls).float().mean())
 
 

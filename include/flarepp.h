@@ -375,7 +375,7 @@ FLAREPP_API void flarepp_test_wait_fault(int kernel, int64_t ring_item, uint64_t
  * aligned, owned by the caller; arguments are checked before anything is enqueued; work is
  * enqueued on `stream` and the call returns. `status` of these calls is NULL or a device int32
  * (4-byte aligned) that the kernels set (and never clear) when something went wrong that only they
- * can see:
+ * can see (without one they set a word of the library's, see flarepp_layers_device_status):
  * FLAREPP_ERR_TIMEOUT for a bounded wait that gave up (the outputs are then invalid),
  * FLAREPP_ERR_INVALID_ARGUMENT for an embedding id beyond the table.
  * ------------------------------------------------------------------------------------------ */
@@ -522,6 +522,16 @@ FLAREPP_API flarepp_status flarepp_adamw_step(const flarepp_adamw_tensor* tensor
 FLAREPP_API flarepp_status flarepp_adamw_moments(const flarepp_adamw_tensor* tensors,
                                                  int64_t n_tensors, float* const* m_out,
                                                  float* const* v_out, void* stream);
+
+/*
+ * What the kernels of the linear layer and the embedding recorded on the current device, since this
+ * was last asked there, for calls that passed status = NULL: FLAREPP_OK, FLAREPP_ERR_TIMEOUT (some call's
+ * outputs are invalid) or FLAREPP_ERR_INVALID_ARGUMENT (some id was beyond its table). The words are
+ * the library's, one set per device for all streams and threads. Waits for the work on `stream` (not
+ * for other streams'), writes the answer to *status_out (host memory) and clears the words. Not while
+ * `stream` is being captured.
+ */
+FLAREPP_API flarepp_status flarepp_layers_device_status(void* stream, int32_t* status_out);
 
 /* Static description of a status code (never NULL). */
 FLAREPP_API const char* flarepp_status_string(flarepp_status status);

@@ -22,7 +22,7 @@
 #include <math.h>
 
 #include "checks.h"
-#include "flarepp_internal.h"
+#include "layer_status.cuh"
 #include "tc_ptx.cuh"
 
 namespace flarepp {
@@ -63,12 +63,13 @@ __device__ __forceinline__ void store_vec(E* p, const Vec<E, N>& v) {
     *reinterpret_cast<R*>(p) = *reinterpret_cast<const R*>(&v);
 }
 
-// The row that an id names, or -1 for an empty position (an id of V or more is recorded).
-template <typename I>
+// The row that an id names, or -1 for an empty position (an id of V or more is one too, and recorded
+// where REPORT).
+template <bool REPORT, typename I>
 __device__ __forceinline__ int64_t row_of(I id, int64_t V, int* status) {
     if (id < 0) return -1;
     if ((int64_t)id >= V) {
-        if (status) atomicExch(status, (int)FLAREPP_ERR_INVALID_ARGUMENT);
+        if (REPORT) record_status(status, FLAREPP_ERR_INVALID_ARGUMENT);
         return -1;
     }
     return (int64_t)id;
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(256)
     int64_t row[kLookupRows];
 #pragma unroll
     for (int k = 0; k < kLookupRows; ++k)
-        row[k] = t0 + k < T ? row_of(ids[t0 + k], V, status) : -1;
+        row[k] = t0 + k < T ? row_of<true>(ids[t0 + k], V, status) : -1;
     for (int64_t c = (int64_t)threadIdx.x * N; c < C; c += (int64_t)blockDim.x * N) {
         Vec<E, N> x[kLookupRows];
 #pragma unroll
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(256)
     int most = 0;
 #pragma unroll
     for (int k = 0; k < kLookupRows; ++k) {
-        const int64_t row = t0 + k < T ? row_of(ids[t0 + k], V, status) : -1;
+        const int64_t row = t0 + k < T ? row_of<true>(ids[t0 + k], V, status) : -1;
         from[k] = row >= 0 ? table + row * C : nullptr;
         const unsigned off = (unsigned)((uintptr_t)(Y + (t0 + k) * C) % 16);
         head[k] = (int)min(C, (int64_t)((16 - off) % 16 / sizeof(E)));
@@ -201,16 +202,16 @@ struct SortPlan {
 };
 
 // An id as a sort key: empty positions come last, as V.
-template <typename I>
+template <bool REPORT, typename I>
 __device__ __forceinline__ uint32_t key_of(I id, int64_t V, int* status) {
-    const int64_t r = row_of(id, V, status);
+    const int64_t r = row_of<REPORT>(id, V, status);
     return r < 0 ? (uint32_t)V : (uint32_t)r;
 }
 // That of position i, from the pass before if there was one.
-template <typename I>
+template <bool REPORT, typename I>
 __device__ __forceinline__ uint32_t key_at(const I* ids, const uint32_t* keys, int64_t i,
                                            int64_t V, int* status) {
-    return keys ? keys[i] : key_of(ids[i], V, status);
+    return keys ? keys[i] : key_of<REPORT>(ids[i], V, status);
 }
 
 // hist[digit][tile] = how often the tile has the digit. The first pass also clears the words that the sums
@@ -231,7 +232,7 @@ __global__ void __launch_bounds__(kSortThreads)
     const int64_t i0 = (int64_t)blockIdx.x * tile, i1 = min(T, i0 + tile);
 #pragma unroll 4
     for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
-        atomicAdd(&cnt[(key_at(ids, keys, i, V, status) >> shift) & (bins - 1)], 1u);
+        atomicAdd(&cnt[(key_at<true>(ids, keys, i, V, status) >> shift) & (bins - 1)], 1u);
     __syncthreads();
     for (int d = threadIdx.x; d < bins; d += kSortThreads)
         hist[(int64_t)d * gridDim.x + blockIdx.x] = cnt[d];
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
             const int64_t i = b + 32 * k + lane;
-            key[k] = i < i1 ? key_at(ids, keys, i, V, nullptr) : (uint32_t)V;
+            key[k] = i < i1 ? key_at<false>(ids, keys, i, V, nullptr) : (uint32_t)V;
         }
     };
     load_keys(i0);
@@ -384,7 +385,9 @@ __global__ void __launch_bounds__(kFewThreads)
     for (int k = 0; k < kFewPositions / kFewThreads; ++k) {
         const int i = k * kFewThreads + threadIdx.x;
         if (i < 4 * groups)
-            key[i] = i < T ? key_of(id[k], V, blockIdx.x ? nullptr : status) : 0xffffffffu;
+            key[i] = i >= T         ? 0xffffffffu
+                     : blockIdx.x == 0 ? key_of<true>(id[k], V, status)
+                                       : key_of<false>(id[k], V, status);
     }
     __syncthreads();
     const int i = blockIdx.x * kFewPlaced + threadIdx.x / kFewSplit;
@@ -801,7 +804,7 @@ cudaError_t sort(const flarepp_embedding_shape& s, const Layout& L, const void* 
         cudaError_t e = launch_pdl(count_kernel<I>, dim3(tiles), dim3(kSortThreads), bins * 4, st,
                                    (const I*)ids, keys, s.T, s.V, L.sort.tile, shift, bins, hist,
                                    (uint32_t*)(ws + L.off_met), p == 0 ? words : 0,
-                                   p == 0 ? status : nullptr);
+                                   status);
         if (e == cudaSuccess)
             e = launch_pdl(scan_kernel, dim3((unsigned)cdiv(bins, 8)), dim3(256), 0, st, hist,
                            L.sort.tiles, bins, total);
@@ -949,6 +952,9 @@ flarepp_status embedding_bwd(const flarepp_embedding_shape* shape, const void* i
 }
 
 }  // namespace
+
+cudaError_t take_embedding_status(int32_t* out, cudaStream_t st) { return take_library_status(out, st); }
+
 }  // namespace flarepp
 
 extern "C" {

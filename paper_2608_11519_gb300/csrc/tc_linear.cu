@@ -534,6 +534,8 @@ cudaError_t launch(const CUtensorMap* m, const Gemm& p, cudaStream_t st) {
 
 }  // namespace
 
+cudaError_t take_product_status(int32_t* out, cudaStream_t st) { return take_library_status(out, st); }
+
 LinPlan lin_plan(int64_t M, int64_t N, int64_t K) {
     LinPlan p{};
     // equal column tiles, in whole 32-column blocks where there are several

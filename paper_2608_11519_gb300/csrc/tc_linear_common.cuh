@@ -6,6 +6,7 @@
 
 #include <atomic>
 
+#include "layer_status.cuh"
 #include "linear_internal.h"
 #include "tc_pair_ptx.cuh"
 
@@ -24,8 +25,8 @@ constexpr int kMaxSmem = 232448;
 // the launches' numbers for the test hook of the bounded waits (flarepp_test_wait_fault)
 enum LinKernel { kProductKernel = 16, kFewKernel = 17, kFusedKernel = 18 };
 
-// The bound of every wait of a launch, where a wait that gave up is recorded, and (for tests) the ring
-// item that CTA 0's producer never loads, or -1.
+// The bound of every wait of a launch, where a wait that gave up is recorded (null: the library's word),
+// and (for tests) the ring item that CTA 0's producer never loads, or -1.
 struct Waits {
     uint64_t limit_ns;
     int* status;
@@ -51,7 +52,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
                 if (*abort_flag) break;
                 if (globaltimer_ns() - t0 > w.limit_ns) {
                     *abort_flag = 1;
-                    if (w.status) atomicExch(w.status, (int)FLAREPP_ERR_TIMEOUT);
+                    record_status(w.status, FLAREPP_ERR_TIMEOUT);
                     break;
                 }
             }

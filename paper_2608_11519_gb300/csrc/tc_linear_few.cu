@@ -231,6 +231,8 @@ cudaError_t launch_few(const CUtensorMap* m, const Few& p, unsigned tiles, cudaS
 
 }  // namespace
 
+cudaError_t take_few_status(int32_t* out, cudaStream_t st) { return take_library_status(out, st); }
+
 cudaError_t lin_few(int64_t rows, int64_t cols, int64_t K, const LinOperand& x,
                     const LinOperand& w, const LinEpilogue& e, int* status, cudaStream_t st) {
     Few p{};

@@ -399,6 +399,8 @@ cudaError_t launch(const CUtensorMap* m, const Fused& p, int* ctas, cudaStream_t
 
 }  // namespace
 
+cudaError_t take_fused_status(int32_t* out, cudaStream_t st) { return take_library_status(out, st); }
+
 cudaError_t lin_fused(int64_t T, int64_t K, int64_t N, int act, const void* dY, const void* Z,
                       const LinOperand& w, void* dX, void* dZ, float* db_part, int64_t ldz,
                       int* ctas, int* status, cudaStream_t st) {

@@ -36,7 +36,8 @@ EXPORTED = ("flarepp_route_workspace_bytes", "flarepp_route_fwd", "flarepp_route
             "flarepp_linear_workspace_bytes", "flarepp_linear_fwd",
             "flarepp_linear_bwd_workspace_bytes", "flarepp_linear_bwd",
             "flarepp_embedding_fwd", "flarepp_embedding_bwd_workspace_bytes",
-            "flarepp_embedding_bwd", "flarepp_adamw_step", "flarepp_adamw_moments")
+            "flarepp_embedding_bwd", "flarepp_adamw_step", "flarepp_adamw_moments",
+            "flarepp_layers_device_status")
 N_STAGE_EVENTS = 6
 STAGES = ("encode1", "combine1", "encode2", "combine2", "decode")
 
@@ -166,7 +167,8 @@ def load(path: str = None):
             ("embedding_fwd", [ep, vp, vp, ctypes.c_float, vp, vp, vp]),
             ("embedding_bwd", [ep, vp, vp, ctypes.c_float, vp, vp, sz, vp, vp]),
             ("adamw_step", [tp, ctypes.c_int64, hp, vp]),
-            ("adamw_moments", [tp, ctypes.c_int64, vp, vp, vp])):
+            ("adamw_moments", [tp, ctypes.c_int64, vp, vp, vp]),
+            ("layers_device_status", [vp, ctypes.POINTER(ctypes.c_int32)])):
         getattr(lib, "flarepp_" + name).restype = ctypes.c_int
         getattr(lib, "flarepp_" + name).argtypes = args
     lib.flarepp_status_string.restype = ctypes.c_char_p
@@ -806,6 +808,25 @@ def _status_word(status, device):
     return 0 if status is None else _need(status, "status", (1,), torch.int32, device)
 
 
+def layers_status(device=None, stream=None) -> int:
+    """What the kernels of ``linear_*`` and ``embedding_*`` calls without ``status`` recorded on
+    ``device`` (default: torch's current one) since this was last asked: OK, ERR_TIMEOUT (a bounded
+    wait gave up: outputs are invalid) or ERR_INVALID_ARGUMENT (an id beyond the table). Waits for
+    ``stream`` (default: torch's current one there)."""
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    if dev.type != "cuda":
+        raise ValueError(f"the layers run on CUDA devices, not {dev}")
+    with torch.cuda.device(dev):
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        out = ctypes.c_int32(-1)
+        rc = _entry("layers_device_status")(handle, ctypes.byref(out))
+    if rc != OK:
+        raise FlareppError(rc, "flarepp_layers_device_status")
+    return int(out.value)
+
+
 def _linear_shape(X, W, act):
     """(shape, address of X, address of W) of a linear layer on device tensors X and W."""
     code = ACTIVATIONS.get(act)
@@ -855,7 +876,8 @@ def _linear(X, W, b, residual, act, Y, Z, keep, workspace, status, stream):
 def linear_fwd(X, W, b=None, residual=None, act="none", Y=None, workspace=None, status=None,
                stream=None):
     """Y = act(X W^T + b) + residual [..., out] for X [..., in], W [out, in], b [out], in bf16;
-    ``act`` one of ``ACTIVATIONS``. ``status``: a device int32 [1] that a timeout sets."""
+    ``act`` one of ``ACTIVATIONS``. ``status``: a device int32 [1] that a timeout sets (without one,
+    ``layers_status`` tells)."""
     return _linear(X, W, b, residual, act, Y, None, False, workspace, status, stream)[0]
 
 
@@ -918,7 +940,7 @@ def _float_dtype(t, what):
 def embedding_fwd(ids, table, scale=1.0, Y=None, status=None, stream=None):
     """Y [..., C] = scale * table[ids] for ids [...] (int32 or int64) and table [V, C] (float32 or
     bf16). A negative id gives a row of zeros; one of V or more too, and sets ``status`` (a device
-    int32 [1]) to ERR_INVALID_ARGUMENT."""
+    int32 [1]; without one, ``layers_status`` tells) to ERR_INVALID_ARGUMENT."""
     dev, ip, size = _ids_of(ids)
     if stream is not None:
         with _current(stream, dev):

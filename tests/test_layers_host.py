@@ -11,3 +11,7 @@ def test_status_words_off_four_bytes_are_refused(lib):  # noqa: F811
         assert bwd(lib, linear_shape(act=2), status=word) == INVALID
         assert emb_fwd(lib, emb_shape(), status=word) == INVALID
         assert emb_bwd(lib, emb_shape(), status=word) == INVALID
+
+
+def test_status_question_wants_an_answer_s_place(lib):  # noqa: F811
+    assert lib.flarepp_layers_device_status(None, None) == INVALID
