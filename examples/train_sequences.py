@@ -93,7 +93,8 @@ def train(steps=60, B=16, N=1024, state_bits=8, lr=2e-3, seed=0, log=None):
     model = Model(dev=dev, seed=seed)
     names = list(model.p)
     opt = flarepp.AdamW([model.p[k] for k in names], [model.g[k] for k in names], lr=lr,
-                        state_bits=state_bits, masters=True)
+                        state_bits=state_bits, masters=True,
+                        state_rounding="unbiased" if state_bits == 8 else "nearest")
     losses = []
     for k in range(steps):
         loss, _ = model.step(*batch(gen, B, N, model.V, dev))

@@ -59,7 +59,10 @@ struct Table {
 };
 struct Coef {
     float b1, c1, b2, c2, by_bias, eps, keep, rate;
+    uint32_t seed;  // of the step (kUnbiased8)
 };
+// The moments: float32, or codes of 8 bits, rounded to nearest or without bias.
+enum State { kFull, kNearest8, kUnbiased8 };
 
 template <int CAP>
 __device__ __forceinline__ int find_tensor(const Table<CAP>& t, uint32_t block) {
@@ -187,6 +190,32 @@ __device__ __forceinline__ uint32_t pack_r(float y) {
     return max(y < 1.f ? low : high, min(bits, 1u));
 }
 
+// Rounding without bias: a value goes up to the next code with a probability that is its distance from the
+// code below in steps, so that changes of less than half a step (a second moment moves by (1 - beta2) of
+// itself) are kept on average instead of lost. Random bits are a hash of the value's place in
+// its tensor and of the step: xor-shifts and multiplications by odd numbers (the fractional digits of the
+// square roots of 2 and 3), each output bit a function of all input bits; the lower half is for m,
+// the upper for sqrt(v).
+__host__ __device__ __forceinline__ uint32_t hashed(uint32_t x) {
+    x ^= x >> 16;
+    x *= 0x6A09E667u;
+    x ^= x >> 15;
+    x *= 0xBB67AE85u;
+    return x ^ (x >> 16);
+}
+// The e4m3 value above or below y: 3 mantissa bits, steps of 2^-9 below 2^-6 (which adding 2^-6 gives).
+__device__ __forceinline__ float dither_m(float y, uint32_t random) {
+    const float a = fabsf(y), lift = a < 0x1p-6f ? 0x1p-6f : 0.f;
+    const uint32_t bits = __float_as_uint(__fadd_rn(a, lift)) + ((random & 0xffffu) << 4);
+    return copysignf(__fsub_rn(__uint_as_float(bits & 0xfff00000u), lift), y);
+}
+// The code above or below y, as pack_r's codes (sixteenths below 1, which adding 1 gives).
+__device__ __forceinline__ uint32_t dither_r(float y, uint32_t random) {
+    const bool small = y < 1.f;
+    const uint32_t bits = __float_as_uint(small ? __fadd_rn(y, 1.f) : y) + (random >> 16 << 3);
+    return max((bits >> 19) - (126u << 4) - (small ? 16u : 0u), min(__float_as_uint(y), 1u));
+}
+
 // The largest |x| over the warp, as bits (so that a NaN is the largest of all).
 __device__ __forceinline__ float warp_most(const float (*x)[4]) {
     uint32_t most = 0;
@@ -198,10 +227,11 @@ __device__ __forceinline__ float warp_most(const float (*x)[4]) {
 }
 
 // 256 values from `at` on, by one warp. P, G: types of the weights and the gradients. MASTER: the
-// weights have a float32 master. Q8: 8-bit states. FULL: all 256 exist. A lane holds values
+// weights have a float32 master. S: the moments. FULL: all 256 exist. A lane holds values
 // 4 lane + 128 h + (0..3).
-template <typename P, typename G, bool MASTER, bool Q8, bool FULL>
+template <typename P, typename G, bool MASTER, State S, bool FULL>
 __device__ __forceinline__ void step_block(const Entry& e, const Coef& c, int64_t at) {
+    constexpr bool Q8 = S != kFull;
     const int lane = threadIdx.x % 32;
     const int64_t n = e.n;
     const int64_t block = at / kBlockVals;
@@ -271,7 +301,15 @@ __device__ __forceinline__ void step_block(const Entry& e, const Coef& c, int64_
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             y[k] = __fmul_rn(m[h][k], m_by);
-            rc[k] = pack_r(__fmul_rn(r[h][k], r_by));
+            const float root = __fmul_rn(r[h][k], r_by);
+            if (S == kUnbiased8) {
+                const uint64_t j = (uint64_t)(i + k);
+                const uint32_t random = hashed(((uint32_t)j + (uint32_t)(j >> 32) * 0x9E3779B9u) ^ c.seed);
+                y[k] = dither_m(y[k], random);
+                rc[k] = dither_r(root, random);
+            } else {
+                rc[k] = pack_r(root);
+            }
         }
         const uint32_t code = __byte_perm(__byte_perm(rc[0], rc[1], 0x0040),
                                           __byte_perm(rc[2], rc[3], 0x0040), 0x5410);
@@ -284,15 +322,15 @@ __device__ __forceinline__ void step_block(const Entry& e, const Coef& c, int64_
     }
 }
 
-template <typename P, typename G, bool MASTER, bool Q8, int CAP>
+template <typename P, typename G, bool MASTER, State S, int CAP>
 __global__ void __launch_bounds__(kThreads, 5)
     adamw_kernel(const __grid_constant__ Table<CAP> table, const Coef c) {
     const int t = find_tensor(table, blockIdx.x);
     const Entry& e = table.e[t];
     const int64_t n = e.n;
     const int64_t at = (int64_t)(blockIdx.x - table.first[t]) * kItem + threadIdx.x / 32 * kBlockVals;
-    if (at + kBlockVals <= n) step_block<P, G, MASTER, Q8, true>(e, c, at);
-    else if (at < n) step_block<P, G, MASTER, Q8, false>(e, c, at);
+    if (at + kBlockVals <= n) step_block<P, G, MASTER, S, true>(e, c, at);
+    else if (at < n) step_block<P, G, MASTER, S, false>(e, c, at);
 }
 
 // The values of 8-bit states; e.param and e.master are the outputs for m and v.
@@ -413,13 +451,13 @@ cudaError_t each_table(int64_t n_tensors, Pick pick, Fill fill, Go go) {
     return cudaSuccess;
 }
 
-template <typename P, typename G, bool MASTER, bool Q8, int CAP>
+template <typename P, typename G, bool MASTER, State S, int CAP>
 cudaError_t go_step(const Table<CAP>& t, unsigned blocks, const Coef& c, cudaStream_t st) {
-    adamw_kernel<P, G, MASTER, Q8, CAP><<<blocks, kThreads, 0, st>>>(t, c);
+    adamw_kernel<P, G, MASTER, S, CAP><<<blocks, kThreads, 0, st>>>(t, c);
     return cudaGetLastError();
 }
 
-template <bool Q8, int CAP>
+template <State S, int CAP>
 cudaError_t step_all(const flarepp_adamw_tensor* ts, int64_t n, const Coef& c, cudaStream_t st) {
     for (int kind = 0; kind < 6; ++kind) {
         const cudaError_t e = each_table<CAP>(
@@ -431,23 +469,31 @@ cudaError_t step_all(const flarepp_adamw_tensor* ts, int64_t n, const Coef& c, c
             [&](const Table<CAP>& t, unsigned blocks) {
                 using B = __nv_bfloat16;
                 switch (kind) {
-                    case 0: return go_step<float, float, false, Q8, CAP>(t, blocks, c, st);
-                    case 1: return go_step<float, B, false, Q8, CAP>(t, blocks, c, st);
-                    case 2: return go_step<B, float, false, Q8, CAP>(t, blocks, c, st);
-                    case 3: return go_step<B, B, false, Q8, CAP>(t, blocks, c, st);
-                    case 4: return go_step<B, float, true, Q8, CAP>(t, blocks, c, st);
+                    case 0: return go_step<float, float, false, S, CAP>(t, blocks, c, st);
+                    case 1: return go_step<float, B, false, S, CAP>(t, blocks, c, st);
+                    case 2: return go_step<B, float, false, S, CAP>(t, blocks, c, st);
+                    case 3: return go_step<B, B, false, S, CAP>(t, blocks, c, st);
+                    case 4: return go_step<B, float, true, S, CAP>(t, blocks, c, st);
                 }
-                return go_step<B, B, true, Q8, CAP>(t, blocks, c, st);
+                return go_step<B, B, true, S, CAP>(t, blocks, c, st);
             });
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
+template <int CAP>
+cudaError_t step_any(State s, const flarepp_adamw_tensor* ts, int64_t n, const Coef& c,
+                     cudaStream_t st) {
+    return s == kFull       ? step_all<kFull, CAP>(ts, n, c, st)
+           : s == kNearest8 ? step_all<kNearest8, CAP>(ts, n, c, st)
+                            : step_all<kUnbiased8, CAP>(ts, n, c, st);
+}
+
 flarepp_status adamw_step(const flarepp_adamw_tensor* ts, int64_t n, const flarepp_adamw_hyper* h,
-                          cudaStream_t st) {
+                          bool unbiased, cudaStream_t st) {
     if (!h || n < 0 || (n && !ts)) return FLAREPP_ERR_INVALID_ARGUMENT;
-    if (h->state_bits != 32 && h->state_bits != 8) return FLAREPP_ERR_INVALID_ARGUMENT;
+    if ((h->state_bits != 32 || unbiased) && h->state_bits != 8) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (!isfinite(h->lr) || !isfinite(h->weight_decay) || !(h->eps >= 0) || !isfinite(h->eps) ||
         !(h->beta1 >= 0 && h->beta1 < 1) || !(h->beta2 >= 0 && h->beta2 < 1) || h->step < 1)
         return FLAREPP_ERR_INVALID_ARGUMENT;
@@ -465,10 +511,9 @@ flarepp_status adamw_step(const flarepp_adamw_tensor* ts, int64_t n, const flare
     c.eps = (float)h->eps;
     c.keep = (float)(1 - h->lr * h->weight_decay);
     c.rate = (float)(h->lr / (1 - pow(h->beta1, (double)h->step)));
-    const cudaError_t e = n <= kFew ? (q8 ? step_all<true, kFew>(ts, n, c, st)
-                                          : step_all<false, kFew>(ts, n, c, st))
-                                    : (q8 ? step_all<true, kMany>(ts, n, c, st)
-                                          : step_all<false, kMany>(ts, n, c, st));
+    c.seed = hashed((uint32_t)(uint64_t)h->step * 0x9E3779B9u + (uint32_t)((uint64_t)h->step >> 32));
+    const State s = !q8 ? kFull : unbiased ? kUnbiased8 : kNearest8;
+    const cudaError_t e = n <= kFew ? step_any<kFew>(s, ts, n, c, st) : step_any<kMany>(s, ts, n, c, st);
     return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
 }
 
@@ -516,7 +561,12 @@ extern "C" {
 
 flarepp_status flarepp_adamw_step(const flarepp_adamw_tensor* tensors, int64_t n_tensors,
                                   const flarepp_adamw_hyper* hyper, void* stream) {
-    return flarepp::adamw_step(tensors, n_tensors, hyper, (cudaStream_t)stream);
+    return flarepp::adamw_step(tensors, n_tensors, hyper, false, (cudaStream_t)stream);
+}
+
+flarepp_status flarepp_adamw_step_unbiased(const flarepp_adamw_tensor* tensors, int64_t n_tensors,
+                                           const flarepp_adamw_hyper* hyper, void* stream) {
+    return flarepp::adamw_step(tensors, n_tensors, hyper, true, (cudaStream_t)stream);
 }
 
 flarepp_status flarepp_adamw_moments(const flarepp_adamw_tensor* tensors, int64_t n_tensors,

@@ -37,7 +37,7 @@ EXPORTED = ("flarepp_route_workspace_bytes", "flarepp_route_fwd", "flarepp_route
             "flarepp_linear_bwd_workspace_bytes", "flarepp_linear_bwd",
             "flarepp_embedding_fwd", "flarepp_embedding_bwd_workspace_bytes",
             "flarepp_embedding_bwd", "flarepp_adamw_step", "flarepp_adamw_moments",
-            "flarepp_layers_device_status")
+            "flarepp_layers_device_status", "flarepp_adamw_step_unbiased")
 N_STAGE_EVENTS = 6
 STAGES = ("encode1", "combine1", "encode2", "combine2", "decode")
 
@@ -167,6 +167,7 @@ def load(path: str = None):
             ("embedding_fwd", [ep, vp, vp, ctypes.c_float, vp, vp, vp]),
             ("embedding_bwd", [ep, vp, vp, ctypes.c_float, vp, vp, sz, vp, vp]),
             ("adamw_step", [tp, ctypes.c_int64, hp, vp]),
+            ("adamw_step_unbiased", [tp, ctypes.c_int64, hp, vp]),
             ("adamw_moments", [tp, ctypes.c_int64, vp, vp, vp]),
             ("layers_device_status", [vp, ctypes.POINTER(ctypes.c_int32)])):
         getattr(lib, "flarepp_" + name).restype = ctypes.c_int
@@ -996,18 +997,25 @@ class AdamW:
     list gives them (None where there is none); masters that ``state`` holds are used before any is
     made, and with ``masters=None`` too (False: none). state_bits: 32, or 8 (the moments in 8 bits with
     a scale for every ``STATE_BLOCK`` values: a quarter of the memory; include/flarepp.h says how).
+    state_rounding: of 8-bit states, "nearest", or "unbiased" (by a hash of place and step), without
+    which the second moment of a long run with a large beta2 stops following its average.
     state: the state to go on from, as ``state_dict`` returns it (its tensors are used, not
     copied). The optimiser works on the buffers that it was given, whose storage it keeps alive:
     a parameter or gradient that moves to another buffer needs a new optimiser (give it
     ``state_dict()``). ``lr`` and ``weight_decay`` are attributes that a schedule may change."""
 
     def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2,
-                 state_bits=32, masters=None, state=None):
+                 state_bits=32, masters=None, state=None, state_rounding="nearest"):
         params, grads = [p.detach() for p in params], [g.detach() for g in grads]
         if len(params) != len(grads):
             raise ValueError(f"{len(params)} parameters, {len(grads)} gradients")
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
+        if state_rounding not in ("nearest", "unbiased"):
+            raise ValueError("state_rounding must be 'nearest' or 'unbiased'")
+        if state_rounding == "unbiased" and state_bits != 8:
+            raise ValueError("only 8-bit states are rounded without bias")
+        self.state_rounding = state_rounding
         self.lr, self.betas, self.eps = lr, betas, eps
         self.weight_decay, self.state_bits = weight_decay, state_bits
         self.params, self.grads = params, grads
@@ -1072,8 +1080,8 @@ class AdamW:
             return
         h = AdamwHyper(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
                        self.steps + 1, self.state_bits)
-        _enqueue("adamw_step", self.device, stream, self._table, len(self.params),
-                 ctypes.byref(h))
+        _enqueue("adamw_step_unbiased" if self.state_rounding == "unbiased" else "adamw_step",
+                 self.device, stream, self._table, len(self.params), ctypes.byref(h))
         self.steps += 1
 
     def moments(self, m_out=None, v_out=None, stream=None):

@@ -1,6 +1,9 @@
 """More host-side checks of the linear layer, the embedding and AdamW. Nothing here launches a kernel, so
 these tests run without a GPU; the addresses are never dereferenced."""
-from test_layers_abi import INVALID, at, bwd, emb_bwd, emb_fwd, emb_shape, fwd, lib, linear_shape  # noqa: F401
+import ctypes
+
+from paper_2608_11519_gb300 import flarepp
+from test_layers_abi import INVALID, at, bwd, emb_bwd, emb_fwd, emb_shape, fwd, lib, linear_shape, tensor  # noqa: F401
 
 
 def test_status_words_off_four_bytes_are_refused(lib):  # noqa: F811
@@ -15,3 +18,17 @@ def test_status_words_off_four_bytes_are_refused(lib):  # noqa: F811
 
 def test_status_question_wants_an_answer_s_place(lib):  # noqa: F811
     assert lib.flarepp_layers_device_status(None, None) == INVALID
+
+
+def test_only_8_bit_states_are_rounded_without_bias(lib):  # noqa: F811
+    table = (flarepp.AdamwTensor * 1)(tensor())
+
+    def step(n, bits, **over):
+        h = flarepp.AdamwHyper(1e-3, 0.9, 0.999, 1e-8, 0.0, over.get("step", 1), bits)
+        return lib.flarepp_adamw_step_unbiased(table, n, ctypes.byref(h), None)
+
+    assert step(0, 8) == flarepp.OK
+    assert step(0, 32) == step(0, 16) == step(0, 8, step=0) == INVALID
+    table[0] = tensor(m_scale=0)
+    assert step(1, 8) == INVALID
+    assert lib.flarepp_adamw_step_unbiased(table, 0, None, None) == INVALID
