@@ -506,9 +506,9 @@ typedef struct {
  * sqrt(v) as unsigned 8-bit floats with 4 exponent and 4 mantissa bits (code c stands for c / 16
  * below 16 and for (1 + (c % 16) / 16) 2^(c / 16 - 1) from there on) times max sqrt(v) / 2^14, both
  * rounded to nearest (over many steps sqrt(v) then does not follow its average, see
- * flarepp_adamw_step_unbiased); a v that is not zero never becomes zero, and a block whose largest value is
- * below 2^-100 is stored as zeros with scale 0. A gradient that is not finite spoils its value (8-bit
- * states: the block of 256).
+ * flarepp_adamw_step_unbiased); a v that is not zero never becomes zero, and a block whose largest
+ * value is below 2^-100 is stored as zeros with scale 0. A gradient that is not finite spoils its
+ * value (8-bit states: the block of 256).
  * `tensors` and `hyper` are host memory, read before the call returns; the hyperparameters are
  * part of the launch (a captured graph replays them). n_tensors = 0 is a no-op.
  */
