@@ -100,9 +100,10 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t minus_u) {
 }
 // The normal distribution function as 1 / (1 + 2^-u), u(z) = log2(Phi(z) / Phi(-z)): odd and smooth,
 // so an odd polynomial of degree 13 does, fitted for the least largest error of z Phi(z) over
-// |z| <= 5 (2.2e-7; 3.3e-7 with float32 arithmetic; beyond 5 it grows faster than u, and z Phi(z)
-// is below 1.5e-6 from its limits). Both tails keep relative precision (2e-3 at z = -5, half a unit of
-// the bf16 result), and it takes about 8 issue slots a value in pairs, where the epilogue of a
+// |z| <= 5 (2.3e-7; 5e-7 with float32 arithmetic; beyond 5 it grows faster than u, and z Phi(z)
+// is below 1.5e-6 from its limits). Down to z = -5 Phi keeps a relative precision of 2.2e-3 (half a unit of
+// the bf16 result); below that only an absolute one: z Phi(z) is off by 1.8e-8 at most, which is 4 % of it at
+// -5.25 and all of it from -6.5 on. It takes about 8 issue slots a value in pairs, where the epilogue of a
 // memory-bound layer has about 16 for everything.
 __device__ __forceinline__ uint64_t normal_cdf2(uint64_t z) {
     const uint64_t s = mul2(z, z);
