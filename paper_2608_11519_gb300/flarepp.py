@@ -772,6 +772,8 @@ def _current(stream, device):
         handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
         stream = (torch.cuda.ExternalStream(handle, device) if handle
                   else torch.cuda.default_stream(device))
+    if stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, the call's tensors on {device}")
     return torch.cuda.stream(stream)
 
 

@@ -1,6 +1,10 @@
 """More host-side checks of the linear layer, the embedding and AdamW. Nothing here launches a kernel, so
 these tests run without a GPU; the addresses are never dereferenced."""
 import ctypes
+from unittest import mock
+
+import pytest
+import torch
 
 from paper_2608_11519_gb300 import flarepp
 from test_layers_abi import INVALID, at, bwd, emb_bwd, emb_fwd, emb_shape, fwd, lib, linear_shape, tensor  # noqa: F401
@@ -32,3 +36,10 @@ def test_only_8_bit_states_are_rounded_without_bias(lib):  # noqa: F811
     table[0] = tensor(m_scale=0)
     assert step(1, 8) == INVALID
     assert lib.flarepp_adamw_step_unbiased(table, 0, None, None) == INVALID
+
+
+def test_a_stream_of_another_device_is_refused():
+    """The call would run on the current stream of its tensors' device, in no order with the given one."""
+    stream = mock.Mock(spec=torch.cuda.Stream, device=torch.device("cuda", 1), cuda_stream=16)
+    with pytest.raises(ValueError):
+        flarepp._current(stream, torch.device("cuda", 0))
