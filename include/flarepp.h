@@ -473,8 +473,9 @@ FLAREPP_API flarepp_status flarepp_embedding_bwd(const flarepp_embedding_shape* 
  * the float32 weights that a bf16 param is a rounded copy of. m, v: the moments; with 32-bit
  * states float32 [n] (m_scale, v_scale NULL); with 8-bit states one byte per value and one
  * float32 scale per block of 256 values (the last block may be shorter), [ceil(n / 256)].
- * Every pointer 16-byte aligned but the scales' (4 bytes); no two buffers that a step writes may
- * overlap.
+ * Every pointer 16-byte aligned but the scales' (4 bytes); no buffer that a step writes may overlap
+ * another one of the step's. A call checks that for each tensor by itself; that no two tensors share
+ * what is written is the caller's to see to, once for all steps.
  */
 typedef struct {
     void* param;

@@ -987,6 +987,19 @@ def embedding_bwd(ids, dY, V, scale=1.0, dtable=None, workspace=None, status=Non
     return dtable
 
 
+def _check_apart(spans):
+    """Refuse spans (begin, end, whether it is written, name) of which one that is written overlaps
+    another."""
+    most, written = (0, None), (0, None)  # the largest ends so far, of all and of those written
+    for begin, end, writes, name in sorted(x for x in spans if x[0] < x[1]):
+        other = most if writes else written
+        if begin < other[0]:
+            raise FlareppError(ERR_INVALID_ARGUMENT, f"AdamW: {name} overlaps {other[1]}")
+        most = max(most, (end, name), key=lambda x: x[0])
+        if writes:
+            written = max(written, (end, name), key=lambda x: x[0])
+
+
 class AdamW:
     """AdamW over fixed buffers: parameters, their gradients, and the state it keeps.
 
@@ -1004,7 +1017,7 @@ class AdamW:
     state: the state to go on from, as ``state_dict`` returns it (its tensors are used, not
     copied). The optimiser works on the buffers that it was given, whose storage it keeps alive:
     a parameter or gradient that moves to another buffer needs a new optimiser (give it
-    ``state_dict()``). ``lr`` and ``weight_decay`` are attributes that a schedule may change."""
+    ``state_dict()``); no two buffers of which one is written may overlap. ``lr`` and ``weight_decay`` are attributes that a schedule may change."""
 
     def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2,
                  state_bits=32, masters=None, state=None, state_rounding="nearest"):
@@ -1043,6 +1056,11 @@ class AdamW:
             raise ValueError("the lists of tensors differ in length")
         for i, p in enumerate(params):
             self._fill(i, p)
+        _check_apart([(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), ts is not grads,
+                       f"{name}[{i}]")
+                      for name, ts in zip(("params", "grads", "masters", "m", "v", "m_scale", "v_scale"),
+                                          (params, *lists))
+                      for i, t in enumerate(ts) if t is not None])
 
     def _zero_state(self):
         def zeros(n, dtype):

@@ -43,3 +43,17 @@ def test_a_stream_of_another_device_is_refused():
     stream = mock.Mock(spec=torch.cuda.Stream, device=torch.device("cuda", 1), cuda_stream=16)
     with pytest.raises(ValueError):
         flarepp._current(stream, torch.device("cuda", 0))
+
+
+def test_buffers_that_a_step_writes_lie_apart():
+    apart = flarepp._check_apart
+    apart([])
+    apart([(0, 16, True, "a"), (16, 32, True, "b"), (40, 44, False, "c"), (40, 60, False, "d")])
+    apart([(8, 8, True, "empty"), (0, 16, True, "a")])
+    for bad in ([(0, 16, True, "a"), (0, 16, True, "b")],                              # the same twice
+                [(8, 20, False, "b"), (0, 16, True, "a")],                             # read where written
+                [(0, 100, False, "a"), (10, 20, False, "b"), (30, 40, True, "c")],     # inside another
+                [(0, 100, True, "a"), (10, 20, False, "b"), (30, 40, False, "c")]):
+        with pytest.raises(flarepp.FlareppError) as e:
+            apart(bad)
+        assert e.value.status == INVALID
