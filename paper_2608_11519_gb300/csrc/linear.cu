@@ -17,14 +17,15 @@ constexpr int kDzThreads = 256;  // also of the blocks that copy lines
 
 // Up to four rows the layer can run on the CUDA cores (gemv_kernel): a weight then meets so few
 // multiplications that its bytes are the bound, and one launch without tensor maps is the shortest
-// path. That ends where rows x weights pass about 12 M: 2 rows of 4096 -> 1001 take 4.4 us here and 5.6 in
-// lin_few, 4 rows 7.2 and 5.6, 2 rows of 4096 -> 4096 11.2 and 7.8. One row is always faster here.
+// path. That ends where rows x weights pass about 12 M (with weights from memory, in a graph): 2 rows of
+// 4096 -> 1001 take 4.6 us here and 6.0 in lin_few, 4 rows 7.8 and 6.1; 2 rows of 4096 -> 4096, beyond it, 9.5
+// and 10.1. One row is always faster here (4096 -> 4096: 8.2 and 10.1).
 constexpr int64_t kGemvRows = 4;
 bool use_gemv(int64_t T, int64_t K, int64_t N) {
     return K % 8 == 0 && (T == 1 || (T <= kGemvRows && T * K * N <= 12000000));
 }
-// Rows up to which lin_few is faster than tiles of 256 rows: 200 rows of 4096 -> 4096 take 13.2 us in
-// lin_few and 22 in tiles, 200 rows of 256 -> 512 10.5 and 9.0 (a short contraction leaves lin_few's CTAs
+// Rows up to which lin_few is faster than tiles of 256 rows: 200 rows of 4096 -> 4096 take 14.4 us in
+// lin_few and 19.5 in tiles, 200 rows of 256 -> 512 8.7 and 6.5 (a short contraction leaves lin_few's CTAs
 // mostly with their epilogues).
 bool use_few(int64_t T, int64_t depth) { return T <= (depth >= 1024 ? kFewRows : kFewRows / 2); }
 constexpr int kGemvWarps = 8;
@@ -35,8 +36,8 @@ constexpr int64_t kPadWRows = 4096;
 // a TMA box is one line and not parts of two.
 int64_t pitch_of(int64_t n) { return cdiv(n, 64) * 64; }
 // What TMA cannot address is laid out anew; so is W where its lines are not whole 128-byte lines and
-// 16 or more row tiles read it (20,011 rows of 1000 -> 1544: 72 us as it lies, 61 with the copy, which is 3 of
-// them; the lines of X, read as often as written, are not worth one).
+// 16 or more row tiles read it (20,011 rows of 1000 -> 1544: 65 us as it lies, 60 with the copy; the
+// lines of X, read as often as written, are not worth one).
 bool pad_x(int64_t K) { return K % 8 != 0; }
 bool pad_w(int64_t K, int64_t T) { return K % 8 != 0 || (K % 64 != 0 && T >= kPadWRows); }
 

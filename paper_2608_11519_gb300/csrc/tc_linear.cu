@@ -20,15 +20,16 @@
 // status word, every role leaves its loops, the producer waits for its copies in flight, the issuer for
 // its products, and TMEM is freed.
 //
-// What bounds it: long contractions the tensor cores (16384 x 4096 x 4096: 280 us cold, 1965 TFLOP/s; 317 us
-// once the power limit holds the clock); wide outputs of short contractions the writes, which HBM
-// takes at 4.0 TB/s where nothing is read (measured with fills) and at up to 2.4 beside twice as many reads. With
-// GELU or SiLU a pair of outputs takes 24 cycles of the special-function unit and 22 of the multiply-add
-// pipe per scheduler, about what the writes leave, and a group waits for its accumulator's next products after
-// that: 65,536 x 256 -> 512 takes 23.6 us without an activation and 32.0 with GELU. Measured and left: sixteen
-// warps on every tile (36 us: a tile's fixed latencies are then in every warp's way), 16-column halves with the
-// next loads ahead (38 us: too few independent chains), eight warps of 64 columns and unpaired arithmetic
-// (46 us), more registers for the epilogue by setmaxnreg (spills).
+// What bounds it: long contractions the tensor cores (16384 x 4096 x 4096: 317 us, 1732 TFLOP/s, after a pause
+// of 50 ms; 323 one after another, the clock then held at 1.5 GHz by the power limit); wide outputs of short
+// contractions the writes, which HBM takes at 4.0 TB/s where nothing is read (measured with fills) and at up to
+// 2.4 beside twice as many reads. GELU takes 24 cycles of the special-function unit and 20 of the multiply-add
+// pipe (22 with the bias) per pair of outputs and scheduler, about what the writes leave, and a group waits for
+// its accumulator's next products after that: 65,536 x 256 -> 512 takes 23.0 us without an activation, 28.1 with
+// SiLU and 31.3 with GELU. Measured and left: sixteen warps on every tile (36 us: a tile's fixed latencies are
+// then in every warp's way), 16-column halves with the next loads ahead (38 us: too few independent chains),
+// eight warps of 64 columns and unpaired arithmetic (46 us), more registers for the epilogue by setmaxnreg
+// (spills).
 #include <type_traits>
 
 #include "tc_linear_common.cuh"

@@ -718,6 +718,8 @@ def flare_fwd_host(Q, K, V, scale=None, Y_host=None, device="cuda", workspace=No
 
 
 # ---------------------------------------------------------------- layers around the mixer
+# As the chain's entry points, these record no autograd graph: what they return requires no gradient,
+# whatever their inputs do, and linear_bwd and embedding_bwd write gradients (they add to nothing).
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 STATE_BLOCK = 256  # values that share one scale in an 8-bit optimiser state
 
