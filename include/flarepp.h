@@ -361,8 +361,8 @@ FLAREPP_API flarepp_status flarepp_route_device_status(const flarepp_shape* shap
  *   wait_ns: the bound of every wait of that launch (0: the default of 2 s).
  * Process-wide state, for tests only: it applies to every later call from any thread until it
  * is turned off. A launch whose wait ran out stops early and records FLAREPP_ERR_TIMEOUT in
- * the device status word (flarepp_route_device_status; the linear layer: its `status`); its outputs
- * are invalid.
+ * the device status word (flarepp_route_device_status; the linear layer: its `status`, or the word
+ * that flarepp_layers_device_status reads); its outputs are invalid.
  */
 FLAREPP_API void flarepp_test_wait_fault(int kernel, int64_t ring_item, uint64_t wait_ns);
 
