@@ -354,7 +354,8 @@ FLAREPP_API flarepp_status flarepp_route_device_status(const flarepp_shape* shap
  *     3, the decode; 4 + p, pass p of flarepp_route_bwd's tensor-core passes (0: the route
  *     pass of call 3, 1: of call 2, 2: of call 1, 3: the token pass of calls 2 and 3, 4: of
  *     call 1, 5: the merged token pass of calls 2 and 3); 16, the tiled products of the linear
- *     layer; 17, its product for few rows; 18, its fused dZ and dX; 0 turns the hook off (the default).
+ *     layer; 17, its product for few rows; 18, its fused dZ and dX; 19, the walks of the decay
+ *     attention; 0 turns the hook off (the default).
  *   ring_item: the index, in the order it is loaded, of an item of CTA 0's ring of K/V (or
  *     Q/Z) tiles that the kernel's load warp then never loads, so that the waits for it run
  *     out (-1: none).
@@ -377,7 +378,8 @@ FLAREPP_API void flarepp_test_wait_fault(int kernel, int64_t ring_item, uint64_t
  * (4-byte aligned) that the kernels set (and never clear) when something went wrong that only they
  * can see (without one they set a word of the library's, see flarepp_layers_device_status):
  * FLAREPP_ERR_TIMEOUT for a bounded wait that gave up (the outputs are then invalid),
- * FLAREPP_ERR_INVALID_ARGUMENT for an embedding id beyond the table.
+ * FLAREPP_ERR_INVALID_ARGUMENT for an embedding id beyond the table (below: for an offset, a length or
+ * a decay out of its range).
  * ------------------------------------------------------------------------------------------ */
 typedef enum {
     FLAREPP_ACT_NONE = 0,
@@ -544,10 +546,170 @@ FLAREPP_API flarepp_status flarepp_adamw_moments(const flarepp_adamw_tensor* ten
                                                  int64_t n_tensors, float* const* m_out,
                                                  float* const* v_out, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * A causal block: linear attention with a decay for each head (a token mixer that, unlike the routing
+ * chain, knows the tokens' order and gives one token at a time), rotary positions, and group norm.
+ *
+ * The conventions above hold, and `status` is that of the layers; but tensors of heads are given by strides.
+ * ------------------------------------------------------------------------------------------ */
+
 /*
- * What the kernels of the linear layer and the embedding recorded on the current device, since this
- * was last asked there, for calls that passed status = NULL: FLAREPP_OK, FLAREPP_ERR_TIMEOUT (some call's
- * outputs are invalid) or FLAREPP_ERR_INVALID_ARGUMENT (some id was beyond its table). The words are
+ * A tensor [B, H, N, D] whose D values lie side by side: the distances, in values, of two batch
+ * elements, heads and tokens. [B, N, H, D] buffers and parts of a larger one ([B, N, 3, H, D]) are such
+ * tensors too. Strides are not negative; an input's may be 0 (one head for all); no two values of an output
+ * may be the same place. The stride of a dimension of size 1 does not matter to what is computed.
+ */
+typedef struct {
+    void* data;
+    int64_t stride_b, stride_h, stride_n;
+} flarepp_heads;
+
+typedef struct {
+    int64_t B, Hq, Hk, N; /* Hq query heads share Hk key and value heads, Hq / Hk neighbours each */
+    int64_t Dk, Dv;       /* channels of queries and keys, of values: multiples of 8 from 8 to 128 */
+    int64_t sequences;    /* 0: B sequences of N tokens; else (B = 1) that many in N packed tokens */
+    int32_t dtype;        /* FLAREPP_BF16 (FLAREPP_F32: FLAREPP_ERR_UNSUPPORTED) */
+    float scale;
+} flarepp_decay_shape;
+
+/*
+ * Linear attention with a decay g = exp(log_decay[h]) for each query head: over the tokens t of a
+ * sequence, from the state S_0 [Dk, Dv] (`state`, or zeros),
+ *     S_t = g S_(t-1) + k_t v_t^T,     y_t = scale * q_t S_t.
+ *   Q [B, Hq, N, Dk]; K [B, Hk, N, Dk]; V [B, Hk, N, Dv]; Y [B, Hq, N, Dv], bf16, addresses and strides
+ *     multiples of 16 bytes.
+ *   log_decay [Hq] float32, at most 0 (-inf: no memory of earlier tokens); one above 0 counts as 0 and a
+ *     NaN as -inf, and both set `status`.
+ *   offsets: with packed sequences, int32 [sequences + 1]: sequence i is the tokens offsets[i] to
+ *     offsets[i + 1] (it may be empty). Tokens before the first and behind the last sequence are not read,
+ *     and their outputs are 0. Offsets that fall or leave 0 to N are brought back to what came before them
+ *     and into that range, and set `status` (FLAREPP_ERR_INVALID_ARGUMENT). Without packing: NULL.
+ *   state, state_out: NULL or float32 [sequences or B, Hq, Dk, Dv], dense: S_0 and the state behind the
+ *     last token, which continues the sequence in another call or in flarepp_decay_attention_step (an empty
+ *     sequence's is its S_0). They may be the same buffer.
+ * The products' operands are bf16 (scores with their decay, states and decayed values are rounded to it),
+ * sums and states are float32. The sums run in a fixed order: two calls on the same inputs give the same bits.
+ *   workspace: at least flarepp_decay_attention_workspace_bytes(shape) bytes, 256-byte aligned.
+ *   Y, state_out and the workspace must not overlap each other or an input (but state_out the state).
+ */
+FLAREPP_API size_t flarepp_decay_attention_workspace_bytes(const flarepp_decay_shape* shape);
+FLAREPP_API flarepp_status flarepp_decay_attention_fwd(
+    const flarepp_decay_shape* shape, const flarepp_heads* Q, const flarepp_heads* K,
+    const flarepp_heads* V, const float* log_decay, const int32_t* offsets, const float* state,
+    const flarepp_heads* Y, float* state_out, void* workspace, size_t workspace_bytes, int32_t* status,
+    void* stream);
+
+/*
+ * The gradients of flarepp_decay_attention_fwd for dY [B, Hq, N, Dv] and, when it is not NULL, dstate_out
+ * (of state_out): with G_N = dstate_out + scale q_N dY_N^T and G_t = g G_(t+1) + scale q_t dY_t^T,
+ *     dq_t = scale S_t dY_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,  dstate = g G_1,
+ * written, not accumulated; dK and dV are summed over the query heads that share them (in float32, in
+ * order). log_decay is a constant of the model: it gets no gradient.
+ *   state: as in the forward. dQ, dK, dV: as Q, K, V; dstate: NULL or as state.
+ *   workspace: at least flarepp_decay_attention_bwd_workspace_bytes(shape) bytes, 256-byte aligned.
+ */
+FLAREPP_API size_t flarepp_decay_attention_bwd_workspace_bytes(const flarepp_decay_shape* shape);
+FLAREPP_API flarepp_status flarepp_decay_attention_bwd(
+    const flarepp_decay_shape* shape, const flarepp_heads* Q, const flarepp_heads* K,
+    const flarepp_heads* V, const float* log_decay, const int32_t* offsets, const float* state,
+    const flarepp_heads* dY, const float* dstate_out, const flarepp_heads* dQ, const flarepp_heads* dK,
+    const flarepp_heads* dV, float* dstate, void* workspace, size_t workspace_bytes, int32_t* status,
+    void* stream);
+
+/*
+ * One more token for each of B sequences (shape with N = 1 and sequences = 0): state [B, Hq, Dk, Dv],
+ * float32, becomes g state + k v^T in place, and Y = scale * q state. Everything is computed in float32.
+ * One launch, no workspace.
+ */
+FLAREPP_API flarepp_status flarepp_decay_attention_step(
+    const flarepp_decay_shape* shape, const flarepp_heads* Q, const flarepp_heads* K,
+    const flarepp_heads* V, const float* log_decay, float* state, const flarepp_heads* Y, int32_t* status,
+    void* stream);
+
+#define FLAREPP_ROTARY_AXES 4
+typedef enum {
+    FLAREPP_ROTARY_HALVES = 0,     /* pair p: channels p and p + P, of P pairs */
+    FLAREPP_ROTARY_ADJACENT = 1,   /* channels 2 p and 2 p + 1 */
+    FLAREPP_ROTARY_AXES_APART = 2  /* halves within each axis's own channels: axis a with n pairs behind
+                                      s earlier ones has channels 2 s to 2 (s + n), pairs 2 s + i and
+                                      2 s + n + i */
+} flarepp_rotary_pairing;
+
+typedef struct {
+    int64_t B, Hq, Hk, N, D;   /* D from 1 to 1024 */
+    int32_t dtype;             /* flarepp_dtype of q, k and the outputs */
+    int32_t axes;              /* 1 to FLAREPP_ROTARY_AXES */
+    int32_t sections[FLAREPP_ROTARY_AXES]; /* pairs that turn with each axis, in order; 2 P <= D */
+    int32_t pairing;           /* flarepp_rotary_pairing */
+    int32_t real_positions;    /* positions are float32 (coordinates), else int32 */
+    int32_t inverse;           /* turn back: the gradient, or the inverse */
+    int64_t pos_stride_b;      /* values from one batch element's positions to the next's; 0: shared */
+} flarepp_rotary_shape;
+
+/*
+ * Rotary positions: each of the P pairs of channels (x, y) of a token of q and k is turned by the angle
+ * a = position[axis of the pair] * freqs[pair],
+ *     x' = x cos a - y sin a,  y' = y cos a + x sin a;
+ * channels from 2 P on are copied. Angles are exact to some 2^-22 rad however far the positions; products in
+ * float32, rounded once.
+ *   q [B, Hq, N, D], k [B, Hk, N, D], outputs the same: any addresses and strides (16-byte ones are
+ *     fast). Hq or Hk may be 0 (that tensor and its output may then be NULL). An output may be its own
+ *     input (the same address and strides); otherwise outputs overlap nothing.
+ *   positions [B, N, axes], tokens dense; freqs float32 [P].
+ * Errors: as above. Several launches never share anything: no workspace.
+ */
+FLAREPP_API flarepp_status flarepp_rotary(const flarepp_rotary_shape* shape, const void* positions,
+                                          const float* freqs, const flarepp_heads* q,
+                                          const flarepp_heads* k, const flarepp_heads* q_out,
+                                          const flarepp_heads* k_out, void* stream);
+
+typedef struct {
+    int64_t B, N, C; /* samples, rows (positions) of each, channels (up to 2^20) */
+    int64_t G;       /* groups of C / G channels side by side */
+    int32_t dtype;       /* flarepp_dtype of X, Y, dX, dY */
+    int32_t param_dtype; /* flarepp_dtype of gamma, beta and their gradients */
+    int32_t act;         /* flarepp_activation */
+    float eps;           /* above 0 */
+} flarepp_norm_shape;
+
+/*
+ * Group norm with an activation, channels last, X [B, N, C]: over each sample's N rows and each group's
+ * C / G channels, mean and 1 / sqrt(variance + eps) (the variance without Bessel's correction), then
+ *     Y = act(gamma (X - mean) rstd + beta).
+ * N = 1 normalises every token by itself (the heads of an attention's output, G = 1: layer norm).
+ *   gamma, beta [C], each or both NULL (1 and 0).
+ *   lengths: NULL, or int32 [B]: only the first lengths[b] rows of sample b count; the others are not read,
+ *     and are 0 in Y. A length outside 0 to N is brought into it and sets `status`.
+ *   stats: NULL, or float32 [B, 2, G]: the means and the rstds, which flarepp_group_norm_bwd takes.
+ *   workspace: at least flarepp_group_norm_workspace_bytes(shape) bytes, 256-byte aligned.
+ *   Outputs and workspace must not overlap each other or an input.
+ * Statistics are float32 sums of squares about the mean, in a fixed order.
+ */
+FLAREPP_API size_t flarepp_group_norm_workspace_bytes(const flarepp_norm_shape* shape);
+FLAREPP_API flarepp_status flarepp_group_norm_fwd(const flarepp_norm_shape* shape, const void* X,
+                                                  const void* gamma, const void* beta,
+                                                  const int32_t* lengths, void* Y, float* stats,
+                                                  void* workspace, size_t workspace_bytes,
+                                                  int32_t* status, void* stream);
+
+/*
+ * The gradients of flarepp_group_norm_fwd for dY [B, N, C], written, not accumulated: dX (0 in rows that
+ * do not count), dgamma and dbeta [C] (param_dtype; each may be NULL), summed in float32 in a fixed order.
+ * gamma, beta, lengths, stats: the forward's.
+ */
+FLAREPP_API size_t flarepp_group_norm_bwd_workspace_bytes(const flarepp_norm_shape* shape);
+FLAREPP_API flarepp_status flarepp_group_norm_bwd(const flarepp_norm_shape* shape, const void* X,
+                                                  const void* dY, const void* gamma, const void* beta,
+                                                  const int32_t* lengths, const float* stats, void* dX,
+                                                  void* dgamma, void* dbeta, void* workspace,
+                                                  size_t workspace_bytes, int32_t* status,
+                                                  void* stream);
+
+/*
+ * What the kernels of the linear layer, the embedding, the decay attention and the group norm recorded
+ * on the current device, since this was last asked there, for calls that passed status = NULL: FLAREPP_OK, FLAREPP_ERR_TIMEOUT (some call's
+ * outputs are invalid) or FLAREPP_ERR_INVALID_ARGUMENT (some id was beyond its table, some offset, length
+ * or decay out of its range). The words are
  * the library's, one set per device for all streams and threads. Waits for the work on `stream` (not
  * for other streams'), writes the answer to *status_out (host memory) and clears the words. Not while
  * `stream` is being captured.

@@ -35,5 +35,8 @@ cudaError_t take_product_status(int32_t* out, cudaStream_t st);    // tc_linear.
 cudaError_t take_few_status(int32_t* out, cudaStream_t st);        // tc_linear_few.cu
 cudaError_t take_fused_status(int32_t* out, cudaStream_t st);      // tc_linear_fused.cu
 cudaError_t take_embedding_status(int32_t* out, cudaStream_t st);  // embedding.cu
+cudaError_t take_decay_status(int32_t* out, cudaStream_t st);      // tc_decay.cu
+cudaError_t take_decay_step_status(int32_t* out, cudaStream_t st); // decay_step.cu
+cudaError_t take_norm_status(int32_t* out, cudaStream_t st);       // norm.cu
 
 }  // namespace flarepp

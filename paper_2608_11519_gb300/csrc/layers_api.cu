@@ -6,12 +6,15 @@ extern "C" flarepp_status flarepp_layers_device_status(void* stream, int32_t* st
     using namespace flarepp;
     if (!status_out) return FLAREPP_ERR_INVALID_ARGUMENT;
     *status_out = FLAREPP_OK;
-    cudaError_t (*const take[])(int32_t*, cudaStream_t) = {take_embedding_status, take_product_status,
-                                                           take_few_status, take_fused_status};
-    for (auto* from : take) {  // a wait that gave up counts for more than an id beyond the table
+    cudaError_t (*const take[])(int32_t*, cudaStream_t) = {take_embedding_status, take_norm_status,
+                                                           take_decay_step_status, take_decay_status,
+                                                           take_product_status, take_few_status,
+                                                           take_fused_status};
+    for (auto* from : take) {  // a wait that gave up counts for more than a wrong id, offset or length
         int32_t word = FLAREPP_OK;
         if (from(&word, (cudaStream_t)stream) != cudaSuccess) return FLAREPP_ERR_CUDA;
-        if (word != FLAREPP_OK) *status_out = word;
+        if (word > *status_out) *status_out = word;
     }
     return FLAREPP_OK;
 }
+static_assert(FLAREPP_ERR_TIMEOUT > FLAREPP_ERR_INVALID_ARGUMENT, "the larger word counts");

@@ -23,7 +23,7 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int kBlockBytes = 32 * 32 * 2;  // what an epilogue warp stages at a time
 constexpr int kMaxSmem = 232448;
 // the launches' numbers for the test hook of the bounded waits (flarepp_test_wait_fault)
-enum LinKernel { kProductKernel = 16, kFewKernel = 17, kFusedKernel = 18 };
+enum LinKernel { kProductKernel = 16, kFewKernel = 17, kFusedKernel = 18, kDecayKernel = 19 };
 
 // The bound of every wait of a launch, where a wait that gave up is recorded (null: the library's word),
 // and (for tests) the ring item that CTA 0's producer never loads, or -1.

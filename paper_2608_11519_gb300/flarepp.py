@@ -37,7 +37,12 @@ EXPORTED = ("flarepp_route_workspace_bytes", "flarepp_route_fwd", "flarepp_route
             "flarepp_linear_bwd_workspace_bytes", "flarepp_linear_bwd",
             "flarepp_embedding_fwd", "flarepp_embedding_bwd_workspace_bytes",
             "flarepp_embedding_bwd", "flarepp_adamw_step", "flarepp_adamw_moments",
-            "flarepp_layers_device_status", "flarepp_adamw_step_unbiased")
+            "flarepp_layers_device_status", "flarepp_adamw_step_unbiased",
+            "flarepp_decay_attention_workspace_bytes", "flarepp_decay_attention_fwd",
+            "flarepp_decay_attention_bwd_workspace_bytes", "flarepp_decay_attention_bwd",
+            "flarepp_decay_attention_step", "flarepp_rotary",
+            "flarepp_group_norm_workspace_bytes", "flarepp_group_norm_fwd",
+            "flarepp_group_norm_bwd_workspace_bytes", "flarepp_group_norm_bwd")
 N_STAGE_EVENTS = 6
 STAGES = ("encode1", "combine1", "encode2", "combine2", "decode")
 
@@ -74,6 +79,38 @@ class AdamwHyper(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
                 ("step", ctypes.c_int64), ("state_bits", ctypes.c_int32)]
+
+
+class Heads(ctypes.Structure):
+    """Mirror of ``flarepp_heads`` in include/flarepp.h."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+
+
+class DecayShape(ctypes.Structure):
+    """Mirror of ``flarepp_decay_shape`` in include/flarepp.h."""
+    _fields_ = [("B", ctypes.c_int64), ("Hq", ctypes.c_int64), ("Hk", ctypes.c_int64),
+                ("N", ctypes.c_int64), ("Dk", ctypes.c_int64), ("Dv", ctypes.c_int64),
+                ("sequences", ctypes.c_int64), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+ROTARY_AXES = 4
+
+
+class RotaryShape(ctypes.Structure):
+    """Mirror of ``flarepp_rotary_shape`` in include/flarepp.h."""
+    _fields_ = [("B", ctypes.c_int64), ("Hq", ctypes.c_int64), ("Hk", ctypes.c_int64),
+                ("N", ctypes.c_int64), ("D", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("axes", ctypes.c_int32), ("sections", ctypes.c_int32 * ROTARY_AXES),
+                ("pairing", ctypes.c_int32), ("real_positions", ctypes.c_int32),
+                ("inverse", ctypes.c_int32), ("pos_stride_b", ctypes.c_int64)]
+
+
+class NormShape(ctypes.Structure):
+    """Mirror of ``flarepp_norm_shape`` in include/flarepp.h."""
+    _fields_ = [("B", ctypes.c_int64), ("N", ctypes.c_int64), ("C", ctypes.c_int64),
+                ("G", ctypes.c_int64), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
 class FlareppError(RuntimeError):
@@ -161,7 +198,20 @@ def load(path: str = None):
             ("embedding_bwd_workspace_bytes", [ep])):
         getattr(lib, "flarepp_" + name).restype = sz
         getattr(lib, "flarepp_" + name).argtypes = args
+    dp, rp = ctypes.POINTER(DecayShape), ctypes.POINTER(RotaryShape)
+    np_, hd = ctypes.POINTER(NormShape), ctypes.POINTER(Heads)
+    for name, shape in (("decay_attention", dp), ("group_norm", np_)):
+        for way in ("", "_bwd"):
+            fn = getattr(lib, f"flarepp_{name}{way}_workspace_bytes")
+            fn.restype, fn.argtypes = sz, [shape]
     for name, args in (
+            ("decay_attention_fwd", [dp, hd, hd, hd, vp, vp, vp, hd, vp, vp, sz, vp, vp]),
+            ("decay_attention_bwd",
+             [dp, hd, hd, hd, vp, vp, vp, hd, vp, hd, hd, hd, vp, vp, sz, vp, vp]),
+            ("decay_attention_step", [dp, hd, hd, hd, vp, vp, hd, vp, vp]),
+            ("rotary", [rp, vp, vp, hd, hd, hd, hd, vp]),
+            ("group_norm_fwd", [np_] + [vp] * 7 + [sz, vp, vp]),
+            ("group_norm_bwd", [np_] + [vp] * 10 + [sz, vp, vp]),
             ("linear_fwd", [lp] + [vp] * 7 + [sz, vp, vp]),
             ("linear_bwd", [lp] + [vp] * 8 + [sz, vp, vp]),
             ("embedding_fwd", [ep, vp, vp, ctypes.c_float, vp, vp, vp]),
@@ -814,9 +864,10 @@ def _status_word(status, device):
 
 
 def layers_status(device=None, stream=None) -> int:
-    """What the kernels of ``linear_*`` and ``embedding_*`` calls without ``status`` recorded on
-    ``device`` (default: torch's current one) since this was last asked: OK, ERR_TIMEOUT (a bounded
-    wait gave up: outputs are invalid) or ERR_INVALID_ARGUMENT (an id beyond the table). Waits for
+    """What the kernels of ``linear_*``, ``embedding_*``, ``decay_attention_*`` and ``group_norm_*``
+    calls without ``status`` recorded on ``device`` (default: torch's current one) since this was last
+    asked: OK, ERR_TIMEOUT (a bounded wait gave up: outputs are invalid) or ERR_INVALID_ARGUMENT (an id
+    beyond the table; an offset, length or decay out of its range). Waits for
     ``stream`` (default: torch's current one there)."""
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
     if dev.type != "cuda":
@@ -1134,3 +1185,307 @@ class AdamW:
         """The state to save and to go on from, masters among it; its tensors are the optimiser's own."""
         return {"m": self.m, "v": self.v, "m_scale": self.m_scale, "v_scale": self.v_scale,
                 "masters": self.masters, "step": self.steps}
+
+
+# ---------------------------------------------------------------- a causal block
+# Decay attention, rotary positions and group norm: no autograd graph here either, and gradients are
+# written. Tensors of heads are [B, H, N, D] views with any strides whose last dimension is dense, so
+# projections [B, N, H, D] are passed as X.transpose(1, 2).
+PAIRINGS = {"halves": 0, "adjacent": 1, "axes": 2}
+
+
+def _head_view(t, what, shape, dtype, device):
+    """The ``flarepp_heads`` of a tensor of this shape ([B, H, N, D], or [B, H, D] for one token)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a torch tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what} has dtype {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, expected {device}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{what}: the values of a head must lie side by side")
+    return Heads(t.data_ptr(), st[0], st[1], st[2] if len(st) == 4 else 0)
+
+
+def _head_sizes(Q, K, V, dims):
+    """(device, B, Hq, Hk, N, Dk, Dv) of queries, keys and values with ``dims`` dimensions."""
+    dev = _cuda_device(Q, "Q")
+    for t, what in ((K, "K"), (V, "V")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{what} must be a torch tensor")
+    if Q.dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {Q.dtype}; the decay attention takes bfloat16")
+    if not Q.dim() == K.dim() == V.dim() == dims:
+        raise ValueError(f"expected Q, K and V with {dims} dimensions, got {Q.dim()}, {K.dim()} and "
+                         f"{V.dim()}")
+    N = Q.shape[2] if dims == 4 else 1
+    return dev, Q.shape[0], Q.shape[1], K.shape[1], N, Q.shape[-1], V.shape[-1]
+
+
+def _blank_heads(like, D):
+    """A new tensor [B, H, N, D] with ``like``'s first three sizes and its order of memory."""
+    B, H, N = like.shape[:3]
+    if like.stride(1) < like.stride(2) and H > 1 and N > 1:
+        return torch.empty(B, N, H, D, dtype=like.dtype, device=like.device).transpose(1, 2)
+    return torch.empty(B, H, N, D, dtype=like.dtype, device=like.device)
+
+
+class _DecayCall:
+    """Shape, views and checked addresses that a whole-prompt call and its gradients share."""
+
+    def __init__(self, Q, K, V, log_decay, scale, state, offsets):
+        self.dev, B, Hq, Hk, N, Dk, Dv = _head_sizes(Q, K, V, 4)
+        dt = Q.dtype
+        self.q, self.k = (B, Hq, N, Dk), (B, Hk, N, Dk)
+        self.v, self.y = (B, Hk, N, Dv), (B, Hq, N, Dv)
+        self.views = [_head_view(t, w, s, dt, self.dev)
+                      for t, w, s in ((Q, "Q", self.q), (K, "K", self.k), (V, "V", self.v))]
+        sequences = 0
+        self.offsets = 0
+        if offsets is not None:
+            if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.numel() < 2:
+                raise ValueError("offsets must be an int32 tensor [sequences + 1] of one sequence or more")
+            if B != 1:
+                raise ValueError("packed sequences are a batch of 1")
+            sequences = offsets.numel() - 1
+            self.offsets = _need(offsets, "offsets", offsets.shape, torch.int32, self.dev)
+        self.states = (sequences or B, Hq, Dk, Dv)
+        if scale is None:
+            scale = 1.0 / math.sqrt(Dk)
+        self.shape = DecayShape(B, Hq, Hk, N, Dk, Dv, sequences, _DTYPES[dt], float(scale))
+        self.decay = _need(log_decay, "log_decay", (Hq,), torch.float32, self.dev)
+        self.state = self.state_of(state, "state")
+
+    def state_of(self, t, what):
+        return _need(t, what, self.states, torch.float32, self.dev, optional=True)
+
+
+def decay_attention_fwd(Q, K, V, log_decay, scale=None, state=None, offsets=None, need_state=False, Y=None,
+                        state_out=None, workspace=None, status=None, stream=None):
+    """Causal linear attention with a decay for each head: y_t = scale * q_t S_t with
+    S_t = exp(log_decay) S_(t-1) + k_t v_t^T, for Q [B, Hq, N, Dk], K [B, Hk, N, Dk], V [B, Hk, N, Dv]
+    (bf16; Hq / Hk neighbouring query heads share a key and value head; Dk and Dv multiples of 8 up to
+    128) and log_decay [Hq] (float32, at most 0). Returns (Y [B, Hq, N, Dv], the state behind the last
+    token, float32 [B, Hq, Dk, Dv], or None unless ``need_state`` or ``state_out``).
+
+    ``state``: the state in front of the first token. ``offsets``: int32 [sequences + 1] on the device,
+    for sequences packed along N (B = 1); states are then [sequences, Hq, Dk, Dv], and rows outside all
+    sequences are 0. ``scale`` defaults to 1 / sqrt(Dk). ``status`` as for :func:`linear_fwd`."""
+    if stream is not None:
+        with _current(stream, _cuda_device(Q, "Q")):
+            return decay_attention_fwd(Q, K, V, log_decay, scale, state, offsets, need_state, Y, state_out,
+                                       workspace, status)
+    c = _DecayCall(Q, K, V, log_decay, scale, state, offsets)
+    if Y is None:
+        Y = _blank_heads(Q, V.shape[-1])
+    if need_state and state_out is None:
+        state_out = torch.empty(c.states, dtype=torch.float32, device=c.dev)
+    y = _head_view(Y, "Y", c.y, Q.dtype, c.dev)
+    ref = ctypes.byref(c.shape)
+    buf, wsp, wsn = _scratch(workspace, _entry("decay_attention_workspace_bytes")(ref), c.dev)
+    _enqueue("decay_attention_fwd", c.dev, None, ref, *(ctypes.byref(v) for v in c.views), c.decay,
+             c.offsets, c.state, ctypes.byref(y), c.state_of(state_out, "state_out"), wsp, wsn,
+             _status_word(status, c.dev))
+    return Y, state_out
+
+
+def decay_attention_bwd(Q, K, V, log_decay, dY, scale=None, state=None, offsets=None, dstate_out=None,
+                        need_dstate=False, dQ=None, dK=None, dV=None, dstate=None, workspace=None,
+                        status=None, stream=None):
+    """(dQ, dK, dV, dstate): the gradients of :func:`decay_attention_fwd` (same ``scale``, ``state`` and
+    ``offsets``) for dY [B, Hq, N, Dv] and, where the state behind the last token was used,
+    ``dstate_out``. dstate, the gradient of ``state``, is None unless ``need_dstate`` or given.
+    log_decay is a constant of the model."""
+    if stream is not None:
+        with _current(stream, _cuda_device(Q, "Q")):
+            return decay_attention_bwd(Q, K, V, log_decay, dY, scale, state, offsets, dstate_out,
+                                       need_dstate, dQ, dK, dV, dstate, workspace, status)
+    c = _DecayCall(Q, K, V, log_decay, scale, state, offsets)
+    dQ = _blank_heads(Q, Q.shape[-1]) if dQ is None else dQ
+    dK = _blank_heads(K, K.shape[-1]) if dK is None else dK
+    dV = _blank_heads(V, V.shape[-1]) if dV is None else dV
+    if need_dstate and dstate is None:
+        dstate = torch.empty(c.states, dtype=torch.float32, device=c.dev)
+    views = [_head_view(t, w, s, Q.dtype, c.dev) for t, w, s in
+             ((dY, "dY", c.y), (dQ, "dQ", c.q), (dK, "dK", c.k), (dV, "dV", c.v))]
+    ref = ctypes.byref(c.shape)
+    buf, wsp, wsn = _scratch(workspace, _entry("decay_attention_bwd_workspace_bytes")(ref), c.dev)
+    _enqueue("decay_attention_bwd", c.dev, None, ref, *(ctypes.byref(v) for v in c.views), c.decay,
+             c.offsets, c.state, ctypes.byref(views[0]), c.state_of(dstate_out, "dstate_out"),
+             *(ctypes.byref(v) for v in views[1:]), c.state_of(dstate, "dstate"), wsp, wsn,
+             _status_word(status, c.dev))
+    return dQ, dK, dV, dstate
+
+
+def decay_attention_step(Q, K, V, log_decay, state, scale=None, Y=None, status=None, stream=None):
+    """One more token for each of B sequences: ``state`` [B, Hq, Dk, Dv] (float32) becomes
+    exp(log_decay) state + k v^T in place, and Y [B, Hq, Dv] = scale * q state is returned, for
+    Q [B, Hq, Dk], K [B, Hk, Dk], V [B, Hk, Dv] in bf16."""
+    if stream is not None:
+        with _current(stream, _cuda_device(Q, "Q")):
+            return decay_attention_step(Q, K, V, log_decay, state, scale, Y, status)
+    dev, B, Hq, Hk, _, Dk, Dv = _head_sizes(Q, K, V, 3)
+    dt = Q.dtype
+    if Y is None:
+        Y = torch.empty((B, Hq, Dv), dtype=dt, device=dev)
+    s = DecayShape(B, Hq, Hk, 1, Dk, Dv, 0, _DTYPES[dt],
+                   1.0 / math.sqrt(Dk) if scale is None else float(scale))
+    q, k = _head_view(Q, "Q", (B, Hq, Dk), dt, dev), _head_view(K, "K", (B, Hk, Dk), dt, dev)
+    v, y = _head_view(V, "V", (B, Hk, Dv), dt, dev), _head_view(Y, "Y", (B, Hq, Dv), dt, dev)
+    ref = ctypes.byref
+    _enqueue("decay_attention_step", dev, None, ref(s), ref(q), ref(k), ref(v),
+             _need(log_decay, "log_decay", (Hq,), torch.float32, dev),
+             _need(state, "state", (B, Hq, Dk, Dv), torch.float32, dev), ref(y),
+             _status_word(status, dev))
+    return Y
+
+
+def _rotary(q, k, positions, freqs, sections, pairing, q_out, k_out, inverse, stream):
+    code = PAIRINGS.get(pairing)
+    if code is None:
+        raise ValueError(f"pairing must be one of {tuple(PAIRINGS)}")
+    dev = _cuda_device(q, "the first tensor")
+    if stream is not None:
+        with _current(stream, dev):
+            return _rotary(q, k, positions, freqs, sections, pairing, q_out, k_out, inverse, None)
+    dt = _float_dtype(q, "the first tensor")
+    sections = [int(n) for n in sections]
+    if not 1 <= len(sections) <= ROTARY_AXES or min(sections) < 0:
+        raise ValueError(f"sections must be 1 to {ROTARY_AXES} numbers of pairs, one for each axis")
+    if q.dim() != 4 or (k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 4)):
+        raise ValueError("expected tensors [B, H, N, D]")
+    B, Hq, N, D = q.shape
+    A, P = len(sections), sum(sections)
+    if 2 * P > D:
+        raise ValueError(f"{P} pairs of channels do not fit into {D} channels")
+    if not isinstance(positions, torch.Tensor):
+        raise TypeError("positions must be a torch tensor")
+    if positions.dtype not in (torch.int32, torch.float32):
+        raise TypeError(f"positions have dtype {positions.dtype}, expected int32 or float32")
+    shared = positions.dim() == 2
+    pp = _need(positions, "positions", (N, A) if shared else (B, N, A), positions.dtype, dev)
+    s = RotaryShape(B, Hq, 0 if k is None else k.shape[1], N, D, _DTYPES[dt], A,
+                    (ctypes.c_int32 * ROTARY_AXES)(*sections), code,
+                    int(positions.dtype is torch.float32), int(inverse), 0 if shared else N * A)
+    fp = _need(freqs, "freqs", (P,), torch.float32, dev)
+    views = [_head_view(q, "q", q.shape, dt, dev)]
+    q_out = _blank_heads(q, D) if q_out is None else q_out
+    views.append(_head_view(q_out, "q_out", q.shape, dt, dev))
+    if k is not None:
+        views.append(_head_view(k, "k", (B, k.shape[1], N, D), dt, dev))
+        k_out = _blank_heads(k, D) if k_out is None else k_out
+        views.append(_head_view(k_out, "k_out", k.shape, dt, dev))
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    r = [ctypes.byref(v) for v in views] + [None, None]
+    _enqueue("rotary", dev, None, ctypes.byref(s), pp, fp, r[0], r[2], r[1], r[3])
+    return q_out, k_out
+
+
+def rotary_fwd(q, k, positions, freqs, sections, pairing="halves", q_out=None, k_out=None, stream=None):
+    """Rotary positions with several axes: (q', k') for q [B, Hq, N, D] and k [B, Hk, N, D] (or None),
+    float32 or bf16. Pair p of channels is turned by positions[..., axis of p] * freqs[p].
+
+    positions: [B, N, axes], or [N, axes] for the whole batch, int32 or float32 (coordinates). sections: how
+    many pairs turn with each axis, in order (their sum P is at most D / 2; channels from 2 P on stay as
+    they are); freqs: float32 [P], see :func:`rotary_frequencies`. pairing: "halves" (p, p + P),
+    "adjacent" (2 p, 2 p + 1) or "axes" (halves within each axis's own 2 n channels). The outputs may be
+    q and k themselves."""
+    return _rotary(q, k, positions, freqs, sections, pairing, q_out, k_out, False, stream)
+
+
+def rotary_bwd(dq, dk, positions, freqs, sections, pairing="halves", dq_out=None, dk_out=None, stream=None):
+    """The gradients of :func:`rotary_fwd` for those of its outputs: the same turns backwards (which
+    also undoes a forward). Positions get no gradient."""
+    return _rotary(dq, dk, positions, freqs, sections, pairing, dq_out, dk_out, True, stream)
+
+
+def rotary_frequencies(sections, base=10000.0, device="cuda"):
+    """float32 [sum of sections]: base^(-i / n) for pair i of an axis with n pairs."""
+    return torch.tensor([base ** (-i / n) for n in sections for i in range(n)], dtype=torch.float64,
+                        device="cpu").float().to(device)
+
+
+def _norm_shape(X, groups, gamma, beta, eps, act):
+    code = ACTIVATIONS.get(act)
+    if code is None:
+        raise ValueError(f"act must be one of {tuple(ACTIVATIONS)}")
+    dev, dt = _cuda_device(X, "X"), _float_dtype(X, "X")
+    if X.dim() != 3:
+        raise ValueError("expected X [B, N, C]")
+    if not X.is_contiguous():
+        raise ValueError("X must be contiguous")
+    B, N, C = X.shape
+    if groups < 1 or C % groups:
+        raise ValueError(f"{C} channels do not make {groups} groups")
+    if (gamma is None) != (beta is None):
+        raise ValueError("gamma and beta come together")
+    pt = dt if gamma is None else _float_dtype(gamma, "gamma")
+    gp = _need(gamma, "gamma", (C,), pt, dev, optional=True)
+    bp = _need(beta, "beta", (C,), pt, dev, optional=True)
+    return NormShape(B, N, C, groups, _DTYPES[dt], _DTYPES[pt], code, float(eps)), gp, bp, pt
+
+
+def _norm(X, groups, gamma, beta, eps, act, lengths, Y, stats, keep, workspace, status, stream):
+    dev = _cuda_device(X, "X")
+    if stream is not None:
+        with _current(stream, dev):
+            return _norm(X, groups, gamma, beta, eps, act, lengths, Y, stats, keep, workspace, status, None)
+    s, gp, bp, _ = _norm_shape(X, groups, gamma, beta, eps, act)
+    Y = torch.empty_like(X) if Y is None else Y
+    if keep and stats is None:
+        stats = torch.empty((s.B, 2, s.G), dtype=torch.float32, device=dev)
+    ref = ctypes.byref(s)
+    buf, wsp, wsn = _scratch(workspace, _entry("group_norm_workspace_bytes")(ref), dev)
+    _enqueue("group_norm_fwd", dev, None, ref, X.data_ptr(), gp, bp,
+             _need(lengths, "lengths", (s.B,), torch.int32, dev, optional=True),
+             _need(Y, "Y", X.shape, X.dtype, dev),
+             _need(stats, "stats", (s.B, 2, s.G), torch.float32, dev, optional=True), wsp, wsn,
+             _status_word(status, dev))
+    return Y, stats
+
+
+def group_norm_fwd(X, groups, gamma=None, beta=None, eps=1e-5, act="none", lengths=None, Y=None,
+                   workspace=None, status=None, stream=None):
+    """Y = act(gamma (X - mean) / sqrt(var + eps) + beta) for X [B, N, C] (float32 or bf16, channels
+    last), with mean and variance of each sample over its N rows and each of ``groups`` groups of
+    channels. gamma, beta: [C], float32 or bf16, both or neither. lengths: int32 [B], rows that count (the
+    others are 0 in Y). N = 1 normalises each token by itself, groups=1 then is a layer norm."""
+    return _norm(X, groups, gamma, beta, eps, act, lengths, Y, None, False, workspace, status, stream)[0]
+
+
+def group_norm_fwd_train(X, groups, gamma=None, beta=None, eps=1e-5, act="none", lengths=None, Y=None,
+                         stats=None, workspace=None, status=None, stream=None):
+    """``group_norm_fwd`` that also returns the statistics (float32 [B, 2, groups]: means, and
+    1 / deviations) which ``group_norm_bwd`` takes."""
+    return _norm(X, groups, gamma, beta, eps, act, lengths, Y, stats, True, workspace, status, stream)
+
+
+def group_norm_bwd(X, dY, stats, groups, gamma=None, beta=None, act="none", lengths=None, dX=None,
+                   dgamma=None, dbeta=None, workspace=None, status=None, stream=None):
+    """(dX, dgamma, dbeta), the gradients of ``group_norm_fwd_train`` for dY; the last two are None without
+    gamma and beta."""
+    dev = _cuda_device(X, "X")
+    if stream is not None:
+        with _current(stream, dev):
+            return group_norm_bwd(X, dY, stats, groups, gamma, beta, act, lengths, dX, dgamma, dbeta,
+                                  workspace, status)
+    s, gp, bp, pt = _norm_shape(X, groups, gamma, beta, 1.0, act)
+    dX = torch.empty_like(X) if dX is None else dX
+    if gamma is None and (dgamma is not None or dbeta is not None):
+        raise ValueError("dgamma and dbeta without gamma and beta")
+    if gamma is not None:
+        dgamma = torch.empty_like(gamma) if dgamma is None else dgamma
+        dbeta = torch.empty_like(beta) if dbeta is None else dbeta
+    ref = ctypes.byref(s)
+    buf, wsp, wsn = _scratch(workspace, _entry("group_norm_bwd_workspace_bytes")(ref), dev)
+    _enqueue("group_norm_bwd", dev, None, ref, X.data_ptr(), _need(dY, "dY", X.shape, X.dtype, dev), gp,
+             bp, _need(lengths, "lengths", (s.B,), torch.int32, dev, optional=True),
+             _need(stats, "stats", (s.B, 2, s.G), torch.float32, dev),
+             _need(dX, "dX", X.shape, X.dtype, dev),
+             _need(dgamma, "dgamma", (s.C,), pt, dev, optional=True),
+             _need(dbeta, "dbeta", (s.C,), pt, dev, optional=True), wsp, wsn, _status_word(status, dev))
+    return dX, dgamma, dbeta
