@@ -10,24 +10,26 @@
 // and sequences are fewer than the SMs, sequences are cut into pieces, whose states a first walk
 // (only A and V, only S) and a join over the pieces find.
 //
-// No power of g is ever above 1, whatever the decay: W below the diagonal blocks of 32 x 32 is the product
-// g^(i - last j of the block) g^(last j - j), both at most 1, and on them an exponential each. W o (X A^T),
-// S and w o V are rounded to bf16 as operands; sums, states and what r multiplies are float32.
+// No power of g passes float32, whatever the decay: in blocks of 32 x 32 W is the product
+// g^(i - last j of the block) g^(last j - j), a factor of the thread's and one of a table's, both at most 1
+// below the diagonal; on it the first is g^-31 at most, and a strong decay takes an exponential each there.
+// W o (X A^T), S and w o V are rounded to bf16 as operands; sums, states and what r multiplies are float32.
 //
-// Roles (10 warps): warp 0 loads tiles (A, X, V of each chunk, a ring of five), warp 1 issues the products,
-// warps 2 to 5 make W o (X A^T) and Y (a thread a row), warps 6 to 9 make w o V and keep the state. With
-// both widths up to 64 two blocks share an SM. Every wait is bounded.
+// Roles (24 warps, a block an SM): warp 0 loads tiles (A, X, V of each chunk, a ring), warps 1 and 2 issue the
+// products, warps 4 to 11 make W o (X A^T), warps 12 to 15 write Y, warps 16 to 19 keep the state, warps 20 to
+// 23 make w o V. A chunk passes through them like through a pipeline; the longest way round is
+// the state's (scale it, add to it). Every wait is bounded.
 #include "decay.h"
 #include "tc_linear_common.cuh"
 
 namespace flarepp {
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int kThreads = 768;
 constexpr int kChunk = kDecayChunk;
 constexpr int kAtomBytes = kChunk * 128;  // 128 tokens of 64 channels
-constexpr int kSlots = 5;
-constexpr int kPowers = 4 * 32 * 4;  // bytes of the warps' powers of g
+constexpr int kTable = 160;                // powers of g: gaps of -32 to 127
+constexpr int kPowers = 2 * kTable * 4;    // bytes of two such tables
 constexpr size_t kWsAlign = 256;
 
 // A piece of a sequence, as a block walks it.
@@ -45,7 +47,7 @@ struct Walk {
     int mx, ma, mv;       // whether a batch element has its own
     const Piece* pieces;  // packed sequences, else NULL
     const int* count;
-    int64_t n_pieces;
+    int n_pieces;
     int per_sequence, piece_rows;
     float scale_p, scale_w, scale_r;  // what scores, decayed values and X S are multiplied by
     int lead;                         // r_i = g^(i + lead), w_j = g^(n - lead - j)
@@ -64,26 +66,28 @@ struct Walk {
 template <int TK, int TV>
 struct Cfg {
     static constexpr int kSlot = (TK > TV ? TK : TV) * kChunk * 2;
+    // Values of up to 64 channels leave room for two sets of scores, of X S and of decayed values.
+    static constexpr int kSets = TV == 64 ? 2 : 1;
     static constexpr int kVw = TV * kChunk * 2;
     static constexpr int kSt = TK * TV * 2;
-    static constexpr bool kShared = TV == 64;  // X S lies over the scores' second half
-    static constexpr uint32_t kCtas = TK == 64 && TV == 64 ? 2 : 1;
-    static constexpr uint32_t kColY = 128;
-    static constexpr uint32_t kColX = kShared ? 64 : 128 + TV;
-    static constexpr uint32_t kColS = kShared ? 128 + TV : 128 + 2 * TV;
-    static constexpr uint32_t kTmem = kShared ? 256 : 512;
-    static constexpr int kBars = 2 * kSlots + 7;
-    static constexpr int kBody = kSlots * kSlot + kVw + kSt;
+    static constexpr uint32_t kColY = kSets * 128;  // from 0 on: scores, and W o scores as bf16 over them
+    static constexpr uint32_t kColX = kColY + TV;
+    static constexpr uint32_t kColS = kColX + kSets * TV;
+    static constexpr uint32_t kTmem = 512;
+    static constexpr int kRoom = kMaxSmem - 1024 - kPowers - kSets * kVw - kSt - 512;
+    static constexpr int kSlots = kRoom / kSlot < 12 ? kRoom / kSlot : 12;
+    static constexpr int kBars = 2 * kSlots + 15;
+    static constexpr int kBody = kSlots * kSlot + kSets * kVw + kSt;
     static constexpr int kSmem = 1024 + kBody + kPowers + kBars * 8 + 16;
-    static_assert(kSmem <= kMaxSmem, "shared memory");
+    static_assert(kSlots >= 5 && kBars * 8 + 16 <= 512 && kSmem <= kMaxSmem, "shared memory");
     static_assert(kColS + TV <= kTmem, "TMEM");
 };
 
-__device__ __forceinline__ Piece piece_of(const Walk& p, int64_t i) {
+__device__ __forceinline__ Piece piece_of(const Walk& p, int i) {
     if (p.pieces) return p.pieces[i];
     Piece x;
-    x.sequence = (int)(i / p.per_sequence);
-    const int k = (int)(i - (int64_t)x.sequence * p.per_sequence);
+    x.sequence = i / p.per_sequence;
+    const int k = i - x.sequence * p.per_sequence;
     x.start = k * p.piece_rows;
     x.rows = min(p.piece_rows, p.N - x.start);
     x.flags = (k == 0 ? kFirst : 0) | (k == p.per_sequence - 1 ? kLast : 0);
@@ -110,6 +114,26 @@ __device__ __forceinline__ float head_decay(const Walk& p, int h, bool record) {
     return lg;
 }
 
+// warp_wait whose tries sleep in the barrier (up to a millisecond each) instead of polling: most of a block's
+// warps wait most of the time, and polling they took three of four issue slots from those that work.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                         const Waits& w) {
+    bool got = mbar_sleep_wait(bar, parity, 1000000u);
+    if (!got) {
+        const uint64_t t0 = globaltimer_ns();
+        const uint32_t nap = w.limit_ns < 4000000u ? (uint32_t)(w.limit_ns / 4) : 1000000u;
+        while (!(got = mbar_sleep_wait(bar, parity, nap))) {
+            if (*abort_flag) break;
+            if (globaltimer_ns() - t0 > w.limit_ns) {
+                *abort_flag = 1;
+                record_status(w.status, FLAREPP_ERR_TIMEOUT);
+                break;
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, got);
+}
+
 template <int T>
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, int token, int head, int b,
                                           uint32_t bar) {
@@ -117,55 +141,129 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, in
     for (int k = 0; k < T / 64; ++k) tma_load_4d(dst + k * kAtomBytes, m, 64 * k, token, head, b, bar);
 }
 
-// 16 contraction values at step s of a tile of 128 rows whose channels are contracted
-__device__ __forceinline__ uint64_t by_channel(uint32_t tile, int s) {
-    return smem_desc(tile + s / 4 * kAtomBytes + s % 4 * 32, 16, 1024, kSw128);
+// The operands of a product lie in tiles of 128-byte rows, swizzled. The upper halves of their descriptors
+// (8 rows every 1,024 bytes, version, swizzle) are all the same, the lower ones a start and a stride:
+// with the upper half a constant a step costs one addition, and a chunk's products are issued in a few
+// hundred cycles (whole descriptors took three times that, and their issue was what bounded a chunk).
+constexpr uint32_t kUpper = (1024u >> 4) | (1u << 14) | ((uint32_t)kSw128 << 29);
+__device__ __forceinline__ uint32_t lower(uint32_t start, uint32_t stride) {
+    return (start >> 4) | (stride >> 4) << 16;
 }
-// 16 rows at step s of a tile whose rows are contracted; `atom` bytes from 64 channels to the next 64
-__device__ __forceinline__ uint64_t by_row(uint32_t tile, int s, uint32_t atom) {
-    return smem_desc(tile + s * 16 * 128, atom, 1024, kSw128);
+// what step s (16 contraction values) adds: of a tile whose channels are contracted, whose rows are
+__device__ __forceinline__ uint32_t by_channel(int s) { return (uint32_t)(s / 4 * kAtomBytes + s % 4 * 32) >> 4; }
+__device__ __forceinline__ uint32_t by_row(int s) { return (uint32_t)(s * 16 * 128) >> 4; }
+
+__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                           uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 x, {%1, %4};\n\tmov.b64 y, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(kUpper), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                           uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 y, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(kUpper), "r"(accumulate)
+        : "memory");
 }
 
-__device__ __forceinline__ uint32_t scaled_pair(uint32_t v, float w) {
-    const __nv_bfloat162 r = __floats2bfloat162_rn(__uint_as_float(v << 16) * w,
-                                                   __uint_as_float(v & 0xffff0000u) * w);
-    return *reinterpret_cast<const uint32_t*>(&r);
+__device__ __forceinline__ uint4 scaled(uint4 d, float w) {
+    const uint64_t w2 = pair(w, w);
+    return make_uint4(pack_bf16x2(mul2(unpack_bf16x2(d.x), w2)), pack_bf16x2(mul2(unpack_bf16x2(d.y), w2)),
+                      pack_bf16x2(mul2(unpack_bf16x2(d.z), w2)), pack_bf16x2(mul2(unpack_bf16x2(d.w), w2)));
 }
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
+// tcgen05.wait::ld that names the 8 registers of a load before it
+__device__ __forceinline__ void wait_ld8(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+                 :
+                 : "memory");
+}
+
+// Of 16 bf16 values in 8 words those whose bit is set; the others become 0, whatever they were. The
+// shifts put the bits of two values that share a byte into its top place, from where a byte permute
+// spreads them over a word.
+__device__ __forceinline__ void keep_keys(uint32_t* w, uint32_t bits) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int b = j / 4, i = 2 * j % 8;  // values 8 b + i and the next
+        uint32_t mask;                       // a selector of 8 and more takes the byte's top bit eight times
+        asm("prmt.b32 %0, %1, %2, %3;"
+            : "=r"(mask)
+            : "r"(bits << (7 - i)), "r"(bits << (6 - i)), "r"(0x1100u * (12 + b) + 0x0011u * (8 + b)));
+        w[j] &= mask;
+    }
+}
+
+// The chunks of a block's pieces, one after the other, for the roles that only count them.
+struct Cursor {
+    int u, left;
+};
+__device__ __forceinline__ bool next_chunk(const Walk& p, int units, Cursor& c) {
+    while (c.left == 0) {
+        if (c.u >= units) return false;
+        c.left = chunks_of(p, piece_of(p, c.u / p.Hq));
+        c.u += gridDim.x;
+    }
+    --c.left;
+    return true;
+}
+
+__device__ __forceinline__ uint32_t bf16_bits(uint32_t a, uint32_t b) {
+    return bf16_pair(__uint_as_float(a), __uint_as_float(b));
+}
+
 template <int TK, int TV>
-__global__ void __launch_bounds__(kThreads, (Cfg<TK, TV>::kCtas))
+__global__ void __launch_bounds__(kThreads, 1)
     walk_kernel(const __grid_constant__ CUtensorMap tX, const __grid_constant__ CUtensorMap tA,
                 const __grid_constant__ CUtensorMap tV, const Walk p) {
     using C = Cfg<TK, TV>;
+    constexpr int kSlots = C::kSlots;
+    constexpr uint32_t kSets = C::kSets;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* vw = smem + kSlots * C::kSlot;
-    uint8_t* st = vw + C::kVw;
-    float* powers = reinterpret_cast<float*>(smem + C::kBody);  // [4 warps][32]
+    uint8_t* st = vw + kSets * C::kVw;
+    float* powers = reinterpret_cast<float*>(smem + C::kBody);  // [2][kTable]
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBody + kPowers);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8u * kSlots;
-    const uint32_t s_ready = empty0 + 8u * kSlots, p_ready = s_ready + 8, b_ready = s_ready + 16,
-                   u_ready = s_ready + 24, y_ready = s_ready + 32, y_free = s_ready + 40, done = s_ready + 48;
+    // Of each but the last two there are two, for even and odd chunks: whoever waits for chunk n's phase must
+    // not find that of chunk n + 1 done too, and no barrier's phase n + 2 comes before all have seen n.
+    const uint32_t s_ready = empty0 + 8u * kSlots, p_ready = s_ready + 16, v_ready = s_ready + 32,
+                   u_ready = s_ready + 48, y_ready = s_ready + 64, y_free = s_ready + 80;
+    const uint32_t b_ready = s_ready + 96, done = s_ready + 104, t_ready = s_ready + 112;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSlots; ++s) {
             mbar_init(full0 + 8u * s, 1);
-            mbar_init(empty0 + 8u * s, 1);
+            mbar_init(empty0 + 8u * s, 2);
         }
-        mbar_init(s_ready, 1);
-        mbar_init(p_ready, 128);
-        mbar_init(b_ready, 128);
-        mbar_init(u_ready, 1);
-        mbar_init(y_ready, 1);
-        mbar_init(y_free, 128);
-        mbar_init(done, 1);
+        for (uint32_t s = 0; s < 16; s += 8) {
+            mbar_init(s_ready + s, 1);
+            mbar_init(p_ready + s, 256);
+            mbar_init(v_ready + s, 128);
+            mbar_init(u_ready + s, 1);
+            mbar_init(y_ready + s, 1);
+            mbar_init(y_free + s, 128);
+        }
+        mbar_init(b_ready, TK);
+        mbar_init(done, 2);
+        mbar_init(t_ready, 256);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tmap(&tX);
@@ -183,16 +281,27 @@ __global__ void __launch_bounds__(kThreads, (Cfg<TK, TV>::kCtas))
     pdl_trigger();
     pdl_wait();
 
-    const int64_t units = (p.pieces ? (int64_t)*p.count : p.n_pieces) * p.Hq;
+    const int units = (p.pieces ? *p.count : p.n_pieces) * p.Hq;
     const int per = p.only_state ? 2 : 3;  // tiles of a chunk
+    const int width = (p.Dv + 15) / 16 * 16;  // columns of the products
+    const int steps = (p.Da + 15) / 16;       // steps of a product over Da
+    // the barrier of chunk n, and its phase there
+    auto of = [](uint32_t bar, uint32_t n) { return bar + 8u * (n & 1); };
+    auto wait_chunk = [&](uint32_t bar, uint32_t n) {
+        return wait_for(bar + 8u * (n & 1), (n >> 1) & 1, abort_flag, p.waits);
+    };
+    auto wait_tile = [&](uint32_t t) {
+        return wait_for(full0 + 8u * (t % kSlots), (t / kSlots) & 1, abort_flag, p.waits);
+    };
+    auto tile = [&](uint32_t t) { return smem_u32(smem + t % kSlots * C::kSlot); };
 
     if (warp == 0) {
         // ------------------------------------------------------------ loads: A, X, V
         uint32_t it = 0;
         bool ok = true;
-        for (int64_t u = blockIdx.x; u < units && ok; u += gridDim.x) {
-            const int64_t i = u / p.Hq;
-            const int h = (int)(u - i * p.Hq);
+        for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+            const int i = u / p.Hq;
+            const int h = u - i * p.Hq;
             const Piece x = piece_of(p, i);
             const int n = chunks_of(p, x), b = p.pieces ? 0 : x.sequence;
             for (int k = 0; k < n && ok; ++k) {
@@ -202,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, (Cfg<TK, TV>::kCtas))
                     const int s = it % kSlots;
                     const uint32_t full = full0 + 8u * s;
                     if (it >= (uint32_t)kSlots &&
-                        !warp_wait<1>(empty0 + 8u * s, (it / kSlots - 1) & 1, abort_flag, p.waits)) {
+                        !wait_for(empty0 + 8u * s, (it / kSlots - 1) & 1, abort_flag, p.waits)) {
                         ok = false;
                         break;
                     }
@@ -231,66 +340,42 @@ __global__ void __launch_bounds__(kThreads, (Cfg<TK, TV>::kCtas))
             }
         }
     } else if (warp == 1) {
-        // ------------------------------------------------------------ products
-        constexpr uint32_t kScores = idesc_bf16_f32(128, 128, false, false);
-        constexpr uint32_t kState = idesc_bf16_f32(128, TV, true, true);
-        constexpr uint32_t kOut = idesc_bf16_f32(128, TV, false, true);
-        const uint32_t vw_at = smem_u32(vw), st_at = smem_u32(st);
-        uint32_t it = 0, n = 0;  // tiles, chunks
+        // ------------------------------------------------------------ products: X A^T, and (W o X A^T) V
+        // A tile is released by the warps that wait for its last product: a commit of its own
+        // for each kept this warp from issuing for hundreds of cycles.
+        const uint32_t scores = idesc_bf16_f32(128, 128, false, false);
+        const uint32_t outs = idesc_bf16_f32(128, 16, false, true) + ((uint32_t)(width / 8 - 2) << 17);
+        Cursor ahead{(int)blockIdx.x, 0}, here{(int)blockIdx.x, 0};
         bool ok = true;
-        for (int64_t u = blockIdx.x; u < units && ok; u += gridDim.x) {
-            const int total = chunks_of(p, piece_of(p, u / p.Hq));
-            for (int k = 0; k < total; ++k, it += per, ++n) {
-                const uint32_t ia = it, ix = it + 1, iv = it + per - 1;
-                const uint32_t a = smem_u32(smem + ia % kSlots * C::kSlot);
-                const uint32_t x = smem_u32(smem + ix % kSlots * C::kSlot);
-                const uint32_t v = smem_u32(smem + iv % kSlots * C::kSlot);
-                ok = warp_wait<1>(full0 + 8u * (ia % kSlots), (ia / kSlots) & 1, abort_flag, p.waits);
-                if (!ok) break;
-                if (!p.only_state) {
-                    ok = warp_wait<1>(full0 + 8u * (ix % kSlots), (ix / kSlots) & 1, abort_flag, p.waits);
-                    // the scores' columns still hold the last chunk's X S
-                    if (ok && C::kShared && n)
-                        ok = warp_wait<1>(y_free, (n - 1) & 1, abort_flag, p.waits);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int s = 0; s < TK / 16; ++s)
-                            mma_ss(tmem, by_channel(x, s), by_channel(a, s), kScores, s > 0);
-                        mma_commit(s_ready);
-                    }
-                    __syncwarp();
-                }
-                // S += A^T (w o V); rows from 64 on are not used where TK is 64
-                ok = warp_wait<1>(b_ready, n & 1, abort_flag, p.waits);
+        auto issue_scores = [&](uint32_t n) {
+            if (!wait_tile(3 * n) || !wait_tile(3 * n + 1)) return false;
+            tc_fence_after();
+            const uint32_t a = lower(tile(3 * n), 16), x = lower(tile(3 * n + 1), 16);
+            const uint32_t to = tmem + n % kSets * 128;
+            if (elect_one()) {
+#pragma unroll 1
+                for (int s = 0; s < steps; ++s)
+                    product_ss(to, x + by_channel(s), a + by_channel(s), scores, s > 0);
+                mma_commit(of(s_ready, n));
+            }
+            __syncwarp();
+            return true;
+        };
+        if (!p.only_state) {
+            if (kSets == 2 && next_chunk(p, units, ahead)) ok = issue_scores(0);
+            for (uint32_t n = 0; ok && next_chunk(p, units, here); ++n) {
+                if (kSets == 1) ok = issue_scores(n);
+                else if (next_chunk(p, units, ahead)) ok = issue_scores(n + 1);
+                ok = ok && wait_chunk(v_ready, n) && wait_chunk(p_ready, n) &&
+                     (n == 0 || wait_chunk(y_free, n - 1));
                 if (!ok) break;
                 tc_fence_after();
+                const uint32_t v = lower(tile(3 * n + 2), kAtomBytes), w = tmem + n % kSets * 128;
                 if (elect_one()) {
-#pragma unroll
+#pragma unroll 2
                     for (int s = 0; s < kChunk / 16; ++s)
-                        mma_ss(tmem + C::kColS, by_row(a, s, kAtomBytes), by_row(vw_at, s, kAtomBytes),
-                               kState, 1u);
-                    mma_commit(u_ready);
-                    mma_commit(empty0 + 8u * (ia % kSlots));
-                    if (p.only_state) mma_commit(empty0 + 8u * (iv % kSlots));
-                }
-                __syncwarp();
-                if (p.only_state) continue;
-                ok = warp_wait<1>(p_ready, n & 1, abort_flag, p.waits);
-                if (ok && !C::kShared && n) ok = warp_wait<1>(y_free, (n - 1) & 1, abort_flag, p.waits);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int s = 0; s < TK / 16; ++s)
-                        mma_ss(tmem + C::kColX, by_channel(x, s), by_row(st_at, s, TK * 128), kOut, s > 0);
-#pragma unroll
-                    for (int s = 0; s < kChunk / 16; ++s)
-                        mma_ts(tmem + C::kColY, tmem + 8 * s, by_row(v, s, kAtomBytes), kOut, s > 0);
-                    mma_commit(y_ready);
-                    mma_commit(empty0 + 8u * (ix % kSlots));
-                    mma_commit(empty0 + 8u * (iv % kSlots));
+                        product_ts(tmem + C::kColY, w + s / 4 * 64 + s % 4 * 8, v + by_row(s), outs, s > 0);
+                    mma_commit(of(y_ready, n));
                 }
                 __syncwarp();
             }
@@ -298,140 +383,184 @@ __global__ void __launch_bounds__(kThreads, (Cfg<TK, TV>::kCtas))
         // no product and no arrival of one is in flight when the block ends
         if (elect_one()) mma_commit(done);
         __syncwarp();
-        warp_wait<1>(done, 0, abort_flag, p.waits);
+        wait_for(done, 0, abort_flag, p.waits);
         if (!ok) linger();
-    } else if (warp < 6) {
-        // ------------------------------------------------------------ scores and outputs
+    } else if (warp == 2) {
+        // ------------------------------------------------------------ products: X S, then S += A^T (w o V)
+        const uint32_t states = idesc_bf16_f32(128, 16, true, true) + ((uint32_t)(width / 8 - 2) << 17);
+        const uint32_t outs = idesc_bf16_f32(128, 16, false, true) + ((uint32_t)(width / 8 - 2) << 17);
+        const uint32_t s0 = lower(smem_u32(st), TK * 128);
+        Cursor here{(int)blockIdx.x, 0};
+        bool ok = true;
+        for (uint32_t n = 0; next_chunk(p, units, here); ++n) {
+            ok = wait_tile(per * n) && (p.only_state || wait_tile(3 * n + 1)) &&
+                 (p.only_state || n < kSets || wait_chunk(y_free, n - kSets)) && wait_chunk(v_ready, n) &&
+                 wait_for(b_ready, n & 1, abort_flag, p.waits);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t a = lower(tile(per * n), kAtomBytes), x = lower(tile(3 * n + 1), 16);
+            const uint32_t v = lower(smem_u32(vw + n % kSets * C::kVw), kAtomBytes);
+            const uint32_t to = tmem + C::kColX + n % kSets * TV;
+            // (where TK is 64, A^T's rows from 64 on are whatever lies behind the tile: they are not used)
+            if (elect_one()) {
+                if (!p.only_state)
+#pragma unroll 1
+                    for (int s = 0; s < steps; ++s)
+                        product_ss(to, x + by_channel(s), s0 + by_row(s), outs, s > 0);
+#pragma unroll 2
+                for (int s = 0; s < kChunk / 16; ++s)
+                    product_ss(tmem + C::kColS, a + by_row(s), v + by_row(s), states, 1u);
+                mma_commit(of(u_ready, n));
+            }
+            __syncwarp();
+        }
+        if (elect_one()) mma_commit(done);
+        __syncwarp();
+        wait_for(done, 0, abort_flag, p.waits);
+        if (!ok) linger();
+    } else if (warp == 3) {
+        // (no role: the next four warps begin a warpgroup, whose warps are TMEM's four quarters)
+    } else if (warp < 12) {
+        // ------------------------------------------------------------ scores
+        // Two warps share 32 tokens: one takes the keys 0 to 63, the other 64 to 127, 16 at a time, each
+        // writing over columns that it has read itself.
+        const int q = warp & 3, half = (warp - 4) >> 2, i = 32 * q + lane;  // the thread's token in the chunk
+        const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + 64 * half;
+        uint32_t n = 0, pieces = 0;
+        bool ok = true;
+        for (int u = blockIdx.x; !p.only_state && u < units && ok; u += gridDim.x) {
+            const int item = u / p.Hq;
+            const Piece x = piece_of(p, item);
+            const int total = chunks_of(p, x);
+            if (total == 0) continue;
+            // The head's powers of g by gap, 0 for gaps below 0, in the order in which keys take them. A warp
+            // that fills a table knows that all have left it: they have filled the other one since.
+            float* table = powers + (pieces & 1) * kTable;
+            {
+                const float lg = head_decay(p, u - item * p.Hq, false);
+                const int k = threadIdx.x - 128, gap = p.back ? k - 32 : 127 - k;
+                if (k < kTable) table[k] = gap < 0 ? 0.f : exp2f(lg * gap) * p.scale_p;
+            }
+            mbar_arrive(t_ready);
+            ok = wait_for(t_ready, pieces & 1, abort_flag, p.waits);
+            ++pieces;
+            if (!ok) break;
+            const float* mine = table + (p.back ? 32 - i : 127 - i) + 64 * half;
+            for (int k = 0; k < total; ++k, ++n) {
+                int rows;
+                chunk_at(p, x, k, total, rows);
+                const uint32_t from = at + n % kSets * 128;
+                ok = wait_chunk(s_ready, n);
+                if (!ok) break;
+                tc_fence_after();
+                if (threadIdx.x == 128) {  // one of two that read A and X
+                    mbar_arrive(empty0 + 8u * (3 * n % kSlots));
+                    mbar_arrive(empty0 + 8u * ((3 * n + 1) % kSlots));
+                }
+#pragma unroll 1
+                for (int c = 0; c < 64; c += 16) {
+                    const int key = 64 * half + c;
+                    uint32_t w[8];
+                    if (p.back ? key + 15 < 32 * q : key > 32 * q + 31) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) w[j] = 0;
+                    } else {
+                        uint32_t r[16];
+                        tmem_ld16(from + c, r);
+                        tmem_wait_ld16(r);
+                        const float* g = mine + c;
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2)
+                            w[j / 2] = pack_bf16x2(mul2(
+                                pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), pair(g[j], g[j + 1])));
+                        // on the diagonal, and in a chunk that ends early, what does not count is 0
+                        // whatever it was
+                        if ((key >> 5) == q || key + 16 > rows) {
+                            const int low = p.back ? i - key : 0;
+                            const int high = min(p.back ? 16 : i + 1 - key, rows - key);
+                            keep_keys(w, (high >= 16 ? 0xffffu : high <= 0 ? 0u : (1u << high) - 1u) &
+                                             (low <= 0 ? ~0u : low >= 16 ? 0u : ~0u << low));
+                        }
+                    }
+                    tmem_st8(from + c / 2, w);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(of(p_ready, n));
+            }
+        }
+    } else if (warp < 16) {
+        // ------------------------------------------------------------ outputs
         const int q = warp & 3, i = 32 * q + lane;  // the thread's token in the chunk
         const uint32_t at = tmem + ((uint32_t)(32 * q) << 16);
-        float* mine = powers + 32 * (warp - 2);
         uint32_t n = 0;
         bool ok = true;
-        for (int64_t u = blockIdx.x; !p.only_state && u < units && ok; u += gridDim.x) {
-            const int64_t item = u / p.Hq;
-            const int h = (int)(u - item * p.Hq);
+        for (int u = blockIdx.x; !p.only_state && u < units && ok; u += gridDim.x) {
+            const int item = u / p.Hq;
+            const int h = u - item * p.Hq;
             const Piece x = piece_of(p, item);
             const int total = chunks_of(p, x), b = p.pieces ? 0 : x.sequence;
             if (total == 0) continue;
             const float lg = head_decay(p, h, false);
-            __syncwarp();
-            mine[lane] = exp2f(lg * (p.back ? lane : 31 - lane));
-            __syncwarp();
             for (int k = 0; k < total; ++k, ++n) {
                 int rows;
                 const int token = chunk_at(p, x, k, total, rows);
-                ok = warp_wait<1>(s_ready, n & 1, abort_flag, p.waits);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {  // 32 keys at a time
-                    uint32_t w[16];
-                    const bool none = p.back ? c < q : c > q;
-                    if (none) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = 0;
-                    } else {
-                        uint32_t r[32];
-                        tmem_ld32(at + 32 * c, r);
-                        tmem_wait_ld32(r);
-                        if (c == q) {
-#pragma unroll
-                            for (int j = 0; j < 32; j += 2) {
-                                float s[2];
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const int gap = p.back ? j + e - lane : lane - j - e;
-                                    const bool in = gap >= 0 && 32 * c + j + e < rows;
-                                    s[e] = in ? __uint_as_float(r[j + e]) *
-                                                    (exp2f(lg * gap) * p.scale_p)
-                                              : 0.f;
-                                }
-                                w[j / 2] = bf16_pair(s[0], s[1]);
-                            }
-                        } else {
-                            const float f =
-                                p.scale_p * exp2f(lg * (p.back ? 32 * c - i : i - 32 * c - 31));
-                            const int in = rows - 32 * c;  // keys of these that are in the chunk
-#pragma unroll
-                            for (int j = 0; j < 32; j += 4) {
-                                const float4 g = *reinterpret_cast<const float4*>(mine + j);
-                                float s[4] = {__uint_as_float(r[j]) * (f * g.x),
-                                              __uint_as_float(r[j + 1]) * (f * g.y),
-                                              __uint_as_float(r[j + 2]) * (f * g.z),
-                                              __uint_as_float(r[j + 3]) * (f * g.w)};
-                                if (in < 32)
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) s[e] = j + e < in ? s[e] : 0.f;
-                                w[j / 2] = bf16_pair(s[0], s[1]);
-                                w[j / 2 + 1] = bf16_pair(s[2], s[3]);
-                            }
-                        }
-                    }
-                    tmem_st16(at + 16 * c, w);
-                }
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(p_ready);
-                ok = warp_wait<1>(y_ready, n & 1, abort_flag, p.waits);
-                if (!ok) break;
-                tc_fence_after();
                 const int since = p.back ? rows - 1 - i : i;
                 const float f = i < rows ? exp2f(lg * (since + p.lead)) * p.scale_r : 0.f;
                 const int64_t to = b * p.yb + h * p.yh + (int64_t)(token + i) * p.yn;
+                ok = wait_chunk(u_ready, n) && wait_chunk(y_ready, n);
+                if (!ok) break;
+                tc_fence_after();
+                if (threadIdx.x == 384)  // V has been read, by the warps that decay it and by its product
+                    mbar_arrive_n(empty0 + 8u * ((3 * n + 2) % kSlots), 2);
 #pragma unroll 1
-                for (int c = 0; c < TV; c += 16) {
-                    if (c >= p.Dv) break;
+                for (int c = 0; c < p.Dv; c += 16) {
                     uint32_t y[16], s[16];
                     tmem_ld16(at + C::kColY + c, y);
-                    tmem_ld16(at + C::kColX + c, s);
+                    tmem_ld16(at + C::kColX + n % kSets * TV + c, s);
                     tmem_wait_ld16(y);
                     tmem_wait_ld16(s);
-                    float o[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        o[j] = fmaf(__uint_as_float(s[j]), f, __uint_as_float(y[j]));
+                        y[j] = __float_as_uint(fmaf(__uint_as_float(s[j]), f, __uint_as_float(y[j])));
                     if (i < rows) {
-#pragma unroll
-                        for (int j = 0; j < 16; j += 8) {
-                            if (c + j >= p.Dv) break;
-                            if (p.y_f32) {
-                                float* d = (float*)p.y + to + c + j;
-                                *reinterpret_cast<float4*>(d) =
-                                    make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                                *reinterpret_cast<float4*>(d + 4) =
-                                    make_float4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
-                            } else {
-                                *reinterpret_cast<uint4*>((__nv_bfloat16*)p.y + to + c + j) = make_uint4(
-                                    bf16_pair(o[j], o[j + 1]), bf16_pair(o[j + 2], o[j + 3]),
-                                    bf16_pair(o[j + 4], o[j + 5]), bf16_pair(o[j + 6], o[j + 7]));
-                            }
+                        const bool both = c + 8 < p.Dv;
+                        if (p.y_f32) {
+                            uint4* d = reinterpret_cast<uint4*>((float*)p.y + to + c);
+                            d[0] = make_uint4(y[0], y[1], y[2], y[3]);
+                            d[1] = make_uint4(y[4], y[5], y[6], y[7]);
+                            if (both) d[2] = make_uint4(y[8], y[9], y[10], y[11]);
+                            if (both) d[3] = make_uint4(y[12], y[13], y[14], y[15]);
+                        } else {
+                            uint4* d = reinterpret_cast<uint4*>((__nv_bfloat16*)p.y + to + c);
+                            d[0] = make_uint4(bf16_bits(y[0], y[1]), bf16_bits(y[2], y[3]),
+                                              bf16_bits(y[4], y[5]), bf16_bits(y[6], y[7]));
+                            if (both)
+                                d[1] = make_uint4(bf16_bits(y[8], y[9]), bf16_bits(y[10], y[11]),
+                                                  bf16_bits(y[12], y[13]), bf16_bits(y[14], y[15]));
                         }
                     }
                     __syncwarp();
                 }
-                __syncwarp();
                 tc_fence_before();
-                mbar_arrive(y_free);
+                mbar_arrive(of(y_free, n));
             }
         }
-    } else {
-        // ------------------------------------------------------------ decayed values and the state
-        const int q = warp & 3, row = 32 * q + lane;  // the thread's row of the state
-        const bool keeps = 32 * q < TK;
-        // where half of the warps keep no state, they alone make the decayed values
-        constexpr int kMakers = TK == 64 ? 64 : 128;
-        const int maker = TK == 64 ? (keeps ? -1 : 32 * (q - 2) + lane) : 32 * q + lane;
+    } else if (warp < 20) {
+        // ------------------------------------------------------------ the state
+        const int q = warp & 3, row = 32 * q + lane;  // the thread's row of it
+        const bool keeps = 32 * q < p.Da;
         const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + C::kColS;
-        uint32_t it = 0, n = 0;
+        uint32_t n = 0;
         bool ok = true;
-        for (int64_t u = blockIdx.x; u < units && ok; u += gridDim.x) {
-            const int64_t item = u / p.Hq;
-            const int h = (int)(u - item * p.Hq);
+        for (int u = blockIdx.x; 32 * q < TK && u < units && ok; u += gridDim.x) {
+            const int item = u / p.Hq;
+            const int h = u - item * p.Hq;
             const Piece x = piece_of(p, item);
             const int total = chunks_of(p, x);
-            const int64_t own = (item * p.Hq + h) * p.Da * p.Dv + (int64_t)row * p.Dv;
+            const int64_t own = (int64_t)u * p.Da * p.Dv + (int64_t)row * p.Dv;
             const int64_t kept = ((int64_t)x.sequence * p.Hq + h) * p.Da * p.Dv + row * p.row_stride;
-            const float lg = head_decay(p, h, threadIdx.x == 192);
+            const float lg = head_decay(p, h, row == 0);
             if (p.only_state && ends(p, x)) continue;
             if (keeps) {  // the state in front of the piece
                 const float* from = nullptr;
@@ -443,85 +572,60 @@ __global__ void __launch_bounds__(kThreads, (Cfg<TK, TV>::kCtas))
                     step = p.col_stride;
                 }
 #pragma unroll 1
-                for (int c = 0; c < TV; c += 16) {
-                    uint32_t r[16];
+                for (int c = 0; c < width; c += 8) {
+                    uint32_t r[8];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
+                    for (int j = 0; j < 8; ++j)
                         r[j] = from && row < p.Da && c + j < p.Dv
                                    ? __float_as_uint(from[(c + j) * step]) : 0u;
-                    tmem_st16(at + c, r);
+                    tmem_st8(at + c, r);
                 }
                 tmem_wait_st();
             }
-            for (int k = 0; k < total; ++k, it += per, ++n) {
+            for (int k = 0; k < total; ++k, ++n) {
                 int rows;
                 chunk_at(p, x, k, total, rows);
-                const uint32_t iv = it + per - 1;
-                ok = warp_wait<1>(full0 + 8u * (iv % kSlots), (iv / kSlots) & 1, abort_flag, p.waits);
-                if (ok && rows < kChunk)
-                    ok = warp_wait<1>(full0 + 8u * (it % kSlots), (it / kSlots) & 1, abort_flag, p.waits);
-                if (!ok) break;
-                if (maker >= 0) {
-                    uint8_t* v = smem + iv % kSlots * C::kSlot;
-                    uint8_t* a = smem + it % kSlots * C::kSlot;
-#pragma unroll 4
-                    for (int e = maker; e < TV * 16; e += kMakers) {
-                        const int r = (e & 1023) >> 3;  // the token of this 16-byte piece
-                        const float w = exp2f(lg * (p.back ? r + 1 - p.lead : rows - p.lead - r)) *
-                                        p.scale_w;
-                        uint4 d = *reinterpret_cast<const uint4*>(v + 16 * e);
-                        d = r < rows ? make_uint4(scaled_pair(d.x, w), scaled_pair(d.y, w),
-                                                  scaled_pair(d.z, w), scaled_pair(d.w, w))
-                                     : make_uint4(0, 0, 0, 0);
-                        *reinterpret_cast<uint4*>(vw + 16 * e) = d;
-                    }
-                    if (rows < kChunk) {
-                        // what lies behind the sequence may be another one, or no numbers at all
-                        for (int e = maker; e < TV * 16; e += kMakers)
-                            if (((e & 1023) >> 3) >= rows)
-                                *reinterpret_cast<uint4*>(v + 16 * e) = make_uint4(0, 0, 0, 0);
-                        for (int e = maker; e < TK * 16; e += kMakers)
-                            if (((e & 1023) >> 3) >= rows)
-                                *reinterpret_cast<uint4*>(a + 16 * e) = make_uint4(0, 0, 0, 0);
-                    }
-                }
-                // the last chunk's product with the state has read it
-                if (!p.only_state && n) {
-                    ok = warp_wait<1>(y_ready, (n - 1) & 1, abort_flag, p.waits);
-                    if (!ok) break;
-                }
                 if (keeps) {
                     const float g = exp2f(lg * rows);
+                    const uint64_t g2 = pair(g, g);
 #pragma unroll 1
-                    for (int c = 0; c < TV; c += 32) {
-                        uint32_t r[32];
-                        tmem_ld32(at + c, r);
-                        tmem_wait_ld32(r);
+                    for (int c = 0; c < p.Dv; c += 16) {
+                        uint32_t r[16];
+                        tmem_ld16(at + c, r);
+                        tmem_wait_ld16(r);
                         if (!p.only_state) {
                             // rows of 64 values, 16-byte pieces swapped as the tiles' are
                             uint8_t* d = st + c / 64 * (TK * 128) + row * 128;
 #pragma unroll
-                            for (int j = 0; j < 32; j += 8) {
+                            for (int j = 0; j < 16; j += 8) {
                                 const int piece = ((c % 64 + j) / 8) ^ (row & 7);
                                 *reinterpret_cast<uint4*>(d + 16 * piece) = make_uint4(
-                                    bf16_pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1])),
-                                    bf16_pair(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])),
-                                    bf16_pair(__uint_as_float(r[j + 4]), __uint_as_float(r[j + 5])),
-                                    bf16_pair(__uint_as_float(r[j + 6]), __uint_as_float(r[j + 7])));
+                                    bf16_bits(r[j], r[j + 1]), bf16_bits(r[j + 2], r[j + 3]),
+                                    bf16_bits(r[j + 4], r[j + 5]), bf16_bits(r[j + 6], r[j + 7]));
                             }
                         }
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * g);
-                        tmem_st32(at + c, r);
+                        for (int j = 0; j < 16; j += 2) {
+                            const float2 v =
+                                halves(mul2(pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), g2));
+                            r[j] = __float_as_uint(v.x);
+                            r[j + 1] = __float_as_uint(v.y);
+                        }
+                        tmem_st16(at + c, r);
                     }
                     tmem_wait_st();
                 }
                 fence_proxy_async();
                 tc_fence_before();
                 mbar_arrive(b_ready);
-                ok = warp_wait<1>(u_ready, n & 1, abort_flag, p.waits);
+                ok = wait_chunk(u_ready, n);
                 if (!ok) break;
                 tc_fence_after();
+                if (row == 0) {  // the other of the two that read A and X; without outputs A and V
+                    const uint32_t times = p.only_state ? 2 : 1;
+                    mbar_arrive_n(empty0 + 8u * (per * n % kSlots), times);
+                    mbar_arrive_n(empty0 + 8u * ((per * n + 1) % kSlots), times);
+                }
             }
             if (!ok) break;
             float* to = nullptr;
@@ -534,16 +638,77 @@ __global__ void __launch_bounds__(kThreads, (Cfg<TK, TV>::kCtas))
             }
             if (keeps && to)
 #pragma unroll 1
-                for (int c = 0; c < TV; c += 16) {
-                    uint32_t r[16];
-                    tmem_ld16(at + c, r);
-                    tmem_wait_ld16(r);
+                for (int c = 0; c < p.Dv; c += 8) {
+                    uint32_t r[8];
+                    tmem_ld8(at + c, r);
+                    wait_ld8(r);
                     if (row < p.Da)
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (c + j < p.Dv) to[(c + j) * step] = __uint_as_float(r[j]);
+                        for (int j = 0; j < 8; ++j) to[(c + j) * step] = __uint_as_float(r[j]);
+                    __syncwarp();
                 }
             __syncwarp();
+        }
+    } else {
+        // ------------------------------------------------------------ decayed values
+        const int maker = threadIdx.x - 640;
+        // a row's 16-byte pieces of a tile of 64 channels that hold values: 8 or 4
+        const int shift = width > 32 ? 3 : 2, turns = 1 << shift;  // tokens of the thread
+        uint32_t n = 0;
+        bool ok = true;
+        for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+            const int item = u / p.Hq;
+            const Piece x = piece_of(p, item);
+            const int total = chunks_of(p, x);
+            if (total == 0) continue;
+            const float lg = head_decay(p, u - item * p.Hq, false);
+            // Of a whole chunk the thread takes a 16-byte piece of every 16th (or 32nd) token, from the one
+            // with the largest weight on: each next one's is `ratio` times the last's.
+            const int stride = 128 >> shift, r0 = p.back ? maker >> shift : 127 - (maker >> shift);
+            const float heaviest = exp2f(lg * (p.back ? r0 + 1 - p.lead : kChunk - p.lead - r0)) * p.scale_w;
+            const float ratio = exp2f(lg * stride);
+            for (int k = 0; k < total; ++k, ++n) {
+                int rows;
+                chunk_at(p, x, k, total, rows);
+                const uint32_t ia = per * n, iv = ia + per - 1;
+                // the buffer's last product is done, and whoever waited for its last filling has seen it
+                ok = wait_tile(iv) && (rows == kChunk || wait_tile(ia)) &&
+                     (n < kSets || wait_chunk(u_ready, n - kSets)) &&
+                     (n < 2 || p.only_state || wait_chunk(y_ready, n - 2));
+                if (!ok) break;
+                uint8_t* v = smem + iv % kSlots * C::kSlot;
+                uint8_t* a = smem + ia % kSlots * C::kSlot;
+                uint8_t* to = vw + n % kSets * C::kVw;
+                if (rows == kChunk) {
+                    float w = heaviest;
+                    // the tiles' pieces are swapped by the row's last three bits
+                    int o = r0 * 128 + 16 * ((maker & ((1 << shift) - 1)) ^ (r0 & 7));
+                    const int step = p.back ? stride * 128 : -stride * 128;
+#pragma unroll 2
+                    for (int e = 0; e < turns; ++e, o += step, w *= ratio)
+#pragma unroll
+                        for (int t = 0; t < TV / 64; ++t)
+                            *reinterpret_cast<uint4*>(to + o + t * kAtomBytes) =
+                                scaled(*reinterpret_cast<const uint4*>(v + o + t * kAtomBytes), w);
+                } else {
+                    // what lies behind the sequence may be another one, or no numbers at all
+#pragma unroll 1
+                    for (int e = maker; e < TV * 16; e += 128) {
+                        const int r = (e & 1023) >> 3;
+                        const float w = exp2f(lg * (p.back ? r + 1 - p.lead : rows - p.lead - r)) * p.scale_w;
+                        uint4 d = make_uint4(0, 0, 0, 0);
+                        if (r < rows) d = scaled(*reinterpret_cast<const uint4*>(v + 16 * e), w);
+                        else *reinterpret_cast<uint4*>(v + 16 * e) = d;
+                        *reinterpret_cast<uint4*>(to + 16 * e) = d;
+                    }
+#pragma unroll 1
+                    for (int e = maker; e < TK * 16; e += 128)
+                        if (((e & 1023) >> 3) >= rows)
+                            *reinterpret_cast<uint4*>(a + 16 * e) = make_uint4(0, 0, 0, 0);
+                }
+                fence_proxy_async();
+                mbar_arrive(of(v_ready, n));
+            }
         }
     }
     __syncwarp();
@@ -771,18 +936,13 @@ cudaError_t launch_walk(const CUtensorMap* m, const Walk& p, int64_t units, cuda
         if (e != cudaSuccess) return e;
         ready.fetch_or(uint64_t(1) << dev);
     }
-    const int64_t most = (int64_t)kNumSMs * C::kCtas;
-    return launch(kernel, units < most ? units : most, kThreads, C::kSmem, st, m[0], m[1], m[2], p);
+    return launch(kernel, units < kNumSMs ? units : kNumSMs, kThreads, C::kSmem, st, m[0], m[1], m[2], p);
 }
 
 cudaError_t launch_for(const CUtensorMap* m, const Walk& p, int64_t units, cudaStream_t st) {
     if (p.Da <= 64)
         return p.Dv <= 64 ? launch_walk<64, 64>(m, p, units, st) : launch_walk<64, 128>(m, p, units, st);
     return p.Dv <= 64 ? launch_walk<128, 64>(m, p, units, st) : launch_walk<128, 128>(m, p, units, st);
-}
-
-int64_t resident(const flarepp_decay_shape& s) {
-    return (int64_t)kNumSMs * (s.Dk <= 64 && s.Dv <= 64 ? 2 : 1);
 }
 
 }  // namespace
@@ -795,7 +955,7 @@ cudaError_t take_decay_status(int32_t* out, cudaStream_t st) { return take_libra
 DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
     DecayPlan p{};
     p.sequences = s.sequences ? s.sequences : s.B;
-    const int64_t all = cdiv(s.N, kChunk), slots = resident(s);
+    const int64_t all = cdiv(s.N, kChunk), slots = kNumSMs;
     if (s.sequences) {
         const int64_t per = cdiv(all * s.Hq, 2 * slots);
         p.chunks = per < 4 ? 4 : per;
@@ -870,7 +1030,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         p.pieces = (const Piece*)(ws + plan.off_pieces);
         p.count = (const int*)(ws + plan.off_first) + s.sequences;
     }
-    p.n_pieces = plan.pieces;
+    p.n_pieces = (int)plan.pieces;
     p.per_sequence = (int)plan.per_sequence;
     p.piece_rows = (int)(plan.chunks * kChunk);
     p.lead = w.back ? 0 : 1;
@@ -890,6 +1050,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
     p.waits.status = w.status;
     test_fault_for(kDecayKernel, &p.waits.limit_ns, &p.waits.withheld);
     const int64_t units = plan.pieces * s.Hq;
+    if (units > INT32_MAX - kNumSMs) return cudaErrorInvalidValue;
     cudaError_t e;
     if (plan.split) {
         float* slots = (float*)(ws + plan.off_states);
