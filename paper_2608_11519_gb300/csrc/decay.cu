@@ -23,8 +23,10 @@ flarepp_status check_shape(const flarepp_decay_shape* s) {
     // tokens, and the units of work that they make, are counted in 31 bits
     const int64_t n = s->sequences ? s->sequences : s->B;
     if (s->N > INT32_MAX - 256 || s->Hq > 65535 || n > INT32_MAX / 64) return FLAREPP_ERR_UNSUPPORTED;
-    if (s->Hq && (n + s->N / kDecayChunk) * s->Hq > (int64_t(1) << 40)) return FLAREPP_ERR_UNSUPPORTED;
-    if (s->Hq && n * s->Hq > INT32_MAX / 64) return FLAREPP_ERR_UNSUPPORTED;
+    if (n * (s->sequences ? 1 : s->N / kDecayChunk + 1) > (INT32_MAX - (1 << 20)) / (s->Hq ? s->Hq : 1))
+        return FLAREPP_ERR_UNSUPPORTED;
+    if (s->sequences && n + s->N / kDecayChunk > (INT32_MAX - (1 << 20)) / (s->Hq ? s->Hq : 1))
+        return FLAREPP_ERR_UNSUPPORTED;
     return FLAREPP_OK;
 }
 

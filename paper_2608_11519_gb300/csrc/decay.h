@@ -46,17 +46,16 @@ struct DecayWalk {
     int32_t* status;
 };
 
-// The cut of the sequences into pieces of up to `chunks` chunks, and the workspace that goes with it.
+// How the walk is shared among the blocks (tc_decay.cu), and the workspace that goes with it.
 struct DecayPlan {
-    int64_t sequences, pieces;  // pieces: their number, or with packing its bound
-    int64_t chunks;             // of a piece
-    int64_t per_sequence;       // pieces of a sequence without packing
-    bool split;                 // whether a sequence may have several pieces
-    size_t off_pieces, off_first, off_cuts, off_states, off_sums, total;
+    int64_t sequences, chunks;  // chunks of a sequence (the longest possible one)
+    bool whole;                 // whether no sequence is cut
+    int64_t blocks, share;      // share: heads or chunks of a block, 0 if the lengths tell
+    size_t off_first, off_cuts, off_left, off_slots, off_sums, total;
 };
 DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward);
 
-// Packed sequences: the table of pieces and the cuts (checked) into the workspace.
+// Packed sequences: the cuts (checked) and the chunks before each into the workspace.
 cudaError_t decay_cut(const flarepp_decay_shape& s, const DecayPlan& p, const int32_t* offsets, char* ws,
                       int32_t* status, cudaStream_t st);
 // The rows that no sequence holds become 0.

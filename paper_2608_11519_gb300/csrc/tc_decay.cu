@@ -6,13 +6,10 @@
 //
 // Bound by bytes at every width: a chunk reads three tiles and writes one, 64 KB at 64 channels, which the
 // card takes 1.45 us for on each of its 152 SMs, and its four products some 0.35 us. So one block walks a
-// piece of a sequence of one head, with the state staying in TMEM, and nothing is read twice; where heads
-// and sequences are fewer than the SMs, sequences are cut into pieces, whose states a first walk
-// (only A and V, only S) and a join over the pieces find.
+// sequence of one head, with the state staying in TMEM, and nothing is read twice; where heads and sequences
+// do not fill the SMs evenly, sequences are cut, and a first walk (only A and V, only S, only in front
+// of the cuts) and a join over the blocks find the states there.
 //
-// No power of g passes float32, whatever the decay: in blocks of 32 x 32 W is the product
-// g^(i - last j of the block) g^(last j - j), a factor of the thread's and one of a table's, both at most 1
-// below the diagonal; on it the first is g^-31 at most, and a strong decay takes an exponential each there.
 // W o (X A^T), S and w o V are rounded to bf16 as operands; sums, states and what r multiplies are float32.
 //
 // Roles (24 warps, a block an SM): warp 0 loads tiles (A, X, V of each chunk, a ring), warps 1 and 2 issue the
@@ -28,35 +25,28 @@ namespace {
 constexpr int kThreads = 768;
 constexpr int kChunk = kDecayChunk;
 constexpr int kAtomBytes = kChunk * 128;  // 128 tokens of 64 channels
-constexpr int kTable = 160;                // powers of g: gaps of -32 to 127
-constexpr int kPowers = 2 * kTable * 4;    // bytes of two such tables
 constexpr size_t kWsAlign = 256;
-
-// A piece of a sequence, as a block walks it.
-struct Piece {
-    int start, rows;  // tokens
-    int sequence;
-    int flags;  // kFirst: nothing before it in the sequence, kLast: nothing behind
-};
-enum { kFirst = 1, kLast = 2 };
 
 struct Walk {
     int Hq, N, Da, Dv;
     int back, only_state;
     int gx, ga, gv;       // query heads that share a head of x, a, v
     int mx, ma, mv;       // whether a batch element has its own
-    const Piece* pieces;  // packed sequences, else NULL
-    const int* count;
-    int n_pieces;
-    int per_sequence, piece_rows;
+    // The list of all sequences' heads' chunks in the order in which they are walked (or of the sequences'
+    // heads, where none is cut), of which every block takes `share` places.
+    int whole;            // the list's places are sequences' heads
+    int sequences, chunks;  // chunks of a sequence, if they are all alike
+    int share;            // 0: from the list's length
+    const int* cuts;      // packed sequences' first tokens, else NULL
+    const int* first;     // chunks of the sequences before each, of packed ones
     float scale_p, scale_w, scale_r;  // what scores, decayed values and X S are multiplied by
     int lead;                         // r_i = g^(i + lead), w_j = g^(n - lead - j)
     const float* log_decay;
     void* y;
     int64_t yb, yh, yn;
     int y_f32;
-    const float* slots;   // the state in front of every piece [piece][Hq][Da][Dv], or NULL
-    float* slots_out;     // with only_state: the state that a piece leaves
+    const float* slots;   // the state in front of every block's first chunk, [blocks][Da][Dv]
+    float* slots_out;     // with only_state: the state that a block's last piece leaves
     const float* state;   // in front of every sequence, or NULL
     float* state_out;
     int64_t row_stride, col_stride;  // of a state between calls
@@ -74,38 +64,91 @@ struct Cfg {
     static constexpr uint32_t kColX = kColY + TV;
     static constexpr uint32_t kColS = kColX + kSets * TV;
     static constexpr uint32_t kTmem = 512;
-    static constexpr int kRoom = kMaxSmem - 1024 - kPowers - kSets * kVw - kSt - 512;
+    static constexpr int kRoom = kMaxSmem - 1024 - kSets * kVw - kSt - 512;
     static constexpr int kSlots = kRoom / kSlot < 12 ? kRoom / kSlot : 12;
-    static constexpr int kBars = 2 * kSlots + 15;
+    static constexpr int kBars = 3 * kSlots + 14;
     static constexpr int kBody = kSlots * kSlot + kSets * kVw + kSt;
-    static constexpr int kSmem = 1024 + kBody + kPowers + kBars * 8 + 16;
+    static constexpr int kSmem = 1024 + kBody + kBars * 8 + 16;
     static_assert(kSlots >= 5 && kBars * 8 + 16 <= 512 && kSmem <= kMaxSmem, "shared memory");
     static_assert(kColS + TV <= kTmem, "TMEM");
 };
 
-__device__ __forceinline__ Piece piece_of(const Walk& p, int i) {
-    if (p.pieces) return p.pieces[i];
-    Piece x;
-    x.sequence = i / p.per_sequence;
-    const int k = i - x.sequence * p.per_sequence;
-    x.start = k * p.piece_rows;
-    x.rows = min(p.piece_rows, p.N - x.start);
-    x.flags = (k == 0 ? kFirst : 0) | (k == p.per_sequence - 1 ? kLast : 0);
-    return x;
+// A part of a sequence of one head, as a block walks it: chunks c0 to c1 of `total`, counted as walked.
+struct Piece {
+    int sequence, h;
+    int start, rows;  // the sequence's tokens
+    int c0, c1, total;
+};
+// Where a block is in its part of the list.
+struct Feed {
+    int at, end;      // places
+    int sequence, h;  // of the next place
+};
+
+__device__ __forceinline__ int tokens_of(const Walk& p, int sequence, int& start) {
+    start = p.cuts ? p.cuts[sequence] : 0;
+    return p.cuts ? p.cuts[sequence + 1] - start : p.N;
 }
-__device__ __forceinline__ bool ends(const Walk& p, const Piece& x) {
-    return x.flags & (p.back ? kFirst : kLast);
+// The places before a sequence's first head, and of each of its heads.
+__device__ __forceinline__ int places_before(const Walk& p, int sequence) {
+    if (p.whole) return sequence * p.Hq;
+    return (p.cuts ? p.first[sequence] : sequence * p.chunks) * p.Hq;
 }
-__device__ __forceinline__ int chunks_of(const Walk& p, const Piece& x) {
-    // the state of a sequence's last piece is not asked for by the first walk
-    if (p.only_state && ends(p, x)) return 0;
-    return (x.rows + kChunk - 1) / kChunk;
+__device__ __forceinline__ int places_of(const Walk& p, int sequence) {
+    if (p.whole) return 1;
+    return p.cuts ? p.first[sequence + 1] - p.first[sequence] : p.chunks;
 }
-// The first token of the piece's k-th chunk, and its tokens.
-__device__ __forceinline__ int chunk_at(const Walk& p, const Piece& x, int k, int n, int& rows) {
-    const int c = p.back ? n - 1 - k : k;
-    rows = min(kChunk, x.rows - c * kChunk);
-    return x.start + c * kChunk;
+__device__ __noinline__ void begin_feed(const Walk& p, int block, Feed& f) {
+    const int all = places_before(p, p.sequences);
+    const int share = p.share ? p.share : (all + (int)gridDim.x - 1) / (int)gridDim.x;
+    f.at = min(block * share, all);  // (at most 2^31: the host has seen to it)
+    f.end = min(f.at + share, all);
+    int low = 0, high = p.sequences;  // the last sequence that begins at this place or before
+    if (f.at < f.end) {
+        while (high - low > 1) {
+            const int mid = (low + high) / 2;
+            if (places_before(p, mid) <= f.at) low = mid;
+            else high = mid;
+        }
+        f.sequence = low;
+        f.h = (f.at - places_before(p, low)) / places_of(p, low);
+    }
+}
+// The next piece; false after the last.
+__device__ __noinline__ bool next_piece(const Walk& p, Feed& f, Piece& x) {
+    if (f.at >= f.end) return false;
+    const int each = places_of(p, f.sequence);
+    const int base = places_before(p, f.sequence) + f.h * each;
+    x.sequence = f.sequence;
+    x.h = f.h;
+    x.rows = tokens_of(p, f.sequence, x.start);
+    x.total = (x.rows + kChunk - 1) / kChunk;
+    x.c0 = p.whole ? 0 : min(f.at - base, x.total);
+    x.c1 = p.whole ? x.total : min(f.end - base, x.total);
+    f.at = base + each;
+    if (++f.h == p.Hq) {
+        f.h = 0;
+        ++f.sequence;
+    }
+    return true;
+}
+// The pieces of a block's walk: all of its part of the list, or, for the states alone, the last
+// one if its sequence goes on in the next block.
+__device__ __forceinline__ bool next_walked(const Walk& p, Feed& f, Piece& x) {
+    while (next_piece(p, f, x))
+        if (!p.only_state || x.c1 < x.total) return true;
+    return false;
+}
+// The first token of chunk c, and its tokens.
+__device__ __forceinline__ int chunk_at(const Walk& p, const Piece& x, int c, int& rows) {
+    const int k = p.back ? x.total - 1 - c : c;
+    rows = min(kChunk, x.rows - k * kChunk);
+    return x.start + k * kChunk;
+}
+// Whether a chunk's outputs are stored as whole tiles: what lies behind a packed sequence is another's (behind
+// the last token of others TMA leaves it).
+__device__ __forceinline__ bool staged(const Walk& p, int rows) {
+    return !p.y_f32 && (rows == kChunk || !p.cuts);
 }
 __device__ __forceinline__ float head_decay(const Walk& p, int h, bool record) {
     bool bad = false;
@@ -115,22 +158,27 @@ __device__ __forceinline__ float head_decay(const Walk& p, int h, bool record) {
 }
 
 // warp_wait whose tries sleep in the barrier (up to a millisecond each) instead of polling: most of a block's
-// warps wait most of the time, and polling they took three of four issue slots from those that work.
+// warps wait most of the time. What follows a first try in vain is kept out of line: in line, in some thirty
+// places, it was half of the kernel's code, and instructions came late.
+__device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                         uint64_t limit_ns, int* status) {
+    const uint64_t t0 = globaltimer_ns();
+    const uint32_t nap = limit_ns < 4000000u ? (uint32_t)(limit_ns / 4) : 1000000u;
+    while (!mbar_sleep_wait(bar, parity, nap)) {
+        if (*abort_flag) return false;
+        if (globaltimer_ns() - t0 > limit_ns) {
+            *abort_flag = 1;
+            record_status(status, FLAREPP_ERR_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                          const Waits& w) {
     bool got = mbar_sleep_wait(bar, parity, 1000000u);
-    if (!got) {
-        const uint64_t t0 = globaltimer_ns();
-        const uint32_t nap = w.limit_ns < 4000000u ? (uint32_t)(w.limit_ns / 4) : 1000000u;
-        while (!(got = mbar_sleep_wait(bar, parity, nap))) {
-            if (*abort_flag) break;
-            if (globaltimer_ns() - t0 > w.limit_ns) {
-                *abort_flag = 1;
-                record_status(w.status, FLAREPP_ERR_TIMEOUT);
-                break;
-            }
-        }
-    }
+    if (__all_sync(0xffffffffu, got)) return true;
+    if (!got) got = wait_longer(bar, parity, abort_flag, w.limit_ns, w.status);
     return __all_sync(0xffffffffu, got);
 }
 
@@ -207,18 +255,14 @@ __device__ __forceinline__ void keep_keys(uint32_t* w, uint32_t bits) {
     }
 }
 
-// The chunks of a block's pieces, one after the other, for the roles that only count them.
-struct Cursor {
-    int u, left;
-};
-__device__ __forceinline__ bool next_chunk(const Walk& p, int units, Cursor& c) {
-    while (c.left == 0) {
-        if (c.u >= units) return false;
-        c.left = chunks_of(p, piece_of(p, c.u / p.Hq));
-        c.u += gridDim.x;
-    }
-    --c.left;
-    return true;
+// How many chunks a block walks.
+__device__ __noinline__ int count_chunks(const Walk& p) {
+    Feed f;
+    Piece x;
+    int n = 0;
+    begin_feed(p, blockIdx.x, f);
+    while (next_walked(p, f, x)) n += x.c1 - x.c0;
+    return n;
 }
 
 __device__ __forceinline__ uint32_t bf16_bits(uint32_t a, uint32_t b) {
@@ -228,7 +272,8 @@ __device__ __forceinline__ uint32_t bf16_bits(uint32_t a, uint32_t b) {
 template <int TK, int TV>
 __global__ void __launch_bounds__(kThreads, 1)
     walk_kernel(const __grid_constant__ CUtensorMap tX, const __grid_constant__ CUtensorMap tA,
-                const __grid_constant__ CUtensorMap tV, const Walk p) {
+                const __grid_constant__ CUtensorMap tV, const __grid_constant__ CUtensorMap tY,
+                const __grid_constant__ Walk p) {
     using C = Cfg<TK, TV>;
     constexpr int kSlots = C::kSlots;
     constexpr uint32_t kSets = C::kSets;
@@ -236,22 +281,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* vw = smem + kSlots * C::kSlot;
     uint8_t* st = vw + kSets * C::kVw;
-    float* powers = reinterpret_cast<float*>(smem + C::kBody);  // [2][kTable]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBody + kPowers);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBody);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8u * kSlots;
+    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8u * kSlots, out0 = empty0 + 8u * kSlots;
     // Of each but the last two there are two, for even and odd chunks: whoever waits for chunk n's phase must
     // not find that of chunk n + 1 done too, and no barrier's phase n + 2 comes before all have seen n.
-    const uint32_t s_ready = empty0 + 8u * kSlots, p_ready = s_ready + 16, v_ready = s_ready + 32,
+    const uint32_t s_ready = out0 + 8u * kSlots, p_ready = s_ready + 16, v_ready = s_ready + 32,
                    u_ready = s_ready + 48, y_ready = s_ready + 64, y_free = s_ready + 80;
-    const uint32_t b_ready = s_ready + 96, done = s_ready + 104, t_ready = s_ready + 112;
+    const uint32_t b_ready = s_ready + 96, done = s_ready + 104;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSlots; ++s) {
             mbar_init(full0 + 8u * s, 1);
             mbar_init(empty0 + 8u * s, 2);
+            mbar_init(out0 + 8u * s, 128);
         }
         for (uint32_t s = 0; s < 16; s += 8) {
             mbar_init(s_ready + s, 1);
@@ -263,7 +308,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         mbar_init(b_ready, TK);
         mbar_init(done, 2);
-        mbar_init(t_ready, 256);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tmap(&tX);
@@ -281,7 +325,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     pdl_trigger();
     pdl_wait();
 
-    const int units = (p.pieces ? *p.count : p.n_pieces) * p.Hq;
+    Feed feed;
+    Piece here;
     const int per = p.only_state ? 2 : 3;  // tiles of a chunk
     const int width = (p.Dv + 15) / 16 * 16;  // columns of the products
     const int steps = (p.Da + 15) / 16;       // steps of a product over Da
@@ -299,14 +344,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------ loads: A, X, V
         uint32_t it = 0;
         bool ok = true;
-        for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-            const int i = u / p.Hq;
-            const int h = u - i * p.Hq;
-            const Piece x = piece_of(p, i);
-            const int n = chunks_of(p, x), b = p.pieces ? 0 : x.sequence;
-            for (int k = 0; k < n && ok; ++k) {
+        begin_feed(p, blockIdx.x, feed);
+        while (ok && next_walked(p, feed, here)) {
+            const Piece x = here;
+            const int b = p.cuts ? 0 : x.sequence, h = x.h;
+            for (int c = x.c0; c < x.c1 && ok; ++c) {
                 int rows;
-                const int token = chunk_at(p, x, k, n, rows);
+                const int token = chunk_at(p, x, c, rows);
                 for (int j = 0; j < per; ++j, ++it) {
                     const int s = it % kSlots;
                     const uint32_t full = full0 + 8u * s;
@@ -345,34 +389,36 @@ __global__ void __launch_bounds__(kThreads, 1)
         // for each kept this warp from issuing for hundreds of cycles.
         const uint32_t scores = idesc_bf16_f32(128, 128, false, false);
         const uint32_t outs = idesc_bf16_f32(128, 16, false, true) + ((uint32_t)(width / 8 - 2) << 17);
-        Cursor ahead{(int)blockIdx.x, 0}, here{(int)blockIdx.x, 0};
+        const int total = p.only_state ? 0 : count_chunks(p);
         bool ok = true;
-        auto issue_scores = [&](uint32_t n) {
-            if (!wait_tile(3 * n) || !wait_tile(3 * n + 1)) return false;
-            tc_fence_after();
-            const uint32_t a = lower(tile(3 * n), 16), x = lower(tile(3 * n + 1), 16);
-            const uint32_t to = tmem + n % kSets * 128;
-            if (elect_one()) {
-#pragma unroll 1
-                for (int s = 0; s < steps; ++s)
-                    product_ss(to, x + by_channel(s), a + by_channel(s), scores, s > 0);
-                mma_commit(of(s_ready, n));
+        // with two sets the scores of a chunk go ahead of the last chunk's outputs
+        for (int m = 0; ok && m < total + (int)kSets - 1; ++m) {
+            if (m < total) {
+                const uint32_t n = m;
+                // (the scores go over the W o scores that an earlier product has read: nothing orders the two
+                // but its end)
+                ok = wait_tile(3 * n) && wait_tile(3 * n + 1) && (n < kSets || wait_chunk(y_ready, n - kSets));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a = lower(tile(3 * n), 16), q = lower(tile(3 * n + 1), 16);
+                const uint32_t to = tmem + n % kSets * 128;
+                if (elect_one()) {
+#pragma unroll
+                    for (int s = 0; s < TK / 16; ++s)
+                        if (s < steps) product_ss(to, q + by_channel(s), a + by_channel(s), scores, s > 0);
+                    mma_commit(of(s_ready, n));
+                }
+                __syncwarp();
             }
-            __syncwarp();
-            return true;
-        };
-        if (!p.only_state) {
-            if (kSets == 2 && next_chunk(p, units, ahead)) ok = issue_scores(0);
-            for (uint32_t n = 0; ok && next_chunk(p, units, here); ++n) {
-                if (kSets == 1) ok = issue_scores(n);
-                else if (next_chunk(p, units, ahead)) ok = issue_scores(n + 1);
-                ok = ok && wait_chunk(v_ready, n) && wait_chunk(p_ready, n) &&
+            if (m >= (int)kSets - 1) {
+                const uint32_t n = m - (kSets - 1);
+                ok = wait_chunk(v_ready, n) && wait_chunk(p_ready, n) &&
                      (n == 0 || wait_chunk(y_free, n - 1));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t v = lower(tile(3 * n + 2), kAtomBytes), w = tmem + n % kSets * 128;
                 if (elect_one()) {
-#pragma unroll 2
+#pragma unroll
                     for (int s = 0; s < kChunk / 16; ++s)
                         product_ts(tmem + C::kColY, w + s / 4 * 64 + s % 4 * 8, v + by_row(s), outs, s > 0);
                     mma_commit(of(y_ready, n));
@@ -390,24 +436,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t states = idesc_bf16_f32(128, 16, true, true) + ((uint32_t)(width / 8 - 2) << 17);
         const uint32_t outs = idesc_bf16_f32(128, 16, false, true) + ((uint32_t)(width / 8 - 2) << 17);
         const uint32_t s0 = lower(smem_u32(st), TK * 128);
-        Cursor here{(int)blockIdx.x, 0};
+        const uint32_t total = count_chunks(p);
         bool ok = true;
-        for (uint32_t n = 0; next_chunk(p, units, here); ++n) {
+        for (uint32_t n = 0; n < total; ++n) {
             ok = wait_tile(per * n) && (p.only_state || wait_tile(3 * n + 1)) &&
                  (p.only_state || n < kSets || wait_chunk(y_free, n - kSets)) && wait_chunk(v_ready, n) &&
                  wait_for(b_ready, n & 1, abort_flag, p.waits);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t a = lower(tile(per * n), kAtomBytes), x = lower(tile(3 * n + 1), 16);
+            const uint32_t a = lower(tile(per * n), kAtomBytes), q = lower(tile(3 * n + 1), 16);
             const uint32_t v = lower(smem_u32(vw + n % kSets * C::kVw), kAtomBytes);
             const uint32_t to = tmem + C::kColX + n % kSets * TV;
             // (where TK is 64, A^T's rows from 64 on are whatever lies behind the tile: they are not used)
             if (elect_one()) {
                 if (!p.only_state)
-#pragma unroll 1
-                    for (int s = 0; s < steps; ++s)
-                        product_ss(to, x + by_channel(s), s0 + by_row(s), outs, s > 0);
-#pragma unroll 2
+#pragma unroll
+                    for (int s = 0; s < TK / 16; ++s)
+                        if (s < steps) product_ss(to, q + by_channel(s), s0 + by_row(s), outs, s > 0);
+#pragma unroll
                 for (int s = 0; s < kChunk / 16; ++s)
                     product_ss(tmem + C::kColS, a + by_row(s), v + by_row(s), states, 1u);
                 mma_commit(of(u_ready, n));
@@ -419,36 +465,65 @@ __global__ void __launch_bounds__(kThreads, 1)
         wait_for(done, 0, abort_flag, p.waits);
         if (!ok) linger();
     } else if (warp == 3) {
-        // (no role: the next four warps begin a warpgroup, whose warps are TMEM's four quarters)
+        // ------------------------------------------------------------ stores of staged outputs
+        // (a barrier a slot, which is released once it is stored: the outputs may be several chunks ahead)
+        uint32_t n = 0, phases = 0;
+        bool ok = true;
+        begin_feed(p, blockIdx.x, feed);
+        while (ok && !p.only_state && next_piece(p, feed, here)) {
+            const Piece x = here;
+            const int b = p.cuts ? 0 : x.sequence, h = x.h;
+            for (int c = x.c0; c < x.c1; ++c, ++n) {
+                int rows;
+                const int token = chunk_at(p, x, c, rows);
+                if (!staged(p, rows)) continue;
+                const uint32_t slot = (3 * n + 2) % kSlots;
+                ok = wait_for(out0 + 8u * slot, phases >> slot & 1, abort_flag, p.waits);
+                if (!ok) break;
+                phases ^= 1u << slot;
+                if (elect_one()) {
+                    const uint32_t from = tile(3 * n + 2);
+#pragma unroll
+                    for (int t = 0; t < TV / 64; ++t)
+                        if (64 * t < p.Dv) tma_store_4d(&tY, from + t * kAtomBytes, 64 * t, token, h, b);
+                    bulk_commit();
+                    bulk_wait_read();
+                    mbar_arrive_n(empty0 + 8u * ((3 * n + 2) % kSlots), 2);
+                }
+                __syncwarp();
+            }
+        }
+        if (elect_one()) bulk_wait_all();
+        __syncwarp();
     } else if (warp < 12) {
         // ------------------------------------------------------------ scores
         // Two warps share 32 tokens: one takes the keys 0 to 63, the other 64 to 127, 16 at a time, each
         // writing over columns that it has read itself.
         const int q = warp & 3, half = (warp - 4) >> 2, i = 32 * q + lane;  // the thread's token in the chunk
         const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + 64 * half;
-        uint32_t n = 0, pieces = 0;
+        // its keys that count: from `low` to before `high`, whole sixteens
+        const int edge = min(max(32 * q - 64 * half, 0), 64);
+        const int low = p.back ? edge : 0, high = p.back ? 64 : min(max(32 * q + 32 - 64 * half, 0), 64);
+        uint32_t n = 0;
         bool ok = true;
-        for (int u = blockIdx.x; !p.only_state && u < units && ok; u += gridDim.x) {
-            const int item = u / p.Hq;
-            const Piece x = piece_of(p, item);
-            const int total = chunks_of(p, x);
-            if (total == 0) continue;
-            // The head's powers of g by gap, 0 for gaps below 0, in the order in which keys take them. A warp
-            // that fills a table knows that all have left it: they have filled the other one since.
-            float* table = powers + (pieces & 1) * kTable;
-            {
-                const float lg = head_decay(p, u - item * p.Hq, false);
-                const int k = threadIdx.x - 128, gap = p.back ? k - 32 : 127 - k;
-                if (k < kTable) table[k] = gap < 0 ? 0.f : exp2f(lg * gap) * p.scale_p;
-            }
-            mbar_arrive(t_ready);
-            ok = wait_for(t_ready, pieces & 1, abort_flag, p.waits);
-            ++pieces;
-            if (!ok) break;
-            const float* mine = table + (p.back ? 32 - i : 127 - i) + 64 * half;
-            for (int k = 0; k < total; ++k, ++n) {
+        begin_feed(p, blockIdx.x, feed);
+        while (ok && !p.only_state && next_piece(p, feed, here)) {
+            const Piece x = here;
+            const float lg = head_decay(p, x.h, false);
+            // Powers of g along the keys, from the gaps of the first two on: times g^2 for each next two keys
+            // backwards, times g^-2 forwards. (On the diagonal gaps may be below 0: those keys do not
+            // count.) From g = 1/2 on the first power, g^127 at least, is one that float32 holds; below
+            // that each takes an exponential of its own. A table of powers in shared memory, which
+            // the products' operands come from too, took longer than the chain.
+            const float way = p.back ? lg : -lg;
+            const int gap0 = p.back ? 64 * half + low - i : i - 64 * half - low;
+            const bool gentle = lg > -1.01f;
+            const float g2 = gentle ? exp2f(2.f * way) : 1.f;
+            const uint64_t next = pair(g2, g2);
+            const uint64_t first = pair(exp2f(lg * gap0) * p.scale_p, exp2f(lg * gap0 + way) * p.scale_p);
+            for (int c = x.c0; c < x.c1; ++c, ++n) {
                 int rows;
-                chunk_at(p, x, k, total, rows);
+                chunk_at(p, x, c, rows);
                 const uint32_t from = at + n % kSets * 128;
                 ok = wait_chunk(s_ready, n);
                 if (!ok) break;
@@ -457,32 +532,45 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive(empty0 + 8u * (3 * n % kSlots));
                     mbar_arrive(empty0 + 8u * ((3 * n + 1) % kSlots));
                 }
+                uint64_t f = first;
 #pragma unroll 1
-                for (int c = 0; c < 64; c += 16) {
-                    const int key = 64 * half + c;
-                    uint32_t w[8];
-                    if (p.back ? key + 15 < 32 * q : key > 32 * q + 31) {
+                for (int t = low; t < high; t += 16) {
+                    const int key = 64 * half + t;
+                    uint32_t r[16], w[8];
+                    tmem_ld16(from + t, r);
+                    tmem_wait_ld16(r);
+                    if (gentle) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) w[j] = 0;
+                        for (int j = 0; j < 16; j += 2, f = mul2(f, next))
+                            w[j / 2] =
+                                pack_bf16x2(mul2(pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), f));
                     } else {
-                        uint32_t r[16];
-                        tmem_ld16(from + c, r);
-                        tmem_wait_ld16(r);
-                        const float* g = mine + c;
+                        const int gap = p.back ? key - i : i - key;
 #pragma unroll
-                        for (int j = 0; j < 16; j += 2)
-                            w[j / 2] = pack_bf16x2(mul2(
-                                pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), pair(g[j], g[j + 1])));
-                        // on the diagonal, and in a chunk that ends early, what does not count is 0
-                        // whatever it was
-                        if ((key >> 5) == q || key + 16 > rows) {
-                            const int low = p.back ? i - key : 0;
-                            const int high = min(p.back ? 16 : i + 1 - key, rows - key);
-                            keep_keys(w, (high >= 16 ? 0xffffu : high <= 0 ? 0u : (1u << high) - 1u) &
-                                             (low <= 0 ? ~0u : low >= 16 ? 0u : ~0u << low));
-                        }
+                        for (int j = 0; j < 16; ++j)
+                            r[j] = __float_as_uint(
+                                __uint_as_float(r[j]) *
+                                (exp2f(lg * max(p.back ? gap + j : gap - j, 0)) * p.scale_p));
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) w[j] = bf16_bits(r[2 * j], r[2 * j + 1]);
                     }
-                    tmem_st8(from + c / 2, w);
+                    // on the diagonal, and in a chunk that ends early, what does not count is 0
+                    // whatever it was
+                    if ((key >> 5) == q || key + 16 > rows) {
+                        const int least = p.back ? i - key : 0;
+                        const int most = min(p.back ? 16 : i + 1 - key, rows - key);
+                        keep_keys(w, (most >= 16 ? 0xffffu : most <= 0 ? 0u : (1u << most) - 1u) &
+                                         (least <= 0 ? ~0u : least >= 16 ? 0u : ~0u << least));
+                    }
+                    tmem_st8(from + t / 2, w);
+                }
+                {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = 0;
+#pragma unroll 1
+                    for (int t = p.back ? 0 : high; t < (p.back ? low : 64); t += 16)
+                        tmem_st8(from + t / 2, w);
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -495,24 +583,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t at = tmem + ((uint32_t)(32 * q) << 16);
         uint32_t n = 0;
         bool ok = true;
-        for (int u = blockIdx.x; !p.only_state && u < units && ok; u += gridDim.x) {
-            const int item = u / p.Hq;
-            const int h = u - item * p.Hq;
-            const Piece x = piece_of(p, item);
-            const int total = chunks_of(p, x), b = p.pieces ? 0 : x.sequence;
-            if (total == 0) continue;
+        begin_feed(p, blockIdx.x, feed);
+        while (ok && !p.only_state && next_piece(p, feed, here)) {
+            const Piece x = here;
+            const int b = p.cuts ? 0 : x.sequence, h = x.h;
             const float lg = head_decay(p, h, false);
-            for (int k = 0; k < total; ++k, ++n) {
+            for (int k = x.c0; k < x.c1; ++k, ++n) {
                 int rows;
-                const int token = chunk_at(p, x, k, total, rows);
+                const int token = chunk_at(p, x, k, rows);
                 const int since = p.back ? rows - 1 - i : i;
                 const float f = i < rows ? exp2f(lg * (since + p.lead)) * p.scale_r : 0.f;
                 const int64_t to = b * p.yb + h * p.yh + (int64_t)(token + i) * p.yn;
                 ok = wait_chunk(u_ready, n) && wait_chunk(y_ready, n);
                 if (!ok) break;
                 tc_fence_after();
-                if (threadIdx.x == 384)  // V has been read, by the warps that decay it and by its product
-                    mbar_arrive_n(empty0 + 8u * ((3 * n + 2) % kSlots), 2);
+                // V has been read, by the warps that decay it and by its product: the outputs go over it, from
+                // where whole lines are stored. (Stores of a thread's own row, 16 bytes of 32 lines an
+                // instruction, held up the state's through the pipe that they share: 241 us instead of 229
+                // for the prefill.)
+                const bool staging = staged(p, rows);
+                uint8_t* stage = smem + (3 * n + 2) % kSlots * C::kSlot + i * 128;
+                if (!staging && threadIdx.x == 384) mbar_arrive_n(empty0 + 8u * ((3 * n + 2) % kSlots), 2);
 #pragma unroll 1
                 for (int c = 0; c < p.Dv; c += 16) {
                     uint32_t y[16], s[16];
@@ -523,7 +614,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         y[j] = __float_as_uint(fmaf(__uint_as_float(s[j]), f, __uint_as_float(y[j])));
-                    if (i < rows) {
+                    if (staging) {
+                        uint8_t* d = stage + c / 64 * kAtomBytes;
+                        const int piece = c % 64 / 8;
+                        *reinterpret_cast<uint4*>(d + 16 * (piece ^ (i & 7))) =
+                            make_uint4(bf16_bits(y[0], y[1]), bf16_bits(y[2], y[3]), bf16_bits(y[4], y[5]),
+                                       bf16_bits(y[6], y[7]));
+                        *reinterpret_cast<uint4*>(d + 16 * ((piece + 1) ^ (i & 7))) =
+                            make_uint4(bf16_bits(y[8], y[9]), bf16_bits(y[10], y[11]),
+                                       bf16_bits(y[12], y[13]), bf16_bits(y[14], y[15]));
+                    } else if (i < rows) {
                         const bool both = c + 8 < p.Dv;
                         if (p.y_f32) {
                             uint4* d = reinterpret_cast<uint4*>((float*)p.y + to + c);
@@ -544,6 +644,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tc_fence_before();
                 mbar_arrive(of(y_free, n));
+                if (staging) {
+                    fence_proxy_async();
+                    mbar_arrive(out0 + 8u * ((3 * n + 2) % kSlots));
+                }
             }
         }
     } else if (warp < 20) {
@@ -553,19 +657,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + C::kColS;
         uint32_t n = 0;
         bool ok = true;
-        for (int u = blockIdx.x; 32 * q < TK && u < units && ok; u += gridDim.x) {
-            const int item = u / p.Hq;
-            const int h = u - item * p.Hq;
-            const Piece x = piece_of(p, item);
-            const int total = chunks_of(p, x);
-            const int64_t own = (int64_t)u * p.Da * p.Dv + (int64_t)row * p.Dv;
-            const int64_t kept = ((int64_t)x.sequence * p.Hq + h) * p.Da * p.Dv + row * p.row_stride;
-            const float lg = head_decay(p, h, row == 0);
-            if (p.only_state && ends(p, x)) continue;
+        begin_feed(p, blockIdx.x, feed);
+        while (32 * q < TK && ok && next_walked(p, feed, here)) {
+            const Piece x = here;
+            const int64_t own = ((int64_t)blockIdx.x * p.Da + row) * p.Dv;
+            const int64_t kept = ((int64_t)x.sequence * p.Hq + x.h) * p.Da * p.Dv + row * p.row_stride;
+            const float lg = head_decay(p, x.h, row == 0);
             if (keeps) {  // the state in front of the piece
                 const float* from = nullptr;
                 int64_t step = 1;
-                if (!p.only_state && p.slots) {
+                if (!p.only_state && x.c0 > 0) {
                     from = p.slots + own;
                 } else if (!p.only_state && p.state) {
                     from = p.state + kept;
@@ -582,9 +683,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tmem_wait_st();
             }
-            for (int k = 0; k < total; ++k, ++n) {
+            for (int k = x.c0; k < x.c1; ++k, ++n) {
                 int rows;
-                chunk_at(p, x, k, total, rows);
+                chunk_at(p, x, k, rows);
                 if (keeps) {
                     const float g = exp2f(lg * rows);
                     const uint64_t g2 = pair(g, g);
@@ -632,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             int64_t step = 1;
             if (p.only_state) {
                 to = p.slots_out + own;
-            } else if (p.state_out && ends(p, x)) {
+            } else if (p.state_out && x.c1 == x.total) {
                 to = p.state_out + kept;
                 step = p.col_stride;
             }
@@ -656,23 +757,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int shift = width > 32 ? 3 : 2, turns = 1 << shift;  // tokens of the thread
         uint32_t n = 0;
         bool ok = true;
-        for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-            const int item = u / p.Hq;
-            const Piece x = piece_of(p, item);
-            const int total = chunks_of(p, x);
-            if (total == 0) continue;
-            const float lg = head_decay(p, u - item * p.Hq, false);
+        begin_feed(p, blockIdx.x, feed);
+        while (ok && next_walked(p, feed, here)) {
+            const Piece x = here;
+            const float lg = head_decay(p, x.h, false);
             // Of a whole chunk the thread takes a 16-byte piece of every 16th (or 32nd) token, from the one
             // with the largest weight on: each next one's is `ratio` times the last's.
             const int stride = 128 >> shift, r0 = p.back ? maker >> shift : 127 - (maker >> shift);
             const float heaviest = exp2f(lg * (p.back ? r0 + 1 - p.lead : kChunk - p.lead - r0)) * p.scale_w;
             const float ratio = exp2f(lg * stride);
-            for (int k = 0; k < total; ++k, ++n) {
+            for (int k = x.c0; k < x.c1; ++k, ++n) {
                 int rows;
-                chunk_at(p, x, k, total, rows);
+                chunk_at(p, x, k, rows);
                 const uint32_t ia = per * n, iv = ia + per - 1;
-                // the buffer's last product is done, and whoever waited for its last filling has seen it
-                ok = wait_tile(iv) && (rows == kChunk || wait_tile(ia)) &&
+                // All tiles in order, though most chunks' V is all that is read: a slot's phase tells odd from
+                // even fillings only, so each one of them has to be seen. Then: the buffer's last product is
+                // done, and whoever waited for its last filling has seen it.
+                ok = wait_tile(ia) && (p.only_state || wait_tile(ia + 1)) && wait_tile(iv) &&
                      (n < kSets || wait_chunk(u_ready, n - kSets)) &&
                      (n < 2 || p.only_state || wait_chunk(y_ready, n - 2));
                 if (!ok) break;
@@ -719,19 +820,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ------------------------------------------------------------------ packed sequences
-// One block: the cuts, brought into 0 to N and never falling (each at least the largest before it), the
-// first piece of every sequence, and the pieces.
+// One block: the cuts, brought into 0 to N and never falling (each at least the largest before it), and the
+// chunks before every sequence (one at least for each, so that an empty one has a place in the list).
 constexpr int kCutThreads = 1024;
 __global__ void __launch_bounds__(kCutThreads)
-    cut_kernel(const int32_t* offsets, int sequences, int N, int piece_rows, Piece* pieces, int* first,
-               int* cuts, int* status) {
-    __shared__ int sm[kCutThreads / 32];
+    cut_kernel(const int32_t* offsets, int sequences, int N, int* first, int* cuts, int* status) {
+    __shared__ int sm[2][kCutThreads / 32];
     tc::pdl_trigger();
     tc::pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     bool bad = false;
-    int base = 0, total = 0;
-    // the largest so far, 1,024 offsets at a time
+    int base = 0, total = 0;  // the largest cut, the chunks so far
     for (int s0 = 0; s0 <= sequences; s0 += kCutThreads) {
         const int s = s0 + threadIdx.x;
         const int raw = s <= sequences ? offsets[s] : 0;
@@ -740,50 +839,36 @@ __global__ void __launch_bounds__(kCutThreads)
             const int o = __shfl_up_sync(0xffffffffu, v, d);
             if (lane >= d) v = max(v, o);
         }
-        if (lane == 31) sm[warp] = v;
+        if (lane == 31) sm[0][warp] = v;
         __syncthreads();
-        int before = base;
-        for (int w = 0; w < warp; ++w) before = max(before, sm[w]);
-        v = max(v, before);
+        for (int w = 0; w < kCutThreads / 32; ++w) {
+            if (w == warp) v = max(v, base);
+            base = max(base, sm[0][w]);
+        }
         if (s <= sequences) {
             cuts[s] = v;
             bad = bad || v != raw;
         }
-        for (int w = 0; w < kCutThreads / 32; ++w) base = max(base, sm[w]);
         __syncthreads();
     }
     if (bad) record_status(status, FLAREPP_ERR_INVALID_ARGUMENT);
-    // the sums of the pieces so far
     for (int s0 = 0; s0 < sequences; s0 += kCutThreads) {
         const int s = s0 + threadIdx.x;
-        int start = 0, rows = 0, n = 0;
-        if (s < sequences) {
-            start = cuts[s];
-            rows = cuts[s + 1] - start;
-            n = max(1, (rows + piece_rows - 1) / piece_rows);
-        }
+        const int n = s < sequences ? max(1, (cuts[s + 1] - cuts[s] + kChunk - 1) / kChunk) : 0;
         int v = n;
         for (int d = 1; d < 32; d <<= 1) {
             const int o = __shfl_up_sync(0xffffffffu, v, d);
             if (lane >= d) v += o;
         }
-        if (lane == 31) sm[warp] = v;
+        if (lane == 31) sm[1][warp] = v;
         __syncthreads();
-        int at = total + v - n;
-        for (int w = 0; w < warp; ++w) at += sm[w];
-        for (int w = 0; w < kCutThreads / 32; ++w) total += sm[w];
-        __syncthreads();
-        if (s < sequences) {
-            first[s] = at;
-            for (int k = 0; k < n; ++k) {
-                Piece x;
-                x.start = start + k * piece_rows;
-                x.rows = min(piece_rows, rows - k * piece_rows);
-                x.sequence = s;
-                x.flags = (k == 0 ? kFirst : 0) | (k == n - 1 ? kLast : 0);
-                pieces[at + k] = x;
-            }
+        int at = v - n;
+        for (int w = 0; w < kCutThreads / 32; ++w) {
+            if (w == warp) at += total;
+            total += sm[1][w];
         }
+        if (s < sequences) first[s] = at;
+        __syncthreads();
     }
     if (threadIdx.x == 0) first[sequences] = total;
 }
@@ -804,52 +889,55 @@ __global__ void __launch_bounds__(256)
 }
 
 // ------------------------------------------------------------------ the join over a sequence's pieces
-// In: the state that every piece but a sequence's last leaves from nothing; out, in place: the state in
-// front of every piece. A thread follows one value of a state, kAhead pieces' values in flight.
-struct Join {
-    int Hq, N, Da, Dv, back;
-    const Piece* pieces;
-    const int* first;
-    int per_sequence, piece_rows;
-    const float* log_decay;
-    const float* state;
-    int64_t row_stride, col_stride;
-    float* slots;
-};
-__global__ void __launch_bounds__(256) join_kernel(const Join p, int blocks_per_state) {
+// In: the state that a block's last piece leaves from nothing, for blocks whose last piece's sequence goes on
+// in the next block. Out, in place: the state in front of every block's first chunk. A group of blocks
+// (blockIdx.y) follows the sequence that begins in walk block y and goes on in the next, a thread one
+// value of the state, kAhead blocks' values in flight.
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk p, const float* left, float* slots,
+                                                   int blocks) {
     tc::pdl_trigger();
     tc::pdl_wait();
     constexpr int kAhead = 8;
-    const int64_t sh = blockIdx.x / blocks_per_state;
-    const int e = (int)(blockIdx.x - sh * blocks_per_state) * 256 + threadIdx.x, size = p.Da * p.Dv;
-    if (e >= size) return;
-    const int64_t s = sh / p.Hq;
-    const int h = (int)(sh - s * p.Hq);
+    const int e = blockIdx.x * 256 + threadIdx.x, size = p.Da * p.Dv, y = blockIdx.y;
+    // the last place of walk block y, and the sequence's head there
+    Walk q = p;
+    const int all = places_before(q, q.sequences);
+    const int share = q.share ? q.share : (all + blocks - 1) / blocks;
+    const int end = min((y + 1) * share, all);
+    if (end >= all || y * share >= end) return;
+    int low = 0, high = q.sequences;
+    while (high - low > 1) {
+        const int mid = (low + high) / 2;
+        if (places_before(q, mid) <= end - 1) low = mid;
+        else high = mid;
+    }
+    const int each = places_of(q, low), before = places_before(q, low), h = (end - 1 - before) / each;
+    const int base = before + h * each;
+    if (base < y * share || base + each <= end || e >= size) return;  // begun before, or all here
     bool bad = false;
-    const float lg = decay_log2(p.log_decay[h], &bad);
-    const int64_t i0 = p.pieces ? p.first[s] : s * p.per_sequence;
-    const int n = p.pieces ? p.first[s + 1] - (int)i0 : p.per_sequence;
-    const int r = e / p.Dv, c = e - r * p.Dv;
-    float run = p.state ? p.state[sh * size + r * p.row_stride + c * p.col_stride] : 0.f;
-    for (int k0 = 0; k0 < n; k0 += kAhead) {
-        float v[kAhead], g[kAhead];
+    const float lg = decay_log2(q.log_decay[h], &bad);
+    int start;
+    const int tokens = tokens_of(q, low, start);
+    // tokens of the places base + c0 to base + c1, as walked
+    const int total = (tokens + kChunk - 1) / kChunk, ragged = total * kChunk - tokens;
+    auto rows_of = [&](int c0, int c1) {
+        const bool holds = q.back ? c0 == 0 : c1 == total;  // the chunk that ends early
+        return (c1 - c0) * kChunk - (holds ? ragged : 0);
+    };
+    const int r = e / q.Dv, c = e - r * q.Dv;
+    float run = q.state ? q.state[((int64_t)low * q.Hq + h) * size + r * q.row_stride + c * q.col_stride] : 0.f;
+    const int last = (base + each - 1) / share;  // the walk block that ends the sequence
+    for (int k0 = y; k0 < last; k0 += kAhead) {
+        float v[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (k0 + j < last) v[j] = left[(int64_t)(k0 + j) * size + e];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int k = k0 + j;
-            if (k >= n) break;
-            const int pos = p.back ? n - 1 - k : k;
-            v[j] = k < n - 1 ? p.slots[((i0 + pos) * p.Hq + h) * size + e] : 0.f;
-            const int rows = p.pieces ? p.pieces[i0 + pos].rows
-                                      : min(p.piece_rows, p.N - pos * p.piece_rows);
-            g[j] = exp2f(lg * rows);
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int k = k0 + j;
-            if (k >= n) break;
-            const int pos = p.back ? n - 1 - k : k;
-            p.slots[((i0 + pos) * p.Hq + h) * size + e] = run;
-            run = fmaf(g[j], run, v[j]);
+            if (k >= last) break;
+            run = fmaf(exp2f(lg * rows_of(max(k * share - base, 0), (k + 1) * share - base)), run, v[j]);
+            slots[(int64_t)(k + 1) * size + e] = run;
         }
     }
 }
@@ -923,7 +1011,7 @@ bool map_of(CUtensorMap* m, const flarepp_heads& t, int64_t B, int64_t H, int64_
 }
 
 template <int TK, int TV>
-cudaError_t launch_walk(const CUtensorMap* m, const Walk& p, int64_t units, cudaStream_t st) {
+cudaError_t launch_walk(const CUtensorMap* m, const Walk& p, int64_t blocks, cudaStream_t st) {
     using C = Cfg<TK, TV>;
     auto kernel = walk_kernel<TK, TV>;
     static std::atomic<uint64_t> ready{0};  // devices whose shared-memory limit is raised
@@ -936,7 +1024,7 @@ cudaError_t launch_walk(const CUtensorMap* m, const Walk& p, int64_t units, cuda
         if (e != cudaSuccess) return e;
         ready.fetch_or(uint64_t(1) << dev);
     }
-    return launch(kernel, units < kNumSMs ? units : kNumSMs, kThreads, C::kSmem, st, m[0], m[1], m[2], p);
+    return launch(kernel, blocks, kThreads, C::kSmem, st, m[0], m[1], m[2], m[3], p);
 }
 
 cudaError_t launch_for(const CUtensorMap* m, const Walk& p, int64_t units, cudaStream_t st) {
@@ -949,33 +1037,27 @@ cudaError_t launch_for(const CUtensorMap* m, const Walk& p, int64_t units, cudaS
 
 cudaError_t take_decay_status(int32_t* out, cudaStream_t st) { return take_library_status(out, st); }
 
-// Where sequences and heads fill the card, a piece is a sequence; otherwise the cut is the one
-// whose blocks have the least to do, a chunk of a cut sequence counting for the walk and for the
-// states' (half as much). Lengths of packed sequences are not known here: pieces for twice the card.
+// Each of the card's blocks walks an equal part of the list of all sequences' heads' chunks, so that a sequence
+// may be cut between two blocks or more, which costs a first walk over what lies in front of the cuts
+// (half a walk's time a chunk) and two launches; or the list is one of whole sequences' heads, and nothing is cut.
+// The cheaper one by the chunks that the busiest block has to do. (Lengths of packed sequences are not known
+// here: they are cut unless even the longest possible one is short.)
 DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
     DecayPlan p{};
     p.sequences = s.sequences ? s.sequences : s.B;
-    const int64_t all = cdiv(s.N, kChunk), slots = kNumSMs;
+    p.chunks = cdiv(s.N, kChunk);
+    const int64_t heads = p.sequences * s.Hq;
     if (s.sequences) {
-        const int64_t per = cdiv(all * s.Hq, 2 * slots);
-        p.chunks = per < 4 ? 4 : per;
-        if (p.chunks > all) p.chunks = all;
-        p.per_sequence = 0;
-        p.pieces = s.sequences + all / p.chunks;
-        p.split = p.chunks < all;
+        p.whole = p.chunks <= 4;
+        p.blocks = p.whole && heads < kNumSMs ? heads : kNumSMs;
+        p.share = p.whole ? cdiv(heads, p.blocks) : 0;
     } else {
-        const int64_t heads = p.sequences * s.Hq;
-        int64_t best = 1;
-        double least = 0.0;
-        for (int64_t n = 1; n <= all && (n == 1 || n * heads <= 4 * slots); ++n) {
-            const double cost =
-                (double)cdiv(heads * n, slots) * (double)cdiv(all, n) * (n > 1 ? 1.5 : 1.0) + (n > 1 ? 4 : 0);
-            if (n == 1 || cost < least) least = cost, best = n;
-        }
-        p.chunks = cdiv(all, best);
-        p.per_sequence = cdiv(all, p.chunks);
-        p.pieces = p.sequences * p.per_sequence;
-        p.split = p.per_sequence > 1;
+        const int64_t whole = cdiv(heads, kNumSMs);          // heads of the busiest block
+        const int64_t cut = cdiv(heads * p.chunks, kNumSMs);  // chunks of every block
+        const double first = 0.5 * (double)(cut < p.chunks ? cut : p.chunks);
+        p.whole = (double)(whole * p.chunks) <= (double)cut + first + 4;
+        p.share = p.whole ? whole : cut;
+        p.blocks = cdiv(p.whole ? heads : heads * p.chunks, p.share);
     }
     size_t at = 0;
     auto place = [&](size_t bytes) {
@@ -984,11 +1066,13 @@ DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
         return here;
     };
     if (s.sequences) {
-        p.off_pieces = place(p.pieces * sizeof(Piece));
         p.off_first = place((p.sequences + 1) * 4);
         p.off_cuts = place((p.sequences + 1) * 4);
     }
-    if (p.split) p.off_states = place((size_t)p.pieces * s.Hq * s.Dk * s.Dv * 4);
+    if (!p.whole) {
+        p.off_left = place((size_t)p.blocks * s.Dk * s.Dv * 4);
+        p.off_slots = place((size_t)p.blocks * s.Dk * s.Dv * 4);
+    }
     if (backward && s.Hq != s.Hk)
         p.off_sums = place((size_t)s.B * s.Hq * s.N * (s.Dk > s.Dv ? s.Dk : s.Dv) * 4);
     p.total = at;
@@ -998,8 +1082,7 @@ DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
 cudaError_t decay_cut(const flarepp_decay_shape& s, const DecayPlan& p, const int32_t* offsets, char* ws,
                       int32_t* status, cudaStream_t st) {
     return launch(cut_kernel, 1, kCutThreads, 0, st, offsets, (int)s.sequences, (int)s.N,
-                  (int)(p.chunks * kChunk), (Piece*)(ws + p.off_pieces), (int*)(ws + p.off_first),
-                  (int*)(ws + p.off_cuts), (int*)status);
+                  (int*)(ws + p.off_first), (int*)(ws + p.off_cuts), (int*)status);
 }
 
 cudaError_t decay_blank(const flarepp_decay_shape& s, const DecayPlan& p, char* ws, const flarepp_heads& y,
@@ -1015,7 +1098,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
     Walk p{};
     p.Hq = (int)s.Hq, p.N = (int)s.N, p.Da = (int)w.Da, p.Dv = (int)w.Dv;
     p.back = w.back;
-    CUtensorMap m[3];
+    CUtensorMap m[4];
     const DecayOperand* of[3] = {&w.x, &w.a, &w.v};
     int* const group[3] = {&p.gx, &p.ga, &p.gv};
     int* const batch[3] = {&p.mx, &p.ma, &p.mv};
@@ -1026,13 +1109,19 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         *group[i] = own_head ? (int)(s.Hq / of[i]->heads) : 0;
         *batch[i] = own_batch;
     }
-    if (s.sequences) {
-        p.pieces = (const Piece*)(ws + plan.off_pieces);
-        p.count = (const int*)(ws + plan.off_first) + s.sequences;
+    m[3] = m[2];  // (float32 outputs are not staged)
+    if (!w.y32) {
+        bool own_head, own_batch;
+        if (!map_of(&m[3], *w.y, s.B, s.Hq, s.N, w.Dv, &own_head, &own_batch)) return cudaErrorInvalidValue;
     }
-    p.n_pieces = (int)plan.pieces;
-    p.per_sequence = (int)plan.per_sequence;
-    p.piece_rows = (int)(plan.chunks * kChunk);
+    if (s.sequences) {
+        p.cuts = (const int*)(ws + plan.off_cuts);
+        p.first = (const int*)(ws + plan.off_first);
+    }
+    p.whole = plan.whole;
+    p.sequences = (int)plan.sequences;
+    p.chunks = (int)plan.chunks;
+    p.share = (int)plan.share;
     p.lead = w.back ? 0 : 1;
     p.scale_p = s.scale;
     p.scale_w = w.back ? s.scale : 1.f;
@@ -1049,33 +1138,31 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
     p.col_stride = w.turned ? w.Da : 1;
     p.waits.status = w.status;
     test_fault_for(kDecayKernel, &p.waits.limit_ns, &p.waits.withheld);
-    const int64_t units = plan.pieces * s.Hq;
-    if (units > INT32_MAX - kNumSMs) return cudaErrorInvalidValue;
-    cudaError_t e;
-    if (plan.split) {
-        float* slots = (float*)(ws + plan.off_states);
+    p.state = w.state;
+    cudaError_t e = cudaSuccess;
+    if (!plan.whole) {
+        float* left = (float*)(ws + plan.off_left);
+        float* slots = (float*)(ws + plan.off_slots);
         Walk first = p;
         first.only_state = 1;
-        first.slots_out = slots;
-        e = launch_for(m, first, units, st);
+        first.slots_out = left;
+        e = launch_for(m, first, plan.blocks, st);
         if (e != cudaSuccess) return e;
-        Join j{};
-        j.Hq = p.Hq, j.N = p.N, j.Da = p.Da, j.Dv = p.Dv, j.back = p.back;
-        j.pieces = p.pieces;
-        j.first = s.sequences ? (const int*)(ws + plan.off_first) : nullptr;
-        j.per_sequence = p.per_sequence, j.piece_rows = p.piece_rows;
-        j.log_decay = p.log_decay;
-        j.state = w.state;
-        j.row_stride = p.row_stride, j.col_stride = p.col_stride;
-        j.slots = slots;
-        const int blocks = (int)cdiv((int64_t)p.Da * p.Dv, 256);
-        e = launch(join_kernel, plan.sequences * s.Hq * blocks, 256, 0, st, j, blocks);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)cdiv((int64_t)p.Da * p.Dv, 256), (unsigned)plan.blocks);
+        cfg.blockDim = dim3(256);
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, join_kernel, p, (const float*)left, slots, (int)plan.blocks);
         if (e != cudaSuccess) return e;
         p.slots = slots;
     }
-    p.state = w.state;
     p.state_out = w.state_out;
-    return launch_for(m, p, units, st);
+    return launch_for(m, p, plan.blocks, st);
 }
 
 cudaError_t decay_group_sum(const flarepp_decay_shape& s, const float* sums, const flarepp_heads& y, int64_t D,
