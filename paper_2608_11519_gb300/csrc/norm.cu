@@ -30,8 +30,11 @@ namespace {
 using namespace vec;
 
 constexpr int kThreads = 256;
-constexpr int kRows = 8;      // rows that a thread of the forward's sums has in flight
-constexpr int kBackRows = 4;  // of the backward's: x and dy
+// Rows that a thread has in flight: of the forward's sums, and of the backward (x and dy).
+template <typename E, int W>
+constexpr int sum_rows() { return sizeof(E) * W >= 8 ? 8 : 16; }
+template <typename E, int W>
+constexpr int back_rows() { return sizeof(E) * W >= 8 ? 4 : 8; }
 constexpr int kFewRows = 4;
 constexpr int64_t kWsAlign = 256;
 
@@ -52,6 +55,7 @@ struct Norm {
     int* status;
     // threads: tx vectors of W channels by ty rows; tiles of tc = tx W channels
     int tx, ty, tc, tiles, segs;
+    int cell;           // channels that go into a group's sums as one: W, or 1 where groups cut vectors
     int b0, bn;         // samples of this launch
     int chunks, rows;   // chunks of rows a sample, rows of each
     int per;            // samples that a block of the sums takes (1 unless chunks is 1)
@@ -76,48 +80,72 @@ __device__ __forceinline__ float param(const void* t, int f32, int c, float none
 }
 
 // ---- the activation and its slope: 16-bit results from the linear layer's approximations in pairs,
-// 32-bit ones from the functions themselves
+// 32-bit ones from the functions themselves. The choice is outside the loops over a vector, whose values
+// then go through the exponentials together: inside them it took the backward of 65,536 rows of 256
+// 99 us instead of 56.
+// 1 / (1 + exp(-z)): the exponential's relative error is |z| 2^-24 and two units more, of which the result's
+// is a quarter at most.
+__device__ __forceinline__ float logistic(float z) {
+    return rcp_approx(1.f + ex2_approx(-1.44269504f * z));
+}
+template <int ACT, int W>
+__device__ __forceinline__ void value_pairs(float* z) {
+#pragma unroll
+    for (int i = 0; i < W; i += 2) {
+        const float2 v = halves(act_value2(ACT, pair(z[i], W > 1 ? z[(i + 1) % W] : 0.f)));
+        z[i] = v.x;
+        if (W > 1) z[(i + 1) % W] = v.y;
+    }
+}
+template <int ACT, int W>
+__device__ __forceinline__ void slope_pairs(float* z) {
+#pragma unroll
+    for (int i = 0; i < W; i += 2) {
+        const float2 v = halves(act_slope2(ACT, pair(z[i], W > 1 ? z[(i + 1) % W] : 0.f)));
+        z[i] = v.x;
+        if (W > 1) z[(i + 1) % W] = v.y;
+    }
+}
 template <typename E, int W>
 __device__ __forceinline__ void act_value(int act, float* z) {
-    if (act == FLAREPP_ACT_NONE) return;
-    if (std::is_same<E, float>::value) {
+    constexpr bool exact = std::is_same<E, float>::value;
+    if (act == FLAREPP_ACT_RELU) {
+        value_pairs<FLAREPP_ACT_RELU, W>(z);
+    } else if (act == FLAREPP_ACT_GELU) {
+        if (!exact) value_pairs<FLAREPP_ACT_GELU, W>(z);
+        else
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if (act == FLAREPP_ACT_RELU) z[i] = z[i] < 0.f ? 0.f : z[i];
-            else if (act == FLAREPP_ACT_GELU) z[i] *= normcdff(z[i]);
-            else z[i] /= 1.f + expf(-z[i]);
-        }
-    } else {
+            for (int i = 0; i < W; ++i) z[i] *= normcdff(z[i]);
+    } else if (act == FLAREPP_ACT_SILU) {
+        if (!exact) value_pairs<FLAREPP_ACT_SILU, W>(z);
+        else
 #pragma unroll
-        for (int i = 0; i < W; i += 2) {
-            const float2 v = halves(act_value2(act, pair(z[i], W > 1 ? z[(i + 1) % W] : 0.f)));
-            z[i] = v.x;
-            if (W > 1) z[(i + 1) % W] = v.y;
-        }
+            for (int i = 0; i < W; ++i) z[i] *= logistic(z[i]);
     }
 }
 // z becomes act'(z)
 template <typename E, int W>
 __device__ __forceinline__ void act_slope(int act, float* z) {
-    if (std::is_same<E, float>::value) {
+    constexpr bool exact = std::is_same<E, float>::value;
+    if (act == FLAREPP_ACT_RELU) {
+        slope_pairs<FLAREPP_ACT_RELU, W>(z);
+    } else if (act == FLAREPP_ACT_GELU) {
+        if (!exact) slope_pairs<FLAREPP_ACT_GELU, W>(z);
+        else
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if (act == FLAREPP_ACT_NONE) z[i] = 1.f;
-            else if (act == FLAREPP_ACT_RELU) z[i] = z[i] > 0.f ? 1.f : 0.f;
-            else if (act == FLAREPP_ACT_GELU)
+            for (int i = 0; i < W; ++i)
                 z[i] = normcdff(z[i]) + z[i] * 0.39894228f * expf(-0.5f * z[i] * z[i]);
-            else {
-                const float s = 1.f / (1.f + expf(-z[i]));
+    } else if (act == FLAREPP_ACT_SILU) {
+        if (!exact) slope_pairs<FLAREPP_ACT_SILU, W>(z);
+        else
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float s = logistic(z[i]);
                 z[i] = s * (1.f + z[i] * (1.f - s));
             }
-        }
     } else {
 #pragma unroll
-        for (int i = 0; i < W; i += 2) {
-            const float2 v = halves(act_slope2(act, pair(z[i], W > 1 ? z[(i + 1) % W] : 0.f)));
-            z[i] = v.x;
-            if (W > 1) z[(i + 1) % W] = v.y;
-        }
+        for (int i = 0; i < W; ++i) z[i] = 1.f;
     }
 }
 
@@ -139,6 +167,13 @@ __device__ __forceinline__ void segment(const Norm& p, int g, int c0, int c1, in
 __device__ __forceinline__ float2* slot(const Norm& p, int64_t b, int chunk, int g, int tile) {
     const int first = g * p.w / p.tc;
     return p.part + ((b * p.chunks + chunk) * p.G + g) * p.segs + (tile - first);
+}
+
+// Lanes that share a group of so many entries: a power of two, so that small groups share a warp.
+__device__ __forceinline__ int lanes_for(int entries) {
+    int n = 1;
+    while (n < 32 && n < entries) n *= 2;
+    return n;
 }
 
 // What a block is of a launch: a tile of channels, and a chunk of rows of a sample (or several samples).
@@ -165,8 +200,9 @@ __device__ __forceinline__ Place place_of(const Norm& p, int64_t block) {
 // ------------------------------------------------------------------ sums of the forward
 // Bound by reading X once: 8 rows of 16 bytes in flight a thread.
 template <typename E, int W>
-__global__ void __launch_bounds__(kThreads) stats_kernel(const Norm p) {
+__global__ void __launch_bounds__(kThreads, 4) stats_kernel(const Norm p) {
     __shared__ float sm[2][kThreads * W];
+    constexpr int kRows = sum_rows<E, W>();
     tc::pdl_trigger();
     tc::pdl_wait();
     const Place a = place_of<W>(p, blockIdx.x);
@@ -214,74 +250,137 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const Norm p) {
                 sq[i] = fmaf(d * d, q, sq[i]);
             }
         }
+        if (p.cell == W) {  // the vector's channels are one group's
+            float m = 0.f, q = 0.f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            sm[0][a.ty * p.tc + a.c - a.c0 + i] = mean[i];
-            sm[1][a.ty * p.tc + a.c - a.c0 + i] = sq[i];
+            for (int i = 0; i < W; ++i) m += mean[i];
+            m *= 1.f / W;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float d = mean[i] - m;
+                q += fmaf(d * d, (float)mine, sq[i]);
+            }
+            sm[0][a.ty * p.tx + a.tx] = m;
+            sm[1][a.ty * p.tx + a.tx] = q;
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                sm[0][a.ty * p.tc + a.c - a.c0 + i] = mean[i];
+                sm[1][a.ty * p.tc + a.c - a.c0 + i] = sq[i];
+            }
         }
     }
+    __shared__ float count[kThreads];
+    if (threadIdx.x < p.ty) count[threadIdx.x] = (float)(rows_of(rows, threadIdx.x, p.ty) * p.cell);
     __syncthreads();
-    // a warp takes a group: the mean of the means, then the squares about it
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int g = a.c0 / p.w + warp; g * p.w < a.c1; g += kThreads / 32) {
-        int from, to;
-        segment(p, g, a.c0, a.c1, from, to);
-        const int width = to - from;
+    // some lanes take a group: the mean of the means, then the squares about it
+    const int row = p.tc / p.cell, most = min(p.w, a.c1 - a.c0) / p.cell * p.ty;
+    const int lanes = lanes_for(most), lane = threadIdx.x % lanes;
+    const int g0 = a.c0 / p.w, groups = (a.c1 - 1) / p.w - g0 + 1;
+    for (int k = threadIdx.x / lanes; k - threadIdx.x % 32 / lanes < groups; k += kThreads / lanes) {
+        const int g = g0 + k;
+        int from = 0, to = 0;
+        if (k < groups) segment(p, g, a.c0, a.c1, from, to);
+        const int per = (to - from) / p.cell, at0 = (from - a.c0) / p.cell;
         float n = 0.f, m = 0.f;
-        for (int e = lane; e < width * p.ty; e += 32) {
-            const int y = e / width, at = y * p.tc + from - a.c0 + e - y * width;
-            const float k = (float)rows_of(rows, y, p.ty);
-            n += k;
-            m = fmaf(k, sm[0][at], m);
+        for (int e = lane; e < per * p.ty; e += lanes) {
+            const int y = per == 1 ? e : e / per, at = y * row + at0 + e - y * per;
+            n += count[y];
+            m = fmaf(count[y], sm[0][at], m);
         }
-        n = warp_sum(n);
-        m = warp_sum(m);
+        n = warp_sum(n, lanes);
+        m = warp_sum(m, lanes);
         m = n > 0.f ? m / n : 0.f;
-        float s = 0.f;
-        for (int e = lane; e < width * p.ty; e += 32) {
-            const int y = e / width, at = y * p.tc + from - a.c0 + e - y * width;
+        float q = 0.f;
+        for (int e = lane; e < per * p.ty; e += lanes) {
+            const int y = per == 1 ? e : e / per, at = y * row + at0 + e - y * per;
             const float d = sm[0][at] - m;
-            s += fmaf(d * d, (float)rows_of(rows, y, p.ty), sm[1][at]);
+            q += fmaf(d * d, count[y], sm[1][at]);
         }
-        s = warp_sum(s);
-        if (lane == 0) *slot(p, b, chunk, g, a.tile) = make_float2(m, s);
+        q = warp_sum(q, lanes);
+        if (lane == 0 && k < groups) *slot(p, b, chunk, g, a.tile) = make_float2(m, q);
     }
 }
 
-// The chunks' parts of group g of sample b, joined by a warp: (mean, 1 / deviation).
-__device__ __forceinline__ float2 join_stats(const Norm& p, int64_t b, int g, int live, int lane) {
-    const int first = g * p.w / p.tc, segs = ((g + 1) * p.w - 1) / p.tc - first + 1;
-    const float2* part = p.part + (b * p.chunks * p.G + g) * (int64_t)p.segs;
-    const int64_t step = (int64_t)p.G * p.segs;
-    float n = 0.f, m = 0.f;
-    for (int e = lane; e < p.chunks * segs; e += 32) {
-        const int k = e / segs, s = e - k * segs;
+// What a block's threads make of the chunks' parts, before they go over the rows again: `lanes` lanes take a
+// group, all of the tile's groups at once where they can, so that the parts' latency is met once. Up to
+// kHeld parts of a lane stay in registers between the mean and the squares.
+constexpr int kHeld = 16;
+__device__ __forceinline__ int join_lanes(int groups, int entries) {
+    int n = 32;
+    while (n > 1 && (n / 2 >= entries || groups * n > kThreads)) n /= 2;
+    return n;
+}
+struct Parts {
+    const float2* at;
+    int64_t step;  // from a chunk's to the next's
+    int first, segs, entries;
+};
+__device__ __forceinline__ Parts parts_of(const Norm& p, int64_t b, int g) {
+    Parts q;
+    q.first = g * p.w / p.tc;
+    q.segs = ((g + 1) * p.w - 1) / p.tc - q.first + 1;
+    q.at = p.part + (b * p.chunks * p.G + g) * (int64_t)p.segs;
+    q.step = (int64_t)p.G * p.segs;
+    q.entries = p.chunks * q.segs;
+    return q;
+}
+// Entry e and how many values it stands for.
+__device__ __forceinline__ float2 part_of(const Norm& p, const Parts& q, int g, int live, int e, float& n) {
+    const int k = q.segs == 1 ? e : e / q.segs, s = e - k * q.segs;
+    int width = p.w;
+    if (q.segs > 1) {
         int from, to;
-        segment(p, g, (first + s) * p.tc, (first + s + 1) * p.tc, from, to);
-        const float c = (float)max(0, min(live - k * p.rows, p.rows)) * (to - from);
-        n += c;
-        m = fmaf(c, part[k * step + s].x, m);
+        segment(p, g, (q.first + s) * p.tc, (q.first + s + 1) * p.tc, from, to);
+        width = to - from;
     }
-    n = warp_sum(n);
-    m = warp_sum(m);
+    n = (float)max(0, min(live - k * p.rows, p.rows)) * width;
+    return q.at[k * q.step + s];
+}
+// (mean, 1 / deviation) of group g of sample b
+__device__ __forceinline__ float2 join_stats(const Norm& p, int64_t b, int g, int live, int lane, int lanes) {
+    const Parts q = parts_of(p, b, g);
+    float2 v[kHeld];
+    float c[kHeld], n = 0.f, m = 0.f;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        v[j] = make_float2(0.f, 0.f);
+        c[j] = 0.f;
+        if (lane + j * lanes < q.entries) v[j] = part_of(p, q, g, live, lane + j * lanes, c[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        n += c[j];
+        m = fmaf(c[j], v[j].x, m);
+    }
+    for (int e = lane + kHeld * lanes; e < q.entries; e += lanes) {
+        float k;
+        const float2 u = part_of(p, q, g, live, e, k);
+        n += k;
+        m = fmaf(k, u.x, m);
+    }
+    n = warp_sum(n, lanes);
+    m = warp_sum(m, lanes);
     m = n > 0.f ? m / n : 0.f;
-    float q = 0.f;
-    for (int e = lane; e < p.chunks * segs; e += 32) {
-        const int k = e / segs, s = e - k * segs;
-        int from, to;
-        segment(p, g, (first + s) * p.tc, (first + s + 1) * p.tc, from, to);
-        const float c = (float)max(0, min(live - k * p.rows, p.rows)) * (to - from);
-        const float2 v = part[k * step + s];
-        const float d = v.x - m;
-        q += fmaf(d * d, c, v.y);
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        const float d = v[j].x - m;
+        s += fmaf(d * d, c[j], v[j].y);
     }
-    q = warp_sum(q);
-    return make_float2(m, rsqrtf((n > 0.f ? q / n : 0.f) + p.eps));
+    for (int e = lane + kHeld * lanes; e < q.entries; e += lanes) {
+        float k;
+        const float2 u = part_of(p, q, g, live, e, k);
+        const float d = u.x - m;
+        s += fmaf(d * d, k, u.y);
+    }
+    s = warp_sum(s, lanes);
+    return make_float2(m, rsqrtf((n > 0.f ? s / n : 0.f) + p.eps));
 }
 
 // ------------------------------------------------------------------ the forward's second pass
-template <typename E, int W>
-__global__ void __launch_bounds__(kThreads) apply_kernel(const Norm p) {
+template <typename E, int W, bool ONE>
+__global__ void __launch_bounds__(kThreads, 3) apply_kernel(const Norm p) {
     __shared__ float2 sm[kThreads * W];  // of the tile's groups
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -289,10 +388,12 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(const Norm p) {
     const int64_t b = p.b0 + a.unit / p.chunks;
     const int chunk = a.unit % p.chunks;
     const int live = live_rows(p, b);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g0 = a.c0 / p.w;
-    for (int g = g0 + warp; g * p.w < a.c1; g += kThreads / 32) {
-        const float2 v = join_stats(p, b, g, live, lane);
-        if (lane == 0) {
+    const int g0 = a.c0 / p.w, groups = (a.c1 - 1) / p.w - g0 + 1;
+    const int lanes = join_lanes(groups, p.chunks * p.segs), lane = threadIdx.x % lanes;
+    for (int k = threadIdx.x / lanes; k - threadIdx.x % 32 / lanes < groups; k += kThreads / lanes) {
+        const int g = min(g0 + k, g0 + groups - 1);  // (all lanes take part)
+        const float2 v = join_stats(p, b, g, live, lane, lanes);
+        if (lane == 0 && k < groups) {
             sm[g - g0] = v;
             if (p.stats && chunk == 0 && g * p.w >= a.c0) {
                 p.stats[b * 2 * p.G + g] = v.x;
@@ -302,11 +403,12 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(const Norm p) {
     }
     __syncthreads();
     if (!a.on) return;
-    float m[W], f[W], s[W];
+    constexpr int M = ONE ? 1 : W;
+    float m[M], f[W], s[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        const float2 v = sm[(a.c + i) / p.w - g0];
-        m[i] = v.x;
+        const float2 v = sm[(a.c + i % M) / p.w - g0];
+        m[i % M] = v.x;
         f[i] = v.y * param(p.gamma, p.param_f32, a.c + i, 1.f);
         s[i] = param(p.beta, p.param_f32, a.c + i, 0.f);
     }
@@ -315,7 +417,7 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(const Norm p) {
     const E* x = (const E*)p.x + at;
     E* y = (E*)p.y + at;
     const int all = rows_of(r1 - r0, a.ty, p.ty), mine = rows_of(max(0, live - r0), a.ty, p.ty);
-    constexpr int U = 4;
+    constexpr int U = 8;
     for (int k = 0; k < all; k += U, x += U * step, y += U * step) {
         Pack<E, W> v[U];
 #pragma unroll
@@ -326,7 +428,7 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(const Norm p) {
             if (k + j >= all) break;
             float z[W];
 #pragma unroll
-            for (int i = 0; i < W; ++i) z[i] = k + j < mine ? fmaf(widen(v[j].v[i]) - m[i], f[i], s[i]) : 0.f;
+            for (int i = 0; i < W; ++i) z[i] = k + j < mine ? fmaf(widen(v[j].v[i]) - m[i % M], f[i], s[i]) : 0.f;
             if (k + j < mine) act_value<E, W>(p.act, z);
 #pragma unroll
             for (int i = 0; i < W; ++i) narrow(v[j].v[i], z[i]);
@@ -336,34 +438,37 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(const Norm p) {
 }
 
 // ------------------------------------------------------------------ the backward
-// A thread's channels: xhat = (x - m) r, z = gamma xhat + beta.
-template <int W>
+// A thread's channels: xhat = (x - m) r, z = gamma xhat + beta. Where groups do not cut vectors (ONE) the vector
+// has one m and one r, which spares 14 registers of 8 channels (and as many averages').
+template <int W, bool ONE>
 struct Channels {
-    float r[W], m[W], gamma[W], beta[W];
+    float r[ONE ? 1 : W], m[ONE ? 1 : W], gamma[W], beta[W];
+    __device__ __forceinline__ float rstd(int i) const { return r[ONE ? 0 : i]; }
+    __device__ __forceinline__ float mean(int i) const { return m[ONE ? 0 : i]; }
 };
-template <int W>
-__device__ __forceinline__ void params_of(const Norm& p, int c, Channels<W>& h) {
+template <int W, bool ONE>
+__device__ __forceinline__ void params_of(const Norm& p, int c, Channels<W, ONE>& h) {
 #pragma unroll
     for (int i = 0; i < W; ++i) {
         h.gamma[i] = param(p.gamma, p.param_f32, c + i, 1.f);
         h.beta[i] = param(p.beta, p.param_f32, c + i, 0.f);
     }
 }
-template <int W>
-__device__ __forceinline__ void stats_of(const Norm& p, int64_t b, int c, Channels<W>& h) {
+template <int W, bool ONE>
+__device__ __forceinline__ void stats_of(const Norm& p, int64_t b, int c, Channels<W, ONE>& h) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
+    for (int i = 0; i < (ONE ? 1 : W); ++i) {
         const int g = (c + i) / p.w;
         h.r[i] = p.stats[(b * 2 + 1) * p.G + g];
         h.m[i] = p.stats[b * 2 * p.G + g];
     }
 }
 // xhat and dz of a row's vector
-template <typename E, int W>
-__device__ __forceinline__ void row_of(const Norm& p, const Channels<W>& h, const Pack<E, W>& x,
+template <typename E, int W, bool ONE>
+__device__ __forceinline__ void row_of(const Norm& p, const Channels<W, ONE>& h, const Pack<E, W>& x,
                                        const Pack<E, W>& dy, float* xhat, float* dz) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) xhat[i] = (widen(x.v[i]) - h.m[i]) * h.r[i];
+    for (int i = 0; i < W; ++i) xhat[i] = (widen(x.v[i]) - h.mean(i)) * h.rstd(i);
     if (p.act == FLAREPP_ACT_NONE) {
 #pragma unroll
         for (int i = 0; i < W; ++i) dz[i] = widen(dy.v[i]);
@@ -378,8 +483,8 @@ __device__ __forceinline__ void row_of(const Norm& p, const Channels<W>& h, cons
 
 // The sums over a chunk of rows (or over all rows of several samples): by group, sum g and sum g xhat, for
 // dx; by channel, sum dz xhat and sum dz, for dgamma and dbeta.
-template <typename E, int W>
-__global__ void __launch_bounds__(kThreads) back_sums_kernel(const Norm p) {
+template <typename E, int W, bool ONE>
+__global__ void __launch_bounds__(kThreads, 3) back_sums_kernel(const Norm p) {
     __shared__ float sm[2][kThreads * W];
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -387,12 +492,10 @@ __global__ void __launch_bounds__(kThreads) back_sums_kernel(const Norm p) {
     const int64_t from_b = p.b0 + (p.chunks > 1 ? a.unit / p.chunks : (int64_t)a.unit * p.per);
     const int64_t to_b = p.chunks > 1 ? from_b + 1 : min((int64_t)p.b0 + p.bn, from_b + p.per);
     const int chunk = p.chunks > 1 ? a.unit % p.chunks : 0;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    Channels<W> h;
-    float all_u[W], all_v[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) all_u[i] = all_v[i] = 0.f;
-    if (a.on) params_of<W>(p, a.c, h);
+    constexpr int kBackRows = back_rows<E, W>();
+    Channels<W, ONE> h;
+    __shared__ float all[2][kThreads * W];  // of the block's samples, by channel and row of threads
+    if (a.on) params_of<W, ONE>(p, a.c, h);
     for (int64_t b = from_b; b < to_b; ++b) {
         const int live = live_rows(p, b);
         const int r0 = chunk * p.rows, rows = max(0, min(live, r0 + p.rows) - r0);
@@ -400,7 +503,7 @@ __global__ void __launch_bounds__(kThreads) back_sums_kernel(const Norm p) {
 #pragma unroll
         for (int i = 0; i < W; ++i) u[i] = v[i] = 0.f;
         if (a.on) {
-            stats_of<W>(p, b, a.c, h);
+            stats_of<W, ONE>(p, b, a.c, h);
             const int mine = rows_of(rows, a.ty, p.ty);
             const int64_t at = (b * p.N + r0 + a.ty) * p.C + a.c, step = (int64_t)p.ty * p.C;
             const E* x = (const E*)p.x + at;
@@ -417,7 +520,7 @@ __global__ void __launch_bounds__(kThreads) back_sums_kernel(const Norm p) {
                 for (int j = 0; j < kBackRows; ++j)
                     if (k + j < mine) {
                         float xhat[W], dz[W];
-                        row_of<E, W>(p, h, px[j], pd[j], xhat, dz);
+                        row_of<E, W, ONE>(p, h, px[j], pd[j], xhat, dz);
 #pragma unroll
                         for (int i = 0; i < W; ++i) {
                             u[i] = fmaf(dz[i], xhat[i], u[i]);
@@ -425,53 +528,62 @@ __global__ void __launch_bounds__(kThreads) back_sums_kernel(const Norm p) {
                         }
                     }
             }
+            float s0 = 0.f, s1 = 0.f;
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                const int at_s = a.ty * p.tc + a.c - a.c0 + i;
-                sm[0][at_s] = v[i] * h.gamma[i];
-                sm[1][at_s] = u[i] * h.gamma[i];
-                all_u[i] += u[i];
-                all_v[i] += v[i];
+                const float g0 = v[i] * h.gamma[i], g1 = u[i] * h.gamma[i];
+                if (p.channels) {
+                    const int at = a.ty * p.tc + a.c - a.c0 + i;
+                    all[0][at] = b > from_b ? all[0][at] + u[i] : u[i];
+                    all[1][at] = b > from_b ? all[1][at] + v[i] : v[i];
+                }
+                s0 += g0;
+                s1 += g1;
+                if (p.cell != W) {
+                    sm[0][a.ty * p.tc + a.c - a.c0 + i] = g0;
+                    sm[1][a.ty * p.tc + a.c - a.c0 + i] = g1;
+                }
+            }
+            if (p.cell == W) {
+                sm[0][a.ty * p.tx + a.tx] = s0;
+                sm[1][a.ty * p.tx + a.tx] = s1;
             }
         }
         __syncthreads();
-        for (int g = a.c0 / p.w + warp; g * p.w < a.c1; g += kThreads / 32) {
-            int from, to;
-            segment(p, g, a.c0, a.c1, from, to);
-            const int width = to - from;
+        const int row = p.tc / p.cell, most = min(p.w, a.c1 - a.c0) / p.cell * p.ty;
+        const int lanes = lanes_for(most), lane = threadIdx.x % lanes;
+        const int g0 = a.c0 / p.w, groups = (a.c1 - 1) / p.w - g0 + 1;
+        for (int k = threadIdx.x / lanes; k - threadIdx.x % 32 / lanes < groups; k += kThreads / lanes) {
+            const int g = g0 + k;
+            int from = 0, to = 0;
+            if (k < groups) segment(p, g, a.c0, a.c1, from, to);
+            const int per = (to - from) / p.cell, at0 = (from - a.c0) / p.cell;
             float s0 = 0.f, s1 = 0.f;
-            for (int e = lane; e < width * p.ty; e += 32) {
-                const int y = e / width, at = y * p.tc + from - a.c0 + e - y * width;
+            for (int e = lane; e < per * p.ty; e += lanes) {
+                const int y = per == 1 ? e : e / per, at = y * row + at0 + e - y * per;
                 s0 += sm[0][at];
                 s1 += sm[1][at];
             }
-            s0 = warp_sum(s0);
-            s1 = warp_sum(s1);
-            if (lane == 0) *slot(p, b, chunk, g, a.tile) = make_float2(s0, s1);
+            s0 = warp_sum(s0, lanes);
+            s1 = warp_sum(s1, lanes);
+            if (lane == 0 && k < groups) *slot(p, b, chunk, g, a.tile) = make_float2(s0, s1);
         }
         __syncthreads();
     }
     if (!p.channels) return;
-    if (a.on)
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            sm[0][a.ty * p.tc + a.c - a.c0 + i] = all_u[i];
-            sm[1][a.ty * p.tc + a.c - a.c0 + i] = all_v[i];
-        }
-    __syncthreads();
     float2* out = p.channels + (int64_t)(p.channel_rows + a.unit) * p.C;
     for (int c = a.c0 + threadIdx.x; c < a.c1; c += kThreads) {
         float s0 = 0.f, s1 = 0.f;
         for (int y = 0; y < p.ty; ++y) {
-            s0 += sm[0][y * p.tc + c - a.c0];
-            s1 += sm[1][y * p.tc + c - a.c0];
+            s0 += all[0][y * p.tc + c - a.c0];
+            s1 += all[1][y * p.tc + c - a.c0];
         }
         out[c] = make_float2(s0, s1);
     }
 }
 
-template <typename E, int W>
-__global__ void __launch_bounds__(kThreads) back_apply_kernel(const Norm p) {
+template <typename E, int W, bool ONE>
+__global__ void __launch_bounds__(kThreads, 3) back_apply_kernel(const Norm p) {
     __shared__ float2 sm[kThreads * W];
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -479,30 +591,35 @@ __global__ void __launch_bounds__(kThreads) back_apply_kernel(const Norm p) {
     const int64_t b = p.b0 + a.unit / p.chunks;
     const int chunk = a.unit % p.chunks;
     const int live = live_rows(p, b);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g0 = a.c0 / p.w;
+    const int g0 = a.c0 / p.w;
+    constexpr int kBackRows = back_rows<E, W>();
     const float each = 1.f / fmaxf(1.f, (float)live * p.w);
-    for (int g = g0 + warp; g * p.w < a.c1; g += kThreads / 32) {
-        const int first = g * p.w / p.tc, segs = ((g + 1) * p.w - 1) / p.tc - first + 1;
-        const float2* part = p.part + (b * p.chunks * p.G + g) * (int64_t)p.segs;
+    const int groups = (a.c1 - 1) / p.w - g0 + 1;
+    const int lanes = join_lanes(groups, p.chunks * p.segs), lane = threadIdx.x % lanes;
+    for (int k = threadIdx.x / lanes; k - threadIdx.x % 32 / lanes < groups; k += kThreads / lanes) {
+        const int g = min(g0 + k, g0 + groups - 1);
+        const Parts q = parts_of(p, b, g);
         float s0 = 0.f, s1 = 0.f;
-        for (int e = lane; e < p.chunks * segs; e += 32) {
-            const int k = e / segs;
-            const float2 v = part[k * (int64_t)p.G * p.segs + e - k * segs];
+#pragma unroll 8
+        for (int e = lane; e < q.entries; e += lanes) {
+            const int c = q.segs == 1 ? e : e / q.segs;
+            const float2 v = q.at[c * q.step + e - c * q.segs];
             s0 += v.x;
             s1 += v.y;
         }
-        s0 = warp_sum(s0);
-        s1 = warp_sum(s1);
-        if (lane == 0) sm[g - g0] = make_float2(s0 * each, s1 * each);
+        s0 = warp_sum(s0, lanes);
+        s1 = warp_sum(s1, lanes);
+        if (lane == 0 && k < groups) sm[g - g0] = make_float2(s0 * each, s1 * each);
     }
     __syncthreads();
     if (!a.on) return;
-    Channels<W> h;
-    params_of<W>(p, a.c, h);
-    stats_of<W>(p, b, a.c, h);
-    float m0[W], m1[W];
+    Channels<W, ONE> h;
+    params_of<W, ONE>(p, a.c, h);
+    stats_of<W, ONE>(p, b, a.c, h);
+    constexpr int M = ONE ? 1 : W;
+    float m0[M], m1[M];
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
+    for (int i = 0; i < M; ++i) {
         const float2 v = sm[(a.c + i) / p.w - g0];
         m0[i] = v.x;
         m1[i] = v.y;
@@ -527,10 +644,10 @@ __global__ void __launch_bounds__(kThreads) back_apply_kernel(const Norm p) {
             if (k + j >= all) break;
             float xhat[W], dz[W];
             if (k + j < mine) {
-                row_of<E, W>(p, h, px[j], pd[j], xhat, dz);
+                row_of<E, W, ONE>(p, h, px[j], pd[j], xhat, dz);
 #pragma unroll
                 for (int i = 0; i < W; ++i)
-                    dz[i] = h.r[i] * (fmaf(dz[i], h.gamma[i], -m0[i]) - xhat[i] * m1[i]);
+                    dz[i] = h.rstd(i) * (fmaf(dz[i], h.gamma[i], -m0[i % M]) - xhat[i] * m1[i % M]);
             } else {
 #pragma unroll
                 for (int i = 0; i < W; ++i) dz[i] = 0.f;
@@ -542,196 +659,225 @@ __global__ void __launch_bounds__(kThreads) back_apply_kernel(const Norm p) {
     }
 }
 
-// dgamma and dbeta from rows [R][C] of (sum dz xhat, sum dz): a block takes 32 channels, its 32 warps every
-// 32nd row, in order; then the warps' sums in order.
-constexpr int kReduceThreads = 1024;
+// dgamma and dbeta from rows [R][C] of (sum dz xhat, sum dz): a block takes 8 channels, each of 128 threads
+// every 128th row of one, in order; then their sums by halves.
+constexpr int kReduceThreads = 1024, kReduceChannels = 8, kReduceRows = kReduceThreads / kReduceChannels;
 template <typename P>
 __global__ void __launch_bounds__(kReduceThreads)
     channels_kernel(const float2* rows, int R, int C, P* dgamma, P* dbeta) {
-    __shared__ float2 sm[32][33];
+    __shared__ float2 sm[kReduceRows][kReduceChannels];
     tc::pdl_trigger();
     tc::pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    const int x = threadIdx.x % kReduceChannels, y = threadIdx.x / kReduceChannels;
+    const int c = blockIdx.x * kReduceChannels + x;
     float2 s = make_float2(0.f, 0.f);
     if (c < C)
-        for (int r = warp; r < R; r += 32) {
+#pragma unroll 4
+        for (int r = y; r < R; r += kReduceRows) {
             const float2 v = rows[(int64_t)r * C + c];
             s.x += v.x;
             s.y += v.y;
         }
-    sm[warp][lane] = s;
-    __syncthreads();
-    if (warp || c >= C) return;
-    for (int k = 1; k < 32; ++k) {
-        s.x += sm[k][lane].x;
-        s.y += sm[k][lane].y;
+    sm[y][x] = s;
+    for (int k = kReduceRows / 2; k; k >>= 1) {
+        __syncthreads();
+        if (y >= k) continue;
+        s.x += sm[y + k][x].x;
+        s.y += sm[y + k][x].y;
+        sm[y][x] = s;
     }
+    if (y || c >= C) return;
     if (dgamma) narrow(dgamma[c], s.x);
     if (dbeta) narrow(dbeta[c], s.y);
 }
 
 // ------------------------------------------------------------------ few rows a sample
-// A group's w channels are the vectors of `lanes` lanes (a power of two), a sample's K rows stay in their
-// registers: one pass over the data and one launch. Blocks walk the samples.
-template <typename E, int W, int K>
+// `lanes` lanes (a power of two) take a sample's group, its K rows of V vectors a lane staying in registers:
+// one pass over the data and one launch. A block's 256 / lanes such teams and all blocks' together are a
+// multiple of G, so that a team walks the samples with the same channels.
+struct Team {
+    int g, lane;
+    int64_t row, rows;  // of the teams with this g: the team's place, their number
+};
+__device__ __forceinline__ Team team_of(const Norm& p, int lanes) {
+    const int per = kThreads / lanes;
+    const int64_t id = (int64_t)blockIdx.x * per + threadIdx.x / lanes;
+    Team t;
+    t.lane = threadIdx.x % lanes;
+    t.row = id / p.G;
+    t.g = (int)(id - t.row * p.G);
+    t.rows = (int64_t)gridDim.x * per / p.G;
+    return t;
+}
+__device__ __forceinline__ int live_rows_few(const Norm& p, int64_t b, bool on) {
+    if (!on) return 0;
+    if (!p.lengths) return (int)p.N;
+    const int n = p.lengths[b];
+    if (n >= 0 && n <= p.N) return n;
+    record_status(p.status, FLAREPP_ERR_INVALID_ARGUMENT);
+    return n < 0 ? 0 : (int)p.N;
+}
+
+template <typename E, int W, int K, int V>
 __global__ void __launch_bounds__(kThreads) few_kernel(const Norm p, int lanes) {
     tc::pdl_trigger();
     tc::pdl_wait();
-    const Place a = place_of<W>(p, blockIdx.x);
-    float f[W], s[W];
+    const Team t = team_of(p, lanes);
+    const int vectors = p.w / W;
+    float f[V * W], s[V * W];
+    bool has[V];
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-        f[i] = a.on ? param(p.gamma, p.param_f32, a.c + i, 1.f) : 0.f;
-        s[i] = a.on ? param(p.beta, p.param_f32, a.c + i, 0.f) : 0.f;
-    }
-    const int64_t step = gridDim.x / p.tiles * (int64_t)p.ty;
-    const int64_t turns = (p.B + step - 1) / step;
-    for (int64_t t = 0; t < turns; ++t) {  // all lanes take part in the sums
-        const int64_t b = t * step + (int64_t)a.unit * p.ty + a.ty;
-        const bool on = a.on && b < p.B;
-        int live = 0;
-        if (on) {
-            live = (int)p.N;
-            if (p.lengths) {
-                live = p.lengths[b];
-                if (live < 0 || live > p.N) {
-                    record_status(p.status, FLAREPP_ERR_INVALID_ARGUMENT);
-                    live = live < 0 ? 0 : (int)p.N;
-                }
-            }
+    for (int v = 0; v < V; ++v) {
+        has[v] = v * lanes + t.lane < vectors;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const int c = t.g * p.w + (v * lanes + t.lane) * W + i;
+            f[v * W + i] = has[v] ? param(p.gamma, p.param_f32, c, 1.f) : 0.f;
+            s[v * W + i] = has[v] ? param(p.beta, p.param_f32, c, 0.f) : 0.f;
         }
-        const int64_t at = b * p.N * p.C + a.c;
-        Pack<E, W> x[K];
+    }
+    const int64_t turns = (p.B + t.rows - 1) / t.rows;
+    for (int64_t k = 0; k < turns; ++k) {  // all lanes take part in the sums
+        const int64_t b = k * t.rows + t.row;
+        const bool on = b < p.B;
+        const int live = live_rows_few(p, b, on);
+        const int64_t at = b * p.N * p.C + t.g * p.w + t.lane * W;
+        Pack<E, W> x[K][V];
         float m = 0.f, q = 0.f;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (k < live) {
-                x[k] = load<E, W>((const E*)p.x + at + (int64_t)k * p.C);
+        for (int r = 0; r < K; ++r)
 #pragma unroll
-                for (int i = 0; i < W; ++i) m += widen(x[k].v[i]);
-            }
+            for (int v = 0; v < V; ++v)
+                if (r < live && has[v]) x[r][v] = load<E, W>((const E*)p.x + at + (int64_t)r * p.C + v * lanes * W);
+#pragma unroll
+        for (int r = 0; r < K; ++r)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (r < live && has[v])
+#pragma unroll
+                    for (int i = 0; i < W; ++i) m += widen(x[r][v].v[i]);
         const float each = 1.f / fmaxf(1.f, (float)live * p.w);
         m = warp_sum(m, lanes) * each;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (k < live)
+        for (int r = 0; r < K; ++r)
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const float d = widen(x[k].v[i]) - m;
-                    q = fmaf(d, d, q);
-                }
+            for (int v = 0; v < V; ++v)
+                if (r < live && has[v])
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const float d = widen(x[r][v].v[i]) - m;
+                        q = fmaf(d, d, q);
+                    }
         q = rsqrtf(warp_sum(q, lanes) * each + p.eps);
         if (!on) continue;
-        if (p.stats && a.c % p.w == 0) {
-            p.stats[b * 2 * p.G + a.c / p.w] = m;
-            p.stats[(b * 2 + 1) * p.G + a.c / p.w] = q;
+        if (p.stats && t.lane == 0) {
+            p.stats[b * 2 * p.G + t.g] = m;
+            p.stats[(b * 2 + 1) * p.G + t.g] = q;
         }
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (k >= p.N) break;
-            float z[W];
+        for (int r = 0; r < K; ++r) {
+            if (r >= p.N) break;
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                z[i] = k < live ? fmaf(widen(x[k].v[i]) - m, q * f[i], s[i]) : 0.f;
+            for (int v = 0; v < V; ++v) {
+                if (!has[v]) continue;
+                float z[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    z[i] = r < live ? fmaf(widen(x[r][v].v[i]) - m, q * f[v * W + i], s[v * W + i]) : 0.f;
+                if (r < live) act_value<E, W>(p.act, z);
+#pragma unroll
+                for (int i = 0; i < W; ++i) narrow(x[r][v].v[i], z[i]);
+                store<E, W>((E*)p.y + at + (int64_t)r * p.C + v * lanes * W, x[r][v]);
             }
-            if (k < live) act_value<E, W>(p.act, z);
-#pragma unroll
-            for (int i = 0; i < W; ++i) narrow(x[k].v[i], z[i]);
-            store<E, W>((E*)p.y + at + (int64_t)k * p.C, x[k]);
         }
     }
 }
 
-template <typename E, int W, int K>
+template <typename E, int W, int K, int V>
 __global__ void __launch_bounds__(kThreads) back_few_kernel(const Norm p, int lanes) {
-    __shared__ float sm[2][kThreads * W];
     tc::pdl_trigger();
     tc::pdl_wait();
-    const Place a = place_of<W>(p, blockIdx.x);
-    Channels<W> h;
-    float u[W], v[W];
+    const Team t = team_of(p, lanes);
+    const int vectors = p.w / W;
+    Channels<W, true> h[V];
+    float u[V * W], w[V * W];
+    bool has[V];
 #pragma unroll
-    for (int i = 0; i < W; ++i) u[i] = v[i] = h.r[i] = h.m[i] = h.gamma[i] = h.beta[i] = 0.f;
-    if (a.on) params_of<W>(p, a.c, h);
-    const int64_t step = gridDim.x / p.tiles * (int64_t)p.ty;
-    const int64_t turns = (p.B + step - 1) / step;
-    for (int64_t t = 0; t < turns; ++t) {
-        const int64_t b = t * step + (int64_t)a.unit * p.ty + a.ty;
-        const bool on = a.on && b < p.B;
-        int live = 0;
-        if (on) {
-            live = (int)p.N;
-            if (p.lengths) {
-                live = p.lengths[b];
-                if (live < 0 || live > p.N) {
-                    record_status(p.status, FLAREPP_ERR_INVALID_ARGUMENT);
-                    live = live < 0 ? 0 : (int)p.N;
-                }
-            }
-            stats_of<W>(p, b, a.c, h);
-        }
-        const int64_t at = b * p.N * p.C + a.c;
-        Pack<E, W> x[K], dy[K];
+    for (int v = 0; v < V; ++v) {
+        has[v] = v * lanes + t.lane < vectors;
+        if (has[v]) params_of<W, true>(p, t.g * p.w + (v * lanes + t.lane) * W, h[v]);
+#pragma unroll
+        for (int i = 0; i < W; ++i) u[v * W + i] = w[v * W + i] = 0.f;
+    }
+    const int64_t turns = (p.B + t.rows - 1) / t.rows;
+    for (int64_t k = 0; k < turns; ++k) {
+        const int64_t b = k * t.rows + t.row;
+        const bool on = b < p.B;
+        const int live = live_rows_few(p, b, on);
+        if (on)
+#pragma unroll
+            for (int v = 0; v < V; ++v) stats_of<W, true>(p, b, t.g * p.w, h[v]);
+        const int64_t at = b * p.N * p.C + t.g * p.w + t.lane * W;
+        Pack<E, W> x[K][V], dy[K][V];
         float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (k < live) {
-                x[k] = load<E, W>((const E*)p.x + at + (int64_t)k * p.C);
-                dy[k] = load<E, W>((const E*)p.dy + at + (int64_t)k * p.C);
-            }
+        for (int r = 0; r < K; ++r)
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (k < live) {
-                float xhat[W], dz[W];
-                row_of<E, W>(p, h, x[k], dy[k], xhat, dz);
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    u[i] = fmaf(dz[i], xhat[i], u[i]);
-                    v[i] += dz[i];
-                    const float g = dz[i] * h.gamma[i];
-                    s0 += g;
-                    s1 = fmaf(g, xhat[i], s1);
+            for (int v = 0; v < V; ++v)
+                if (r < live && has[v]) {
+                    x[r][v] = load<E, W>((const E*)p.x + at + (int64_t)r * p.C + v * lanes * W);
+                    dy[r][v] = load<E, W>((const E*)p.dy + at + (int64_t)r * p.C + v * lanes * W);
                 }
-            }
+#pragma unroll
+        for (int r = 0; r < K; ++r)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (r < live && has[v]) {
+                    float xhat[W], dz[W];
+                    row_of<E, W, true>(p, h[v], x[r][v], dy[r][v], xhat, dz);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        u[v * W + i] = fmaf(dz[i], xhat[i], u[v * W + i]);
+                        w[v * W + i] += dz[i];
+                        const float g = dz[i] * h[v].gamma[i];
+                        s0 += g;
+                        s1 = fmaf(g, xhat[i], s1);
+                    }
+                }
         const float each = 1.f / fmaxf(1.f, (float)live * p.w);
         s0 = warp_sum(s0, lanes) * each;
         s1 = warp_sum(s1, lanes) * each;
         if (!on) continue;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (k >= p.N) break;
-            float xhat[W], dz[W];
-            if (k < live) {
-                row_of<E, W>(p, h, x[k], dy[k], xhat, dz);
+        for (int r = 0; r < K; ++r) {
+            if (r >= p.N) break;
 #pragma unroll
-                for (int i = 0; i < W; ++i)
-                    dz[i] = h.r[i] * (fmaf(dz[i], h.gamma[i], -s0) - xhat[i] * s1);
-            } else {
+            for (int v = 0; v < V; ++v) {
+                if (!has[v]) continue;
+                float xhat[W], dz[W];
+                if (r < live) {
+                    row_of<E, W, true>(p, h[v], x[r][v], dy[r][v], xhat, dz);
 #pragma unroll
-                for (int i = 0; i < W; ++i) dz[i] = 0.f;
+                    for (int i = 0; i < W; ++i)
+                        dz[i] = h[v].rstd(i) * (fmaf(dz[i], h[v].gamma[i], -s0) - xhat[i] * s1);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) dz[i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < W; ++i) narrow(x[r][v].v[i], dz[i]);
+                store<E, W>((E*)p.y + at + (int64_t)r * p.C + v * lanes * W, x[r][v]);
             }
-#pragma unroll
-            for (int i = 0; i < W; ++i) narrow(x[k].v[i], dz[i]);
-            store<E, W>((E*)p.y + at + (int64_t)k * p.C, x[k]);
         }
     }
     if (!p.channels) return;
-    if (a.on)
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            sm[0][a.ty * p.tc + a.c - a.c0 + i] = u[i];
-            sm[1][a.ty * p.tc + a.c - a.c0 + i] = v[i];
-        }
-    __syncthreads();
-    float2* out = p.channels + (int64_t)a.unit * p.C;
-    for (int c = a.c0 + threadIdx.x; c < a.c1; c += kThreads) {
-        float s0 = 0.f, s1 = 0.f;
-        for (int y = 0; y < p.ty; ++y) {
-            s0 += sm[0][y * p.tc + c - a.c0];
-            s1 += sm[1][y * p.tc + c - a.c0];
-        }
-        out[c] = make_float2(s0, s1);
-    }
+    for (int v = 0; v < V; ++v)
+        if (has[v])
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                p.channels[t.row * p.C + t.g * p.w + (v * lanes + t.lane) * W + i] =
+                    make_float2(u[v * W + i], w[v * W + i]);
 }
 
 // ------------------------------------------------------------------ host side
@@ -755,11 +901,12 @@ size_t up(size_t n) { return (n + kWsAlign - 1) / kWsAlign * kWsAlign; }
 
 // How a call is cut: the same for sizing its workspace and for running it.
 struct Plan {
-    int W, tx, ty, tc, tiles, segs;
-    int lanes;        // > 0: few rows, groups of that many lanes
+    int W, tx, ty, tc, tiles, segs, cell;
+    int lanes, each;  // > 0: few rows, groups of that many lanes of `each` vectors a row
     int chunks, rows, per;
     int64_t group;    // samples that go through together
     int64_t units;    // rows of `channels` that a call leaves
+    int64_t blocks;   // with few rows
     size_t off_channels, total;
 };
 
@@ -768,29 +915,38 @@ int64_t elem_of(const flarepp_norm_shape& s) { return s.dtype == FLAREPP_BF16 ? 
 Plan plan_of(const flarepp_norm_shape& s, bool backward) {
     Plan p{};
     const int64_t e = elem_of(s);
-    p.W = (int)(16 / e);
+    p.W = 4;
     while (s.C % p.W) p.W /= 2;
     const int64_t vectors = s.C / p.W, w = s.C / s.G;
-    // Few rows: the groups' lanes must divide a warp. (A sample of one row and 512 channels: 1 launch.)
+    // Few rows, whose vectors do not cut groups: a warp or a part of one takes a group, if it has room
+    // (1,024 channels of one row; a layer norm of more goes the long way).
     if (s.N <= kFewRows && w % p.W == 0) {
-        const int64_t lanes = w / p.W;
-        if (lanes <= 32 && (lanes & (lanes - 1)) == 0) p.lanes = (int)lanes;
+        const int64_t vectors_of = w / p.W;
+        p.lanes = 1;
+        while (p.lanes < 32 && p.lanes < vectors_of) p.lanes *= 2;
+        p.each = 1;
+        while (p.each * p.lanes < vectors_of) p.each *= 2;
+        if (p.each > (s.N == 1 && p.W == 4 ? 8 : 1)) p.lanes = 0;
     }
-    // tiles as even as can be, of whole groups' lanes where they matter
     p.tiles = (int)cdiv(vectors, kThreads);
     p.tx = (int)cdiv(vectors, p.tiles);
-    if (p.lanes) p.tx = (int)cdiv(p.tx, p.lanes) * p.lanes;
     p.tiles = (int)cdiv(vectors, p.tx);
     p.ty = kThreads / p.tx;
     p.tc = p.tx * p.W;
+    p.cell = w % p.W == 0 ? p.W : 1;
     // the most tiles that w channels side by side can touch
     p.segs = (int)(w < 2 ? 1 : (w - 2) / p.tc + 2);
     if (p.segs > p.tiles) p.segs = p.tiles;
     p.per = 1;
     if (p.lanes) {
-        p.units = cdiv(s.B, p.ty);
-        const int64_t most = cdiv(kNumSMs * 4, p.tiles);
-        if (p.units > most) p.units = most;
+        // blocks in steps of as many as hold whole sets of G teams; 4 an SM at most
+        const int64_t teams = kThreads / p.lanes;
+        int64_t step = s.G;
+        for (int64_t d = teams; d > 1 && step % 2 == 0; d /= 2) step /= 2;
+        int64_t blocks = cdiv(s.B * s.G, teams);
+        if (blocks > kNumSMs * 4) blocks = kNumSMs * 4;
+        p.blocks = cdiv(blocks, step) * step;
+        p.units = p.blocks * teams / s.G;
         p.chunks = 1;
         p.rows = (int)s.N;
         p.group = s.B;
@@ -801,14 +957,16 @@ Plan plan_of(const flarepp_norm_shape& s, bool backward) {
         if (p.group < 1) p.group = 1;
         if (p.group > s.B) p.group = s.B;
         p.group = cdiv(s.B, cdiv(s.B, p.group));
-        const int64_t wanted = cdiv(kNumSMs * 6, p.group * p.tiles);
-        const int64_t least = (int64_t)p.ty * kRows;  // rows that keep a block's threads busy
+        // Three blocks an SM, with 32 rows a thread where there are so many: a block's own sums take as long
+        // as some ten rows of its threads.
+        const int64_t wanted = cdiv(kNumSMs * 3, p.group * p.tiles);
+        const int64_t least = (int64_t)p.ty * 8;
         p.chunks = (int)(wanted < cdiv(s.N, least) ? wanted : cdiv(s.N, least));
         if (p.chunks < 1) p.chunks = 1;
         p.rows = (int)cdiv(s.N, p.chunks);
         p.chunks = (int)cdiv(s.N, p.rows);
         if (p.chunks == 1) {
-            const int64_t blocks = cdiv(kNumSMs * 6, p.tiles);
+            const int64_t blocks = cdiv(kNumSMs * 3, p.tiles);
             p.per = (int)cdiv(p.group, blocks);
         }
         const int64_t whole = s.B / p.group, rest = s.B - whole * p.group;
@@ -821,19 +979,24 @@ Plan plan_of(const flarepp_norm_shape& s, bool backward) {
     return p;
 }
 
+// The kernel for few rows: of one row and up to 8 vectors a lane, or of up to four rows.
+#define FLAREPP_FEW(kernel)                                                                   \
+    (a.N > 1         ? launch(kernel<E, W, kFewRows, 1>, p.blocks, kThreads, st, a, p.lanes)  \
+     : p.each == 1   ? launch(kernel<E, W, 1, 1>, p.blocks, kThreads, st, a, p.lanes)         \
+     : p.each == 2   ? launch(kernel<E, W, 1, W == 4 ? 2 : 1>, p.blocks, kThreads, st, a, p.lanes) \
+     : p.each == 4   ? launch(kernel<E, W, 1, W == 4 ? 4 : 1>, p.blocks, kThreads, st, a, p.lanes) \
+                     : launch(kernel<E, W, 1, W == 4 ? 8 : 1>, p.blocks, kThreads, st, a, p.lanes))
+
 template <typename E, int W>
 cudaError_t forward(Norm a, const Plan& p, cudaStream_t st) {
-    if (p.lanes) {
-        const int64_t blocks = p.units * p.tiles;
-        return a.N == 1 ? launch(few_kernel<E, W, 1>, blocks, kThreads, st, a, p.lanes)
-                        : launch(few_kernel<E, W, kFewRows>, blocks, kThreads, st, a, p.lanes);
-    }
+    if (p.lanes) return FLAREPP_FEW(few_kernel);
     for (int64_t b = 0; b < a.B; b += p.group) {
         a.b0 = (int)b;
         a.bn = (int)(a.B - b < p.group ? a.B - b : p.group);
         const int64_t blocks = (int64_t)a.bn * p.chunks * p.tiles;
         cudaError_t e = launch(stats_kernel<E, W>, blocks, kThreads, st, a);
-        if (e == cudaSuccess) e = launch(apply_kernel<E, W>, blocks, kThreads, st, a);
+        if (e == cudaSuccess)
+            e = launch(a.cell == W ? apply_kernel<E, W, true> : apply_kernel<E, W, W == 1>, blocks, kThreads, st, a);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -841,12 +1004,7 @@ cudaError_t forward(Norm a, const Plan& p, cudaStream_t st) {
 
 template <typename E, int W>
 cudaError_t backward(Norm a, const Plan& p, cudaStream_t st) {
-    if (p.lanes) {
-        const int64_t blocks = p.units * p.tiles;
-        a.channel_rows = 0;
-        return a.N == 1 ? launch(back_few_kernel<E, W, 1>, blocks, kThreads, st, a, p.lanes)
-                        : launch(back_few_kernel<E, W, kFewRows>, blocks, kThreads, st, a, p.lanes);
-    }
+    if (p.lanes) return FLAREPP_FEW(back_few_kernel);
     int rows = 0;
     for (int64_t b = 0; b < a.B; b += p.group) {
         a.b0 = (int)b;
@@ -854,30 +1012,24 @@ cudaError_t backward(Norm a, const Plan& p, cudaStream_t st) {
         a.channel_rows = rows;
         const int64_t units = p.chunks > 1 ? (int64_t)a.bn * p.chunks : cdiv(a.bn, p.per);
         rows += (int)units;
-        cudaError_t e = launch(back_sums_kernel<E, W>, units * p.tiles, kThreads, st, a);
+        cudaError_t e = launch(a.cell == W ? back_sums_kernel<E, W, true> : back_sums_kernel<E, W, W == 1>,
+                               units * p.tiles, kThreads, st, a);
         if (e == cudaSuccess)
-            e = launch(back_apply_kernel<E, W>, (int64_t)a.bn * p.chunks * p.tiles, kThreads, st, a);
+            e = launch(a.cell == W ? back_apply_kernel<E, W, true> : back_apply_kernel<E, W, W == 1>,
+                       (int64_t)a.bn * p.chunks * p.tiles, kThreads, st, a);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
+// Vectors of 4 channels for 16 bits, too: with 8 the constants of the activations and two vectors' values and
+// sums do not fit the registers of 3 blocks an SM.
 template <typename E>
 cudaError_t run(bool back, const Norm& a, const Plan& p, cudaStream_t st) {
-    constexpr int M = 16 / sizeof(E);
     switch (p.W) {
-        case M: return back ? backward<E, M>(a, p, st) : forward<E, M>(a, p, st);
-        case M / 2: return back ? backward<E, M / 2>(a, p, st) : forward<E, M / 2>(a, p, st);
+        case 4: return back ? backward<E, 4>(a, p, st) : forward<E, 4>(a, p, st);
         case 2: return back ? backward<E, 2>(a, p, st) : forward<E, 2>(a, p, st);
         default: return back ? backward<E, 1>(a, p, st) : forward<E, 1>(a, p, st);
-    }
-}
-template <>
-cudaError_t run<float>(bool back, const Norm& a, const Plan& p, cudaStream_t st) {
-    switch (p.W) {
-        case 4: return back ? backward<float, 4>(a, p, st) : forward<float, 4>(a, p, st);
-        case 2: return back ? backward<float, 2>(a, p, st) : forward<float, 2>(a, p, st);
-        default: return back ? backward<float, 1>(a, p, st) : forward<float, 1>(a, p, st);
     }
 }
 
@@ -937,13 +1089,13 @@ flarepp_status group_norm(bool back, const flarepp_norm_shape* shape, const void
     a.lengths = lengths, a.stats = stats;
     a.B = s.B, a.N = s.N, a.C = (int)s.C, a.G = (int)s.G, a.w = (int)(s.C / s.G);
     a.act = s.act, a.eps = s.eps, a.status = status;
-    a.tx = p.tx, a.ty = p.ty, a.tc = p.tc, a.tiles = p.tiles, a.segs = p.segs;
+    a.tx = p.tx, a.ty = p.ty, a.tc = p.tc, a.cell = p.cell, a.tiles = p.tiles, a.segs = p.segs;
     a.chunks = p.chunks, a.rows = p.rows, a.per = p.per;
     a.part = (float2*)workspace;
     a.channels = sums ? (float2*)((char*)workspace + p.off_channels) : nullptr;
     e = s.dtype == FLAREPP_BF16 ? run<__nv_bfloat16>(back, a, p, st) : run<float>(back, a, p, st);
     if (e == cudaSuccess && sums) {
-        const int64_t blocks = cdiv(s.C, 32);
+        const int64_t blocks = cdiv(s.C, kReduceChannels);
         if (s.param_dtype == FLAREPP_F32)
             e = launch(channels_kernel<float>, blocks, kReduceThreads, st, (const float2*)a.channels,
                        (int)p.units, (int)s.C, (float*)dgamma, (float*)dbeta);

@@ -27,7 +27,7 @@ using namespace vec;
 
 constexpr int kThreads = 256;
 constexpr int kMaxAxes = FLAREPP_ROTARY_AXES;
-constexpr int64_t kMaxDim = 1024;
+constexpr int kMaxDim = 1024;
 
 struct Side {  // one of q and k
     const void* x;
@@ -38,7 +38,7 @@ struct Side {  // one of q and k
 struct Rotary {
     Side side[2];
     int Hq, H;  // heads of q; of q and k together
-    int64_t B, N;
+    int rows, N;    // tokens of the batch, of an element
     int D, P;       // channels, pairs
     int ends[kMaxAxes];  // pairs up to each axis's last
     int axes, pairing;
@@ -65,9 +65,9 @@ __device__ __forceinline__ void turn_of(float p, float q, float f, float& c, flo
 }
 
 // The position of row n in two floats
-__device__ __forceinline__ void position(const Rotary& a, int64_t b, int64_t n, int axis, float& p,
+__device__ __forceinline__ void position(const Rotary& a, int64_t b, int n, int axis, float& p,
                                          float& q) {
-    const int64_t at = b * a.pos_stride + n * a.axes + axis;
+    const int64_t at = b * a.pos_stride + (int64_t)n * a.axes + axis;
     if (a.real) {
         p = ((const float*)a.positions)[at];
         q = 0.f;
@@ -84,46 +84,79 @@ __device__ __forceinline__ int axis_of(const Rotary& a, int pair) {
     return k;
 }
 
-__device__ __forceinline__ const Side& side_of(const Rotary& a, int h, int& local) {
-    const bool k = h >= a.Hq;
-    local = k ? h - a.Hq : h;
-    return a.side[k];
+// The part of one side's heads in [h0, h1): how many, and where the first one's row n of batch element b is.
+template <typename E>
+struct Rows {
+    const E* x;
+    E* y;
+    int64_t xh, yh;
+    int heads;
+};
+template <typename E>
+__device__ __forceinline__ Rows<E> rows_on(const Rotary& a, int k, int64_t b, int64_t n, int h0, int h1) {
+    const Side& s = a.side[k];
+    const int first = k ? max(h0 - a.Hq, 0) : h0, last = k ? h1 - a.Hq : min(h1, a.Hq);
+    Rows<E> r;
+    r.heads = max(last - first, 0);
+    r.xh = s.xh;
+    r.yh = s.yh;
+    r.x = (const E*)s.x + b * s.xb + first * s.xh + n * s.xn;
+    r.y = (E*)s.y + b * s.yb + first * s.yh + n * s.yn;
+    return r;
+}
+
+template <typename E, int W>
+__device__ __forceinline__ void widen_all(const Pack<E, W>& v, float* x) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = widen(v.v[i]);
+}
+template <typename E>
+__device__ __forceinline__ void narrow_all(Pack<E, 1>& v, const float* x) {
+    narrow(v.v[0], x[0]);
+}
+__device__ __forceinline__ void narrow_all(Pack<float, 4>& v, const float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.v[i] = x[i];
+}
+__device__ __forceinline__ void narrow_all(Pack<__nv_bfloat16, 8>& v, const float* x) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+        *reinterpret_cast<__nv_bfloat162*>(&v.v[i]) = __floats2bfloat162_rn(x[i], x[i + 1]);
 }
 
 // A thread holds W pairs (two vectors of W channels, or with W = 1 two channels) of a token, or a vector
 // of channels that no pair holds, for `per` heads, four of them in flight. Pairs whose channels lie apart:
 // channels first and second; adjacent ones: 2 W channels side by side.
-template <typename E, int W>
-__global__ void __launch_bounds__(kThreads) pairs_kernel(const Rotary a) {
+template <typename E, int W, bool ADJACENT>
+__global__ void __launch_bounds__(kThreads, 3) pairs_kernel(const Rotary a) {
     tc::pdl_trigger();
     tc::pdl_wait();
     const int blocks = a.P / W, units = blocks + (a.copies ? (a.D - 2 * a.P) / W : 0);
-    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (id >= a.B * a.N * units) return;
-    const int64_t row = id / units;
-    const int unit = (int)(id - row * units);
-    const int64_t b = row / a.N, n = row - b * a.N;
+    // the block's first row and unit, and from there (units are at most 1,024)
+    const int64_t id0 = (int64_t)blockIdx.x * kThreads;
+    const int row0 = (int)(id0 / units), in0 = (int)(id0 - (int64_t)row0 * units) + threadIdx.x;
+    const int row = row0 + in0 / units, unit = in0 % units;
+    if (row >= a.rows) return;
+    const int b = row / a.N, n = row - b * a.N;
     const int h0 = blockIdx.y * a.per, h1 = min(a.H, h0 + a.per);
     if (unit >= blocks) {
         const int c = 2 * a.P + (unit - blocks) * W;
-        for (int h = h0; h < h1; ++h) {
-            int hh;
-            const Side& s = side_of(a, h, hh);
-            store<E, W>((E*)s.y + b * s.yb + hh * s.yh + n * s.yn + c,
-                        load<E, W>((const E*)s.x + b * s.xb + hh * s.xh + n * s.xn + c));
+        for (int k = 0; k < 2; ++k) {
+            Rows<E> r = rows_on<E>(a, k, b, n, h0, h1);
+            for (; r.heads > 0; --r.heads, r.x += r.xh, r.y += r.yh)
+                store<E, W>(r.y + c, load<E, W>(r.x + c));
         }
         return;
     }
     const int p0 = unit * W;
-    int first = 2 * p0, second = 2 * p0 + W;
-    const bool adjacent = a.pairing == FLAREPP_ROTARY_ADJACENT;
+    int first = 2 * p0, second = 2 * p0 + W;  // adjacent ones
+    constexpr bool adjacent = ADJACENT && W > 1;
     if (a.pairing == FLAREPP_ROTARY_HALVES) first = p0, second = p0 + a.P;
     if (a.pairing == FLAREPP_ROTARY_AXES_APART) {
         const int k = axis_of(a, p0), start = k ? a.ends[k - 1] : 0;
         first = p0 + start;
         second = first + a.ends[k] - start;
     }
-    if (adjacent && W == 1) second = first + 1;
     float cs[W], sn[W];
     int held = -1;
     float p = 0.f, q = 0.f;
@@ -135,126 +168,161 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(const Rotary a) {
         sn[i] *= a.sign;
     }
     constexpr int kFlight = 4;
-    for (int h = h0; h < h1; h += kFlight) {
-        Pack<E, W> u[kFlight], v[kFlight];
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        Rows<E> r = rows_on<E>(a, k, b, n, h0, h1);
+#pragma unroll 1
+        for (; r.heads > 0; r.heads -= kFlight) {
+            Pack<E, W> u[kFlight], v[kFlight];
 #pragma unroll
-        for (int j = 0; j < kFlight; ++j)
-            if (h + j < h1) {
-                int hh;
-                const Side& s = side_of(a, h + j, hh);
-                const E* x = (const E*)s.x + b * s.xb + hh * s.xh + n * s.xn;
-                u[j] = load<E, W>(x + first);
-                v[j] = load<E, W>(x + second);
-            }
-#pragma unroll
-        for (int j = 0; j < kFlight; ++j)
-            if (h + j < h1) {
-                int hh;
-                const Side& s = side_of(a, h + j, hh);
-                if (adjacent && W > 1) {
-#pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        E& ex = i < W / 2 ? u[j].v[2 * i % W] : v[j].v[2 * i % W];
-                        E& ey = i < W / 2 ? u[j].v[(2 * i + 1) % W] : v[j].v[(2 * i + 1) % W];
-                        const float x = widen(ex), y = widen(ey);
-                        narrow(ex, x * cs[i] - y * sn[i]);
-                        narrow(ey, y * cs[i] + x * sn[i]);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        const float x = widen(u[j].v[i]), y = widen(v[j].v[i]);
-                        narrow(u[j].v[i], x * cs[i] - y * sn[i]);
-                        narrow(v[j].v[i], y * cs[i] + x * sn[i]);
-                    }
+            for (int j = 0; j < kFlight; ++j)
+                if (j < r.heads) {
+                    u[j] = load<E, W>(r.x + first);
+                    v[j] = load<E, W>(r.x + second);
+                    r.x += r.xh;
                 }
-                E* o = (E*)s.y + b * s.yb + hh * s.yh + n * s.yn;
-                store<E, W>(o + first, u[j]);
-                store<E, W>(o + second, v[j]);
-            }
+#pragma unroll
+            for (int j = 0; j < kFlight; ++j)
+                if (j < r.heads) {
+                    float x[2 * W];
+                    widen_all<E, W>(u[j], x);
+                    widen_all<E, W>(v[j], x + W);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {  // adjacent pairs lie side by side in u and v
+                        float& p0 = adjacent ? x[2 * i] : x[i];
+                        float& p1 = adjacent ? x[2 * i + 1] : x[W + i];
+                        const float q0 = p0, q1 = p1;
+                        p0 = q0 * cs[i] - q1 * sn[i];
+                        p1 = q1 * cs[i] + q0 * sn[i];
+                    }
+                    narrow_all(u[j], x);
+                    narrow_all(v[j], x + W);
+                    store<E, W>(r.y + first, u[j]);
+                    store<E, W>(r.y + second, v[j]);
+                    r.y += r.yh;
+                }
+        }
     }
 }
 
 // Pairs that no vector divides (sections of 6, 5 and 5, say): a thread holds a vector of a token's channels
-// as they lie, and their partners come through shared memory, four heads at a time. On a mesh of a million
-// points and 16 heads of 32 channels the channels one by one would be 2-byte accesses.
+// as they lie, and their partners come through shared memory, four heads at a time, within a warp. The warp's tokens' sines
+// and cosines are taken once a pair, into a table that every thread reads its channels' from. (On a mesh of a
+// million points and 16 heads of 32 channels a sine for every channel took 610 us instead of 441.)
+// A stage holds vector v (16 bytes) with its words turned by v / 8: the threads of a warp ask for one value each
+// of vectors side by side, which without that lie in 8 of 32 banks.
+__device__ __forceinline__ uint32_t staged_at(int value, int size) {  // the byte where a value lies
+    const uint32_t at = value * size, v = at / 16, w = at % 16 / 4;
+    return v * 16 + ((w + v / 8) & 3) * 4 + at % 4;
+}
+__device__ __forceinline__ uint4 turned(uint4 d, int by) {
+    if (by & 1) d = make_uint4(d.w, d.x, d.y, d.z);
+    if (by & 2) d = make_uint4(d.z, d.w, d.x, d.y);
+    return d;
+}
+
 template <typename E, int W>
-__global__ void __launch_bounds__(kThreads) rows_kernel(const Rotary a, int tokens) {
+__global__ void __launch_bounds__(kThreads, 3) rows_kernel(const Rotary a, int tokens) {
     tc::pdl_trigger();
     tc::pdl_wait();
     constexpr int kFlight = 4;
-    __shared__ __align__(16) E stage[2][kFlight][kThreads * W];
-    const int vectors = a.D / W, t = threadIdx.x;
-    const int token = t / vectors, c0 = (t - token * vectors) * W;
-    const int64_t row = (int64_t)blockIdx.x * tokens + token;
-    const bool live = token < tokens && row < a.B * a.N;
-    const int64_t b = live ? row / a.N : 0, n = live ? row - b * a.N : 0;
-    const int h0 = blockIdx.y * a.per, h1 = min(a.H, h0 + a.per);
-    float cs[W], sn[W];  // a channel's own: its value times cs plus its partner's times sn
-    int other[W];        // where its partner lies in a stage
-    const int rows = token * a.D;
-    {
-        int held = -1;
-        float p = 0.f, q = 0.f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const int c = c0 + i;
-            cs[i] = 1.f;
-            sn[i] = 0.f;
-            other[i] = rows + c;
-            if (!live || c >= 2 * a.P) continue;
-            int pair, partner;
-            float sign = -a.sign;
-            if (a.pairing == FLAREPP_ROTARY_HALVES) {
-                pair = c < a.P ? c : c - a.P;
-                partner = c < a.P ? c + a.P : c - a.P;
-                if (c >= a.P) sign = a.sign;
-            } else if (a.pairing == FLAREPP_ROTARY_ADJACENT) {
-                pair = c >> 1;
-                partner = c ^ 1;
-                if (c & 1) sign = a.sign;
-            } else {
-                int k = 0;
-                while (k < a.axes - 1 && c >= 2 * a.ends[k]) ++k;
-                const int start = k ? a.ends[k - 1] : 0, size = a.ends[k] - start;
-                const bool low = c - 2 * start < size;
-                pair = low ? c - start : c - start - size;
-                partner = low ? c + size : c - size;
-                if (!low) sign = a.sign;
-            }
-            const int k = axis_of(a, pair);
-            if (k != held) position(a, b, n, held = k, p, q);
-            turn_of(p, q, a.freqs[pair], cs[i], sn[i]);
-            sn[i] *= sign;
-            other[i] = rows + partner;
+    constexpr uint32_t kHead = 32 * 16;  // bytes of a head's stage of a warp
+    __shared__ __align__(16) uint8_t stages[kThreads / 32][kFlight * kHead];
+    __shared__ int places[kMaxDim];  // by channel: its pair, its partner, and whether it is the first
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint8_t* const stage = stages[warp];
+    float2* const table = reinterpret_cast<float2*>(stage);  // [tokens][P], before the stage is used
+    for (int pair = threadIdx.x; pair < a.P; pair += kThreads) {
+        int first = 2 * pair, second = 2 * pair + 1;
+        if (a.pairing == FLAREPP_ROTARY_HALVES) first = pair, second = pair + a.P;
+        if (a.pairing == FLAREPP_ROTARY_AXES_APART) {
+            const int k = axis_of(a, pair), start = k ? a.ends[k - 1] : 0;
+            first = pair + start;
+            second = first + a.ends[k] - start;
         }
+        places[first] = pair << 16 | second << 1 | 1;
+        places[second] = pair << 16 | first << 1;
     }
-    int buf = 0;
-    for (int h = h0; h < h1; h += kFlight, buf ^= 1) {
-        Pack<E, W> u[kFlight];
+    __syncthreads();
+    // the warp's tokens, and the lane's vector of one of them
+    const int vectors = a.D / W, token = lane / vectors, c0 = (lane - token * vectors) * W;
+    const int64_t first_row = ((int64_t)blockIdx.x * (kThreads / 32) + warp) * tokens;
+    if (first_row >= a.rows) return;
+    const int row0 = (int)first_row, row = row0 + token;
+    const bool live = token < tokens && row < a.rows;
+    const int b = live ? row / a.N : 0, n = live ? row - b * a.N : 0;
+    const int h0 = blockIdx.y * a.per, h1 = min(a.H, h0 + a.per);
+    for (int e = lane; e < tokens * a.P; e += 32) {
+        const int k = e / a.P, pair = e - k * a.P, r = row0 + k;
+        if (r >= a.rows) break;
+        const int bk = r / a.N;
+        float p, q, c, s;
+        position(a, bk, r - bk * a.N, axis_of(a, pair), p, q);
+        turn_of(p, q, a.freqs[pair], c, s);
+        table[e] = make_float2(c, s * a.sign);
+    }
+    __syncwarp();
+    float cs[W], sn[W];  // a channel's own: its value times cs plus its partner's times sn
+    uint32_t from[W];    // where its partner lies in a stage
+    const int rows = token * a.D;
+    uint32_t own = 0;    // a bit for every channel that has no partner
 #pragma unroll
-        for (int j = 0; j < kFlight; ++j)
-            if (live && h + j < h1) {
-                int hh;
-                const Side& s = side_of(a, h + j, hh);
-                u[j] = load<E, W>((const E*)s.x + b * s.xb + hh * s.xh + n * s.xn + c0);
-            }
+    for (int i = 0; i < W; ++i) {
+        const int c = c0 + i;
+        cs[i] = 1.f;
+        sn[i] = 0.f;
+        from[i] = 0;
+        if (!live || c >= 2 * a.P) {
+            own |= 1u << i;
+            continue;
+        }
+        const int place = places[c];
+        const float2 v = table[token * a.P + (place >> 16)];
+        cs[i] = v.x;
+        sn[i] = place & 1 ? -v.y : v.y;
+        from[i] = staged_at(rows + (place >> 1 & 0x7fff), sizeof(E));
+    }
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        Rows<E> r = rows_on<E>(a, k, b, n, h0, h1);
+        r.x += c0;
+        r.y += c0;
+#pragma unroll 1
+        for (int left = r.heads; left > 0; left -= kFlight) {
+            Pack<E, W> u[kFlight];
+            const int now = live ? left : 0;
 #pragma unroll
-        for (int j = 0; j < kFlight; ++j)
-            if (live && h + j < h1) store<E, W>(&stage[buf][j][rows + c0], u[j]);
-        __syncthreads();  // the stage before is read by all once this one is passed
-#pragma unroll
-        for (int j = 0; j < kFlight; ++j)
-            if (live && h + j < h1) {
-                int hh;
-                const Side& s = side_of(a, h + j, hh);
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const float x = widen(u[j].v[i]), y = widen(stage[buf][j][other[i]]);
-                    if (other[i] != rows + c0 + i) narrow(u[j].v[i], x * cs[i] + y * sn[i]);
+            for (int j = 0; j < kFlight; ++j)
+                if (j < now) {
+                    u[j] = load<E, W>(r.x);
+                    r.x += r.xh;
                 }
-                store<E, W>((E*)s.y + b * s.yb + hh * s.yh + n * s.yn + c0, u[j]);
-            }
+            __syncwarp();  // the stage (or the table) is read
+#pragma unroll
+            for (int j = 0; j < kFlight; ++j)
+                if (j < now)
+                    *reinterpret_cast<uint4*>(stage + lane * 16 + j * kHead) =
+                        turned(*reinterpret_cast<const uint4*>(&u[j]), lane / 8);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kFlight; ++j)
+                if (j < now) {
+                    float x[W];
+                    widen_all<E, W>(u[j], x);
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+                        x[i] = fmaf(widen(*reinterpret_cast<const E*>(stage + from[i] + j * kHead)), sn[i],
+                                    x[i] * cs[i]);
+                    const Pack<E, W> old = u[j];
+                    narrow_all(u[j], x);
+                    if (own)
+#pragma unroll
+                        for (int i = 0; i < W; ++i)
+                            if (own >> i & 1) u[j].v[i] = old.v[i];
+                    store<E, W>(r.y, u[j]);
+                    r.y += r.yh;
+                }
+        }
     }
 }
 
@@ -286,10 +354,11 @@ int heads_per_thread(int64_t threads, int heads) {
 template <typename E>
 cudaError_t enqueue(Rotary a, bool whole, bool pairs_whole, cudaStream_t st) {
     constexpr int W = 16 / sizeof(E);
-    const int64_t rows = a.B * a.N;
+    const int64_t rows = a.rows;
+    if (whole && !pairs_whole && a.D / W > 32) whole = false;  // rows of more than a warp: channel by channel
     if (whole && !pairs_whole) {
-        const int tokens = kThreads / (a.D / W);
-        const int64_t blocks = cdiv(rows, tokens);
+        const int tokens = 32 / (a.D / W);  // of a warp
+        const int64_t blocks = cdiv(rows, tokens * (kThreads / 32));
         a.per = heads_per_thread(blocks * kThreads, a.H);
         if (blocks > INT32_MAX) return cudaErrorInvalidValue;
         return launch(rows_kernel<E, W>, dim3((unsigned)blocks, (unsigned)cdiv(a.H, a.per)), st, a,
@@ -302,7 +371,9 @@ cudaError_t enqueue(Rotary a, bool whole, bool pairs_whole, cudaStream_t st) {
     if (blocks > INT32_MAX) return cudaErrorInvalidValue;
     a.per = heads_per_thread(blocks * kThreads, a.H);
     const dim3 grid((unsigned)blocks, (unsigned)cdiv(a.H, a.per));
-    return whole ? launch(pairs_kernel<E, W>, grid, st, a) : launch(pairs_kernel<E, 1>, grid, st, a);
+    if (!whole) return launch(pairs_kernel<E, 1, false>, grid, st, a);
+    return a.pairing == FLAREPP_ROTARY_ADJACENT ? launch(pairs_kernel<E, W, true>, grid, st, a)
+                                                : launch(pairs_kernel<E, W, false>, grid, st, a);
 }
 
 // One side's tensors: FLAREPP_OK, or what is wrong with them.
@@ -334,7 +405,8 @@ flarepp_status rotary(const flarepp_rotary_shape* s, const void* positions, cons
     if (s->axes < 1 || s->axes > kMaxAxes) return FLAREPP_ERR_INVALID_ARGUMENT;
     if (s->pairing < FLAREPP_ROTARY_HALVES || s->pairing > FLAREPP_ROTARY_AXES_APART)
         return FLAREPP_ERR_INVALID_ARGUMENT;
-    if (s->D > kMaxDim || s->Hq > 65535 || s->Hk > 65535 || s->B > INT32_MAX || s->N > INT32_MAX)
+    if (s->D > kMaxDim || s->Hq > 65535 || s->Hk > 65535 ||
+        s->N > INT32_MAX - 1024 || (s->N && s->B > (INT32_MAX - 1024) / s->N))
         return FLAREPP_ERR_UNSUPPORTED;
     Rotary a{};
     int64_t P = 0;
@@ -371,7 +443,7 @@ flarepp_status rotary(const flarepp_rotary_shape* s, const void* positions, cons
             if (j < i && !apart(*out[i], d[i], *out[j], d[j])) return FLAREPP_ERR_INVALID_ARGUMENT;
         }
     }
-    a.B = s->B, a.N = s->N, a.D = (int)s->D, a.P = (int)P;
+    a.rows = (int)(s->B * s->N), a.N = (int)s->N, a.D = (int)s->D, a.P = (int)P;
     a.Hq = (int)s->Hq, a.H = (int)(s->Hq + s->Hk);
     a.axes = s->axes, a.pairing = s->pairing;
     a.sign = s->inverse ? -1.f : 1.f;

@@ -110,6 +110,14 @@ def test_wide(C, G):
     check(2, 1, C, G, "silu", torch.float32)
 
 
+@pytest.mark.parametrize("C", [8, 96, 132, 512, 1000, 1024, 1028])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_layer_norm(C, dtype):
+    """One group and one row: what one warp holds, and more."""
+    check(700, 1, C, 1, "none", dtype)
+    check(3, 1, C * 3, 3, "gelu", dtype)
+
+
 @pytest.mark.parametrize("B,N", [(1, 40000), (700, 20), (5000, 1), (2000, 7)])
 def test_many(B, N):
     check(B, N, 48, 3, "gelu", torch.bfloat16)
