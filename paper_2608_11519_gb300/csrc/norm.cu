@@ -1062,7 +1062,7 @@ flarepp_status group_norm(bool back, const flarepp_norm_shape* shape, const void
                           (const void*)dbeta, (const void*)stats, (const void*)lengths,
                           (const void*)status})
         if (t && !aligned4(t)) return FLAREPP_ERR_INVALID_ARGUMENT;
-    const Plan p = plan_of(s, back);
+    const Plan p = n ? plan_of(s, back) : Plan{};
     const bool sums = back && (dgamma || dbeta);
     if (n) {
         if (!x || !y || (back && (!dy || !stats))) return FLAREPP_ERR_INVALID_ARGUMENT;
