@@ -10,7 +10,8 @@
 // do not fill the SMs evenly, sequences are cut, and a first walk (only A and V, only S, only in front
 // of the cuts) and a join over the blocks find the states there.
 //
-// W o (X A^T), S and w o V are rounded to bf16 as operands; sums, states and what r multiplies are float32.
+// W o (X A^T) is rounded to bf16 as an operand, w o V and S are two bf16 each (Cfg says why and where not); sums,
+// states and what r multiplies are float32.
 //
 // Roles (24 warps, a block an SM): warp 0 loads tiles (A, X, V of each chunk, a ring), warps 1 and 2 issue the
 // products, warps 4 to 11 make W o (X A^T), warps 12 to 15 write Y, warps 16 to 19 keep the state, warps 20 to
@@ -58,18 +59,23 @@ struct Cfg {
     static constexpr int kSlot = (TK > TV ? TK : TV) * kChunk * 2;
     // Values of up to 64 channels leave room for two sets of scores, of X S and of decayed values.
     static constexpr int kSets = TV == 64 ? 2 : 1;
-    static constexpr int kVw = TV * kChunk * 2;
+    // Decayed values and the state go into their products as two bf16 each, the second what the first's
+    // rounding left: so a state is as good as its 32 bits but for some 2^-17, and X S as good as the state.
+    static constexpr int kVwSets = TK == 64 && TV == 64 ? 2 : 1;
+    static constexpr bool kStTwo = TK * TV < 128 * 128;
+    static constexpr int kVw = TV * kChunk * 2;  // bytes of one of the two
     static constexpr int kSt = TK * TV * 2;
+    static constexpr int kExtra = kVwSets * 2 * kVw + (kStTwo ? 2 : 1) * kSt;
     static constexpr uint32_t kColY = kSets * 128;  // from 0 on: scores, and W o scores as bf16 over them
     static constexpr uint32_t kColX = kColY + TV;
     static constexpr uint32_t kColS = kColX + kSets * TV;
     static constexpr uint32_t kTmem = 512;
-    static constexpr int kRoom = kMaxSmem - 1024 - kSets * kVw - kSt - 512;
+    static constexpr int kRoom = kMaxSmem - 1024 - kExtra - 512;
     static constexpr int kSlots = kRoom / kSlot < 12 ? kRoom / kSlot : 12;
     static constexpr int kBars = 3 * kSlots + 14;
-    static constexpr int kBody = kSlots * kSlot + kSets * kVw + kSt;
+    static constexpr int kBody = kSlots * kSlot + kExtra;
     static constexpr int kSmem = 1024 + kBody + kBars * 8 + 16;
-    static_assert(kSlots >= 5 && kBars * 8 + 16 <= 512 && kSmem <= kMaxSmem, "shared memory");
+    static_assert(kSlots >= (kSets == 2 ? 5 : 3) && kBars * 8 + 16 <= 512 && kSmem <= kMaxSmem, "shared memory");
     static_assert(kColS + TV <= kTmem, "TMEM");
 };
 
@@ -222,10 +228,21 @@ __device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, u
         : "memory");
 }
 
-__device__ __forceinline__ uint4 scaled(uint4 d, float w) {
+// Two values as a pair of bf16, and a pair of what its rounding leaves.
+__device__ __forceinline__ uint32_t split_pair(uint64_t v, uint32_t& rest) {
+    const uint32_t hi = pack_bf16x2(v);
+    rest = pack_bf16x2(fma2(unpack_bf16x2(hi), pair(-1.f, -1.f), v));
+    return hi;
+}
+// 8 bf16 values times w, in two
+__device__ __forceinline__ uint4 scaled(uint4 d, float w, uint4& rest) {
     const uint64_t w2 = pair(w, w);
-    return make_uint4(pack_bf16x2(mul2(unpack_bf16x2(d.x), w2)), pack_bf16x2(mul2(unpack_bf16x2(d.y), w2)),
-                      pack_bf16x2(mul2(unpack_bf16x2(d.z), w2)), pack_bf16x2(mul2(unpack_bf16x2(d.w), w2)));
+    uint4 hi;
+    hi.x = split_pair(mul2(unpack_bf16x2(d.x), w2), rest.x);
+    hi.y = split_pair(mul2(unpack_bf16x2(d.y), w2), rest.y);
+    hi.z = split_pair(mul2(unpack_bf16x2(d.z), w2), rest.z);
+    hi.w = split_pair(mul2(unpack_bf16x2(d.w), w2), rest.w);
+    return hi;
 }
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
@@ -280,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* vw = smem + kSlots * C::kSlot;
-    uint8_t* st = vw + kSets * C::kVw;
+    uint8_t* st = vw + C::kVwSets * 2 * C::kVw;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBody);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -445,17 +462,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok) break;
             tc_fence_after();
             const uint32_t a = lower(tile(per * n), kAtomBytes), q = lower(tile(3 * n + 1), 16);
-            const uint32_t v = lower(smem_u32(vw + n % kSets * C::kVw), kAtomBytes);
+            const uint32_t v = lower(smem_u32(vw + n % C::kVwSets * 2 * C::kVw), kAtomBytes);
             const uint32_t to = tmem + C::kColX + n % kSets * TV;
             // (where TK is 64, A^T's rows from 64 on are whatever lies behind the tile: they are not used)
             if (elect_one()) {
                 if (!p.only_state)
 #pragma unroll
                     for (int s = 0; s < TK / 16; ++s)
-                        if (s < steps) product_ss(to, q + by_channel(s), s0 + by_row(s), outs, s > 0);
+                        if (s < steps) {
+                            product_ss(to, q + by_channel(s), s0 + by_row(s), outs, s > 0);
+                            if (C::kStTwo)
+                                product_ss(to, q + by_channel(s), s0 + (C::kSt >> 4) + by_row(s), outs, 1u);
+                        }
 #pragma unroll
-                for (int s = 0; s < kChunk / 16; ++s)
+                for (int s = 0; s < kChunk / 16; ++s) {
                     product_ss(tmem + C::kColS, a + by_row(s), v + by_row(s), states, 1u);
+                    product_ss(tmem + C::kColS, a + by_row(s), v + (C::kVw >> 4) + by_row(s), states, 1u);
+                }
                 mma_commit(of(u_ready, n));
             }
             __syncwarp();
@@ -697,12 +720,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (!p.only_state) {
                             // rows of 64 values, 16-byte pieces swapped as the tiles' are
                             uint8_t* d = st + c / 64 * (TK * 128) + row * 128;
+                            uint32_t hi[8], lo[8];
 #pragma unroll
-                            for (int j = 0; j < 16; j += 8) {
-                                const int piece = ((c % 64 + j) / 8) ^ (row & 7);
-                                *reinterpret_cast<uint4*>(d + 16 * piece) = make_uint4(
-                                    bf16_bits(r[j], r[j + 1]), bf16_bits(r[j + 2], r[j + 3]),
-                                    bf16_bits(r[j + 4], r[j + 5]), bf16_bits(r[j + 6], r[j + 7]));
+                            for (int j = 0; j < 8; ++j)
+                                hi[j] = split_pair(
+                                    pair(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), lo[j]);
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                uint4* e = reinterpret_cast<uint4*>(d + 16 * ((c % 64 / 8 + j) ^ (row & 7)));
+                                *e = make_uint4(hi[4 * j], hi[4 * j + 1], hi[4 * j + 2], hi[4 * j + 3]);
+                                if (C::kStTwo)
+                                    e[C::kSt / 16] =
+                                        make_uint4(lo[4 * j], lo[4 * j + 1], lo[4 * j + 2], lo[4 * j + 3]);
                             }
                         }
 #pragma unroll
@@ -774,12 +803,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // even fillings only, so each one of them has to be seen. Then: the buffer's last product is
                 // done, and whoever waited for its last filling has seen it.
                 ok = wait_tile(ia) && (p.only_state || wait_tile(ia + 1)) && wait_tile(iv) &&
-                     (n < kSets || wait_chunk(u_ready, n - kSets)) &&
+                     (n < C::kVwSets || wait_chunk(u_ready, n - C::kVwSets)) &&
                      (n < 2 || p.only_state || wait_chunk(y_ready, n - 2));
                 if (!ok) break;
                 uint8_t* v = smem + iv % kSlots * C::kSlot;
                 uint8_t* a = smem + ia % kSlots * C::kSlot;
-                uint8_t* to = vw + n % kSets * C::kVw;
+                uint8_t* to = vw + n % C::kVwSets * 2 * C::kVw;
                 if (rows == kChunk) {
                     float w = heaviest;
                     // the tiles' pieces are swapped by the row's last three bits
@@ -789,18 +818,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int e = 0; e < turns; ++e, o += step, w *= ratio)
 #pragma unroll
                         for (int t = 0; t < TV / 64; ++t)
+                        {
+                            uint4 rest;
                             *reinterpret_cast<uint4*>(to + o + t * kAtomBytes) =
-                                scaled(*reinterpret_cast<const uint4*>(v + o + t * kAtomBytes), w);
+                                scaled(*reinterpret_cast<const uint4*>(v + o + t * kAtomBytes), w, rest);
+                            *reinterpret_cast<uint4*>(to + C::kVw + o + t * kAtomBytes) = rest;
+                        }
                 } else {
                     // what lies behind the sequence may be another one, or no numbers at all
 #pragma unroll 1
                     for (int e = maker; e < TV * 16; e += 128) {
                         const int r = (e & 1023) >> 3;
                         const float w = exp2f(lg * (p.back ? r + 1 - p.lead : rows - p.lead - r)) * p.scale_w;
-                        uint4 d = make_uint4(0, 0, 0, 0);
-                        if (r < rows) d = scaled(*reinterpret_cast<const uint4*>(v + 16 * e), w);
+                        uint4 d = make_uint4(0, 0, 0, 0), rest = d;
+                        if (r < rows) d = scaled(*reinterpret_cast<const uint4*>(v + 16 * e), w, rest);
                         else *reinterpret_cast<uint4*>(v + 16 * e) = d;
                         *reinterpret_cast<uint4*>(to + 16 * e) = d;
+                        *reinterpret_cast<uint4*>(to + C::kVw + 16 * e) = rest;
                     }
 #pragma unroll 1
                     for (int e = maker; e < TK * 16; e += 128)
