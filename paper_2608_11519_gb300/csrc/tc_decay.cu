@@ -56,27 +56,38 @@ struct Walk {
 
 template <int TK, int TV>
 struct Cfg {
-    static constexpr int kSlot = (TK > TV ? TK : TV) * kChunk * 2;
-    // Values of up to 64 channels leave room for two sets of scores, of X S and of decayed values.
+    // Values of up to 64 channels leave room for two sets of scores and of X S.
     static constexpr int kSets = TV == 64 ? 2 : 1;
-    // Decayed values and the state go into their products as two bf16 each, the second what the first's
-    // rounding left: so a state is as good as its 32 bits but for some 2^-17, and X S as good as the state.
-    static constexpr int kVwSets = TK == 64 && TV == 64 ? 2 : 1;
-    static constexpr bool kStTwo = TK * TV < 128 * 128;
-    static constexpr int kVw = TV * kChunk * 2;  // bytes of one of the two
-    static constexpr int kSt = TK * TV * 2;
-    static constexpr int kExtra = kVwSets * 2 * kVw + (kStTwo ? 2 : 1) * kSt;
     static constexpr uint32_t kColY = kSets * 128;  // from 0 on: scores, and W o scores as bf16 over them
     static constexpr uint32_t kColX = kColY + TV;
     static constexpr uint32_t kColS = kColX + kSets * TV;
     static constexpr uint32_t kTmem = 512;
-    static constexpr int kRoom = kMaxSmem - 1024 - kExtra - 512;
-    static constexpr int kSlots = kRoom / kSlot < 12 ? kRoom / kSlot : 12;
-    static constexpr int kBars = 3 * kSlots + 14;
-    static constexpr int kBody = kSlots * kSlot + kExtra;
-    static constexpr int kSmem = 1024 + kBody + kBars * 8 + 16;
-    static_assert(kSlots >= (kSets == 2 ? 5 : 3) && kBars * 8 + 16 <= 512 && kSmem <= kMaxSmem, "shared memory");
     static_assert(kColS + TV <= kTmem, "TMEM");
+    // Shared memory: rings of tiles, as many as there is room for; of A, X and V each, so that a ring's slot
+    // only ever holds one kind.
+    static constexpr bool kWide = TK == 128 && TV == 128;
+    static constexpr int kA = TK == 64 && TV == 64 ? 3 : 2, kX = kWide ? 1 : kA, kV = kA;
+    static constexpr int kTileK = TK * kChunk * 2, kTileV = TV * kChunk * 2;
+    // Decayed values and the state go into their products as two bf16 each, the second what the first's
+    // rounding left: so a state is as good as its 32 bits but for some 2^-17, and X S as good as the state
+    // (with both widths above 64 there is no room for the state's second: X S then carries its rounding).
+    // Decayed values pass in parts of a chunk's tokens, so that some are made while others are multiplied.
+    static constexpr bool kStTwo = !kWide;
+    static constexpr int kParts = TV == 128 ? 4 : TK == 128 ? 2 : 1;
+    static constexpr int kBufs = TV == 128 ? (kWide ? 2 : 4) : 2;
+    static constexpr int kPart = kChunk / kParts;      // tokens
+    static constexpr int kVw = kPart * TV * 2;         // bytes of one of the two
+    static constexpr int kSt = TK * TV * 2;
+    static constexpr int kOffX = kA * kTileK, kOffV = kOffX + kX * kTileK, kOffVw = kOffV + kV * kTileV;
+    static constexpr int kOffSt = kOffVw + kBufs * 2 * kVw;
+    static constexpr int kBody = kOffSt + (kStTwo ? 2 : 1) * kSt;
+    // barriers
+    static constexpr int kFullA = 0, kFullX = kA, kFullV = kFullX + kX, kEmptyA = kFullV + kV,
+                         kEmptyX = kEmptyA + kA, kEmptyV = kEmptyX + kX, kOut = kEmptyV + kV,
+                         kVFull = kOut + kV, kVFree = kVFull + kBufs, kOther = kVFree + kBufs;
+    static constexpr int kBars = kOther + 14;
+    static constexpr int kSmem = 1024 + kBody + kBars * 8 + 16;
+    static_assert(kSmem <= kMaxSmem, "shared memory");
 };
 
 // A part of a sequence of one head, as a block walks it: chunks c0 to c1 of `total`, counted as walked.
@@ -292,33 +303,27 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const __grid_constant__ CUtensorMap tV, const __grid_constant__ CUtensorMap tY,
                 const __grid_constant__ Walk p) {
     using C = Cfg<TK, TV>;
-    constexpr int kSlots = C::kSlots;
     constexpr uint32_t kSets = C::kSets;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    uint8_t* vw = smem + kSlots * C::kSlot;
-    uint8_t* st = vw + C::kVwSets * 2 * C::kVw;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBody);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8u * kSlots, out0 = empty0 + 8u * kSlots;
+    const uint32_t bar0 = smem_u32(bars);
     // Of each but the last two there are two, for even and odd chunks: whoever waits for chunk n's phase must
     // not find that of chunk n + 1 done too, and no barrier's phase n + 2 comes before all have seen n.
-    const uint32_t s_ready = out0 + 8u * kSlots, p_ready = s_ready + 16, v_ready = s_ready + 32,
+    const uint32_t s_ready = bar0 + 8u * C::kOther, p_ready = s_ready + 16, clean = s_ready + 32,
                    u_ready = s_ready + 48, y_ready = s_ready + 64, y_free = s_ready + 80;
     const uint32_t b_ready = s_ready + 96, done = s_ready + 104;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kSlots; ++s) {
-            mbar_init(full0 + 8u * s, 1);
-            mbar_init(empty0 + 8u * s, 2);
-            mbar_init(out0 + 8u * s, 128);
-        }
+        for (int s = 0; s < C::kOther; ++s)
+            mbar_init(bar0 + 8u * s, s >= C::kEmptyA && s < C::kEmptyV ? 2 : s >= C::kOut && s < C::kVFree ? 128 : 1);
         for (uint32_t s = 0; s < 16; s += 8) {
             mbar_init(s_ready + s, 1);
             mbar_init(p_ready + s, 256);
-            mbar_init(v_ready + s, 128);
+            mbar_init(clean + s, 128);
             mbar_init(u_ready + s, 1);
             mbar_init(y_ready + s, 1);
             mbar_init(y_free + s, 128);
@@ -344,7 +349,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     Feed feed;
     Piece here;
-    const int per = p.only_state ? 2 : 3;  // tiles of a chunk
     const int width = (p.Dv + 15) / 16 * 16;  // columns of the products
     const int steps = (p.Da + 15) / 16;       // steps of a product over Da
     // the barrier of chunk n, and its phase there
@@ -352,53 +356,61 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto wait_chunk = [&](uint32_t bar, uint32_t n) {
         return wait_for(bar + 8u * (n & 1), (n >> 1) & 1, abort_flag, p.waits);
     };
-    auto wait_tile = [&](uint32_t t) {
-        return wait_for(full0 + 8u * (t % kSlots), (t / kSlots) & 1, abort_flag, p.waits);
+    // a ring's barrier (of `size`, the first at `first`) for its n-th use, and a wait for that use
+    auto ring = [&](int first, int size, uint32_t n) { return bar0 + 8u * (first + n % size); };
+    auto wait_use = [&](int first, int size, uint32_t n) {
+        return wait_for(bar0 + 8u * (first + n % size), n / size & 1, abort_flag, p.waits);
     };
-    auto tile = [&](uint32_t t) { return smem_u32(smem + t % kSlots * C::kSlot); };
+    auto tile_a = [&](uint32_t n) { return smem + n % C::kA * C::kTileK; };
+    auto tile_x = [&](uint32_t n) { return smem + C::kOffX + n % C::kX * C::kTileK; };
+    auto tile_v = [&](uint32_t n) { return smem + C::kOffV + n % C::kV * C::kTileV; };
 
     if (warp == 0) {
         // ------------------------------------------------------------ loads: A, X, V
-        uint32_t it = 0;
+        uint32_t it = 0, n = 0, used_x = 0;  // tiles and chunks; those of X
         bool ok = true;
         begin_feed(p, blockIdx.x, feed);
         while (ok && next_walked(p, feed, here)) {
             const Piece x = here;
             const int b = p.cuts ? 0 : x.sequence, h = x.h;
-            for (int c = x.c0; c < x.c1 && ok; ++c) {
+            for (int c = x.c0; c < x.c1 && ok; ++c, ++n) {
                 int rows;
                 const int token = chunk_at(p, x, c, rows);
-                for (int j = 0; j < per; ++j, ++it) {
-                    const int s = it % kSlots;
-                    const uint32_t full = full0 + 8u * s;
-                    if (it >= (uint32_t)kSlots &&
-                        !wait_for(empty0 + 8u * s, (it / kSlots - 1) & 1, abort_flag, p.waits)) {
-                        ok = false;
-                        break;
-                    }
+                auto load = [&](int full, int empty, int size, uint32_t bytes, auto&& issue) {
+                    if (n >= (uint32_t)size && !wait_use(empty, size, n - size)) return false;
                     if (elect_one() && !(blockIdx.x == 0 && it == p.waits.withheld)) {
-                        const uint32_t dst = smem_u32(smem + s * C::kSlot);
-                        const int what = p.only_state && j == 1 ? 2 : j;
-                        mbar_expect_tx(full, (what == 2 ? TV : TK) * kChunk * 2);
-                        if (what == 0)
-                            load_rows<TK>(dst, &tA, token, p.ga ? h / p.ga : 0, b * p.ma, full);
-                        else if (what == 1)
-                            load_rows<TK>(dst, &tX, token, p.gx ? h / p.gx : 0, b * p.mx, full);
-                        else
-                            load_rows<TV>(dst, &tV, token, p.gv ? h / p.gv : 0, b * p.mv, full);
+                        mbar_expect_tx(ring(full, size, n), bytes);
+                        issue(ring(full, size, n));
                     }
                     __syncwarp();
+                    ++it;
+                    return true;
+                };
+                ok = load(C::kFullA, C::kEmptyA, C::kA, C::kTileK, [&](uint32_t bar) {
+                    load_rows<TK>(smem_u32(tile_a(n)), &tA, token, p.ga ? h / p.ga : 0, b * p.ma, bar);
+                });
+                if (ok && !p.only_state) {
+                    ok = load(C::kFullX, C::kEmptyX, C::kX, C::kTileK, [&](uint32_t bar) {
+                        load_rows<TK>(smem_u32(tile_x(n)), &tX, token, p.gx ? h / p.gx : 0, b * p.mx, bar);
+                    });
+                    used_x += ok;
                 }
+                ok = ok && load(C::kFullV, C::kEmptyV, C::kV, C::kTileV, [&](uint32_t bar) {
+                    load_rows<TV>(smem_u32(tile_v(n)), &tV, token, p.gv ? h / p.gv : 0, b * p.mv, bar);
+                });
+                if (!ok) break;  // (n stays this chunk's)
             }
         }
         if (!ok) {  // wait (bounded) until every copy issued has landed
             const uint64_t t0 = globaltimer_ns();
-            for (int s = 0; s < kSlots && (uint32_t)s < it; ++s) {
-                const uint32_t last = it - 1 - ((it - 1 - s) % kSlots);
-                while (!mbar_try_wait(full0 + 8u * s, (last / kSlots) & 1) &&
-                       globaltimer_ns() - t0 < kWaitLimitNs) {
-                }
-            }
+            const uint32_t per = p.only_state ? 2 : 3;
+            const uint32_t uses[3] = {(it + per - 1) / per, used_x, it / per};
+            const int first[3] = {C::kFullA, C::kFullX, C::kFullV}, size[3] = {C::kA, C::kX, C::kV};
+            for (int k = 0; k < 3; ++k)
+                for (uint32_t u = uses[k] < (uint32_t)size[k] ? 0 : uses[k] - size[k]; u < uses[k]; ++u)
+                    while (!mbar_try_wait(ring(first[k], size[k], u), u / size[k] & 1) &&
+                           globaltimer_ns() - t0 < kWaitLimitNs) {
+                    }
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ products: X A^T, and (W o X A^T) V
@@ -414,10 +426,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const uint32_t n = m;
                 // (the scores go over the W o scores that an earlier product has read: nothing orders the two
                 // but its end)
-                ok = wait_tile(3 * n) && wait_tile(3 * n + 1) && (n < kSets || wait_chunk(y_ready, n - kSets));
+                ok = wait_use(C::kFullA, C::kA, n) && wait_use(C::kFullX, C::kX, n) &&
+                     (n < kSets || wait_chunk(y_ready, n - kSets));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t a = lower(tile(3 * n), 16), q = lower(tile(3 * n + 1), 16);
+                const uint32_t a = lower(smem_u32(tile_a(n)), 16), q = lower(smem_u32(tile_x(n)), 16);
                 const uint32_t to = tmem + n % kSets * 128;
                 if (elect_one()) {
 #pragma unroll
@@ -429,11 +442,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (m >= (int)kSets - 1) {
                 const uint32_t n = m - (kSets - 1);
-                ok = wait_chunk(v_ready, n) && wait_chunk(p_ready, n) &&
+                ok = wait_use(C::kFullV, C::kV, n) && wait_chunk(clean, n) && wait_chunk(p_ready, n) &&
                      (n == 0 || wait_chunk(y_free, n - 1));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t v = lower(tile(3 * n + 2), kAtomBytes), w = tmem + n % kSets * 128;
+                const uint32_t v = lower(smem_u32(tile_v(n)), kAtomBytes), w = tmem + n % kSets * 128;
                 if (elect_one()) {
 #pragma unroll
                     for (int s = 0; s < kChunk / 16; ++s)
@@ -452,21 +465,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------ products: X S, then S += A^T (w o V)
         const uint32_t states = idesc_bf16_f32(128, 16, true, true) + ((uint32_t)(width / 8 - 2) << 17);
         const uint32_t outs = idesc_bf16_f32(128, 16, false, true) + ((uint32_t)(width / 8 - 2) << 17);
-        const uint32_t s0 = lower(smem_u32(st), TK * 128);
+        const uint32_t s0 = lower(smem_u32(smem + C::kOffSt), TK * 128);
         const uint32_t total = count_chunks(p);
         bool ok = true;
-        for (uint32_t n = 0; n < total; ++n) {
-            ok = wait_tile(per * n) && (p.only_state || wait_tile(3 * n + 1)) &&
-                 (p.only_state || n < kSets || wait_chunk(y_free, n - kSets)) && wait_chunk(v_ready, n) &&
-                 wait_for(b_ready, n & 1, abort_flag, p.waits);
+        uint32_t g = 0;  // parts
+        for (uint32_t n = 0; ok && n < total; ++n) {
+            if (!p.only_state)
+                ok = wait_use(C::kFullX, C::kX, n) && (n < kSets || wait_chunk(y_free, n - kSets));
+            ok = ok && wait_use(C::kFullA, C::kA, n) && wait_for(b_ready, n & 1, abort_flag, p.waits);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t a = lower(tile(per * n), kAtomBytes), q = lower(tile(3 * n + 1), 16);
-            const uint32_t v = lower(smem_u32(vw + n % C::kVwSets * 2 * C::kVw), kAtomBytes);
+            const uint32_t a = lower(smem_u32(tile_a(n)), kAtomBytes), q = lower(smem_u32(tile_x(n)), 16);
             const uint32_t to = tmem + C::kColX + n % kSets * TV;
-            // (where TK is 64, A^T's rows from 64 on are whatever lies behind the tile: they are not used)
-            if (elect_one()) {
-                if (!p.only_state)
+            if (!p.only_state) {
+                if (elect_one()) {
 #pragma unroll
                     for (int s = 0; s < TK / 16; ++s)
                         if (s < steps) {
@@ -474,14 +486,29 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (C::kStTwo)
                                 product_ss(to, q + by_channel(s), s0 + (C::kSt >> 4) + by_row(s), outs, 1u);
                         }
-#pragma unroll
-                for (int s = 0; s < kChunk / 16; ++s) {
-                    product_ss(tmem + C::kColS, a + by_row(s), v + by_row(s), states, 1u);
-                    product_ss(tmem + C::kColS, a + by_row(s), v + (C::kVw >> 4) + by_row(s), states, 1u);
+                    mma_commit(ring(C::kEmptyX, C::kX, n));
                 }
-                mma_commit(of(u_ready, n));
+                __syncwarp();
             }
-            __syncwarp();
+            // (where TK is 64, A^T's rows from 64 on are whatever lies behind the tile: they are not used)
+#pragma unroll 1
+            for (int part = 0; part < C::kParts; ++part, ++g) {
+                ok = wait_use(C::kVFull, C::kBufs, g);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t v = lower(smem_u32(smem + C::kOffVw + g % C::kBufs * 2 * C::kVw), C::kPart * 128);
+                const uint32_t ap = a + by_row(part * (C::kPart / 16));
+                if (elect_one()) {
+#pragma unroll
+                    for (int s = 0; s < C::kPart / 16; ++s) {
+                        product_ss(tmem + C::kColS, ap + by_row(s), v + by_row(s), states, 1u);
+                        product_ss(tmem + C::kColS, ap + by_row(s), v + (C::kVw >> 4) + by_row(s), states, 1u);
+                    }
+                    mma_commit(ring(C::kVFree, C::kBufs, g));
+                    if (part == C::kParts - 1) mma_commit(of(u_ready, n));
+                }
+                __syncwarp();
+            }
         }
         if (elect_one()) mma_commit(done);
         __syncwarp();
@@ -489,7 +516,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) linger();
     } else if (warp == 3) {
         // ------------------------------------------------------------ stores of staged outputs
-        // (a barrier a slot, which is released once it is stored: the outputs may be several chunks ahead)
+        // (a barrier a slot, which is released once it is stored: the outputs may be several chunks ahead; the
+        // slots' phases count their staged uses alone)
         uint32_t n = 0, phases = 0;
         bool ok = true;
         begin_feed(p, blockIdx.x, feed);
@@ -500,18 +528,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                 int rows;
                 const int token = chunk_at(p, x, c, rows);
                 if (!staged(p, rows)) continue;
-                const uint32_t slot = (3 * n + 2) % kSlots;
-                ok = wait_for(out0 + 8u * slot, phases >> slot & 1, abort_flag, p.waits);
+                const uint32_t slot = n % C::kV;
+                ok = wait_for(bar0 + 8u * (C::kOut + slot), phases >> slot & 1, abort_flag, p.waits);
                 if (!ok) break;
                 phases ^= 1u << slot;
                 if (elect_one()) {
-                    const uint32_t from = tile(3 * n + 2);
+                    const uint32_t from = smem_u32(tile_v(n));
 #pragma unroll
                     for (int t = 0; t < TV / 64; ++t)
                         if (64 * t < p.Dv) tma_store_4d(&tY, from + t * kAtomBytes, 64 * t, token, h, b);
                     bulk_commit();
                     bulk_wait_read();
-                    mbar_arrive_n(empty0 + 8u * ((3 * n + 2) % kSlots), 2);
+                    mbar_arrive(ring(C::kEmptyV, C::kV, n));
                 }
                 __syncwarp();
             }
@@ -552,8 +580,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!ok) break;
                 tc_fence_after();
                 if (threadIdx.x == 128) {  // one of two that read A and X
-                    mbar_arrive(empty0 + 8u * (3 * n % kSlots));
-                    mbar_arrive(empty0 + 8u * ((3 * n + 1) % kSlots));
+                    mbar_arrive(ring(C::kEmptyA, C::kA, n));
+                    mbar_arrive(ring(C::kEmptyX, C::kX, n));
                 }
                 uint64_t f = first;
 #pragma unroll 1
@@ -625,8 +653,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // instruction, held up the state's through the pipe that they share: 241 us instead of 229
                 // for the prefill.)
                 const bool staging = staged(p, rows);
-                uint8_t* stage = smem + (3 * n + 2) % kSlots * C::kSlot + i * 128;
-                if (!staging && threadIdx.x == 384) mbar_arrive_n(empty0 + 8u * ((3 * n + 2) % kSlots), 2);
+                uint8_t* stage = tile_v(n) + i * 128;
+                if (!staging && threadIdx.x == 384) mbar_arrive(ring(C::kEmptyV, C::kV, n));
 #pragma unroll 1
                 for (int c = 0; c < p.Dv; c += 16) {
                     uint32_t y[16], s[16];
@@ -669,7 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mbar_arrive(of(y_free, n));
                 if (staging) {
                     fence_proxy_async();
-                    mbar_arrive(out0 + 8u * ((3 * n + 2) % kSlots));
+                    mbar_arrive(bar0 + 8u * (C::kOut + n % C::kV));
                 }
             }
         }
@@ -719,7 +747,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         tmem_wait_ld16(r);
                         if (!p.only_state) {
                             // rows of 64 values, 16-byte pieces swapped as the tiles' are
-                            uint8_t* d = st + c / 64 * (TK * 128) + row * 128;
+                            uint8_t* d = smem + C::kOffSt + c / 64 * (TK * 128) + row * 128;
                             uint32_t hi[8], lo[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
@@ -751,10 +779,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = wait_chunk(u_ready, n);
                 if (!ok) break;
                 tc_fence_after();
-                if (row == 0) {  // the other of the two that read A and X; without outputs A and V
-                    const uint32_t times = p.only_state ? 2 : 1;
-                    mbar_arrive_n(empty0 + 8u * (per * n % kSlots), times);
-                    mbar_arrive_n(empty0 + 8u * ((per * n + 1) % kSlots), times);
+                if (row == 0) {  // the other of the two that read A; without outputs the only one, and of V too
+                    mbar_arrive_n(ring(C::kEmptyA, C::kA, n), p.only_state ? 2 : 1);
+                    if (p.only_state) mbar_arrive(ring(C::kEmptyV, C::kV, n));
                 }
             }
             if (!ok) break;
@@ -782,67 +809,91 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         // ------------------------------------------------------------ decayed values
         const int maker = threadIdx.x - 640;
-        // a row's 16-byte pieces of a tile of 64 channels that hold values: 8 or 4
-        const int shift = width > 32 ? 3 : 2, turns = 1 << shift;  // tokens of the thread
-        uint32_t n = 0;
+        // a row's 16-byte pieces of a tile of 64 channels that hold values: 8, or 4 where parts are whole chunks
+        const int shift = C::kParts == 1 && width <= 32 ? 2 : 3;
+        const int stride = 128 >> shift, turns = C::kPart / stride;  // of a part: the thread's tokens
+        const int r0 = maker >> shift;
+        uint32_t n = 0, g = 0;
         bool ok = true;
         begin_feed(p, blockIdx.x, feed);
         while (ok && next_walked(p, feed, here)) {
             const Piece x = here;
             const float lg = head_decay(p, x.h, false);
-            // Of a whole chunk the thread takes a 16-byte piece of every 16th (or 32nd) token, from the one
-            // with the largest weight on: each next one's is `ratio` times the last's.
-            const int stride = 128 >> shift, r0 = p.back ? maker >> shift : 127 - (maker >> shift);
-            const float heaviest = exp2f(lg * (p.back ? r0 + 1 - p.lead : kChunk - p.lead - r0)) * p.scale_w;
+            // From the end of a part where its weights are largest on, each next one of the thread's tokens has
+            // `ratio` times the last one's weight.
             const float ratio = exp2f(lg * stride);
             for (int k = x.c0; k < x.c1; ++k, ++n) {
                 int rows;
                 chunk_at(p, x, k, rows);
-                const uint32_t ia = per * n, iv = ia + per - 1;
-                // All tiles in order, though most chunks' V is all that is read: a slot's phase tells odd from
-                // even fillings only, so each one of them has to be seen. Then: the buffer's last product is
-                // done, and whoever waited for its last filling has seen it.
-                ok = wait_tile(ia) && (p.only_state || wait_tile(ia + 1)) && wait_tile(iv) &&
-                     (n < C::kVwSets || wait_chunk(u_ready, n - C::kVwSets)) &&
-                     (n < 2 || p.only_state || wait_chunk(y_ready, n - 2));
+                ok = wait_use(C::kFullA, C::kA, n) && wait_use(C::kFullV, C::kV, n) &&
+                     (n < 2 || p.only_state || wait_chunk(y_ready, n - 2));  // clean's last phase is seen
                 if (!ok) break;
-                uint8_t* v = smem + iv % kSlots * C::kSlot;
-                uint8_t* a = smem + ia % kSlots * C::kSlot;
-                uint8_t* to = vw + n % C::kVwSets * 2 * C::kVw;
-                if (rows == kChunk) {
-                    float w = heaviest;
-                    // the tiles' pieces are swapped by the row's last three bits
-                    int o = r0 * 128 + 16 * ((maker & ((1 << shift) - 1)) ^ (r0 & 7));
-                    const int step = p.back ? stride * 128 : -stride * 128;
-#pragma unroll 2
-                    for (int e = 0; e < turns; ++e, o += step, w *= ratio)
+                uint8_t* v = tile_v(n);
+                if (rows < kChunk) {
+                    // what lies behind the sequence may be another one, or no numbers at all
+                    uint8_t* a = tile_a(n);
+#pragma unroll 1
+                    for (int e = 8 * rows + maker; e < 8 * kChunk; e += 128)
 #pragma unroll
                         for (int t = 0; t < TV / 64; ++t)
-                        {
-                            uint4 rest;
-                            *reinterpret_cast<uint4*>(to + o + t * kAtomBytes) =
-                                scaled(*reinterpret_cast<const uint4*>(v + o + t * kAtomBytes), w, rest);
-                            *reinterpret_cast<uint4*>(to + C::kVw + o + t * kAtomBytes) = rest;
-                        }
-                } else {
-                    // what lies behind the sequence may be another one, or no numbers at all
+                            *reinterpret_cast<uint4*>(v + 16 * e + t * kAtomBytes) = make_uint4(0, 0, 0, 0);
 #pragma unroll 1
-                    for (int e = maker; e < TV * 16; e += 128) {
-                        const int r = (e & 1023) >> 3;
-                        const float w = exp2f(lg * (p.back ? r + 1 - p.lead : rows - p.lead - r)) * p.scale_w;
-                        uint4 d = make_uint4(0, 0, 0, 0), rest = d;
-                        if (r < rows) d = scaled(*reinterpret_cast<const uint4*>(v + 16 * e), w, rest);
-                        else *reinterpret_cast<uint4*>(v + 16 * e) = d;
-                        *reinterpret_cast<uint4*>(to + 16 * e) = d;
-                        *reinterpret_cast<uint4*>(to + C::kVw + 16 * e) = rest;
-                    }
-#pragma unroll 1
-                    for (int e = maker; e < TK * 16; e += 128)
-                        if (((e & 1023) >> 3) >= rows)
-                            *reinterpret_cast<uint4*>(a + 16 * e) = make_uint4(0, 0, 0, 0);
+                    for (int e = 8 * rows + maker; e < 8 * kChunk; e += 128)
+#pragma unroll
+                        for (int t = 0; t < TK / 64; ++t)
+                            *reinterpret_cast<uint4*>(a + 16 * e + t * kAtomBytes) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async();
                 }
-                fence_proxy_async();
-                mbar_arrive(of(v_ready, n));
+                mbar_arrive(of(clean, n));
+#pragma unroll 1
+                for (int part = 0; part < C::kParts; ++part, ++g) {
+                    ok = g < (uint32_t)C::kBufs || wait_use(C::kVFree, C::kBufs, g - C::kBufs);
+                    if (!ok) break;
+                    uint8_t* to = smem + C::kOffVw + g % C::kBufs * 2 * C::kVw;
+                    // the thread's token with the part's largest weight, and where its piece lies: the tiles'
+                    // pieces are swapped by the row's last three bits
+                    const int row = p.back ? r0 : C::kPart - stride + r0;
+                    int at = part * C::kPart + row;
+                    int o = row * 128 + 16 * ((maker & ((1 << shift) - 1)) ^ (row & 7));
+                    const uint8_t* from = v + part * C::kPart * 128;
+                    const int step = p.back ? stride * 128 : -stride * 128;
+                    if (rows == kChunk) {
+                        float w = exp2f(lg * (p.back ? at + 1 - p.lead : kChunk - p.lead - at)) * p.scale_w;
+#pragma unroll 1
+                        for (int e = 0; e < turns; e += 4 / (TV / 64)) {
+                            uint4 d[4];  // as many as fit, read before the first is worked on
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                d[j] = *reinterpret_cast<const uint4*>(
+                                    from + o + j / (TV / 64) * step + j % (TV / 64) * kAtomBytes);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint8_t* dst = to + o + j / (TV / 64) * step + j % (TV / 64) * C::kPart * 128;
+                                uint4 rest;
+                                *reinterpret_cast<uint4*>(dst) = scaled(d[j], w, rest);
+                                *reinterpret_cast<uint4*>(dst + C::kVw) = rest;
+                                if (j % (TV / 64) == TV / 64 - 1) w *= ratio;
+                            }
+                            o += 4 / (TV / 64) * step;
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int e = 0; e < turns; ++e, o += step, at += p.back ? stride : -stride) {
+                            const float w = exp2f(lg * (p.back ? at + 1 - p.lead : rows - p.lead - at)) * p.scale_w;
+#pragma unroll
+                            for (int t = 0; t < TV / 64; ++t) {
+                                uint4 d = make_uint4(0, 0, 0, 0), rest = d;
+                                if (at < rows)
+                                    d = scaled(*reinterpret_cast<const uint4*>(from + o + t * kAtomBytes), w, rest);
+                                *reinterpret_cast<uint4*>(to + o + t * C::kPart * 128) = d;
+                                *reinterpret_cast<uint4*>(to + C::kVw + o + t * C::kPart * 128) = rest;
+                            }
+                        }
+                    }
+                    fence_proxy_async();
+                    mbar_arrive(ring(C::kVFull, C::kBufs, g));
+                }
+                if (!ok) break;
             }
         }
     }
