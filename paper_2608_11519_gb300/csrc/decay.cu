@@ -189,7 +189,7 @@ flarepp_status attention(const flarepp_decay_shape* shape, bool back, const Call
     }
     if (e == cudaSuccess) {
         w.Da = s.Dk, w.Dv = s.Dv;
-        w.x = ok, w.a = oq, w.v = og, w.y = c.dV, w.y32 = sums, w.turned = 0;
+        w.x = ok, w.a = oq, w.v = og, w.y = c.dV, w.y32 = sums, w.turned = 0, w.again = 1;
         w.state_out = c.dstate;
         e = decay_walk(plan, ws, w, st);
     }

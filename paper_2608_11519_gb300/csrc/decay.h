@@ -43,6 +43,8 @@ struct DecayWalk {
     const float* state;
     float* state_out;
     int turned;
+    // the walk before this one had the same state, turned: what it found in front of cut sequences' parts holds
+    int again;
     int32_t* status;
 };
 

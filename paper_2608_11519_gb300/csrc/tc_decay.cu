@@ -46,7 +46,8 @@ struct Walk {
     void* y;
     int64_t yb, yh, yn;
     int y_f32;
-    const float* slots;   // the state in front of every block's first chunk, [blocks][Da][Dv]
+    const float* slots;   // the state in front of every block's first chunk, [blocks] of Da x Dv
+    int slot_row, slot_col;  // its strides
     float* slots_out;     // with only_state: the state that a block's last piece leaves
     const float* state;   // in front of every sequence, or NULL
     float* state_out;
@@ -472,7 +473,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (uint32_t n = 0; ok && n < total; ++n) {
             if (!p.only_state)
                 ok = wait_use(C::kFullX, C::kX, n) && (n < kSets || wait_chunk(y_free, n - kSets));
-            ok = ok && wait_use(C::kFullA, C::kA, n) && wait_for(b_ready, n & 1, abort_flag, p.waits);
+            ok = ok && wait_use(C::kFullA, C::kA, n) &&
+                 ((p.only_state && n > 0) || wait_for(b_ready, n & 1, abort_flag, p.waits));
             if (!ok) break;
             tc_fence_after();
             const uint32_t a = lower(smem_u32(tile_a(n)), kAtomBytes), q = lower(smem_u32(tile_x(n)), 16);
@@ -505,7 +507,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                         product_ss(tmem + C::kColS, ap + by_row(s), v + (C::kVw >> 4) + by_row(s), states, 1u);
                     }
                     mma_commit(ring(C::kVFree, C::kBufs, g));
-                    if (part == C::kParts - 1) mma_commit(of(u_ready, n));
+                    if (part == C::kParts - 1) {
+                        if (p.only_state) {  // nobody else reads A and V
+                            mma_commit(ring(C::kEmptyA, C::kA, n));
+                            mma_commit(ring(C::kEmptyA, C::kA, n));
+                            mma_commit(ring(C::kEmptyV, C::kV, n));
+                        } else {
+                            mma_commit(of(u_ready, n));
+                        }
+                    }
                 }
                 __syncwarp();
             }
@@ -718,7 +728,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float* from = nullptr;
                 int64_t step = 1;
                 if (!p.only_state && x.c0 > 0) {
-                    from = p.slots + own;
+                    from = p.slots + (int64_t)blockIdx.x * p.Da * p.Dv + row * p.slot_row;
+                    step = p.slot_col;
                 } else if (!p.only_state && p.state) {
                     from = p.state + kept;
                     step = p.col_stride;
@@ -734,7 +745,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tmem_wait_st();
             }
-            for (int k = x.c0; k < x.c1; ++k, ++n) {
+            if (p.only_state) {
+                // (a block's one piece, without any decay between its chunks: the values' weights hold it)
+                tc_fence_before();
+                mbar_arrive(b_ready);
+                ok = wait_for(done, 0, abort_flag, p.waits);
+                tc_fence_after();
+            }
+            for (int k = x.c0; k < x.c1 && !p.only_state; ++k, ++n) {
                 int rows;
                 chunk_at(p, x, k, rows);
                 if (keeps) {
@@ -745,22 +763,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                         uint32_t r[16];
                         tmem_ld16(at + c, r);
                         tmem_wait_ld16(r);
-                        if (!p.only_state) {
-                            // rows of 64 values, 16-byte pieces swapped as the tiles' are
-                            uint8_t* d = smem + C::kOffSt + c / 64 * (TK * 128) + row * 128;
-                            uint32_t hi[8], lo[8];
+                        // rows of 64 values, 16-byte pieces swapped as the tiles' are
+                        uint8_t* d = smem + C::kOffSt + c / 64 * (TK * 128) + row * 128;
+                        uint32_t hi[8], lo[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                hi[j] = split_pair(
-                                    pair(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), lo[j]);
+                        for (int j = 0; j < 8; ++j)
+                            hi[j] = split_pair(pair(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])),
+                                               lo[j]);
 #pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                uint4* e = reinterpret_cast<uint4*>(d + 16 * ((c % 64 / 8 + j) ^ (row & 7)));
-                                *e = make_uint4(hi[4 * j], hi[4 * j + 1], hi[4 * j + 2], hi[4 * j + 3]);
-                                if (C::kStTwo)
-                                    e[C::kSt / 16] =
-                                        make_uint4(lo[4 * j], lo[4 * j + 1], lo[4 * j + 2], lo[4 * j + 3]);
-                            }
+                        for (int j = 0; j < 2; ++j) {
+                            uint4* e = reinterpret_cast<uint4*>(d + 16 * ((c % 64 / 8 + j) ^ (row & 7)));
+                            *e = make_uint4(hi[4 * j], hi[4 * j + 1], hi[4 * j + 2], hi[4 * j + 3]);
+                            if (C::kStTwo)
+                                e[C::kSt / 16] =
+                                    make_uint4(lo[4 * j], lo[4 * j + 1], lo[4 * j + 2], lo[4 * j + 3]);
                         }
 #pragma unroll
                         for (int j = 0; j < 16; j += 2) {
@@ -779,10 +795,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = wait_chunk(u_ready, n);
                 if (!ok) break;
                 tc_fence_after();
-                if (row == 0) {  // the other of the two that read A; without outputs the only one, and of V too
-                    mbar_arrive_n(ring(C::kEmptyA, C::kA, n), p.only_state ? 2 : 1);
-                    if (p.only_state) mbar_arrive(ring(C::kEmptyV, C::kV, n));
-                }
+                if (row == 0) mbar_arrive(ring(C::kEmptyA, C::kA, n));  // the other of the two that read A
             }
             if (!ok) break;
             float* to = nullptr;
@@ -845,6 +858,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     fence_proxy_async();
                 }
                 mbar_arrive(of(clean, n));
+                // without outputs the state is not decayed from chunk to chunk: all of its decay is in the values
+                const int behind = p.only_state ? (x.c1 - 1 - k) * kChunk : 0;
 #pragma unroll 1
                 for (int part = 0; part < C::kParts; ++part, ++g) {
                     ok = g < (uint32_t)C::kBufs || wait_use(C::kVFree, C::kBufs, g - C::kBufs);
@@ -858,7 +873,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint8_t* from = v + part * C::kPart * 128;
                     const int step = p.back ? stride * 128 : -stride * 128;
                     if (rows == kChunk) {
-                        float w = exp2f(lg * (p.back ? at + 1 - p.lead : kChunk - p.lead - at)) * p.scale_w;
+                        float w = exp2f(lg * (behind + (p.back ? at + 1 - p.lead : kChunk - p.lead - at))) * p.scale_w;
 #pragma unroll 1
                         for (int e = 0; e < turns; e += 4 / (TV / 64)) {
                             uint4 d[4];  // as many as fit, read before the first is worked on
@@ -879,7 +894,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     } else {
 #pragma unroll 1
                         for (int e = 0; e < turns; ++e, o += step, at += p.back ? stride : -stride) {
-                            const float w = exp2f(lg * (p.back ? at + 1 - p.lead : rows - p.lead - at)) * p.scale_w;
+                            const float w =
+                                exp2f(lg * (behind + (p.back ? at + 1 - p.lead : rows - p.lead - at))) * p.scale_w;
 #pragma unroll
                             for (int t = 0; t < TV / 64; ++t) {
                                 uint4 d = make_uint4(0, 0, 0, 0), rest = d;
@@ -1221,6 +1237,8 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
     }
     p.row_stride = w.turned ? 1 : w.Dv;
     p.col_stride = w.turned ? w.Da : 1;
+    p.slot_row = w.again ? 1 : p.Dv;
+    p.slot_col = w.again ? p.Da : 1;
     p.waits.status = w.status;
     test_fault_for(kDecayKernel, &p.waits.limit_ns, &p.waits.withheld);
     p.state = w.state;
@@ -1228,6 +1246,11 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
     if (!plan.whole) {
         float* left = (float*)(ws + plan.off_left);
         float* slots = (float*)(ws + plan.off_slots);
+        p.slots = slots;
+        if (w.again) {
+            p.state_out = w.state_out;
+            return launch_for(m, p, plan.blocks, st);
+        }
         Walk first = p;
         first.only_state = 1;
         first.slots_out = left;
@@ -1244,7 +1267,6 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         cfg.numAttrs = 1;
         e = cudaLaunchKernelEx(&cfg, join_kernel, p, (const float*)left, slots, (int)plan.blocks);
         if (e != cudaSuccess) return e;
-        p.slots = slots;
     }
     p.state_out = w.state_out;
     return launch_for(m, p, plan.blocks, st);
