@@ -86,7 +86,7 @@ struct Cfg {
     static constexpr int kFullA = 0, kFullX = kA, kFullV = kFullX + kX, kEmptyA = kFullV + kV,
                          kEmptyX = kEmptyA + kA, kEmptyV = kEmptyX + kX, kOut = kEmptyV + kV,
                          kVFull = kOut + kV, kVFree = kVFull + kBufs, kOther = kVFree + kBufs;
-    static constexpr int kBars = kOther + 14;
+    static constexpr int kBars = kOther + 18;
     static constexpr int kSmem = 1024 + kBody + kBars * 8 + 16;
     static_assert(kSmem <= kMaxSmem, "shared memory");
 };
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // not find that of chunk n + 1 done too, and no barrier's phase n + 2 comes before all have seen n.
     const uint32_t s_ready = bar0 + 8u * C::kOther, p_ready = s_ready + 16, clean = s_ready + 32,
                    u_ready = s_ready + 48, y_ready = s_ready + 64, y_free = s_ready + 80;
-    const uint32_t b_ready = s_ready + 96, done = s_ready + 104;
+    const uint32_t x_ready = s_ready + 96, made = s_ready + 112, b_ready = s_ready + 128, done = s_ready + 136;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -328,6 +328,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(u_ready + s, 1);
             mbar_init(y_ready + s, 1);
             mbar_init(y_free + s, 128);
+            mbar_init(x_ready + s, 1);
+            mbar_init(made + s, 128);
         }
         mbar_init(b_ready, TK);
         mbar_init(done, 2);
@@ -489,6 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 product_ss(to, q + by_channel(s), s0 + (C::kSt >> 4) + by_row(s), outs, 1u);
                         }
                     mma_commit(ring(C::kEmptyX, C::kX, n));
+                    mma_commit(of(x_ready, n));
                 }
                 __syncwarp();
             }
@@ -655,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int since = p.back ? rows - 1 - i : i;
                 const float f = i < rows ? exp2f(lg * (since + p.lead)) * p.scale_r : 0.f;
                 const int64_t to = b * p.yb + h * p.yh + (int64_t)(token + i) * p.yn;
-                ok = wait_chunk(u_ready, n) && wait_chunk(y_ready, n);
+                ok = wait_chunk(made, n) && wait_chunk(x_ready, n) && wait_chunk(y_ready, n);
                 if (!ok) break;
                 tc_fence_after();
                 // V has been read, by the warps that decay it and by its product: the outputs go over it, from
@@ -839,7 +842,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 int rows;
                 chunk_at(p, x, k, rows);
                 ok = wait_use(C::kFullA, C::kA, n) && wait_use(C::kFullV, C::kV, n) &&
-                     (n < 2 || p.only_state || wait_chunk(y_ready, n - 2));  // clean's last phase is seen
+                     (n < 2 || p.only_state || wait_chunk(y_free, n - 2));  // clean's and made's last phases are seen
                 if (!ok) break;
                 uint8_t* v = tile_v(n);
                 if (rows < kChunk) {
@@ -910,6 +913,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive(ring(C::kVFull, C::kBufs, g));
                 }
                 if (!ok) break;
+                mbar_arrive(of(made, n));
             }
         }
     }
