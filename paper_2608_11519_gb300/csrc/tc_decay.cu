@@ -57,9 +57,12 @@ struct Walk {
 
 template <int TK, int TV>
 struct Cfg {
-    // Values of up to 64 channels leave room for two sets of scores and of X S.
+    // TMEM columns: scores (W o scores as bf16 over a half of them), (W o scores) V, X S, the state. Values of
+    // up to 64 channels leave room for two sets of scores and of X S. (With what a chunk adds in columns of
+    // its own, so that the next one's is multiplied before this one's is added, and (W o scores) V in the
+    // scores' other half to make room, a walk took longer: 712 us instead of 677 for the long backward.)
     static constexpr int kSets = TV == 64 ? 2 : 1;
-    static constexpr uint32_t kColY = kSets * 128;  // from 0 on: scores, and W o scores as bf16 over them
+    static constexpr uint32_t kColY = kSets * 128;
     static constexpr uint32_t kColX = kColY + TV;
     static constexpr uint32_t kColS = kColX + kSets * TV;
     static constexpr uint32_t kTmem = 512;
@@ -473,15 +476,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         uint32_t g = 0;  // parts
         for (uint32_t n = 0; ok && n < total; ++n) {
-            if (!p.only_state)
-                ok = wait_use(C::kFullX, C::kX, n) && (n < kSets || wait_chunk(y_free, n - kSets));
-            ok = ok && wait_use(C::kFullA, C::kA, n) &&
-                 ((p.only_state && n > 0) || wait_for(b_ready, n & 1, abort_flag, p.waits));
-            if (!ok) break;
-            tc_fence_after();
             const uint32_t a = lower(smem_u32(tile_a(n)), kAtomBytes), q = lower(smem_u32(tile_x(n)), 16);
             const uint32_t to = tmem + C::kColX + n % kSets * TV;
-            if (!p.only_state) {
+            auto states_of = [&]() {
+                // (where TK is 64, A^T's rows from 64 on are whatever lies behind the tile: they are not used)
+#pragma unroll 1
+                for (int part = 0; part < C::kParts; ++part, ++g) {
+                    if (!wait_use(C::kVFull, C::kBufs, g)) return false;
+                    tc_fence_after();
+                    const uint32_t v =
+                        lower(smem_u32(smem + C::kOffVw + g % C::kBufs * 2 * C::kVw), C::kPart * 128);
+                    const uint32_t ap = a + by_row(part * (C::kPart / 16));
+                    if (elect_one()) {
+#pragma unroll
+                        for (int s = 0; s < C::kPart / 16; ++s) {
+                            product_ss(tmem + C::kColS, ap + by_row(s), v + by_row(s), states, 1u);
+                            product_ss(tmem + C::kColS, ap + by_row(s), v + (C::kVw >> 4) + by_row(s), states, 1u);
+                        }
+                        mma_commit(ring(C::kVFree, C::kBufs, g));
+                        if (part == C::kParts - 1) {
+                            if (p.only_state) {  // nobody else reads A and V
+                                mma_commit(ring(C::kEmptyA, C::kA, n));
+                                mma_commit(ring(C::kEmptyA, C::kA, n));
+                                mma_commit(ring(C::kEmptyV, C::kV, n));
+                            } else {
+                                mma_commit(of(u_ready, n));
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+                return true;
+            };
+            ok = wait_use(C::kFullA, C::kA, n);
+            if (ok && p.only_state) {
+                ok = (n > 0 || wait_for(b_ready, 0, abort_flag, p.waits)) && states_of();
+            } else if (ok) {
+                ok = wait_use(C::kFullX, C::kX, n) && (n < kSets || wait_chunk(y_free, n - kSets)) &&
+                     wait_for(b_ready, n & 1, abort_flag, p.waits);
+                if (!ok) break;
+                tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
                     for (int s = 0; s < TK / 16; ++s)
@@ -494,33 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mma_commit(of(x_ready, n));
                 }
                 __syncwarp();
-            }
-            // (where TK is 64, A^T's rows from 64 on are whatever lies behind the tile: they are not used)
-#pragma unroll 1
-            for (int part = 0; part < C::kParts; ++part, ++g) {
-                ok = wait_use(C::kVFull, C::kBufs, g);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t v = lower(smem_u32(smem + C::kOffVw + g % C::kBufs * 2 * C::kVw), C::kPart * 128);
-                const uint32_t ap = a + by_row(part * (C::kPart / 16));
-                if (elect_one()) {
-#pragma unroll
-                    for (int s = 0; s < C::kPart / 16; ++s) {
-                        product_ss(tmem + C::kColS, ap + by_row(s), v + by_row(s), states, 1u);
-                        product_ss(tmem + C::kColS, ap + by_row(s), v + (C::kVw >> 4) + by_row(s), states, 1u);
-                    }
-                    mma_commit(ring(C::kVFree, C::kBufs, g));
-                    if (part == C::kParts - 1) {
-                        if (p.only_state) {  // nobody else reads A and V
-                            mma_commit(ring(C::kEmptyA, C::kA, n));
-                            mma_commit(ring(C::kEmptyA, C::kA, n));
-                            mma_commit(ring(C::kEmptyV, C::kV, n));
-                        } else {
-                            mma_commit(of(u_ready, n));
-                        }
-                    }
-                }
-                __syncwarp();
+                ok = states_of();
             }
         }
         if (elect_one()) mma_commit(done);
