@@ -53,11 +53,11 @@ struct DecayPlan {
     int64_t sequences, chunks;  // chunks of a sequence (the longest possible one)
     bool whole;                 // whether no sequence is cut
     int64_t blocks, share;      // share: heads or chunks of a block, 0 if the lengths tell
-    size_t off_first, off_cuts, off_left, off_slots, off_sums, total;
+    size_t off_first, off_cuts, off_starts, off_left, off_slots, off_sums, total;
 };
 DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward);
 
-// Packed sequences: the cuts (checked) and the chunks before each into the workspace.
+// Packed sequences: the cuts (checked), the chunks before each and the blocks' first places into the workspace.
 cudaError_t decay_cut(const flarepp_decay_shape& s, const DecayPlan& p, const int32_t* offsets, char* ws,
                       int32_t* status, cudaStream_t st);
 // The rows that no sequence holds become 0.

@@ -40,6 +40,7 @@ struct Walk {
     int share;            // 0: from the list's length
     const int* cuts;      // packed sequences' first tokens, else NULL
     const int* first;     // chunks of the sequences before each, of packed ones
+    const int2* starts;   // and the sequence and head of every block's first place, where they are cut
     float scale_p, scale_w, scale_r;  // what scores, decayed values and X S are multiplied by
     int lead;                         // r_i = g^(i + lead), w_j = g^(n - lead - j)
     const float* log_decay;
@@ -119,20 +120,20 @@ __device__ __forceinline__ int places_of(const Walk& p, int sequence) {
     if (p.whole) return 1;
     return p.cuts ? p.first[sequence + 1] - p.first[sequence] : p.chunks;
 }
-__device__ __noinline__ void begin_feed(const Walk& p, int block, Feed& f) {
+__device__ __noinline__ void begin_feed(const Walk& p, int block, int blocks, Feed& f) {
     const int all = places_before(p, p.sequences);
-    const int share = p.share ? p.share : (all + (int)gridDim.x - 1) / (int)gridDim.x;
+    const int share = p.share ? p.share : (all + blocks - 1) / blocks;
     f.at = min(block * share, all);  // (at most 2^31: the host has seen to it)
     f.end = min(f.at + share, all);
-    int low = 0, high = p.sequences;  // the last sequence that begins at this place or before
-    if (f.at < f.end) {
-        while (high - low > 1) {
-            const int mid = (low + high) / 2;
-            if (places_before(p, mid) <= f.at) low = mid;
-            else high = mid;
-        }
-        f.sequence = low;
-        f.h = (f.at - places_before(p, low)) / places_of(p, low);
+    if (f.at >= f.end) return;
+    if (p.starts) {  // (a search of the packed sequences by every block would be one load after another)
+        const int2 s = p.starts[block];
+        f.sequence = s.x;
+        f.h = s.y;
+    } else {
+        const int head = f.at / (p.whole ? 1 : p.chunks);
+        f.sequence = head / p.Hq;
+        f.h = head - f.sequence * p.Hq;
     }
 }
 // The next piece; false after the last.
@@ -292,7 +293,7 @@ __device__ __noinline__ int count_chunks(const Walk& p) {
     Feed f;
     Piece x;
     int n = 0;
-    begin_feed(p, blockIdx.x, f);
+    begin_feed(p, blockIdx.x, gridDim.x, f);
     while (next_walked(p, f, x)) n += x.c1 - x.c0;
     return n;
 }
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------ loads: A, X, V
         uint32_t it = 0, n = 0, used_x = 0;  // tiles and chunks; those of X
         bool ok = true;
-        begin_feed(p, blockIdx.x, feed);
+        begin_feed(p, blockIdx.x, gridDim.x, feed);
         while (ok && next_walked(p, feed, here)) {
             const Piece x = here;
             const int b = p.cuts ? 0 : x.sequence, h = x.h;
@@ -541,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // slots' phases count their staged uses alone)
         uint32_t n = 0, phases = 0;
         bool ok = true;
-        begin_feed(p, blockIdx.x, feed);
+        begin_feed(p, blockIdx.x, gridDim.x, feed);
         while (ok && !p.only_state && next_piece(p, feed, here)) {
             const Piece x = here;
             const int b = p.cuts ? 0 : x.sequence, h = x.h;
@@ -578,7 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int low = p.back ? edge : 0, high = p.back ? 64 : min(max(32 * q + 32 - 64 * half, 0), 64);
         uint32_t n = 0;
         bool ok = true;
-        begin_feed(p, blockIdx.x, feed);
+        begin_feed(p, blockIdx.x, gridDim.x, feed);
         while (ok && !p.only_state && next_piece(p, feed, here)) {
             const Piece x = here;
             const float lg = head_decay(p, x.h, false);
@@ -655,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t at = tmem + ((uint32_t)(32 * q) << 16);
         uint32_t n = 0;
         bool ok = true;
-        begin_feed(p, blockIdx.x, feed);
+        begin_feed(p, blockIdx.x, gridDim.x, feed);
         while (ok && !p.only_state && next_piece(p, feed, here)) {
             const Piece x = here;
             const int b = p.cuts ? 0 : x.sequence, h = x.h;
@@ -729,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + C::kColS;
         uint32_t n = 0;
         bool ok = true;
-        begin_feed(p, blockIdx.x, feed);
+        begin_feed(p, blockIdx.x, gridDim.x, feed);
         while (32 * q < TK && ok && next_walked(p, feed, here)) {
             const Piece x = here;
             const int64_t own = ((int64_t)blockIdx.x * p.Da + row) * p.Dv;
@@ -839,7 +840,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int r0 = maker >> shift;
         uint32_t n = 0, g = 0;
         bool ok = true;
-        begin_feed(p, blockIdx.x, feed);
+        begin_feed(p, blockIdx.x, gridDim.x, feed);
         while (ok && next_walked(p, feed, here)) {
             const Piece x = here;
             const float lg = head_decay(p, x.h, false);
@@ -934,10 +935,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ------------------------------------------------------------------ packed sequences
 // One block: the cuts, brought into 0 to N and never falling (each at least the largest before it), and the
-// chunks before every sequence (one at least for each, so that an empty one has a place in the list).
+// chunks before every sequence (one at least for each, so that an empty one has a place in the list). And
+// where every block's equal part of that list begins.
 constexpr int kCutThreads = 1024;
 __global__ void __launch_bounds__(kCutThreads)
-    cut_kernel(const int32_t* offsets, int sequences, int N, int* first, int* cuts, int* status) {
+    cut_kernel(const int32_t* offsets, int sequences, int N, int* first, int* cuts, int Hq, int blocks,
+               int2* starts, int* status) {
     __shared__ int sm[2][kCutThreads / 32];
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -984,6 +987,19 @@ __global__ void __launch_bounds__(kCutThreads)
         __syncthreads();
     }
     if (threadIdx.x == 0) first[sequences] = total;
+    if (!starts) return;
+    __syncthreads();
+    const int all = total * Hq, share = (all + blocks - 1) / blocks;  // (the host has seen to 31 bits)
+    for (int b = threadIdx.x; b < blocks && b * share < all; b += kCutThreads) {
+        const int at = b * share;
+        int low = 0, high = sequences;  // the last sequence that begins at this place or before
+        while (high - low > 1) {
+            const int mid = (low + high) / 2;
+            if (first[mid] * Hq <= at) low = mid;
+            else high = mid;
+        }
+        starts[b] = make_int2(low, (at - first[low] * Hq) / (first[low + 1] - first[low]));
+    }
 }
 
 __global__ void __launch_bounds__(256)
@@ -1012,21 +1028,14 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk 
     tc::pdl_wait();
     constexpr int kAhead = 8;
     const int e = blockIdx.x * 256 + threadIdx.x, size = p.Da * p.Dv, y = blockIdx.y;
-    // the last place of walk block y, and the sequence's head there
-    Walk q = p;
-    const int all = places_before(q, q.sequences);
-    const int share = q.share ? q.share : (all + blocks - 1) / blocks;
-    const int end = min((y + 1) * share, all);
-    if (end >= all || y * share >= end) return;
-    int low = 0, high = q.sequences;
-    while (high - low > 1) {
-        const int mid = (low + high) / 2;
-        if (places_before(q, mid) <= end - 1) low = mid;
-        else high = mid;
-    }
-    const int each = places_of(q, low), before = places_before(q, low), h = (end - 1 - before) / each;
-    const int base = before + h * each;
-    if (base < y * share || base + each <= end || e >= size) return;  // begun before, or all here
+    // what walk block y + 1 begins with, where its first place is in a sequence's head
+    const Walk& q = p;
+    Feed f;
+    begin_feed(q, y + 1, blocks, f);
+    if (f.at >= f.end) return;
+    const int end = f.at, share = end / (y + 1);
+    const int low = f.sequence, h = f.h, each = places_of(q, low), base = places_before(q, low) + h * each;
+    if (base < y * share || base >= end || e >= size) return;  // begun before block y, or behind it
     bool bad = false;
     const float lg = decay_log2(q.log_decay[h], &bad);
     int start;
@@ -1181,6 +1190,7 @@ DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
     if (s.sequences) {
         p.off_first = place((p.sequences + 1) * 4);
         p.off_cuts = place((p.sequences + 1) * 4);
+        if (!p.whole) p.off_starts = place(p.blocks * sizeof(int2));
     }
     if (!p.whole) {
         p.off_left = place((size_t)p.blocks * s.Dk * s.Dv * 4);
@@ -1195,7 +1205,8 @@ DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
 cudaError_t decay_cut(const flarepp_decay_shape& s, const DecayPlan& p, const int32_t* offsets, char* ws,
                       int32_t* status, cudaStream_t st) {
     return launch(cut_kernel, 1, kCutThreads, 0, st, offsets, (int)s.sequences, (int)s.N,
-                  (int*)(ws + p.off_first), (int*)(ws + p.off_cuts), (int*)status);
+                  (int*)(ws + p.off_first), (int*)(ws + p.off_cuts), (int)s.Hq, (int)p.blocks,
+                  p.whole ? (int2*)nullptr : (int2*)(ws + p.off_starts), (int*)status);
 }
 
 cudaError_t decay_blank(const flarepp_decay_shape& s, const DecayPlan& p, char* ws, const flarepp_heads& y,
@@ -1231,6 +1242,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         p.cuts = (const int*)(ws + plan.off_cuts);
         p.first = (const int*)(ws + plan.off_first);
     }
+    if (s.sequences && !plan.whole) p.starts = (const int2*)(ws + plan.off_starts);
     p.whole = plan.whole;
     p.sequences = (int)plan.sequences;
     p.chunks = (int)plan.chunks;
