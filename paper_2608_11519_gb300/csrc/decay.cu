@@ -25,7 +25,7 @@ flarepp_status check_shape(const flarepp_decay_shape* s) {
     if (s->N > INT32_MAX - 256 || s->Hq > 65535 || n > INT32_MAX / 64) return FLAREPP_ERR_UNSUPPORTED;
     if (n * (s->sequences ? 1 : s->N / kDecayChunk + 1) > (INT32_MAX - (1 << 20)) / (s->Hq ? s->Hq : 1))
         return FLAREPP_ERR_UNSUPPORTED;
-    if (s->sequences && n + s->N / kDecayChunk > (INT32_MAX - (1 << 20)) / (s->Hq ? s->Hq : 1))
+    if (s->sequences && n * (1 + kDecayFront) + s->N / kDecayChunk > (INT32_MAX - (1 << 20)) / (s->Hq ? s->Hq : 1))
         return FLAREPP_ERR_UNSUPPORTED;
     return FLAREPP_OK;
 }

@@ -4,16 +4,20 @@
 // with W_ij = g^(i-j) for j <= i (0 above), r_i = g^(i+1), w_j = g^(n-1-j): four products of 128 rows. The
 // same walk from the sequence's end makes the gradients of keys and values (DecayWalk says how).
 //
-// Bound by bytes at every width: a chunk reads three tiles and writes one, 64 KB at 64 channels, which the
-// card takes 1.45 us for on each of its 152 SMs, and its four products some 0.35 us. So one block walks a
-// sequence of one head, with the state staying in TMEM, and nothing is read twice; where heads and sequences
-// do not fill the SMs evenly, sequences are cut, and a first walk (only A and V, only S, only in front
-// of the cuts) and a join over the blocks find the states there.
+// The floor is bytes at every width: a chunk reads three tiles and writes one, 64 KB at 64 channels, 1.45 us of
+// an SM's share of HBM. So one block walks a sequence of one head, with the state staying in TMEM, and
+// nothing is read twice; where heads and sequences do not fill the SMs evenly, sequences are cut, and a
+// first walk (only A and V, only S, only in front of the cuts) and a join over the blocks find the states
+// there. What bounds it is shared memory and the state's way round: a chunk's products, whose operands are read from
+// it, its tiles, decayed values and state move 580 KB through it at 128 channels, 4,500 of the 6,100
+// cycles that a chunk takes (keys, values of 64, 64: 3,800; 128, 64: 5,000; 64, 128: 6,000), and a chunk's state is
+// scaled, multiplied and added to before the next one's. 8 x 32 heads of 4,096 tokens and 128 channels take
+// 196 us (3.4 TB/s of what has to move), the gradients of 8 heads of 131,072 tokens 678.
 //
 // W o (X A^T) is rounded to bf16 as an operand, w o V and S are two bf16 each (Cfg says why and where not); sums,
 // states and what r multiplies are float32.
 //
-// Roles (24 warps, a block an SM): warp 0 loads tiles (A, X, V of each chunk, a ring), warps 1 and 2 issue the
+// Roles (24 warps, a block an SM): warp 0 loads tiles (A, X, V of each chunk, a ring of each), warps 1 and 2 issue the
 // products, warps 4 to 11 make W o (X A^T), warps 12 to 15 write Y, warps 16 to 19 keep the state, warps 20 to
 // 23 make w o V. A chunk passes through them like through a pipeline; the longest way round is
 // the state's (scale it, add to it). Every wait is bounded.
@@ -39,7 +43,8 @@ struct Walk {
     int sequences, chunks;  // chunks of a sequence, if they are all alike
     int share;            // 0: from the list's length
     const int* cuts;      // packed sequences' first tokens, else NULL
-    const int* first;     // chunks of the sequences before each, of packed ones
+    const int* first;     // places of the sequences before each, of packed ones
+    int front;            // places that a sequence's head has in front of its chunks
     const int2* starts;   // and the sequence and head of every block's first place, where they are cut
     float scale_p, scale_w, scale_r;  // what scores, decayed values and X S are multiplied by
     int lead;                         // r_i = g^(i + lead), w_j = g^(n - lead - j)
@@ -145,8 +150,8 @@ __device__ __noinline__ bool next_piece(const Walk& p, Feed& f, Piece& x) {
     x.h = f.h;
     x.rows = tokens_of(p, f.sequence, x.start);
     x.total = (x.rows + kChunk - 1) / kChunk;
-    x.c0 = p.whole ? 0 : min(f.at - base, x.total);
-    x.c1 = p.whole ? x.total : min(f.end - base, x.total);
+    x.c0 = p.whole ? 0 : min(max(f.at - base - p.front, 0), x.total);
+    x.c1 = p.whole ? x.total : min(max(f.end - base - p.front, 0), x.total);
     f.at = base + each;
     if (++f.h == p.Hq) {
         f.h = 0;
@@ -673,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // V has been read, by the warps that decay it and by its product: the outputs go over it, from
                 // where whole lines are stored. (Stores of a thread's own row, 16 bytes of 32 lines an
                 // instruction, held up the state's through the pipe that they share: 241 us instead of 229
-                // for the prefill.)
+                // for the prefill, when this was chosen.)
                 const bool staging = staged(p, rows);
                 uint8_t* stage = tile_v(n) + i * 128;
                 if (!staging && threadIdx.x == 384) mbar_arrive(ring(C::kEmptyV, C::kV, n));
@@ -935,8 +940,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ------------------------------------------------------------------ packed sequences
 // One block: the cuts, brought into 0 to N and never falling (each at least the largest before it), and the
-// chunks before every sequence (one at least for each, so that an empty one has a place in the list). And
-// where every block's equal part of that list begins.
+// places before every sequence in the list of chunks, where each has some more in front (kDecayFront). And where
+// every block's equal part of that list begins.
 constexpr int kCutThreads = 1024;
 __global__ void __launch_bounds__(kCutThreads)
     cut_kernel(const int32_t* offsets, int sequences, int N, int* first, int* cuts, int Hq, int blocks,
@@ -970,7 +975,7 @@ __global__ void __launch_bounds__(kCutThreads)
     if (bad) record_status(status, FLAREPP_ERR_INVALID_ARGUMENT);
     for (int s0 = 0; s0 < sequences; s0 += kCutThreads) {
         const int s = s0 + threadIdx.x;
-        const int n = s < sequences ? max(1, (cuts[s + 1] - cuts[s] + kChunk - 1) / kChunk) : 0;
+        const int n = s < sequences ? kDecayFront + (cuts[s + 1] - cuts[s] + kChunk - 1) / kChunk : 0;
         int v = n;
         for (int d = 1; d < 32; d <<= 1) {
             const int o = __shfl_up_sync(0xffffffffu, v, d);
@@ -1040,12 +1045,13 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk 
     const float lg = decay_log2(q.log_decay[h], &bad);
     int start;
     const int tokens = tokens_of(q, low, start);
-    // tokens of the places base + c0 to base + c1, as walked
+    // tokens of chunks c0 to c1, as walked, and the chunks up to a place
     const int total = (tokens + kChunk - 1) / kChunk, ragged = total * kChunk - tokens;
     auto rows_of = [&](int c0, int c1) {
-        const bool holds = q.back ? c0 == 0 : c1 == total;  // the chunk that ends early
+        const bool holds = c0 < c1 && (q.back ? c0 == 0 : c1 == total);  // the chunk that ends early
         return (c1 - c0) * kChunk - (holds ? ragged : 0);
     };
+    auto chunks_to = [&](int place) { return max(place - base - q.front, 0); };
     const int r = e / q.Dv, c = e - r * q.Dv;
     float run = q.state ? q.state[((int64_t)low * q.Hq + h) * size + r * q.row_stride + c * q.col_stride] : 0.f;
     const int last = (base + each - 1) / share;  // the walk block that ends the sequence
@@ -1058,7 +1064,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk 
         for (int j = 0; j < kAhead; ++j) {
             const int k = k0 + j;
             if (k >= last) break;
-            run = fmaf(exp2f(lg * rows_of(max(k * share - base, 0), (k + 1) * share - base)), run, v[j]);
+            run = fmaf(exp2f(lg * rows_of(chunks_to(k * share), chunks_to((k + 1) * share))), run, v[j]);
             slots[(int64_t)(k + 1) * size + e] = run;
         }
     }
@@ -1242,7 +1248,10 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         p.cuts = (const int*)(ws + plan.off_cuts);
         p.first = (const int*)(ws + plan.off_first);
     }
-    if (s.sequences && !plan.whole) p.starts = (const int2*)(ws + plan.off_starts);
+    if (s.sequences && !plan.whole) {
+        p.starts = (const int2*)(ws + plan.off_starts);
+        p.front = kDecayFront;
+    }
     p.whole = plan.whole;
     p.sequences = (int)plan.sequences;
     p.chunks = (int)plan.chunks;
