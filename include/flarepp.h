@@ -587,8 +587,11 @@ typedef struct {
  *   state, state_out: NULL or float32 [sequences or B, Hq, Dk, Dv], dense: S_0 and the state behind the
  *     last token, which continues the sequence in another call or in flarepp_decay_attention_step (an empty
  *     sequence's is its S_0). They may be the same buffer.
- * The products' operands are bf16 (scores with their decay, states and decayed values are rounded to it),
- * sums and states are float32. The sums run in a fixed order: two calls on the same inputs give the same bits.
+ * The products' operands are bf16 and their sums float32, as are states. Scores with their decay are rounded to
+ * bf16; decayed values are two bf16 each, which keep 17 bits (a state is off by some 3e-6 of the sum of
+ * its terms' magnitudes, tensor cores' sums included), and so is the state that outputs are made from,
+ * but where Dk and Dv are both above 64: there it is one. The sums run in a fixed order: two calls on
+ * the same inputs give the same bits.
  *   workspace: at least flarepp_decay_attention_workspace_bytes(shape) bytes, 256-byte aligned.
  *   Y, state_out and the workspace must not overlap each other or an input (but state_out the state).
  */

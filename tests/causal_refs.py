@@ -35,9 +35,11 @@ def walk(x, a, v, g, S, back=False):
 def decay_refs(Q, K, V, log_decay, scale, state, dY=None, dstate_out=None):
     """{name: (value, bound)} of a forward, and with dY of its gradients, for one batch of sequences. The
     bounds: an operand that is rounded to bf16 is off by U of itself, so by U of the sums of magnitudes
-    of the terms that it is in. Scores with their decay are rounded once, decayed values and the state
-    made of them each once: at most two roundings in a term; then the output's own. Sums of float32 terms
-    in chunks of 128 and powers of g from exponentials: 1e-5 of the sum of magnitudes."""
+    of the terms that it is in. A term within a chunk has its score rounded once; one through the state has its
+    value as two bf16, of which the second is off by U of what the first leaves, U of it, and the state
+    the same again or (Dk and Dv above 64) rounded once: at most U + U^2 for either, and 2 U^2 else; then
+    the output's own. Sums of float32 terms in chunks of 128 and powers of g from exponentials: 1e-5 of
+    the sum of magnitudes."""
     Q, K, V = Q.double(), K.double(), V.double()
     group = Q.shape[1] // K.shape[1]
     g = log_decay.double().exp()
@@ -50,7 +52,7 @@ def decay_refs(Q, K, V, log_decay, scale, state, dY=None, dstate_out=None):
     def both(x, a, v, S, back=False, c=1.0):
         y, last = walk(x * c, a, v, g, S, back)
         ya, la = walk(x.abs() * abs(c), a.abs(), v.abs(), g, S.abs(), back)
-        return y, 2 * U * ya + 1e-5 * ya, last, U * la + 1e-5 * la
+        return y, (U + U * U) * ya + 1e-5 * ya, last, U * U * la + 1e-5 * la
 
     def put(name, y, e):
         out[name] = (y, e + U * y.abs() + 1e-30)
