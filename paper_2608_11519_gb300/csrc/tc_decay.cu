@@ -34,7 +34,7 @@ constexpr size_t kWsAlign = 256;
 
 struct Walk {
     int Hq, N, Da, Dv;
-    int back, only_state;
+    int back;
     int gx, ga, gv;       // query heads that share a head of x, a, v
     int mx, ma, mv;       // whether a batch element has its own
     // The list of all sequences' heads' chunks in the order in which they are walked (or of the sequences'
@@ -54,14 +54,16 @@ struct Walk {
     int y_f32;
     const float* slots;   // the state in front of every block's first chunk, [blocks] of Da x Dv
     int slot_row, slot_col;  // its strides
-    float* slots_out;     // with only_state: the state that a block's last piece leaves
+    float* slots_out;     // of the first walk: the state that a block's last piece leaves
     const float* state;   // in front of every sequence, or NULL
     float* state_out;
     int64_t row_stride, col_stride;  // of a state between calls
     Waits waits;
 };
 
-template <int TK, int TV>
+// STATES: the first walk over what lies in front of the cuts, which only finds states. (A choice at run time
+// in one kernel left it with the shallow rings of the other and both with more code.)
+template <int TK, int TV, bool STATES>
 struct Cfg {
     // TMEM columns: scores (W o scores as bf16 over a half of them), (W o scores) V, X S, the state. Values of
     // up to 64 channels leave room for two sets of scores and of X S. (With what a chunk adds in columns of
@@ -76,7 +78,8 @@ struct Cfg {
     // Shared memory: rings of tiles, as many as there is room for; of A, X and V each, so that a ring's slot
     // only ever holds one kind.
     static constexpr bool kWide = TK == 128 && TV == 128;
-    static constexpr int kA = TK == 64 && TV == 64 ? 3 : 2, kX = kWide ? 1 : kA, kV = kA;
+    static constexpr int kA = STATES ? (TK == 64 && TV == 64 ? 5 : TV == 64 ? 4 : 3) : TK == 64 && TV == 64 ? 3 : 2;
+    static constexpr int kX = kWide || STATES ? 1 : kA, kV = kA;  // (of X no use is made then)
     static constexpr int kTileK = TK * kChunk * 2, kTileV = TV * kChunk * 2;
     // Decayed values and the state go into their products as two bf16 each, the second what the first's
     // rounding left: so a state is as good as its 32 bits but for some 2^-17, and X S as good as the state
@@ -87,8 +90,8 @@ struct Cfg {
     static constexpr int kBufs = TV == 128 ? (kWide ? 2 : 4) : 2;
     static constexpr int kPart = kChunk / kParts;      // tokens
     static constexpr int kVw = kPart * TV * 2;         // bytes of one of the two
-    static constexpr int kSt = TK * TV * 2;
-    static constexpr int kOffX = kA * kTileK, kOffV = kOffX + kX * kTileK, kOffVw = kOffV + kV * kTileV;
+    static constexpr int kSt = STATES ? 0 : TK * TV * 2;
+    static constexpr int kOffX = kA * kTileK, kOffV = kOffX + (STATES ? 0 : kX) * kTileK, kOffVw = kOffV + kV * kTileV;
     static constexpr int kOffSt = kOffVw + kBufs * 2 * kVw;
     static constexpr int kBody = kOffSt + (kStTwo ? 2 : 1) * kSt;
     // barriers
@@ -161,9 +164,10 @@ __device__ __noinline__ bool next_piece(const Walk& p, Feed& f, Piece& x) {
 }
 // The pieces of a block's walk: all of its part of the list, or, for the states alone, the last
 // one if its sequence goes on in the next block.
+template <bool STATES>
 __device__ __forceinline__ bool next_walked(const Walk& p, Feed& f, Piece& x) {
     while (next_piece(p, f, x))
-        if (!p.only_state || x.c1 < x.total) return true;
+        if (!STATES || x.c1 < x.total) return true;
     return false;
 }
 // The first token of chunk c, and its tokens.
@@ -294,12 +298,13 @@ __device__ __forceinline__ void keep_keys(uint32_t* w, uint32_t bits) {
 }
 
 // How many chunks a block walks.
+template <bool STATES>
 __device__ __noinline__ int count_chunks(const Walk& p) {
     Feed f;
     Piece x;
     int n = 0;
     begin_feed(p, blockIdx.x, gridDim.x, f);
-    while (next_walked(p, f, x)) n += x.c1 - x.c0;
+    while (next_walked<STATES>(p, f, x)) n += x.c1 - x.c0;
     return n;
 }
 
@@ -307,12 +312,12 @@ __device__ __forceinline__ uint32_t bf16_bits(uint32_t a, uint32_t b) {
     return bf16_pair(__uint_as_float(a), __uint_as_float(b));
 }
 
-template <int TK, int TV>
+template <int TK, int TV, bool STATES>
 __global__ void __launch_bounds__(kThreads, 1)
     walk_kernel(const __grid_constant__ CUtensorMap tX, const __grid_constant__ CUtensorMap tA,
                 const __grid_constant__ CUtensorMap tV, const __grid_constant__ CUtensorMap tY,
                 const __grid_constant__ Walk p) {
-    using C = Cfg<TK, TV>;
+    using C = Cfg<TK, TV, STATES>;
     constexpr uint32_t kSets = C::kSets;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -382,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t it = 0, n = 0, used_x = 0;  // tiles and chunks; those of X
         bool ok = true;
         begin_feed(p, blockIdx.x, gridDim.x, feed);
-        while (ok && next_walked(p, feed, here)) {
+        while (ok && next_walked<STATES>(p, feed, here)) {
             const Piece x = here;
             const int b = p.cuts ? 0 : x.sequence, h = x.h;
             for (int c = x.c0; c < x.c1 && ok; ++c, ++n) {
@@ -401,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = load(C::kFullA, C::kEmptyA, C::kA, C::kTileK, [&](uint32_t bar) {
                     load_rows<TK>(smem_u32(tile_a(n)), &tA, token, p.ga ? h / p.ga : 0, b * p.ma, bar);
                 });
-                if (ok && !p.only_state) {
+                if (ok && !STATES) {
                     ok = load(C::kFullX, C::kEmptyX, C::kX, C::kTileK, [&](uint32_t bar) {
                         load_rows<TK>(smem_u32(tile_x(n)), &tX, token, p.gx ? h / p.gx : 0, b * p.mx, bar);
                     });
@@ -415,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!ok) {  // wait (bounded) until every copy issued has landed
             const uint64_t t0 = globaltimer_ns();
-            const uint32_t per = p.only_state ? 2 : 3;
+            const uint32_t per = STATES ? 2 : 3;
             const uint32_t uses[3] = {(it + per - 1) / per, used_x, it / per};
             const int first[3] = {C::kFullA, C::kFullX, C::kFullV}, size[3] = {C::kA, C::kX, C::kV};
             for (int k = 0; k < 3; ++k)
@@ -430,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // for each kept this warp from issuing for hundreds of cycles.
         const uint32_t scores = idesc_bf16_f32(128, 128, false, false);
         const uint32_t outs = idesc_bf16_f32(128, 16, false, true) + ((uint32_t)(width / 8 - 2) << 17);
-        const int total = p.only_state ? 0 : count_chunks(p);
+        const int total = STATES ? 0 : count_chunks<STATES>(p);
         bool ok = true;
         // with two sets the scores of a chunk go ahead of the last chunk's outputs
         for (int m = 0; ok && m < total + (int)kSets - 1; ++m) {
@@ -478,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t states = idesc_bf16_f32(128, 16, true, true) + ((uint32_t)(width / 8 - 2) << 17);
         const uint32_t outs = idesc_bf16_f32(128, 16, false, true) + ((uint32_t)(width / 8 - 2) << 17);
         const uint32_t s0 = lower(smem_u32(smem + C::kOffSt), TK * 128);
-        const uint32_t total = count_chunks(p);
+        const uint32_t total = count_chunks<STATES>(p);
         bool ok = true;
         uint32_t g = 0;  // parts
         for (uint32_t n = 0; ok && n < total; ++n) {
@@ -501,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         mma_commit(ring(C::kVFree, C::kBufs, g));
                         if (part == C::kParts - 1) {
-                            if (p.only_state) {  // nobody else reads A and V
+                            if (STATES) {  // nobody else reads A and V
                                 mma_commit(ring(C::kEmptyA, C::kA, n));
                                 mma_commit(ring(C::kEmptyA, C::kA, n));
                                 mma_commit(ring(C::kEmptyV, C::kV, n));
@@ -515,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 return true;
             };
             ok = wait_use(C::kFullA, C::kA, n);
-            if (ok && p.only_state) {
+            if (ok && STATES) {
                 ok = (n > 0 || wait_for(b_ready, 0, abort_flag, p.waits)) && states_of();
             } else if (ok) {
                 ok = wait_use(C::kFullX, C::kX, n) && (n < kSets || wait_chunk(y_free, n - kSets)) &&
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t n = 0, phases = 0;
         bool ok = true;
         begin_feed(p, blockIdx.x, gridDim.x, feed);
-        while (ok && !p.only_state && next_piece(p, feed, here)) {
+        while (ok && !STATES && next_piece(p, feed, here)) {
             const Piece x = here;
             const int b = p.cuts ? 0 : x.sequence, h = x.h;
             for (int c = x.c0; c < x.c1; ++c, ++n) {
@@ -585,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t n = 0;
         bool ok = true;
         begin_feed(p, blockIdx.x, gridDim.x, feed);
-        while (ok && !p.only_state && next_piece(p, feed, here)) {
+        while (ok && !STATES && next_piece(p, feed, here)) {
             const Piece x = here;
             const float lg = head_decay(p, x.h, false);
             // Powers of g along the keys, from the gaps of the first two on: times g^2 for each next two keys
@@ -662,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t n = 0;
         bool ok = true;
         begin_feed(p, blockIdx.x, gridDim.x, feed);
-        while (ok && !p.only_state && next_piece(p, feed, here)) {
+        while (ok && !STATES && next_piece(p, feed, here)) {
             const Piece x = here;
             const int b = p.cuts ? 0 : x.sequence, h = x.h;
             const float lg = head_decay(p, h, false);
@@ -736,7 +741,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t n = 0;
         bool ok = true;
         begin_feed(p, blockIdx.x, gridDim.x, feed);
-        while (32 * q < TK && ok && next_walked(p, feed, here)) {
+        while (32 * q < TK && ok && next_walked<STATES>(p, feed, here)) {
             const Piece x = here;
             const int64_t own = ((int64_t)blockIdx.x * p.Da + row) * p.Dv;
             const int64_t kept = ((int64_t)x.sequence * p.Hq + x.h) * p.Da * p.Dv + row * p.row_stride;
@@ -744,10 +749,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (keeps) {  // the state in front of the piece
                 const float* from = nullptr;
                 int64_t step = 1;
-                if (!p.only_state && x.c0 > 0) {
+                if (!STATES && x.c0 > 0) {
                     from = p.slots + (int64_t)blockIdx.x * p.Da * p.Dv + row * p.slot_row;
                     step = p.slot_col;
-                } else if (!p.only_state && p.state) {
+                } else if (!STATES && p.state) {
                     from = p.state + kept;
                     step = p.col_stride;
                 }
@@ -762,14 +767,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tmem_wait_st();
             }
-            if (p.only_state) {
+            if (STATES) {
                 // (a block's one piece, without any decay between its chunks: the values' weights hold it)
                 tc_fence_before();
                 mbar_arrive(b_ready);
                 ok = wait_for(done, 0, abort_flag, p.waits);
                 tc_fence_after();
             }
-            for (int k = x.c0; k < x.c1 && !p.only_state; ++k, ++n) {
+            for (int k = x.c0; k < x.c1 && !STATES; ++k, ++n) {
                 int rows;
                 chunk_at(p, x, k, rows);
                 if (keeps) {
@@ -817,7 +822,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok) break;
             float* to = nullptr;
             int64_t step = 1;
-            if (p.only_state) {
+            if (STATES) {
                 to = p.slots_out + own;
             } else if (p.state_out && x.c1 == x.total) {
                 to = p.state_out + kept;
@@ -846,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t n = 0, g = 0;
         bool ok = true;
         begin_feed(p, blockIdx.x, gridDim.x, feed);
-        while (ok && next_walked(p, feed, here)) {
+        while (ok && next_walked<STATES>(p, feed, here)) {
             const Piece x = here;
             const float lg = head_decay(p, x.h, false);
             // From the end of a part where its weights are largest on, each next one of the thread's tokens has
@@ -856,7 +861,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 int rows;
                 chunk_at(p, x, k, rows);
                 ok = wait_use(C::kFullA, C::kA, n) && wait_use(C::kFullV, C::kV, n) &&
-                     (n < 2 || p.only_state || wait_chunk(y_free, n - 2));  // clean's and made's last phases are seen
+                     (n < 2 || STATES || wait_chunk(y_free, n - 2));  // clean's and made's last phases are seen
                 if (!ok) break;
                 uint8_t* v = tile_v(n);
                 if (rows < kChunk) {
@@ -876,7 +881,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 mbar_arrive(of(clean, n));
                 // without outputs the state is not decayed from chunk to chunk: all of its decay is in the values
-                const int behind = p.only_state ? (x.c1 - 1 - k) * kChunk : 0;
+                const int behind = STATES ? (x.c1 - 1 - k) * kChunk : 0;
 #pragma unroll 1
                 for (int part = 0; part < C::kParts; ++part, ++g) {
                     ok = g < (uint32_t)C::kBufs || wait_use(C::kVFree, C::kBufs, g - C::kBufs);
@@ -1138,10 +1143,10 @@ bool map_of(CUtensorMap* m, const flarepp_heads& t, int64_t B, int64_t H, int64_
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int TK, int TV>
+template <int TK, int TV, bool STATES>
 cudaError_t launch_walk(const CUtensorMap* m, const Walk& p, int64_t blocks, cudaStream_t st) {
-    using C = Cfg<TK, TV>;
-    auto kernel = walk_kernel<TK, TV>;
+    using C = Cfg<TK, TV, STATES>;
+    auto kernel = walk_kernel<TK, TV, STATES>;
     static std::atomic<uint64_t> ready{0};  // devices whose shared-memory limit is raised
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -1155,10 +1160,13 @@ cudaError_t launch_walk(const CUtensorMap* m, const Walk& p, int64_t blocks, cud
     return launch(kernel, blocks, kThreads, C::kSmem, st, m[0], m[1], m[2], m[3], p);
 }
 
-cudaError_t launch_for(const CUtensorMap* m, const Walk& p, int64_t units, cudaStream_t st) {
+template <bool STATES>
+cudaError_t launch_for(const CUtensorMap* m, const Walk& p, int64_t blocks, cudaStream_t st) {
     if (p.Da <= 64)
-        return p.Dv <= 64 ? launch_walk<64, 64>(m, p, units, st) : launch_walk<64, 128>(m, p, units, st);
-    return p.Dv <= 64 ? launch_walk<128, 64>(m, p, units, st) : launch_walk<128, 128>(m, p, units, st);
+        return p.Dv <= 64 ? launch_walk<64, 64, STATES>(m, p, blocks, st)
+                          : launch_walk<64, 128, STATES>(m, p, blocks, st);
+    return p.Dv <= 64 ? launch_walk<128, 64, STATES>(m, p, blocks, st)
+                      : launch_walk<128, 128, STATES>(m, p, blocks, st);
 }
 
 }  // namespace
@@ -1282,12 +1290,11 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         p.slots = slots;
         if (w.again) {
             p.state_out = w.state_out;
-            return launch_for(m, p, plan.blocks, st);
+            return launch_for<false>(m, p, plan.blocks, st);
         }
         Walk first = p;
-        first.only_state = 1;
         first.slots_out = left;
-        e = launch_for(m, first, plan.blocks, st);
+        e = launch_for<true>(m, first, plan.blocks, st);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)cdiv((int64_t)p.Da * p.Dv, 256), (unsigned)plan.blocks);
@@ -1302,7 +1309,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         if (e != cudaSuccess) return e;
     }
     p.state_out = w.state_out;
-    return launch_for(m, p, plan.blocks, st);
+    return launch_for<false>(m, p, plan.blocks, st);
 }
 
 cudaError_t decay_group_sum(const flarepp_decay_shape& s, const float* sums, const flarepp_heads& y, int64_t D,
