@@ -11,8 +11,9 @@
 // there. What bounds it is shared memory and the state's way round: a chunk's products, whose operands are read from
 // it, its tiles, decayed values and state move 580 KB through it at 128 channels, 4,500 of the 6,100
 // cycles that a chunk takes (keys, values of 64, 64: 3,800; 128, 64: 5,000; 64, 128: 6,000), and a chunk's state is
-// scaled, multiplied and added to before the next one's. 8 x 32 heads of 4,096 tokens and 128 channels take
-// 196 us (3.4 TB/s of what has to move), the gradients of 8 heads of 131,072 tokens 678.
+// scaled, multiplied and added to before the next one's. 4 x 32 heads of 8,192 tokens and 128 channels take
+// 196 us (3.4 TB/s of what has to move), the gradients of 8 heads of 131,072 tokens, 64 and 128 channels, 650
+// (HBM at 55 to 70 % in each of the walks).
 //
 // W o (X A^T) is rounded to bf16 as an operand, w o V and S are two bf16 each (Cfg says why and where not); sums,
 // states and what r multiplies are float32.
@@ -1175,7 +1176,7 @@ cudaError_t take_decay_status(int32_t* out, cudaStream_t st) { return take_libra
 
 // Each of the card's blocks walks an equal part of the list of all sequences' heads' chunks, so that a sequence
 // may be cut between two blocks or more, which costs a first walk over what lies in front of the cuts
-// (half a walk's time a chunk) and two launches; or the list is one of whole sequences' heads, and nothing is cut.
+// (a third to a half of a walk's time a chunk) and two launches; or the list is one of whole sequences' heads, and nothing is cut.
 // The cheaper one by the chunks that the busiest block has to do. (Lengths of packed sequences are not known
 // here: they are cut unless even the longest possible one is short.)
 DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
