@@ -82,6 +82,33 @@ def test_long_sequences_are_cut_and_joined(B, H, N, D):
     check(*inputs(B, H, H, N, D, D))
 
 
+@pytest.mark.parametrize("Dk,Dv", [(64, 128), (128, 64), (40, 104), (96, 24), (128, 128)])
+def test_cut_sequences_of_unlike_widths(Dk, Dv):
+    """The states in front of the parts of one gradient's walk are those of another's, turned."""
+    check(*inputs(1, 2, 1, 1700, Dk, Dv))
+
+
+@pytest.mark.parametrize("Dk,Dv", [(64, 128), (128, 24)])
+def test_packed_and_cut(Dk, Dv):
+    """Parts that begin in front of a sequence's first chunk, at it and behind it; empty sequences among them."""
+    lens = [0, 1, 700, 0, 0, 128, 129, 3, 900, 256, 0]
+    cuts = [5]
+    for n in lens:
+        cuts.append(cuts[-1] + n)
+    q, k, v, ld, dy, S, G = inputs(1, 4, 2, cuts[-1] + 3, Dk, Dv, n=len(lens))
+    off = torch.tensor(cuts, dtype=torch.int32, device="cuda")
+    Y, out = flarepp.decay_attention_fwd(q, k, v, ld, state=S, offsets=off, need_state=True)
+    dQ, dK, dV, dS = flarepp.decay_attention_bwd(q, k, v, ld, dy, state=S, offsets=off, dstate_out=G,
+                                                 need_dstate=True)
+    for i, (a, b) in enumerate(zip(cuts, cuts[1:])):
+        part = [x[:, :, a:b] for x in (q, k, v)]
+        ref = decay_refs(*part, ld, 1 / math.sqrt(Dk), S[i:i + 1], dy[:, :, a:b], G[i:i + 1])
+        for name, got in (("Y", Y), ("dQ", dQ), ("dK", dK), ("dV", dV)):
+            within(got[:, :, a:b], *ref[name], f"{name} of sequence {i}")
+        within(out[i:i + 1], *ref["state"], f"state of sequence {i}")
+        within(dS[i:i + 1], *ref["dstate"], f"dstate of sequence {i}")
+
+
 OFFSETS = {"even": [0, 128, 256, 400], "ragged": [3, 4, 4, 131, 133, 389, 390], "one": [0, 400],
            "empty": [7, 7, 7], "tail": [0, 50, 129]}
 
