@@ -1175,26 +1175,28 @@ cudaError_t launch_for(const CUtensorMap* m, const Walk& p, int64_t blocks, cuda
 cudaError_t take_decay_status(int32_t* out, cudaStream_t st) { return take_library_status(out, st); }
 
 // Each of the card's blocks walks an equal part of the list of all sequences' heads' chunks, so that a sequence
-// may be cut between two blocks or more, which costs a first walk over what lies in front of the cuts
-// (a third to a half of a walk's time a chunk) and two launches; or the list is one of whole sequences' heads, and nothing is cut.
-// The cheaper one by the chunks that the busiest block has to do. (Lengths of packed sequences are not known
-// here: they are cut unless even the longest possible one is short.)
+// may be cut between two blocks or more, which costs a first walk over what lies in front of the cuts and two
+// launches; or the list is one of whole sequences' heads, and nothing is cut. The cheaper one by the chunks that
+// the busiest block has to do, those of the first walk as 0.8 (it reads half of the bytes, and may be
+// as long again), the launches as ten. Whole and cut, us a forward in a graph: 128 heads of 8,192
+// tokens and 128 channels 187 and 313; of 64 channels 160 of 4,096 116 and 126, 76 of 8,192 109 and 110, 128 of 1,024
+// 22 and 52, 8 of 700 15 and 26, 8 of 1,200 22 and 28. (Lengths of packed sequences are not known here: the
+// longest possible one counts.)
 DecayPlan decay_plan(const flarepp_decay_shape& s, bool backward) {
     DecayPlan p{};
     p.sequences = s.sequences ? s.sequences : s.B;
     p.chunks = cdiv(s.N, kChunk);
     const int64_t heads = p.sequences * s.Hq;
+    const int64_t places = s.sequences ? s.Hq * (p.chunks + kDecayFront * s.sequences) : heads * p.chunks;
+    const int64_t whole = cdiv(heads, kNumSMs);  // heads of the busiest block
+    const int64_t cut = cdiv(places, kNumSMs);   // chunks of every block
+    p.whole = (double)(whole * p.chunks) <= (double)cut + 0.8 * (double)(cut < p.chunks ? cut : p.chunks) + 10;
     if (s.sequences) {
-        p.whole = p.chunks <= 4;
         p.blocks = p.whole && heads < kNumSMs ? heads : kNumSMs;
         p.share = p.whole ? cdiv(heads, p.blocks) : 0;
     } else {
-        const int64_t whole = cdiv(heads, kNumSMs);          // heads of the busiest block
-        const int64_t cut = cdiv(heads * p.chunks, kNumSMs);  // chunks of every block
-        const double first = 0.5 * (double)(cut < p.chunks ? cut : p.chunks);
-        p.whole = (double)(whole * p.chunks) <= (double)cut + first + 4;
         p.share = p.whole ? whole : cut;
-        p.blocks = cdiv(p.whole ? heads : heads * p.chunks, p.share);
+        p.blocks = cdiv(p.whole ? heads : places, p.share);
     }
     size_t at = 0;
     auto place = [&](size_t bytes) {
