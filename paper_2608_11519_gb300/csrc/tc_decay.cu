@@ -53,8 +53,11 @@ struct Walk {
     void* y;
     int64_t yb, yh, yn;
     int y_f32;
-    const float* slots;   // the state in front of every block's first chunk, [blocks] of Da x Dv
-    int slot_row, slot_col;  // its strides
+    // States in front of every block's first chunk, [blocks] of Da x Dv, and of its last piece's first if the
+    // sequence begins there and goes on in the next block: a copy of `state`, since the block that ends the
+    // sequence may have written state_out, which may be the same buffer, before this one begins.
+    const float *slots, *begins;
+    int slot_row, slot_col;  // their strides
     float* slots_out;     // of the first walk: the state that a block's last piece leaves
     const float* state;   // in front of every sequence, or NULL
     float* state_out;
@@ -109,6 +112,7 @@ struct Piece {
     int sequence, h;
     int start, rows;  // the sequence's tokens
     int c0, c1, total;
+    int begun;        // whether the block before has begun with it
 };
 // Where a block is in its part of the list.
 struct Feed {
@@ -156,6 +160,7 @@ __device__ __noinline__ bool next_piece(const Walk& p, Feed& f, Piece& x) {
     x.total = (x.rows + kChunk - 1) / kChunk;
     x.c0 = p.whole ? 0 : min(max(f.at - base - p.front, 0), x.total);
     x.c1 = p.whole ? x.total : min(max(f.end - base - p.front, 0), x.total);
+    x.begun = f.at > base;
     f.at = base + each;
     if (++f.h == p.Hq) {
         f.h = 0;
@@ -750,8 +755,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (keeps) {  // the state in front of the piece
                 const float* from = nullptr;
                 int64_t step = 1;
-                if (!STATES && x.c0 > 0) {
-                    from = p.slots + (int64_t)blockIdx.x * p.Da * p.Dv + row * p.slot_row;
+                // (an empty sequence's places, in two blocks perhaps, all take `state` itself)
+                if (!STATES && x.total > 0 && (x.begun || (p.state && x.c1 < x.total))) {
+                    from = (x.begun ? p.slots : p.begins) + (int64_t)blockIdx.x * p.Da * p.Dv + row * p.slot_row;
                     step = p.slot_col;
                 } else if (!STATES && p.state) {
                     from = p.state + kept;
@@ -1030,10 +1036,11 @@ __global__ void __launch_bounds__(256)
 
 // ------------------------------------------------------------------ the join over a sequence's pieces
 // In: the state that a block's last piece leaves from nothing, for blocks whose last piece's sequence goes on
-// in the next block. Out, in place: the state in front of every block's first chunk. A group of blocks
+// in the next block. Out: the state in front of every block's first chunk, and, in place of what the block left
+// with which a sequence begins, the state in front of the sequence (if there is one: Walk::begins). A group of blocks
 // (blockIdx.y) follows the sequence that begins in walk block y and goes on in the next, a thread one
 // value of the state, kAhead blocks' values in flight.
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk p, const float* left, float* slots,
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk p, float* left, float* slots,
                                                    int blocks) {
     tc::pdl_trigger();
     tc::pdl_wait();
@@ -1061,6 +1068,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk 
     const int r = e / q.Dv, c = e - r * q.Dv;
     float run = q.state ? q.state[((int64_t)low * q.Hq + h) * size + r * q.row_stride + c * q.col_stride] : 0.f;
     const int last = (base + each - 1) / share;  // the walk block that ends the sequence
+    const float begin = run;
     for (int k0 = y; k0 < last; k0 += kAhead) {
         float v[kAhead];
 #pragma unroll
@@ -1073,6 +1081,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk 
             run = fmaf(exp2f(lg * rows_of(chunks_to(k * share), chunks_to((k + 1) * share))), run, v[j]);
             slots[(int64_t)(k + 1) * size + e] = run;
         }
+        if (k0 == y && q.state) left[(int64_t)y * size + e] = begin;
     }
 }
 
@@ -1291,6 +1300,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         float* left = (float*)(ws + plan.off_left);
         float* slots = (float*)(ws + plan.off_slots);
         p.slots = slots;
+        p.begins = left;
         if (w.again) {
             p.state_out = w.state_out;
             return launch_for<false>(m, p, plan.blocks, st);
@@ -1308,7 +1318,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
         attr[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        e = cudaLaunchKernelEx(&cfg, join_kernel, p, (const float*)left, slots, (int)plan.blocks);
+        e = cudaLaunchKernelEx(&cfg, join_kernel, p, left, slots, (int)plan.blocks);
         if (e != cudaSuccess) return e;
     }
     p.state_out = w.state_out;

@@ -202,6 +202,20 @@ def test_parts_of_one_buffer_and_shared_heads():
     within(Y, *decay_refs(both, k, v, ld, 0.125, None)["Y"], "Y with one batch element's queries")
 
 
+def test_cut_sequences_go_on_in_place():
+    """40 heads of 29 chunks in parts of 8: blocks that end a sequence, and write its state, are done long before
+    the one that begins with it comes to its state."""
+    q, k, v, ld, dy, S, G = inputs(1, 40, 40, 29 * 128 - 5, 32, 32)
+    Y, out = flarepp.decay_attention_fwd(q, k, v, ld, state=S, need_state=True)
+    dQ, dK, dV, dS = flarepp.decay_attention_bwd(q, k, v, ld, dy, state=S, dstate_out=G, need_dstate=True)
+    for _ in range(5):
+        s, g = S.clone(), G.clone()
+        Y1, s1 = flarepp.decay_attention_fwd(q, k, v, ld, state=s, state_out=s)
+        grads = flarepp.decay_attention_bwd(q, k, v, ld, dy, state=S, dstate_out=g, dstate=g)
+        for a, b in zip((Y, out, dQ, dK, dV, dS), (Y1, s1) + tuple(grads)):
+            assert torch.equal(a, b)
+
+
 def test_a_sequence_in_parts_goes_on_in_place():
     """Prompt, further prompt and single tokens, the state kept in one buffer."""
     B, H, N, D = 2, 4, 330, 64
