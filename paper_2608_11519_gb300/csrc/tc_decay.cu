@@ -12,7 +12,7 @@
 // it, its tiles, decayed values and state move 580 KB through it at 128 channels, 4,500 of the 6,100
 // cycles that a chunk takes (keys, values of 64, 64: 3,800; 128, 64: 5,000; 64, 128: 6,000), and a chunk's state is
 // scaled, multiplied and added to before the next one's. 4 x 32 heads of 8,192 tokens and 128 channels take
-// 196 us (3.4 TB/s of what has to move), the gradients of 8 heads of 131,072 tokens, 64 and 128 channels, 650
+// 196 us (3.4 TB/s of what has to move), the gradients of 8 heads of 131,072 tokens, 64 and 128 channels, 658
 // (HBM at 55 to 70 % in each of the walks).
 //
 // W o (X A^T) is rounded to bf16 as an operand, w o V and S are two bf16 each (Cfg says why and where not); sums,
@@ -66,7 +66,8 @@ struct Walk {
 };
 
 // STATES: the first walk over what lies in front of the cuts, which only finds states. (A choice at run time
-// in one kernel left it with the shallow rings of the other and both with more code.)
+// in one kernel left it with the shallow rings of the other and both with more code: the long backward took
+// 680 us instead of 650.)
 template <int TK, int TV, bool STATES>
 struct Cfg {
     // TMEM columns: scores (W o scores as bf16 over a half of them), (W o scores) V, X S, the state. Values of
