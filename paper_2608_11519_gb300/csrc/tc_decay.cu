@@ -48,6 +48,7 @@ struct Walk {
     int front;            // places that a sequence's head has in front of its chunks
     const int2* starts;   // and the sequence and head of every block's first place, where they are cut
     float scale_p, scale_w, scale_r;  // what scores, decayed values and X S are multiplied by
+    float gentle;                     // decays above it (base 2, per token) make powers by products along a row
     int lead;                         // r_i = g^(i + lead), w_j = g^(n - lead - j)
     const float* log_decay;
     void* y;
@@ -603,11 +604,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             // Powers of g along the keys, from the gaps of the first two on: times g^2 for each next two keys
             // backwards, times g^-2 forwards. (On the diagonal gaps may be below 0: those keys do not
             // count.) From g = 1/2 on the first power, g^127 at least, is one that float32 holds; below
-            // that each takes an exponential of its own. A table of powers in shared memory, which
-            // the products' operands come from too, took longer than the chain.
+            // that each takes an exponential of its own. So it does with a scale below 2^-40: the chain begins up to
+            // 64 keys in front of those that count, at 2^-77 times the scale, and what float32 does not hold
+            // there would be 0 where it counts. A table of powers in shared memory, which the products' operands
+            // come from too, took longer than the chain.
             const float way = p.back ? lg : -lg;
             const int gap0 = p.back ? 64 * half + low - i : i - 64 * half - low;
-            const bool gentle = lg > -1.01f;
+            const bool gentle = lg > p.gentle;
             const float g2 = gentle ? exp2f(2.f * way) : 1.f;
             const uint64_t next = pair(g2, g2);
             const uint64_t first = pair(exp2f(lg * gap0) * p.scale_p, exp2f(lg * gap0 + way) * p.scale_p);
@@ -1279,6 +1282,7 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
     p.share = (int)plan.share;
     p.lead = w.back ? 0 : 1;
     p.scale_p = s.scale;
+    p.gentle = fabsf(s.scale) >= 0x1p-40f || s.scale == 0.f ? -1.01f : 0.f;
     p.scale_w = w.back ? s.scale : 1.f;
     p.scale_r = w.back ? 1.f : s.scale;
     p.log_decay = w.log_decay;
