@@ -653,8 +653,8 @@ typedef struct {
  * Rotary positions: each of the P pairs of channels (x, y) of a token of q and k is turned by the angle
  * a = position[axis of the pair] * freqs[pair],
  *     x' = x cos a - y sin a,  y' = y cos a + x sin a;
- * channels from 2 P on are copied. Angles are exact to some 2^-22 rad however far the positions; products in
- * float32, rounded once.
+ * channels from 2 P on are copied. Angles are exact to 2^-20 rad for every int32 position, and for real ones whose
+ * angles are below 2^40 rad; products in float32, rounded once.
  *   q [B, Hq, N, D], k [B, Hk, N, D], outputs the same: any addresses and strides (16-byte ones are
  *     fast). Hq or Hk may be 0 (that tensor and its output may then be NULL). An output may be its own
  *     input (the same address and strides); otherwise outputs overlap nothing.

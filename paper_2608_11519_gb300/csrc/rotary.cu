@@ -8,9 +8,10 @@
 //
 // The angle. Far positions leave no bits of position * freq behind the point in 32 bits (10^6 rad has
 // a unit of 0.06), so it is taken in turns as a sum of products whose rounding errors are kept (each by
-// a fused multiply-add) and whose whole turns are dropped one by one: freq / (2 pi) in three floats, the
-// position in two (an int32 has 31 bits). What is left is off by a few 2^-25 turns, whatever
-// the position.
+// a fused multiply-add) and whose whole turns are dropped one by one: freq / (2 pi) in three floats (72 bits), the
+// position in two (an int32 has 31 bits). What is left is off by four roundings of 2^-25 turns at most, 2^-20 rad
+// with the sine's own, for any int32 position and real ones up to 2^40 rad. (With the third float rounded from the
+// second one's rounded error, 51 bits in all, angles were off by 2^-17 rad at 2^31 and by 2^-9 at 2^40.)
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -53,15 +54,28 @@ struct Rotary {
 
 __device__ __forceinline__ float fraction(float x) { return x - rintf(x); }
 
-// cos and sin of (p + q) f, p and q floats
-__device__ __forceinline__ void turn_of(float p, float q, float f, float& c, float& s) {
+// f / (2 pi) as a sum of three floats. (The _rn forms are not contracted into multiply-adds.)
+struct Turns {
+    float hi, mid, lo;
+};
+__device__ __forceinline__ Turns turns_of(float f) {
     const float kHi = 0.159154937f, kLo = 6.42063824e-09f, kLast = 7.3427387e-17f;  // 1 / (2 pi)
-    const float f0 = f * kHi, rest = fmaf(f, kHi, -f0), f1 = fmaf(f, kLo, rest);
-    const float f2 = fmaf(f, kLast, fmaf(f, kLo, rest - f1));
-    const float m = p * f0, n = q * f0, l = p * f1;
-    const float r = fraction(m) + fraction(fmaf(p, f0, -m)) + fraction(n) + fraction(l) +
-                    (fmaf(q, f0, -n) + fmaf(p, f1, -l) + p * f2 + q * f1);
-    sincospif(2.f * fraction(r), &s, &c);
+    Turns t;
+    t.hi = __fmul_rn(f, kHi);
+    const float a = fmaf(f, kHi, -t.hi), b = __fmul_rn(f, kLo);
+    t.mid = __fadd_rn(a, b);
+    const float z = __fsub_rn(t.mid, b);  // what that sum leaves, exactly
+    const float rest = __fadd_rn(__fsub_rn(b, __fsub_rn(t.mid, z)), __fsub_rn(a, z));
+    t.lo = fmaf(f, kLast, __fadd_rn(rest, fmaf(f, kLo, -b)));
+    return t;
+}
+
+// cos and sin of (p + q) f, p and q floats
+__device__ __forceinline__ void turn_of(float p, float q, const Turns& f, float& c, float& s) {
+    const float m = __fmul_rn(p, f.hi), n = __fmul_rn(q, f.hi), l = __fmul_rn(p, f.mid);
+    const float r = fraction(fraction(m) + fraction(fmaf(p, f.hi, -m))) + fraction(fraction(n) + fraction(l));
+    const float small = fmaf(q, f.hi, -n) + fmaf(p, f.mid, -l) + p * f.lo + q * f.mid;
+    sincospif(2.f * fraction(r + small), &s, &c);
 }
 
 // The position of row n in two floats
@@ -164,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 3) pairs_kernel(const Rotary a) {
     for (int i = 0; i < W; ++i) {
         const int k = axis_of(a, p0 + i);
         if (k != held) position(a, b, n, held = k, p, q);
-        turn_of(p, q, a.freqs[p0 + i], cs[i], sn[i]);
+        turn_of(p, q, turns_of(a.freqs[p0 + i]), cs[i], sn[i]);
         sn[i] *= a.sign;
     }
     constexpr int kFlight = 4;
@@ -229,6 +243,7 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const Rotary a, int t
     constexpr uint32_t kHead = 32 * 16;  // bytes of a head's stage of a warp
     __shared__ __align__(16) uint8_t stages[kThreads / 32][kFlight * kHead];
     __shared__ int places[kMaxDim];  // by channel: its pair, its partner, and whether it is the first
+    __shared__ Turns freqs[kMaxDim / 2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint8_t* const stage = stages[warp];
     float2* const table = reinterpret_cast<float2*>(stage);  // [tokens][P], before the stage is used
@@ -240,6 +255,7 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const Rotary a, int t
             first = pair + start;
             second = first + a.ends[k] - start;
         }
+        freqs[pair] = turns_of(a.freqs[pair]);
         places[first] = pair << 16 | second << 1 | 1;
         places[second] = pair << 16 | first << 1;
     }
@@ -258,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const Rotary a, int t
         const int bk = r / a.N;
         float p, q, c, s;
         position(a, bk, r - bk * a.N, axis_of(a, pair), p, q);
-        turn_of(p, q, a.freqs[pair], c, s);
+        turn_of(p, q, freqs[pair], c, s);
         table[e] = make_float2(c, s * a.sign);
     }
     __syncwarp();
