@@ -578,8 +578,9 @@ typedef struct {
  *     S_t = g S_(t-1) + k_t v_t^T,     y_t = scale * q_t S_t.
  *   Q [B, Hq, N, Dk]; K [B, Hk, N, Dk]; V [B, Hk, N, Dv]; Y [B, Hq, N, Dv], bf16, addresses and strides
  *     multiples of 16 bytes.
- *   log_decay [Hq] float32, at most 0 (-inf: no memory of earlier tokens); one above 0 counts as 0 and a
- *     NaN as -inf, and both set `status`.
+ *   log_decay [Hq] float32, at most 0 (-inf, or less than float32's exponential holds: no memory of earlier tokens
+ *     or of a state, not even of values that are not finite); one above 0 counts as 0 and a NaN as -inf, and both
+ *     set `status`.
  *   offsets: with packed sequences, int32 [sequences + 1]: sequence i is the tokens offsets[i] to
  *     offsets[i + 1] (it may be empty). Tokens before the first and behind the last sequence are not read,
  *     and their outputs are 0. Offsets that fall or leave 0 to N are brought back to what came before them

@@ -15,10 +15,9 @@ __device__ __forceinline__ float decay_log2(float log_decay, bool* bad) {
     if (!(log_decay <= 0.f)) *bad = true;
     return log_decay > -1e6f ? log_decay * 1.44269504f : -1e6f;
 }
-
-}  // namespace flarepp
-
-namespace flarepp {
+// Whether nothing is left of the token before (2^lg is 0 in float32): then nothing is left of what is not finite
+// either, which a product with 0 would keep.
+__device__ __forceinline__ bool forgets(float lg) { return lg <= -150.f; }
 
 constexpr int kDecayChunk = 128;  // tokens
 // A packed sequence's head counts as so many chunks more than it has, in front: what it takes to begin with it

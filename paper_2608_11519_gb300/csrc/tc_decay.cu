@@ -305,6 +305,28 @@ __device__ __forceinline__ void keep_keys(uint32_t* w, uint32_t bits) {
     }
 }
 
+// What a head without memory has in TMEM or in a tile of what it does not remember becomes 0, whatever it was. Out of
+// line: in the loops over columns that every head takes, a choice took up to 6 % of a walk.
+__device__ __noinline__ void clear_columns(uint32_t at, int columns, bool keep) {
+    for (int c = 0; c < columns; c += 16) {
+        uint32_t r[16];
+        tmem_ld16(at + c, r);
+        tmem_wait_ld16(r);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) r[j] = keep ? r[j] : 0u;
+        tmem_st16(at + c, r);
+    }
+    tmem_wait_st();
+}
+template <int T>
+__device__ __noinline__ void clear_rows(uint8_t* tile, int thread, int but) {
+    for (int e = thread; e < 8 * kChunk; e += 128)
+        if (e / 8 != but)
+#pragma unroll
+            for (int t = 0; t < T / 64; ++t)
+                *reinterpret_cast<uint4*>(tile + 16 * e + t * kAtomBytes) = make_uint4(0, 0, 0, 0);
+}
+
 // How many chunks a block walks.
 template <bool STATES>
 __device__ __noinline__ int count_chunks(const Walk& p) {
@@ -610,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // come from too, took longer than the chain.
             const float way = p.back ? lg : -lg;
             const int gap0 = p.back ? 64 * half + low - i : i - 64 * half - low;
-            const bool gentle = lg > p.gentle;
+            const bool gentle = lg > p.gentle, alone = forgets(lg);
             const float g2 = gentle ? exp2f(2.f * way) : 1.f;
             const uint64_t next = pair(g2, g2);
             const uint64_t first = pair(exp2f(lg * gap0) * p.scale_p, exp2f(lg * gap0 + way) * p.scale_p);
@@ -647,11 +669,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 8; ++j) w[j] = bf16_bits(r[2 * j], r[2 * j + 1]);
                     }
-                    // on the diagonal, and in a chunk that ends early, what does not count is 0
+                    // on the diagonal, in a chunk that ends early and without memory, what does not count is 0
                     // whatever it was
-                    if ((key >> 5) == q || key + 16 > rows) {
-                        const int least = p.back ? i - key : 0;
-                        const int most = min(p.back ? 16 : i + 1 - key, rows - key);
+                    if ((key >> 5) == q || key + 16 > rows || alone) {
+                        const int least = p.back || alone ? i - key : 0;
+                        const int most = min(p.back && !alone ? 16 : i + 1 - key, rows - key);
                         keep_keys(w, (most >= 16 ? 0xffffu : most <= 0 ? 0u : (1u << most) - 1u) &
                                          (least <= 0 ? ~0u : least >= 16 ? 0u : ~0u << least));
                     }
@@ -694,6 +716,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // where whole lines are stored. (Stores of a thread's own row, 16 bytes of 32 lines an
                 // instruction, held up the state's through the pipe that they share: 241 us instead of 229
                 // for the prefill, when this was chosen.)
+                // (without memory the state in front is at most the first token's)
+                if (forgets(lg)) clear_columns(at + C::kColX + n % kSets * TV, p.Dv, since + p.lead == 0);
                 const bool staging = staged(p, rows);
                 uint8_t* stage = tile_v(n) + i * 128;
                 if (!staging && threadIdx.x == 384) mbar_arrive(ring(C::kEmptyV, C::kV, n));
@@ -756,6 +780,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int64_t own = ((int64_t)blockIdx.x * p.Da + row) * p.Dv;
             const int64_t kept = ((int64_t)x.sequence * p.Hq + x.h) * p.Da * p.Dv + row * p.row_stride;
             const float lg = head_decay(p, x.h, row == 0);
+            const bool alone = forgets(lg);
             if (keeps) {  // the state in front of the piece
                 const float* from = nullptr;
                 int64_t step = 1;
@@ -821,6 +846,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         tmem_st16(at + c, r);
                     }
                     tmem_wait_st();
+                    if (alone) clear_columns(at, p.Dv, false);
                 }
                 fence_proxy_async();
                 tc_fence_before();
@@ -868,6 +894,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // From the end of a part where its weights are largest on, each next one of the thread's tokens has
             // `ratio` times the last one's weight.
             const float ratio = exp2f(lg * stride);
+            const bool alone = forgets(lg);
             for (int k = x.c0; k < x.c1; ++k, ++n) {
                 int rows;
                 chunk_at(p, x, k, rows);
@@ -890,9 +917,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                             *reinterpret_cast<uint4*>(a + 16 * e + t * kAtomBytes) = make_uint4(0, 0, 0, 0);
                     fence_proxy_async();
                 }
-                mbar_arrive(of(clean, n));
                 // without outputs the state is not decayed from chunk to chunk: all of its decay is in the values
                 const int behind = STATES ? (x.c1 - 1 - k) * kChunk : 0;
+                // Without memory only a token whose weight is a power of 0 is left in the state, and of the others not
+                // even what is not finite: their rows of A become 0, when the scores are made.
+                const int last = !alone || p.back || behind ? -1 : rows - 1;
+                if (alone) {
+                    ok = STATES || wait_chunk(s_ready, n);
+                    if (!ok) break;
+                    clear_rows<TK>(tile_a(n), maker, last);
+                    fence_proxy_async();
+                }
+                mbar_arrive(of(clean, n));
 #pragma unroll 1
                 for (int part = 0; part < C::kParts; ++part, ++g) {
                     ok = g < (uint32_t)C::kBufs || wait_use(C::kVFree, C::kBufs, g - C::kBufs);
@@ -905,7 +941,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     int o = row * 128 + 16 * ((maker & ((1 << shift) - 1)) ^ (row & 7));
                     const uint8_t* from = v + part * C::kPart * 128;
                     const int step = p.back ? stride * 128 : -stride * 128;
-                    if (rows == kChunk) {
+                    if (rows == kChunk && !alone) {
                         float w = exp2f(lg * (behind + (p.back ? at + 1 - p.lead : kChunk - p.lead - at))) * p.scale_w;
 #pragma unroll 1
                         for (int e = 0; e < turns; e += 4 / (TV / 64)) {
@@ -932,7 +968,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                             for (int t = 0; t < TV / 64; ++t) {
                                 uint4 d = make_uint4(0, 0, 0, 0), rest = d;
-                                if (at < rows)
+                                if (alone ? at == last : at < rows)
                                     d = scaled(*reinterpret_cast<const uint4*>(from + o + t * kAtomBytes), w, rest);
                                 *reinterpret_cast<uint4*>(to + o + t * C::kPart * 128) = d;
                                 *reinterpret_cast<uint4*>(to + C::kVw + o + t * C::kPart * 128) = rest;
@@ -1082,7 +1118,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Walk 
         for (int j = 0; j < kAhead; ++j) {
             const int k = k0 + j;
             if (k >= last) break;
-            run = fmaf(exp2f(lg * rows_of(chunks_to(k * share), chunks_to((k + 1) * share))), run, v[j]);
+            const int rows = rows_of(chunks_to(k * share), chunks_to((k + 1) * share));
+            run = rows > 0 && forgets(lg) ? v[j] : fmaf(exp2f(lg * rows), run, v[j]);
             slots[(int64_t)(k + 1) * size + e] = run;
         }
         if (k0 == y && q.state) left[(int64_t)y * size + e] = begin;
