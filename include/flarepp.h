@@ -593,6 +593,8 @@ typedef struct {
  * its terms' magnitudes, tensor cores' sums included), and so is the state that outputs are made from,
  * but where Dk and Dv are both above 64: there it is one. The sums run in a fixed order: two calls on
  * the same inputs give the same bits.
+ * Infinities and NaN reach what the recurrence takes them to: later tokens of their sequence (in the gradients' walks
+ * from the end earlier ones), no others. Chunks of 128 tokens that hold some are slow (up to 1 ms each).
  *   workspace: at least flarepp_decay_attention_workspace_bytes(shape) bytes, 256-byte aligned.
  *   Y, state_out and the workspace must not overlap each other or an input (but state_out the state).
  */

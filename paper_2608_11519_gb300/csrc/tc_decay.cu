@@ -33,6 +33,12 @@ constexpr int kChunk = kDecayChunk;
 constexpr int kAtomBytes = kChunk * 128;  // 128 tokens of 64 channels
 constexpr size_t kWsAlign = 256;
 
+// Where an operand's values are, for what is not loaded as tiles; in values.
+struct Source {
+    const __nv_bfloat16* t;
+    int64_t b, h, n;
+};
+
 struct Walk {
     int Hq, N, Da, Dv;
     int back;
@@ -51,6 +57,7 @@ struct Walk {
     float gentle;                     // decays above it (base 2, per token) make powers by products along a row
     int lead;                         // r_i = g^(i + lead), w_j = g^(n - lead - j)
     const float* log_decay;
+    Source x, a, v;
     void* y;
     int64_t yb, yh, yn;
     int y_f32;
@@ -325,6 +332,95 @@ __device__ __noinline__ void clear_rows(uint8_t* tile, int thread, int but) {
 #pragma unroll
             for (int t = 0; t < T / 64; ++t)
                 *reinterpret_cast<uint4*>(tile + 16 * e + t * kAtomBytes) = make_uint4(0, 0, 0, 0);
+}
+
+// (W o X A^T) V has every token of a chunk in every output, those that do not count with a weight of 0, and 0 times an
+// infinity or NaN is NaN. So where a warp's outputs from the chunk are NaN (TMEM tells with the load), its tokens' are
+// made again one product after another, of the tokens that count alone: what is no number then reaches what it
+// reaches in the recurrence. The weights, rounded as they were, take the place of the outputs in TMEM, two in a word.
+// Such a chunk takes 0.3 ms at 64 channels, 0.75 at 128, a chunk whose outputs are numbers no more than before but for
+// the code's place in registers: 3 % of the packed training, 4 of the prefill, none of the long backward. (With eight keys
+// in flight it took half, but all others 1 to 6 % more; a look at the values before their product took 4 to 15 % of every
+// walk, whichever warps did it.)
+__device__ __forceinline__ const __nv_bfloat16* source(const Source& s, int b, int own_batch, int h, int group,
+                                                       int64_t token) {
+    return s.t + (int64_t)b * own_batch * s.b + (int64_t)(group ? h / group : 0) * s.h + token * s.n;
+}
+__device__ __forceinline__ void eight(const __nv_bfloat16* t, float* v) {
+    const uint4 d = *reinterpret_cast<const uint4*>(t);
+    const uint32_t w[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[2 * j] = __uint_as_float(w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+}
+// One warp: lane's token i of the chunk that begins at `token`; `mine`: whether its outputs are written, into the tile
+// row `stage` or to p.y + to; y_at, x_at: columns of outputs and of X S, which has the factor f.
+__device__ __forceinline__ void outputs_again(const Walk& p, uint32_t y_at, uint32_t x_at, int b, int h, int token,
+                                           int rows, int i, bool mine, float lg, float f, uint8_t* stage,
+                                           int64_t to) {
+    const bool alone = forgets(lg);
+    auto counts = [&](int key) { return key < rows && (key == i || (!alone && (p.back ? key > i : key < i))); };
+    const __nv_bfloat16* x = source(p.x, b, p.mx, h, p.gx, token + min(i, rows - 1));
+    const __nv_bfloat16* a = source(p.a, b, p.ma, h, p.ga, token);
+    const __nv_bfloat16* v = source(p.v, b, p.mv, h, p.gv, token);
+#pragma unroll 1
+    for (int key = 0; key < rows; key += 2) {
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (!counts(key + k)) continue;
+            const __nv_bfloat16* row = a + (int64_t)(key + k) * p.a.n;
+#pragma unroll 1
+            for (int d = 0; d < p.Da; d += 8) {
+                float u[8], w[8];
+                eight(x + d, u);
+                eight(row + d, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[k] = fmaf(u[j], w[j], s[k]);
+            }
+            s[k] *= exp2f(lg * abs(key + k - i)) * p.scale_p;
+        }
+        __syncwarp();
+        tmem_st1(y_at + key / 2, bf16_pair(s[0], s[1]));
+    }
+    tmem_wait_st();
+#pragma unroll 1
+    for (int c = 0; c < p.Dv; c += 8) {
+        float y[8];
+        uint32_t s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = 0.f;
+#pragma unroll 1
+        for (int key = 0; key < rows; key += 2) {
+            const uint32_t w = tmem_ld1(y_at + key / 2);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (!counts(key + k)) continue;
+                float u[8];
+                eight(v + (int64_t)(key + k) * p.v.n + c, u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = fmaf(__uint_as_float(k ? w & 0xffff0000u : w << 16), u[j], y[j]);
+            }
+            __syncwarp();
+        }
+        tmem_ld8(x_at + c, s);
+        wait_ld8(s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = fmaf(__uint_as_float(s[j]), f, y[j]);
+        if (mine && p.y_f32 && !stage) {
+            float4* d = reinterpret_cast<float4*>((float*)p.y + to + c);
+            d[0] = make_float4(y[0], y[1], y[2], y[3]);
+            d[1] = make_float4(y[4], y[5], y[6], y[7]);
+        } else if (mine) {
+            uint4* d = stage ? reinterpret_cast<uint4*>(stage + c / 64 * kAtomBytes + 16 * ((c % 64 / 8) ^ (i & 7)))
+                             : reinterpret_cast<uint4*>((__nv_bfloat16*)p.y + to + c);
+            *d = make_uint4(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]),
+                            bf16_pair(y[6], y[7]));
+        }
+        __syncwarp();
+    }
 }
 
 // How many chunks a block walks.
@@ -721,13 +817,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool staging = staged(p, rows);
                 uint8_t* stage = tile_v(n) + i * 128;
                 if (!staging && threadIdx.x == 384) mbar_arrive(ring(C::kEmptyV, C::kV, n));
+                bool no_number = false;
 #pragma unroll 1
                 for (int c = 0; c < p.Dv; c += 16) {
                     uint32_t y[16], s[16];
-                    tmem_ld16(at + C::kColY + c, y);
+                    float most = tmem_ldmaxnan16(at + C::kColY + c, y);
                     tmem_ld16(at + C::kColX + n % kSets * TV + c, s);
                     tmem_wait_ld16(y);
                     tmem_wait_ld16(s);
+                    reg_after_wait16(y, most);
+                    no_number = no_number || most != most;
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         y[j] = __float_as_uint(fmaf(__uint_as_float(s[j]), f, __uint_as_float(y[j])));
@@ -759,6 +858,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     __syncwarp();
                 }
+                if (__builtin_expect(__any_sync(0xffffffffu, no_number && i < rows), 0))
+                    outputs_again(p, at + C::kColY, at + C::kColX + n % kSets * TV, b, h, token, rows, i,
+                                  no_number && i < rows, lg, f, staging ? stage : nullptr, to);
                 tc_fence_before();
                 mbar_arrive(of(y_free, n));
                 if (staging) {
@@ -1323,6 +1425,11 @@ cudaError_t decay_walk(const DecayPlan& plan, char* ws, const DecayWalk& w, cuda
     p.scale_w = w.back ? s.scale : 1.f;
     p.scale_r = w.back ? 1.f : s.scale;
     p.log_decay = w.log_decay;
+    Source* const sources[3] = {&p.x, &p.a, &p.v};
+    for (int i = 0; i < 3; ++i) {
+        const flarepp_heads& t = *of[i]->t;
+        *sources[i] = {(const __nv_bfloat16*)t.data, t.stride_b, t.stride_h, t.stride_n};
+    }
     if (w.y32) {
         p.y = w.y32, p.y_f32 = 1;
         p.yn = w.Dv, p.yh = s.N * w.Dv, p.yb = s.Hq * p.yh;
