@@ -686,7 +686,8 @@ typedef struct {
  *   gamma, beta [C], each or both NULL (1 and 0).
  *   lengths: NULL, or int32 [B]: only the first lengths[b] rows of sample b count; the others are not read,
  *     and are 0 in Y. A length outside 0 to N is brought into it and sets `status`.
- *   stats: NULL, or float32 [B, 2, G]: the means and the rstds, which flarepp_group_norm_bwd takes.
+ *   stats: NULL, or float32 [B, 2, G]: the means and the rstds, which flarepp_group_norm_bwd takes (of a sample
+ *     without rows that count: 0 and 1 / sqrt(eps)).
  *   workspace: at least flarepp_group_norm_workspace_bytes(shape) bytes, 256-byte aligned.
  *   Outputs and workspace must not overlap each other or an input.
  * Statistics are float32 sums of squares about the mean, in a fixed order.

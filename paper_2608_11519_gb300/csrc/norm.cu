@@ -880,6 +880,14 @@ __global__ void __launch_bounds__(kThreads) back_few_kernel(const Norm p, int la
                     make_float2(u[v * W + i], w[v * W + i]);
 }
 
+// Statistics of samples without rows: those of one whose length is 0.
+__global__ void __launch_bounds__(kThreads) empty_kernel(float* stats, int64_t n, int G, float eps) {
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads)
+        stats[i] = i / G % 2 ? rsqrtf(eps) : 0.f;
+}
+
 // ------------------------------------------------------------------ host side
 template <typename... Args>
 cudaError_t launch(void (*kernel)(Args...), int64_t blocks, int threads, cudaStream_t st,
@@ -1079,6 +1087,10 @@ flarepp_status group_norm(bool back, const flarepp_norm_shape* shape, const void
     if (!disjoint(outs, 6, ins, 6)) return FLAREPP_ERR_INVALID_ARGUMENT;
     cudaError_t e = cudaSuccess;
     if (n == 0) {
+        const int64_t values = s.B * 2 * s.G;
+        if (!back && stats && values)
+            e = launch(empty_kernel, values < kNumSMs * kThreads ? cdiv(values, kThreads) : kNumSMs, kThreads, st,
+                       stats, values, (int)s.G, s.eps);
         if (back && dgamma) e = cudaMemsetAsync(dgamma, 0, pn, st);
         if (back && dbeta && e == cudaSuccess) e = cudaMemsetAsync(dbeta, 0, pn, st);
         return e == cudaSuccess ? FLAREPP_OK : FLAREPP_ERR_CUDA;
