@@ -379,7 +379,7 @@ FLAREPP_API void flarepp_test_wait_fault(int kernel, int64_t ring_item, uint64_t
  * can see (without one they set a word of the library's, see flarepp_layers_device_status):
  * FLAREPP_ERR_TIMEOUT for a bounded wait that gave up (the outputs are then invalid),
  * FLAREPP_ERR_INVALID_ARGUMENT for an embedding id beyond the table (below: for an offset, a length or
- * a decay out of its range).
+ * a decay out of its range). The caller sets it to FLAREPP_OK; of several that are recorded the worst stays.
  * ------------------------------------------------------------------------------------------ */
 typedef enum {
     FLAREPP_ACT_NONE = 0,

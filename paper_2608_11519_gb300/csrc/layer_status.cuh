@@ -12,9 +12,13 @@ namespace {
 
 __device__ int32_t library_status;
 
+// The larger word stays: a call may record a wait that gave up, whose outputs are invalid, and in another block or a
+// later launch an argument that it brought into its range, whose are not.
 __device__ __forceinline__ void record_status(int32_t* status, flarepp_status what) {
-    atomicExch(status ? status : &library_status, (int32_t)what);
+    atomicMax(status ? status : &library_status, (int32_t)what);
 }
+static_assert(FLAREPP_ERR_TIMEOUT > FLAREPP_ERR_INVALID_ARGUMENT && FLAREPP_ERR_INVALID_ARGUMENT > FLAREPP_OK,
+              "the worse word is the larger");
 
 // The word of the current device once the work on `st` is done; FLAREPP_OK again afterwards.
 cudaError_t take_library_status(int32_t* out, cudaStream_t st) {

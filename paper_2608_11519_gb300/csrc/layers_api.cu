@@ -17,4 +17,3 @@ extern "C" flarepp_status flarepp_layers_device_status(void* stream, int32_t* st
     }
     return FLAREPP_OK;
 }
-static_assert(FLAREPP_ERR_TIMEOUT > FLAREPP_ERR_INVALID_ARGUMENT, "the larger word counts");
