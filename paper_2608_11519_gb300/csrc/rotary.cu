@@ -403,13 +403,15 @@ flarepp_status check_side(const HeadDims& d, const flarepp_heads* x, const flare
     return FLAREPP_OK;
 }
 
-bool same(const flarepp_heads& x, const flarepp_heads& y) {
-    return x.data == y.data && x.stride_b == y.stride_b && x.stride_h == y.stride_h &&
-           x.stride_n == y.stride_n;
+// Strides of dimensions of size 1 do not matter.
+bool same(const flarepp_heads& x, const flarepp_heads& y, const HeadDims& d) {
+    return x.data == y.data && (d.B <= 1 || x.stride_b == y.stride_b) && (d.H <= 1 || x.stride_h == y.stride_h) &&
+           (d.N <= 1 || x.stride_n == y.stride_n);
 }
 
-bool vectors_ok(const flarepp_heads& t, int64_t per) {
-    return aligned16(t.data) && t.stride_b % per == 0 && t.stride_h % per == 0 && t.stride_n % per == 0;
+bool vectors_ok(const flarepp_heads& t, const HeadDims& d, int64_t per) {
+    return aligned16(t.data) && (d.B <= 1 || t.stride_b % per == 0) && (d.H <= 1 || t.stride_h % per == 0) &&
+           (d.N <= 1 || t.stride_n % per == 0);
 }
 
 flarepp_status rotary(const flarepp_rotary_shape* s, const void* positions, const float* freqs,
@@ -454,7 +456,7 @@ flarepp_status rotary(const flarepp_rotary_shape* s, const void* positions, cons
         for (int j = 0; j < 2; ++j) {
             if (overlaps(o.p, o.bytes, about[j].p, about[j].bytes)) return FLAREPP_ERR_INVALID_ARGUMENT;
             if (d[j].H == 0) continue;
-            if (!(i == j && same(*in[i], *out[i])) && !apart(*out[i], d[i], *in[j], d[j]))
+            if (!(i == j && same(*in[i], *out[i], d[i])) && !apart(*out[i], d[i], *in[j], d[j]))
                 return FLAREPP_ERR_INVALID_ARGUMENT;
             if (j < i && !apart(*out[i], d[i], *out[j], d[j])) return FLAREPP_ERR_INVALID_ARGUMENT;
         }
@@ -469,8 +471,8 @@ flarepp_status rotary(const flarepp_rotary_shape* s, const void* positions, cons
     bool whole = s->D % per == 0, in_place = true;
     for (int i = 0; i < 2; ++i) {
         if (d[i].H == 0) continue;
-        whole = whole && vectors_ok(*in[i], per) && vectors_ok(*out[i], per);
-        in_place = in_place && same(*in[i], *out[i]);
+        whole = whole && vectors_ok(*in[i], d[i], per) && vectors_ok(*out[i], d[i], per);
+        in_place = in_place && same(*in[i], *out[i], d[i]);
         a.side[i] = {in[i]->data,      out[i]->data,      in[i]->stride_b,  in[i]->stride_h,
                      in[i]->stride_n,  out[i]->stride_b,  out[i]->stride_h, out[i]->stride_n};
     }

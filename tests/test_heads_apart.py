@@ -72,6 +72,23 @@ def test_unlike_heads(lib):  # noqa: F811
     assert in_place(lib, s, (0, block), (Hq * N * D - D, block)) == INVALID
 
 
+@pytest.mark.parametrize("B,H,N", [(1, 4, 10), (2, 1, 10), (2, 4, 1), (1, 1, 1)])
+def test_an_output_that_is_its_input(lib, B, H, N):  # noqa: F811
+    """The same places, whatever the strides of sizes of 1 say."""
+    D = 64
+    s = rotary_shape(B=B, Hq=H, Hk=0, N=N, D=D, sections=(0,), pos=0)
+    st = [H * N * D, N * D, D]
+    other = [x if n > 1 else x + 72 for x, n in zip(st, (B, H, N))]
+    call = lambda a, b: lib.flarepp_rotary(ctypes.byref(s), None, None, ctypes.byref(flarepp.Heads(at(1), *a)), None,
+                                           ctypes.byref(flarepp.Heads(at(1), *b)), None, None)
+    assert call(st, st) == call(st, other) == call(other, st) == flarepp.OK
+    for i, n in enumerate((B, H, N)):
+        if n > 1:
+            wrong = list(st)
+            wrong[i] += 2 * H * N * D
+            assert call(st, wrong) == INVALID
+
+
 def places(first, strides, B, H, N, D):
     return [first + b * strides[0] + h * strides[1] + n * strides[2] + d
             for b in range(B) for h in range(H) for n in range(N) for d in range(D)]
