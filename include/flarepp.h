@@ -690,7 +690,8 @@ typedef struct {
  *     without rows that count: 0 and 1 / sqrt(eps)).
  *   workspace: at least flarepp_group_norm_workspace_bytes(shape) bytes, 256-byte aligned.
  *   Outputs and workspace must not overlap each other or an input.
- * Statistics are float32 sums of squares about the mean, in a fixed order.
+ * Statistics are float32 sums of squares about the mean, in a fixed order; what follows from them is computed in float32
+ * (bf16 tensors' activations by approximations good to bf16).
  */
 FLAREPP_API size_t flarepp_group_norm_workspace_bytes(const flarepp_norm_shape* shape);
 FLAREPP_API flarepp_status flarepp_group_norm_fwd(const flarepp_norm_shape* shape, const void* X,

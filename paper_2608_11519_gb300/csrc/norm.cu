@@ -5,7 +5,7 @@
 //   dx = rstd (g - avg(g) - xhat avg(g xhat)),  dgamma = sum dz xhat,  dbeta = sum dz.
 //
 // Bound by bytes: x (and dy) are needed twice, for the sums and for what follows from them. Samples of up to
-// kFewRows rows stay in registers in between (few_*). Larger ones are read twice, by a kernel that leaves
+// kTeamRows rows stay in registers in between (few_*). Larger ones are read twice, by a kernel that leaves
 // the sums of chunks of rows and one that joins them and goes over the rows again (from the last chunk to
 // the first, so that it begins with what the L2 still holds); a batch whose tensors pass the L2 goes
 // through in groups of samples that fit.
@@ -35,7 +35,7 @@ template <typename E, int W>
 constexpr int sum_rows() { return sizeof(E) * W >= 8 ? 8 : 16; }
 template <typename E, int W>
 constexpr int back_rows() { return sizeof(E) * W >= 8 ? 4 : 8; }
-constexpr int kFewRows = 4;
+constexpr int kTeamRows = 4;
 constexpr int64_t kWsAlign = 256;
 
 // One call, and how it is cut.
@@ -80,11 +80,13 @@ __device__ __forceinline__ float param(const void* t, int f32, int c, float none
 }
 
 // ---- the activation and its slope: 16-bit results from the linear layer's approximations in pairs,
-// 32-bit ones from the functions themselves. The choice is outside the loops over a vector, whose values
-// then go through the exponentials together: inside them it took the backward of 65,536 rows of 256
-// 99 us instead of 56.
-// 1 / (1 + exp(-z)): the exponential's relative error is |z| 2^-24 and two units more, of which the result's
-// is a quarter at most.
+// 32-bit ones from the functions themselves, but for SiLU's exponential and reciprocal: with expf and a
+// division the errors of Y, dX, dgamma and dbeta are the same but for a few per cent (8e-8 to 1.6e-7 of their
+// norms, which are the sums'), and the backward of 6 x 99,991 x 250 takes 695 us instead of 590. The choice is
+// outside the loops over a vector, whose values then go through the exponentials together: inside them it took
+// the backward of 65,536 rows of 256 99 us instead of 56.
+// 1 / (1 + exp(-z)): the exponential's relative error is |z| 2^-24 and two units more, and the result's the
+// same for z far below 0, where it goes to 0, and less elsewhere.
 __device__ __forceinline__ float logistic(float z) {
     return rcp_approx(1.f + ex2_approx(-1.44269504f * z));
 }
@@ -198,7 +200,7 @@ __device__ __forceinline__ Place place_of(const Norm& p, int64_t block) {
 }
 
 // ------------------------------------------------------------------ sums of the forward
-// Bound by reading X once: 8 rows of 16 bytes in flight a thread.
+// Bound by reading X once: 8 rows of 8 or 16 bytes (or 16 of less) in flight a thread.
 template <typename E, int W>
 __global__ void __launch_bounds__(kThreads, 4) stats_kernel(const Norm p) {
     __shared__ float sm[2][kThreads * W];
@@ -928,7 +930,7 @@ Plan plan_of(const flarepp_norm_shape& s, bool backward) {
     const int64_t vectors = s.C / p.W, w = s.C / s.G;
     // Few rows, whose vectors do not cut groups: a warp or a part of one takes a group, if it has room
     // (1,024 channels of one row; a layer norm of more goes the long way).
-    if (s.N <= kFewRows && w % p.W == 0) {
+    if (s.N <= kTeamRows && w % p.W == 0) {
         const int64_t vectors_of = w / p.W;
         p.lanes = 1;
         while (p.lanes < 32 && p.lanes < vectors_of) p.lanes *= 2;
@@ -965,7 +967,7 @@ Plan plan_of(const flarepp_norm_shape& s, bool backward) {
         if (p.group < 1) p.group = 1;
         if (p.group > s.B) p.group = s.B;
         p.group = cdiv(s.B, cdiv(s.B, p.group));
-        // Three blocks an SM, with 32 rows a thread where there are so many: a block's own sums take as long
+        // Three blocks an SM, with 8 rows a thread at least where there are so many: a block's own sums take as long
         // as some ten rows of its threads.
         const int64_t wanted = cdiv(kNumSMs * 3, p.group * p.tiles);
         const int64_t least = (int64_t)p.ty * 8;
@@ -989,7 +991,7 @@ Plan plan_of(const flarepp_norm_shape& s, bool backward) {
 
 // The kernel for few rows: of one row and up to 8 vectors a lane, or of up to four rows.
 #define FLAREPP_FEW(kernel)                                                                   \
-    (a.N > 1         ? launch(kernel<E, W, kFewRows, 1>, p.blocks, kThreads, st, a, p.lanes)  \
+    (a.N > 1         ? launch(kernel<E, W, kTeamRows, 1>, p.blocks, kThreads, st, a, p.lanes) \
      : p.each == 1   ? launch(kernel<E, W, 1, 1>, p.blocks, kThreads, st, a, p.lanes)         \
      : p.each == 2   ? launch(kernel<E, W, 1, W == 4 ? 2 : 1>, p.blocks, kThreads, st, a, p.lanes) \
      : p.each == 4   ? launch(kernel<E, W, 1, W == 4 ? 4 : 1>, p.blocks, kThreads, st, a, p.lanes) \

@@ -8,12 +8,12 @@
 // an SM's share of HBM. So one block walks a sequence of one head, with the state staying in TMEM, and
 // nothing is read twice; where heads and sequences do not fill the SMs evenly, sequences are cut, and a
 // first walk (only A and V, only S, only in front of the cuts) and a join over the blocks find the states
-// there. What bounds it is shared memory and the state's way round: a chunk's products, whose operands are read from
-// it, its tiles, decayed values and state move 580 KB through it at 128 channels, 4,500 of the 6,100
-// cycles that a chunk takes (keys, values of 64, 64: 3,800; 128, 64: 5,000; 64, 128: 6,000), and a chunk's state is
-// scaled, multiplied and added to before the next one's. 4 x 32 heads of 8,192 tokens and 128 channels take
-// 196 us (3.4 TB/s of what has to move), the gradients of 8 heads of 131,072 tokens, 64 and 128 channels, 658
-// (HBM at 55 to 70 % in each of the walks).
+// there. What bounds it is shared memory and the state's way round. By count a chunk's products, whose operands
+// are read from it, its tiles, decayed values and state move 580 KB through it at 128 channels, 4,500 of the
+// 6,300 cycles that a chunk takes (no counter has the tensor pipe's reads; threads' accesses alone are 23 % of
+// it); of keys and values of 64 channels it takes 3,800, of 128 and 64 5,000, of 64 and 128 6,000. And a
+// chunk's state is scaled, multiplied and added to before the next one's. 4 x 32 heads of 8,192 tokens and 128 channels take 203 us (3.3 TB/s of what has to move), the
+// gradients of 8 heads of 131,072 tokens, 64 and 128 channels, 664 (HBM at 54 to 68 % in each of the walks).
 //
 // W o (X A^T) is rounded to bf16 as an operand, w o V and S are two bf16 each (Cfg says why and where not); sums,
 // states and what r multiplies are float32.
@@ -338,10 +338,10 @@ __device__ __noinline__ void clear_rows(uint8_t* tile, int thread, int but) {
 // infinity or NaN is NaN. So where a warp's outputs from the chunk are NaN (TMEM tells with the load), its tokens' are
 // made again one product after another, of the tokens that count alone: what is no number then reaches what it
 // reaches in the recurrence. The weights, rounded as they were, take the place of the outputs in TMEM, two in a word.
-// Such a chunk takes 0.3 ms at 64 channels, 0.75 at 128, a chunk whose outputs are numbers no more than before but for
-// the code's place in registers: 3 % of the packed training, 4 of the prefill, none of the long backward. (With eight keys
-// in flight it took half, but all others 1 to 6 % more; a look at the values before their product took 4 to 15 % of every
-// walk, whichever warps did it.)
+// Such a chunk takes 0.3 ms at 64 channels, 0.75 at 128; others no more than before but for the code's place in
+// registers: 3 % of the packed training, 4 of the prefill, none of the long backward. (With eight keys in flight it
+// took half, but all others 1 to 6 % more; a look at the values before their product took 4 to 15 % of every walk,
+// whichever warps did it.)
 __device__ __forceinline__ const __nv_bfloat16* source(const Source& s, int b, int own_batch, int h, int group,
                                                        int64_t token) {
     return s.t + (int64_t)b * own_batch * s.b + (int64_t)(group ? h / group : 0) * s.h + token * s.n;
